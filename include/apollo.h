@@ -337,6 +337,119 @@ APOLLO_API int apollo_mini_step_static(void* d_W, const void* d_G, int64_t rows,
                                        const apollo_config* cfg, uint32_t matrix, int64_t t,
                                        float lr, float wd, void* cuda_stream);
 
+/*
+ * Orthogonalised updates: the other rule with little state for the same list of 2-D weights (the paper has no
+ * counterpart).  For each weight W with gradient G and momentum M, viewed as m x n with m <= n (transposed when
+ * rows > cols):
+ *   M <- mu M + (1 - mu) G,   U = nesterov ? (1 - mu) G + mu M : M,
+ *   X <- U / (|U|_F + eps),   `ns_steps` times:  A = X X^T,  X <- a X + (b A + c A^2) X      (Newton-Schulz),
+ *   W <- W - lr (s X + wd W),
+ * which with the coefficients (a, b, c) = (3.4445, -4.7750, 2.0315) takes every singular value of U that is not
+ * negligible to about 1 in five steps (it ends in 0.7 ... 1.2, not at 1).  s is 1, sqrt(max(1, rows / cols)) or
+ * 0.2 sqrt(max(rows, cols)).
+ *
+ * Precision.  The products run on the tensor cores with fp32 accumulators.  With APOLLO_DT_BF16 the iterates are
+ * held in 16-bit floats with 11 significant bits, scaled by powers of two (bfloat16's 8 bits would leave an error
+ * of 1e-2 in X; measured here: 1e-3, below the rounding of a bfloat16 result); with APOLLO_DT_F32 as unevaluated
+ * sums of two such numbers, three products for one (error below 1e-5).  M is fp32 in both.
+ */
+#define APOLLO_MUON_SCALE_NONE 0
+#define APOLLO_MUON_SCALE_SHAPE 1 /* sqrt(max(1, rows / cols)) */
+#define APOLLO_MUON_SCALE_RMS 2   /* 0.2 sqrt(max(rows, cols)): entries of the size of an AdamW update */
+#define APOLLO_MUON_MAX_STEPS 32
+
+typedef struct apollo_muon_ctx apollo_muon_ctx; /* opaque HOST object */
+
+typedef struct {
+    int32_t dtype;        /* APOLLO_DT_* of W and G, and of both operands of apollo_muon_orthogonalize */
+    int32_t ns_steps;     /* 1 .. APOLLO_MUON_MAX_STEPS (5) */
+    float coef[3];        /* a, b, c; refused when some start in [0, 1] leaves |x| <= 8 under x <- a x + b x^3 + c x^5 */
+    float momentum;       /* mu, 0 <= mu < 1 (0.95) */
+    int32_t nesterov;     /* 0 or 1 */
+    int32_t scale;        /* APOLLO_MUON_SCALE_* */
+    float eps;            /* > 0 (1e-7) */
+    int32_t workspace_mb; /* the matrices are worked on in groups whose iterates fit this many MB (a single matrix may
+                             exceed it); 0 = default (2048) */
+} apollo_muon_config;
+
+/*
+ * As apollo_workspace_bytes / apollo_create: a caller-owned DEVICE workspace (256-byte aligned), nothing launched, no
+ * stream touched.  A side may be at most 2^20 (APOLLO_ERR_SHAPE).  The workspace holds iterates of one group at a time
+ * and nothing from one step to the next; the momenta are the caller's.
+ */
+APOLLO_API int apollo_muon_workspace_bytes(const apollo_shape* shapes, int32_t n_matrices, const apollo_muon_config* cfg,
+                                           size_t* out_bytes);
+APOLLO_API int apollo_muon_create(apollo_muon_ctx** out_ctx, const apollo_shape* shapes, int32_t n_matrices,
+                                  const apollo_muon_config* cfg, void* d_workspace, size_t workspace_bytes);
+APOLLO_API int apollo_muon_destroy(apollo_muon_ctx* ctx);
+
+/*
+ * One step over the list.  d_W, d_G, d_M: HOST arrays of DEVICE pointers (16-byte aligned, row-major rows x cols,
+ * contiguous); W and M (fp32, zeroed by the caller before the first step) are updated in place.  Asynchronous on
+ * `cuda_stream`; two calls of one context must not overlap on the GPU (they share the workspace).
+ */
+APOLLO_API int apollo_muon_step(apollo_muon_ctx* ctx, void* const* d_W, const void* const* d_G, float* const* d_M,
+                                float lr, float wd, void* cuda_stream);
+
+/* O = the X above for U = d_U[i], for every matrix of the list: no momentum, no weights.  O may be U. */
+APOLLO_API int apollo_muon_orthogonalize(apollo_muon_ctx* ctx, const void* const* d_U, void* const* d_O, void* cuda_stream);
+
+/* As apollo_status: waits for the stream, returns and clears the device status word.  While the word is set, W and O
+ * are not written (M has been updated). */
+APOLLO_API int apollo_muon_status(apollo_muon_ctx* ctx, void* cuda_stream);
+
+/* Kernel launches issued by the last step or orthogonalisation (HOST counter). */
+APOLLO_API int apollo_muon_last_launches(const apollo_muon_ctx* ctx, int32_t* out);
+
+/*
+ * Embedding lookup with scaling, and its gradient (stateless, asynchronous on `cuda_stream`).
+ *   lookup:    out[t, :] = scale table[index[t], :]                                       t < n_tokens
+ *   gradient:  dtable[v, :] = scale sum over {t : index[t] = v} dout[t, :]                (+ dtable[v, :], accumulate = 1)
+ * An index outside [0, rows) (padding, any negative number) gives a zero row and no gradient.  table, dtable: DEVICE,
+ * rows x dim, contiguous; out, dout: DEVICE, n_tokens rows of `dim` elements, out_stride >= dim elements apart; all of
+ * `dtype`; index: DEVICE, int32 or int64.  Pointers need the alignment of their elements; rows that are whole 16-byte
+ * vectors are faster.  With accumulate = 0 every row of dtable is written (zeros where no token points); with 1 only
+ * the rows that occur are read and written.  Sums are fp32 in the order of the positions (in fixed pieces where a
+ * token is frequent), rounded once: equal bits in every run, no float atomics.  The gradient needs a DEVICE workspace
+ * (16-byte aligned) of apollo_embedding_grad_workspace_bytes(); it keeps nothing there between calls.
+ */
+#define APOLLO_INDEX_I32 0
+#define APOLLO_INDEX_I64 1
+APOLLO_API int apollo_embedding(const void* d_table, int64_t rows, int64_t dim, int32_t dtype, const void* d_index,
+                                int32_t index_type, int64_t n_tokens, float scale, void* d_out, int64_t out_stride,
+                                void* cuda_stream);
+APOLLO_API int apollo_embedding_grad_workspace_bytes(int64_t n_tokens, int64_t rows, int64_t dim, size_t* out_bytes);
+APOLLO_API int apollo_embedding_grad(const void* d_out, int64_t out_stride, const void* d_index, int32_t index_type,
+                                     int64_t n_tokens, int64_t rows, int64_t dim, int32_t dtype, float scale,
+                                     int32_t accumulate, void* d_table_grad, void* d_workspace, size_t workspace_bytes,
+                                     void* cuda_stream);
+
+/*
+ * Log probabilities of given tokens with entropy and the best alternatives, and their gradient (stateless,
+ * asynchronous on `cuda_stream`).  Per row of logits, with z = scale * logit (scale = 1 / temperature, > 0):
+ *   lse = log sum_j exp z_j,   logprob = z_t - lse,   entropy = -sum_j p_j log p_j,   p_j = exp(z_j - lse),
+ *   the `top` largest z in falling order (equal ones by rising index) as z - lse with their indices;
+ *   dlogit_j = scale (grad_logprob (1[j = t] - p_j) - grad_entropy p_j (z_j - lse + entropy)).
+ * Logits of -inf are masked words: p = 0 and no gradient.  A row with every word masked has lse = logprob = -inf,
+ * entropy = 0, alternatives of -inf by rising index, and no gradient.  A target outside [0, vocab) is ignored:
+ * logprob = 0 and its grad_logprob counts as 0.  A NaN or +inf logit makes lse, logprob and entropy of its row NaN.
+ * logits: DEVICE, n_rows rows of `vocab` elements of `dtype`, row_stride >= vocab elements apart; targets: DEVICE,
+ * int32 or int64; logprob, entropy, lse: DEVICE, n_rows floats; top_logprob, top_index: DEVICE, n_rows x top (may be
+ * null with top = 0).  Pointers need the alignment of their elements.  The gradient takes lse and entropy of the
+ * forward pass; grad_entropy (and then entropy) may be null: no entropy term.  grad_logits may be the logits
+ * themselves (same stride).  Statistics are fp32.
+ */
+#define APOLLO_MAX_TOP 32
+APOLLO_API int apollo_token_logprobs(const void* d_logits, int64_t row_stride, int64_t n_rows, int64_t vocab, int32_t dtype,
+                                     const void* d_targets, int32_t index_type, float scale, int32_t top, float* d_logprob,
+                                     float* d_entropy, float* d_lse, float* d_top_logprob, int32_t* d_top_index,
+                                     void* cuda_stream);
+APOLLO_API int apollo_token_logprobs_grad(const void* d_logits, int64_t row_stride, int64_t n_rows, int64_t vocab,
+                                          int32_t dtype, const void* d_targets, int32_t index_type, float scale,
+                                          const float* d_lse, const float* d_entropy, const float* d_grad_logprob,
+                                          const float* d_grad_entropy, void* d_grad_logits, int64_t grad_stride,
+                                          void* cuda_stream);
+
 /* Self-test of the error path (the paper has no counterpart).  Every wait inside the tensor-core
  * kernel is bounded: after 2^20 polls it gives up, sets the context's device status word and the
  * kernel winds down instead of hanging.  This call launches, on the stream, a one-block kernel whose

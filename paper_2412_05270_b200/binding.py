@@ -6,8 +6,10 @@ import of this module's symbols raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 from pathlib import Path
+from typing import NamedTuple
 
 import torch
 
@@ -29,6 +31,10 @@ FLAG_KEEP_P = 4
 TC_KERNEL_PAIR, TC_KERNEL_RING = 0, 1
 P_SCRATCH, P_SHARED = 0, 1
 PATH_STREAM, PATH_SIMT, PATH_TENSOR = 0, 1, 2
+MUON_SCALE_NONE, MUON_SCALE_SHAPE, MUON_SCALE_RMS = 0, 1, 2
+MUON_MAX_STEPS = 32
+INDEX_I32, INDEX_I64 = 0, 1
+MAX_TOP = 32
 
 EXPORTS = [
     "apollo_workspace_bytes", "apollo_create", "apollo_step", "apollo_destroy", "apollo_step_count",
@@ -37,6 +43,9 @@ EXPORTS = [
     "apollo_set_timing", "apollo_get_timing", "apollo_mini_step_static", "apollo_cuda_error_string", "apollo_adamw_step",
     "apollo_state_bytes", "apollo_state_export", "apollo_state_import", "apollo_step_range", "apollo_set_projection",
     "apollo_selftest_bounded_wait", "apollo_workspace_bytes_tuned", "apollo_create_tuned",
+    "apollo_muon_workspace_bytes", "apollo_muon_create", "apollo_muon_destroy", "apollo_muon_step", "apollo_muon_orthogonalize",
+    "apollo_muon_status", "apollo_muon_last_launches", "apollo_embedding", "apollo_embedding_grad_workspace_bytes",
+    "apollo_embedding_grad", "apollo_token_logprobs", "apollo_token_logprobs_grad",
 ]
 
 
@@ -59,6 +68,13 @@ class Config(ctypes.Structure):
         ("beta1", ctypes.c_float), ("beta2", ctypes.c_float), ("eps", ctypes.c_float),
         ("bias_correction", ctypes.c_int32), ("flags", ctypes.c_uint32),
     ]
+
+
+class MuonConfig(ctypes.Structure):
+    """apollo_muon_config."""
+    _fields_ = [("dtype", ctypes.c_int32), ("ns_steps", ctypes.c_int32), ("coef", ctypes.c_float * 3),
+                ("momentum", ctypes.c_float), ("nesterov", ctypes.c_int32), ("scale", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("workspace_mb", ctypes.c_int32)]
 
 
 class Tuning(ctypes.Structure):
@@ -139,6 +155,21 @@ def _load_from(path: Path):
     lib.apollo_state_bytes.argtypes = [vp, ctypes.POINTER(ctypes.c_size_t)]
     lib.apollo_state_export.argtypes = [vp, vp, vp]
     lib.apollo_state_import.argtypes = [vp, vp, ctypes.c_int64, vp]
+    lib.apollo_muon_workspace_bytes.argtypes = [ctypes.POINTER(Shape), i32, ctypes.POINTER(MuonConfig),
+                                                ctypes.POINTER(ctypes.c_size_t)]
+    lib.apollo_muon_create.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(Shape), i32, ctypes.POINTER(MuonConfig), vp,
+                                       ctypes.c_size_t]
+    lib.apollo_muon_destroy.argtypes = [vp]
+    lib.apollo_muon_step.argtypes = [vp, ctypes.POINTER(vp), ctypes.POINTER(vp), ctypes.POINTER(vp), f32, f32, vp]
+    lib.apollo_muon_orthogonalize.argtypes = [vp, ctypes.POINTER(vp), ctypes.POINTER(vp), vp]
+    lib.apollo_muon_status.argtypes = [vp, vp]
+    lib.apollo_muon_last_launches.argtypes = [vp, ctypes.POINTER(i32)]
+    i64 = ctypes.c_int64
+    lib.apollo_embedding.argtypes = [vp, i64, i64, i32, vp, i32, i64, f32, vp, i64, vp]
+    lib.apollo_embedding_grad_workspace_bytes.argtypes = [i64, i64, i64, ctypes.POINTER(ctypes.c_size_t)]
+    lib.apollo_embedding_grad.argtypes = [vp, i64, vp, i32, i64, i64, i64, i32, f32, i32, vp, vp, ctypes.c_size_t, vp]
+    lib.apollo_token_logprobs.argtypes = [vp, i64, i64, i64, i32, vp, i32, f32, i32, vp, vp, vp, vp, vp, vp]
+    lib.apollo_token_logprobs_grad.argtypes = [vp, i64, i64, i64, i32, vp, i32, f32, vp, vp, vp, vp, vp, i64, vp]
     lib.apollo_cuda_error_string.argtypes = []
     lib.apollo_cuda_error_string.restype = ctypes.c_char_p
     for name in EXPORTS:
@@ -240,6 +271,221 @@ def adamw_step(params, grads, ms, vs, t, lr, beta1=0.9, beta2=0.999, eps=1e-8, w
     _check(load().apollo_adamw_step(arr(params), arr(grads), arr(ms), arr(vs), numel, n, dtype, lr, beta1, beta2, eps,
                                     wd, t, int(bool(bias_correction)), arr(deltas) if deltas is not None else None,
                                     _stream_ptr(stream)), "apollo_adamw_step")
+
+
+def _dtype_of(x: torch.Tensor, what: str) -> int:
+    if x.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"{what} must be bfloat16 or float32, got {x.dtype}")
+    return DT_BF16 if x.dtype == torch.bfloat16 else DT_F32
+
+
+def _index_of(x: torch.Tensor, what: str) -> int:
+    if x.dtype not in (torch.int32, torch.int64) or not x.is_cuda or not x.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous CUDA tensor of int32 or int64")
+    return INDEX_I64 if x.dtype == torch.int64 else INDEX_I32
+
+
+def _rows_of(x: torch.Tensor, what: str) -> int:
+    """The row stride of a 2-D CUDA tensor whose rows are contiguous."""
+    if not x.is_cuda or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError(f"{what} must be a 2-D CUDA tensor with contiguous rows")
+    if x.shape[0] <= 1:
+        return max(x.shape[1], 1)
+    if x.stride(0) < x.shape[1]:
+        raise ValueError(f"{what} must not have overlapping rows")
+    return x.stride(0)
+
+
+def _on(stream, device):
+    """What the call allocates belongs to the stream that it runs on."""
+    return torch.cuda.device(device) if stream is None else torch.cuda.stream(stream)
+
+
+def embedding(table, index, scale: float = 1.0, out=None, stream=None) -> torch.Tensor:
+    """apollo_embedding: scale * table[index], a zero row where the index is outside the table.
+
+    table: (rows, dim), contiguous; index: any shape, int32 or int64; out: (index.numel(), dim) rows, made if None
+    (then of the index's shape with dim appended)."""
+    dtype, itype = _dtype_of(table, "table"), _index_of(index, "index")
+    if table.dim() != 2 or not table.is_contiguous() or not table.is_cuda:
+        raise ValueError("table must be a 2-D contiguous CUDA tensor")
+    rows, dim = table.shape
+    n = index.numel()
+    with _on(stream, table.device):
+        res = flat = out
+        if out is None:
+            res = torch.empty((*index.shape, dim), dtype=table.dtype, device=table.device)
+            flat = res.view(n, dim)
+        elif out.dtype != table.dtype or tuple(out.shape) != (n, dim):
+            raise ValueError("out must have the table's dtype and one row per index")
+        _check(load().apollo_embedding(table.data_ptr(), rows, dim, dtype, index.data_ptr(), itype, n, scale,
+                                       flat.data_ptr(), _rows_of(flat, "out"), _stream_ptr(stream)), "apollo_embedding")
+    return res
+
+
+def embedding_grad_workspace_bytes(n_tokens: int, rows: int, dim: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().apollo_embedding_grad_workspace_bytes(n_tokens, rows, dim, ctypes.byref(out)),
+           "apollo_embedding_grad_workspace_bytes")
+    return out.value
+
+
+def embedding_grad(d_out, index, rows: int, scale: float = 1.0, out=None, accumulate: bool = False, workspace=None,
+                   stream=None) -> torch.Tensor:
+    """apollo_embedding_grad: the gradient of `embedding` for its table, (rows, dim) in d_out's dtype.
+
+    d_out: (index.numel(), dim) rows; out: made if None, else overwritten (accumulate: added to); workspace: a uint8
+    CUDA tensor of embedding_grad_workspace_bytes(), made if None."""
+    dtype, itype = _dtype_of(d_out, "d_out"), _index_of(index, "index")
+    stride = _rows_of(d_out, "d_out")
+    n, dim = d_out.shape
+    if n != index.numel():
+        raise ValueError("d_out must have one row per index")
+    with _on(stream, d_out.device):
+        if out is None:
+            if accumulate:
+                raise ValueError("accumulate needs the gradient to add to")
+            out = torch.empty((rows, dim), dtype=d_out.dtype, device=d_out.device)
+        elif out.dtype != d_out.dtype or tuple(out.shape) != (rows, dim) or not out.is_contiguous() or not out.is_cuda:
+            raise ValueError("out must be a contiguous CUDA tensor (rows, dim) of d_out's dtype")
+        if workspace is None:
+            workspace = torch.empty(embedding_grad_workspace_bytes(n, rows, dim), dtype=torch.uint8, device=d_out.device)
+        _check(load().apollo_embedding_grad(d_out.data_ptr(), stride, index.data_ptr(), itype, n, rows, dim, dtype, scale,
+                                            int(bool(accumulate)), out.data_ptr(), workspace.data_ptr(),
+                                            workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
+               "apollo_embedding_grad")
+    return out
+
+
+class TokenLogprobs(NamedTuple):
+    logprob: torch.Tensor
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    top_logprob: torch.Tensor | None
+    top_index: torch.Tensor | None
+
+
+def token_logprobs(logits, targets, scale: float = 1.0, top: int = 0, stream=None) -> TokenLogprobs:
+    """apollo_token_logprobs over the rows of `logits` (n, vocab); targets: n of int32 or int64, outside [0, vocab) =
+    ignored; top: how many of the best alternatives (<= MAX_TOP) come back as (n, top) log probabilities and indices."""
+    dtype, itype = _dtype_of(logits, "logits"), _index_of(targets, "targets")
+    stride = _rows_of(logits, "logits")
+    n, vocab = logits.shape
+    if targets.numel() != n:
+        raise ValueError("targets must have one entry per row of logits")
+    with _on(stream, logits.device):
+        stats = torch.empty((3, n), dtype=torch.float32, device=logits.device)
+        best = best_at = None
+        if top > 0:
+            best = torch.empty((n, top), dtype=torch.float32, device=logits.device)
+            best_at = torch.empty((n, top), dtype=torch.int32, device=logits.device)
+        base = stats.data_ptr()
+        _check(load().apollo_token_logprobs(logits.data_ptr(), stride, n, vocab, dtype, targets.data_ptr(), itype, scale, top,
+                                            base, base + 4 * n, base + 8 * n, None if best is None else best.data_ptr(),
+                                            None if best_at is None else best_at.data_ptr(), _stream_ptr(stream)),
+               "apollo_token_logprobs")
+    logprob, entropy, lse = stats.unbind(0)
+    return TokenLogprobs(logprob, entropy, lse, best, best_at)
+
+
+def token_logprobs_grad(logits, targets, lse, entropy, d_logprob, d_entropy=None, scale: float = 1.0, out=None,
+                        stream=None) -> torch.Tensor:
+    """apollo_token_logprobs_grad: the gradient of the logits for upstream gradients of logprob and (or None) entropy,
+    with lse and entropy as `token_logprobs` returned them; out may be the logits themselves."""
+    dtype, itype = _dtype_of(logits, "logits"), _index_of(targets, "targets")
+    stride = _rows_of(logits, "logits")
+    n, vocab = logits.shape
+    for x, what in ((lse, "lse"), (entropy, "entropy"), (d_logprob, "d_logprob"), (d_entropy, "d_entropy")):
+        if x is not None and (x.dtype != torch.float32 or x.numel() != n or not x.is_contiguous() or not x.is_cuda):
+            raise ValueError(f"{what} must be a contiguous float32 CUDA tensor with one entry per row")
+    if targets.numel() != n:
+        raise ValueError("targets must have one entry per row of logits")
+    with _on(stream, logits.device):
+        if out is None:
+            out = torch.empty((n, vocab), dtype=logits.dtype, device=logits.device)
+        elif out.dtype != logits.dtype or tuple(out.shape) != (n, vocab):
+            raise ValueError("out must have the logits' dtype and shape")
+        _check(load().apollo_token_logprobs_grad(
+            logits.data_ptr(), stride, n, vocab, dtype, targets.data_ptr(), itype, scale, lse.data_ptr(),
+            None if entropy is None else entropy.data_ptr(), d_logprob.data_ptr(),
+            None if d_entropy is None else d_entropy.data_ptr(), out.data_ptr(), _rows_of(out, "out"), _stream_ptr(stream)),
+            "apollo_token_logprobs_grad")
+    return out
+
+
+def make_muon_config(dtype=DT_BF16, steps=5, coef=(3.4445, -4.7750, 2.0315), momentum=0.95, nesterov=True,
+                     scale=MUON_SCALE_SHAPE, eps=1e-7, workspace_mb=0) -> MuonConfig:
+    return MuonConfig(int(dtype), int(steps), (ctypes.c_float * 3)(*coef), float(momentum), int(bool(nesterov)),
+                      int(scale), float(eps), int(workspace_mb))
+
+
+def muon_workspace_bytes(shapes, cfg: MuonConfig) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().apollo_muon_workspace_bytes(_shape_array(shapes), len(shapes), ctypes.byref(cfg), ctypes.byref(out)),
+           "apollo_muon_workspace_bytes")
+    return out.value
+
+
+class Muon:
+    """apollo_muon_create / apollo_muon_step: orthogonalised updates of a list of 2-D CUDA tensors (one dtype,
+    contiguous); the fp32 momenta are the caller's."""
+
+    def __init__(self, shapes, cfg: MuonConfig, device="cuda"):
+        self.lib = load()
+        self.shapes = [(int(r), int(c)) for r, c in shapes]
+        self.cfg = cfg
+        self.device = torch.device(device)
+        nbytes = muon_workspace_bytes(self.shapes, cfg)
+        self.workspace_bytes = nbytes
+        with torch.cuda.device(self.device):
+            self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+            base = (self.workspace.data_ptr() + 255) // 256 * 256
+            ctx = ctypes.c_void_p()
+            _check(self.lib.apollo_muon_create(ctypes.byref(ctx), _shape_array(self.shapes), len(self.shapes),
+                                               ctypes.byref(cfg), base, nbytes), "apollo_muon_create")
+        self.ctx = ctx
+        n = len(self.shapes)
+        self._arrays = [(ctypes.c_void_p * n)() for _ in range(3)]
+
+    def close(self):
+        if getattr(self, "ctx", None):
+            self.lib.apollo_muon_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        with contextlib.suppress(Exception):
+            self.close()
+
+    def _marshal(self, lists):
+        want = torch.bfloat16 if self.cfg.dtype == DT_BF16 else torch.float32
+        for k, (arr, xs) in enumerate(zip(self._arrays, lists)):
+            if len(xs) != len(self.shapes):
+                raise ValueError("parameter list length differs from the context's")
+            dt = torch.float32 if k == 2 else want
+            for i, (x, shp) in enumerate(zip(xs, self.shapes)):
+                if x.dtype != dt or x.shape != shp or not x.is_cuda or not x.is_contiguous():
+                    raise ValueError("tensors must be contiguous CUDA tensors of the context's dtype and shapes (momenta: float32)")
+                arr[i] = x.data_ptr()
+
+    def step(self, Ws, Gs, Ms, lr: float, wd: float = 0.0, stream=None):
+        """One update of the weights Ws and the momenta Ms (float32, zero before the first step) from the gradients Gs."""
+        self._marshal((Ws, Gs, Ms))
+        w, g, m = self._arrays
+        _check(self.lib.apollo_muon_step(self.ctx, w, g, m, lr, wd, _stream_ptr(stream)), "apollo_muon_step")
+
+    def orthogonalize(self, Us, Os, stream=None):
+        """Os <- the orthogonalised Us (Os may be Us)."""
+        self._marshal((Os, Us))
+        o, u, _ = self._arrays
+        _check(self.lib.apollo_muon_orthogonalize(self.ctx, u, o, _stream_ptr(stream)), "apollo_muon_orthogonalize")
+
+    def status(self, stream=None) -> int:
+        return self.lib.apollo_muon_status(self.ctx, _stream_ptr(stream))
+
+    def last_launches(self) -> int:
+        out = ctypes.c_int32(0)
+        _check(self.lib.apollo_muon_last_launches(self.ctx, ctypes.byref(out)), "apollo_muon_last_launches")
+        return out.value
 
 
 class Apollo:

@@ -1,0 +1,518 @@
+// Host side of the orthogonalised update: validation, workspace planning, the products of every phase, launches.
+//
+// The iteration X <- a X + (b A + c A^2) X, A = X X^T, is a sequence of products that depend on one another; the
+// matrices of a list do not.  So a list is worked on in groups, and a launch (a phase) does the p-th product of
+// every matrix of its group.  Two ways to take two steps, whichever has fewer tile k-blocks for the matrix:
+//   one by one   A = X X^T, B = b A + c A^2, X <- a X + B X, twice
+//   together     A, B as before; P = a I + B;  T = P A, A' = P T (= X' X'^T of the step in between, without X'),
+//                B' = b A' + c A'^2, Q = P' P, X <- Q X
+// The second replaces two long products (m x n) by three m x m ones: it pays when n > m.  (Three steps together would
+// save more and lose too much: an error of A' is multiplied by a^2 = 12 a step.)
+// A, B, T, A', B', Q are polynomials of one symmetric matrix: symmetric, so only half their tiles are computed.
+//
+// Rounding.  What is stored in 16 bits has 11 of them.  B is stored shifted, B + s I, with s such that its diagonal
+// lies near 0 where most singular values are near 1 (X <- (a - s) X + (B + s I) X); likewise Q - I.  The rounding of
+// the large diagonal entries was the largest error of all: measured on normal gradients (512 x 512 ... 1024 x 2736)
+// 1.4e-3 -> 1.0e-3 in X one by one, 2.2e-3 -> 1.0e-3 together.
+#include "../../include/apollo.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "apollo_internal.h"
+#include "muon.h"
+
+using namespace apollo;
+
+namespace {
+
+constexpr size_t ALIGN = 256;
+constexpr int MAX_SIDE = 1 << 20;
+constexpr double Q_SHIFT = 1.0;
+
+size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
+int round_up(int x, int to) { return (x + to - 1) / to * to; }
+
+struct Mat {
+    int rows, cols, m, n, tall, pitch_x, pitch_s, n_part;
+    bool together;
+    size_t x[2][2], s[3][2], part;       // workspace offsets: [buffer][high, low]
+    size_t maps;                         // offset of its tensor maps
+};
+
+struct Phase { int op_begin, n_ops, prefix_begin, tiles; };
+
+struct Group {
+    std::vector<int> mats;
+    std::vector<Phase> phases;
+};
+
+// The powers of two that stored values carry, and the constants of the iteration.
+struct Scales { double x, a, b, t, q, shift; };
+
+struct Plan {
+    std::vector<Mat> mats;
+    std::vector<Group> groups;
+    size_t off_status, off_table, table_bytes, off_maps, off_ops, off_prefix, total;
+    int n_ops, n_prefix, maps_per_mat, parts;
+    Scales sc;
+};
+
+double poly(const float* c, double x) { const double y = x * x; return x * (c[0] + y * (c[1] + y * c[2])); }
+
+// Bounds of everything stored, from the iteration on [0, 1] (the singular values of X start there).
+bool find_scales(const apollo_muon_config& cfg, Scales& sc)
+{
+    const double a = cfg.coef[0], b = cfg.coef[1], c = cfg.coef[2];
+    const int N = 8192;
+    double top = 1.0, now = 1.0;
+    for (int k = 0; k < cfg.ns_steps; ++k) {
+        double next = 0.0;
+        for (int i = 0; i <= N; ++i) next = std::max(next, std::fabs(poly(cfg.coef, now * i / N)));
+        now = next;
+        if (!(now <= 8.0)) return false;
+        top = std::max(top, now);
+    }
+    double b_min = 0.0, b_max = 0.0, t_max = 0.0, p_max = 0.0;
+    for (int i = 0; i <= N; ++i) {
+        const double y = top * top * i / N, v = y * (b + c * y), p = a + v;
+        b_min = std::min(b_min, v); b_max = std::max(b_max, v);
+        t_max = std::max(t_max, std::fabs(y * p));
+        p_max = std::max(p_max, std::fabs(p));
+    }
+    sc.shift = -(0.7 * b_min + 0.3 * b_max);
+    // the largest power of two that keeps a value of this size at or below 2^15 (16-bit floats end at 65504)
+    auto scale_for = [](double v) { return std::exp2(std::floor(15.0 - std::log2(std::max(v, 1.0)))); };
+    sc.x = scale_for(top);
+    sc.a = scale_for(top * top);
+    sc.b = scale_for(std::max(b_max - b_min, 1.0) + std::fabs(sc.shift));
+    sc.t = scale_for(t_max);
+    sc.q = scale_for(p_max * p_max + Q_SHIFT);
+    return true;
+}
+
+int validate(const apollo_muon_config* cfg, Scales& sc)
+{
+    if (!cfg) return APOLLO_ERR_INVALID_ARG;
+    if (cfg->dtype != APOLLO_DT_F32 && cfg->dtype != APOLLO_DT_BF16) return APOLLO_ERR_INVALID_ARG;
+    if (cfg->ns_steps < 1 || cfg->ns_steps > APOLLO_MUON_MAX_STEPS) return APOLLO_ERR_INVALID_ARG;
+    for (float c : cfg->coef)
+        if (!std::isfinite(c)) return APOLLO_ERR_INVALID_ARG;
+    if (!(cfg->momentum >= 0.0f && cfg->momentum < 1.0f) || (cfg->nesterov != 0 && cfg->nesterov != 1)) return APOLLO_ERR_INVALID_ARG;
+    if (cfg->scale < APOLLO_MUON_SCALE_NONE || cfg->scale > APOLLO_MUON_SCALE_RMS) return APOLLO_ERR_INVALID_ARG;
+    if (!std::isfinite(cfg->eps) || !(cfg->eps > 0.0f)) return APOLLO_ERR_INVALID_ARG;
+    if (cfg->workspace_mb < 0 || cfg->workspace_mb > 65536) return APOLLO_ERR_INVALID_ARG;
+    return find_scales(*cfg, sc) ? APOLLO_OK : APOLLO_ERR_INVALID_ARG;
+}
+
+// Tile k-blocks of one step, and of two steps together: what a pair of CTAs works off.
+void costs(int m, int n, double& one, double& two)
+{
+    const double t = (m + MUON_TILE - 1) / MUON_TILE, u = (n + MUON_TILE - 1) / MUON_TILE, km = (m + 63) / 64, kn = (n + 63) / 64;
+    const double sym = t * (t + 1) / 2;
+    one = sym * kn + sym * km + t * u * km;
+    two = sym * kn + 5 * sym * km + t * u * km;
+}
+
+int phases_of(const Mat& m, int steps) { return m.together ? steps / 2 * 7 + steps % 2 * 3 : steps * 3; }
+
+int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_config* cfg, Plan& plan)
+{
+    if (!shapes || n_mat < 1) return APOLLO_ERR_INVALID_ARG;
+    const int rc = validate(cfg, plan.sc);
+    if (rc != APOLLO_OK) return rc;
+    plan.parts = cfg->dtype == APOLLO_DT_F32 ? 2 : 1;
+    plan.maps_per_mat = (2 * 2 + 3 * 3) * plan.parts;
+    plan.mats.resize(n_mat);
+    std::vector<size_t> need(n_mat);
+    for (int i = 0; i < n_mat; ++i) {
+        const int64_t rows = shapes[i].rows, cols = shapes[i].cols;
+        if (rows < 1 || cols < 1 || rows > MAX_SIDE || cols > MAX_SIDE) return APOLLO_ERR_SHAPE;
+        Mat& m = plan.mats[i];
+        m.rows = (int)rows; m.cols = (int)cols;
+        m.tall = rows > cols;
+        m.m = m.tall ? m.cols : m.rows;
+        m.n = m.tall ? m.rows : m.cols;
+        m.pitch_x = round_up(m.n, 64);
+        m.pitch_s = round_up(m.m, 64);
+        const int64_t numel = rows * cols;
+        m.n_part = (int)std::min<int64_t>(MUON_PART, (numel + 8191) / 8192);
+        double one, two;
+        costs(m.m, m.n, one, two);
+        m.together = cfg->ns_steps >= 2 && two < 2 * one;
+        size_t off = 0;
+        for (int b = 0; b < 2; ++b)
+            for (int h = 0; h < plan.parts; ++h) { m.x[b][h] = off; off = align_up(off + 2 * (size_t)m.m * m.pitch_x); }
+        for (int b = 0; b < 3; ++b)
+            for (int h = 0; h < plan.parts; ++h) { m.s[b][h] = off; off = align_up(off + 2 * (size_t)m.m * m.pitch_s); }
+        m.part = off; off = align_up(off + sizeof(double) * (size_t)m.n_part);
+        need[i] = off;
+    }
+    // groups: like matrices together (their phases then end together), as many as fit
+    std::vector<int> order(n_mat);
+    for (int i = 0; i < n_mat; ++i) order[i] = i;
+    std::stable_sort(order.begin(), order.end(), [&](int p, int q) {
+        const Mat &x = plan.mats[p], &y = plan.mats[q];
+        if (x.m != y.m) return x.m > y.m;
+        return x.n > y.n;
+    });
+    const size_t budget = (size_t)(cfg->workspace_mb ? cfg->workspace_mb : 2048) << 20;
+    plan.groups.clear();
+    size_t used = 0, largest = 0;
+    for (int i : order) {
+        if (plan.groups.empty() || (used > 0 && used + need[i] > budget)) { plan.groups.push_back(Group()); used = 0; }
+        Mat& m = plan.mats[i];
+        for (auto& b : m.x) for (size_t& o : b) o += used;
+        for (auto& b : m.s) for (size_t& o : b) o += used;
+        m.part += used;
+        used += need[i];
+        largest = std::max(largest, used);
+        plan.groups.back().mats.push_back(i);
+    }
+    plan.n_ops = 0; plan.n_prefix = 0;
+    for (Group& g : plan.groups) {
+        int phases = 0;
+        for (int i : g.mats) phases = std::max(phases, phases_of(plan.mats[i], cfg->ns_steps));
+        for (int p = 0; p < phases; ++p) {
+            Phase ph = { plan.n_ops, 0, plan.n_prefix, 0 };
+            for (int i : g.mats) ph.n_ops += p < phases_of(plan.mats[i], cfg->ns_steps) ? 1 : 0;
+            plan.n_ops += ph.n_ops;
+            plan.n_prefix += ph.n_ops + 1;
+            g.phases.push_back(ph);
+        }
+    }
+    size_t off = 0;
+    plan.off_status = off; off += ALIGN;
+    plan.off_table = off;
+    plan.off_maps = off; off = align_up(off + 128 * (size_t)plan.maps_per_mat * n_mat);
+    plan.off_ops = off; off = align_up(off + sizeof(GemmOp) * (size_t)plan.n_ops);
+    plan.off_prefix = off; off = align_up(off + sizeof(int) * (size_t)plan.n_prefix);
+    plan.table_bytes = off - plan.off_table;
+    for (int i = 0; i < n_mat; ++i) {
+        Mat& m = plan.mats[i];
+        for (auto& b : m.x) for (size_t& o : b) o += off;
+        for (auto& b : m.s) for (size_t& o : b) o += off;
+        m.part += off;
+        m.maps = plan.off_maps + 128 * (size_t)plan.maps_per_mat * i;
+    }
+    plan.total = off + largest;
+    return APOLLO_OK;
+}
+
+}  // namespace
+
+struct apollo_muon_ctx {
+    apollo_muon_config cfg;
+    Plan plan;
+    char* ws;
+    char* table;          // pinned host copy of the device tables
+    bool pinned;
+    bool first;
+    int last_launches;
+    MuonLaunch launch;
+};
+
+namespace {
+
+// The products of one matrix, in order.
+void ops_of(const apollo_muon_ctx* ctx, const Mat& m, std::vector<GemmOp>& out)
+{
+    const Plan& plan = ctx->plan;
+    const Scales& sc = plan.sc;
+    const double a = ctx->cfg.coef[0], b = ctx->cfg.coef[1], c = ctx->cfg.coef[2], p = a - sc.shift;
+    const int parts = plan.parts;
+    char* ws = ctx->ws;
+    auto x_map = [&](int buf, int h, int kind) { return (const void*)(ws + m.maps + 128 * (size_t)((buf * parts + h) * 2 + kind)); };
+    auto s_map = [&](int buf, int h, int kind) { return (const void*)(ws + m.maps + 128 * (size_t)(4 * parts + (buf * parts + h) * 3 + kind)); };
+    auto x_ptr = [&](int buf, int h) { return (const __half*)(ws + m.x[buf][h]); };
+    auto s_ptr = [&](int buf, int h) { return (const __half*)(ws + m.s[buf][h]); };
+    auto square = [&](int l, int r, int dst, double alpha, int e1, double b1, int e2, double b2, double diag, bool of_x) {
+        GemmOp o;
+        std::memset(&o, 0, sizeof(o));
+        for (int h = 0; h < parts; ++h) {
+            o.l_map[h] = of_x ? x_map(l, h, 0) : s_map(l, h, 0);
+            o.r_map[h] = of_x ? x_map(r, h, 0) : s_map(r, h, 0);
+            o.out_map[h] = s_map(dst, h, 1);
+            o.mir_map[h] = s_map(dst, h, 2);
+            if (e1 >= 0) o.e1[h] = s_ptr(e1, h);
+            if (e2 >= 0) o.e2[h] = s_ptr(e2, h);
+        }
+        o.alpha = (float)alpha; o.b1 = (float)b1; o.b2 = (float)b2; o.diag = (float)diag;
+        o.M = o.N = m.m; o.K = of_x ? m.n : m.m; o.e_pitch = m.pitch_s;
+        o.tiles_m = o.tiles_n = (m.m + MUON_TILE - 1) / MUON_TILE;
+        o.sym = 1;
+        out.push_back(o);
+    };
+    auto update = [&](int s, int src, double alpha, double b1) {
+        GemmOp o;
+        std::memset(&o, 0, sizeof(o));
+        for (int h = 0; h < parts; ++h) {
+            o.l_map[h] = s_map(s, h, 0);
+            o.r_map[h] = x_map(src, h, 0);
+            o.out_map[h] = x_map(src ^ 1, h, 1);
+            o.e1[h] = x_ptr(src, h);
+        }
+        o.alpha = (float)alpha; o.b1 = (float)b1;
+        o.M = m.m; o.N = m.n; o.K = m.m; o.e_pitch = m.pitch_x;
+        o.tiles_m = (m.m + MUON_TILE - 1) / MUON_TILE; o.tiles_n = (m.n + MUON_TILE - 1) / MUON_TILE;
+        o.r_mn = 1;
+        out.push_back(o);
+    };
+    int x = 0;
+    for (int k = 0; k < ctx->cfg.ns_steps;) {
+        square(x, x, 0, sc.a / (sc.x * sc.x), -1, 0, -1, 0, 0, true);                                   // S0 = A
+        square(0, 0, 1, c * sc.b / (sc.a * sc.a), 0, b * sc.b / sc.a, -1, 0, sc.shift * sc.b, false);   // S1 = B + s I
+        if (m.together && k + 2 <= ctx->cfg.ns_steps) {
+            square(1, 0, 2, sc.t / (sc.b * sc.a), 0, p * sc.t / sc.a, -1, 0, 0, false);                 // S2 = T = P A
+            square(1, 2, 0, sc.a / (sc.b * sc.t), 2, p * sc.a / sc.t, -1, 0, 0, false);                 // S0 = A' = P T
+            square(0, 0, 2, c * sc.b / (sc.a * sc.a), 0, b * sc.b / sc.a, -1, 0, sc.shift * sc.b, false);   // S2 = B' + s I
+            square(2, 1, 0, sc.q / (sc.b * sc.b), 2, p * sc.q / sc.b, 1, p * sc.q / sc.b, (p * p - Q_SHIFT) * sc.q, false);   // S0 = Q - I
+            update(0, x, 1.0 / sc.q, Q_SHIFT);
+            k += 2;
+        } else {
+            update(1, x, 1.0 / sc.b, p);
+            k += 1;
+        }
+        x ^= 1;
+    }
+}
+
+// Fills the host copy of the tables.
+int build_table(apollo_muon_ctx* ctx)
+{
+    Plan& plan = ctx->plan;
+    char* t = ctx->table;                                   // corresponds to ws + off_table
+    auto at = [&](size_t off) { return t + (off - plan.off_table); };
+    std::vector<std::vector<GemmOp>> ops(plan.mats.size());
+    for (size_t i = 0; i < plan.mats.size(); ++i) {
+        const Mat& m = plan.mats[i];
+        char* maps = at(m.maps);
+        for (int b = 0; b < 2; ++b)
+            for (int h = 0; h < plan.parts; ++h, maps += 256) {
+                const int rc = muon_encode_maps((const __half*)(ctx->ws + m.x[b][h]), m.m, m.n, m.pitch_x, maps, maps + 128, nullptr);
+                if (rc != APOLLO_OK) return rc;
+            }
+        for (int b = 0; b < 3; ++b)
+            for (int h = 0; h < plan.parts; ++h, maps += 384) {
+                const int rc = muon_encode_maps((const __half*)(ctx->ws + m.s[b][h]), m.m, m.m, m.pitch_s, maps, maps + 128, maps + 256);
+                if (rc != APOLLO_OK) return rc;
+            }
+        ops_of(ctx, m, ops[i]);
+    }
+    GemmOp* d_ops = reinterpret_cast<GemmOp*>(at(plan.off_ops));
+    int* prefix = reinterpret_cast<int*>(at(plan.off_prefix));
+    for (Group& g : plan.groups) {
+        for (size_t p = 0; p < g.phases.size(); ++p) {
+            Phase& ph = g.phases[p];
+            std::vector<const GemmOp*> list;
+            for (int i : g.mats)
+                if (p < ops[i].size()) list.push_back(&ops[i][p]);
+            // tiles are dealt out in order: the longest ones first, so that the last ones dealt are short
+            std::stable_sort(list.begin(), list.end(), [](const GemmOp* x, const GemmOp* y) { return x->K > y->K; });
+            int64_t tiles = 0;
+            for (size_t k = 0; k < list.size(); ++k) {
+                d_ops[ph.op_begin + k] = *list[k];
+                prefix[ph.prefix_begin + k] = (int)tiles;
+                tiles += list[k]->sym ? (int64_t)list[k]->tiles_m * (list[k]->tiles_m + 1) / 2 : (int64_t)list[k]->tiles_m * list[k]->tiles_n;
+                if (tiles > INT32_MAX) return APOLLO_ERR_SHAPE;
+            }
+            prefix[ph.prefix_begin + list.size()] = (int)tiles;
+            ph.tiles = (int)tiles;
+        }
+    }
+    return APOLLO_OK;
+}
+
+double gain_of(const apollo_muon_config& cfg, const Mat& m)
+{
+    if (cfg.scale == APOLLO_MUON_SCALE_SHAPE) return std::sqrt(std::max(1.0, (double)m.rows / m.cols));
+    if (cfg.scale == APOLLO_MUON_SCALE_RMS) return 0.2 * std::sqrt((double)std::max(m.rows, m.cols));
+    return 1.0;
+}
+
+// `step`: momentum and weights; else U in d_G, O in d_W.
+int run(apollo_muon_ctx* ctx, void* const* d_W, const void* const* d_G, float* const* d_M, float lr, float wd, bool step, void* cuda_stream)
+{
+    if (!ctx || !d_W || !d_G || (step && !d_M)) return APOLLO_ERR_INVALID_ARG;
+    if (!std::isfinite(lr) || !std::isfinite(wd)) return APOLLO_ERR_INVALID_ARG;
+    const Plan& plan = ctx->plan;
+    for (size_t i = 0; i < plan.mats.size(); ++i) {
+        if (!d_W[i] || !d_G[i] || (step && !d_M[i])) return APOLLO_ERR_INVALID_ARG;
+        if ((uintptr_t)d_W[i] % 16 || (uintptr_t)d_G[i] % 16 || (step && (uintptr_t)d_M[i] % 16)) return APOLLO_ERR_ALIGN;
+    }
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    int32_t* d_status = reinterpret_cast<int32_t*>(ctx->ws + plan.off_status);
+    if (ctx->first) {
+        if (cudaMemsetAsync(d_status, 0, ALIGN, stream) != cudaSuccess ||
+            cudaMemcpyAsync(ctx->ws + plan.off_table, ctx->table, plan.table_bytes, cudaMemcpyHostToDevice, stream) != cudaSuccess) {
+            cudaGetLastError();
+            return APOLLO_ERR_CUDA;
+        }
+    }
+    const GemmOp* d_ops = reinterpret_cast<const GemmOp*>(ctx->ws + plan.off_ops);
+    const int* d_prefix = reinterpret_cast<const int*>(ctx->ws + plan.off_prefix);
+    const int dtype = ctx->cfg.dtype;
+    int launches = 0;
+    cudaError_t err = cudaSuccess;
+    for (const Group& g : plan.groups) {
+        // streaming passes: up to MUON_CHUNK matrices a launch, their pointers as kernel parameters
+        auto pass = [&](int which) {
+            for (size_t at = 0; at < g.mats.size() && err == cudaSuccess; at += MUON_CHUNK) {
+                MuonArgs a;
+                a.n = (int)std::min<size_t>(MUON_CHUNK, g.mats.size() - at);
+                a.mu = ctx->cfg.momentum; a.eps = ctx->cfg.eps; a.x_scale = (float)plan.sc.x; a.lr = lr; a.wd = wd; a.nesterov = ctx->cfg.nesterov;
+                int64_t tiles = 0;
+                for (int k = 0; k < a.n; ++k) {
+                    const int i = g.mats[at + k];
+                    const Mat& m = plan.mats[i];
+                    MuonItem& it = a.item[k];
+                    const int steps = ctx->cfg.ns_steps;
+                    const int updates = m.together ? (steps + 1) / 2 : steps;
+                    const int buf = which == 2 ? updates & 1 : 0;
+                    it.w = d_W[i]; it.g = d_G[i]; it.m = step ? d_M[i] : nullptr;
+                    it.x[0] = reinterpret_cast<__half*>(ctx->ws + m.x[buf][0]);
+                    it.x[1] = plan.parts == 2 ? reinterpret_cast<__half*>(ctx->ws + m.x[buf][1]) : nullptr;
+                    it.part = reinterpret_cast<double*>(ctx->ws + m.part);
+                    it.rows = m.rows; it.cols = m.cols; it.x_pitch = m.pitch_x; it.n_part = m.n_part; it.tall = m.tall;
+                    it.gain = (float)gain_of(ctx->cfg, m);
+                    a.tile_begin[k] = (int)tiles;
+                    tiles += which == 0 ? m.n_part : muon_stream_tiles(m.rows, m.cols);
+                }
+                for (int k = a.n; k <= MUON_CHUNK; ++k) a.tile_begin[k] = (int)tiles;
+                if (tiles > INT32_MAX) { err = cudaErrorInvalidValue; return; }
+                if (which == 0) err = launch_muon_moment(dtype, step, a, (int)tiles, d_status, stream);
+                else if (which == 1) err = launch_muon_load(dtype, step, a, (int)tiles, d_status, stream);
+                else err = launch_muon_apply(dtype, step, a, (int)tiles, d_status, stream);
+                ++launches;
+            }
+        };
+        pass(0);
+        pass(1);
+        for (const Phase& ph : g.phases) {
+            if (err != cudaSuccess) break;
+            err = launch_muon_gemm(plan.parts == 2, d_ops + ph.op_begin, d_prefix + ph.prefix_begin, ph.n_ops, ph.tiles, ctx->launch, d_status, stream);
+            ++launches;
+        }
+        pass(2);
+    }
+    if (err != cudaSuccess) { cudaGetLastError(); return APOLLO_ERR_CUDA; }
+    ctx->first = false;
+    ctx->last_launches = launches;
+    return APOLLO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int apollo_muon_workspace_bytes(const apollo_shape* shapes, int32_t n_matrices, const apollo_muon_config* cfg, size_t* out_bytes)
+{
+    if (!out_bytes) return APOLLO_ERR_INVALID_ARG;
+    try {
+        Plan plan;
+        const int rc = make_plan(shapes, n_matrices, cfg, plan);
+        if (rc != APOLLO_OK) return rc;
+        *out_bytes = plan.total;
+        return APOLLO_OK;
+    } catch (...) {
+        return APOLLO_ERR_INVALID_ARG;
+    }
+}
+
+int apollo_muon_create(apollo_muon_ctx** out_ctx, const apollo_shape* shapes, int32_t n_matrices, const apollo_muon_config* cfg,
+                       void* d_workspace, size_t workspace_bytes)
+{
+    if (!out_ctx) return APOLLO_ERR_INVALID_ARG;
+    *out_ctx = nullptr;
+    apollo_muon_ctx* ctx = new (std::nothrow) apollo_muon_ctx();
+    if (!ctx) return APOLLO_ERR_INVALID_ARG;
+    ctx->table = nullptr;
+    ctx->pinned = false;
+    int rc;
+    try {
+        rc = make_plan(shapes, n_matrices, cfg, ctx->plan);
+        if (rc == APOLLO_OK && !d_workspace) rc = APOLLO_ERR_INVALID_ARG;
+        if (rc == APOLLO_OK && ((uintptr_t)d_workspace % ALIGN || workspace_bytes < ctx->plan.total)) rc = APOLLO_ERR_WORKSPACE;
+        int device = 0, major = 0, sms = 0;
+        if (rc == APOLLO_OK && (cudaGetDevice(&device) != cudaSuccess ||
+                                cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, device) != cudaSuccess ||
+                                cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)) {
+            cudaGetLastError();
+            rc = APOLLO_ERR_CUDA;
+        }
+        if (rc == APOLLO_OK && major != 10) rc = APOLLO_ERR_UNSUPPORTED;
+        if (rc == APOLLO_OK) {
+            ctx->cfg = *cfg;
+            ctx->ws = static_cast<char*>(d_workspace);
+            ctx->first = true;
+            ctx->last_launches = 0;
+            ctx->launch = MuonLaunch{ sms, 0, false };
+            void* host = nullptr;
+            if (cudaHostAlloc(&host, ctx->plan.table_bytes, cudaHostAllocDefault) == cudaSuccess) {
+                ctx->pinned = true;
+            } else {
+                cudaGetLastError();                     // no pinned memory to be had: the upload goes from pageable memory
+                host = new char[ctx->plan.table_bytes];
+            }
+            ctx->table = static_cast<char*>(host);
+            std::memset(ctx->table, 0, ctx->plan.table_bytes);
+            rc = build_table(ctx);
+        }
+    } catch (...) {
+        rc = APOLLO_ERR_INVALID_ARG;
+    }
+    if (rc != APOLLO_OK) {
+        apollo_muon_destroy(ctx);
+        return rc;
+    }
+    *out_ctx = ctx;
+    return APOLLO_OK;
+}
+
+int apollo_muon_destroy(apollo_muon_ctx* ctx)
+{
+    if (!ctx) return APOLLO_ERR_INVALID_ARG;
+    if (ctx->table) {
+        if (ctx->pinned) cudaFreeHost(ctx->table);      // waits for an upload in flight
+        else delete[] ctx->table;
+    }
+    delete ctx;
+    return APOLLO_OK;
+}
+
+int apollo_muon_step(apollo_muon_ctx* ctx, void* const* d_W, const void* const* d_G, float* const* d_M, float lr, float wd, void* cuda_stream)
+{
+    return run(ctx, d_W, d_G, d_M, lr, wd, true, cuda_stream);
+}
+
+int apollo_muon_orthogonalize(apollo_muon_ctx* ctx, const void* const* d_U, void* const* d_O, void* cuda_stream)
+{
+    return run(ctx, d_O, d_U, nullptr, 0.0f, 0.0f, false, cuda_stream);
+}
+
+int apollo_muon_status(apollo_muon_ctx* ctx, void* cuda_stream)
+{
+    if (!ctx) return APOLLO_ERR_INVALID_ARG;
+    if (cudaStreamSynchronize(static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return APOLLO_ERR_CUDA;
+    if (ctx->first) return APOLLO_OK;                   // nothing has run; the status word is not initialised yet
+    int32_t word = 0;
+    char* d_status = ctx->ws + ctx->plan.off_status;
+    if (cudaMemcpy(&word, d_status, sizeof(word), cudaMemcpyDeviceToHost) != cudaSuccess) return APOLLO_ERR_CUDA;
+    if (word != STATUS_OK) {
+        cudaMemset(d_status, 0, 2 * sizeof(word));
+        return word == STATUS_BOUNDS ? APOLLO_ERR_INTERNAL : APOLLO_ERR_TIMEOUT;
+    }
+    return APOLLO_OK;
+}
+
+int apollo_muon_last_launches(const apollo_muon_ctx* ctx, int32_t* out)
+{
+    if (!ctx || !out) return APOLLO_ERR_INVALID_ARG;
+    *out = ctx->last_launches;
+    return APOLLO_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,549 @@
+// Embedding lookup and its gradient: the first parameter of the model that the method does not project, whose
+// gradient feeds apollo_adamw_step.
+//
+//   lookup    out[t] = scale E[index[t]]
+//   gradient  dE[v]  = scale sum over {t : index[t] = v} of dOut[t]   (+ dE[v] when accumulating)
+//
+// A position whose index lies outside [0, rows) (padding) gives a zero row and no gradient.
+//
+// The gradient is a sum over positions grouped by token.  Positions are sorted by token (stable, so a token's
+// positions stay in order), the sorted order is cut into windows of EMB_WINDOW positions, and a window sums the
+// runs of equal tokens inside it in fp32: a run that is a token's whole segment is written at once, a piece of a
+// longer segment goes to a partial row that embed_join_kernel adds up in window order.  A frequent token is so
+// spread over the chip, and the order of every sum is a function of the indices alone: no float atomics, equal
+// bits in every run.
+#include "../../include/apollo.h"
+
+#include <cooperative_groups.h>
+
+#include <cmath>
+
+#include "device_utils.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace apollo {
+
+namespace {
+
+constexpr int EMB_THREADS = 256;
+constexpr int EMB_WINDOW = 32;         // sorted positions per window
+constexpr int SORT_THREADS = 512;
+constexpr int SORT_WARPS = SORT_THREADS / 32;
+constexpr int SORT_ITEMS = 8;          // keys per thread and tile
+constexpr int SORT_TILE = SORT_THREADS * SORT_ITEMS;
+constexpr int SORT_CLUSTER = 8;        // CTAs that share one sort through distributed shared memory
+constexpr int SORT_BITS = 8, SORT_BINS = 1 << SORT_BITS;
+constexpr size_t EMB_ALIGN = 256;
+
+size_t emb_align(size_t x) { return (x + EMB_ALIGN - 1) / EMB_ALIGN * EMB_ALIGN; }
+
+// Index t of the caller's array as a key in [0, rows]: everything outside [0, rows) becomes `rows`.
+template <typename I>
+__device__ __forceinline__ uint32_t index_key(const I* __restrict__ index, int64_t t, int64_t rows)
+{
+    const long long v = (long long)index[t];
+    return v >= 0 && v < rows ? (uint32_t)v : (uint32_t)rows;
+}
+
+template <typename T> __device__ __forceinline__ void emb_store1(T* p, float v);
+template <> __device__ __forceinline__ void emb_store1<float>(float* p, float v) { *p = v; }
+template <> __device__ __forceinline__ void emb_store1<__nv_bfloat16>(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// 16 bytes: VEC elements of T
+template <typename T> struct Vec16;
+template <> struct Vec16<float> {
+    static constexpr int N = 4;
+    __device__ static __forceinline__ void unpack(const uint4& r, float (&v)[4])
+    {
+        v[0] = __uint_as_float(r.x); v[1] = __uint_as_float(r.y); v[2] = __uint_as_float(r.z); v[3] = __uint_as_float(r.w);
+    }
+    __device__ static __forceinline__ uint4 pack(const float (&v)[4])
+    {
+        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    }
+};
+template <> struct Vec16<__nv_bfloat16> {
+    static constexpr int N = 8;
+    __device__ static __forceinline__ void unpack(const uint4& r, float (&v)[8]) { unpack_bf16x8(r, v); }
+    __device__ static __forceinline__ uint4 pack(const float (&v)[8])
+    {
+        return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+    }
+};
+
+// ---------------------------------------------------------------- lookup
+// Bound: HBM, the distinct rows read once (repeats come from L2) and T x dim written.  `tpr` threads (a power of
+// two) share a row; a thread has four vectors in flight.  VECTOR: table and output rows are whole 16-byte vectors.
+template <typename T, typename I, bool VECTOR>
+__global__ void __launch_bounds__(EMB_THREADS)
+embed_kernel(const T* __restrict__ table, int64_t rows, int dim, const I* __restrict__ index, int64_t n_tokens, float scale,
+             T* __restrict__ out, int64_t out_stride, int tpr_log2)
+{
+    const int tpr = 1 << tpr_log2, per_block = EMB_THREADS >> tpr_log2;
+    const int lane = threadIdx.x & (tpr - 1), row_in_block = threadIdx.x >> tpr_log2;
+    constexpr int V = VECTOR ? Vec16<T>::N : 1;
+    const int units = dim / V;
+    for (int64_t t = (int64_t)blockIdx.x * per_block + row_in_block; t < n_tokens; t += (int64_t)gridDim.x * per_block) {
+        const uint32_t key = index_key(index, t, rows);
+        const bool live = key < rows;
+        const T* src = table + (int64_t)key * dim;
+        T* dst = out + t * out_stride;
+        for (int u0 = lane; u0 < units; u0 += 4 * tpr) {
+            if constexpr (VECTOR) {
+                uint4 raw[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int u = u0 + k * tpr;
+                    raw[k] = live && u < units ? __ldg(reinterpret_cast<const uint4*>(src) + u) : make_uint4(0, 0, 0, 0);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int u = u0 + k * tpr;
+                    if (u >= units) break;
+                    float v[V];
+                    Vec16<T>::unpack(raw[k], v);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[e] *= scale;
+                    __stcs(reinterpret_cast<uint4*>(dst) + u, Vec16<T>::pack(v));
+                }
+            } else {
+                float v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int u = u0 + k * tpr;
+                    v[k] = live && u < units ? load1(src + u) : 0.0f;
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int u = u0 + k * tpr;
+                    if (u < units) emb_store1<T>(dst + u, v[k] * scale);
+                }
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- sort (and zero fill beside it)
+// Stable least-significant-digit radix sort of (token, position) by ONE cluster of SORT_CLUSTER CTAs; the other
+// clusters of the launch write zeros over dE meanwhile (when not accumulating), which no step of the sort waits
+// for: the sort costs no time as long as it is shorter than that fill (V dim e bytes of writes).
+//
+// A pass over one 8-bit digit: every CTA counts the digits of its contiguous share; the counts are exchanged
+// through distributed shared memory (base of a digit = all smaller digits anywhere + the same digit in CTAs of
+// lower rank); then it ranks its share tile by tile and scatters.  Inside a tile a warp owns 32 x SORT_ITEMS
+// consecutive keys and takes them 32 at a time: __match_any_sync gives the lanes with the same digit, the
+// warp's running count of the digit the keys before them.
+struct SortArgs {
+    uint2* buf[2];          // (key, position) ping-pong
+    int64_t n;
+    int passes;
+    uint32_t rows;          // sentinel key of positions without a row
+};
+
+template <typename I>
+__global__ void __cluster_dims__(SORT_CLUSTER, 1, 1) __launch_bounds__(SORT_THREADS)
+embed_sort_kernel(const I* __restrict__ index, SortArgs a, uint4* __restrict__ zero, int64_t zero_vecs, char* __restrict__ zero_tail,
+                  int zero_tail_bytes)
+{
+    if (blockIdx.x >= SORT_CLUSTER) {
+        const int64_t stride = (int64_t)(gridDim.x - SORT_CLUSTER) * SORT_THREADS;
+        const int64_t first = (int64_t)(blockIdx.x - SORT_CLUSTER) * SORT_THREADS + threadIdx.x;
+        for (int64_t v = first; v < zero_vecs; v += stride) zero[v] = make_uint4(0, 0, 0, 0);
+        if (first < zero_tail_bytes) zero_tail[first] = 0;
+        return;
+    }
+    __shared__ uint32_t hist[SORT_BINS];                 // this CTA's digit counts, read by the whole cluster
+    __shared__ uint32_t base[SORT_BINS];                 // where the next key of a digit goes
+    __shared__ uint32_t warp_hist[SORT_WARPS][SORT_BINS];
+    __shared__ uint32_t scan[SORT_WARPS];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int cta = (int)cluster.block_rank();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int64_t share = (a.n + SORT_CLUSTER - 1) / SORT_CLUSTER;
+    const int64_t begin = min((int64_t)cta * share, a.n), end = min(begin + share, a.n);
+
+    for (int pass = 0; pass < a.passes; ++pass) {
+        const int shift = pass * SORT_BITS;
+        const uint2* src = a.buf[(pass + 1) & 1];        // pass 0 reads the caller's indices
+        uint2* dst = a.buf[pass & 1];
+        for (int d = tid; d < SORT_BINS; d += SORT_THREADS) hist[d] = 0;
+        __syncthreads();
+        for (int64_t t = begin + tid; t < end; t += SORT_THREADS) {
+            const uint32_t key = pass == 0 ? index_key(index, t, (int64_t)a.rows) : __ldcg(src + t).x;   // other CTAs wrote it in this launch: from L2
+            atomicAdd(&hist[(key >> shift) & (SORT_BINS - 1)], 1u);
+        }
+        cluster.sync();
+        // digit totals over the cluster, their exclusive sum, and the counts of this digit in CTAs before this one
+        uint32_t total = 0, before = 0;
+        if (tid < SORT_BINS) {
+            for (int c = 0; c < SORT_CLUSTER; ++c) {
+                const uint32_t h = cluster.map_shared_rank(hist, c)[tid];
+                total += h;
+                if (c < cta) before += h;
+            }
+        }
+        uint32_t incl = total;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, incl, off);
+            if (lane >= off) incl += up;
+        }
+        if (lane == 31) scan[warp] = incl;
+        __syncthreads();
+        if (tid < SORT_BINS) {
+            uint32_t lower = 0;
+            for (int w = 0; w < warp; ++w) lower += scan[w];
+            base[tid] = lower + incl - total + before;
+        }
+        cluster.sync();                                  // everyone has read hist: it may be cleared in the next pass
+        for (int64_t tile = begin; tile < end; tile += SORT_TILE) {
+            for (int d = tid; d < SORT_BINS * SORT_WARPS; d += SORT_THREADS) (&warp_hist[0][0])[d] = 0;
+            __syncthreads();
+            uint2 kv[SORT_ITEMS];
+            uint32_t rank[SORT_ITEMS];
+            const int64_t first = tile + (int64_t)warp * (32 * SORT_ITEMS) + lane;
+#pragma unroll
+            for (int k = 0; k < SORT_ITEMS; ++k) {
+                const int64_t t = first + k * 32;
+                kv[k] = t >= end ? make_uint2(0xFFFFFFFFu, 0)
+                                 : (pass == 0 ? make_uint2(index_key(index, t, (int64_t)a.rows), (uint32_t)t) : __ldcg(src + t));
+            }
+#pragma unroll
+            for (int k = 0; k < SORT_ITEMS; ++k) {
+                const bool valid = first + k * 32 < end;
+                const uint32_t d = (kv[k].x >> shift) & (SORT_BINS - 1);
+                const uint32_t same = __match_any_sync(0xFFFFFFFFu, valid ? d : 0xFFFFFFFFu);
+                const uint32_t below = __popc(same & ((1u << lane) - 1u));
+                rank[k] = below;
+                if (valid) rank[k] += warp_hist[warp][d];
+                __syncwarp();
+                if (valid && below == 0) warp_hist[warp][d] += __popc(same);
+                __syncwarp();
+            }
+            __syncthreads();
+            // exclusive sums over the warps of each digit, then the digit's running base
+            if (tid < SORT_BINS) {
+                uint32_t run = base[tid];
+                for (int w = 0; w < SORT_WARPS; ++w) {
+                    const uint32_t h = warp_hist[w][tid];
+                    warp_hist[w][tid] = run;
+                    run += h;
+                }
+                base[tid] = run;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < SORT_ITEMS; ++k)
+                if (first + k * 32 < end) dst[warp_hist[warp][(kv[k].x >> shift) & (SORT_BINS - 1)] + rank[k]] = kv[k];
+            __syncthreads();
+        }
+        __threadfence();
+        cluster.sync();                                  // the other CTAs read what this one scattered
+    }
+}
+
+// ---------------------------------------------------------------- sums
+// Columns [c0, c0 + V) of dE row `row` <- acc (scaled), added to what is there when accumulating.
+template <typename T, int V>
+__device__ __forceinline__ void grad_write(T* __restrict__ d_table, int64_t row, int dim, int c, const float (&acc)[V], float scale, bool accumulate)
+{
+    T* p = d_table + row * dim + c;
+    if constexpr (V > 1) {
+        float v[V];
+        if (accumulate) {
+            Vec16<T>::unpack(*reinterpret_cast<const uint4*>(p), v);
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = fmaf(acc[e], scale, v[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = acc[e] * scale;
+        }
+        __stcs(reinterpret_cast<uint4*>(p), Vec16<T>::pack(v));
+    } else {
+        emb_store1<T>(p, accumulate ? fmaf(acc[0], scale, load1(p)) : acc[0] * scale);
+    }
+}
+
+// One window of sorted positions and `tpw` x V columns per thread group.  A run of equal tokens that both starts
+// and ends in the window is written to dE; the first run, when it began in an earlier window, goes to partial row
+// 2 w, and the last one, when it goes on in the next window, to partial row 2 w + 1 (a run that does both counts
+// as the first).  Bound: HBM, every row of dOut read once; eight rows' loads are issued before the first is added.
+template <typename T, bool VECTOR>
+__global__ void __launch_bounds__(EMB_THREADS)
+embed_sum_kernel(const T* __restrict__ d_out, int64_t out_stride, const uint2* __restrict__ sorted, int64_t n, uint32_t rows, int dim,
+                 float scale, bool accumulate, T* __restrict__ d_table, float* __restrict__ partial, int tpw_log2, int64_t windows)
+{
+    constexpr int V = VECTOR ? Vec16<T>::N : 1;
+    __shared__ uint2 entry[EMB_THREADS / 8][EMB_WINDOW];
+    const int tpw = 1 << tpw_log2, groups = EMB_THREADS >> tpw_log2;
+    const int g = threadIdx.x >> tpw_log2, lane = threadIdx.x & (tpw - 1);
+    for (int i = threadIdx.x; i < groups * EMB_WINDOW; i += EMB_THREADS) {
+        const int64_t at = ((int64_t)blockIdx.x * groups + i / EMB_WINDOW) * EMB_WINDOW + (i & (EMB_WINDOW - 1));
+        entry[i / EMB_WINDOW][i & (EMB_WINDOW - 1)] = at < n ? sorted[at] : make_uint2(rows, 0);
+    }
+    __syncthreads();
+    const int64_t w = (int64_t)blockIdx.x * groups + g;
+    if (w >= windows) return;
+    const int64_t at0 = w * EMB_WINDOW;
+    const int count = (int)min((int64_t)EMB_WINDOW, n - at0);
+    const bool from_before = at0 > 0 && sorted[at0 - 1].x == entry[g][0].x;
+    const bool goes_on = at0 + EMB_WINDOW < n && sorted[at0 + EMB_WINDOW].x == entry[g][EMB_WINDOW - 1].x;
+    for (int c = ((int)blockIdx.y * tpw + lane) * V; c < dim; c += (int)gridDim.y * tpw * V) {
+        float acc[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+        bool first_run = true;
+        for (int i0 = 0; i0 < count; i0 += 8) {
+            float v[8][V];
+            uint4 raw[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const bool in = i0 + k < count && entry[g][(i0 + k) & (EMB_WINDOW - 1)].x < rows;
+                const T* p = d_out + (int64_t)entry[g][(i0 + k) & (EMB_WINDOW - 1)].y * out_stride + c;
+                if constexpr (VECTOR) raw[k] = in ? __ldcs(reinterpret_cast<const uint4*>(p)) : make_uint4(0, 0, 0, 0);
+                else v[k][0] = in ? load1(p) : 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int i = i0 + k;
+                if (i >= count) break;
+                if constexpr (VECTOR) Vec16<T>::unpack(raw[k], v[k]);
+#pragma unroll
+                for (int e = 0; e < V; ++e) acc[e] += v[k][e];
+                const uint32_t key = entry[g][i].x;
+                const bool last = i + 1 == count;
+                if (!last && entry[g][i + 1].x == key) continue;
+                if (key < rows) {
+                    const bool piece_first = first_run && from_before, piece_last = last && goes_on;
+                    if (piece_first || piece_last) {
+                        float* p = partial + (2 * w + (piece_first ? 0 : 1)) * dim + c;
+#pragma unroll
+                        for (int e = 0; e < V; ++e) p[e] = acc[e];
+                    } else {
+                        grad_write<T, V>(d_table, (int64_t)key, dim, c, acc, scale, accumulate);
+                    }
+                }
+                first_run = false;
+#pragma unroll
+                for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+            }
+        }
+    }
+}
+
+// The segments that span windows: the block of the window in which such a segment starts adds up its partial rows
+// in window order.  Warps take contiguous ranges of the windows and their sums are added in warp order.
+template <typename T>
+__global__ void __launch_bounds__(EMB_THREADS)
+embed_join_kernel(const uint2* __restrict__ sorted, int64_t n, uint32_t rows, int dim, float scale, bool accumulate,
+                  T* __restrict__ d_table, const float* __restrict__ partial)
+{
+    __shared__ float sums[EMB_THREADS / 32][32];
+    const int64_t w = blockIdx.x, next = (w + 1) * EMB_WINDOW;
+    if (next >= n) return;
+    const uint32_t key = sorted[next - 1].x;
+    if (key >= rows || sorted[next].x != key) return;            // nothing goes on into the next window
+    if (w > 0 && sorted[w * EMB_WINDOW].x == key && sorted[w * EMB_WINDOW - 1].x == key) return;   // it began earlier
+    // first position after `next` with another token
+    int64_t lo = next, hi = n;                                   // sorted[lo] == key, sorted[hi] != key (or hi == n)
+    while (hi - lo > 1) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (sorted[mid].x == key) lo = mid; else hi = mid;
+    }
+    const int64_t last = (hi - 1) / EMB_WINDOW;                  // windows w + 1 .. last hold partial rows 2 x index, w its 2 w + 1
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t pieces = last - w + 1, per = (pieces + EMB_THREADS / 32 - 1) / (EMB_THREADS / 32);
+    const int64_t p0 = warp * per, p1 = min(p0 + per, pieces);
+    for (int c0 = blockIdx.y * 32; c0 < dim; c0 += gridDim.y * 32) {
+        const int c = c0 + lane;
+        float acc = 0.0f;
+        if (c < dim) {
+#pragma unroll 4
+            for (int64_t p = p0; p < p1; ++p) acc += partial[(2 * (w + p) + (p == 0 ? 1 : 0)) * dim + c];
+        }
+        sums[warp][lane] = acc;
+        __syncthreads();
+        if (warp == 0 && c < dim) {
+            float total[1] = { 0.0f };
+            for (int k = 0; k < EMB_THREADS / 32; ++k) total[0] += sums[k][lane];
+            grad_write<T, 1>(d_table, (int64_t)key, dim, c, total, scale, accumulate);
+        }
+        __syncthreads();
+    }
+}
+
+int log2_ceil(int64_t x)
+{
+    int b = 0;
+    while (((int64_t)1 << b) < x) ++b;
+    return b;
+}
+
+struct EmbLayout { size_t buf0, buf1, partial, total; };
+
+EmbLayout embed_layout(int64_t n, int64_t dim)
+{
+    EmbLayout l;
+    const int64_t windows = (n + EMB_WINDOW - 1) / EMB_WINDOW;
+    l.buf0 = 0;
+    l.buf1 = emb_align(sizeof(uint2) * (size_t)n);
+    l.partial = 2 * l.buf1;
+    l.total = l.partial + emb_align(sizeof(float) * 2 * (size_t)windows * (size_t)dim);
+    if (l.total == 0) l.total = EMB_ALIGN;
+    return l;
+}
+
+int check_embed(int64_t rows, int64_t dim, int32_t dtype, int32_t index_type, int64_t n, float scale, int64_t stride)
+{
+    if (dtype != APOLLO_DT_F32 && dtype != APOLLO_DT_BF16) return APOLLO_ERR_INVALID_ARG;
+    if (index_type != APOLLO_INDEX_I32 && index_type != APOLLO_INDEX_I64) return APOLLO_ERR_INVALID_ARG;
+    if (!std::isfinite(scale)) return APOLLO_ERR_INVALID_ARG;
+    if (rows < 1 || dim < 1 || n < 0 || rows > INT32_MAX || dim > (int64_t)1 << 24 || n > INT32_MAX || stride < dim) return APOLLO_ERR_SHAPE;
+    return APOLLO_OK;
+}
+
+int device_sms(int* sms)
+{
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) {
+        cudaGetLastError();
+        return APOLLO_ERR_CUDA;
+    }
+    return APOLLO_OK;
+}
+
+template <typename T, typename I>
+void run_embed(const void* table, int64_t rows, int dim, const void* index, int64_t n, float scale, void* out, int64_t stride, int sms, cudaStream_t stream)
+{
+    const bool vector = (size_t)dim * sizeof(T) % 16 == 0 && (size_t)stride * sizeof(T) % 16 == 0 &&
+                        (uintptr_t)table % 16 == 0 && (uintptr_t)out % 16 == 0;
+    const int units = vector ? dim / Vec16<T>::N : dim;
+    int lg = log2_ceil((units + 3) / 4);
+    if (lg < 3) lg = 3;
+    if (lg > 8) lg = 8;
+    const int64_t blocks = (n + (EMB_THREADS >> lg) - 1) / (EMB_THREADS >> lg), most = 16LL * sms;
+    const int grid = (int)(blocks < most ? blocks : most);
+    if (vector) embed_kernel<T, I, true><<<grid, EMB_THREADS, 0, stream>>>((const T*)table, rows, dim, (const I*)index, n, scale, (T*)out, stride, lg);
+    else embed_kernel<T, I, false><<<grid, EMB_THREADS, 0, stream>>>((const T*)table, rows, dim, (const I*)index, n, scale, (T*)out, stride, lg);
+}
+
+template <typename T>
+void run_embed_sum(const void* d_out, int64_t stride, const uint2* sorted, int64_t n, uint32_t rows, int dim, float scale, bool accumulate,
+                   void* d_table, float* partial, cudaStream_t stream)
+{
+    const bool vector = (size_t)dim * sizeof(T) % 16 == 0 && (size_t)stride * sizeof(T) % 16 == 0 &&
+                        (uintptr_t)d_out % 16 == 0 && (uintptr_t)d_table % 16 == 0;
+    const int units = vector ? dim / Vec16<T>::N : dim;
+    int lg = log2_ceil(units);
+    if (lg < 3) lg = 3;
+    if (lg > 8) lg = 8;
+    const int64_t windows = (n + EMB_WINDOW - 1) / EMB_WINDOW;
+    const int groups = EMB_THREADS >> lg;
+    const int cols = (units + (1 << lg) - 1) >> lg;
+    const dim3 grid((unsigned)((windows + groups - 1) / groups), (unsigned)(cols < 1024 ? cols : 1024));
+    if (vector) embed_sum_kernel<T, true><<<grid, EMB_THREADS, 0, stream>>>((const T*)d_out, stride, sorted, n, rows, dim, scale, accumulate, (T*)d_table, partial, lg, windows);
+    else embed_sum_kernel<T, false><<<grid, EMB_THREADS, 0, stream>>>((const T*)d_out, stride, sorted, n, rows, dim, scale, accumulate, (T*)d_table, partial, lg, windows);
+    if (windows > 1) {
+        const int cb = (dim + 31) / 32;
+        embed_join_kernel<T><<<dim3((unsigned)(windows - 1), (unsigned)(cb < 64 ? cb : 64)), EMB_THREADS, 0, stream>>>(sorted, n, rows, dim, scale, accumulate, (T*)d_table, partial);
+    }
+}
+
+}  // namespace
+
+}  // namespace apollo
+
+using namespace apollo;
+
+extern "C" int apollo_embedding(const void* d_table, int64_t rows, int64_t dim, int32_t dtype, const void* d_index, int32_t index_type,
+                                int64_t n_tokens, float scale, void* d_out, int64_t out_stride, void* cuda_stream)
+{
+    const int rc = check_embed(rows, dim, dtype, index_type, n_tokens, scale, out_stride);
+    if (rc != APOLLO_OK) return rc;
+    if (n_tokens == 0) return APOLLO_OK;
+    if (!d_table || !d_index || !d_out) return APOLLO_ERR_INVALID_ARG;
+    const size_t e = dtype == APOLLO_DT_BF16 ? 2 : 4, ie = index_type == APOLLO_INDEX_I64 ? 8 : 4;
+    if ((uintptr_t)d_table % e || (uintptr_t)d_out % e || (uintptr_t)d_index % ie) return APOLLO_ERR_ALIGN;
+    int sms = 0;
+    const int drc = device_sms(&sms);
+    if (drc != APOLLO_OK) return drc;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (dtype == APOLLO_DT_BF16) {
+        if (index_type == APOLLO_INDEX_I64) run_embed<__nv_bfloat16, long long>(d_table, rows, (int)dim, d_index, n_tokens, scale, d_out, out_stride, sms, stream);
+        else run_embed<__nv_bfloat16, int>(d_table, rows, (int)dim, d_index, n_tokens, scale, d_out, out_stride, sms, stream);
+    } else {
+        if (index_type == APOLLO_INDEX_I64) run_embed<float, long long>(d_table, rows, (int)dim, d_index, n_tokens, scale, d_out, out_stride, sms, stream);
+        else run_embed<float, int>(d_table, rows, (int)dim, d_index, n_tokens, scale, d_out, out_stride, sms, stream);
+    }
+    return cudaGetLastError() == cudaSuccess ? APOLLO_OK : APOLLO_ERR_CUDA;
+}
+
+extern "C" int apollo_embedding_grad_workspace_bytes(int64_t n_tokens, int64_t rows, int64_t dim, size_t* out_bytes)
+{
+    if (!out_bytes) return APOLLO_ERR_INVALID_ARG;
+    const int rc = check_embed(rows, dim, APOLLO_DT_F32, APOLLO_INDEX_I32, n_tokens, 1.0f, dim);
+    if (rc != APOLLO_OK) return rc;
+    *out_bytes = embed_layout(n_tokens, dim).total;
+    return APOLLO_OK;
+}
+
+extern "C" int apollo_embedding_grad(const void* d_out, int64_t out_stride, const void* d_index, int32_t index_type, int64_t n_tokens,
+                                     int64_t rows, int64_t dim, int32_t dtype, float scale, int32_t accumulate, void* d_table_grad,
+                                     void* d_workspace, size_t workspace_bytes, void* cuda_stream)
+{
+    const int rc = check_embed(rows, dim, dtype, index_type, n_tokens, scale, out_stride);
+    if (rc != APOLLO_OK) return rc;
+    if ((accumulate != 0 && accumulate != 1) || !d_table_grad) return APOLLO_ERR_INVALID_ARG;
+    const size_t e = dtype == APOLLO_DT_BF16 ? 2 : 4, ie = index_type == APOLLO_INDEX_I64 ? 8 : 4;
+    if ((uintptr_t)d_table_grad % e || (uintptr_t)d_out % e || (uintptr_t)d_index % ie) return APOLLO_ERR_ALIGN;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const size_t bytes = (size_t)rows * (size_t)dim * e;
+    if (n_tokens == 0) {
+        if (!accumulate && cudaMemsetAsync(d_table_grad, 0, bytes, stream) != cudaSuccess) return APOLLO_ERR_CUDA;
+        return APOLLO_OK;
+    }
+    if (!d_out || !d_index || !d_workspace) return APOLLO_ERR_INVALID_ARG;
+    const EmbLayout l = embed_layout(n_tokens, dim);
+    if ((uintptr_t)d_workspace % 16 || workspace_bytes < l.total) return APOLLO_ERR_WORKSPACE;
+    int sms = 0;
+    const int drc = device_sms(&sms);
+    if (drc != APOLLO_OK) return drc;
+    char* ws = static_cast<char*>(d_workspace);
+    SortArgs a;
+    a.buf[0] = reinterpret_cast<uint2*>(ws + l.buf0);
+    a.buf[1] = reinterpret_cast<uint2*>(ws + l.buf1);
+    a.n = n_tokens;
+    a.rows = (uint32_t)rows;
+    a.passes = (log2_ceil(rows + 1) + SORT_BITS - 1) / SORT_BITS;
+    // zero fill: whole 16-byte vectors from the first 16-byte boundary on, the few bytes before and after by the tail threads
+    char* z = static_cast<char*>(d_table_grad);
+    int clusters = 1;
+    int64_t vecs = 0;
+    int tail = 0;
+    char* tail_at = z;
+    if (!accumulate) {
+        if ((uintptr_t)z % 16) {
+            if (cudaMemsetAsync(z, 0, bytes, stream) != cudaSuccess) return APOLLO_ERR_CUDA;
+        } else {
+            vecs = (int64_t)(bytes / 16);
+            tail = (int)(bytes % 16);
+            tail_at = z + vecs * 16;
+            const int64_t want = (vecs + (int64_t)SORT_CLUSTER * SORT_THREADS * 8 - 1) / ((int64_t)SORT_CLUSTER * SORT_THREADS * 8);
+            const int64_t most = 4LL * sms / SORT_CLUSTER;
+            clusters += (int)(want < 1 ? 1 : want < most ? want : most);
+        }
+    }
+    const dim3 grid((unsigned)(clusters * SORT_CLUSTER));
+    if (index_type == APOLLO_INDEX_I64)
+        embed_sort_kernel<long long><<<grid, SORT_THREADS, 0, stream>>>((const long long*)d_index, a, (uint4*)z, vecs, tail_at, tail);
+    else
+        embed_sort_kernel<int><<<grid, SORT_THREADS, 0, stream>>>((const int*)d_index, a, (uint4*)z, vecs, tail_at, tail);
+    const uint2* sorted = a.buf[(a.passes - 1) & 1];
+    float* partial = reinterpret_cast<float*>(ws + l.partial);
+    if (dtype == APOLLO_DT_BF16)
+        run_embed_sum<__nv_bfloat16>(d_out, out_stride, sorted, n_tokens, (uint32_t)rows, (int)dim, scale, accumulate != 0, d_table_grad, partial, stream);
+    else
+        run_embed_sum<float>(d_out, out_stride, sorted, n_tokens, (uint32_t)rows, (int)dim, scale, accumulate != 0, d_table_grad, partial, stream);
+    return cudaGetLastError() == cudaSuccess ? APOLLO_OK : APOLLO_ERR_CUDA;
+}

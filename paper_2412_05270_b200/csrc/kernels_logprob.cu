@@ -1,0 +1,516 @@
+// Log probabilities of given tokens with entropy and the best alternatives, and their gradient: the loss at the
+// output head, whose weight the method does not project either.
+//
+//   z = scale * logit,  lse = log sum_j exp z_j,  logp = z_t - lse,  H = -sum_j p_j log p_j,  p_j = exp(z_j - lse)
+//   d logit_j = scale (g (1[j = t] - p_j) - h p_j (z_j - lse + H))        for upstream g = d logp, h = d H
+//
+// Conventions: logits of -inf are masked words (p = 0, no gradient).  A row in which every word is masked has
+// lse = -inf, logp = -inf, H = 0, no gradient.  A target outside [0, vocab) is ignored: logp = 0, g counts as 0.
+//
+// Forward: one pass.  A thread keeps the running maximum m of its elements, s = sum exp(z - m) and
+// u = sum exp(z - m) (z - m); a new maximum rescales both (u by the shift too).  Joined over the block, then over
+// the cluster of CTAs that share a row, H = log s - u / s: the difference of small numbers, not of lse and a mean.
+#include "../../include/apollo.h"
+
+#include <cooperative_groups.h>
+
+#include <cmath>
+
+#include "device_utils.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace apollo {
+
+namespace {
+
+constexpr int LP_THREADS = 256;
+constexpr int LP_MAX_TOP = APOLLO_MAX_TOP;
+constexpr int LP_CAND = 1024;        // candidates one CTA collects before it falls back to picking one by one
+constexpr float LOG2E = 1.4426950408889634f;
+
+template <typename T> struct LpVec;
+template <> struct LpVec<float> {
+    static constexpr int N = 4;
+    __device__ static __forceinline__ void unpack(const uint4& r, float (&v)[4])
+    {
+        v[0] = __uint_as_float(r.x); v[1] = __uint_as_float(r.y); v[2] = __uint_as_float(r.z); v[3] = __uint_as_float(r.w);
+    }
+    __device__ static __forceinline__ uint4 pack(const float (&v)[4])
+    {
+        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    }
+    __device__ static __forceinline__ void store1(float* p, float v) { *p = v; }
+};
+template <> struct LpVec<__nv_bfloat16> {
+    static constexpr int N = 8;
+    __device__ static __forceinline__ void unpack(const uint4& r, float (&v)[8]) { unpack_bf16x8(r, v); }
+    __device__ static __forceinline__ uint4 pack(const float (&v)[8])
+    {
+        return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+    }
+    __device__ static __forceinline__ void store1(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+};
+
+// 2^x on the special-function unit (relative error about 2^-22; results below the normal range become 0)
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Running softmax statistics: m = max z, s = sum exp(z - m), u = sum exp(z - m) (z - m).  The difference comes first,
+// the factor log2 e after it: masks of the type's lowest value are finite numbers, and z log2 e would overflow there.
+struct Stat { float m, s, u; };
+
+__device__ __forceinline__ Stat stat_empty() { return Stat{ -INFINITY, 0.0f, 0.0f }; }
+
+// Moves st to the maximum m >= st.m (m > -inf).
+__device__ __forceinline__ void stat_shift(Stat& st, float m)
+{
+    if (st.s != 0.0f) {                     // (a NaN s is != 0 and stays NaN)
+        const float d = st.m - m, f = ex2(d * LOG2E);
+        st.u = f * fmaf(fmaxf(d, -1e30f), st.s, st.u);     // f is 0 long before the bound matters
+        st.s *= f;
+    }
+    st.m = m;
+}
+
+__device__ __forceinline__ Stat stat_join(Stat a, Stat b)
+{
+    const float m = fmaxf(a.m, b.m);
+    if (m == -INFINITY) return Stat{ m, a.s + b.s, a.u + b.u };   // nothing on either side (or NaN sums)
+    stat_shift(a, m);
+    stat_shift(b, m);
+    return Stat{ m, a.s + b.s, a.u + b.u };
+}
+
+// Adds N values z.
+template <int N>
+__device__ __forceinline__ void stat_add(Stat& st, const float (&z)[N])
+{
+    float top = z[0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) top = fmaxf(top, z[e]);
+    if (top > st.m) stat_shift(st, top);
+    if (st.m == -INFINITY) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (z[e] != z[e]) st.s = NAN;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const float d = z[e] - st.m, p = ex2(d * LOG2E);
+        st.s += p;
+        st.u = fmaf(p, fmaxf(d, -1e30f), st.u);            // p is 0 where d is -inf: keep the product 0
+    }
+}
+
+// Order of the alternatives: larger value first, then the lower index.  As one 64-bit key: the value's bits made
+// monotone, then the complement of the index.  -0 counts as +0, NaN as the lowest value.  0 is "no entry".
+__device__ __forceinline__ uint64_t top_key(float v, uint32_t index)
+{
+    uint32_t b = __float_as_uint(v + 0.0f);
+    b = (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+    if (v != v) b = 1u;
+    return ((uint64_t)b << 32) | (uint64_t)(~index);
+}
+__device__ __forceinline__ float top_value(uint64_t key)
+{
+    const uint32_t b = (uint32_t)(key >> 32);
+    return __uint_as_float((b & 0x80000000u) ? (b & 0x7FFFFFFFu) : ~b);
+}
+
+__device__ __forceinline__ uint64_t warp_max(uint64_t k)
+{
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        const uint64_t o = __shfl_xor_sync(0xFFFFFFFFu, k, off);
+        if (o > k) k = o;
+    }
+    return k;
+}
+
+struct LogprobArgs {
+    const void* logits;
+    const void* targets;
+    int64_t stride, n_rows;
+    int vocab, index64, top;
+    float scale;
+    float* logprob;
+    float* entropy;
+    float* lse;
+    float* top_logprob;
+    int* top_index;
+};
+
+// The elements of [begin, end) of a row in 16-byte vectors: f1(index, value) for the few before the first 16-byte
+// boundary and after the last, fv(index of the first, values) for whole vectors, four loads in flight.
+template <typename T, int THREADS, class F1, class FV>
+__device__ __forceinline__ void for_row(const T* __restrict__ row, int begin, int end, F1&& f1, FV&& fv)
+{
+    constexpr int V = LpVec<T>::N;
+    const int mis = (int)(((uintptr_t)(row + begin) % 16) / sizeof(T));
+    int head = mis ? V - mis : 0;
+    if (head > end - begin) head = end - begin;
+    const int vecs = (end - begin - head) / V;
+    const int v0 = begin + head, tail0 = v0 + vecs * V;
+    const int tid = threadIdx.x;
+    if (tid < head) f1(begin + tid, load1(row + begin + tid));
+    if (tid < end - tail0) f1(tail0 + tid, load1(row + tail0 + tid));
+    const uint4* p = reinterpret_cast<const uint4*>(row + v0);
+    int u = tid;
+    for (; u + 3 * THREADS < vecs; u += 4 * THREADS) {
+        uint4 raw[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) raw[k] = __ldg(p + u + k * THREADS);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float v[V];
+            LpVec<T>::unpack(raw[k], v);
+            fv(v0 + (u + k * THREADS) * V, v);
+        }
+    }
+    for (; u < vecs; u += THREADS) {
+        float v[V];
+        LpVec<T>::unpack(__ldg(p + u), v);
+        fv(v0 + u * V, v);
+    }
+}
+
+// A cluster of gridDim.x / n_rows CTAs per row (1, 2, 4 or 8); each takes a contiguous part of the vocabulary.
+// TOP: also the `top` best words.  In the pass a thread remembers the best key of its elements; the top-th
+// largest of the threads' keys is a lower bound of the top-th largest of all, so a second look at the part (it
+// has just been read: L2 at most) collects the few words at or above that bound, and ranking them by counting
+// gives the list.  Should more than LP_CAND words pass (a part sorted against the stride), they are picked one by
+// one instead: slow, and right.
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(LP_THREADS)
+logprob_kernel(LogprobArgs a)
+{
+    constexpr int V = LpVec<T>::N;
+    __shared__ Stat part;                             // this CTA's statistics, read by rank 0 of the cluster
+    __shared__ Stat warp_stat[LP_THREADS / 32];
+    __shared__ uint64_t keys[TOP ? LP_THREADS : 1];
+    __shared__ uint64_t cand[TOP ? LP_CAND : 1];
+    __shared__ uint64_t best[TOP ? LP_MAX_TOP : 1];   // this CTA's list, read by rank 0 of the cluster
+    __shared__ uint64_t bound;
+    __shared__ int n_cand;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int parts = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int64_t r = blockIdx.x / parts;
+    const T* row = static_cast<const T*>(a.logits) + r * a.stride;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    int per = ((a.vocab + parts - 1) / parts + V - 1) / V * V;
+    const int begin = min(rank * per, a.vocab), end = min(begin + per, a.vocab);
+
+    Stat st = stat_empty();
+    uint64_t mine = 0;
+    float mine_v = -INFINITY;
+    bool any = false;
+    const float scale = a.scale;
+    auto one = [&](int i, float v) {
+        const float z[1] = { v * scale };
+        stat_add(st, z);
+        if constexpr (TOP) {
+            const uint64_t k = top_key(z[0], (uint32_t)i);
+            if (k > mine) { mine = k; mine_v = z[0]; any = true; }
+        }
+    };
+    for_row<T, LP_THREADS>(row, begin, end, one, [&](int i, const float (&v)[V]) {
+        float z[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) z[e] = v[e] * scale;
+        stat_add(st, z);
+        if constexpr (TOP) {
+            float top = z[0];
+#pragma unroll
+            for (int e = 1; e < V; ++e) top = fmaxf(top, z[e]);
+            if (!any || !(top < mine_v)) {            // ties are settled by the index, which is in the key
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const uint64_t k = top_key(z[e], (uint32_t)(i + e));
+                    if (k > mine) { mine = k; mine_v = z[e]; }
+                }
+                any = true;
+            }
+        }
+    });
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        Stat o;
+        o.m = __shfl_xor_sync(0xFFFFFFFFu, st.m, off);
+        o.s = __shfl_xor_sync(0xFFFFFFFFu, st.s, off);
+        o.u = __shfl_xor_sync(0xFFFFFFFFu, st.u, off);
+        st = stat_join(st, o);
+    }
+    if (lane == 0) warp_stat[warp] = st;
+    if constexpr (TOP) {
+        keys[tid] = mine;
+        if (tid == 0) { n_cand = 0; bound = 0; }
+        if (tid < LP_MAX_TOP) best[tid] = 0;
+    }
+    __syncthreads();
+    if (tid == 0) {
+        Stat all = warp_stat[0];
+        for (int w = 1; w < LP_THREADS / 32; ++w) all = stat_join(all, warp_stat[w]);
+        part = all;
+    }
+    if constexpr (TOP) {
+        // the top-th largest of the threads' keys (0 where fewer threads have one: then everything passes)
+        int above = 0;
+        for (int k = 0; k < LP_THREADS; ++k) above += keys[k] > mine ? 1 : 0;
+        if (mine != 0 && above == a.top - 1) bound = mine;
+        __syncthreads();
+        const uint64_t lim = bound;
+        const float lim_v = lim ? top_value(lim) : -INFINITY;
+        auto pick = [&](int i, float z) {
+            if (lim != 0 && z < lim_v) return;
+            const uint64_t k = top_key(z, (uint32_t)i);
+            if (k < lim) return;
+            const int at = atomicAdd(&n_cand, 1);
+            if (at < LP_CAND) cand[at] = k;
+        };
+        for_row<T, LP_THREADS>(row, begin, end, [&](int i, float v) { pick(i, v * scale); }, [&](int i, const float (&v)[V]) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) pick(i + e, v[e] * scale);
+        });
+        __syncthreads();
+        const int n = n_cand;
+        if (n <= LP_CAND) {
+            for (int c = tid; c < n; c += LP_THREADS) {
+                const uint64_t k = cand[c];
+                int ahead = 0;
+                for (int o = 0; o < n; ++o) ahead += cand[o] > k ? 1 : 0;
+                if (ahead < a.top) best[ahead] = k;
+            }
+        } else {
+            uint64_t last = ~0ull;
+            for (int t = 0; t < a.top; ++t) {
+                uint64_t b = 0;
+                auto next = [&](int i, float z) {
+                    const uint64_t k = top_key(z, (uint32_t)i);
+                    if (k < last && k > b) b = k;
+                };
+                for_row<T, LP_THREADS>(row, begin, end, [&](int i, float v) { next(i, v * scale); }, [&](int i, const float (&v)[V]) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) next(i + e, v[e] * scale);
+                });
+                b = warp_max(b);
+                __syncthreads();
+                if (lane == 0) keys[warp] = b;
+                __syncthreads();
+                for (int w = 0; w < LP_THREADS / 32; ++w) b = keys[w] > b ? keys[w] : b;
+                if (tid == 0) best[t] = b;
+                last = b;
+            }
+        }
+    }
+    if (parts > 1) cluster.sync(); else __syncthreads();
+    if (rank == 0) {
+        Stat all = stat_empty();
+        for (int c = 0; c < parts; ++c) all = stat_join(all, *cluster.map_shared_rank(&part, c));
+        const bool dead = all.m == -INFINITY && all.s == 0.0f;
+        const float log_s = dead ? 0.0f : logf(all.s);
+        const float lse = dead ? -INFINITY : all.m + log_s;
+        if (tid == 0) {
+            const long long t = a.index64 ? static_cast<const long long*>(a.targets)[r] : (long long)static_cast<const int*>(a.targets)[r];
+            const bool live = t >= 0 && t < a.vocab;
+            a.lse[r] = lse;
+            a.entropy[r] = dead ? 0.0f : log_s - all.u / all.s;
+            a.logprob[r] = !live ? 0.0f : dead ? -INFINITY : __fmul_rn(load1(row + t), scale) - lse;
+        }
+        if constexpr (TOP) {
+            // keys are distinct: an entry's place in the joined list is the number of larger ones
+            const int n = parts * a.top;              // at most 8 x 32
+            for (int c = tid; c < n; c += LP_THREADS) cand[c] = cluster.map_shared_rank(best, c / a.top)[c % a.top];
+            __syncthreads();
+            for (int c = tid; c < n; c += LP_THREADS) {
+                const uint64_t k = cand[c];
+                int ahead = 0;
+                for (int o = 0; o < n; ++o) ahead += cand[o] > k ? 1 : 0;
+                if (k != 0 && ahead < a.top) {
+                    const float z = (uint32_t)(k >> 32) == 1u ? NAN : top_value(k);
+                    a.top_index[r * a.top + ahead] = (int)~(uint32_t)k;
+                    a.top_logprob[r * a.top + ahead] = dead ? -INFINITY : z - lse;
+                }
+            }
+        }
+    }
+    if (parts > 1) cluster.sync();                     // the other CTAs' shared memory has been read
+}
+
+struct LogprobGradArgs {
+    const void* logits;
+    const void* targets;
+    int64_t stride, out_stride, n_rows;
+    int vocab, index64;
+    float scale;
+    const float* lse;
+    const float* entropy;
+    const float* d_logprob;
+    const float* d_entropy;      // may be null
+    void* out;
+};
+
+// One block per row and column chunk; reads the logits and writes their gradient, 2 e bytes an element: HBM-bound.
+// VECTOR: logits and gradient rows start on 16-byte boundaries.  In place works: a thread writes what it has read.
+template <typename T, bool VECTOR>
+__global__ void __launch_bounds__(LP_THREADS)
+logprob_grad_kernel(LogprobGradArgs a)
+{
+    constexpr int V = VECTOR ? LpVec<T>::N : 1;
+    const int64_t r = blockIdx.x;
+    const T* row = static_cast<const T*>(a.logits) + r * a.stride;
+    T* out = static_cast<T*>(a.out) + r * a.out_stride;
+    const long long t = a.index64 ? static_cast<const long long*>(a.targets)[r] : (long long)static_cast<const int*>(a.targets)[r];
+    const bool live = t >= 0 && t < a.vocab;
+    const float lse = a.lse[r], scale = a.scale;
+    const float g = live ? a.d_logprob[r] : 0.0f, h = a.d_entropy ? a.d_entropy[r] : 0.0f;
+    const bool dead = lse == -INFINITY;
+    const float ent = a.entropy ? a.entropy[r] : 0.0f;
+    const int at = live && !dead ? (int)t : -1;
+    // -scale p (g + h (z - lse + H)) = p (k0 + k1 (z - lse))
+    const float k1 = -scale * h, k0 = -scale * fmaf(h, ent, g), gs = scale * g;
+    auto value = [&](float v, int i) {
+        const float d = __fmul_rn(v, scale) - lse;              // the z of the forward pass, rounded the same way
+        const float p = ex2(d * LOG2E);
+        float x = p == 0.0f || dead ? 0.0f : p * fmaf(k1, d, k0);
+        if (i == at) x += gs;
+        return x;
+    };
+    const int units = a.vocab / V;
+    const int step = (int)gridDim.y * LP_THREADS;
+    for (int u0 = (int)blockIdx.y * LP_THREADS + threadIdx.x; u0 < units; u0 += 4 * step) {
+        if constexpr (VECTOR) {
+            uint4 raw[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (u0 + k * step < units) raw[k] = __ldcs(reinterpret_cast<const uint4*>(row) + u0 + k * step);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int u = u0 + k * step;
+                if (u >= units) break;
+                float v[V];
+                LpVec<T>::unpack(raw[k], v);
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] = value(v[e], u * V + e);
+                __stcs(reinterpret_cast<uint4*>(out) + u, LpVec<T>::pack(v));
+            }
+        } else {
+            float v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = u0 + k * step < units ? load1(row + u0 + k * step) : 0.0f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (u0 + k * step < units) LpVec<T>::store1(out + u0 + k * step, value(v[k], u0 + k * step));
+        }
+    }
+    if constexpr (VECTOR) {
+        const int i = units * V + (int)threadIdx.x;
+        if (blockIdx.y == 0 && i < a.vocab) LpVec<T>::store1(out + i, value(load1(row + i), i));
+    }
+}
+
+int check_rows(int64_t n_rows, int64_t vocab, int64_t stride, int32_t dtype, int32_t index_type, float scale)
+{
+    if (dtype != APOLLO_DT_F32 && dtype != APOLLO_DT_BF16) return APOLLO_ERR_INVALID_ARG;
+    if (index_type != APOLLO_INDEX_I32 && index_type != APOLLO_INDEX_I64) return APOLLO_ERR_INVALID_ARG;
+    if (!std::isfinite(scale) || scale <= 0.0f) return APOLLO_ERR_INVALID_ARG;
+    if (n_rows < 0 || vocab < 1 || n_rows > INT32_MAX / 8 || vocab > (int64_t)1 << 30 || stride < vocab) return APOLLO_ERR_SHAPE;
+    return APOLLO_OK;
+}
+
+template <typename T>
+cudaError_t run_logprob(const LogprobArgs& a, int sms, cudaStream_t stream)
+{
+    // A row is shared by as many CTAs as keep the chip busy: up to 8 while there are fewer CTAs than SMs and every
+    // CTA still has a few vectors per thread.
+    int parts = 1;
+    while (parts < 8 && a.n_rows * parts * 2 <= sms && a.vocab / (parts * 2) >= 2 * LP_THREADS) parts *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.n_rows * parts));
+    cfg.blockDim = dim3(LP_THREADS);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)parts; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return a.top > 0 ? cudaLaunchKernelEx(&cfg, logprob_kernel<T, true>, a) : cudaLaunchKernelEx(&cfg, logprob_kernel<T, false>, a);
+}
+
+template <typename T>
+void run_logprob_grad(const LogprobGradArgs& a, cudaStream_t stream)
+{
+    const bool vector = (uintptr_t)a.logits % 16 == 0 && (uintptr_t)a.out % 16 == 0 &&
+                        (size_t)a.stride * sizeof(T) % 16 == 0 && (size_t)a.out_stride * sizeof(T) % 16 == 0;
+    const int units = vector ? a.vocab / LpVec<T>::N : a.vocab;
+    int chunks = (units + 4 * LP_THREADS - 1) / (4 * LP_THREADS);
+    if (chunks < 1) chunks = 1;
+    if (chunks > 65535) chunks = 65535;
+    const dim3 grid((unsigned)a.n_rows, (unsigned)chunks);
+    if (vector) logprob_grad_kernel<T, true><<<grid, LP_THREADS, 0, stream>>>(a);
+    else logprob_grad_kernel<T, false><<<grid, LP_THREADS, 0, stream>>>(a);
+}
+
+}  // namespace
+
+}  // namespace apollo
+
+using namespace apollo;
+
+extern "C" int apollo_token_logprobs(const void* d_logits, int64_t row_stride, int64_t n_rows, int64_t vocab, int32_t dtype,
+                                     const void* d_targets, int32_t index_type, float scale, int32_t top, float* d_logprob,
+                                     float* d_entropy, float* d_lse, float* d_top_logprob, int32_t* d_top_index, void* cuda_stream)
+{
+    const int rc = check_rows(n_rows, vocab, row_stride, dtype, index_type, scale);
+    if (rc != APOLLO_OK) return rc;
+    if (top < 0 || top > APOLLO_MAX_TOP || top > vocab) return APOLLO_ERR_INVALID_ARG;
+    if (n_rows == 0) return APOLLO_OK;
+    if (!d_logits || !d_targets || !d_logprob || !d_entropy || !d_lse || (top > 0 && (!d_top_logprob || !d_top_index))) return APOLLO_ERR_INVALID_ARG;
+    const size_t e = dtype == APOLLO_DT_BF16 ? 2 : 4, ie = index_type == APOLLO_INDEX_I64 ? 8 : 4;
+    if ((uintptr_t)d_logits % e || (uintptr_t)d_targets % ie || (uintptr_t)d_logprob % 4 || (uintptr_t)d_entropy % 4 || (uintptr_t)d_lse % 4 ||
+        (uintptr_t)d_top_logprob % 4 || (uintptr_t)d_top_index % 4)
+        return APOLLO_ERR_ALIGN;
+    int device = 0, sms = 0;
+    if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) {
+        cudaGetLastError();
+        return APOLLO_ERR_CUDA;
+    }
+    LogprobArgs a;
+    a.logits = d_logits; a.targets = d_targets; a.stride = row_stride; a.n_rows = n_rows; a.vocab = (int)vocab;
+    a.index64 = index_type == APOLLO_INDEX_I64; a.top = top; a.scale = scale;
+    a.logprob = d_logprob; a.entropy = d_entropy; a.lse = d_lse; a.top_logprob = d_top_logprob; a.top_index = d_top_index;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const cudaError_t err = dtype == APOLLO_DT_BF16 ? run_logprob<__nv_bfloat16>(a, sms, stream) : run_logprob<float>(a, sms, stream);
+    if (err != cudaSuccess) { cudaGetLastError(); return APOLLO_ERR_CUDA; }
+    return APOLLO_OK;
+}
+
+extern "C" int apollo_token_logprobs_grad(const void* d_logits, int64_t row_stride, int64_t n_rows, int64_t vocab, int32_t dtype,
+                                          const void* d_targets, int32_t index_type, float scale, const float* d_lse,
+                                          const float* d_entropy, const float* d_grad_logprob, const float* d_grad_entropy,
+                                          void* d_grad_logits, int64_t grad_stride, void* cuda_stream)
+{
+    int rc = check_rows(n_rows, vocab, row_stride, dtype, index_type, scale);
+    if (rc != APOLLO_OK) return rc;
+    if (grad_stride < vocab) return APOLLO_ERR_SHAPE;
+    if (n_rows == 0) return APOLLO_OK;
+    if (!d_logits || !d_targets || !d_lse || !d_grad_logprob || !d_grad_logits || (d_grad_entropy && !d_entropy)) return APOLLO_ERR_INVALID_ARG;
+    if (d_grad_logits == d_logits && grad_stride != row_stride) return APOLLO_ERR_INVALID_ARG;
+    const size_t e = dtype == APOLLO_DT_BF16 ? 2 : 4, ie = index_type == APOLLO_INDEX_I64 ? 8 : 4;
+    if ((uintptr_t)d_logits % e || (uintptr_t)d_grad_logits % e || (uintptr_t)d_targets % ie || (uintptr_t)d_lse % 4 || (uintptr_t)d_entropy % 4 ||
+        (uintptr_t)d_grad_logprob % 4 || (uintptr_t)d_grad_entropy % 4)
+        return APOLLO_ERR_ALIGN;
+    LogprobGradArgs a;
+    a.logits = d_logits; a.targets = d_targets; a.stride = row_stride; a.out_stride = grad_stride; a.n_rows = n_rows; a.vocab = (int)vocab;
+    a.index64 = index_type == APOLLO_INDEX_I64; a.scale = scale; a.lse = d_lse; a.entropy = d_grad_entropy ? d_entropy : nullptr;
+    a.d_logprob = d_grad_logprob; a.d_entropy = d_grad_entropy; a.out = d_grad_logits;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (dtype == APOLLO_DT_BF16) run_logprob_grad<__nv_bfloat16>(a, stream);
+    else run_logprob_grad<float>(a, stream);
+    return cudaGetLastError() == cudaSuccess ? APOLLO_OK : APOLLO_ERR_CUDA;
+}

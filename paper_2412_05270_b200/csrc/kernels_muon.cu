@@ -1,0 +1,651 @@
+// Kernels of the orthogonalised update (Newton-Schulz products).
+//
+// muon_gemm_kernel  every product of an iteration, on CTA pairs: tcgen05.mma cta_group::2 fed by TMA, two 256-column
+//                   accumulators in TMEM, so that the epilogue of a tile runs under the main loop of the next
+// muon_moment / muon_load / muon_apply   the streaming passes before and after
+//
+// A product's tile is 256 x 256: each CTA of a pair loads its 128 rows of L and half of the 256 columns of R, 32 KB
+// per 64-deep k-block, five stages; four MMAs of 256 x 256 x 16 consume them.  Roles of the 12 warps: 0 TMA producer,
+// 1 MMA issuer (leader CTA) and TMEM owner, 4-11 epilogue (a warp reads the 32 TMEM lanes it may read and one half
+// of the columns).  The epilogue adds the terms that the iteration needs beside the product, rounds to 16 bits and
+// hands 32 x 64 pieces to TMA stores; a symmetric product's tile above the diagonal is stored a second time,
+// transposed, so that half of the symmetric products is never computed.
+// Bound: the tensor pipe (and with it the board's power).
+//
+// Every mbarrier wait is bounded, as in the projection kernels: a wait that gives up sets the status word, the roles
+// leave the tile loop, what is in flight is drained, TMEM is freed.
+#include "muon.h"
+
+#include "../../include/apollo.h"
+#include "device_utils.cuh"
+#include "tc_common.cuh"
+#include "tc_ptx.cuh"
+
+namespace apollo {
+
+namespace {
+
+constexpr int MG_THREADS = 384;
+constexpr int MG_STAGES = 5;
+constexpr int MG_HALF = 8192;                            // 64 x 64 16-bit floats: one TMA box
+constexpr int MG_OPERAND = 2 * MG_HALF;                  // a CTA's 128 rows of L, or half of R
+constexpr int MG_STAGE = 2 * MG_OPERAND;
+constexpr int MG_EPI_WARPS = 8;
+constexpr int MG_STAGING = MG_EPI_WARPS * 8192;          // per epilogue warp: 4 KB as stored, 4 KB transposed
+constexpr int MG_SMEM = MG_STAGES * MG_STAGE + MG_STAGING + 256 + 1024;
+static_assert(MG_SMEM <= 227 * 1024, "shared memory of a CTA");
+
+__device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void st_shared_u16(uint32_t addr, uint16_t v)
+{
+    asm volatile("st.shared.b16 [%0], %1;" ::"r"(addr), "h"(v) : "memory");
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi)
+{
+    const __half2 p = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&p);
+}
+__device__ __forceinline__ float2 unpack_half2(uint32_t w)
+{
+    return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+
+// v += b * (32 values at p): 64 contiguous bytes of one row
+__device__ __forceinline__ void add_term(float (&v)[32], float b, const uint4 (&e)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w[4] = { e[i].x, e[i].y, e[i].z, e[i].w };
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 f = unpack_half2(w[k]);
+            v[8 * i + 2 * k] = fmaf(b, f.x, v[8 * i + 2 * k]);
+            v[8 * i + 2 * k + 1] = fmaf(b, f.y, v[8 * i + 2 * k + 1]);
+        }
+    }
+}
+__device__ __forceinline__ void load_term(uint4 (&e)[4], const __half* p, bool in)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e[i] = in ? *(reinterpret_cast<const uint4*>(p) + i) : make_uint4(0, 0, 0, 0);
+}
+
+}  // namespace
+
+// SPLIT: operands are sums of two 16-bit floats, and the contraction runs over three segments into one accumulator:
+// hi hi + lo hi + hi lo (what is dropped, lo lo, is 2^-24 of a term).
+template <bool SPLIT>
+__global__ void __launch_bounds__(MG_THREADS, 1)
+muon_gemm_kernel(const GemmOp* __restrict__ ops, const int* __restrict__ prefix, int n_ops, int tiles, int32_t* __restrict__ status)
+{
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem_base = (ptx::smem_addr(smem_raw) + 1023u) & ~1023u;
+    uint8_t* smem_gen = smem_raw + (smem_base - ptx::smem_addr(smem_raw));
+    const uint32_t staging = smem_base + MG_STAGES * MG_STAGE;
+    const uint32_t bars = staging + MG_STAGING;
+    const uint32_t bar_full = bars, bar_done = bars + 64, bar_acc_full = bars + 128, bar_acc_empty = bars + 144, bar_drain = bars + 160;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + MG_STAGES * MG_STAGE + MG_STAGING + 176);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + MG_STAGES * MG_STAGE + MG_STAGING + 180);
+
+    const uint32_t rank = ptx::cluster_ctarank();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int s = 0; s < MG_STAGES; ++s) {
+            ptx::mbar_init(bar_full + 8 * s, 1);         // the leader's arrive.expect_tx for the bytes of both CTAs
+            ptx::mbar_init(bar_done + 8 * s, 1);         // the leader's commit
+        }
+        for (int b = 0; b < 2; ++b) {
+            ptx::mbar_init(bar_acc_full + 8 * b, 1);
+            ptx::mbar_init(bar_acc_empty + 8 * b, 2 * MG_EPI_WARPS);
+        }
+        ptx::mbar_init(bar_drain, 1);
+        *abort_flag = 0;
+        ptx::fence_mbar_init();
+    }
+    if (warp == 1) {
+        ptx::tmem_alloc_pair(ptx::smem_addr(tmem_slot), 512);
+        ptx::tmem_relinquish_pair();
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::cluster_sync();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem_base = *tmem_slot;
+    // everything above may run while the launch before this one is still at work; its results are read below
+    ptx::grid_launch_dependents();
+    ptx::grid_wait_previous();
+
+    uint32_t it = 0, tile_iter = 0, stage = 0, phase = 0;
+    auto next_stage = [&]() { ++it; if (++stage == (uint32_t)MG_STAGES) { stage = 0; phase ^= 1; } };
+
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    int op_at = 0, fenced = -1;
+    for (int tile = pair; tile < tiles; tile += pairs, ++tile_iter) {
+        while (op_at + 1 < n_ops && __ldg(prefix + op_at + 1) <= tile) ++op_at;
+        const GemmOp* op = ops + op_at;
+        const int local = tile - __ldg(prefix + op_at);
+        const int tiles_m = __ldg(&op->tiles_m);
+        const bool sym = __ldg(&op->sym) != 0;
+        int tm, tn;
+        if (sym) {
+            // upper triangle, column by column: column tn holds the tiles (0 .. tn, tn)
+            tn = (int)((sqrtf(8.0f * (float)local + 1.0f) - 1.0f) * 0.5f);
+            while ((tn + 1) * (tn + 2) / 2 <= local) ++tn;
+            while (tn * (tn + 1) / 2 > local) --tn;
+            tm = local - tn * (tn + 1) / 2;
+        } else {
+            tn = local / tiles_m;
+            tm = local - tn * tiles_m;
+        }
+        const int K = __ldg(&op->K);
+        const int nkb = (K + 63) / 64;
+        const int num_kb = SPLIT ? 3 * nkb : nkb;
+        const bool r_mn = __ldg(&op->r_mn) != 0;
+        const uint32_t buf = tile_iter & 1, use = tile_iter >> 1;
+
+        if (warp == 0) {
+            // ---------------- TMA producer (one thread in each CTA) ----------------
+            if (lane == 0) {
+                if (fenced != op_at) {
+                    for (int h = 0; h < (SPLIT ? 2 : 1); ++h) {
+                        ptx::fence_tensormap_acquire(op->l_map[h]);
+                        ptx::fence_tensormap_acquire(op->r_map[h]);
+                    }
+                    fenced = op_at;
+                }
+                const void* l_hi = op->l_map[0];
+                const void* r_hi = op->r_map[0];
+                const void* l_lo = SPLIT ? op->l_map[1] : nullptr;
+                const void* r_lo = SPLIT ? op->r_map[1] : nullptr;
+                const uint64_t pol = ptx::policy_evict_normal();
+                const uint32_t full0 = ptx::map_to_cta(bar_full, 0);
+                const int m0 = tm * MUON_TILE + (int)rank * 128, n0 = tn * MUON_TILE + (int)rank * 128;
+                int k = 0, seg = 0;
+                for (int kb = 0; kb < num_kb; ++kb, next_stage()) {
+                    const uint32_t s = stage;
+                    if (!wait_phase(bar_done + 8 * s, phase ^ 1, abort_flag, status, 201)) break;
+                    const uint32_t dst = smem_base + s * MG_STAGE, full = full0 + 8 * s;
+                    if (rank == 0) ptx::mbar_arrive_expect_tx(bar_full + 8 * s, 2u * MG_STAGE);
+                    const void* lm = SPLIT && seg == 1 ? l_lo : l_hi;
+                    const void* rm = SPLIT && seg == 2 ? r_lo : r_hi;
+                    ptx::tma_load_2d_pair(dst, lm, k, m0, full, pol);
+                    ptx::tma_load_2d_pair(dst + MG_HALF, lm, k, m0 + 64, full, pol);
+                    if (r_mn) {
+                        ptx::tma_load_2d_pair(dst + MG_OPERAND, rm, n0, k, full, pol);
+                        ptx::tma_load_2d_pair(dst + MG_OPERAND + MG_HALF, rm, n0 + 64, k, full, pol);
+                    } else {
+                        ptx::tma_load_2d_pair(dst + MG_OPERAND, rm, k, n0, full, pol);
+                        ptx::tma_load_2d_pair(dst + MG_OPERAND + MG_HALF, rm, k, n0 + 64, full, pol);
+                    }
+                    k += 64;
+                    if (SPLIT && k >= nkb * 64) { k = 0; ++seg; }
+                }
+            }
+            __syncwarp();
+            if (__shfl_sync(0xFFFFFFFFu, *abort_flag, 0) != 0) break;
+        } else if (warp == 1) {
+            // ---------------- MMA issuer (leader only) ----------------
+            if (lane == 0 && rank == 0) {
+                const uint32_t idesc = ptx::instr_desc_f16_pair(MUON_TILE, r_mn);
+                const uint32_t d_tmem = tmem_base + buf * MUON_TILE;
+                bool ok = wait_phase(bar_acc_empty + 8 * buf, (use & 1) ^ 1, abort_flag, status, 202);
+                ptx::tc_fence_after_sync();
+                // K-major operand: 64 k = 128 bytes a row, 8-row groups 1024 bytes apart, 16 k = 32 bytes on.
+                // n-contiguous R: 64 n = 128 bytes a k-row, 16 k-rows = 2048 bytes on, the next 64 n one box further.
+                const uint64_t a_desc0 = ptx::smem_desc_sw128(smem_base, 16, 1024);
+                const uint64_t b_desc0 = r_mn ? ptx::smem_desc_sw128(smem_base + MG_OPERAND, MG_HALF, 1024)
+                                              : ptx::smem_desc_sw128(smem_base + MG_OPERAND, 16, 1024);
+                const uint32_t b_step = r_mn ? 2048u >> 4 : 32u >> 4;
+                int kb = 0;
+                for (; ok && kb < num_kb; ++kb, next_stage()) {
+                    const uint32_t s = stage;
+                    if (!wait_phase(bar_full + 8 * s, phase, abort_flag, status, 203)) break;
+                    ptx::tc_fence_after_sync();
+                    const uint64_t a_desc = a_desc0 + s * (MG_STAGE >> 4), b_desc = b_desc0 + s * (MG_STAGE >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk)
+                        ptx::mma_bf16_pair(d_tmem, a_desc + kk * 2, b_desc + kk * b_step, idesc, (kb | kk) != 0 ? 1u : 0u);
+                    ptx::mma_commit_pair(bar_done + 8 * s, 3);
+                }
+                if (ok && kb == num_kb) ptx::mma_commit_pair(bar_acc_full + 8 * buf, 3);
+            }
+            __syncwarp();
+            if (__shfl_sync(0xFFFFFFFFu, *abort_flag, 0) != 0) break;
+        } else if (warp >= 4) {
+            // ---------------- epilogue ----------------
+            const int q = warp & 3, half = (warp - 4) >> 2;
+            const int M = __ldg(&op->M), N = __ldg(&op->N), e_pitch = __ldg(&op->e_pitch);
+            const int row0 = tm * MUON_TILE + (int)rank * 128 + q * 32, row = row0 + lane;
+            const bool mirror = sym && tm != tn;
+            const float alpha = __ldg(&op->alpha), b1 = __ldg(&op->b1), b2 = __ldg(&op->b2), diag = __ldg(&op->diag);
+            const __half* e1 = op->e1[0];
+            const __half* e2 = op->e2[0];
+            const uint32_t mine = staging + (uint32_t)(warp - 4) * 8192u, mine_t = mine + 4096u;
+            if (lane == 0 && fenced != op_at) {
+                for (int h = 0; h < (SPLIT ? 2 : 1); ++h) {
+                    ptx::fence_tensormap_acquire(op->out_map[h]);
+                    if (sym) ptx::fence_tensormap_acquire(op->mir_map[h]);
+                }
+                fenced = op_at;
+            }
+            const bool acc_ok = __all_sync(0xFFFFFFFFu, wait_phase_idle(bar_acc_full + 8 * buf, use & 1, abort_flag, status, 204));
+            ptx::tc_fence_after_sync();
+            if (acc_ok && row0 < M) {
+#pragma unroll 1
+                for (int ch = 0; ch < 2; ++ch) {
+                    const int col0 = tn * MUON_TILE + half * 128 + ch * 64;
+                    if (col0 >= N) break;
+                    uint32_t lo_bits[SPLIT ? 32 : 1];
+                    if (lane == 0) ptx::bulk_wait_read();            // the stores of the last piece have read the staging
+                    __syncwarp();
+#pragma unroll
+                    for (int sub = 0; sub < 2; ++sub) {
+                        const int col = col0 + sub * 32;
+                        const int64_t at = (int64_t)row * e_pitch + col;
+                        const bool in = row < M;
+                        uint4 t1[4], t2[4], t1l[SPLIT ? 4 : 1], t2l[SPLIT ? 4 : 1];
+                        if (e1) load_term(t1, e1 + at, in);
+                        if (e2) load_term(t2, e2 + at, in);
+                        if constexpr (SPLIT) {
+                            if (e1) load_term(t1l, op->e1[1] + at, in);
+                            if (e2) load_term(t2l, op->e2[1] + at, in);
+                        }
+                        float v[32];
+                        ptx::tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + buf * MUON_TILE + (uint32_t)(half * 128 + ch * 64 + sub * 32), v);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] *= alpha;
+                        if (e1) add_term(v, b1, t1);
+                        if (e2) add_term(v, b2, t2);
+                        if constexpr (SPLIT) {
+                            if (e1) add_term(v, b1, t1l);
+                            if (e2) add_term(v, b2, t2l);
+                        }
+                        if (sym && diag != 0.0f && row >= col && row < col + 32) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) v[i] += row == col + i ? diag : 0.0f;
+                        }
+                        uint32_t w[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) w[i] = pack_half2(v[2 * i], v[2 * i + 1]);
+                        if constexpr (SPLIT) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const float2 f = unpack_half2(w[i]);
+                                lo_bits[sub * 16 + i] = pack_half2(v[2 * i] - f.x, v[2 * i + 1] - f.y);
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            st_shared_v4(mine + (uint32_t)(lane * 128 + (((sub * 4 + i) ^ (lane & 7)) << 4)), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                        if (mirror) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                st_shared_u16(mine_t + (uint32_t)(((sub * 32 + 2 * i) * 32 + lane) * 2), (uint16_t)(w[i] & 0xFFFFu));
+                                st_shared_u16(mine_t + (uint32_t)(((sub * 32 + 2 * i + 1) * 32 + lane) * 2), (uint16_t)(w[i] >> 16));
+                            }
+                        }
+                    }
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        ptx::tma_store_2d(op->out_map[0], col0, row0, mine);
+                        if (mirror) ptx::tma_store_2d(op->mir_map[0], row0, col0, mine_t);
+                        ptx::bulk_commit();
+                    }
+                    if constexpr (SPLIT) {
+                        if (lane == 0) ptx::bulk_wait_read();
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            st_shared_v4(mine + (uint32_t)(lane * 128 + ((i ^ (lane & 7)) << 4)), lo_bits[4 * i], lo_bits[4 * i + 1], lo_bits[4 * i + 2], lo_bits[4 * i + 3]);
+                        if (mirror) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                st_shared_u16(mine_t + (uint32_t)(((2 * i) * 32 + lane) * 2), (uint16_t)(lo_bits[i] & 0xFFFFu));
+                                st_shared_u16(mine_t + (uint32_t)(((2 * i + 1) * 32 + lane) * 2), (uint16_t)(lo_bits[i] >> 16));
+                            }
+                        }
+                        ptx::fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            ptx::tma_store_2d(op->out_map[1], col0, row0, mine);
+                            if (mirror) ptx::tma_store_2d(op->mir_map[1], row0, col0, mine_t);
+                            ptx::bulk_commit();
+                        }
+                    }
+                }
+            }
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0 && acc_ok) ptx::mbar_arrive_remote(ptx::map_to_cta(bar_acc_empty + 8 * buf, 0));
+            if (__shfl_sync(0xFFFFFFFFu, *abort_flag, 0) != 0) break;
+        } else if (__shfl_sync(0xFFFFFFFFu, *abort_flag, 0) != 0) {
+            break;
+        }
+    }
+
+    if (warp >= 4 && lane == 0) ptx::bulk_wait_all();
+    // The leader lets the loads of both CTAs and its MMAs finish before either CTA gives up shared memory or TMEM.
+    if (tid == 0 && rank == 0) {
+        for (uint32_t s = 0; s < (uint32_t)MG_STAGES && s < it; ++s) {
+            const uint32_t last = s + (it - 1 - s) / MG_STAGES * MG_STAGES;
+            drain_phase(bar_full + 8 * s, (last / MG_STAGES) & 1);
+        }
+    }
+    if (rank == 0 && tid == 32) {
+        ptx::mma_commit_pair(bar_drain, 1);
+        drain_phase(bar_drain, 0);
+    }
+    // the peer cannot watch the leader's barriers: after a wait gave up it lets its last loads land for 2 ms
+    if (rank == 1 && tid == 0 && *abort_flag)
+        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::cluster_sync();
+    if (warp == 1) ptx::tmem_dealloc_pair(tmem_base, 512);
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// Streaming passes.  Elements of U: with `STEP` from the momentum (already updated) and the gradient, else U itself.
+namespace {
+
+constexpr int MS_THREADS = 256;
+constexpr int MS_ROWS = 64, MS_COLS = 64;               // tile of the load and apply kernels
+
+__device__ __forceinline__ int find_item(const MuonArgs& a, int tile)
+{
+    int lo = 0, hi = a.n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (a.tile_begin[mid] <= tile) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+template <bool STEP>
+__device__ __forceinline__ float update_of(float g, float m, const MuonArgs& a)
+{
+    if constexpr (!STEP) return g;
+    return a.nesterov ? fmaf(a.mu, m, (1.0f - a.mu) * g) : m;
+}
+
+__device__ __forceinline__ void store_elem(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_elem(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+}  // namespace
+
+// A block takes one of the matrix's n_part contiguous pieces (a multiple of 8 elements long): momentum in place,
+// squares added in fp32 over eight elements and in fp64 from there on, one partial sum per block in a fixed order.
+template <typename T, bool STEP>
+__global__ void __launch_bounds__(MS_THREADS)
+muon_moment_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ status)
+{
+    __shared__ double scratch[32];
+    const int k = find_item(a, blockIdx.x);
+    const MuonItem& it = a.item[k];
+    const int piece = (int)blockIdx.x - a.tile_begin[k];
+    const int64_t numel = (int64_t)it.rows * it.cols;
+    const int64_t len = ((numel + it.n_part - 1) / it.n_part + 7) / 8 * 8;
+    const int64_t begin = min((int64_t)piece * len, numel), end = min(begin + len, numel);
+    const T* __restrict__ G = static_cast<const T*>(it.g);
+    float* __restrict__ M = it.m;
+    double sum = 0.0;
+    auto one = [&](float g, float& m) {
+        if constexpr (STEP) m = fmaf(a.mu, m, (1.0f - a.mu) * g);
+        const float u = update_of<STEP>(g, m, a);
+        return u * u;
+    };
+    for (int64_t e = begin + (int64_t)threadIdx.x * 8; e < end; e += MS_THREADS * 16) {
+        // two vectors of eight per round, all loads before the first use
+        float g[2][8], m[2][8];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int64_t p = e + u * (MS_THREADS * 8);
+            const int count = (int)min((int64_t)8, end - p);
+            if (count == 8 && APOLLO_DBG_RANGE(p, p + 7, numel, status)) {
+                load8_stream(G + p, g[u]);
+                if constexpr (STEP) load8_stream(M + p, m[u]);
+            } else {
+                load8_guarded(G + p, count, g[u]);
+                if constexpr (STEP) load8_guarded(M + p, count, m[u]);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int64_t p = e + u * (MS_THREADS * 8);
+            const int count = (int)min((int64_t)8, end - p);
+            if (count <= 0) break;
+            float s = 0.0f;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) s += one(g[u][x], m[u][x]);
+            sum += (double)s;
+            if constexpr (STEP) {
+                if (count == 8 && APOLLO_DBG_RANGE(p, p + 7, numel, status)) {
+                    reinterpret_cast<float4*>(M + p)[0] = make_float4(m[u][0], m[u][1], m[u][2], m[u][3]);
+                    reinterpret_cast<float4*>(M + p)[1] = make_float4(m[u][4], m[u][5], m[u][6], m[u][7]);
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 8; ++x)
+                        if (x < count) M[p + x] = m[u][x];
+                }
+            }
+        }
+    }
+    const double total = block_sum(sum, scratch);
+    if (threadIdx.x == 0) it.part[piece] = total;
+}
+
+// X = U x_scale / (|U| + eps) as 16-bit floats (high and low part with `SPLIT` = fp32 weights), transposed when tall.
+template <typename T, bool STEP>
+__global__ void __launch_bounds__(MS_THREADS)
+muon_load_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ status)
+{
+    constexpr bool SPLIT = sizeof(T) == 4;
+    __shared__ double scratch[32];
+    __shared__ float tile[MS_ROWS][MS_COLS + 1];
+    const int k = find_item(a, blockIdx.x);
+    const MuonItem& it = a.item[k];
+    const int local = (int)blockIdx.x - a.tile_begin[k];
+    const int rows = it.rows, cols = it.cols, tiles_c = (cols + MS_COLS - 1) / MS_COLS;
+    const int r0 = local / tiles_c * MS_ROWS, c0 = (local - local / tiles_c * tiles_c) * MS_COLS;
+    const T* __restrict__ G = static_cast<const T*>(it.g);
+    const float* __restrict__ M = it.m;
+    const int c = threadIdx.x & 63, rr = threadIdx.x >> 6;
+    float u[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int r = r0 + rr + 4 * i;
+        const int64_t at = (int64_t)r * cols + c0 + c;
+        const bool in = r < rows && c0 + c < cols && APOLLO_DBG_RANGE(at, at, (int64_t)rows * cols, status);
+        const float g = in ? load1(G + at) : 0.0f;
+        float m = 0.0f;
+        if constexpr (STEP) m = in ? M[at] : 0.0f;
+        u[i] = update_of<STEP>(g, m, a);
+    }
+    const double total = block_sum((int)threadIdx.x < it.n_part ? it.part[threadIdx.x] : 0.0, scratch);
+    const float f = a.x_scale / ((float)sqrt(total) + a.eps);
+    __half* __restrict__ hi = it.x[0];
+    __half* __restrict__ lo = it.x[1];
+    const int64_t extent = (int64_t)(it.tall ? cols : rows) * it.x_pitch;
+    auto put = [&](int64_t at, float v) {
+        if (!APOLLO_DBG_RANGE(at, at, extent, status)) return;
+        const __half h = __float2half_rn(v);
+        hi[at] = h;
+        if constexpr (SPLIT) lo[at] = __float2half_rn(v - __half2float(h));
+    };
+    if (!it.tall) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = r0 + rr + 4 * i;
+            if (r < rows && c0 + c < cols) put((int64_t)r * it.x_pitch + c0 + c, u[i] * f);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) tile[rr + 4 * i][c] = u[i] * f;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int cc = rr + 4 * i;                   // source column = row of X
+            if (c0 + cc < cols && r0 + c < rows) put((int64_t)(c0 + cc) * it.x_pitch + r0 + c, tile[c][cc]);
+        }
+    }
+}
+
+// W <- W - lr (gain X + wd W), or O = X; X is read back transposed when tall.
+template <typename T, bool STEP>
+__global__ void __launch_bounds__(MS_THREADS)
+muon_apply_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ status)
+{
+    constexpr bool SPLIT = sizeof(T) == 4;
+    __shared__ float tile[MS_ROWS][MS_COLS + 1];
+    ptx::grid_wait_previous();
+    if (*reinterpret_cast<volatile int32_t*>(status) != STATUS_OK) return;      // a product gave up: leave the weights
+    const int k = find_item(a, blockIdx.x);
+    const MuonItem& it = a.item[k];
+    const int local = (int)blockIdx.x - a.tile_begin[k];
+    const int rows = it.rows, cols = it.cols, tiles_c = (cols + MS_COLS - 1) / MS_COLS;
+    const int r0 = local / tiles_c * MS_ROWS, c0 = (local - local / tiles_c * tiles_c) * MS_COLS;
+    T* __restrict__ W = static_cast<T*>(it.w);
+    const __half* hi = it.x[0];
+    const __half* lo = it.x[1];
+    const int c = threadIdx.x & 63, rr = threadIdx.x >> 6;
+    const float f = 1.0f / a.x_scale;                    // a power of two
+    const int64_t extent = (int64_t)(it.tall ? cols : rows) * it.x_pitch;
+    auto get = [&](int64_t at) {
+        if (!APOLLO_DBG_RANGE(at, at, extent, status)) return 0.0f;
+        float v = __half2float(hi[at]);
+        if constexpr (SPLIT) v += __half2float(lo[at]);
+        return v * f;
+    };
+    float x[16];
+    if (!it.tall) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = r0 + rr + 4 * i;
+            x[i] = r < rows && c0 + c < cols ? get((int64_t)r * it.x_pitch + c0 + c) : 0.0f;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int cc = rr + 4 * i;
+            tile[c][cc] = c0 + cc < cols && r0 + c < rows ? get((int64_t)(c0 + cc) * it.x_pitch + r0 + c) : 0.0f;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = tile[rr + 4 * i][c];
+    }
+    float w[16];
+    if constexpr (STEP) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = r0 + rr + 4 * i;
+            w[i] = r < rows && c0 + c < cols ? load1(W + (int64_t)r * cols + c0 + c) : 0.0f;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int r = r0 + rr + 4 * i;
+        const int64_t at = (int64_t)r * cols + c0 + c;
+        if (r >= rows || c0 + c >= cols || !APOLLO_DBG_RANGE(at, at, (int64_t)rows * cols, status)) continue;
+        if constexpr (STEP) store_elem(W + at, fmaf(-a.lr, fmaf(a.wd, w[i], it.gain * x[i]), w[i]));
+        else store_elem(W + at, x[i]);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+int muon_stream_tiles(int rows, int cols)
+{
+    return ((rows + MS_ROWS - 1) / MS_ROWS) * ((cols + MS_COLS - 1) / MS_COLS);
+}
+
+cudaError_t launch_muon_moment(int dtype, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream)
+{
+    if (dtype == APOLLO_DT_BF16) {
+        if (step) muon_moment_kernel<__nv_bfloat16, true><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
+        else muon_moment_kernel<__nv_bfloat16, false><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
+    } else {
+        if (step) muon_moment_kernel<float, true><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
+        else muon_moment_kernel<float, false><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
+    }
+    return cudaGetLastError();
+}
+
+cudaError_t launch_muon_load(int dtype, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream)
+{
+    if (dtype == APOLLO_DT_BF16) {
+        if (step) muon_load_kernel<__nv_bfloat16, true><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
+        else muon_load_kernel<__nv_bfloat16, false><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
+    } else {
+        if (step) muon_load_kernel<float, true><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
+        else muon_load_kernel<float, false><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
+    }
+    return cudaGetLastError();
+}
+
+cudaError_t launch_muon_apply(int dtype, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream)
+{
+    if (dtype == APOLLO_DT_BF16) {
+        if (step) muon_apply_kernel<__nv_bfloat16, true><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
+        else muon_apply_kernel<__nv_bfloat16, false><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
+    } else {
+        if (step) muon_apply_kernel<float, true><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
+        else muon_apply_kernel<float, false><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
+    }
+    return cudaGetLastError();
+}
+
+cudaError_t launch_muon_gemm(bool split, const GemmOp* d_ops, const int* d_prefix, int n_ops, int tiles, MuonLaunch& state,
+                             int32_t* d_status, cudaStream_t stream)
+{
+    typedef void (*Kernel)(const GemmOp*, const int*, int, int, int32_t*);
+    const Kernel kernel = split ? muon_gemm_kernel<true> : muon_gemm_kernel<false>;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(state.sm_count / 2 * 2));
+    cfg.blockDim = dim3(MG_THREADS);
+    cfg.dynamicSmemBytes = MG_SMEM;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (!state.attr_set) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MG_SMEM);
+        if (e != cudaSuccess) return e;
+        // persistent over the tiles: as many pairs as can be resident at once
+        int clusters = 0;
+        if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) != cudaSuccess || clusters < 1) {
+            cudaGetLastError();
+            clusters = state.sm_count / 2;
+        }
+        state.max_pairs = clusters;
+        state.attr_set = true;
+    }
+    cfg.numAttrs = 2;
+    cfg.gridDim = dim3((unsigned)(2 * (tiles < state.max_pairs ? tiles : state.max_pairs)));
+    return cudaLaunchKernelEx(&cfg, kernel, d_ops, d_prefix, n_ops, tiles, d_status);
+}
+
+int muon_encode_maps(const __half* base, int rows, int cols, int pitch, void* load, void* store, void* mirror)
+{
+    EncodeTiledFn encode = encode_fn();
+    if (!encode) return APOLLO_ERR_CUDA;
+    const cuuint64_t dims[2] = { (cuuint64_t)cols, (cuuint64_t)rows };
+    const cuuint64_t strides[1] = { (cuuint64_t)pitch * 2 };
+    const cuuint32_t elem[2] = { 1u, 1u };
+    auto make = [&](void* out, cuuint32_t w, cuuint32_t h, CUtensorMapSwizzle sw) {
+        const cuuint32_t box[2] = { w, h };
+        return encode(static_cast<CUtensorMap*>(out), CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<__half*>(base), dims, strides, box, elem,
+                      CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    if (!make(load, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B) || !make(store, 64, 32, CU_TENSOR_MAP_SWIZZLE_128B)) return APOLLO_ERR_CUDA;
+    if (mirror && !make(mirror, 32, 64, CU_TENSOR_MAP_SWIZZLE_NONE)) return APOLLO_ERR_CUDA;
+    return APOLLO_OK;
+}
+
+}  // namespace apollo

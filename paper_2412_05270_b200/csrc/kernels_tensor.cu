@@ -32,6 +32,7 @@
 #include "../../include/apollo.h"
 #include "device_utils.cuh"
 #include "philox.cuh"
+#include "tc_common.cuh"
 #include "tc_ptx.cuh"
 
 namespace apollo {
@@ -48,24 +49,6 @@ constexpr int TC_MISC_BYTES = 256 + 3 * 512 * 8 + 8 * 512 * 4 + 1024;   // barri
 constexpr int TC_MAX_SMEM = 227 * 1024;
 constexpr int TC_PREFETCH = 2;             // k-blocks of G asked into L2 ahead of the load that needs them
 constexpr uint32_t TC_PACE_CAP = 1u << 12; // polls (100 ns apart) of the prefetchers' pacing wait; expiry is harmless
-constexpr uint32_t TC_WAIT_CAP = 1u << 20;   // polls before a wait gives up (normal waits are far below 1 ms)
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn()
-{
-    static EncodeTiledFn fn = nullptr;
-    if (!fn) {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<EncodeTiledFn>(p);
-    }
-    return fn;
-}
 
 }  // namespace
 
@@ -235,50 +218,6 @@ int tensor_path_prepare(MatDesc* h_descs, int n_mat, int rank, const TcTiling& t
 }
 
 namespace {
-
-// Bounded wait on an mbarrier phase.  On expiry the CTA-wide abort flag and the global
-// status word are set; later waits return at once, so the kernel always terminates.
-// Bounded wait on an mbarrier phase.  false = this wait, or an earlier one of this CTA, gave up: the
-// caller stops issuing work and falls through to the barriers and the drain at the end of the kernel.
-// `where` names the wait (role and barrier); the first one of a launch that gives up is kept in the word after
-// the status word, for whoever has to find out what stalled.
-__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status,
-                                           int where = 0)
-{
-    if (ptx::mbar_try_wait(bar, parity)) return true;      // the common case costs one poll and no flag read
-    if (*abort_flag) return false;
-    for (uint32_t i = 0; i < TC_WAIT_CAP; ++i)
-        if (ptx::mbar_try_wait(bar, parity)) return true;
-    *abort_flag = 1;
-    atomicCAS(status + 1, 0, where);
-    atomicExch(status, STATUS_TIMEOUT);
-    return false;
-}
-
-// The same for waits that have slack (an epilogue waiting for its accumulator): sleeps between polls,
-// which costs nothing there and saves issue slots, i.e. power, on a board that runs at its power cap.
-__device__ __forceinline__ bool wait_phase_idle(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status,
-                                                int where = 0)
-{
-    if (ptx::mbar_try_wait(bar, parity)) return true;
-    if (*abort_flag) return false;
-    for (uint32_t i = 0; i < TC_WAIT_CAP; ++i) {
-        __nanosleep(200);
-        if (ptx::mbar_try_wait(bar, parity)) return true;
-    }
-    *abort_flag = 1;
-    atomicCAS(status + 1, 0, where);
-    atomicExch(status, STATUS_TIMEOUT);
-    return false;
-}
-
-// Bounded wait that neither reads nor sets the abort flag: lets copies and MMAs that are already in
-// flight finish before the CTA gives up its shared memory and TMEM.
-__device__ __forceinline__ void drain_phase(uint32_t bar, uint32_t parity)
-{
-    for (uint32_t i = 0; i < TC_WAIT_CAP; ++i)
-        if (ptx::mbar_try_wait(bar, parity)) return;
-}
 
 // Counters in global memory that CTAs of one launch signal each other through (P generated by spare warps).
 __device__ __forceinline__ uint32_t ld_acquire_gpu(const uint32_t* p)

@@ -1,0 +1,69 @@
+// Structures shared by the host side of the orthogonalised update and its kernels.
+#pragma once
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace apollo {
+
+constexpr int MUON_TILE = 256;          // a product's tile: 256 x 256, shared by the two CTAs of a pair
+constexpr int MUON_CHUNK = 48;          // matrices whose pointers travel in one launch of a streaming kernel
+constexpr int MUON_PART = 256;          // most partial sums of squares per matrix
+
+// out = alpha L R + b1 E1 + b2 E2 + diag I on stored (scaled) values; L is M x K with k contiguous, R is K x N, with
+// k contiguous (r_mn = 0: given as the N x K matrix) or with n contiguous (r_mn = 1).  [0] / [1]: the high and low
+// parts of split operands.  sym: M = N and the result is symmetric: tiles on and above the diagonal are computed,
+// the ones above also written transposed.
+struct GemmOp {
+    const void* l_map[2];               // DEVICE tensor maps (boxes of 64 x 64)
+    const void* r_map[2];
+    const void* out_map[2];             // boxes of 64 x 32 rows
+    const void* mir_map[2];             // boxes of 32 x 64 rows (sym)
+    const __half* e1[2];                // same place and pitch as the output; null = none
+    const __half* e2[2];
+    float alpha, b1, b2, diag;
+    int32_t M, N, K, e_pitch, tiles_m, tiles_n, sym, r_mn;
+};
+
+// One matrix of a streaming kernel.
+struct MuonItem {
+    void* w;                            // weights / the orthogonalised result
+    const void* g;
+    float* m;
+    __half* x[2];                       // iterate, m x n (transposed when tall), high and low parts
+    double* part;                       // partial sums of squares of U
+    int32_t rows, cols, x_pitch, n_part;
+    int32_t tall;
+    float gain;                         // s of the update
+};
+
+struct MuonArgs {
+    MuonItem item[MUON_CHUNK];
+    int32_t tile_begin[MUON_CHUNK + 1];
+    int32_t n;
+    float mu, eps, x_scale, lr, wd;     // x_scale: the power of two the iterates carry
+    int32_t nesterov;
+};
+
+struct MuonLaunch {                     // what the launches of a context need to know about the device
+    int sm_count, max_pairs;
+    bool attr_set;
+};
+
+// Sum of squares of U (and M <- mu M + (1 - mu) G with `step`), X = U x_scale / (|U| + eps) in 16 bits, and the end:
+// W <- W - lr (gain X + wd W) with `step`, O = X without.
+cudaError_t launch_muon_moment(int dtype, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream);
+cudaError_t launch_muon_load(int dtype, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream);
+cudaError_t launch_muon_apply(int dtype, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream);
+// Tiles of one matrix in the load and apply kernels.
+int muon_stream_tiles(int rows, int cols);
+
+// One phase: ops[0 .. n_ops) with their tile prefix (DEVICE).
+cudaError_t launch_muon_gemm(bool split, const GemmOp* d_ops, const int* d_prefix, int n_ops, int tiles, MuonLaunch& state,
+                             int32_t* d_status, cudaStream_t stream);
+
+// Tensor maps of a rows x cols matrix of 16-bit floats (pitch a multiple of 8): what the products load, store and
+// store transposed.  `out`: 128 bytes each.
+int muon_encode_maps(const __half* base, int rows, int cols, int pitch, void* load, void* store, void* mirror);
+
+}  // namespace apollo
