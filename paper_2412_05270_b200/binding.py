@@ -6,7 +6,6 @@ import of this module's symbols raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 from pathlib import Path
 from typing import NamedTuple
@@ -453,8 +452,10 @@ class Muon:
             self.ctx = None
 
     def __del__(self):
-        with contextlib.suppress(Exception):
+        try:
             self.close()
+        except Exception:
+            pass
 
     def _marshal(self, lists):
         want = torch.bfloat16 if self.cfg.dtype == DT_BF16 else torch.float32

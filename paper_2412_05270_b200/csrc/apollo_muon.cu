@@ -125,7 +125,7 @@ int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_confi
     const int rc = validate(cfg, plan.sc);
     if (rc != APOLLO_OK) return rc;
     plan.parts = cfg->dtype == APOLLO_DT_F32 ? 2 : 1;
-    plan.maps_per_mat = (2 * 2 + 3 * 3) * plan.parts;
+    plan.maps_per_mat = (2 + 3) * MUON_MAPS * plan.parts;
     plan.mats.resize(n_mat);
     std::vector<size_t> need(n_mat);
     for (int i = 0; i < n_mat; ++i) {
@@ -225,18 +225,18 @@ void ops_of(const apollo_muon_ctx* ctx, const Mat& m, std::vector<GemmOp>& out)
     const double a = ctx->cfg.coef[0], b = ctx->cfg.coef[1], c = ctx->cfg.coef[2], p = a - sc.shift;
     const int parts = plan.parts;
     char* ws = ctx->ws;
-    auto x_map = [&](int buf, int h, int kind) { return (const void*)(ws + m.maps + 128 * (size_t)((buf * parts + h) * 2 + kind)); };
-    auto s_map = [&](int buf, int h, int kind) { return (const void*)(ws + m.maps + 128 * (size_t)(4 * parts + (buf * parts + h) * 3 + kind)); };
+    auto x_map = [&](int buf, int h, int kind) { return (const void*)(ws + m.maps + 128 * (size_t)((buf * parts + h) * MUON_MAPS + kind)); };
+    auto s_map = [&](int buf, int h, int kind) { return x_map(2 + buf, h, kind); };
     auto x_ptr = [&](int buf, int h) { return (const __half*)(ws + m.x[buf][h]); };
     auto s_ptr = [&](int buf, int h) { return (const __half*)(ws + m.s[buf][h]); };
     auto square = [&](int l, int r, int dst, double alpha, int e1, double b1, int e2, double b2, double diag, bool of_x) {
         GemmOp o;
         std::memset(&o, 0, sizeof(o));
         for (int h = 0; h < parts; ++h) {
-            o.l_map[h] = of_x ? x_map(l, h, 0) : s_map(l, h, 0);
-            o.r_map[h] = of_x ? x_map(r, h, 0) : s_map(r, h, 0);
-            o.out_map[h] = s_map(dst, h, 1);
-            o.mir_map[h] = s_map(dst, h, 2);
+            o.l_map[h] = of_x ? x_map(l, h, MAP_ROWS) : s_map(l, h, MAP_ROWS);
+            o.r_map[h] = of_x ? x_map(r, h, MAP_ROWS) : s_map(r, h, MAP_ROWS);
+            o.out_map[h] = s_map(dst, h, MAP_STORE);
+            o.mir_map[h] = s_map(dst, h, MAP_MIRROR);
             if (e1 >= 0) o.e1[h] = s_ptr(e1, h);
             if (e2 >= 0) o.e2[h] = s_ptr(e2, h);
         }
@@ -250,9 +250,9 @@ void ops_of(const apollo_muon_ctx* ctx, const Mat& m, std::vector<GemmOp>& out)
         GemmOp o;
         std::memset(&o, 0, sizeof(o));
         for (int h = 0; h < parts; ++h) {
-            o.l_map[h] = s_map(s, h, 0);
-            o.r_map[h] = x_map(src, h, 0);
-            o.out_map[h] = x_map(src ^ 1, h, 1);
+            o.l_map[h] = s_map(s, h, MAP_ROWS);
+            o.r_map[h] = x_map(src, h, MAP_COLS);
+            o.out_map[h] = x_map(src ^ 1, h, MAP_STORE);
             o.e1[h] = x_ptr(src, h);
         }
         o.alpha = (float)alpha; o.b1 = (float)b1;
@@ -290,14 +290,10 @@ int build_table(apollo_muon_ctx* ctx)
     for (size_t i = 0; i < plan.mats.size(); ++i) {
         const Mat& m = plan.mats[i];
         char* maps = at(m.maps);
-        for (int b = 0; b < 2; ++b)
-            for (int h = 0; h < plan.parts; ++h, maps += 256) {
-                const int rc = muon_encode_maps((const __half*)(ctx->ws + m.x[b][h]), m.m, m.n, m.pitch_x, maps, maps + 128, nullptr);
-                if (rc != APOLLO_OK) return rc;
-            }
-        for (int b = 0; b < 3; ++b)
-            for (int h = 0; h < plan.parts; ++h, maps += 384) {
-                const int rc = muon_encode_maps((const __half*)(ctx->ws + m.s[b][h]), m.m, m.m, m.pitch_s, maps, maps + 128, maps + 256);
+        for (int b = 0; b < 5; ++b)
+            for (int h = 0; h < plan.parts; ++h, maps += 128 * MUON_MAPS) {
+                const size_t at_ws = b < 2 ? m.x[b][h] : m.s[b - 2][h];
+                const int rc = muon_encode_maps((const __half*)(ctx->ws + at_ws), m.m, b < 2 ? m.n : m.m, b < 2 ? m.pitch_x : m.pitch_s, maps);
                 if (rc != APOLLO_OK) return rc;
             }
         ops_of(ctx, m, ops[i]);

@@ -5,10 +5,10 @@
 // muon_moment / muon_load / muon_apply   the streaming passes before and after
 //
 // A product's tile is 256 x 256: each CTA of a pair loads its 128 rows of L and half of the 256 columns of R, 32 KB
-// per 64-deep k-block, five stages; four MMAs of 256 x 256 x 16 consume them.  Roles of the 12 warps: 0 TMA producer,
+// per 64-deep k-block, six stages; four MMAs of 256 x 256 x 16 consume them.  Roles of the 12 warps: 0 TMA producer,
 // 1 MMA issuer (leader CTA) and TMEM owner, 4-11 epilogue (a warp reads the 32 TMEM lanes it may read and one half
 // of the columns).  The epilogue adds the terms that the iteration needs beside the product, rounds to 16 bits and
-// hands 32 x 64 pieces to TMA stores; a symmetric product's tile above the diagonal is stored a second time,
+// hands 32 x 32 pieces to TMA stores; a symmetric product's tile above the diagonal is stored a second time,
 // transposed, so that half of the symmetric products is never computed.
 // Bound: the tensor pipe (and with it the board's power).
 //
@@ -26,12 +26,12 @@ namespace apollo {
 namespace {
 
 constexpr int MG_THREADS = 384;
-constexpr int MG_STAGES = 5;
+constexpr int MG_STAGES = 6;
 constexpr int MG_HALF = 8192;                            // 64 x 64 16-bit floats: one TMA box
 constexpr int MG_OPERAND = 2 * MG_HALF;                  // a CTA's 128 rows of L, or half of R
 constexpr int MG_STAGE = 2 * MG_OPERAND;
 constexpr int MG_EPI_WARPS = 8;
-constexpr int MG_STAGING = MG_EPI_WARPS * 8192;          // per epilogue warp: 4 KB as stored, 4 KB transposed
+constexpr int MG_STAGING = MG_EPI_WARPS * 4096;          // per epilogue warp: 2 KB as stored, 2 KB transposed
 constexpr int MG_SMEM = MG_STAGES * MG_STAGE + MG_STAGING + 256 + 1024;
 static_assert(MG_SMEM <= 227 * 1024, "shared memory of a CTA");
 
@@ -172,13 +172,11 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const int* __restrict__ prefix,
                     const void* lm = SPLIT && seg == 1 ? l_lo : l_hi;
                     const void* rm = SPLIT && seg == 2 ? r_lo : r_hi;
                     ptx::tma_load_2d_pair(dst, lm, k, m0, full, pol);
-                    ptx::tma_load_2d_pair(dst + MG_HALF, lm, k, m0 + 64, full, pol);
                     if (r_mn) {
                         ptx::tma_load_2d_pair(dst + MG_OPERAND, rm, n0, k, full, pol);
                         ptx::tma_load_2d_pair(dst + MG_OPERAND + MG_HALF, rm, n0 + 64, k, full, pol);
                     } else {
                         ptx::tma_load_2d_pair(dst + MG_OPERAND, rm, k, n0, full, pol);
-                        ptx::tma_load_2d_pair(dst + MG_OPERAND + MG_HALF, rm, k, n0 + 64, full, pol);
                     }
                     k += 64;
                     if (SPLIT && k >= nkb * 64) { k = 0; ++seg; }
@@ -223,7 +221,7 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const int* __restrict__ prefix,
             const float alpha = __ldg(&op->alpha), b1 = __ldg(&op->b1), b2 = __ldg(&op->b2), diag = __ldg(&op->diag);
             const __half* e1 = op->e1[0];
             const __half* e2 = op->e2[0];
-            const uint32_t mine = staging + (uint32_t)(warp - 4) * 8192u, mine_t = mine + 4096u;
+            const uint32_t mine = staging + (uint32_t)(warp - 4) * 4096u, mine_t = mine + 2048u;
             if (lane == 0 && fenced != op_at) {
                 for (int h = 0; h < (SPLIT ? 2 : 1); ++h) {
                     ptx::fence_tensormap_acquire(op->out_map[h]);
@@ -235,85 +233,64 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const int* __restrict__ prefix,
             ptx::tc_fence_after_sync();
             if (acc_ok && row0 < M) {
 #pragma unroll 1
-                for (int ch = 0; ch < 2; ++ch) {
-                    const int col0 = tn * MUON_TILE + half * 128 + ch * 64;
-                    if (col0 >= N) break;
-                    uint32_t lo_bits[SPLIT ? 32 : 1];
-                    if (lane == 0) ptx::bulk_wait_read();            // the stores of the last piece have read the staging
-                    __syncwarp();
+                for (int ch = 0; ch < 4; ++ch) {
+                    const int col = tn * MUON_TILE + half * 128 + ch * 32;
+                    if (col >= N) break;
+                    const int64_t at = (int64_t)row * e_pitch + col;
+                    const bool in = row < M;
+                    uint4 t1[4], t2[4], t1l[SPLIT ? 4 : 1], t2l[SPLIT ? 4 : 1];
+                    if (e1) load_term(t1, e1 + at, in);
+                    if (e2) load_term(t2, e2 + at, in);
+                    if constexpr (SPLIT) {
+                        if (e1) load_term(t1l, op->e1[1] + at, in);
+                        if (e2) load_term(t2l, op->e2[1] + at, in);
+                    }
+                    float v[32];
+                    ptx::tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + buf * MUON_TILE + (uint32_t)(half * 128 + ch * 32), v);
 #pragma unroll
-                    for (int sub = 0; sub < 2; ++sub) {
-                        const int col = col0 + sub * 32;
-                        const int64_t at = (int64_t)row * e_pitch + col;
-                        const bool in = row < M;
-                        uint4 t1[4], t2[4], t1l[SPLIT ? 4 : 1], t2l[SPLIT ? 4 : 1];
-                        if (e1) load_term(t1, e1 + at, in);
-                        if (e2) load_term(t2, e2 + at, in);
-                        if constexpr (SPLIT) {
-                            if (e1) load_term(t1l, op->e1[1] + at, in);
-                            if (e2) load_term(t2l, op->e2[1] + at, in);
-                        }
-                        float v[32];
-                        ptx::tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + buf * MUON_TILE + (uint32_t)(half * 128 + ch * 64 + sub * 32), v);
+                    for (int i = 0; i < 32; ++i) v[i] *= alpha;
+                    if (e1) add_term(v, b1, t1);
+                    if (e2) add_term(v, b2, t2);
+                    if constexpr (SPLIT) {
+                        if (e1) add_term(v, b1, t1l);
+                        if (e2) add_term(v, b2, t2l);
+                    }
+                    if (sym && diag != 0.0f && row >= col && row < col + 32) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] *= alpha;
-                        if (e1) add_term(v, b1, t1);
-                        if (e2) add_term(v, b2, t2);
-                        if constexpr (SPLIT) {
-                            if (e1) add_term(v, b1, t1l);
-                            if (e2) add_term(v, b2, t2l);
-                        }
-                        if (sym && diag != 0.0f && row >= col && row < col + 32) {
+                        for (int i = 0; i < 32; ++i) v[i] += row == col + i ? diag : 0.0f;
+                    }
+                    uint32_t w[16];
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) v[i] += row == col + i ? diag : 0.0f;
-                        }
-                        uint32_t w[16];
+                    for (int i = 0; i < 16; ++i) w[i] = pack_half2(v[2 * i], v[2 * i + 1]);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) w[i] = pack_half2(v[2 * i], v[2 * i + 1]);
-                        if constexpr (SPLIT) {
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const float2 f = unpack_half2(w[i]);
-                                lo_bits[sub * 16 + i] = pack_half2(v[2 * i] - f.x, v[2 * i + 1] - f.y);
-                            }
-                        }
+                    for (int h = 0; h < (SPLIT ? 2 : 1); ++h) {
+                        if (lane == 0) ptx::bulk_wait_read();        // the stores of the last piece have read the staging
+                        __syncwarp();
+                        // rows of 64 bytes in the 64-byte swizzle of the store's map: the 16-byte unit of a row is
+                        // exchanged with bits 1..2 of the row, so that eight lanes hit eight different units
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            st_shared_v4(mine + (uint32_t)(lane * 128 + (((sub * 4 + i) ^ (lane & 7)) << 4)), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                            st_shared_v4(mine + (uint32_t)(lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
                         if (mirror) {
 #pragma unroll
                             for (int i = 0; i < 16; ++i) {
-                                st_shared_u16(mine_t + (uint32_t)(((sub * 32 + 2 * i) * 32 + lane) * 2), (uint16_t)(w[i] & 0xFFFFu));
-                                st_shared_u16(mine_t + (uint32_t)(((sub * 32 + 2 * i + 1) * 32 + lane) * 2), (uint16_t)(w[i] >> 16));
-                            }
-                        }
-                    }
-                    ptx::fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        ptx::tma_store_2d(op->out_map[0], col0, row0, mine);
-                        if (mirror) ptx::tma_store_2d(op->mir_map[0], row0, col0, mine_t);
-                        ptx::bulk_commit();
-                    }
-                    if constexpr (SPLIT) {
-                        if (lane == 0) ptx::bulk_wait_read();
-                        __syncwarp();
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            st_shared_v4(mine + (uint32_t)(lane * 128 + ((i ^ (lane & 7)) << 4)), lo_bits[4 * i], lo_bits[4 * i + 1], lo_bits[4 * i + 2], lo_bits[4 * i + 3]);
-                        if (mirror) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                st_shared_u16(mine_t + (uint32_t)(((2 * i) * 32 + lane) * 2), (uint16_t)(lo_bits[i] & 0xFFFFu));
-                                st_shared_u16(mine_t + (uint32_t)(((2 * i + 1) * 32 + lane) * 2), (uint16_t)(lo_bits[i] >> 16));
+                                st_shared_u16(mine_t + (uint32_t)(((2 * i) * 32 + lane) * 2), (uint16_t)(w[i] & 0xFFFFu));
+                                st_shared_u16(mine_t + (uint32_t)(((2 * i + 1) * 32 + lane) * 2), (uint16_t)(w[i] >> 16));
                             }
                         }
                         ptx::fence_proxy_async_smem();
                         __syncwarp();
                         if (lane == 0) {
-                            ptx::tma_store_2d(op->out_map[1], col0, row0, mine);
-                            if (mirror) ptx::tma_store_2d(op->mir_map[1], row0, col0, mine_t);
+                            ptx::tma_store_2d(op->out_map[h], col, row0, mine);
+                            if (mirror) ptx::tma_store_2d(op->mir_map[h], row0, col, mine_t);
                             ptx::bulk_commit();
+                        }
+                        if (SPLIT && h == 0) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const float2 f = unpack_half2(w[i]);
+                                w[i] = pack_half2(v[2 * i] - f.x, v[2 * i + 1] - f.y);
+                            }
                         }
                     }
                 }
@@ -370,6 +347,40 @@ __device__ __forceinline__ float update_of(float g, float m, const MuonArgs& a)
 {
     if constexpr (!STEP) return g;
     return a.nesterov ? fmaf(a.mu, m, (1.0f - a.mu) * g) : m;
+}
+
+// Two neighbours at p + at, `left` of them inside the row; as one access where rows are whole pairs.
+__device__ __forceinline__ void pair_at(const float* p, float (&v)[2])
+{
+    const float2 t = __ldcs(reinterpret_cast<const float2*>(p));
+    v[0] = t.x; v[1] = t.y;
+}
+__device__ __forceinline__ void pair_at(const __nv_bfloat16* p, float (&v)[2])
+{
+    const uint32_t t = __ldcs(reinterpret_cast<const uint32_t*>(p));
+    v[0] = __uint_as_float(t << 16); v[1] = __uint_as_float(t & 0xFFFF0000u);
+}
+template <typename T>
+__device__ __forceinline__ void load_pair(const T* p, int64_t at, int left, bool pairs, int64_t numel, float (&v)[2], int32_t* status)
+{
+    v[0] = v[1] = 0.0f;
+    if (left >= 2 && pairs) {
+        if (APOLLO_DBG_RANGE(at, at + 1, numel, status)) pair_at(p + at, v);
+    } else {
+        if (left >= 1 && APOLLO_DBG_RANGE(at, at, numel, status)) v[0] = load1(p + at);
+        if (left >= 2 && APOLLO_DBG_RANGE(at + 1, at + 1, numel, status)) v[1] = load1(p + at + 1);
+    }
+}
+__device__ __forceinline__ void store2(float* p, const float (&v)[2]) { *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]); }
+__device__ __forceinline__ void store2(__nv_bfloat16* p, const float (&v)[2]) { *reinterpret_cast<uint32_t*>(p) = pack_bf16x2(v[0], v[1]); }
+__device__ __forceinline__ void store8(float* p, const float (&v)[8])
+{
+    __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
+    __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8])
+{
+    __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])));
 }
 
 __device__ __forceinline__ void store_elem(float* p, float v) { *p = v; }
@@ -453,43 +464,92 @@ muon_load_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ statu
     const int r0 = local / tiles_c * MS_ROWS, c0 = (local - local / tiles_c * tiles_c) * MS_COLS;
     const T* __restrict__ G = static_cast<const T*>(it.g);
     const float* __restrict__ M = it.m;
-    const int c = threadIdx.x & 63, rr = threadIdx.x >> 6;
-    float u[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int r = r0 + rr + 4 * i;
-        const int64_t at = (int64_t)r * cols + c0 + c;
-        const bool in = r < rows && c0 + c < cols && APOLLO_DBG_RANGE(at, at, (int64_t)rows * cols, status);
-        const float g = in ? load1(G + at) : 0.0f;
-        float m = 0.0f;
-        if constexpr (STEP) m = in ? M[at] : 0.0f;
-        u[i] = update_of<STEP>(g, m, a);
-    }
-    const double total = block_sum((int)threadIdx.x < it.n_part ? it.part[threadIdx.x] : 0.0, scratch);
-    const float f = a.x_scale / ((float)sqrt(total) + a.eps);
+    const int64_t numel = (int64_t)rows * cols, extent = (int64_t)(it.tall ? cols : rows) * it.x_pitch;
     __half* __restrict__ hi = it.x[0];
     __half* __restrict__ lo = it.x[1];
-    const int64_t extent = (int64_t)(it.tall ? cols : rows) * it.x_pitch;
-    auto put = [&](int64_t at, float v) {
-        if (!APOLLO_DBG_RANGE(at, at, extent, status)) return;
-        const __half h = __float2half_rn(v);
-        hi[at] = h;
-        if constexpr (SPLIT) lo[at] = __float2half_rn(v - __half2float(h));
+    // the sum of squares comes last: its loads and the reduction hide behind those of the elements
+    auto factor = [&]() {
+        const double total = block_sum((int)threadIdx.x < it.n_part ? it.part[threadIdx.x] : 0.0, scratch);
+        return a.x_scale / ((float)sqrt(total) + a.eps);
+    };
+    if (!it.tall && cols % 8 == 0) {
+        // rows are whole vectors on both sides
+        const int c = c0 + (threadIdx.x & 7) * 8, r1 = r0 + (threadIdx.x >> 3);
+        float u[2][8];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = r1 + 32 * i;
+            const int64_t at = (int64_t)r * cols + c;
+            float m[8];
+            if (r < rows && c < cols && APOLLO_DBG_RANGE(at, at + 7, numel, status)) {
+                load8_stream(G + at, u[i]);
+                if constexpr (STEP) load8_stream(M + at, m);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[i][e] = m[e] = 0.0f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[i][e] = update_of<STEP>(u[i][e], m[e], a);
+        }
+        const float f = factor();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = r1 + 32 * i;
+            const int64_t at = (int64_t)r * it.x_pitch + c;
+            if (r >= rows || c >= cols || !APOLLO_DBG_RANGE(at, at + 7, extent, status)) continue;
+            uint32_t w[4], l[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float v0 = u[i][2 * e] * f, v1 = u[i][2 * e + 1] * f;
+                w[e] = pack_half2(v0, v1);
+                if constexpr (SPLIT) {
+                    const float2 h = unpack_half2(w[e]);
+                    l[e] = pack_half2(v0 - h.x, v1 - h.y);
+                }
+            }
+            *reinterpret_cast<uint4*>(hi + at) = make_uint4(w[0], w[1], w[2], w[3]);
+            if constexpr (SPLIT) *reinterpret_cast<uint4*>(lo + at) = make_uint4(l[0], l[1], l[2], l[3]);
+        }
+        return;
+    }
+    // two columns per thread (a pair of elements is read at once where rows are whole pairs), eight rows
+    const int c = (threadIdx.x & 31) * 2, rr = threadIdx.x >> 5;
+    float u[8][2];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = r0 + rr + 8 * i;
+        const int64_t at = (int64_t)r * cols + c0 + c;
+        float m[2];
+        load_pair(G, at, r < rows ? cols - c0 - c : 0, cols % 2 == 0, numel, u[i], status);
+        if constexpr (STEP) load_pair(M, at, r < rows ? cols - c0 - c : 0, cols % 2 == 0, numel, m, status);
+        u[i][0] = update_of<STEP>(u[i][0], m[0], a);
+        u[i][1] = update_of<STEP>(u[i][1], m[1], a);
+    }
+    const float f = factor();
+    // two neighbours of one row of X (its pitch is a multiple of 64: pairs are always aligned)
+    auto put = [&](int64_t at, float v0, float v1) {
+        if (!APOLLO_DBG_RANGE(at, at + 1, extent, status)) return;
+        const uint32_t w = pack_half2(v0, v1);
+        *reinterpret_cast<uint32_t*>(hi + at) = w;
+        if constexpr (SPLIT) {
+            const float2 h = unpack_half2(w);
+            *reinterpret_cast<uint32_t*>(lo + at) = pack_half2(v0 - h.x, v1 - h.y);
+        }
     };
     if (!it.tall) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int r = r0 + rr + 4 * i;
-            if (r < rows && c0 + c < cols) put((int64_t)r * it.x_pitch + c0 + c, u[i] * f);
+        for (int i = 0; i < 8; ++i) {
+            const int r = r0 + rr + 8 * i;
+            if (r < rows && c0 + c < cols) put((int64_t)r * it.x_pitch + c0 + c, u[i][0] * f, u[i][1] * f);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) tile[rr + 4 * i][c] = u[i] * f;
+        for (int i = 0; i < 8; ++i) { tile[rr + 8 * i][c] = u[i][0] * f; tile[rr + 8 * i][c + 1] = u[i][1] * f; }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int cc = rr + 4 * i;                   // source column = row of X
-            if (c0 + cc < cols && r0 + c < rows) put((int64_t)(c0 + cc) * it.x_pitch + r0 + c, tile[c][cc]);
+        for (int i = 0; i < 8; ++i) {
+            const int cc = rr + 8 * i;                   // source column = row of X
+            if (c0 + cc < cols && r0 + c < rows) put((int64_t)(c0 + cc) * it.x_pitch + r0 + c, tile[c][cc], tile[c + 1][cc]);
         }
     }
 }
@@ -511,47 +571,100 @@ muon_apply_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ stat
     T* __restrict__ W = static_cast<T*>(it.w);
     const __half* hi = it.x[0];
     const __half* lo = it.x[1];
-    const int c = threadIdx.x & 63, rr = threadIdx.x >> 6;
     const float f = 1.0f / a.x_scale;                    // a power of two
-    const int64_t extent = (int64_t)(it.tall ? cols : rows) * it.x_pitch;
-    auto get = [&](int64_t at) {
-        if (!APOLLO_DBG_RANGE(at, at, extent, status)) return 0.0f;
-        float v = __half2float(hi[at]);
-        if constexpr (SPLIT) v += __half2float(lo[at]);
-        return v * f;
+    const int64_t numel = (int64_t)rows * cols, extent = (int64_t)(it.tall ? cols : rows) * it.x_pitch;
+    auto moved = [&](float w, float x) {
+        if constexpr (STEP) return fmaf(-a.lr, fmaf(a.wd, w, it.gain * x), w);
+        return x;
     };
-    float x[16];
+    if (!it.tall && cols % 8 == 0) {
+        const int c = c0 + (threadIdx.x & 7) * 8, r1 = r0 + (threadIdx.x >> 3);
+        uint4 x[2], y[SPLIT ? 2 : 1];
+        float w[2][8];
+        bool in[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = r1 + 32 * i;
+            const int64_t at = (int64_t)r * it.x_pitch + c, aw = (int64_t)r * cols + c;
+            in[i] = r < rows && c < cols && APOLLO_DBG_RANGE(at, at + 7, extent, status) && APOLLO_DBG_RANGE(aw, aw + 7, numel, status);
+            if (!in[i]) continue;
+            x[i] = __ldcs(reinterpret_cast<const uint4*>(hi + at));
+            if constexpr (SPLIT) y[i] = __ldcs(reinterpret_cast<const uint4*>(lo + at));
+            if constexpr (STEP) load8_stream(W + aw, w[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (!in[i]) continue;
+            const uint32_t xw[4] = { x[i].x, x[i].y, x[i].z, x[i].w };
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float2 h = unpack_half2(xw[e]);
+                v[2 * e] = h.x; v[2 * e + 1] = h.y;
+            }
+            if constexpr (SPLIT) {
+                const uint32_t yw[4] = { y[i].x, y[i].y, y[i].z, y[i].w };
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 h = unpack_half2(yw[e]);
+                    v[2 * e] += h.x; v[2 * e + 1] += h.y;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = moved(STEP ? w[i][e] : 0.0f, v[e] * f);
+            store8(W + (int64_t)(r1 + 32 * i) * cols + c, v);
+        }
+        return;
+    }
+    const int c = (threadIdx.x & 31) * 2, rr = threadIdx.x >> 5;
+    auto get = [&](int64_t at, float (&v)[2]) {          // two neighbours of one row of X; the second may be padding
+        if (!APOLLO_DBG_RANGE(at, at + 1, extent, status)) { v[0] = v[1] = 0.0f; return; }
+        float2 h = unpack_half2(*reinterpret_cast<const uint32_t*>(hi + at));
+        if constexpr (SPLIT) {
+            const float2 l = unpack_half2(*reinterpret_cast<const uint32_t*>(lo + at));
+            h.x += l.x; h.y += l.y;
+        }
+        v[0] = h.x * f; v[1] = h.y * f;
+    };
+    float x[8][2];
     if (!it.tall) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int r = r0 + rr + 4 * i;
-            x[i] = r < rows && c0 + c < cols ? get((int64_t)r * it.x_pitch + c0 + c) : 0.0f;
+        for (int i = 0; i < 8; ++i) {
+            const int r = r0 + rr + 8 * i;
+            if (r < rows && c0 + c < cols) get((int64_t)r * it.x_pitch + c0 + c, x[i]);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int cc = rr + 4 * i;
-            tile[c][cc] = c0 + cc < cols && r0 + c < rows ? get((int64_t)(c0 + cc) * it.x_pitch + r0 + c) : 0.0f;
+        for (int i = 0; i < 8; ++i) {
+            const int cc = rr + 8 * i;
+            float v[2] = { 0.0f, 0.0f };
+            if (c0 + cc < cols && r0 + c < rows) get((int64_t)(c0 + cc) * it.x_pitch + r0 + c, v);
+            tile[c][cc] = v[0]; tile[c + 1][cc] = v[1];
         }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = tile[rr + 4 * i][c];
+        for (int i = 0; i < 8; ++i) { x[i][0] = tile[rr + 8 * i][c]; x[i][1] = tile[rr + 8 * i][c + 1]; }
     }
-    float w[16];
+    float w[8][2];
     if constexpr (STEP) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int r = r0 + rr + 4 * i;
-            w[i] = r < rows && c0 + c < cols ? load1(W + (int64_t)r * cols + c0 + c) : 0.0f;
+        for (int i = 0; i < 8; ++i) {
+            const int r = r0 + rr + 8 * i;
+            load_pair(W, (int64_t)r * cols + c0 + c, r < rows ? cols - c0 - c : 0, cols % 2 == 0, numel, w[i], status);
         }
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int r = r0 + rr + 4 * i;
+    for (int i = 0; i < 8; ++i) {
+        const int r = r0 + rr + 8 * i, left = r < rows ? cols - c0 - c : 0;
         const int64_t at = (int64_t)r * cols + c0 + c;
-        if (r >= rows || c0 + c >= cols || !APOLLO_DBG_RANGE(at, at, (int64_t)rows * cols, status)) continue;
-        if constexpr (STEP) store_elem(W + at, fmaf(-a.lr, fmaf(a.wd, w[i], it.gain * x[i]), w[i]));
-        else store_elem(W + at, x[i]);
+        const float v[2] = { moved(STEP ? w[i][0] : 0.0f, x[i][0]), moved(STEP ? w[i][1] : 0.0f, x[i][1]) };
+        if (left >= 2 && cols % 2 == 0) {
+            if (APOLLO_DBG_RANGE(at, at + 1, numel, status)) store2(W + at, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (e < left && APOLLO_DBG_RANGE(at + e, at + e, numel, status)) store_elem(W + at + e, v[e]);
+        }
     }
 }
 
@@ -631,21 +744,21 @@ cudaError_t launch_muon_gemm(bool split, const GemmOp* d_ops, const int* d_prefi
     return cudaLaunchKernelEx(&cfg, kernel, d_ops, d_prefix, n_ops, tiles, d_status);
 }
 
-int muon_encode_maps(const __half* base, int rows, int cols, int pitch, void* load, void* store, void* mirror)
+int muon_encode_maps(const __half* base, int rows, int cols, int pitch, void* maps)
 {
     EncodeTiledFn encode = encode_fn();
     if (!encode) return APOLLO_ERR_CUDA;
     const cuuint64_t dims[2] = { (cuuint64_t)cols, (cuuint64_t)rows };
     const cuuint64_t strides[1] = { (cuuint64_t)pitch * 2 };
     const cuuint32_t elem[2] = { 1u, 1u };
-    auto make = [&](void* out, cuuint32_t w, cuuint32_t h, CUtensorMapSwizzle sw) {
+    auto make = [&](int kind, cuuint32_t w, cuuint32_t h, CUtensorMapSwizzle sw) {
         const cuuint32_t box[2] = { w, h };
-        return encode(static_cast<CUtensorMap*>(out), CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<__half*>(base), dims, strides, box, elem,
+        return encode(static_cast<CUtensorMap*>(maps) + kind, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<__half*>(base), dims, strides, box, elem,
                       CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     };
-    if (!make(load, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B) || !make(store, 64, 32, CU_TENSOR_MAP_SWIZZLE_128B)) return APOLLO_ERR_CUDA;
-    if (mirror && !make(mirror, 32, 64, CU_TENSOR_MAP_SWIZZLE_NONE)) return APOLLO_ERR_CUDA;
-    return APOLLO_OK;
+    return make(MAP_ROWS, 64, 128, CU_TENSOR_MAP_SWIZZLE_128B) && make(MAP_COLS, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B) &&
+           make(MAP_STORE, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B) && make(MAP_MIRROR, 32, 32, CU_TENSOR_MAP_SWIZZLE_NONE)
+               ? APOLLO_OK : APOLLO_ERR_CUDA;
 }
 
 }  // namespace apollo

@@ -15,10 +15,10 @@ constexpr int MUON_PART = 256;          // most partial sums of squares per matr
 // parts of split operands.  sym: M = N and the result is symmetric: tiles on and above the diagonal are computed,
 // the ones above also written transposed.
 struct GemmOp {
-    const void* l_map[2];               // DEVICE tensor maps (boxes of 64 x 64)
+    const void* l_map[2];               // DEVICE tensor maps
     const void* r_map[2];
-    const void* out_map[2];             // boxes of 64 x 32 rows
-    const void* mir_map[2];             // boxes of 32 x 64 rows (sym)
+    const void* out_map[2];
+    const void* mir_map[2];             // sym
     const __half* e1[2];                // same place and pitch as the output; null = none
     const __half* e2[2];
     float alpha, b1, b2, diag;
@@ -62,8 +62,10 @@ int muon_stream_tiles(int rows, int cols);
 cudaError_t launch_muon_gemm(bool split, const GemmOp* d_ops, const int* d_prefix, int n_ops, int tiles, MuonLaunch& state,
                              int32_t* d_status, cudaStream_t stream);
 
-// Tensor maps of a rows x cols matrix of 16-bit floats (pitch a multiple of 8): what the products load, store and
-// store transposed.  `out`: 128 bytes each.
-int muon_encode_maps(const __half* base, int rows, int cols, int pitch, void* load, void* store, void* mirror);
+// Tensor maps of a rows x cols matrix of 16-bit floats (pitch a multiple of 8), 128 bytes each at maps[kind]:
+// boxes of 64 x 128 rows (an operand whose rows are contiguous along k), 64 x 64 (along n), and 32 x 32 to store a
+// piece, and to store it transposed.
+enum { MAP_ROWS, MAP_COLS, MAP_STORE, MAP_MIRROR, MUON_MAPS };
+int muon_encode_maps(const __half* base, int rows, int cols, int pitch, void* maps);
 
 }  // namespace apollo
