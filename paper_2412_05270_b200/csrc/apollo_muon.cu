@@ -1,8 +1,9 @@
 // Host side of the orthogonalised update: validation, workspace planning, the products of every phase, launches.
 //
 // The iteration X <- a X + (b A + c A^2) X, A = X X^T, is a sequence of products that depend on one another; the
-// matrices of a list do not.  So a list is worked on in groups, and a launch (a phase) does the p-th product of
-// every matrix of its group.  Two ways to take two steps, whichever has fewer tile k-blocks for the matrix:
+// matrices of a list do not.  So a list is worked on in groups, one launch for all products of a group, whose tiles
+// are listed product by product: the first product of every matrix, the second of every matrix, and so on.
+// Two ways to take two steps, whichever has fewer tile k-blocks for the matrix:
 //   one by one   A = X X^T, B = b A + c A^2, X <- a X + B X, twice
 //   together     A, B as before; P = a I + B;  T = P A, A' = P T (= X' X'^T of the step in between, without X'),
 //                B' = b A' + c A'^2, Q = P' P, X <- Q X
@@ -32,6 +33,7 @@ namespace {
 constexpr size_t ALIGN = 256;
 constexpr int MAX_SIDE = 1 << 20;
 constexpr double Q_SHIFT = 1.0;
+constexpr int WIDE_TILES = 148;
 
 size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
 int round_up(int x, int to) { return (x + to - 1) / to * to; }
@@ -43,11 +45,10 @@ struct Mat {
     size_t maps;                         // offset of its tensor maps
 };
 
-struct Phase { int op_begin, n_ops, prefix_begin, tiles; };
-
 struct Group {
     std::vector<int> mats;
-    std::vector<Phase> phases;
+    int bn;                              // columns of a tile
+    int64_t tile_begin, tiles;           // in the list of tiles
 };
 
 // The powers of two that stored values carry, and the constants of the iteration.
@@ -56,8 +57,9 @@ struct Scales { double x, a, b, t, q, shift; };
 struct Plan {
     std::vector<Mat> mats;
     std::vector<Group> groups;
-    size_t off_status, off_table, table_bytes, off_maps, off_ops, off_prefix, total;
-    int n_ops, n_prefix, maps_per_mat, parts;
+    size_t off_status, off_counters, off_table, table_bytes, off_maps, off_ops, off_list, total;
+    int n_ops, maps_per_mat, parts;
+    int64_t n_tiles;
     Scales sc;
 };
 
@@ -108,16 +110,33 @@ int validate(const apollo_muon_config* cfg, Scales& sc)
     return find_scales(*cfg, sc) ? APOLLO_OK : APOLLO_ERR_INVALID_ARG;
 }
 
+int tiles_of(int x, int per) { return (x + per - 1) / per; }
+
+// Tiles of a symmetric m x m product: 256-row blocks against the columns from the block's own on.
+int64_t sym_tiles(int m, int bn)
+{
+    int64_t t = 0;
+    for (int tm = 0; tm < tiles_of(m, MUON_TILE); ++tm) t += tiles_of(m, bn) - (int64_t)tm * (MUON_TILE / bn);
+    return t;
+}
+
 // Tile k-blocks of one step, and of two steps together: what a pair of CTAs works off.
 void costs(int m, int n, double& one, double& two)
 {
-    const double t = (m + MUON_TILE - 1) / MUON_TILE, u = (n + MUON_TILE - 1) / MUON_TILE, km = (m + 63) / 64, kn = (n + 63) / 64;
-    const double sym = t * (t + 1) / 2;
-    one = sym * kn + sym * km + t * u * km;
-    two = sym * kn + 5 * sym * km + t * u * km;
+    const double km = tiles_of(m, 64), kn = tiles_of(n, 64), sym = (double)sym_tiles(m, MUON_TILE);
+    const double up = (double)tiles_of(m, MUON_TILE) * tiles_of(n, MUON_TILE) * km;
+    one = sym * kn + sym * km + up;
+    two = sym * kn + 5 * sym * km + up;
 }
 
-int phases_of(const Mat& m, int steps) { return m.together ? steps / 2 * 7 + steps % 2 * 3 : steps * 3; }
+// Products of a matrix: A and B, then one by one: X, or together: T, A', B', Q, X.
+int products_of(const Mat& m, int steps) { return m.together ? steps / 2 * 7 + steps % 2 * 3 : steps * 3; }
+int updates_of(const Mat& m, int steps) { return m.together ? (steps + 1) / 2 : steps; }
+int64_t all_tiles(const Mat& m, int steps, int bn)
+{
+    const int up = updates_of(m, steps);
+    return up * ((int64_t)tiles_of(m.m, MUON_TILE) * tiles_of(m.n, bn)) + (products_of(m, steps) - up) * sym_tiles(m.m, bn);
+}
 
 int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_config* cfg, Plan& plan)
 {
@@ -172,24 +191,29 @@ int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_confi
         largest = std::max(largest, used);
         plan.groups.back().mats.push_back(i);
     }
-    plan.n_ops = 0; plan.n_prefix = 0;
+    plan.n_ops = 0; plan.n_tiles = 0;
     for (Group& g : plan.groups) {
-        int phases = 0;
-        for (int i : g.mats) phases = std::max(phases, phases_of(plan.mats[i], cfg->ns_steps));
-        for (int p = 0; p < phases; ++p) {
-            Phase ph = { plan.n_ops, 0, plan.n_prefix, 0 };
-            for (int i : g.mats) ph.n_ops += p < phases_of(plan.mats[i], cfg->ns_steps) ? 1 : 0;
-            plan.n_ops += ph.n_ops;
-            plan.n_prefix += ph.n_ops + 1;
-            g.phases.push_back(ph);
+        // Wide tiles move the fewest bytes per product; narrow ones halve the latency of a product and give twice as
+        // many: taken when the smallest product of the group would not fill the chip twice over.
+        int64_t sym = 0;
+        for (int i : g.mats) sym += sym_tiles(plan.mats[i].m, 256);
+        g.bn = sym >= WIDE_TILES ? 256 : 128;
+        g.tile_begin = plan.n_tiles;
+        g.tiles = 0;
+        for (int i : g.mats) {
+            g.tiles += all_tiles(plan.mats[i], cfg->ns_steps, g.bn);
+            plan.n_ops += products_of(plan.mats[i], cfg->ns_steps);
         }
+        if (g.tiles > INT32_MAX / 2) return APOLLO_ERR_SHAPE;
+        plan.n_tiles += g.tiles;
     }
     size_t off = 0;
     plan.off_status = off; off += ALIGN;
+    plan.off_counters = off; off = align_up(off + sizeof(uint32_t) * ((size_t)n_mat + 1));   // the ticket, then one per matrix
     plan.off_table = off;
     plan.off_maps = off; off = align_up(off + 128 * (size_t)plan.maps_per_mat * n_mat);
     plan.off_ops = off; off = align_up(off + sizeof(GemmOp) * (size_t)plan.n_ops);
-    plan.off_prefix = off; off = align_up(off + sizeof(int) * (size_t)plan.n_prefix);
+    plan.off_list = off; off = align_up(off + sizeof(uint4) * (size_t)plan.n_tiles);
     plan.table_bytes = off - plan.off_table;
     for (int i = 0; i < n_mat; ++i) {
         Mat& m = plan.mats[i];
@@ -218,8 +242,9 @@ struct apollo_muon_ctx {
 namespace {
 
 // The products of one matrix, in order.
-void ops_of(const apollo_muon_ctx* ctx, const Mat& m, std::vector<GemmOp>& out)
+void ops_of(const apollo_muon_ctx* ctx, int index, int bn, std::vector<GemmOp>& out)
 {
+    const Mat& m = ctx->plan.mats[index];
     const Plan& plan = ctx->plan;
     const Scales& sc = plan.sc;
     const double a = ctx->cfg.coef[0], b = ctx->cfg.coef[1], c = ctx->cfg.coef[2], p = a - sc.shift;
@@ -229,12 +254,22 @@ void ops_of(const apollo_muon_ctx* ctx, const Mat& m, std::vector<GemmOp>& out)
     auto s_map = [&](int buf, int h, int kind) { return x_map(2 + buf, h, kind); };
     auto x_ptr = [&](int buf, int h) { return (const __half*)(ws + m.x[buf][h]); };
     auto s_ptr = [&](int buf, int h) { return (const __half*)(ws + m.s[buf][h]); };
+    // the load of R: 128 rows of a 256-column tile at once, else boxes of 64
+    const int r_kind = bn == 256 ? MAP_ROWS : MAP_COLS;
+    uint32_t* counter = reinterpret_cast<uint32_t*>(ws + plan.off_counters) + 1 + index;
+    uint32_t done = 0;
+    auto push = [&](GemmOp& o) {
+        o.counter = counter;
+        o.need = done;
+        done += MUON_WARPS_PER_TILE * (uint32_t)(o.sym ? sym_tiles(o.M, bn) : (int64_t)tiles_of(o.M, MUON_TILE) * tiles_of(o.N, bn));
+        out.push_back(o);
+    };
     auto square = [&](int l, int r, int dst, double alpha, int e1, double b1, int e2, double b2, double diag, bool of_x) {
         GemmOp o;
         std::memset(&o, 0, sizeof(o));
         for (int h = 0; h < parts; ++h) {
             o.l_map[h] = of_x ? x_map(l, h, MAP_ROWS) : s_map(l, h, MAP_ROWS);
-            o.r_map[h] = of_x ? x_map(r, h, MAP_ROWS) : s_map(r, h, MAP_ROWS);
+            o.r_map[h] = of_x ? x_map(r, h, r_kind) : s_map(r, h, r_kind);
             o.out_map[h] = s_map(dst, h, MAP_STORE);
             o.mir_map[h] = s_map(dst, h, MAP_MIRROR);
             if (e1 >= 0) o.e1[h] = s_ptr(e1, h);
@@ -242,9 +277,8 @@ void ops_of(const apollo_muon_ctx* ctx, const Mat& m, std::vector<GemmOp>& out)
         }
         o.alpha = (float)alpha; o.b1 = (float)b1; o.b2 = (float)b2; o.diag = (float)diag;
         o.M = o.N = m.m; o.K = of_x ? m.n : m.m; o.e_pitch = m.pitch_s;
-        o.tiles_m = o.tiles_n = (m.m + MUON_TILE - 1) / MUON_TILE;
         o.sym = 1;
-        out.push_back(o);
+        push(o);
     };
     auto update = [&](int s, int src, double alpha, double b1) {
         GemmOp o;
@@ -257,9 +291,8 @@ void ops_of(const apollo_muon_ctx* ctx, const Mat& m, std::vector<GemmOp>& out)
         }
         o.alpha = (float)alpha; o.b1 = (float)b1;
         o.M = m.m; o.N = m.n; o.K = m.m; o.e_pitch = m.pitch_x;
-        o.tiles_m = (m.m + MUON_TILE - 1) / MUON_TILE; o.tiles_n = (m.n + MUON_TILE - 1) / MUON_TILE;
         o.r_mn = 1;
-        out.push_back(o);
+        push(o);
     };
     int x = 0;
     for (int k = 0; k < ctx->cfg.ns_steps;) {
@@ -286,7 +319,6 @@ int build_table(apollo_muon_ctx* ctx)
     Plan& plan = ctx->plan;
     char* t = ctx->table;                                   // corresponds to ws + off_table
     auto at = [&](size_t off) { return t + (off - plan.off_table); };
-    std::vector<std::vector<GemmOp>> ops(plan.mats.size());
     for (size_t i = 0; i < plan.mats.size(); ++i) {
         const Mat& m = plan.mats[i];
         char* maps = at(m.maps);
@@ -296,28 +328,32 @@ int build_table(apollo_muon_ctx* ctx)
                 const int rc = muon_encode_maps((const __half*)(ctx->ws + at_ws), m.m, b < 2 ? m.n : m.m, b < 2 ? m.pitch_x : m.pitch_s, maps);
                 if (rc != APOLLO_OK) return rc;
             }
-        ops_of(ctx, m, ops[i]);
     }
     GemmOp* d_ops = reinterpret_cast<GemmOp*>(at(plan.off_ops));
-    int* prefix = reinterpret_cast<int*>(at(plan.off_prefix));
-    for (Group& g : plan.groups) {
-        for (size_t p = 0; p < g.phases.size(); ++p) {
-            Phase& ph = g.phases[p];
-            std::vector<const GemmOp*> list;
-            for (int i : g.mats)
-                if (p < ops[i].size()) list.push_back(&ops[i][p]);
-            // tiles are dealt out in order: the longest ones first, so that the last ones dealt are short
-            std::stable_sort(list.begin(), list.end(), [](const GemmOp* x, const GemmOp* y) { return x->K > y->K; });
-            int64_t tiles = 0;
-            for (size_t k = 0; k < list.size(); ++k) {
-                d_ops[ph.op_begin + k] = *list[k];
-                prefix[ph.prefix_begin + k] = (int)tiles;
-                tiles += list[k]->sym ? (int64_t)list[k]->tiles_m * (list[k]->tiles_m + 1) / 2 : (int64_t)list[k]->tiles_m * list[k]->tiles_n;
-                if (tiles > INT32_MAX) return APOLLO_ERR_SHAPE;
-            }
-            prefix[ph.prefix_begin + list.size()] = (int)tiles;
-            ph.tiles = (int)tiles;
+    uint4* list = reinterpret_cast<uint4*>(at(plan.off_list));
+    int op = 0;
+    for (const Group& g : plan.groups) {
+        std::vector<std::vector<GemmOp>> ops(g.mats.size());
+        size_t products = 0;
+        for (size_t k = 0; k < g.mats.size(); ++k) {
+            ops_of(ctx, g.mats[k], g.bn, ops[k]);
+            products = std::max(products, ops[k].size());
         }
+        uint4* out = list + g.tile_begin;
+        for (size_t p = 0; p < products; ++p)
+            for (size_t k = 0; k < g.mats.size(); ++k) {
+                if (p >= ops[k].size()) continue;
+                const GemmOp& o = ops[k][p];
+                d_ops[op] = o;
+                const int rows = tiles_of(o.M, MUON_TILE), cols = tiles_of(o.N, g.bn), per = MUON_TILE / g.bn;
+                const uint32_t kb = (uint32_t)(plan.parts == 2 ? 3 : 1) * (uint32_t)tiles_of(o.K, 64);
+                // column by column: the tiles at work at one time share few columns of R and all rows of L
+                for (int tn = 0; tn < cols; ++tn)
+                    for (int tm = 0; tm < (o.sym ? std::min(rows, tn / per + 1) : rows); ++tm)
+                        *out++ = make_uint4((uint32_t)op, (uint32_t)tm | (uint32_t)tn << 16, kb, (uint32_t)o.r_mn);
+                ++op;
+            }
+        if (out != list + g.tile_begin + g.tiles) return APOLLO_ERR_INVALID_ARG;      // the plan counted otherwise
     }
     return APOLLO_OK;
 }
@@ -349,7 +385,8 @@ int run(apollo_muon_ctx* ctx, void* const* d_W, const void* const* d_G, float* c
         }
     }
     const GemmOp* d_ops = reinterpret_cast<const GemmOp*>(ctx->ws + plan.off_ops);
-    const int* d_prefix = reinterpret_cast<const int*>(ctx->ws + plan.off_prefix);
+    const uint4* d_list = reinterpret_cast<const uint4*>(ctx->ws + plan.off_list);
+    uint32_t* d_ticket = reinterpret_cast<uint32_t*>(ctx->ws + plan.off_counters);
     const int dtype = ctx->cfg.dtype;
     int launches = 0;
     cudaError_t err = cudaSuccess;
@@ -360,18 +397,18 @@ int run(apollo_muon_ctx* ctx, void* const* d_W, const void* const* d_G, float* c
                 MuonArgs a;
                 a.n = (int)std::min<size_t>(MUON_CHUNK, g.mats.size() - at);
                 a.mu = ctx->cfg.momentum; a.eps = ctx->cfg.eps; a.x_scale = (float)plan.sc.x; a.lr = lr; a.wd = wd; a.nesterov = ctx->cfg.nesterov;
+                a.ticket = d_ticket;
                 int64_t tiles = 0;
                 for (int k = 0; k < a.n; ++k) {
                     const int i = g.mats[at + k];
                     const Mat& m = plan.mats[i];
                     MuonItem& it = a.item[k];
-                    const int steps = ctx->cfg.ns_steps;
-                    const int updates = m.together ? (steps + 1) / 2 : steps;
-                    const int buf = which == 2 ? updates & 1 : 0;
+                    const int buf = which == 2 ? updates_of(m, ctx->cfg.ns_steps) & 1 : 0;
                     it.w = d_W[i]; it.g = d_G[i]; it.m = step ? d_M[i] : nullptr;
                     it.x[0] = reinterpret_cast<__half*>(ctx->ws + m.x[buf][0]);
                     it.x[1] = plan.parts == 2 ? reinterpret_cast<__half*>(ctx->ws + m.x[buf][1]) : nullptr;
                     it.part = reinterpret_cast<double*>(ctx->ws + m.part);
+                    it.counter = d_ticket + 1 + i;
                     it.rows = m.rows; it.cols = m.cols; it.x_pitch = m.pitch_x; it.n_part = m.n_part; it.tall = m.tall;
                     it.gain = (float)gain_of(ctx->cfg, m);
                     a.tile_begin[k] = (int)tiles;
@@ -387,9 +424,8 @@ int run(apollo_muon_ctx* ctx, void* const* d_W, const void* const* d_G, float* c
         };
         pass(0);
         pass(1);
-        for (const Phase& ph : g.phases) {
-            if (err != cudaSuccess) break;
-            err = launch_muon_gemm(plan.parts == 2, d_ops + ph.op_begin, d_prefix + ph.prefix_begin, ph.n_ops, ph.tiles, ctx->launch, d_status, stream);
+        if (err == cudaSuccess) {
+            err = launch_muon_gemm(plan.parts == 2, g.bn, d_ops, d_list + g.tile_begin, (int)g.tiles, d_ticket, ctx->launch, d_status, stream);
             ++launches;
         }
         pass(2);
@@ -445,7 +481,7 @@ int apollo_muon_create(apollo_muon_ctx** out_ctx, const apollo_shape* shapes, in
             ctx->ws = static_cast<char*>(d_workspace);
             ctx->first = true;
             ctx->last_launches = 0;
-            ctx->launch = MuonLaunch{ sms, 0, false };
+            ctx->launch = MuonLaunch{ sms, { 0, 0 } };
             void* host = nullptr;
             if (cudaHostAlloc(&host, ctx->plan.table_bytes, cudaHostAllocDefault) == cudaSuccess) {
                 ctx->pinned = true;

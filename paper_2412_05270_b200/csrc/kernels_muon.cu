@@ -4,8 +4,8 @@
 //                   accumulators in TMEM, so that the epilogue of a tile runs under the main loop of the next
 // muon_moment / muon_load / muon_apply   the streaming passes before and after
 //
-// A product's tile is 256 x 256: each CTA of a pair loads its 128 rows of L and half of the 256 columns of R, 32 KB
-// per 64-deep k-block, six stages; four MMAs of 256 x 256 x 16 consume them.  Roles of the 12 warps: 0 TMA producer,
+// A product's tile is 256 x 256 (256 x 128 in short lists): each CTA of a pair loads its 128 rows of L and half of the
+// columns of R, 32 KB per 64-deep k-block, six stages; four MMAs of 256 x 256 x 16 consume them.  Roles of the 12 warps: 0 TMA producer,
 // 1 MMA issuer (leader CTA) and TMEM owner, 4-11 epilogue (a warp reads the 32 TMEM lanes it may read and one half
 // of the columns).  The epilogue adds the terms that the iteration needs beside the product, rounds to 16 bits and
 // hands 32 x 32 pieces to TMA stores; a symmetric product's tile above the diagonal is stored a second time,
@@ -26,14 +26,33 @@ namespace apollo {
 namespace {
 
 constexpr int MG_THREADS = 384;
-constexpr int MG_STAGES = 6;
 constexpr int MG_HALF = 8192;                            // 64 x 64 16-bit floats: one TMA box
 constexpr int MG_OPERAND = 2 * MG_HALF;                  // a CTA's 128 rows of L, or half of R
-constexpr int MG_STAGE = 2 * MG_OPERAND;
 constexpr int MG_EPI_WARPS = 8;
 constexpr int MG_STAGING = MG_EPI_WARPS * 4096;          // per epilogue warp: 2 KB as stored, 2 KB transposed
-constexpr int MG_SMEM = MG_STAGES * MG_STAGE + MG_STAGING + 256 + 1024;
-static_assert(MG_SMEM <= 227 * 1024, "shared memory of a CTA");
+template <int BN> struct GemmCfg {
+    static constexpr int STAGE = MG_OPERAND + BN * 64;   // 128 rows of L and BN / 2 of R, 64 deep
+    static constexpr int STAGES = BN == 256 ? 6 : 8;
+    static constexpr int SMEM = STAGES * STAGE + MG_STAGING + 320 + 1024;
+    static_assert(SMEM <= 227 * 1024 && STAGES <= 8, "shared memory and barriers of a CTA");
+};
+
+// Bounded wait until *counter >= need, polling every `ns` nanoseconds; a set status word ends it at once.
+__device__ __forceinline__ bool wait_count(const uint32_t* counter, uint32_t need, uint32_t ns, volatile int* abort_flag,
+                                           int32_t* status, int where)
+{
+    if (need == 0 || ld_acquire_gpu(counter) >= need) return true;
+    if (*abort_flag) return false;
+    for (uint32_t i = 0; i < TC_WAIT_CAP; ++i) {
+        __nanosleep(ns);
+        if (ld_acquire_gpu(counter) >= need) return true;
+        if ((i & 63u) == 63u && *reinterpret_cast<volatile int32_t*>(status) != STATUS_OK) break;
+    }
+    *abort_flag = 1;
+    atomicCAS(status + 1, 0, where);
+    atomicExch(status, STATUS_TIMEOUT);
+    return false;
+}
 
 __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
@@ -70,36 +89,54 @@ __device__ __forceinline__ void add_term(float (&v)[32], float b, const uint4 (&
 __device__ __forceinline__ void load_term(uint4 (&e)[4], const __half* p, bool in)
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) e[i] = in ? *(reinterpret_cast<const uint4*>(p) + i) : make_uint4(0, 0, 0, 0);
+    for (int i = 0; i < 4; ++i) e[i] = in ? __ldcg(reinterpret_cast<const uint4*>(p) + i) : make_uint4(0, 0, 0, 0);
 }
 
 }  // namespace
 
+// One launch does all products of a group: the host lists the tiles of the first product of every matrix, then those of
+// the second, and so on, and the pairs draw them in this order.  A tile waits (bounded) until the products before its
+// own are complete for ITS matrix: a counter per matrix, one count per epilogue warp and tile, added after the warp's
+// stores have landed.  Whoever runs draws the next tile, so the earliest unfinished one is always at work and waits
+// for nothing that is not: no CTA has to be resident for another to finish.  With several matrices the products before
+// are complete by the time a tile comes up, and there is neither a launch nor a drained pipeline between products.
+// (Dealing the tiles out by index instead let the pairs drift apart where long and short contractions meet; what
+// neighbours share then no longer met in L2: a 7B layer took 12.9 ms instead of 11.6 ms, at equal cycles.)
+// The leader's producer thread draws: the ticket at the start of a tile, the entry of the list a few k-blocks later,
+// from where st.async puts it into a ring of four slots in both CTAs (`sched` barriers), one tile ahead of its use.
+//
 // SPLIT: operands are sums of two 16-bit floats, and the contraction runs over three segments into one accumulator:
-// hi hi + lo hi + hi lo (what is dropped, lo lo, is 2^-24 of a term).
-template <bool SPLIT>
+// hi hi + lo hi + hi lo (what is dropped, lo lo, is 2^-24 of a term).  BN: columns of a tile.
+template <bool SPLIT, int BN>
 __global__ void __launch_bounds__(MG_THREADS, 1)
-muon_gemm_kernel(const GemmOp* __restrict__ ops, const int* __restrict__ prefix, int n_ops, int tiles, int32_t* __restrict__ status)
+muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list, uint32_t tiles, uint32_t* __restrict__ ticket,
+                 int32_t* __restrict__ status)
 {
+    using Cfg = GemmCfg<BN>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (ptx::smem_addr(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem_gen = smem_raw + (smem_base - ptx::smem_addr(smem_raw));
-    const uint32_t staging = smem_base + MG_STAGES * MG_STAGE;
+    const uint32_t staging = smem_base + Cfg::STAGES * Cfg::STAGE;
     const uint32_t bars = staging + MG_STAGING;
-    const uint32_t bar_full = bars, bar_done = bars + 64, bar_acc_full = bars + 128, bar_acc_empty = bars + 144, bar_drain = bars + 160;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + MG_STAGES * MG_STAGE + MG_STAGING + 176);
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + MG_STAGES * MG_STAGE + MG_STAGING + 180);
+    const uint32_t bar_full = bars, bar_done = bars + 64, bar_acc_full = bars + 128, bar_acc_empty = bars + 144, bar_drain = bars + 160,
+                   bar_sched_full = bars + 192, bar_sched_empty = bars + 224, slots = bars + 256;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + Cfg::STAGES * Cfg::STAGE + MG_STAGING + 176);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + Cfg::STAGES * Cfg::STAGE + MG_STAGING + 180);
 
     const uint32_t rank = ptx::cluster_ctarank();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
-        for (int s = 0; s < MG_STAGES; ++s) {
+        for (int s = 0; s < Cfg::STAGES; ++s) {
             ptx::mbar_init(bar_full + 8 * s, 1);         // the leader's arrive.expect_tx for the bytes of both CTAs
             ptx::mbar_init(bar_done + 8 * s, 1);         // the leader's commit
         }
         for (int b = 0; b < 2; ++b) {
             ptx::mbar_init(bar_acc_full + 8 * b, 1);
             ptx::mbar_init(bar_acc_empty + 8 * b, 2 * MG_EPI_WARPS);
+        }
+        for (int b = 0; b < 4; ++b) {
+            ptx::mbar_init(bar_sched_full + 8 * b, 1);                            // this CTA's producer, and the entry's 16 bytes
+            ptx::mbar_init(bar_sched_empty + 8 * b, 2 * MG_EPI_WARPS + 2);        // leader's copy: all readers but the writer
         }
         ptx::mbar_init(bar_drain, 1);
         *abort_flag = 0;
@@ -114,81 +151,88 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const int* __restrict__ prefix,
     ptx::cluster_sync();
     ptx::tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_slot;
-    // everything above may run while the launch before this one is still at work; its results are read below
-    ptx::grid_launch_dependents();
-    ptx::grid_wait_previous();
 
     uint32_t it = 0, tile_iter = 0, stage = 0, phase = 0;
-    auto next_stage = [&]() { ++it; if (++stage == (uint32_t)MG_STAGES) { stage = 0; phase ^= 1; } };
+    auto next_stage = [&]() { ++it; if (++stage == (uint32_t)Cfg::STAGES) { stage = 0; phase ^= 1; } };
 
-    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    int op_at = 0, fenced = -1;
-    for (int tile = pair; tile < tiles; tile += pairs, ++tile_iter) {
-        while (op_at + 1 < n_ops && __ldg(prefix + op_at + 1) <= tile) ++op_at;
-        const GemmOp* op = ops + op_at;
-        const int local = tile - __ldg(prefix + op_at);
-        const int tiles_m = __ldg(&op->tiles_m);
-        const bool sym = __ldg(&op->sym) != 0;
-        int tm, tn;
-        if (sym) {
-            // upper triangle, column by column: column tn holds the tiles (0 .. tn, tn)
-            tn = (int)((sqrtf(8.0f * (float)local + 1.0f) - 1.0f) * 0.5f);
-            while ((tn + 1) * (tn + 2) / 2 <= local) ++tn;
-            while (tn * (tn + 1) / 2 > local) --tn;
-            tm = local - tn * (tn + 1) / 2;
-        } else {
-            tn = local / tiles_m;
-            tm = local - tn * tiles_m;
-        }
-        const int K = __ldg(&op->K);
-        const int nkb = (K + 63) / 64;
-        const int num_kb = SPLIT ? 3 * nkb : nkb;
-        const bool r_mn = __ldg(&op->r_mn) != 0;
+    const uint32_t sched_empty0 = ptx::map_to_cta(bar_sched_empty, 0);
+    // leader's producer: fetches entry `n` (ticket t) and hands it to both CTAs
+    auto deal = [&](uint32_t n, uint32_t t) {
+        const uint32_t b = n & 3;
+        if (!wait_phase(bar_sched_empty + 8 * b, ((n >> 2) & 1) ^ 1, abort_flag, status, 207)) return;
+        const uint4 e = t < tiles ? __ldg(list + t) : make_uint4(0xFFFFFFFFu, 0, 0, 0);
+        for (uint32_t c = 0; c < 2; ++c)
+            ptx::st_async_v4(ptx::map_to_cta(slots + 16 * b, c), e.x, e.y, e.z, e.w, ptx::map_to_cta(bar_sched_full + 8 * b, c));
+    };
+    if (tid == 0) {
+        ptx::mbar_arrive_expect_tx(bar_sched_full, 16);
+        if (rank == 0) deal(0, atomicAdd(ticket, 1u));
+    }
+    const bool reader = warp == 0 || (warp == 1 && rank == 0) || warp >= 4;
+    int ready = -1;                                      // the last op whose operands this role knows to be complete
+    for (; reader; ++tile_iter) {
+        // the entry {op, tm | tn << 16, k-blocks, R along n}
+        const uint32_t sb = tile_iter & 3;
+        if (!__all_sync(0xFFFFFFFFu, wait_phase(bar_sched_full + 8 * sb, (tile_iter >> 2) & 1, abort_flag, status, 208))) break;
+        const uint4 entry = ptx::ld_shared_v4(slots + 16 * sb);
+        __syncwarp();
+        if (lane == 0 && !(warp == 0 && rank == 0)) ptx::mbar_arrive_release_cluster(sched_empty0 + 8 * sb);
+        if (entry.x == 0xFFFFFFFFu) break;
+        const GemmOp* op = ops + entry.x;
+        const int tm = (int)(entry.y & 0xFFFFu), tn = (int)(entry.y >> 16), num_kb = (int)entry.z;
+        const bool r_mn = entry.w != 0;
         const uint32_t buf = tile_iter & 1, use = tile_iter >> 1;
 
         if (warp == 0) {
             // ---------------- TMA producer (one thread in each CTA) ----------------
             if (lane == 0) {
-                if (fenced != op_at) {
-                    for (int h = 0; h < (SPLIT ? 2 : 1); ++h) {
-                        ptx::fence_tensormap_acquire(op->l_map[h]);
-                        ptx::fence_tensormap_acquire(op->r_map[h]);
-                    }
-                    fenced = op_at;
-                }
+                ptx::mbar_arrive_expect_tx(bar_sched_full + 8 * ((tile_iter + 1) & 3), 16);
+                const uint32_t drawn = rank == 0 ? atomicAdd(ticket, 1u) : 0u;
+                const int deal_at = rank == 0 ? (num_kb > 4 ? 4 : num_kb - 1) : -1;
                 const void* l_hi = op->l_map[0];
                 const void* r_hi = op->r_map[0];
                 const void* l_lo = SPLIT ? op->l_map[1] : nullptr;
                 const void* r_lo = SPLIT ? op->r_map[1] : nullptr;
+                bool ok = true;
+                if (ready != (int)entry.x) {
+                    ptx::fence_tensormap_acquire(l_hi);
+                    ptx::fence_tensormap_acquire(r_hi);
+                    if (SPLIT) { ptx::fence_tensormap_acquire(l_lo); ptx::fence_tensormap_acquire(r_lo); }
+                    ok = wait_count(op->counter, __ldg(&op->need), 32, abort_flag, status, 205);
+                    ptx::fence_proxy_async_global();     // other SMs' results, before this thread's loads through the async proxy
+                    ready = (int)entry.x;
+                }
                 const uint64_t pol = ptx::policy_evict_normal();
                 const uint32_t full0 = ptx::map_to_cta(bar_full, 0);
-                const int m0 = tm * MUON_TILE + (int)rank * 128, n0 = tn * MUON_TILE + (int)rank * 128;
+                const int m0 = tm * MUON_TILE + (int)rank * 128, n0 = tn * BN + (int)rank * (BN / 2);
+                const int seg_k = SPLIT ? num_kb / 3 * 64 : 0;
                 int k = 0, seg = 0;
-                for (int kb = 0; kb < num_kb; ++kb, next_stage()) {
+                for (int kb = 0; ok && kb < num_kb; ++kb, next_stage()) {
                     const uint32_t s = stage;
                     if (!wait_phase(bar_done + 8 * s, phase ^ 1, abort_flag, status, 201)) break;
-                    const uint32_t dst = smem_base + s * MG_STAGE, full = full0 + 8 * s;
-                    if (rank == 0) ptx::mbar_arrive_expect_tx(bar_full + 8 * s, 2u * MG_STAGE);
+                    const uint32_t dst = smem_base + s * Cfg::STAGE, full = full0 + 8 * s;
+                    if (rank == 0) ptx::mbar_arrive_expect_tx(bar_full + 8 * s, 2u * Cfg::STAGE);
                     const void* lm = SPLIT && seg == 1 ? l_lo : l_hi;
                     const void* rm = SPLIT && seg == 2 ? r_lo : r_hi;
                     ptx::tma_load_2d_pair(dst, lm, k, m0, full, pol);
                     if (r_mn) {
                         ptx::tma_load_2d_pair(dst + MG_OPERAND, rm, n0, k, full, pol);
-                        ptx::tma_load_2d_pair(dst + MG_OPERAND + MG_HALF, rm, n0 + 64, k, full, pol);
+                        if (BN == 256) ptx::tma_load_2d_pair(dst + MG_OPERAND + MG_HALF, rm, n0 + 64, k, full, pol);
                     } else {
                         ptx::tma_load_2d_pair(dst + MG_OPERAND, rm, k, n0, full, pol);
                     }
                     k += 64;
-                    if (SPLIT && k >= nkb * 64) { k = 0; ++seg; }
+                    if (SPLIT && k >= seg_k) { k = 0; ++seg; }
+                    if (kb == deal_at) deal(tile_iter + 1, drawn);
                 }
             }
             __syncwarp();
             if (__shfl_sync(0xFFFFFFFFu, *abort_flag, 0) != 0) break;
         } else if (warp == 1) {
             // ---------------- MMA issuer (leader only) ----------------
-            if (lane == 0 && rank == 0) {
-                const uint32_t idesc = ptx::instr_desc_f16_pair(MUON_TILE, r_mn);
-                const uint32_t d_tmem = tmem_base + buf * MUON_TILE;
+            if (lane == 0) {
+                const uint32_t idesc = ptx::instr_desc_f16_pair(BN, r_mn);
+                const uint32_t d_tmem = tmem_base + buf * BN;
                 bool ok = wait_phase(bar_acc_empty + 8 * buf, (use & 1) ^ 1, abort_flag, status, 202);
                 ptx::tc_fence_after_sync();
                 // K-major operand: 64 k = 128 bytes a row, 8-row groups 1024 bytes apart, 16 k = 32 bytes on.
@@ -202,7 +246,7 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const int* __restrict__ prefix,
                     const uint32_t s = stage;
                     if (!wait_phase(bar_full + 8 * s, phase, abort_flag, status, 203)) break;
                     ptx::tc_fence_after_sync();
-                    const uint64_t a_desc = a_desc0 + s * (MG_STAGE >> 4), b_desc = b_desc0 + s * (MG_STAGE >> 4);
+                    const uint64_t a_desc = a_desc0 + s * (Cfg::STAGE >> 4), b_desc = b_desc0 + s * (Cfg::STAGE >> 4);
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk)
                         ptx::mma_bf16_pair(d_tmem, a_desc + kk * 2, b_desc + kk * b_step, idesc, (kb | kk) != 0 ? 1u : 0u);
@@ -212,48 +256,66 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const int* __restrict__ prefix,
             }
             __syncwarp();
             if (__shfl_sync(0xFFFFFFFFu, *abort_flag, 0) != 0) break;
-        } else if (warp >= 4) {
+        } else {
             // ---------------- epilogue ----------------
             const int q = warp & 3, half = (warp - 4) >> 2;
             const int M = __ldg(&op->M), N = __ldg(&op->N), e_pitch = __ldg(&op->e_pitch);
             const int row0 = tm * MUON_TILE + (int)rank * 128 + q * 32, row = row0 + lane;
-            const bool mirror = sym && tm != tn;
+            const int col_first = tn * BN + half * (BN / 2);
+            const bool sym = __ldg(&op->sym) != 0, mirror = sym && tn * BN >= (tm + 1) * MUON_TILE;
             const float alpha = __ldg(&op->alpha), b1 = __ldg(&op->b1), b2 = __ldg(&op->b2), diag = __ldg(&op->diag);
+            const int64_t at0 = (int64_t)row * e_pitch + col_first;
             const __half* e1 = op->e1[0];
             const __half* e2 = op->e2[0];
             const uint32_t mine = staging + (uint32_t)(warp - 4) * 4096u, mine_t = mine + 2048u;
-            if (lane == 0 && fenced != op_at) {
-                for (int h = 0; h < (SPLIT ? 2 : 1); ++h) {
-                    ptx::fence_tensormap_acquire(op->out_map[h]);
-                    if (sym) ptx::fence_tensormap_acquire(op->mir_map[h]);
+            bool ok = true;
+            if (ready != (int)entry.x) {
+                if (lane == 0) {
+                    for (int h = 0; h < (SPLIT ? 2 : 1); ++h) {
+                        ptx::fence_tensormap_acquire(op->out_map[h]);
+                        if (sym) ptx::fence_tensormap_acquire(op->mir_map[h]);
+                    }
+                    ok = wait_count(op->counter, __ldg(&op->need), 300, abort_flag, status, 206);
                 }
-                fenced = op_at;
+                ok = __shfl_sync(0xFFFFFFFFu, ok ? 1 : 0, 0) != 0;
+                ready = (int)entry.x;
             }
-            const bool acc_ok = __all_sync(0xFFFFFFFFu, wait_phase_idle(bar_acc_full + 8 * buf, use & 1, abort_flag, status, 204));
+            const bool some = ok && row0 < M && col_first < N, in = some && row < M;
+            // the terms beside the product come from L2 (other SMs wrote them in this launch), one piece ahead
+            uint4 t1[4], t1l[SPLIT ? 4 : 1];
+            if (e1) {
+                load_term(t1, e1 + at0, in);
+                if constexpr (SPLIT) load_term(t1l, op->e1[1] + at0, in);
+            }
+            const bool acc_ok = ok && __all_sync(0xFFFFFFFFu, num_kb > 8 ? wait_phase_idle(bar_acc_full + 8 * buf, use & 1, abort_flag, status, 204)
+                                                                            : wait_phase(bar_acc_full + 8 * buf, use & 1, abort_flag, status, 204));
             ptx::tc_fence_after_sync();
-            if (acc_ok && row0 < M) {
+            if (acc_ok && some) {
 #pragma unroll 1
-                for (int ch = 0; ch < 4; ++ch) {
-                    const int col = tn * MUON_TILE + half * 128 + ch * 32;
+                for (int ch = 0; ch < BN / 64; ++ch) {
+                    const int col = col_first + ch * 32;
                     if (col >= N) break;
-                    const int64_t at = (int64_t)row * e_pitch + col;
-                    const bool in = row < M;
-                    uint4 t1[4], t2[4], t1l[SPLIT ? 4 : 1], t2l[SPLIT ? 4 : 1];
-                    if (e1) load_term(t1, e1 + at, in);
-                    if (e2) load_term(t2, e2 + at, in);
-                    if constexpr (SPLIT) {
-                        if (e1) load_term(t1l, op->e1[1] + at, in);
-                        if (e2) load_term(t2l, op->e2[1] + at, in);
+                    const int64_t at = at0 + ch * 32;
+                    uint4 t2[4], t2l[SPLIT ? 4 : 1];
+                    if (e2) {
+                        load_term(t2, e2 + at, in);
+                        if constexpr (SPLIT) load_term(t2l, op->e2[1] + at, in);
                     }
                     float v[32];
-                    ptx::tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + buf * MUON_TILE + (uint32_t)(half * 128 + ch * 32), v);
+                    ptx::tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + buf * BN + (uint32_t)(half * (BN / 2) + ch * 32), v);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] *= alpha;
-                    if (e1) add_term(v, b1, t1);
-                    if (e2) add_term(v, b2, t2);
-                    if constexpr (SPLIT) {
-                        if (e1) add_term(v, b1, t1l);
-                        if (e2) add_term(v, b2, t2l);
+                    if (e1) {
+                        add_term(v, b1, t1);
+                        if constexpr (SPLIT) add_term(v, b1, t1l);
+                        if (ch + 1 < BN / 64 && col + 32 < N) {
+                            load_term(t1, e1 + at + 32, in);
+                            if constexpr (SPLIT) load_term(t1l, op->e1[1] + at + 32, in);
+                        }
+                    }
+                    if (e2) {
+                        add_term(v, b2, t2);
+                        if constexpr (SPLIT) add_term(v, b2, t2l);
                     }
                     if (sym && diag != 0.0f && row >= col && row < col + 32) {
 #pragma unroll
@@ -297,19 +359,21 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const int* __restrict__ prefix,
             }
             ptx::tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0 && acc_ok) ptx::mbar_arrive_remote(ptx::map_to_cta(bar_acc_empty + 8 * buf, 0));
+            if (lane == 0 && acc_ok) {
+                ptx::mbar_arrive_remote(ptx::map_to_cta(bar_acc_empty + 8 * buf, 0));
+                ptx::bulk_wait_all();                    // this warp's part of the tile is in memory (a completed bulk
+                red_release_gpu_add(op->counter, 1u);    // store needs no further proxy fence): count it
+            }
             if (__shfl_sync(0xFFFFFFFFu, *abort_flag, 0) != 0) break;
-        } else if (__shfl_sync(0xFFFFFFFFu, *abort_flag, 0) != 0) {
-            break;
         }
     }
 
     if (warp >= 4 && lane == 0) ptx::bulk_wait_all();
     // The leader lets the loads of both CTAs and its MMAs finish before either CTA gives up shared memory or TMEM.
     if (tid == 0 && rank == 0) {
-        for (uint32_t s = 0; s < (uint32_t)MG_STAGES && s < it; ++s) {
-            const uint32_t last = s + (it - 1 - s) / MG_STAGES * MG_STAGES;
-            drain_phase(bar_full + 8 * s, (last / MG_STAGES) & 1);
+        for (uint32_t s = 0; s < (uint32_t)Cfg::STAGES && s < it; ++s) {
+            const uint32_t last = s + (it - 1 - s) / Cfg::STAGES * Cfg::STAGES;
+            drain_phase(bar_full + 8 * s, (last / Cfg::STAGES) & 1);
         }
     }
     if (rank == 0 && tid == 32) {
@@ -397,6 +461,10 @@ muon_moment_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ sta
     __shared__ double scratch[32];
     const int k = find_item(a, blockIdx.x);
     const MuonItem& it = a.item[k];
+    if ((int)blockIdx.x == a.tile_begin[k] && threadIdx.x == 0) {      // counters of the products that follow
+        *it.counter = 0;
+        *a.ticket = 0;
+    }
     const int piece = (int)blockIdx.x - a.tile_begin[k];
     const int64_t numel = (int64_t)it.rows * it.cols;
     const int64_t len = ((numel + it.n_part - 1) / it.n_part + 7) / 8 * 8;
@@ -561,7 +629,6 @@ muon_apply_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ stat
 {
     constexpr bool SPLIT = sizeof(T) == 4;
     __shared__ float tile[MS_ROWS][MS_COLS + 1];
-    ptx::grid_wait_previous();
     if (*reinterpret_cast<volatile int32_t*>(status) != STATUS_OK) return;      // a product gave up: leave the weights
     const int k = find_item(a, blockIdx.x);
     const MuonItem& it = a.item[k];
@@ -710,38 +777,43 @@ cudaError_t launch_muon_apply(int dtype, bool step, const MuonArgs& a, int tiles
     return cudaGetLastError();
 }
 
-cudaError_t launch_muon_gemm(bool split, const GemmOp* d_ops, const int* d_prefix, int n_ops, int tiles, MuonLaunch& state,
-                             int32_t* d_status, cudaStream_t stream)
+namespace {
+
+template <bool SPLIT, int BN>
+cudaError_t launch_gemm(const GemmOp* d_ops, const uint4* d_list, int tiles, uint32_t* d_ticket, MuonLaunch& state, int32_t* d_status, cudaStream_t stream)
 {
-    typedef void (*Kernel)(const GemmOp*, const int*, int, int, int32_t*);
-    const Kernel kernel = split ? muon_gemm_kernel<true> : muon_gemm_kernel<false>;
+    const auto kernel = muon_gemm_kernel<SPLIT, BN>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(state.sm_count / 2 * 2));
     cfg.blockDim = dim3(MG_THREADS);
-    cfg.dynamicSmemBytes = MG_SMEM;
+    cfg.dynamicSmemBytes = GemmCfg<BN>::SMEM;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
+    cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (!state.attr_set) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MG_SMEM);
+    int& pairs = state.max_pairs[BN == 256 ? 0 : 1];
+    if (pairs == 0) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmCfg<BN>::SMEM);
         if (e != cudaSuccess) return e;
-        // persistent over the tiles: as many pairs as can be resident at once
         int clusters = 0;
-        if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) != cudaSuccess || clusters < 1) {
-            cudaGetLastError();
-            clusters = state.sm_count / 2;
-        }
-        state.max_pairs = clusters;
-        state.attr_set = true;
+        const cudaError_t o = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg);
+        if (o != cudaSuccess) return o;
+        if (clusters < 1) return cudaErrorLaunchOutOfResources;
+        pairs = clusters;
     }
-    cfg.numAttrs = 2;
-    cfg.gridDim = dim3((unsigned)(2 * (tiles < state.max_pairs ? tiles : state.max_pairs)));
-    return cudaLaunchKernelEx(&cfg, kernel, d_ops, d_prefix, n_ops, tiles, d_status);
+    cfg.gridDim = dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs)));
+    return cudaLaunchKernelEx(&cfg, kernel, d_ops, d_list, (uint32_t)tiles, d_ticket, d_status);
+}
+
+}  // namespace
+
+cudaError_t launch_muon_gemm(bool split, int bn, const GemmOp* d_ops, const uint4* d_list, int tiles, uint32_t* d_ticket, MuonLaunch& state,
+                             int32_t* d_status, cudaStream_t stream)
+{
+    if (bn == 256) return split ? launch_gemm<true, 256>(d_ops, d_list, tiles, d_ticket, state, d_status, stream) : launch_gemm<false, 256>(d_ops, d_list, tiles, d_ticket, state, d_status, stream);
+    return split ? launch_gemm<true, 128>(d_ops, d_list, tiles, d_ticket, state, d_status, stream) : launch_gemm<false, 128>(d_ops, d_list, tiles, d_ticket, state, d_status, stream);
 }
 
 int muon_encode_maps(const __half* base, int rows, int cols, int pitch, void* maps)

@@ -219,17 +219,6 @@ int tensor_path_prepare(MatDesc* h_descs, int n_mat, int rank, const TcTiling& t
 
 namespace {
 
-// Counters in global memory that CTAs of one launch signal each other through (P generated by spare warps).
-__device__ __forceinline__ uint32_t ld_acquire_gpu(const uint32_t* p)
-{
-    uint32_t v;
-    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-    return v;
-}
-__device__ __forceinline__ void red_release_gpu_add(uint32_t* p, uint32_t v)
-{
-    asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
-}
 // Bounded wait until *counter >= target.  All CTAs of the launch are resident (the grid is sized by the
 // occupancy query), so the writers run; the bound covers the case that one of them gave up.  A set status
 // word ends the wait at once.  false = gave up (abort flag and status word are set).

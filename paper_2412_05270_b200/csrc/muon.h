@@ -6,7 +6,7 @@
 
 namespace apollo {
 
-constexpr int MUON_TILE = 256;          // a product's tile: 256 x 256, shared by the two CTAs of a pair
+constexpr int MUON_TILE = 256;          // rows of a product's tile, shared by the two CTAs of a pair; it has 256 or 128 columns
 constexpr int MUON_CHUNK = 48;          // matrices whose pointers travel in one launch of a streaming kernel
 constexpr int MUON_PART = 256;          // most partial sums of squares per matrix
 
@@ -22,8 +22,11 @@ struct GemmOp {
     const __half* e1[2];                // same place and pitch as the output; null = none
     const __half* e2[2];
     float alpha, b1, b2, diag;
-    int32_t M, N, K, e_pitch, tiles_m, tiles_n, sym, r_mn;
+    int32_t M, N, K, e_pitch, sym, r_mn;
+    uint32_t* counter;                  // DEVICE: epilogue warps of this matrix that are done, over all its products
+    uint32_t need;                      // its value once the products before this one are complete
 };
+constexpr int MUON_WARPS_PER_TILE = 16; // counts that a finished tile adds
 
 // One matrix of a streaming kernel.
 struct MuonItem {
@@ -32,6 +35,7 @@ struct MuonItem {
     float* m;
     __half* x[2];                       // iterate, m x n (transposed when tall), high and low parts
     double* part;                       // partial sums of squares of U
+    uint32_t* counter;                  // GemmOp::counter, zeroed by the first pass
     int32_t rows, cols, x_pitch, n_part;
     int32_t tall;
     float gain;                         // s of the update
@@ -43,11 +47,12 @@ struct MuonArgs {
     int32_t n;
     float mu, eps, x_scale, lr, wd;     // x_scale: the power of two the iterates carry
     int32_t nesterov;
+    uint32_t* ticket;                   // DEVICE: next tile of the products, zeroed by the first pass
 };
 
 struct MuonLaunch {                     // what the launches of a context need to know about the device
-    int sm_count, max_pairs;
-    bool attr_set;
+    int sm_count;
+    int max_pairs[2];                   // resident pairs of the kernels with 256 and 128 columns a tile; 0 = not asked yet
 };
 
 // Sum of squares of U (and M <- mu M + (1 - mu) G with `step`), X = U x_scale / (|U| + eps) in 16 bits, and the end:
@@ -58,8 +63,9 @@ cudaError_t launch_muon_apply(int dtype, bool step, const MuonArgs& a, int tiles
 // Tiles of one matrix in the load and apply kernels.
 int muon_stream_tiles(int rows, int cols);
 
-// One phase: ops[0 .. n_ops) with their tile prefix (DEVICE).
-cudaError_t launch_muon_gemm(bool split, const GemmOp* d_ops, const int* d_prefix, int n_ops, int tiles, MuonLaunch& state,
+// All products of a group: d_list holds per tile {op, tm | tn << 16, k-blocks of its contraction, R along n} (DEVICE);
+// d_ticket: DEVICE, zero.
+cudaError_t launch_muon_gemm(bool split, int bn, const GemmOp* d_ops, const uint4* d_list, int tiles, uint32_t* d_ticket, MuonLaunch& state,
                              int32_t* d_status, cudaStream_t stream);
 
 // Tensor maps of a rows x cols matrix of 16-bit floats (pitch a multiple of 8), 128 bytes each at maps[kind]:

@@ -72,4 +72,16 @@ __device__ __forceinline__ void drain_phase(uint32_t bar, uint32_t parity)
         if (ptx::mbar_try_wait(bar, parity)) return;
 }
 
+// Counters in global memory that CTAs of one launch signal each other through.
+__device__ __forceinline__ uint32_t ld_acquire_gpu(const uint32_t* p)
+{
+    uint32_t v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ void red_release_gpu_add(uint32_t* p, uint32_t v)
+{
+    asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+}
+
 }  // namespace apollo
