@@ -261,7 +261,7 @@ void ops_of(const apollo_muon_ctx* ctx, int index, int bn, std::vector<GemmOp>& 
     auto push = [&](GemmOp& o) {
         o.counter = counter;
         o.need = done;
-        done += MUON_WARPS_PER_TILE * (uint32_t)(o.sym ? sym_tiles(o.M, bn) : (int64_t)tiles_of(o.M, MUON_TILE) * tiles_of(o.N, bn));
+        done += MUON_COUNTS_PER_TILE * (uint32_t)(o.sym ? sym_tiles(o.M, bn) : (int64_t)tiles_of(o.M, MUON_TILE) * tiles_of(o.N, bn));
         out.push_back(o);
     };
     auto square = [&](int l, int r, int dst, double alpha, int e1, double b1, int e2, double b2, double diag, bool of_x) {

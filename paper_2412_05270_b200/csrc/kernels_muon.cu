@@ -6,7 +6,7 @@
 //
 // A product's tile is 256 x 256 (256 x 128 in short lists): each CTA of a pair loads its 128 rows of L and half of the
 // columns of R, 32 KB per 64-deep k-block, six stages; four MMAs of 256 x 256 x 16 consume them.  Roles of the 12 warps: 0 TMA producer,
-// 1 MMA issuer (leader CTA) and TMEM owner, 4-11 epilogue (a warp reads the 32 TMEM lanes it may read and one half
+// 1 MMA issuer (leader CTA) and TMEM owner, 2 and 3 bookkeeping, 4-11 epilogue (a warp reads the 32 TMEM lanes it may read and one half
 // of the columns).  The epilogue adds the terms that the iteration needs beside the product, rounds to 16 bits and
 // hands 32 x 32 pieces to TMA stores; a symmetric product's tile above the diagonal is stored a second time,
 // transposed, so that half of the symmetric products is never computed.
@@ -29,11 +29,13 @@ constexpr int MG_THREADS = 384;
 constexpr int MG_HALF = 8192;                            // 64 x 64 16-bit floats: one TMA box
 constexpr int MG_OPERAND = 2 * MG_HALF;                  // a CTA's 128 rows of L, or half of R
 constexpr int MG_EPI_WARPS = 8;
-constexpr int MG_STAGING = MG_EPI_WARPS * 4096;          // per epilogue warp: 2 KB as stored, 2 KB transposed
+constexpr int MG_STAGING = MG_EPI_WARPS * 4096;          // per epilogue warp: a piece of 32 x 32, and the piece transposed
+constexpr uint32_t MG_RING = 16;                         // entries of the list in flight
+constexpr uint32_t MG_END = 0xFFFFFFFFu;                 // no more entries
 template <int BN> struct GemmCfg {
     static constexpr int STAGE = MG_OPERAND + BN * 64;   // 128 rows of L and BN / 2 of R, 64 deep
     static constexpr int STAGES = BN == 256 ? 6 : 8;
-    static constexpr int SMEM = STAGES * STAGE + MG_STAGING + 320 + 1024;
+    static constexpr int SMEM = STAGES * STAGE + MG_STAGING + 768 + 1024;
     static_assert(SMEM <= 227 * 1024 && STAGES <= 8, "shared memory and barriers of a CTA");
 };
 
@@ -54,14 +56,6 @@ __device__ __forceinline__ bool wait_count(const uint32_t* counter, uint32_t nee
     return false;
 }
 
-__device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
-{
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
-}
-__device__ __forceinline__ void st_shared_u16(uint32_t addr, uint16_t v)
-{
-    asm volatile("st.shared.b16 [%0], %1;" ::"r"(addr), "h"(v) : "memory");
-}
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi)
 {
     const __half2 p = __floats2half2_rn(lo, hi);
@@ -96,14 +90,25 @@ __device__ __forceinline__ void load_term(uint4 (&e)[4], const __half* p, bool i
 
 // One launch does all products of a group: the host lists the tiles of the first product of every matrix, then those of
 // the second, and so on, and the pairs draw them in this order.  A tile waits (bounded) until the products before its
-// own are complete for ITS matrix: a counter per matrix, one count per epilogue warp and tile, added after the warp's
-// stores have landed.  Whoever runs draws the next tile, so the earliest unfinished one is always at work and waits
-// for nothing that is not: no CTA has to be resident for another to finish.  With several matrices the products before
-// are complete by the time a tile comes up, and there is neither a launch nor a drained pipeline between products.
+// own are complete for ITS matrix: a counter per matrix, one count per CTA and tile, added after the CTA's stores have
+// landed.  Whoever runs draws the next tile, so the earliest unfinished one is always at work and waits for nothing
+// that is not: no CTA has to be resident for another to finish.  With several matrices the products before are
+// complete by the time a tile comes up, and there is neither a launch nor a drained pipeline between products.
 // (Dealing the tiles out by index instead let the pairs drift apart where long and short contractions meet; what
 // neighbours share then no longer met in L2: a 7B layer took 12.9 ms instead of 11.6 ms, at equal cycles.)
-// The leader's producer thread draws: the ticket at the start of a tile, the entry of the list a few k-blocks later,
-// from where st.async puts it into a ring of four slots in both CTAs (`sched` barriers), one tile ahead of its use.
+//
+// Roles that keep latency off the loads and the epilogue:
+//   leader's producer  draws: the ticket at the start of a tile, the entry of the list a few k-blocks later, from where
+//                      st.async puts it into a ring of 16 slots in both CTAs, one tile ahead of its use.  Nobody has to
+//                      say that a slot is free: the producer is at most STAGES k-blocks (>= one tile each) ahead of the
+//                      MMAs, those at most two tiles ahead of the epilogue, so a slot is read long before its turn.
+//   warp 2             waits for the tile's operands and passes that on (`dep` barriers, same ring)
+//   warp 3             counts the tile once the eight epilogue warps say that their stores have landed
+//
+// Symmetric results are computed in 256-row blocks from the diagonal on; a tile beyond the diagonal block is stored a
+// second time, transposed.  (Storing it once, and reading what lies below the diagonal as the transposed tile of what
+// lies above, which the tensor cores also take, saves those stores and cost 5 % on 4096 x 4096: operands in that
+// order take 10 % more cycles per k-block.)
 //
 // SPLIT: operands are sums of two 16-bit floats, and the contraction runs over three segments into one accumulator:
 // hi hi + lo hi + hi lo (what is dropped, lo lo, is 2^-24 of a term).  BN: columns of a tile.
@@ -116,12 +121,13 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (ptx::smem_addr(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem_gen = smem_raw + (smem_base - ptx::smem_addr(smem_raw));
+    constexpr uint32_t MISC = Cfg::STAGES * Cfg::STAGE + MG_STAGING;
     const uint32_t staging = smem_base + Cfg::STAGES * Cfg::STAGE;
-    const uint32_t bars = staging + MG_STAGING;
+    const uint32_t bars = smem_base + MISC;
     const uint32_t bar_full = bars, bar_done = bars + 64, bar_acc_full = bars + 128, bar_acc_empty = bars + 144, bar_drain = bars + 160,
-                   bar_sched_full = bars + 192, bar_sched_empty = bars + 224, slots = bars + 256;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + Cfg::STAGES * Cfg::STAGE + MG_STAGING + 176);
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + Cfg::STAGES * Cfg::STAGE + MG_STAGING + 180);
+                   bar_landed = bars + 192, bar_entry = bars + 256, bar_dep = bars + 384, slots = bars + 512;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + MISC + 176);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + MISC + 180);
 
     const uint32_t rank = ptx::cluster_ctarank();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -132,11 +138,12 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
         }
         for (int b = 0; b < 2; ++b) {
             ptx::mbar_init(bar_acc_full + 8 * b, 1);
-            ptx::mbar_init(bar_acc_empty + 8 * b, 2 * MG_EPI_WARPS);
+            ptx::mbar_init(bar_acc_empty + 8 * b, 2 * (MG_EPI_WARPS + 1));   // both CTAs' epilogue warps and counting warp
         }
-        for (int b = 0; b < 4; ++b) {
-            ptx::mbar_init(bar_sched_full + 8 * b, 1);                            // this CTA's producer, and the entry's 16 bytes
-            ptx::mbar_init(bar_sched_empty + 8 * b, 2 * MG_EPI_WARPS + 2);        // leader's copy: all readers but the writer
+        for (int b = 0; b < 4; ++b) ptx::mbar_init(bar_landed + 8 * b, MG_EPI_WARPS);
+        for (int b = 0; b < MG_RING; ++b) {
+            ptx::mbar_init(bar_entry + 8 * b, 1);        // this CTA's producer, and the entry's 16 bytes
+            ptx::mbar_init(bar_dep + 8 * b, 1);          // warp 2
         }
         ptx::mbar_init(bar_drain, 1);
         *abort_flag = 0;
@@ -152,62 +159,51 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
     ptx::tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_slot;
 
-    uint32_t it = 0, tile_iter = 0, stage = 0, phase = 0;
+    uint32_t it = 0, stage = 0, phase = 0;
     auto next_stage = [&]() { ++it; if (++stage == (uint32_t)Cfg::STAGES) { stage = 0; phase ^= 1; } };
 
-    const uint32_t sched_empty0 = ptx::map_to_cta(bar_sched_empty, 0);
     // leader's producer: fetches entry `n` (ticket t) and hands it to both CTAs
     auto deal = [&](uint32_t n, uint32_t t) {
-        const uint32_t b = n & 3;
-        if (!wait_phase(bar_sched_empty + 8 * b, ((n >> 2) & 1) ^ 1, abort_flag, status, 207)) return;
-        const uint4 e = t < tiles ? __ldg(list + t) : make_uint4(0xFFFFFFFFu, 0, 0, 0);
+        const uint32_t b = n % MG_RING;
+        const uint4 e = t < tiles ? __ldg(list + t) : make_uint4(MG_END, 0, 0, 0);
         for (uint32_t c = 0; c < 2; ++c)
-            ptx::st_async_v4(ptx::map_to_cta(slots + 16 * b, c), e.x, e.y, e.z, e.w, ptx::map_to_cta(bar_sched_full + 8 * b, c));
+            ptx::st_async_v4(ptx::map_to_cta(slots + 16 * b, c), e.x, e.y, e.z, e.w, ptx::map_to_cta(bar_entry + 8 * b, c));
     };
     if (tid == 0) {
-        ptx::mbar_arrive_expect_tx(bar_sched_full, 16);
+        ptx::mbar_arrive_expect_tx(bar_entry, 16);
         if (rank == 0) deal(0, atomicAdd(ticket, 1u));
     }
-    const bool reader = warp == 0 || (warp == 1 && rank == 0) || warp >= 4;
-    int ready = -1;                                      // the last op whose operands this role knows to be complete
-    for (; reader; ++tile_iter) {
+    int last_op = -1;
+    for (uint32_t n = 0; warp != 1 || rank == 0; ++n) {  // (the peer has no MMA role)
         // the entry {op, tm | tn << 16, k-blocks, R along n}
-        const uint32_t sb = tile_iter & 3;
-        if (!__all_sync(0xFFFFFFFFu, wait_phase(bar_sched_full + 8 * sb, (tile_iter >> 2) & 1, abort_flag, status, 208))) break;
-        const uint4 entry = ptx::ld_shared_v4(slots + 16 * sb);
-        __syncwarp();
-        if (lane == 0 && !(warp == 0 && rank == 0)) ptx::mbar_arrive_release_cluster(sched_empty0 + 8 * sb);
-        if (entry.x == 0xFFFFFFFFu) break;
+        const uint32_t slot = n % MG_RING, ring_phase = (n / MG_RING) & 1;
+        if (!__all_sync(0xFFFFFFFFu, wait_phase(bar_entry + 8 * slot, ring_phase, abort_flag, status, 208))) break;
+        const uint4 entry = ptx::ld_shared_v4(slots + 16 * slot);
+        if (entry.x == MG_END) break;
         const GemmOp* op = ops + entry.x;
         const int tm = (int)(entry.y & 0xFFFFu), tn = (int)(entry.y >> 16), num_kb = (int)entry.z;
         const bool r_mn = entry.w != 0;
-        const uint32_t buf = tile_iter & 1, use = tile_iter >> 1;
+        const uint32_t buf = n & 1, use = n >> 1;
+        const bool new_op = last_op != (int)entry.x;
+        last_op = (int)entry.x;
 
         if (warp == 0) {
             // ---------------- TMA producer (one thread in each CTA) ----------------
             if (lane == 0) {
-                ptx::mbar_arrive_expect_tx(bar_sched_full + 8 * ((tile_iter + 1) & 3), 16);
+                ptx::mbar_arrive_expect_tx(bar_entry + 8 * ((n + 1) % MG_RING), 16);
                 const uint32_t drawn = rank == 0 ? atomicAdd(ticket, 1u) : 0u;
                 const int deal_at = rank == 0 ? (num_kb > 4 ? 4 : num_kb - 1) : -1;
                 const void* l_hi = op->l_map[0];
                 const void* r_hi = op->r_map[0];
                 const void* l_lo = SPLIT ? op->l_map[1] : nullptr;
                 const void* r_lo = SPLIT ? op->r_map[1] : nullptr;
-                bool ok = true;
-                if (ready != (int)entry.x) {
-                    ptx::fence_tensormap_acquire(l_hi);
-                    ptx::fence_tensormap_acquire(r_hi);
-                    if (SPLIT) { ptx::fence_tensormap_acquire(l_lo); ptx::fence_tensormap_acquire(r_lo); }
-                    ok = wait_count(op->counter, __ldg(&op->need), 32, abort_flag, status, 205);
-                    ptx::fence_proxy_async_global();     // other SMs' results, before this thread's loads through the async proxy
-                    ready = (int)entry.x;
-                }
+                const int seg_k = SPLIT ? num_kb / 3 * 64 : 0;
                 const uint64_t pol = ptx::policy_evict_normal();
                 const uint32_t full0 = ptx::map_to_cta(bar_full, 0);
                 const int m0 = tm * MUON_TILE + (int)rank * 128, n0 = tn * BN + (int)rank * (BN / 2);
-                const int seg_k = SPLIT ? num_kb / 3 * 64 : 0;
+                const bool ok = wait_phase(bar_dep + 8 * slot, ring_phase, abort_flag, status, 205);
                 int k = 0, seg = 0;
-                for (int kb = 0; ok && kb < num_kb; ++kb, next_stage()) {
+                for (int i = 0; ok && i < num_kb; ++i, next_stage()) {
                     const uint32_t s = stage;
                     if (!wait_phase(bar_done + 8 * s, phase ^ 1, abort_flag, status, 201)) break;
                     const uint32_t dst = smem_base + s * Cfg::STAGE, full = full0 + 8 * s;
@@ -223,11 +219,10 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
                     }
                     k += 64;
                     if (SPLIT && k >= seg_k) { k = 0; ++seg; }
-                    if (kb == deal_at) deal(tile_iter + 1, drawn);
+                    if (i == deal_at) deal(n + 1, drawn);
                 }
             }
             __syncwarp();
-            if (__shfl_sync(0xFFFFFFFFu, *abort_flag, 0) != 0) break;
         } else if (warp == 1) {
             // ---------------- MMA issuer (leader only) ----------------
             if (lane == 0) {
@@ -241,54 +236,76 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
                 const uint64_t b_desc0 = r_mn ? ptx::smem_desc_sw128(smem_base + MG_OPERAND, MG_HALF, 1024)
                                               : ptx::smem_desc_sw128(smem_base + MG_OPERAND, 16, 1024);
                 const uint32_t b_step = r_mn ? 2048u >> 4 : 32u >> 4;
-                int kb = 0;
-                for (; ok && kb < num_kb; ++kb, next_stage()) {
+                int i = 0;
+                for (; ok && i < num_kb; ++i, next_stage()) {
                     const uint32_t s = stage;
                     if (!wait_phase(bar_full + 8 * s, phase, abort_flag, status, 203)) break;
                     ptx::tc_fence_after_sync();
                     const uint64_t a_desc = a_desc0 + s * (Cfg::STAGE >> 4), b_desc = b_desc0 + s * (Cfg::STAGE >> 4);
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk)
-                        ptx::mma_bf16_pair(d_tmem, a_desc + kk * 2, b_desc + kk * b_step, idesc, (kb | kk) != 0 ? 1u : 0u);
+                        ptx::mma_bf16_pair(d_tmem, a_desc + kk * 2, b_desc + kk * b_step, idesc, (i | kk) != 0 ? 1u : 0u);
                     ptx::mma_commit_pair(bar_done + 8 * s, 3);
                 }
-                if (ok && kb == num_kb) ptx::mma_commit_pair(bar_acc_full + 8 * buf, 3);
+                if (ok && i == num_kb) ptx::mma_commit_pair(bar_acc_full + 8 * buf, 3);
             }
             __syncwarp();
-            if (__shfl_sync(0xFFFFFFFFu, *abort_flag, 0) != 0) break;
+        } else if (warp == 2) {
+            // ---------------- operands complete? ----------------
+            if (lane == 0) {
+                bool ok = true;
+                if (new_op) {
+                    for (int h = 0; h < (SPLIT ? 2 : 1); ++h) {
+                        ptx::fence_tensormap_acquire(op->l_map[h]);
+                        ptx::fence_tensormap_acquire(op->r_map[h]);
+                    }
+                    ok = wait_count(op->counter, __ldg(&op->need), 32, abort_flag, status, 206);
+                    ptx::fence_proxy_async_global();     // other SMs' results, before loads through the async proxy
+                }
+                if (ok) ptx::mbar_arrive(bar_dep + 8 * slot);
+            }
+            __syncwarp();
+        } else if (warp == 3) {
+            // ---------------- count the tile ----------------
+            if (lane == 0) {
+                uint32_t* counter = op->counter;
+                if (wait_phase_idle(bar_landed + 8 * (n & 3), (n >> 2) & 1, abort_flag, status, 209)) {
+                    ptx::mbar_arrive_remote(ptx::map_to_cta(bar_acc_empty + 8 * buf, 0));
+                    red_release_gpu_add(counter, 1u);
+                }
+            }
+            __syncwarp();
         } else {
             // ---------------- epilogue ----------------
             const int q = warp & 3, half = (warp - 4) >> 2;
             const int M = __ldg(&op->M), N = __ldg(&op->N), e_pitch = __ldg(&op->e_pitch);
             const int row0 = tm * MUON_TILE + (int)rank * 128 + q * 32, row = row0 + lane;
             const int col_first = tn * BN + half * (BN / 2);
-            const bool sym = __ldg(&op->sym) != 0, mirror = sym && tn * BN >= (tm + 1) * MUON_TILE;
             const float alpha = __ldg(&op->alpha), b1 = __ldg(&op->b1), b2 = __ldg(&op->b2), diag = __ldg(&op->diag);
             const int64_t at0 = (int64_t)row * e_pitch + col_first;
             const __half* e1 = op->e1[0];
             const __half* e2 = op->e2[0];
+            const __half* e1l = SPLIT ? op->e1[1] : nullptr;
+            const __half* e2l = SPLIT ? op->e2[1] : nullptr;
+            const bool sym = __ldg(&op->sym) != 0, mirror = sym && tn * BN >= (tm + 1) * MUON_TILE;
+            const void* out_map[2] = { op->out_map[0], SPLIT ? op->out_map[1] : nullptr };
+            const void* mir_map[2] = { op->mir_map[0], SPLIT ? op->mir_map[1] : nullptr };
             const uint32_t mine = staging + (uint32_t)(warp - 4) * 4096u, mine_t = mine + 2048u;
-            bool ok = true;
-            if (ready != (int)entry.x) {
-                if (lane == 0) {
-                    for (int h = 0; h < (SPLIT ? 2 : 1); ++h) {
-                        ptx::fence_tensormap_acquire(op->out_map[h]);
-                        if (sym) ptx::fence_tensormap_acquire(op->mir_map[h]);
-                    }
-                    ok = wait_count(op->counter, __ldg(&op->need), 300, abort_flag, status, 206);
+            if (lane == 0 && new_op)
+                for (int h = 0; h < (SPLIT ? 2 : 1); ++h) {
+                    ptx::fence_tensormap_acquire(out_map[h]);
+                    if (sym) ptx::fence_tensormap_acquire(mir_map[h]);
                 }
-                ok = __shfl_sync(0xFFFFFFFFu, ok ? 1 : 0, 0) != 0;
-                ready = (int)entry.x;
-            }
+            const bool ok = __all_sync(0xFFFFFFFFu, wait_phase(bar_dep + 8 * slot, ring_phase, abort_flag, status, 210));
             const bool some = ok && row0 < M && col_first < N, in = some && row < M;
             // the terms beside the product come from L2 (other SMs wrote them in this launch), one piece ahead
             uint4 t1[4], t1l[SPLIT ? 4 : 1];
             if (e1) {
                 load_term(t1, e1 + at0, in);
-                if constexpr (SPLIT) load_term(t1l, op->e1[1] + at0, in);
+                if constexpr (SPLIT) load_term(t1l, e1l + at0, in);
             }
             const bool acc_ok = ok && __all_sync(0xFFFFFFFFu, num_kb > 8 ? wait_phase_idle(bar_acc_full + 8 * buf, use & 1, abort_flag, status, 204)
-                                                                            : wait_phase(bar_acc_full + 8 * buf, use & 1, abort_flag, status, 204));
+                                                                           : wait_phase(bar_acc_full + 8 * buf, use & 1, abort_flag, status, 204));
             ptx::tc_fence_after_sync();
             if (acc_ok && some) {
 #pragma unroll 1
@@ -299,7 +316,7 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
                     uint4 t2[4], t2l[SPLIT ? 4 : 1];
                     if (e2) {
                         load_term(t2, e2 + at, in);
-                        if constexpr (SPLIT) load_term(t2l, op->e2[1] + at, in);
+                        if constexpr (SPLIT) load_term(t2l, e2l + at, in);
                     }
                     float v[32];
                     ptx::tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + buf * BN + (uint32_t)(half * (BN / 2) + ch * 32), v);
@@ -310,14 +327,14 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
                         if constexpr (SPLIT) add_term(v, b1, t1l);
                         if (ch + 1 < BN / 64 && col + 32 < N) {
                             load_term(t1, e1 + at + 32, in);
-                            if constexpr (SPLIT) load_term(t1l, op->e1[1] + at + 32, in);
+                            if constexpr (SPLIT) load_term(t1l, e1l + at + 32, in);
                         }
                     }
                     if (e2) {
                         add_term(v, b2, t2);
                         if constexpr (SPLIT) add_term(v, b2, t2l);
                     }
-                    if (sym && diag != 0.0f && row >= col && row < col + 32) {
+                    if (diag != 0.0f && row >= col && row < col + 32) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] += row == col + i ? diag : 0.0f;
                     }
@@ -326,25 +343,32 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
                     for (int i = 0; i < 16; ++i) w[i] = pack_half2(v[2 * i], v[2 * i + 1]);
 #pragma unroll
                     for (int h = 0; h < (SPLIT ? 2 : 1); ++h) {
+                        // transposed: neighbouring lanes (rows) exchange halves of two columns, the even lane then holds
+                        // both rows of the first column, the odd lane of the second; 32 different banks a store
+                        uint32_t tr[16];
+                        if (mirror) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, w[i], 1);
+                                tr[i] = lane & 1 ? __byte_perm(other, w[i], 0x7632) : __byte_perm(w[i], other, 0x5410);
+                            }
+                        }
                         if (lane == 0) ptx::bulk_wait_read();        // the stores of the last piece have read the staging
                         __syncwarp();
                         // rows of 64 bytes in the 64-byte swizzle of the store's map: the 16-byte unit of a row is
                         // exchanged with bits 1..2 of the row, so that eight lanes hit eight different units
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            st_shared_v4(mine + (uint32_t)(lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                            ptx::st_shared_v4(mine + (uint32_t)(lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
                         if (mirror) {
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                st_shared_u16(mine_t + (uint32_t)(((2 * i) * 32 + lane) * 2), (uint16_t)(w[i] & 0xFFFFu));
-                                st_shared_u16(mine_t + (uint32_t)(((2 * i + 1) * 32 + lane) * 2), (uint16_t)(w[i] >> 16));
-                            }
+                            for (int i = 0; i < 16; ++i) ptx::st_shared_b32(mine_t + (uint32_t)((2 * i + (lane & 1)) * 64 + (lane >> 1) * 4), tr[i]);
                         }
                         ptx::fence_proxy_async_smem();
                         __syncwarp();
                         if (lane == 0) {
-                            ptx::tma_store_2d(op->out_map[h], col, row0, mine);
-                            if (mirror) ptx::tma_store_2d(op->mir_map[h], row0, col, mine_t);
+                            ptx::tma_store_2d(out_map[h], col, row0, mine);
+                            if (mirror) ptx::tma_store_2d(mir_map[h], row0, col, mine_t);
                             ptx::bulk_commit();
                         }
                         if (SPLIT && h == 0) {
@@ -362,10 +386,11 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
             if (lane == 0 && acc_ok) {
                 ptx::mbar_arrive_remote(ptx::map_to_cta(bar_acc_empty + 8 * buf, 0));
                 ptx::bulk_wait_all();                    // this warp's part of the tile is in memory (a completed bulk
-                red_release_gpu_add(op->counter, 1u);    // store needs no further proxy fence): count it
+                ptx::mbar_arrive(bar_landed + 8 * (n & 3));      // store needs no further proxy fence)
             }
-            if (__shfl_sync(0xFFFFFFFFu, *abort_flag, 0) != 0) break;
+            __syncwarp();
         }
+        if (__shfl_sync(0xFFFFFFFFu, *abort_flag, 0) != 0) break;
     }
 
     if (warp >= 4 && lane == 0) ptx::bulk_wait_all();

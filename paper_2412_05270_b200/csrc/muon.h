@@ -12,8 +12,8 @@ constexpr int MUON_PART = 256;          // most partial sums of squares per matr
 
 // out = alpha L R + b1 E1 + b2 E2 + diag I on stored (scaled) values; L is M x K with k contiguous, R is K x N, with
 // k contiguous (r_mn = 0: given as the N x K matrix) or with n contiguous (r_mn = 1).  [0] / [1]: the high and low
-// parts of split operands.  sym: M = N and the result is symmetric: tiles on and above the diagonal are computed,
-// the ones above also written transposed.
+// parts of split operands.  sym: M = N and the result is symmetric: it is computed from the diagonal's 256 x 256 blocks
+// on, and what lies beyond them also stored transposed.
 struct GemmOp {
     const void* l_map[2];               // DEVICE tensor maps
     const void* r_map[2];
@@ -23,10 +23,10 @@ struct GemmOp {
     const __half* e2[2];
     float alpha, b1, b2, diag;
     int32_t M, N, K, e_pitch, sym, r_mn;
-    uint32_t* counter;                  // DEVICE: epilogue warps of this matrix that are done, over all its products
+    uint32_t* counter;                  // DEVICE: CTAs done with tiles of this matrix, over all its products
     uint32_t need;                      // its value once the products before this one are complete
 };
-constexpr int MUON_WARPS_PER_TILE = 16; // counts that a finished tile adds
+constexpr int MUON_COUNTS_PER_TILE = 2;
 
 // One matrix of a streaming kernel.
 struct MuonItem {
@@ -68,9 +68,9 @@ int muon_stream_tiles(int rows, int cols);
 cudaError_t launch_muon_gemm(bool split, int bn, const GemmOp* d_ops, const uint4* d_list, int tiles, uint32_t* d_ticket, MuonLaunch& state,
                              int32_t* d_status, cudaStream_t stream);
 
-// Tensor maps of a rows x cols matrix of 16-bit floats (pitch a multiple of 8), 128 bytes each at maps[kind]:
-// boxes of 64 x 128 rows (an operand whose rows are contiguous along k), 64 x 64 (along n), and 32 x 32 to store a
-// piece, and to store it transposed.
+// Tensor maps of a rows x cols matrix of 16-bit floats (pitch a multiple of 8), 128 bytes each at maps[kind]: boxes of
+// 64 x 128 rows (an operand whose rows are contiguous along k) and 64 x 64 (half as many of them, or contiguous along n) to
+// load, 32 x 32 to store a piece, and to store it transposed.
 enum { MAP_ROWS, MAP_COLS, MAP_STORE, MAP_MIRROR, MUON_MAPS };
 int muon_encode_maps(const __half* base, int rows, int cols, int pitch, void* maps);
 
