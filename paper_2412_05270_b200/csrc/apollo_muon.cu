@@ -33,7 +33,7 @@ namespace {
 constexpr size_t ALIGN = 256;
 constexpr int MAX_SIDE = 1 << 20;
 constexpr double Q_SHIFT = 1.0;
-constexpr int WIDE_TILES = 148;
+constexpr int WIDE_TILES = 64;
 
 size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
 int round_up(int x, int to) { return (x + to - 1) / to * to; }
@@ -193,8 +193,9 @@ int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_confi
     }
     plan.n_ops = 0; plan.n_tiles = 0;
     for (Group& g : plan.groups) {
-        // Wide tiles move the fewest bytes per product; narrow ones halve the latency of a product and give twice as
-        // many: taken when the smallest product of the group would not fill the chip twice over.
+        // Wide tiles (256 columns) move the fewest bytes per product; narrow ones halve the latency of a product and give
+        // twice as many tiles.  By the tiles of the smallest product: 36 (one 2048 x 2048) 401 us narrow, 413 wide;
+        // 40 (four 1024 x 1024) 201, 232; 70 (a layer of 1024) 390, 370; 84 (28 matrices of a 60M model) 286, 282.
         int64_t sym = 0;
         for (int i : g.mats) sym += sym_tiles(plan.mats[i].m, 256);
         g.bn = sym >= WIDE_TILES ? 256 : 128;
