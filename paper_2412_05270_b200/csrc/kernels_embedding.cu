@@ -129,10 +129,11 @@ embed_kernel(const T* __restrict__ table, int64_t rows, int dim, const I* __rest
 // clusters of the launch write zeros over dE meanwhile (when not accumulating), which no step of the sort waits
 // for: the sort costs no time as long as it is shorter than that fill (V dim e bytes of writes).
 //
-// A pass over one 8-bit digit: every CTA counts the digits of its contiguous share; the counts are exchanged
-// through distributed shared memory (base of a digit = all smaller digits anywhere + the same digit in CTAs of
-// lower rank); then it ranks its share tile by tile and scatters.  Inside a tile a warp owns 32 x SORT_ITEMS
-// consecutive keys and takes them 32 at a time: __match_any_sync gives the lanes with the same digit, the
+// A pass over one 8-bit digit: every CTA ranks its contiguous share and counts its digits; the counts are exchanged
+// through distributed shared memory (base of a digit = all smaller digits anywhere + the same digit in CTAs of lower
+// rank); then it scatters.  A share of more than one tile is counted first and ranked tile by tile after the exchange;
+// one that fits a tile (SORT_CLUSTER x SORT_TILE = 32768 tokens) is read once.  Inside a tile a warp owns 32 x
+// SORT_ITEMS consecutive keys and takes them 32 at a time: __match_any_sync gives the lanes with the same digit, the
 // warp's running count of the digit the keys before them.
 struct SortArgs {
     uint2* buf[2];          // (key, position) ping-pong
@@ -149,11 +150,11 @@ embed_sort_kernel(const I* __restrict__ index, SortArgs a, uint4* __restrict__ z
     if (blockIdx.x >= SORT_CLUSTER) {
         const int64_t stride = (int64_t)(gridDim.x - SORT_CLUSTER) * SORT_THREADS;
         const int64_t first = (int64_t)(blockIdx.x - SORT_CLUSTER) * SORT_THREADS + threadIdx.x;
-        for (int64_t v = first; v < zero_vecs; v += stride) zero[v] = make_uint4(0, 0, 0, 0);
+        for (int64_t v = first; v < zero_vecs; v += stride) __stcs(zero + v, make_uint4(0, 0, 0, 0));
         if (first < zero_tail_bytes) zero_tail[first] = 0;
         return;
     }
-    __shared__ uint32_t hist[SORT_BINS];                 // this CTA's digit counts, read by the whole cluster
+    __shared__ uint32_t hist[2][SORT_BINS];              // this CTA's digit counts, read by the whole cluster; by pass parity
     __shared__ uint32_t base[SORT_BINS];                 // where the next key of a digit goes
     __shared__ uint32_t warp_hist[SORT_WARPS][SORT_BINS];
     __shared__ uint32_t scan[SORT_WARPS];
@@ -162,25 +163,82 @@ embed_sort_kernel(const I* __restrict__ index, SortArgs a, uint4* __restrict__ z
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int64_t share = (a.n + SORT_CLUSTER - 1) / SORT_CLUSTER;
     const int64_t begin = min((int64_t)cta * share, a.n), end = min(begin + share, a.n);
+    const bool one_tile = share <= SORT_TILE;
 
+    uint2 kv[SORT_ITEMS];
+    uint32_t rank[SORT_ITEMS];
     for (int pass = 0; pass < a.passes; ++pass) {
         const int shift = pass * SORT_BITS;
         const uint2* src = a.buf[(pass + 1) & 1];        // pass 0 reads the caller's indices
         uint2* dst = a.buf[pass & 1];
-        for (int d = tid; d < SORT_BINS; d += SORT_THREADS) hist[d] = 0;
-        __syncthreads();
-        for (int64_t t = begin + tid; t < end; t += SORT_THREADS) {
-            const uint32_t key = pass == 0 ? index_key(index, t, (int64_t)a.rows) : __ldcg(src + t).x;   // other CTAs wrote it in this launch: from L2
-            atomicAdd(&hist[(key >> shift) & (SORT_BINS - 1)], 1u);
+        uint32_t* const counts = hist[pass & 1];
+        // ranks of a tile within its warp; warp_hist holds the warps' digit counts afterwards
+        auto rank_tile = [&](int64_t tile) {
+            for (int d = tid; d < SORT_BINS * SORT_WARPS; d += SORT_THREADS) (&warp_hist[0][0])[d] = 0;
+            const int64_t first = tile + (int64_t)warp * (32 * SORT_ITEMS) + lane;
+#pragma unroll
+            for (int k = 0; k < SORT_ITEMS; ++k) {
+                const int64_t t = first + k * 32;
+                kv[k] = t >= end ? make_uint2(0xFFFFFFFFu, 0)
+                                 : (pass == 0 ? make_uint2(index_key(index, t, (int64_t)a.rows), (uint32_t)t)
+                                              : __ldcg(src + t));       // other CTAs wrote it in this launch: from L2
+            }
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < SORT_ITEMS; ++k) {
+                const bool valid = first + k * 32 < end;
+                const uint32_t d = (kv[k].x >> shift) & (SORT_BINS - 1);
+                const uint32_t same = __match_any_sync(0xFFFFFFFFu, valid ? d : 0xFFFFFFFFu);
+                const uint32_t below = __popc(same & ((1u << lane) - 1u));
+                rank[k] = below;
+                if (valid) rank[k] += warp_hist[warp][d];
+                __syncwarp();
+                if (valid && below == 0) warp_hist[warp][d] += __popc(same);
+                __syncwarp();
+            }
+            __syncthreads();
+        };
+        // warp_hist -> exclusive sums over the warps; returns the digit's count (threads below SORT_BINS)
+        auto scan_warps = [&](uint32_t run) {
+#pragma unroll
+            for (int w = 0; w < SORT_WARPS; ++w) {
+                const uint32_t h = warp_hist[w][tid];
+                warp_hist[w][tid] = run;
+                run += h;
+            }
+            return run;
+        };
+        auto scatter = [&](int64_t tile, bool add_base) {
+            const int64_t first = tile + (int64_t)warp * (32 * SORT_ITEMS) + lane;
+#pragma unroll
+            for (int k = 0; k < SORT_ITEMS; ++k)
+                if (first + k * 32 < end) {
+                    const uint32_t d = (kv[k].x >> shift) & (SORT_BINS - 1);
+                    dst[warp_hist[warp][d] + rank[k] + (add_base ? base[d] : 0u)] = kv[k];
+                }
+        };
+        if (one_tile) {
+            rank_tile(begin);
+            if (tid < SORT_BINS) counts[tid] = scan_warps(0);
+        } else {
+            for (int d = tid; d < SORT_BINS; d += SORT_THREADS) counts[d] = 0;
+            __syncthreads();
+            for (int64_t t = begin + tid; t < end; t += SORT_THREADS) {
+                const uint32_t key = pass == 0 ? index_key(index, t, (int64_t)a.rows) : __ldcg(src + t).x;
+                atomicAdd(&counts[(key >> shift) & (SORT_BINS - 1)], 1u);
+            }
         }
         cluster.sync();
         // digit totals over the cluster, their exclusive sum, and the counts of this digit in CTAs before this one
         uint32_t total = 0, before = 0;
         if (tid < SORT_BINS) {
+            uint32_t h[SORT_CLUSTER];
+#pragma unroll
+            for (int c = 0; c < SORT_CLUSTER; ++c) h[c] = cluster.map_shared_rank(counts, c)[tid];
+#pragma unroll
             for (int c = 0; c < SORT_CLUSTER; ++c) {
-                const uint32_t h = cluster.map_shared_rank(hist, c)[tid];
-                total += h;
-                if (c < cta) before += h;
+                total += h[c];
+                if (c < cta) before += h[c];
             }
         }
         uint32_t incl = total;
@@ -196,50 +254,20 @@ embed_sort_kernel(const I* __restrict__ index, SortArgs a, uint4* __restrict__ z
             for (int w = 0; w < warp; ++w) lower += scan[w];
             base[tid] = lower + incl - total + before;
         }
-        cluster.sync();                                  // everyone has read hist: it may be cleared in the next pass
-        for (int64_t tile = begin; tile < end; tile += SORT_TILE) {
-            for (int d = tid; d < SORT_BINS * SORT_WARPS; d += SORT_THREADS) (&warp_hist[0][0])[d] = 0;
-            __syncthreads();
-            uint2 kv[SORT_ITEMS];
-            uint32_t rank[SORT_ITEMS];
-            const int64_t first = tile + (int64_t)warp * (32 * SORT_ITEMS) + lane;
-#pragma unroll
-            for (int k = 0; k < SORT_ITEMS; ++k) {
-                const int64_t t = first + k * 32;
-                kv[k] = t >= end ? make_uint2(0xFFFFFFFFu, 0)
-                                 : (pass == 0 ? make_uint2(index_key(index, t, (int64_t)a.rows), (uint32_t)t) : __ldcg(src + t));
+        __syncthreads();
+        if (one_tile) {
+            scatter(begin, true);
+        } else {
+            for (int64_t tile = begin; tile < end; tile += SORT_TILE) {
+                rank_tile(tile);
+                if (tid < SORT_BINS) base[tid] = scan_warps(base[tid]);
+                __syncthreads();
+                scatter(tile, false);
+                __syncthreads();
             }
-#pragma unroll
-            for (int k = 0; k < SORT_ITEMS; ++k) {
-                const bool valid = first + k * 32 < end;
-                const uint32_t d = (kv[k].x >> shift) & (SORT_BINS - 1);
-                const uint32_t same = __match_any_sync(0xFFFFFFFFu, valid ? d : 0xFFFFFFFFu);
-                const uint32_t below = __popc(same & ((1u << lane) - 1u));
-                rank[k] = below;
-                if (valid) rank[k] += warp_hist[warp][d];
-                __syncwarp();
-                if (valid && below == 0) warp_hist[warp][d] += __popc(same);
-                __syncwarp();
-            }
-            __syncthreads();
-            // exclusive sums over the warps of each digit, then the digit's running base
-            if (tid < SORT_BINS) {
-                uint32_t run = base[tid];
-                for (int w = 0; w < SORT_WARPS; ++w) {
-                    const uint32_t h = warp_hist[w][tid];
-                    warp_hist[w][tid] = run;
-                    run += h;
-                }
-                base[tid] = run;
-            }
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < SORT_ITEMS; ++k)
-                if (first + k * 32 < end) dst[warp_hist[warp][(kv[k].x >> shift) & (SORT_BINS - 1)] + rank[k]] = kv[k];
-            __syncthreads();
         }
         __threadfence();
-        cluster.sync();                                  // the other CTAs read what this one scattered
+        cluster.sync();                                  // the other CTAs read what this one scattered, and have read its counts
     }
 }
 
@@ -332,42 +360,86 @@ embed_sum_kernel(const T* __restrict__ d_out, int64_t out_stride, const uint2* _
     }
 }
 
-// The segments that span windows: the block of the window in which such a segment starts adds up its partial rows
-// in window order.  Warps take contiguous ranges of the windows and their sums are added in warp order.
-template <typename T>
+// The segments that span windows: the blocks of the window in which such a segment starts add up its partial rows in
+// window order, V columns per thread; a segment of many windows is shared by the block's warps, which take contiguous
+// ranges of the windows and whose sums are added in warp order.  (V is 4 or 1: partial rows are whole vectors or not.)
+constexpr int JOIN_SPLIT = 32;         // windows from which on a segment is shared
+
+template <int V>
+__device__ __forceinline__ void add_partial(float (&acc)[V], const float* __restrict__ p)
+{
+    if constexpr (V == 4) {
+        const float4 x = *reinterpret_cast<const float4*>(p);
+        acc[0] += x.x; acc[1] += x.y; acc[2] += x.z; acc[3] += x.w;
+    } else {
+        acc[0] += *p;
+    }
+}
+
+template <typename T, int V>
 __global__ void __launch_bounds__(EMB_THREADS)
 embed_join_kernel(const uint2* __restrict__ sorted, int64_t n, uint32_t rows, int dim, float scale, bool accumulate,
                   T* __restrict__ d_table, const float* __restrict__ partial)
 {
-    __shared__ float sums[EMB_THREADS / 32][32];
+    __shared__ float sums[EMB_THREADS / 32][32 * V];
     const int64_t w = blockIdx.x, next = (w + 1) * EMB_WINDOW;
-    if (next >= n) return;
-    const uint32_t key = sorted[next - 1].x;
-    if (key >= rows || sorted[next].x != key) return;            // nothing goes on into the next window
-    if (w > 0 && sorted[w * EMB_WINDOW].x == key && sorted[w * EMB_WINDOW - 1].x == key) return;   // it began earlier
+    const uint32_t key = sorted[next - 1].x, key_next = sorted[next].x, key_first = sorted[w * EMB_WINDOW].x;
+    const uint32_t key_before = w > 0 ? sorted[w * EMB_WINDOW - 1].x : key_first;
+    if (key >= rows || key_next != key) return;                  // nothing goes on into the next window
+    if (w > 0 && key_first == key && key_before == key) return;  // it began earlier
     // first position after `next` with another token
     int64_t lo = next, hi = n;                                   // sorted[lo] == key, sorted[hi] != key (or hi == n)
+    for (int64_t step = EMB_WINDOW; lo + step < hi; step *= 2) { // most segments are short: gallop, then halve
+        if (sorted[lo + step].x != key) { hi = lo + step; break; }
+        lo += step;
+    }
     while (hi - lo > 1) {
         const int64_t mid = (lo + hi) >> 1;
         if (sorted[mid].x == key) lo = mid; else hi = mid;
     }
-    const int64_t last = (hi - 1) / EMB_WINDOW;                  // windows w + 1 .. last hold partial rows 2 x index, w its 2 w + 1
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t pieces = last - w + 1, per = (pieces + EMB_THREADS / 32 - 1) / (EMB_THREADS / 32);
-    const int64_t p0 = warp * per, p1 = min(p0 + per, pieces);
-    for (int c0 = blockIdx.y * 32; c0 < dim; c0 += gridDim.y * 32) {
-        const int c = c0 + lane;
-        float acc = 0.0f;
-        if (c < dim) {
-#pragma unroll 4
-            for (int64_t p = p0; p < p1; ++p) acc += partial[(2 * (w + p) + (p == 0 ? 1 : 0)) * dim + c];
+    const int64_t pieces = (hi - 1) / EMB_WINDOW - w + 1;        // window w holds partial row 2 w + 1, the later ones 2 x index
+    auto piece_at = [&](int64_t p) { return partial + (2 * (w + p) + (p == 0 ? 1 : 0)) * dim; };
+    auto write = [&](int c, const float (&total)[V]) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float one[1] = { total[e] };
+            grad_write<T, 1>(d_table, (int64_t)key, dim, c + e, one, scale, accumulate);
         }
-        sums[warp][lane] = acc;
+    };
+    if (pieces <= JOIN_SPLIT) {
+        for (int c = ((int)blockIdx.y * EMB_THREADS + threadIdx.x) * V; c < dim; c += (int)gridDim.y * EMB_THREADS * V) {
+            float acc[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+#pragma unroll 8
+            for (int64_t p = 0; p < pieces; ++p) add_partial<V>(acc, piece_at(p) + c);
+            write(c, acc);
+        }
+        return;
+    }
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t per = (pieces + EMB_THREADS / 32 - 1) / (EMB_THREADS / 32);
+    const int64_t p0 = warp * per, p1 = min(p0 + per, pieces);
+    for (int c0 = (int)blockIdx.y * 32 * V; c0 < dim; c0 += (int)gridDim.y * 32 * V) {
+        const int c = c0 + lane * V;
+        float acc[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] = 0.0f;
+        if (c < dim) {
+#pragma unroll 8
+            for (int64_t p = p0; p < p1; ++p) add_partial<V>(acc, piece_at(p) + c);
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) sums[warp][lane * V + e] = acc[e];
         __syncthreads();
         if (warp == 0 && c < dim) {
-            float total[1] = { 0.0f };
-            for (int k = 0; k < EMB_THREADS / 32; ++k) total[0] += sums[k][lane];
-            grad_write<T, 1>(d_table, (int64_t)key, dim, c, total, scale, accumulate);
+            float total[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                total[e] = 0.0f;
+                for (int k = 0; k < EMB_THREADS / 32; ++k) total[e] += sums[k][lane * V + e];
+            }
+            write(c, total);
         }
         __syncthreads();
     }
@@ -445,8 +517,11 @@ void run_embed_sum(const void* d_out, int64_t stride, const uint2* sorted, int64
     if (vector) embed_sum_kernel<T, true><<<grid, EMB_THREADS, 0, stream>>>((const T*)d_out, stride, sorted, n, rows, dim, scale, accumulate, (T*)d_table, partial, lg, windows);
     else embed_sum_kernel<T, false><<<grid, EMB_THREADS, 0, stream>>>((const T*)d_out, stride, sorted, n, rows, dim, scale, accumulate, (T*)d_table, partial, lg, windows);
     if (windows > 1) {
-        const int cb = (dim + 31) / 32;
-        embed_join_kernel<T><<<dim3((unsigned)(windows - 1), (unsigned)(cb < 64 ? cb : 64)), EMB_THREADS, 0, stream>>>(sorted, n, rows, dim, scale, accumulate, (T*)d_table, partial);
+        const int v = dim % 4 == 0 ? 4 : 1;
+        const int cb = (dim + EMB_THREADS * v - 1) / (EMB_THREADS * v);
+        const dim3 jgrid((unsigned)(windows - 1), (unsigned)(cb < 64 ? cb : 64));
+        if (v == 4) embed_join_kernel<T, 4><<<jgrid, EMB_THREADS, 0, stream>>>(sorted, n, rows, dim, scale, accumulate, (T*)d_table, partial);
+        else embed_join_kernel<T, 1><<<jgrid, EMB_THREADS, 0, stream>>>(sorted, n, rows, dim, scale, accumulate, (T*)d_table, partial);
     }
 }
 

@@ -7,9 +7,11 @@
 // Conventions: logits of -inf are masked words (p = 0, no gradient).  A row in which every word is masked has
 // lse = -inf, logp = -inf, H = 0, no gradient.  A target outside [0, vocab) is ignored: logp = 0, g counts as 0.
 //
-// Forward: one pass.  A thread keeps the running maximum m of its elements, s = sum exp(z - m) and
-// u = sum exp(z - m) (z - m); a new maximum rescales both (u by the shift too).  Joined over the block, then over
-// the cluster of CTAs that share a row, H = log s - u / s: the difference of small numbers, not of lse and a mean.
+// Forward: one pass.  A thread keeps the running maximum m of its elements and, with t = (logit - m) scale log2 e,
+// s = sum 2^t and u = sum 2^t t; a new maximum rescales both (u by the shift too).  Joined over the block, then over
+// the cluster of CTAs that share a row, H = log s - log 2 u / s: the difference of small numbers, not of lse and a mean.
+// Bound: HBM, N V e bytes; per element one exponential (16 a cycle and SM) and about five other instructions, which is
+// why the sums run on packed pairs (fma.rn.f32x2) and the maximum of bfloat16 words is taken two at a time.
 #include "../../include/apollo.h"
 
 #include <cooperative_groups.h>
@@ -24,10 +26,9 @@ namespace apollo {
 
 namespace {
 
-constexpr int LP_THREADS = 256;
 constexpr int LP_MAX_TOP = APOLLO_MAX_TOP;
 constexpr int LP_CAND = 1024;        // candidates one CTA collects before it falls back to picking one by one
-constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 template <typename T> struct LpVec;
 template <> struct LpVec<float> {
@@ -60,53 +61,115 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-// Running softmax statistics: m = max z, s = sum exp(z - m), u = sum exp(z - m) (z - m).  The difference comes first,
-// the factor log2 e after it: masks of the type's lowest value are finite numbers, and z log2 e would overflow there.
+// Pairs of floats in one 64-bit register.
+__device__ __forceinline__ uint64_t pair2(float lo, float hi)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// Statistics of a set of logits v: m = max v, s = sum 2^t, u = sum 2^t t, t = (v - m) L, L = scale log2 e.
 struct Stat { float m, s, u; };
 
-__device__ __forceinline__ Stat stat_empty() { return Stat{ -INFINITY, 0.0f, 0.0f }; }
-
 // Moves st to the maximum m >= st.m (m > -inf).
-__device__ __forceinline__ void stat_shift(Stat& st, float m)
+__device__ __forceinline__ void stat_shift(Stat& st, float m, float L)
 {
     if (st.s != 0.0f) {                     // (a NaN s is != 0 and stays NaN)
-        const float d = st.m - m, f = ex2(d * LOG2E);
-        st.u = f * fmaf(fmaxf(d, -1e30f), st.s, st.u);     // f is 0 long before the bound matters
+        const float t = (st.m - m) * L, f = ex2(t);
+        st.u = f * fmaf(fmaxf(t, -1000.0f), st.s, st.u);       // f is 0 long before the bound matters
         st.s *= f;
     }
     st.m = m;
 }
 
-__device__ __forceinline__ Stat stat_join(Stat a, Stat b)
+__device__ __forceinline__ Stat stat_join(Stat a, Stat b, float L)
 {
     const float m = fmaxf(a.m, b.m);
     if (m == -INFINITY) return Stat{ m, a.s + b.s, a.u + b.u };   // nothing on either side (or NaN sums)
-    stat_shift(a, m);
-    stat_shift(b, m);
+    stat_shift(a, m, L);
+    stat_shift(b, m, L);
     return Stat{ m, a.s + b.s, a.u + b.u };
 }
 
-// Adds N values z.
-template <int N>
-__device__ __forceinline__ void stat_add(Stat& st, const float (&z)[N])
+// A thread's running statistics, the sums in pairs.  The difference comes first, the factor L after it: masks of the
+// type's lowest value are finite numbers whose multiples would overflow, and the maximum itself has t = 0 exactly.
+struct Running {
+    float m;
+    uint64_t neg_m, s, u;                   // -m twice
+
+    __device__ __forceinline__ void init() { m = -INFINITY; neg_m = s = u = 0ull; }
+    __device__ __forceinline__ void raise(float top, float L)
+    {
+        if (m != -INFINITY || s != 0ull) {
+            const float t = (m - top) * L, f = ex2(t);
+            const uint64_t f2 = pair2(f, f), t2 = pair2(fmaxf(t, -1000.0f), fmaxf(t, -1000.0f));
+            u = fma2(f2, fma2(t2, s, u), 0ull);
+            s = fma2(f2, s, 0ull);
+        }
+        m = top;
+        neg_m = pair2(-top, -top);
+    }
+    // Two logits.  2^t is 0 where t is -inf: keep the product with it 0.
+    __device__ __forceinline__ void add(float v0, float v1, uint64_t L2)
+    {
+        float t0, t1;
+        unpack2(mul2(add2(pair2(v0, v1), neg_m), L2), t0, t1);
+        const uint64_t p = pair2(ex2(t0), ex2(t1));
+        s = add2(s, p);
+        u = fma2(p, pair2(fmaxf(t0, -1000.0f), fmaxf(t1, -1000.0f)), u);
+    }
+    __device__ __forceinline__ Stat stat() const
+    {
+        float s0, s1, u0, u1;
+        unpack2(s, s0, s1);
+        unpack2(u, u0, u1);
+        return Stat{ m, s0 + s1, u0 + u1 };
+    }
+    // N logits whose maximum (NaN aside) is `top`.
+    template <int N>
+    __device__ __forceinline__ void add_all(const float (&v)[N], float top, float L)
+    {
+        if (top > m) raise(top, L);
+        if (m == -INFINITY) {
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (v[e] != v[e]) s = pair2(NAN, 0.0f);
+            return;
+        }
+        const uint64_t L2 = pair2(L, L);
+#pragma unroll
+        for (int e = 0; e < N; e += 2) add(v[e], v[e + 1], L2);
+    }
+};
+
+// The maximum of a 16-byte vector of logits (NaN aside).
+__device__ __forceinline__ float vec_max(const uint4& r, const float (&)[8])
 {
-    float top = z[0];
-#pragma unroll
-    for (int e = 1; e < N; ++e) top = fmaxf(top, z[e]);
-    if (top > st.m) stat_shift(st, top);
-    if (st.m == -INFINITY) {
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            if (z[e] != z[e]) st.s = NAN;
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-        const float d = z[e] - st.m, p = ex2(d * LOG2E);
-        st.s += p;
-        st.u = fmaf(p, fmaxf(d, -1e30f), st.u);            // p is 0 where d is -inf: keep the product 0
-    }
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&r);
+    const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    return fmaxf(__low2float(m), __high2float(m));
 }
+__device__ __forceinline__ float vec_max(const uint4&, const float (&v)[4]) { return fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])); }
 
 // Order of the alternatives: larger value first, then the lower index.  As one 64-bit key: the value's bits made
 // monotone, then the complement of the index.  -0 counts as +0, NaN as the lowest value.  0 is "no entry".
@@ -146,54 +209,23 @@ struct LogprobArgs {
     int* top_index;
 };
 
-// The elements of [begin, end) of a row in 16-byte vectors: f1(index, value) for the few before the first 16-byte
-// boundary and after the last, fv(index of the first, values) for whole vectors, four loads in flight.
-template <typename T, int THREADS, class F1, class FV>
-__device__ __forceinline__ void for_row(const T* __restrict__ row, int begin, int end, F1&& f1, FV&& fv)
-{
-    constexpr int V = LpVec<T>::N;
-    const int mis = (int)(((uintptr_t)(row + begin) % 16) / sizeof(T));
-    int head = mis ? V - mis : 0;
-    if (head > end - begin) head = end - begin;
-    const int vecs = (end - begin - head) / V;
-    const int v0 = begin + head, tail0 = v0 + vecs * V;
-    const int tid = threadIdx.x;
-    if (tid < head) f1(begin + tid, load1(row + begin + tid));
-    if (tid < end - tail0) f1(tail0 + tid, load1(row + tail0 + tid));
-    const uint4* p = reinterpret_cast<const uint4*>(row + v0);
-    int u = tid;
-    for (; u + 3 * THREADS < vecs; u += 4 * THREADS) {
-        uint4 raw[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) raw[k] = __ldg(p + u + k * THREADS);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            float v[V];
-            LpVec<T>::unpack(raw[k], v);
-            fv(v0 + (u + k * THREADS) * V, v);
-        }
-    }
-    for (; u < vecs; u += THREADS) {
-        float v[V];
-        LpVec<T>::unpack(__ldg(p + u), v);
-        fv(v0 + u * V, v);
-    }
-}
-
-// A cluster of gridDim.x / n_rows CTAs per row (1, 2, 4 or 8); each takes a contiguous part of the vocabulary.
-// TOP: also the `top` best words.  In the pass a thread remembers the best key of its elements; the top-th
-// largest of the threads' keys is a lower bound of the top-th largest of all, so a second look at the part (it
-// has just been read: L2 at most) collects the few words at or above that bound, and ranking them by counting
-// gives the list.  Should more than LP_CAND words pass (a part sorted against the stride), they are picked one by
-// one instead: slow, and right.
-template <typename T, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS)
+// A cluster of gridDim.x / n_rows CTAs per row (1, 2, 4 or 8); each takes a contiguous part of the vocabulary, 4 vectors
+// of 16 bytes per thread and round, the few elements before the first 16-byte boundary and after the last beside them.
+//
+// TOP: also the `top` best words, in the same pass.  After the first round the top-th largest of the threads' best keys
+// is a lower bound of the top-th largest of all; from then on a thread looks at a vector's elements only if its maximum
+// (which the statistics need anyway) reaches the bound, and collects those that do.  When the collection is half full it
+// is cut to its `top` best, which raises the bound.  Ranks are found by counting larger keys (they are distinct).  Should
+// one round bring more than the collection holds (rising logits), the words are picked one by one from the row instead:
+// slow, and right.
+template <typename T, bool TOP, int THREADS>
+__global__ void __launch_bounds__(THREADS)
 logprob_kernel(LogprobArgs a)
 {
-    constexpr int V = LpVec<T>::N;
+    constexpr int V = LpVec<T>::N, WARPS = THREADS / 32;
     __shared__ Stat part;                             // this CTA's statistics, read by rank 0 of the cluster
-    __shared__ Stat warp_stat[LP_THREADS / 32];
-    __shared__ uint64_t keys[TOP ? LP_THREADS : 1];
+    __shared__ Stat warp_stat[WARPS];
+    __shared__ uint64_t keys[TOP ? THREADS : 1];
     __shared__ uint64_t cand[TOP ? LP_CAND : 1];
     __shared__ uint64_t best[TOP ? LP_MAX_TOP : 1];   // this CTA's list, read by rank 0 of the cluster
     __shared__ uint64_t bound;
@@ -201,108 +233,164 @@ logprob_kernel(LogprobArgs a)
     cg::cluster_group cluster = cg::this_cluster();
     const int parts = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int64_t r = blockIdx.x / parts;
-    const T* row = static_cast<const T*>(a.logits) + r * a.stride;
+    const T* __restrict__ row = static_cast<const T*>(a.logits) + r * a.stride;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    int per = ((a.vocab + parts - 1) / parts + V - 1) / V * V;
+    const int per = ((a.vocab + parts - 1) / parts + V - 1) / V * V;
     const int begin = min(rank * per, a.vocab), end = min(begin + per, a.vocab);
+    const float scale = a.scale, L = scale * LOG2E;
 
-    Stat st = stat_empty();
-    uint64_t mine = 0;
-    float mine_v = -INFINITY;
-    bool any = false;
-    const float scale = a.scale;
-    auto one = [&](int i, float v) {
-        const float z[1] = { v * scale };
-        stat_add(st, z);
-        if constexpr (TOP) {
-            const uint64_t k = top_key(z[0], (uint32_t)i);
-            if (k > mine) { mine = k; mine_v = z[0]; any = true; }
-        }
+    const int mis = (int)(((uintptr_t)(row + begin) % 16) / sizeof(T));
+    const int head = min(mis ? V - mis : 0, end - begin);
+    const int vecs = (end - begin - head) / V;
+    const int v0 = begin + head, tail0 = v0 + vecs * V;
+    const uint4* vec = reinterpret_cast<const uint4*>(row + v0);
+
+    if constexpr (TOP) {
+        if (tid == 0) { n_cand = 0; bound = 0; }
+        if (tid < LP_MAX_TOP) best[tid] = 0;
+    }
+    Running run;
+    run.init();
+    // at most one element of the head and one of the tail per thread
+    float edge[2] = { -INFINITY, -INFINITY };
+    const int edge_at[2] = { tid < head ? begin + tid : -1, tid < end - tail0 ? tail0 + tid : -1 };
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (edge_at[i] >= 0) edge[i] = load1(row + edge_at[i]);
+    run.add_all(edge, fmaxf(edge[0], edge[1]), L);
+
+    uint64_t lim = 0;
+    float lim_v = -INFINITY;
+    bool flood = false;
+    auto collect = [&](int i, float z) {
+        const uint64_t k = top_key(z, (uint32_t)i);
+        if (k < lim) return;
+        const int at = atomicAdd(&n_cand, 1);
+        if (at < LP_CAND) cand[at] = k;
     };
-    for_row<T, LP_THREADS>(row, begin, end, one, [&](int i, const float (&v)[V]) {
-        float z[V];
+    // keeps the `top` best of the collection and raises the bound to the last of them
+    auto cut = [&](int n) {
+        for (int c = tid; c < n; c += THREADS) {
+            const uint64_t k = cand[c];
+            int ahead = 0;
+            for (int o = 0; o < n; ++o) ahead += cand[o] > k ? 1 : 0;
+            if (ahead < a.top) best[ahead] = k;
+        }
+        __syncthreads();
+    };
+    const int rounds = max(1, (vecs + 4 * THREADS - 1) / (4 * THREADS));
+    uint4 next[4];                                    // one round ahead
 #pragma unroll
-        for (int e = 0; e < V; ++e) z[e] = v[e] * scale;
-        stat_add(st, z);
+    for (int k = 0; k < 4; ++k)
+        if (tid + k * THREADS < vecs) next[k] = __ldg(vec + tid + k * THREADS);
+    for (int round = 0; round < rounds; ++round) {
+        const int u0 = round * 4 * THREADS + tid;
+        uint4 raw[4];
+        float top[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            raw[k] = next[k];
+            if (u0 + (4 + k) * THREADS < vecs) next[k] = __ldg(vec + u0 + (4 + k) * THREADS);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (u0 + k * THREADS >= vecs) break;
+            float v[V];
+            LpVec<T>::unpack(raw[k], v);
+            top[k] = vec_max(raw[k], v);
+            run.add_all(v, top[k], L);
+        }
         if constexpr (TOP) {
-            float top = z[0];
+            if (round == 0) {
+                uint64_t mine = 0;
+                auto see = [&](int i, float v) {
+                    const uint64_t k = top_key(__fmul_rn(v, scale), (uint32_t)i);
+                    if (k > mine) mine = k;
+                };
 #pragma unroll
-            for (int e = 1; e < V; ++e) top = fmaxf(top, z[e]);
-            if (!any || !(top < mine_v)) {            // ties are settled by the index, which is in the key
+                for (int i = 0; i < 2; ++i)
+                    if (edge_at[i] >= 0) see(edge_at[i], edge[i]);
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const uint64_t k = top_key(z[e], (uint32_t)(i + e));
-                    if (k > mine) { mine = k; mine_v = z[e]; }
+                for (int k = 0; k < 4; ++k) {
+                    if (u0 + k * THREADS >= vecs) break;
+                    if (mine != 0 && __fmul_rn(top[k], scale) < top_value(mine)) continue;
+                    float v[V];
+                    LpVec<T>::unpack(raw[k], v);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) see(v0 + (u0 + k * THREADS) * V + e, v[e]);
                 }
-                any = true;
+                keys[tid] = mine;
+                __syncthreads();
+                // the top-th largest of the threads' keys (0 where fewer threads have one: then everything passes)
+                int above = 0;
+                for (int k = 0; k < THREADS; ++k) above += keys[k] > mine ? 1 : 0;
+                if (mine != 0 && above == a.top - 1) bound = mine;
+                __syncthreads();
+                lim = bound;
+                lim_v = lim ? top_value(lim) : -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (edge_at[i] >= 0) collect(edge_at[i], __fmul_rn(edge[i], scale));
+            }
+            if (!flood) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (u0 + k * THREADS >= vecs) break;
+                    if (__fmul_rn(top[k], scale) < lim_v) continue;
+                    float v[V];
+                    LpVec<T>::unpack(raw[k], v);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float z = __fmul_rn(v[e], scale);
+                        if (!(z < lim_v)) collect(v0 + (u0 + k * THREADS) * V + e, z);
+                    }
+                }
+                __syncthreads();
+                const int n = n_cand;
+                flood = n > LP_CAND;
+                if (n > LP_CAND / 2 && !flood) {
+                    cut(n);
+                    if (tid < a.top) cand[tid] = best[tid];
+                    if (tid == 0) n_cand = a.top;
+                    lim = best[a.top - 1];
+                    lim_v = top_value(lim);
+                }
+                __syncthreads();
             }
         }
-    });
+    }
+    Stat st = run.stat();
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
         Stat o;
         o.m = __shfl_xor_sync(0xFFFFFFFFu, st.m, off);
         o.s = __shfl_xor_sync(0xFFFFFFFFu, st.s, off);
         o.u = __shfl_xor_sync(0xFFFFFFFFu, st.u, off);
-        st = stat_join(st, o);
+        st = stat_join(st, o, L);
     }
     if (lane == 0) warp_stat[warp] = st;
-    if constexpr (TOP) {
-        keys[tid] = mine;
-        if (tid == 0) { n_cand = 0; bound = 0; }
-        if (tid < LP_MAX_TOP) best[tid] = 0;
-    }
     __syncthreads();
     if (tid == 0) {
         Stat all = warp_stat[0];
-        for (int w = 1; w < LP_THREADS / 32; ++w) all = stat_join(all, warp_stat[w]);
+        for (int w = 1; w < WARPS; ++w) all = stat_join(all, warp_stat[w], L);
         part = all;
     }
     if constexpr (TOP) {
-        // the top-th largest of the threads' keys (0 where fewer threads have one: then everything passes)
-        int above = 0;
-        for (int k = 0; k < LP_THREADS; ++k) above += keys[k] > mine ? 1 : 0;
-        if (mine != 0 && above == a.top - 1) bound = mine;
-        __syncthreads();
-        const uint64_t lim = bound;
-        const float lim_v = lim ? top_value(lim) : -INFINITY;
-        auto pick = [&](int i, float z) {
-            if (lim != 0 && z < lim_v) return;
-            const uint64_t k = top_key(z, (uint32_t)i);
-            if (k < lim) return;
-            const int at = atomicAdd(&n_cand, 1);
-            if (at < LP_CAND) cand[at] = k;
-        };
-        for_row<T, LP_THREADS>(row, begin, end, [&](int i, float v) { pick(i, v * scale); }, [&](int i, const float (&v)[V]) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) pick(i + e, v[e] * scale);
-        });
-        __syncthreads();
-        const int n = n_cand;
-        if (n <= LP_CAND) {
-            for (int c = tid; c < n; c += LP_THREADS) {
-                const uint64_t k = cand[c];
-                int ahead = 0;
-                for (int o = 0; o < n; ++o) ahead += cand[o] > k ? 1 : 0;
-                if (ahead < a.top) best[ahead] = k;
-            }
+        if (!flood) {
+            cut(n_cand);
         } else {
             uint64_t last = ~0ull;
             for (int t = 0; t < a.top; ++t) {
                 uint64_t b = 0;
-                auto next = [&](int i, float z) {
-                    const uint64_t k = top_key(z, (uint32_t)i);
+                for (int i = begin + tid; i < end; i += THREADS) {
+                    const uint64_t k = top_key(__fmul_rn(load1(row + i), scale), (uint32_t)i);
                     if (k < last && k > b) b = k;
-                };
-                for_row<T, LP_THREADS>(row, begin, end, [&](int i, float v) { next(i, v * scale); }, [&](int i, const float (&v)[V]) {
-#pragma unroll
-                    for (int e = 0; e < V; ++e) next(i + e, v[e] * scale);
-                });
+                }
                 b = warp_max(b);
                 __syncthreads();
                 if (lane == 0) keys[warp] = b;
                 __syncthreads();
-                for (int w = 0; w < LP_THREADS / 32; ++w) b = keys[w] > b ? keys[w] : b;
+                for (int w = 0; w < WARPS; ++w) b = keys[w] > b ? keys[w] : b;
                 if (tid == 0) best[t] = b;
                 last = b;
             }
@@ -310,27 +398,31 @@ logprob_kernel(LogprobArgs a)
     }
     if (parts > 1) cluster.sync(); else __syncthreads();
     if (rank == 0) {
-        Stat all = stat_empty();
-        for (int c = 0; c < parts; ++c) all = stat_join(all, *cluster.map_shared_rank(&part, c));
-        const bool dead = all.m == -INFINITY && all.s == 0.0f;
+        Stat all = *cluster.map_shared_rank(&part, 0);
+        for (int c = 1; c < parts; ++c) all = stat_join(all, *cluster.map_shared_rank(&part, c), L);
+        const bool dead = __fmul_rn(all.m, scale) == -INFINITY && all.s == all.s;     // (and no NaN)
         const float log_s = dead ? 0.0f : logf(all.s);
-        const float lse = dead ? -INFINITY : all.m + log_s;
+        const float lse = dead ? -INFINITY : fmaf(all.m, scale, log_s);
         if (tid == 0) {
             const long long t = a.index64 ? static_cast<const long long*>(a.targets)[r] : (long long)static_cast<const int*>(a.targets)[r];
             const bool live = t >= 0 && t < a.vocab;
             a.lse[r] = lse;
-            a.entropy[r] = dead ? 0.0f : log_s - all.u / all.s;
+            a.entropy[r] = dead ? 0.0f : log_s - LN2 * (all.u / all.s);
             a.logprob[r] = !live ? 0.0f : dead ? -INFINITY : __fmul_rn(load1(row + t), scale) - lse;
         }
         if constexpr (TOP) {
-            // keys are distinct: an entry's place in the joined list is the number of larger ones
             const int n = parts * a.top;              // at most 8 x 32
-            for (int c = tid; c < n; c += LP_THREADS) cand[c] = cluster.map_shared_rank(best, c / a.top)[c % a.top];
-            __syncthreads();
-            for (int c = tid; c < n; c += LP_THREADS) {
-                const uint64_t k = cand[c];
-                int ahead = 0;
-                for (int o = 0; o < n; ++o) ahead += cand[o] > k ? 1 : 0;
+            if (parts > 1) {
+                for (int c = tid; c < n; c += THREADS) cand[c] = cluster.map_shared_rank(best, c / a.top)[c % a.top];
+                __syncthreads();
+            }
+            for (int c = tid; c < n; c += THREADS) {
+                const uint64_t k = parts > 1 ? cand[c] : best[c];
+                int ahead = c;
+                if (parts > 1) {
+                    ahead = 0;
+                    for (int o = 0; o < n; ++o) ahead += cand[o] > k ? 1 : 0;
+                }
                 if (k != 0 && ahead < a.top) {
                     const float z = (uint32_t)(k >> 32) == 1u ? NAN : top_value(k);
                     a.top_index[r * a.top + ahead] = (int)~(uint32_t)k;
@@ -355,10 +447,12 @@ struct LogprobGradArgs {
     void* out;
 };
 
+constexpr int LG_THREADS = 256;
+
 // One block per row and column chunk; reads the logits and writes their gradient, 2 e bytes an element: HBM-bound.
 // VECTOR: logits and gradient rows start on 16-byte boundaries.  In place works: a thread writes what it has read.
 template <typename T, bool VECTOR>
-__global__ void __launch_bounds__(LP_THREADS)
+__global__ void __launch_bounds__(LG_THREADS)
 logprob_grad_kernel(LogprobGradArgs a)
 {
     constexpr int V = VECTOR ? LpVec<T>::N : 1;
@@ -382,8 +476,8 @@ logprob_grad_kernel(LogprobGradArgs a)
         return x;
     };
     const int units = a.vocab / V;
-    const int step = (int)gridDim.y * LP_THREADS;
-    for (int u0 = (int)blockIdx.y * LP_THREADS + threadIdx.x; u0 < units; u0 += 4 * step) {
+    const int step = (int)gridDim.y * LG_THREADS;
+    for (int u0 = (int)blockIdx.y * LG_THREADS + threadIdx.x; u0 < units; u0 += 4 * step) {
         if constexpr (VECTOR) {
             uint4 raw[4];
 #pragma unroll
@@ -427,19 +521,22 @@ template <typename T>
 cudaError_t run_logprob(const LogprobArgs& a, int sms, cudaStream_t stream)
 {
     // A row is shared by as many CTAs as keep the chip busy: up to 8 while there are fewer CTAs than SMs and every
-    // CTA still has a few vectors per thread.
+    // CTA still has a few vectors per thread.  Short rows take small blocks: more rows at once, fewer idle threads.
+    const int threads = (int64_t)a.vocab * (int64_t)sizeof(T) <= 8192 ? 64 : 256;
     int parts = 1;
-    while (parts < 8 && a.n_rows * parts * 2 <= sms && a.vocab / (parts * 2) >= 2 * LP_THREADS) parts *= 2;
+    while (parts < 8 && a.n_rows * parts * 2 <= sms && a.vocab / (parts * 2) >= 512) parts *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(a.n_rows * parts));
-    cfg.blockDim = dim3(LP_THREADS);
+    cfg.blockDim = dim3((unsigned)threads);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)parts; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return a.top > 0 ? cudaLaunchKernelEx(&cfg, logprob_kernel<T, true>, a) : cudaLaunchKernelEx(&cfg, logprob_kernel<T, false>, a);
+    if (threads == 64)
+        return a.top > 0 ? cudaLaunchKernelEx(&cfg, logprob_kernel<T, true, 64>, a) : cudaLaunchKernelEx(&cfg, logprob_kernel<T, false, 64>, a);
+    return a.top > 0 ? cudaLaunchKernelEx(&cfg, logprob_kernel<T, true, 256>, a) : cudaLaunchKernelEx(&cfg, logprob_kernel<T, false, 256>, a);
 }
 
 template <typename T>
@@ -448,12 +545,12 @@ void run_logprob_grad(const LogprobGradArgs& a, cudaStream_t stream)
     const bool vector = (uintptr_t)a.logits % 16 == 0 && (uintptr_t)a.out % 16 == 0 &&
                         (size_t)a.stride * sizeof(T) % 16 == 0 && (size_t)a.out_stride * sizeof(T) % 16 == 0;
     const int units = vector ? a.vocab / LpVec<T>::N : a.vocab;
-    int chunks = (units + 4 * LP_THREADS - 1) / (4 * LP_THREADS);
+    int chunks = (units + 4 * LG_THREADS - 1) / (4 * LG_THREADS);
     if (chunks < 1) chunks = 1;
     if (chunks > 65535) chunks = 65535;
     const dim3 grid((unsigned)a.n_rows, (unsigned)chunks);
-    if (vector) logprob_grad_kernel<T, true><<<grid, LP_THREADS, 0, stream>>>(a);
-    else logprob_grad_kernel<T, false><<<grid, LP_THREADS, 0, stream>>>(a);
+    if (vector) logprob_grad_kernel<T, true><<<grid, LG_THREADS, 0, stream>>>(a);
+    else logprob_grad_kernel<T, false><<<grid, LG_THREADS, 0, stream>>>(a);
 }
 
 }  // namespace
