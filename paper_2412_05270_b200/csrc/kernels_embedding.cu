@@ -143,7 +143,7 @@ struct SortArgs {
 };
 
 template <typename I>
-__global__ void __cluster_dims__(SORT_CLUSTER, 1, 1) __launch_bounds__(SORT_THREADS)
+__global__ void __cluster_dims__(SORT_CLUSTER, 1, 1) __launch_bounds__(SORT_THREADS, 2)
 embed_sort_kernel(const I* __restrict__ index, SortArgs a, uint4* __restrict__ zero, int64_t zero_vecs, char* __restrict__ zero_tail,
                   int zero_tail_bytes)
 {
@@ -272,35 +272,26 @@ embed_sort_kernel(const I* __restrict__ index, SortArgs a, uint4* __restrict__ z
 }
 
 // ---------------------------------------------------------------- sums
-// Columns [c0, c0 + V) of dE row `row` <- acc (scaled), added to what is there when accumulating.
-template <typename T, int V>
-__device__ __forceinline__ void grad_write(T* __restrict__ d_table, int64_t row, int dim, int c, const float (&acc)[V], float scale, bool accumulate)
+// Columns [c, c + V) of dE row `row` <- acc (scaled), added to `old` when accumulating.
+template <typename T, int V, bool ACCUMULATE>
+__device__ __forceinline__ void grad_write(T* __restrict__ d_table, int64_t row, int dim, int c, const float (&acc)[V], float scale, const float (&old)[V])
 {
     T* p = d_table + row * dim + c;
-    if constexpr (V > 1) {
-        float v[V];
-        if (accumulate) {
-            Vec16<T>::unpack(*reinterpret_cast<const uint4*>(p), v);
+    float v[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[e] = fmaf(acc[e], scale, v[e]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e) v[e] = acc[e] * scale;
-        }
-        __stcs(reinterpret_cast<uint4*>(p), Vec16<T>::pack(v));
-    } else {
-        emb_store1<T>(p, accumulate ? fmaf(acc[0], scale, load1(p)) : acc[0] * scale);
-    }
+    for (int e = 0; e < V; ++e) v[e] = ACCUMULATE ? fmaf(acc[e], scale, old[e]) : acc[e] * scale;
+    if constexpr (V > 1) __stcs(reinterpret_cast<uint4*>(p), Vec16<T>::pack(v));
+    else emb_store1<T>(p, v[0]);
 }
 
 // One window of sorted positions and `tpw` x V columns per thread group.  A run of equal tokens that both starts
 // and ends in the window is written to dE; the first run, when it began in an earlier window, goes to partial row
 // 2 w, and the last one, when it goes on in the next window, to partial row 2 w + 1 (a run that does both counts
 // as the first).  Bound: HBM, every row of dOut read once; eight rows' loads are issued before the first is added.
-template <typename T, bool VECTOR>
+template <typename T, bool VECTOR, bool ACCUMULATE>
 __global__ void __launch_bounds__(EMB_THREADS)
 embed_sum_kernel(const T* __restrict__ d_out, int64_t out_stride, const uint2* __restrict__ sorted, int64_t n, uint32_t rows, int dim,
-                 float scale, bool accumulate, T* __restrict__ d_table, float* __restrict__ partial, int tpw_log2, int64_t windows)
+                 float scale, T* d_table, float* __restrict__ partial, int tpw_log2, int64_t windows)
 {
     constexpr int V = VECTOR ? Vec16<T>::N : 1;
     __shared__ uint2 entry[EMB_THREADS / 8][EMB_WINDOW];
@@ -325,6 +316,20 @@ embed_sum_kernel(const T* __restrict__ d_out, int64_t out_stride, const uint2* _
         for (int i0 = 0; i0 < count; i0 += 8) {
             float v[8][V];
             uint4 raw[8];
+            // what a run that ends here is added to: asked for with the rows, not when it is due
+            uint4 old[ACCUMULATE && VECTOR ? 8 : 1];
+            float old1[ACCUMULATE && !VECTOR ? 8 : 1];
+            if constexpr (ACCUMULATE) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int i = i0 + k;
+                    const uint32_t key = entry[g][i & (EMB_WINDOW - 1)].x;
+                    const bool ends = i < count && key < rows && (i + 1 == count || entry[g][(i + 1) & (EMB_WINDOW - 1)].x != key);
+                    const T* p = d_table + (int64_t)key * dim + c;
+                    if constexpr (VECTOR) old[k] = ends ? *reinterpret_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0);
+                    else old1[k] = ends ? load1(p) : 0.0f;
+                }
+            }
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const bool in = i0 + k < count && entry[g][(i0 + k) & (EMB_WINDOW - 1)].x < rows;
@@ -349,7 +354,12 @@ embed_sum_kernel(const T* __restrict__ d_out, int64_t out_stride, const uint2* _
 #pragma unroll
                         for (int e = 0; e < V; ++e) p[e] = acc[e];
                     } else {
-                        grad_write<T, V>(d_table, (int64_t)key, dim, c, acc, scale, accumulate);
+                        float o[V];
+                        if constexpr (ACCUMULATE) {
+                            if constexpr (VECTOR) Vec16<T>::unpack(old[k], o);
+                            else o[0] = old1[k];
+                        }
+                        grad_write<T, V, ACCUMULATE>(d_table, (int64_t)key, dim, c, acc, scale, o);
                     }
                 }
                 first_run = false;
@@ -363,7 +373,7 @@ embed_sum_kernel(const T* __restrict__ d_out, int64_t out_stride, const uint2* _
 // The segments that span windows: the blocks of the window in which such a segment starts add up its partial rows in
 // window order, V columns per thread; a segment of many windows is shared by the block's warps, which take contiguous
 // ranges of the windows and whose sums are added in warp order.  (V is 4 or 1: partial rows are whole vectors or not.)
-constexpr int JOIN_SPLIT = 32;         // windows from which on a segment is shared
+constexpr int JOIN_SPLIT = 256;        // windows from which on a segment is shared (8192 positions of one token)
 
 template <int V>
 __device__ __forceinline__ void add_partial(float (&acc)[V], const float* __restrict__ p)
@@ -376,10 +386,10 @@ __device__ __forceinline__ void add_partial(float (&acc)[V], const float* __rest
     }
 }
 
-template <typename T, int V>
+template <typename T, int V, bool ACCUMULATE>
 __global__ void __launch_bounds__(EMB_THREADS)
-embed_join_kernel(const uint2* __restrict__ sorted, int64_t n, uint32_t rows, int dim, float scale, bool accumulate,
-                  T* __restrict__ d_table, const float* __restrict__ partial)
+embed_join_kernel(const uint2* __restrict__ sorted, int64_t n, uint32_t rows, int dim, float scale, T* d_table,
+                  const float* __restrict__ partial)
 {
     __shared__ float sums[EMB_THREADS / 32][32 * V];
     const int64_t w = blockIdx.x, next = (w + 1) * EMB_WINDOW;
@@ -403,7 +413,9 @@ embed_join_kernel(const uint2* __restrict__ sorted, int64_t n, uint32_t rows, in
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             const float one[1] = { total[e] };
-            grad_write<T, 1>(d_table, (int64_t)key, dim, c + e, one, scale, accumulate);
+            float old[1] = { 0.0f };
+            if constexpr (ACCUMULATE) old[0] = load1(d_table + (int64_t)key * dim + c + e);
+            grad_write<T, 1, ACCUMULATE>(d_table, (int64_t)key, dim, c + e, one, scale, old);
         }
     };
     if (pieces <= JOIN_SPLIT) {
@@ -411,7 +423,7 @@ embed_join_kernel(const uint2* __restrict__ sorted, int64_t n, uint32_t rows, in
             float acc[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) acc[e] = 0.0f;
-#pragma unroll 8
+#pragma unroll 16
             for (int64_t p = 0; p < pieces; ++p) add_partial<V>(acc, piece_at(p) + c);
             write(c, acc);
         }
@@ -500,8 +512,8 @@ void run_embed(const void* table, int64_t rows, int dim, const void* index, int6
     else embed_kernel<T, I, false><<<grid, EMB_THREADS, 0, stream>>>((const T*)table, rows, dim, (const I*)index, n, scale, (T*)out, stride, lg);
 }
 
-template <typename T>
-void run_embed_sum(const void* d_out, int64_t stride, const uint2* sorted, int64_t n, uint32_t rows, int dim, float scale, bool accumulate,
+template <typename T, bool ACCUMULATE>
+void run_embed_sum(const void* d_out, int64_t stride, const uint2* sorted, int64_t n, uint32_t rows, int dim, float scale,
                    void* d_table, float* partial, cudaStream_t stream)
 {
     const bool vector = (size_t)dim * sizeof(T) % 16 == 0 && (size_t)stride * sizeof(T) % 16 == 0 &&
@@ -514,14 +526,14 @@ void run_embed_sum(const void* d_out, int64_t stride, const uint2* sorted, int64
     const int groups = EMB_THREADS >> lg;
     const int cols = (units + (1 << lg) - 1) >> lg;
     const dim3 grid((unsigned)((windows + groups - 1) / groups), (unsigned)(cols < 1024 ? cols : 1024));
-    if (vector) embed_sum_kernel<T, true><<<grid, EMB_THREADS, 0, stream>>>((const T*)d_out, stride, sorted, n, rows, dim, scale, accumulate, (T*)d_table, partial, lg, windows);
-    else embed_sum_kernel<T, false><<<grid, EMB_THREADS, 0, stream>>>((const T*)d_out, stride, sorted, n, rows, dim, scale, accumulate, (T*)d_table, partial, lg, windows);
+    if (vector) embed_sum_kernel<T, true, ACCUMULATE><<<grid, EMB_THREADS, 0, stream>>>((const T*)d_out, stride, sorted, n, rows, dim, scale, (T*)d_table, partial, lg, windows);
+    else embed_sum_kernel<T, false, ACCUMULATE><<<grid, EMB_THREADS, 0, stream>>>((const T*)d_out, stride, sorted, n, rows, dim, scale, (T*)d_table, partial, lg, windows);
     if (windows > 1) {
         const int v = dim % 4 == 0 ? 4 : 1;
         const int cb = (dim + EMB_THREADS * v - 1) / (EMB_THREADS * v);
         const dim3 jgrid((unsigned)(windows - 1), (unsigned)(cb < 64 ? cb : 64));
-        if (v == 4) embed_join_kernel<T, 4><<<jgrid, EMB_THREADS, 0, stream>>>(sorted, n, rows, dim, scale, accumulate, (T*)d_table, partial);
-        else embed_join_kernel<T, 1><<<jgrid, EMB_THREADS, 0, stream>>>(sorted, n, rows, dim, scale, accumulate, (T*)d_table, partial);
+        if (v == 4) embed_join_kernel<T, 4, ACCUMULATE><<<jgrid, EMB_THREADS, 0, stream>>>(sorted, n, rows, dim, scale, (T*)d_table, partial);
+        else embed_join_kernel<T, 1, ACCUMULATE><<<jgrid, EMB_THREADS, 0, stream>>>(sorted, n, rows, dim, scale, (T*)d_table, partial);
     }
 }
 
@@ -616,9 +628,8 @@ extern "C" int apollo_embedding_grad(const void* d_out, int64_t out_stride, cons
         embed_sort_kernel<int><<<grid, SORT_THREADS, 0, stream>>>((const int*)d_index, a, (uint4*)z, vecs, tail_at, tail);
     const uint2* sorted = a.buf[(a.passes - 1) & 1];
     float* partial = reinterpret_cast<float*>(ws + l.partial);
-    if (dtype == APOLLO_DT_BF16)
-        run_embed_sum<__nv_bfloat16>(d_out, out_stride, sorted, n_tokens, (uint32_t)rows, (int)dim, scale, accumulate != 0, d_table_grad, partial, stream);
-    else
-        run_embed_sum<float>(d_out, out_stride, sorted, n_tokens, (uint32_t)rows, (int)dim, scale, accumulate != 0, d_table_grad, partial, stream);
+    const auto sum = dtype == APOLLO_DT_BF16 ? (accumulate ? run_embed_sum<__nv_bfloat16, true> : run_embed_sum<__nv_bfloat16, false>)
+                                             : (accumulate ? run_embed_sum<float, true> : run_embed_sum<float, false>);
+    sum(d_out, out_stride, sorted, n_tokens, (uint32_t)rows, (int)dim, scale, d_table_grad, partial, stream);
     return cudaGetLastError() == cudaSuccess ? APOLLO_OK : APOLLO_ERR_CUDA;
 }
