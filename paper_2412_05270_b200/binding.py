@@ -6,6 +6,7 @@ import of this module's symbols raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 from pathlib import Path
 from typing import NamedTuple
@@ -187,8 +188,15 @@ def _check(code: int, what: str):
         raise ApolloError(code, what)
 
 
+# The current stream's handle without a Stream object around it (3 us less per call), where this torch has it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _stream_ptr(stream) -> int:
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(_current_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream
 
@@ -295,9 +303,14 @@ def _rows_of(x: torch.Tensor, what: str) -> int:
     return x.stride(0)
 
 
+_here = contextlib.nullcontext()
+
+
 def _on(stream, device):
-    """What the call allocates belongs to the stream that it runs on."""
-    return torch.cuda.device(device) if stream is None else torch.cuda.stream(stream)
+    """The tensors' device; what the call allocates belongs to the stream that it runs on."""
+    if stream is not None:
+        return torch.cuda.stream(stream)
+    return _here if device.index == _current_device() else torch.cuda.device(device)
 
 
 def embedding(table, index, scale: float = 1.0, out=None, stream=None) -> torch.Tensor:

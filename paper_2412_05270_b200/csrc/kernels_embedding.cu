@@ -19,6 +19,8 @@
 #include <cmath>
 
 #include "device_utils.cuh"
+#include "host_utils.h"
+#include "tc_ptx.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -133,7 +135,7 @@ embed_kernel(const T* __restrict__ table, int64_t rows, int dim, const I* __rest
 // through distributed shared memory (base of a digit = all smaller digits anywhere + the same digit in CTAs of lower
 // rank); then it scatters.  A share of more than one tile is counted first and ranked tile by tile after the exchange;
 // one that fits a tile (SORT_CLUSTER x SORT_TILE = 32768 tokens) is read once.  Inside a tile a warp owns 32 x
-// SORT_ITEMS consecutive keys and takes them 32 at a time: __match_any_sync gives the lanes with the same digit, the
+// SORT_ITEMS consecutive keys (fewer in a share that does not fill the tile) and takes them 32 at a time: __match_any_sync gives the lanes with the same digit, the
 // warp's running count of the digit the keys before them.
 struct SortArgs {
     uint2* buf[2];          // (key, position) ping-pong
@@ -147,6 +149,7 @@ __global__ void __cluster_dims__(SORT_CLUSTER, 1, 1) __launch_bounds__(SORT_THRE
 embed_sort_kernel(const I* __restrict__ index, SortArgs a, uint4* __restrict__ zero, int64_t zero_vecs, char* __restrict__ zero_tail,
                   int zero_tail_bytes)
 {
+    ptx::grid_launch_dependents();
     if (blockIdx.x >= SORT_CLUSTER) {
         const int64_t stride = (int64_t)(gridDim.x - SORT_CLUSTER) * SORT_THREADS;
         const int64_t first = (int64_t)(blockIdx.x - SORT_CLUSTER) * SORT_THREADS + threadIdx.x;
@@ -164,6 +167,8 @@ embed_sort_kernel(const I* __restrict__ index, SortArgs a, uint4* __restrict__ z
     const int64_t share = (a.n + SORT_CLUSTER - 1) / SORT_CLUSTER;
     const int64_t begin = min((int64_t)cta * share, a.n), end = min(begin + share, a.n);
     const bool one_tile = share <= SORT_TILE;
+    // keys of a warp, in rounds of 32: a short share is spread over all warps
+    const int items = one_tile ? (int)((share + SORT_THREADS - 1) / SORT_THREADS) : SORT_ITEMS;
 
     uint2 kv[SORT_ITEMS];
     uint32_t rank[SORT_ITEMS];
@@ -175,10 +180,10 @@ embed_sort_kernel(const I* __restrict__ index, SortArgs a, uint4* __restrict__ z
         // ranks of a tile within its warp; warp_hist holds the warps' digit counts afterwards
         auto rank_tile = [&](int64_t tile) {
             for (int d = tid; d < SORT_BINS * SORT_WARPS; d += SORT_THREADS) (&warp_hist[0][0])[d] = 0;
-            const int64_t first = tile + (int64_t)warp * (32 * SORT_ITEMS) + lane;
+            const int64_t first = tile + (int64_t)warp * (32 * items) + lane;
 #pragma unroll
             for (int k = 0; k < SORT_ITEMS; ++k) {
-                const int64_t t = first + k * 32;
+                const int64_t t = k < items ? first + k * 32 : end;
                 kv[k] = t >= end ? make_uint2(0xFFFFFFFFu, 0)
                                  : (pass == 0 ? make_uint2(index_key(index, t, (int64_t)a.rows), (uint32_t)t)
                                               : __ldcg(src + t));       // other CTAs wrote it in this launch: from L2
@@ -186,6 +191,7 @@ embed_sort_kernel(const I* __restrict__ index, SortArgs a, uint4* __restrict__ z
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < SORT_ITEMS; ++k) {
+                if (k >= items) break;
                 const bool valid = first + k * 32 < end;
                 const uint32_t d = (kv[k].x >> shift) & (SORT_BINS - 1);
                 const uint32_t same = __match_any_sync(0xFFFFFFFFu, valid ? d : 0xFFFFFFFFu);
@@ -209,10 +215,10 @@ embed_sort_kernel(const I* __restrict__ index, SortArgs a, uint4* __restrict__ z
             return run;
         };
         auto scatter = [&](int64_t tile, bool add_base) {
-            const int64_t first = tile + (int64_t)warp * (32 * SORT_ITEMS) + lane;
+            const int64_t first = tile + (int64_t)warp * (32 * items) + lane;
 #pragma unroll
             for (int k = 0; k < SORT_ITEMS; ++k)
-                if (first + k * 32 < end) {
+                if (k < items && first + k * 32 < end) {
                     const uint32_t d = (kv[k].x >> shift) & (SORT_BINS - 1);
                     dst[warp_hist[warp][d] + rank[k] + (add_base ? base[d] : 0u)] = kv[k];
                 }
@@ -287,16 +293,19 @@ __device__ __forceinline__ void grad_write(T* __restrict__ d_table, int64_t row,
 // One window of sorted positions and `tpw` x V columns per thread group.  A run of equal tokens that both starts
 // and ends in the window is written to dE; the first run, when it began in an earlier window, goes to partial row
 // 2 w, and the last one, when it goes on in the next window, to partial row 2 w + 1 (a run that does both counts
-// as the first).  Bound: HBM, every row of dOut read once; eight rows' loads are issued before the first is added.
+// as the first).  (`sorted` is what the launch before wrote: no pointer here promises the compiler that it never
+// changes, or a load could move ahead of the wait for that launch.)  Bound: HBM, every row of dOut read once; eight rows' loads are issued before the first is added.
 template <typename T, bool VECTOR, bool ACCUMULATE>
-__global__ void __launch_bounds__(EMB_THREADS)
-embed_sum_kernel(const T* __restrict__ d_out, int64_t out_stride, const uint2* __restrict__ sorted, int64_t n, uint32_t rows, int dim,
+__global__ void __launch_bounds__(EMB_THREADS, ACCUMULATE ? 2 : 4)
+embed_sum_kernel(const T* __restrict__ d_out, int64_t out_stride, const uint2* sorted, int64_t n, uint32_t rows, int dim,
                  float scale, T* d_table, float* __restrict__ partial, int tpw_log2, int64_t windows)
 {
     constexpr int V = VECTOR ? Vec16<T>::N : 1;
     __shared__ uint2 entry[EMB_THREADS / 8][EMB_WINDOW];
     const int tpw = 1 << tpw_log2, groups = EMB_THREADS >> tpw_log2;
     const int g = threadIdx.x >> tpw_log2, lane = threadIdx.x & (tpw - 1);
+    ptx::grid_launch_dependents();
+    ptx::grid_wait_previous();
     for (int i = threadIdx.x; i < groups * EMB_WINDOW; i += EMB_THREADS) {
         const int64_t at = ((int64_t)blockIdx.x * groups + i / EMB_WINDOW) * EMB_WINDOW + (i & (EMB_WINDOW - 1));
         entry[i / EMB_WINDOW][i & (EMB_WINDOW - 1)] = at < n ? sorted[at] : make_uint2(rows, 0);
@@ -376,7 +385,7 @@ embed_sum_kernel(const T* __restrict__ d_out, int64_t out_stride, const uint2* _
 constexpr int JOIN_SPLIT = 256;        // windows from which on a segment is shared (8192 positions of one token)
 
 template <int V>
-__device__ __forceinline__ void add_partial(float (&acc)[V], const float* __restrict__ p)
+__device__ __forceinline__ void add_partial(float (&acc)[V], const float* p)
 {
     if constexpr (V == 4) {
         const float4 x = *reinterpret_cast<const float4*>(p);
@@ -388,11 +397,11 @@ __device__ __forceinline__ void add_partial(float (&acc)[V], const float* __rest
 
 template <typename T, int V, bool ACCUMULATE>
 __global__ void __launch_bounds__(EMB_THREADS)
-embed_join_kernel(const uint2* __restrict__ sorted, int64_t n, uint32_t rows, int dim, float scale, T* d_table,
-                  const float* __restrict__ partial)
+embed_join_kernel(const uint2* sorted, int64_t n, uint32_t rows, int dim, float scale, T* d_table, const float* partial)
 {
     __shared__ float sums[EMB_THREADS / 32][32 * V];
     const int64_t w = blockIdx.x, next = (w + 1) * EMB_WINDOW;
+    ptx::grid_wait_previous();
     const uint32_t key = sorted[next - 1].x, key_next = sorted[next].x, key_first = sorted[w * EMB_WINDOW].x;
     const uint32_t key_before = w > 0 ? sorted[w * EMB_WINDOW - 1].x : key_first;
     if (key >= rows || key_next != key) return;                  // nothing goes on into the next window
@@ -487,16 +496,6 @@ int check_embed(int64_t rows, int64_t dim, int32_t dtype, int32_t index_type, in
     return APOLLO_OK;
 }
 
-int device_sms(int* sms)
-{
-    int device = 0;
-    if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) {
-        cudaGetLastError();
-        return APOLLO_ERR_CUDA;
-    }
-    return APOLLO_OK;
-}
-
 template <typename T, typename I>
 void run_embed(const void* table, int64_t rows, int dim, const void* index, int64_t n, float scale, void* out, int64_t stride, int sms, cudaStream_t stream)
 {
@@ -526,14 +525,14 @@ void run_embed_sum(const void* d_out, int64_t stride, const uint2* sorted, int64
     const int groups = EMB_THREADS >> lg;
     const int cols = (units + (1 << lg) - 1) >> lg;
     const dim3 grid((unsigned)((windows + groups - 1) / groups), (unsigned)(cols < 1024 ? cols : 1024));
-    if (vector) embed_sum_kernel<T, true, ACCUMULATE><<<grid, EMB_THREADS, 0, stream>>>((const T*)d_out, stride, sorted, n, rows, dim, scale, (T*)d_table, partial, lg, windows);
-    else embed_sum_kernel<T, false, ACCUMULATE><<<grid, EMB_THREADS, 0, stream>>>((const T*)d_out, stride, sorted, n, rows, dim, scale, (T*)d_table, partial, lg, windows);
+    launch_after(vector ? embed_sum_kernel<T, true, ACCUMULATE> : embed_sum_kernel<T, false, ACCUMULATE>, grid, dim3(EMB_THREADS), stream,
+                 (const T*)d_out, stride, sorted, n, rows, dim, scale, (T*)d_table, partial, lg, windows);
     if (windows > 1) {
         const int v = dim % 4 == 0 ? 4 : 1;
         const int cb = (dim + EMB_THREADS * v - 1) / (EMB_THREADS * v);
         const dim3 jgrid((unsigned)(windows - 1), (unsigned)(cb < 64 ? cb : 64));
-        if (v == 4) embed_join_kernel<T, 4, ACCUMULATE><<<jgrid, EMB_THREADS, 0, stream>>>(sorted, n, rows, dim, scale, (T*)d_table, partial);
-        else embed_join_kernel<T, 1, ACCUMULATE><<<jgrid, EMB_THREADS, 0, stream>>>(sorted, n, rows, dim, scale, (T*)d_table, partial);
+        launch_after(v == 4 ? embed_join_kernel<T, 4, ACCUMULATE> : embed_join_kernel<T, 1, ACCUMULATE>, jgrid, dim3(EMB_THREADS), stream,
+                     sorted, n, rows, dim, scale, (T*)d_table, partial);
     }
 }
 

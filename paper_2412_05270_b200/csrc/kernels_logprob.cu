@@ -19,6 +19,7 @@
 #include <cmath>
 
 #include "device_utils.cuh"
+#include "host_utils.h"
 
 namespace cg = cooperative_groups;
 
@@ -689,11 +690,9 @@ extern "C" int apollo_token_logprobs(const void* d_logits, int64_t row_stride, i
     if ((uintptr_t)d_logits % e || (uintptr_t)d_targets % ie || (uintptr_t)d_logprob % 4 || (uintptr_t)d_entropy % 4 || (uintptr_t)d_lse % 4 ||
         (uintptr_t)d_top_logprob % 4 || (uintptr_t)d_top_index % 4)
         return APOLLO_ERR_ALIGN;
-    int device = 0, sms = 0;
-    if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) {
-        cudaGetLastError();
-        return APOLLO_ERR_CUDA;
-    }
+    int sms = 0;
+    const int drc = device_sms(&sms);
+    if (drc != APOLLO_OK) return drc;
     LogprobArgs a;
     a.logits = d_logits; a.targets = d_targets; a.stride = row_stride; a.n_rows = n_rows; a.vocab = (int)vocab;
     a.index64 = index_type == APOLLO_INDEX_I64; a.top = top; a.scale = scale;

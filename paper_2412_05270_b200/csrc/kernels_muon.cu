@@ -18,6 +18,7 @@
 
 #include "../../include/apollo.h"
 #include "device_utils.cuh"
+#include "host_utils.h"
 #include "tc_common.cuh"
 #include "tc_ptx.cuh"
 
@@ -158,6 +159,9 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
     ptx::cluster_sync();
     ptx::tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_slot;
+    // all of the above may run while the pass before is still at work
+    ptx::grid_launch_dependents();
+    ptx::grid_wait_previous();
 
     uint32_t it = 0, stage = 0, phase = 0;
     auto next_stage = [&]() { ++it; if (++stage == (uint32_t)Cfg::STAGES) { stage = 0; phase ^= 1; } };
@@ -449,6 +453,8 @@ __device__ __forceinline__ void pair_at(const __nv_bfloat16* p, float (&v)[2])
     const uint32_t t = __ldcs(reinterpret_cast<const uint32_t*>(p));
     v[0] = __uint_as_float(t << 16); v[1] = __uint_as_float(t & 0xFFFF0000u);
 }
+__device__ __forceinline__ float one_at(const float* p) { return __ldcs(p); }
+__device__ __forceinline__ float one_at(const __nv_bfloat16* p) { return bf16_bits_to_float((uint32_t)__ldcs(reinterpret_cast<const unsigned short*>(p))); }
 template <typename T>
 __device__ __forceinline__ void load_pair(const T* p, int64_t at, int left, bool pairs, int64_t numel, float (&v)[2], int32_t* status)
 {
@@ -456,8 +462,8 @@ __device__ __forceinline__ void load_pair(const T* p, int64_t at, int left, bool
     if (left >= 2 && pairs) {
         if (APOLLO_DBG_RANGE(at, at + 1, numel, status)) pair_at(p + at, v);
     } else {
-        if (left >= 1 && APOLLO_DBG_RANGE(at, at, numel, status)) v[0] = load1(p + at);
-        if (left >= 2 && APOLLO_DBG_RANGE(at + 1, at + 1, numel, status)) v[1] = load1(p + at + 1);
+        if (left >= 1 && APOLLO_DBG_RANGE(at, at, numel, status)) v[0] = one_at(p + at);
+        if (left >= 2 && APOLLO_DBG_RANGE(at + 1, at + 1, numel, status)) v[1] = one_at(p + at + 1);
     }
 }
 __device__ __forceinline__ void store2(float* p, const float (&v)[2]) { *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]); }
@@ -484,6 +490,7 @@ __global__ void __launch_bounds__(MS_THREADS)
 muon_moment_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ status)
 {
     __shared__ double scratch[32];
+    ptx::grid_launch_dependents();
     const int k = find_item(a, blockIdx.x);
     const MuonItem& it = a.item[k];
     if ((int)blockIdx.x == a.tile_begin[k] && threadIdx.x == 0) {      // counters of the products that follow
@@ -556,7 +563,9 @@ muon_load_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ statu
     const int rows = it.rows, cols = it.cols, tiles_c = (cols + MS_COLS - 1) / MS_COLS;
     const int r0 = local / tiles_c * MS_ROWS, c0 = (local - local / tiles_c * tiles_c) * MS_COLS;
     const T* __restrict__ G = static_cast<const T*>(it.g);
-    const float* __restrict__ M = it.m;
+    const float* M = it.m;
+    ptx::grid_launch_dependents();
+    ptx::grid_wait_previous();
     const int64_t numel = (int64_t)rows * cols, extent = (int64_t)(it.tall ? cols : rows) * it.x_pitch;
     __half* __restrict__ hi = it.x[0];
     __half* __restrict__ lo = it.x[1];
@@ -654,6 +663,7 @@ muon_apply_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ stat
 {
     constexpr bool SPLIT = sizeof(T) == 4;
     __shared__ float tile[MS_ROWS][MS_COLS + 1];
+    ptx::grid_wait_previous();
     if (*reinterpret_cast<volatile int32_t*>(status) != STATUS_OK) return;      // a product gave up: leave the weights
     const int k = find_item(a, blockIdx.x);
     const MuonItem& it = a.item[k];
@@ -780,26 +790,16 @@ cudaError_t launch_muon_moment(int dtype, bool step, const MuonArgs& a, int tile
 
 cudaError_t launch_muon_load(int dtype, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream)
 {
-    if (dtype == APOLLO_DT_BF16) {
-        if (step) muon_load_kernel<__nv_bfloat16, true><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
-        else muon_load_kernel<__nv_bfloat16, false><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
-    } else {
-        if (step) muon_load_kernel<float, true><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
-        else muon_load_kernel<float, false><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
-    }
-    return cudaGetLastError();
+    const auto kernel = dtype == APOLLO_DT_BF16 ? (step ? muon_load_kernel<__nv_bfloat16, true> : muon_load_kernel<__nv_bfloat16, false>)
+                                                : (step ? muon_load_kernel<float, true> : muon_load_kernel<float, false>);
+    return launch_after(kernel, dim3((unsigned)tiles), dim3(MS_THREADS), stream, a, d_status);
 }
 
 cudaError_t launch_muon_apply(int dtype, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream)
 {
-    if (dtype == APOLLO_DT_BF16) {
-        if (step) muon_apply_kernel<__nv_bfloat16, true><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
-        else muon_apply_kernel<__nv_bfloat16, false><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
-    } else {
-        if (step) muon_apply_kernel<float, true><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
-        else muon_apply_kernel<float, false><<<tiles, MS_THREADS, 0, stream>>>(a, d_status);
-    }
-    return cudaGetLastError();
+    const auto kernel = dtype == APOLLO_DT_BF16 ? (step ? muon_apply_kernel<__nv_bfloat16, true> : muon_apply_kernel<__nv_bfloat16, false>)
+                                                : (step ? muon_apply_kernel<float, true> : muon_apply_kernel<float, false>);
+    return launch_after(kernel, dim3((unsigned)tiles), dim3(MS_THREADS), stream, a, d_status);
 }
 
 namespace {
@@ -813,9 +813,11 @@ cudaError_t launch_gemm(const GemmOp* d_ops, const uint4* d_list, int tiles, uin
     cfg.blockDim = dim3(MG_THREADS);
     cfg.dynamicSmemBytes = GemmCfg<BN>::SMEM;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     int& pairs = state.max_pairs[BN == 256 ? 0 : 1];
@@ -828,6 +830,7 @@ cudaError_t launch_gemm(const GemmOp* d_ops, const uint4* d_list, int tiles, uin
         if (clusters < 1) return cudaErrorLaunchOutOfResources;
         pairs = clusters;
     }
+    cfg.numAttrs = 2;
     cfg.gridDim = dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs)));
     return cudaLaunchKernelEx(&cfg, kernel, d_ops, d_list, (uint32_t)tiles, d_ticket, d_status);
 }
