@@ -40,14 +40,13 @@ template <int BN> struct GemmCfg {
     static_assert(SMEM <= 227 * 1024 && STAGES <= 8, "shared memory and barriers of a CTA");
 };
 
-// Bounded wait until *counter >= need, polling every `ns` nanoseconds; a set status word ends it at once.
-__device__ __forceinline__ bool wait_count(const uint32_t* counter, uint32_t need, uint32_t ns, volatile int* abort_flag,
-                                           int32_t* status, int where)
+// Bounded wait until *counter >= need; a set status word ends it at once.
+__device__ __forceinline__ bool wait_count(const uint32_t* counter, uint32_t need, volatile int* abort_flag, int32_t* status, int where)
 {
     if (need == 0 || ld_acquire_gpu(counter) >= need) return true;
     if (*abort_flag) return false;
     for (uint32_t i = 0; i < TC_WAIT_CAP; ++i) {
-        __nanosleep(ns);
+        if (i > 64) __nanosleep(64);
         if (ld_acquire_gpu(counter) >= need) return true;
         if ((i & 63u) == 63u && *reinterpret_cast<volatile int32_t*>(status) != STATUS_OK) break;
     }
@@ -188,6 +187,7 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
         const int tm = (int)(entry.y & 0xFFFFu), tn = (int)(entry.y >> 16), num_kb = (int)entry.z;
         const bool r_mn = entry.w != 0;
         const uint32_t buf = n & 1, use = n >> 1;
+        const bool soft = num_kb > 24;                   // long contraction: waits have slack, and sleeping saves power
         const bool new_op = last_op != (int)entry.x;
         last_op = (int)entry.x;
 
@@ -263,7 +263,7 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
                         ptx::fence_tensormap_acquire(op->l_map[h]);
                         ptx::fence_tensormap_acquire(op->r_map[h]);
                     }
-                    ok = wait_count(op->counter, __ldg(&op->need), 32, abort_flag, status, 206);
+                    ok = wait_count(op->counter, __ldg(&op->need), abort_flag, status, 206);
                     ptx::fence_proxy_async_global();     // other SMs' results, before loads through the async proxy
                 }
                 if (ok) ptx::mbar_arrive(bar_dep + 8 * slot);
@@ -273,9 +273,10 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
             // ---------------- count the tile ----------------
             if (lane == 0) {
                 uint32_t* counter = op->counter;
-                if (wait_phase_idle(bar_landed + 8 * (n & 3), (n >> 2) & 1, abort_flag, status, 209)) {
-                    ptx::mbar_arrive_remote(ptx::map_to_cta(bar_acc_empty + 8 * buf, 0));
+                if (soft ? wait_phase_idle(bar_landed + 8 * (n & 3), (n >> 2) & 1, abort_flag, status, 209)
+                         : wait_phase(bar_landed + 8 * (n & 3), (n >> 2) & 1, abort_flag, status, 209)) {
                     red_release_gpu_add(counter, 1u);
+                    ptx::mbar_arrive_remote(ptx::map_to_cta(bar_acc_empty + 8 * buf, 0));
                 }
             }
             __syncwarp();
@@ -308,8 +309,8 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
                 load_term(t1, e1 + at0, in);
                 if constexpr (SPLIT) load_term(t1l, e1l + at0, in);
             }
-            const bool acc_ok = ok && __all_sync(0xFFFFFFFFu, num_kb > 8 ? wait_phase_idle(bar_acc_full + 8 * buf, use & 1, abort_flag, status, 204)
-                                                                           : wait_phase(bar_acc_full + 8 * buf, use & 1, abort_flag, status, 204));
+            const bool acc_ok = ok && __all_sync(0xFFFFFFFFu, soft ? wait_phase_idle(bar_acc_full + 8 * buf, use & 1, abort_flag, status, 204)
+                                                                    : wait_phase(bar_acc_full + 8 * buf, use & 1, abort_flag, status, 204));
             ptx::tc_fence_after_sync();
             if (acc_ok && some) {
 #pragma unroll 1
