@@ -3,18 +3,23 @@
 // The iteration X <- a X + (b A + c A^2) X, A = X X^T, is a sequence of products that depend on one another; the
 // matrices of a list do not.  So a list is worked on in groups, one launch for all products of a group, whose tiles
 // are listed product by product: the first product of every matrix, the second of every matrix, and so on.
-// Two ways to take two steps, whichever has fewer tile k-blocks for the matrix:
-//   one by one   A = X X^T, B = b A + c A^2, X <- a X + B X, twice
-//   together     A, B as before; P = a I + B;  T = P A, A' = P T (= X' X'^T of the step in between, without X'),
+// Two ways to take two steps, P = a I + B:
+//   one by one   A = X X^T, B = b A + c A^2, X <- P X, twice
+//   together     A, B as before, T = P A, A' = P T (= X' X'^T of the step in between, without X'),
 //                B' = b A' + c A'^2, Q = P' P, X <- Q X
-// The second replaces two long products (m x n) by three m x m ones: it pays when n > m.  (Three steps together would
-// save more and lose too much: an error of A' is multiplied by a^2 = 12 a step.)
-// A, B, T, A', B', Q are polynomials of one symmetric matrix: symmetric, so only half their tiles are computed.
+// The second replaces two long products (m x n) by three m x m ones: taken from n = 1.5 m on, where it also has fewer
+// tile k-blocks.  (Three steps together would save more and lose too much: an error of A' is multiplied by a^2 = 12 a
+// step.)  A, B, T, A', B', Q are polynomials of one symmetric matrix: symmetric, so only half their tiles are computed.
 //
-// Rounding.  What is stored in 16 bits has 11 of them.  B is stored shifted, B + s I, with s such that its diagonal
-// lies near 0 where most singular values are near 1 (X <- (a - s) X + (B + s I) X); likewise Q - I.  The rounding of
-// the large diagonal entries was the largest error of all: measured on normal gradients (512 x 512 ... 1024 x 2736)
-// 1.4e-3 -> 1.0e-3 in X one by one, 2.2e-3 -> 1.0e-3 together.
+// Rounding.  What is stored in 16 bits has 11 of them, and how much of the identity B + s I holds matters:
+//   bfloat16 weights  s = a: the products that use P read nothing beside their operands, and nothing is added in their
+//                     epilogues.  64-bit models of this arithmetic on normal gradients (512 x 512 ... 1024 x 2736): X is
+//                     1.0e-3 ... 1.3e-3 off one by one, 1.2e-3 ... 1.4e-3 together; the rounding of the bfloat16
+//                     result is 1.65e-3.  (s such that B + s I lies near 0 where most singular values are near 1, and
+//                     (a - s) X added in fp32: 0.8e-3 ... 1.0e-3; a 60M model's 28 matrices 274 us instead of 239, a
+//                     7B layer 12.1 ms instead of 11.9.  Nearly square matrices together: 2.2e-3, hence the 1.5.)
+//   fp32 weights      the second form: the sums of the tensor cores lose more on a X + B X as one product than the
+//                     fp32 addition does (200 x 200, five steps: 6e-6 instead of 2e-6).
 #include "../../include/apollo.h"
 
 #include <algorithm>
@@ -32,7 +37,6 @@ namespace {
 
 constexpr size_t ALIGN = 256;
 constexpr int MAX_SIDE = 1 << 20;
-constexpr double Q_SHIFT = 1.0;
 constexpr int WIDE_TILES = 64;
 
 size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
@@ -52,7 +56,7 @@ struct Group {
 };
 
 // The powers of two that stored values carry, and the constants of the iteration.
-struct Scales { double x, a, b, t, q, shift; };
+struct Scales { double x, a, b, t, q, shift, q_shift; };     // B + shift I, Q - q_shift I are stored
 
 struct Plan {
     std::vector<Mat> mats;
@@ -85,14 +89,16 @@ bool find_scales(const apollo_muon_config& cfg, Scales& sc)
         t_max = std::max(t_max, std::fabs(y * p));
         p_max = std::max(p_max, std::fabs(p));
     }
-    sc.shift = -(0.7 * b_min + 0.3 * b_max);
+    const bool fold = cfg.dtype == APOLLO_DT_BF16;
+    sc.shift = fold ? a : -(0.7 * b_min + 0.3 * b_max);
+    sc.q_shift = fold ? 0.0 : 1.0;
     // the largest power of two that keeps a value of this size at or below 2^15 (16-bit floats end at 65504)
     auto scale_for = [](double v) { return std::exp2(std::floor(15.0 - std::log2(std::max(v, 1.0)))); };
     sc.x = scale_for(top);
     sc.a = scale_for(top * top);
     sc.b = scale_for(std::max(b_max - b_min, 1.0) + std::fabs(sc.shift));
     sc.t = scale_for(t_max);
-    sc.q = scale_for(p_max * p_max + Q_SHIFT);
+    sc.q = scale_for(p_max * p_max + sc.q_shift);
     return true;
 }
 
@@ -161,7 +167,7 @@ int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_confi
         m.n_part = (int)std::min<int64_t>(MUON_PART, (numel + 8191) / 8192);
         double one, two;
         costs(m.m, m.n, one, two);
-        m.together = cfg->ns_steps >= 2 && two < 2 * one;
+        m.together = cfg->ns_steps >= 2 && 2 * m.n >= 3 * m.m && two < 2 * one;
         size_t off = 0;
         for (int b = 0; b < 2; ++b)
             for (int h = 0; h < plan.parts; ++h) { m.x[b][h] = off; off = align_up(off + 2 * (size_t)m.m * m.pitch_x); }
@@ -273,8 +279,8 @@ void ops_of(const apollo_muon_ctx* ctx, int index, int bn, std::vector<GemmOp>& 
             o.r_map[h] = of_x ? x_map(r, h, r_kind) : s_map(r, h, r_kind);
             o.out_map[h] = s_map(dst, h, MAP_STORE);
             o.mir_map[h] = s_map(dst, h, MAP_MIRROR);
-            if (e1 >= 0) o.e1[h] = s_ptr(e1, h);
-            if (e2 >= 0) o.e2[h] = s_ptr(e2, h);
+            if (b1 != 0.0) o.e1[h] = s_ptr(e1, h);
+            if (b2 != 0.0) o.e2[h] = s_ptr(e2, h);
         }
         o.alpha = (float)alpha; o.b1 = (float)b1; o.b2 = (float)b2; o.diag = (float)diag;
         o.M = o.N = m.m; o.K = of_x ? m.n : m.m; o.e_pitch = m.pitch_s;
@@ -288,7 +294,7 @@ void ops_of(const apollo_muon_ctx* ctx, int index, int bn, std::vector<GemmOp>& 
             o.l_map[h] = s_map(s, h, MAP_ROWS);
             o.r_map[h] = x_map(src, h, MAP_COLS);
             o.out_map[h] = x_map(src ^ 1, h, MAP_STORE);
-            o.e1[h] = x_ptr(src, h);
+            if (b1 != 0.0) o.e1[h] = x_ptr(src, h);
         }
         o.alpha = (float)alpha; o.b1 = (float)b1;
         o.M = m.m; o.N = m.n; o.K = m.m; o.e_pitch = m.pitch_x;
@@ -303,8 +309,8 @@ void ops_of(const apollo_muon_ctx* ctx, int index, int bn, std::vector<GemmOp>& 
             square(1, 0, 2, sc.t / (sc.b * sc.a), 0, p * sc.t / sc.a, -1, 0, 0, false);                 // S2 = T = P A
             square(1, 2, 0, sc.a / (sc.b * sc.t), 2, p * sc.a / sc.t, -1, 0, 0, false);                 // S0 = A' = P T
             square(0, 0, 2, c * sc.b / (sc.a * sc.a), 0, b * sc.b / sc.a, -1, 0, sc.shift * sc.b, false);   // S2 = B' + s I
-            square(2, 1, 0, sc.q / (sc.b * sc.b), 2, p * sc.q / sc.b, 1, p * sc.q / sc.b, (p * p - Q_SHIFT) * sc.q, false);   // S0 = Q - I
-            update(0, x, 1.0 / sc.q, Q_SHIFT);
+            square(2, 1, 0, sc.q / (sc.b * sc.b), 2, p * sc.q / sc.b, 1, p * sc.q / sc.b, (p * p - sc.q_shift) * sc.q, false);   // S0 = Q - q I
+            update(0, x, 1.0 / sc.q, sc.q_shift);
             k += 2;
         } else {
             update(1, x, 1.0 / sc.b, p);

@@ -7,7 +7,7 @@
 // A product's tile is 256 x 256 (256 x 128 in short lists): each CTA of a pair loads its 128 rows of L and half of the
 // columns of R, 32 KB per 64-deep k-block, six stages; four MMAs of 256 x 256 x 16 consume them.  Roles of the 12 warps: 0 TMA producer,
 // 1 MMA issuer (leader CTA) and TMEM owner, 2 and 3 bookkeeping, 4-11 epilogue (a warp reads the 32 TMEM lanes it may read and one half
-// of the columns).  The epilogue adds the terms that the iteration needs beside the product, rounds to 16 bits and
+// of the columns).  The epilogue adds the terms that the iteration needs beside some products, rounds to 16 bits and
 // hands 32 x 32 pieces to TMA stores; a symmetric product's tile above the diagonal is stored a second time,
 // transposed, so that half of the symmetric products is never computed.
 // Bound: the tensor pipe (and with it the board's power).
@@ -289,7 +289,7 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
             const float alpha = __ldg(&op->alpha), b1 = __ldg(&op->b1), b2 = __ldg(&op->b2), diag = __ldg(&op->diag);
             const int64_t at0 = (int64_t)row * e_pitch + col_first;
             const __half* e1 = op->e1[0];
-            const __half* e2 = op->e2[0];
+            const __half* e2 = SPLIT ? op->e2[0] : nullptr;
             const __half* e1l = SPLIT ? op->e1[1] : nullptr;
             const __half* e2l = SPLIT ? op->e2[1] : nullptr;
             const bool sym = __ldg(&op->sym) != 0, mirror = sym && tn * BN >= (tm + 1) * MUON_TILE;
@@ -318,10 +318,12 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
                     const int col = col_first + ch * 32;
                     if (col >= N) break;
                     const int64_t at = at0 + ch * 32;
-                    uint4 t2[4], t2l[SPLIT ? 4 : 1];
-                    if (e2) {
-                        load_term(t2, e2 + at, in);
-                        if constexpr (SPLIT) load_term(t2l, e2l + at, in);
+                    uint4 t2[SPLIT ? 4 : 1], t2l[SPLIT ? 4 : 1];
+                    if constexpr (SPLIT) {
+                        if (e2) {
+                            load_term(t2, e2 + at, in);
+                            load_term(t2l, e2l + at, in);
+                        }
                     }
                     float v[32];
                     ptx::tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + buf * BN + (uint32_t)(half * (BN / 2) + ch * 32), v);
@@ -335,9 +337,11 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
                             if constexpr (SPLIT) load_term(t1l, e1l + at + 32, in);
                         }
                     }
-                    if (e2) {
-                        add_term(v, b2, t2);
-                        if constexpr (SPLIT) add_term(v, b2, t2l);
+                    if constexpr (SPLIT) {
+                        if (e2) {
+                            add_term(v, b2, t2);
+                            add_term(v, b2, t2l);
+                        }
                     }
                     if (diag != 0.0f && row >= col && row < col + 32) {
 #pragma unroll

@@ -20,7 +20,7 @@ struct GemmOp {
     const void* out_map[2];
     const void* mir_map[2];             // sym
     const __half* e1[2];                // same place and pitch as the output; null = none
-    const __half* e2[2];
+    const __half* e2[2];                // (split operands only)
     float alpha, b1, b2, diag;
     int32_t M, N, K, e_pitch, sym, r_mn;
     uint32_t* counter;                  // DEVICE: CTAs done with tiles of this matrix, over all its products
