@@ -419,7 +419,7 @@ int run(apollo_muon_ctx* ctx, void* const* d_W, const void* const* d_G, float* c
                     it.rows = m.rows; it.cols = m.cols; it.x_pitch = m.pitch_x; it.n_part = m.n_part; it.tall = m.tall;
                     it.gain = (float)gain_of(ctx->cfg, m);
                     a.tile_begin[k] = (int)tiles;
-                    tiles += which == 0 ? m.n_part : muon_stream_tiles(m.rows, m.cols);
+                    tiles += which == 0 ? m.n_part : muon_stream_tiles(m.rows, m.cols, m.tall != 0, which == 2);
                 }
                 for (int k = a.n; k <= MUON_CHUNK; ++k) a.tile_begin[k] = (int)tiles;
                 if (tiles > INT32_MAX) { err = cudaErrorInvalidValue; return; }

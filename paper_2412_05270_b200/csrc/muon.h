@@ -60,8 +60,10 @@ struct MuonLaunch {                     // what the launches of a context need t
 cudaError_t launch_muon_moment(int dtype, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream);
 cudaError_t launch_muon_load(int dtype, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream);
 cudaError_t launch_muon_apply(int dtype, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream);
-// Tiles of one matrix in the load and apply kernels.
-int muon_stream_tiles(int rows, int cols);
+// Tiles of one matrix in the load and apply kernels, and whether they go by vectors of eight (rows of the matrix and of
+// the iterate are whole vectors, and nothing is transposed).
+__host__ __device__ inline bool muon_stream_vectors(int cols, bool tall) { return !tall && cols % 8 == 0; }
+int muon_stream_tiles(int rows, int cols, bool tall, bool apply);
 
 // All products of a group: d_list holds per tile {op, tm | tn << 16, k-blocks of its contraction, R along n} (DEVICE);
 // d_ticket: DEVICE, zero.
