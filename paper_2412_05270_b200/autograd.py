@@ -1,0 +1,49 @@
+"""The two ends of a language model as autograd functions: token embedding and token log probabilities.
+
+Both call the library's kernels in either direction (no PyTorch arithmetic in between); see `binding` for the shapes
+and types they take."""
+from __future__ import annotations
+
+import torch
+
+from . import binding as B
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, index, scale):
+        ctx.save_for_backward(index)
+        ctx.rows, ctx.scale = table.shape[0], scale
+        return B.embedding(table, index, scale)
+
+    @staticmethod
+    def backward(ctx, d_out):
+        index, = ctx.saved_tensors
+        return B.embedding_grad(d_out.reshape(index.numel(), -1), index, ctx.rows, scale=ctx.scale), None, None
+
+
+class _TokenLogprobs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, targets, scale):
+        r = B.token_logprobs(logits, targets, scale=scale)
+        ctx.save_for_backward(logits, targets, r.lse, r.entropy)
+        ctx.scale = scale
+        return r.logprob, r.entropy
+
+    @staticmethod
+    def backward(ctx, d_logprob, d_entropy):
+        logits, targets, lse, entropy = ctx.saved_tensors
+        if d_logprob is None:
+            d_logprob = torch.zeros_like(lse)
+        return B.token_logprobs_grad(logits, targets, lse, entropy, d_logprob.contiguous(),
+                                     None if d_entropy is None else d_entropy.contiguous(), scale=ctx.scale), None, None
+
+
+def embedding(table: torch.Tensor, index: torch.Tensor, scale: float = 1.0) -> torch.Tensor:
+    """scale * table[index] with the gradient for the table (a zero row and no gradient for indices outside it)."""
+    return _Embedding.apply(table, index, float(scale))
+
+
+def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, scale: float = 1.0):
+    """(log probability of the target, entropy) per row of `logits`, with the gradient for the logits."""
+    return _TokenLogprobs.apply(logits, targets, float(scale))
