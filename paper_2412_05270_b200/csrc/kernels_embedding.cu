@@ -74,9 +74,37 @@ template <> struct Vec16<__nv_bfloat16> {
     }
 };
 
+// The 16 bytes at p, wherever p lies: cut out of two aligned loads by a funnel shift per word, unless those would leave
+// [first, last) (the row that p points into), where the elements are loaded one by one.
+template <typename T>
+__device__ __forceinline__ uint4 load16_anywhere(const T* p, const T* first, const T* last)
+{
+    const uint32_t mis = (uint32_t)((uintptr_t)p & 15u);
+    const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(p) - mis);
+    if (mis == 0) return __ldg(src);
+    if (reinterpret_cast<uintptr_t>(src) < reinterpret_cast<uintptr_t>(first) || reinterpret_cast<uintptr_t>(src + 2) > reinterpret_cast<uintptr_t>(last)) {
+        float v[Vec16<T>::N];
+#pragma unroll
+        for (int e = 0; e < Vec16<T>::N; ++e) v[e] = load1(p + e);
+        return Vec16<T>::pack(v);
+    }
+    const uint4 lo = __ldg(src), hi = __ldg(src + 1);
+    const uint32_t w[8] = { lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w };
+    const uint32_t wsel = mis >> 2, sh = (mis & 2u) * 8u;
+    uint32_t x[5];                                       // words wsel .. wsel + 4
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+        const uint32_t a = wsel & 1u ? w[i + 1] : w[i], b = wsel & 1u ? w[i + 3 < 8 ? i + 3 : 7] : w[i + 2];
+        x[i] = wsel & 2u ? b : a;
+    }
+    return make_uint4(__funnelshift_r(x[0], x[1], sh), __funnelshift_r(x[1], x[2], sh), __funnelshift_r(x[2], x[3], sh), __funnelshift_r(x[3], x[4], sh));
+}
+
 // ---------------------------------------------------------------- lookup
 // Bound: HBM, the distinct rows read once (repeats come from L2) and T x dim written.  `tpr` threads (a power of
-// two) share a row; a thread has four vectors in flight.  VECTOR: table and output rows are whole 16-byte vectors.
+// two) share a row; a thread has four vectors in flight.  VECTOR: table and output rows are whole aligned vectors.
+// Else stores are vectors wherever the output row starts, the elements around them go one by one, and table rows at
+// another offset are shifted into place (32768 x 2047 bf16: 76 us element by element, 46 us so; whole rows of 2048: 29).
 template <typename T, typename I, bool VECTOR>
 __global__ void __launch_bounds__(EMB_THREADS)
 embed_kernel(const T* __restrict__ table, int64_t rows, int dim, const I* __restrict__ index, int64_t n_tokens, float scale,
@@ -84,44 +112,40 @@ embed_kernel(const T* __restrict__ table, int64_t rows, int dim, const I* __rest
 {
     const int tpr = 1 << tpr_log2, per_block = EMB_THREADS >> tpr_log2;
     const int lane = threadIdx.x & (tpr - 1), row_in_block = threadIdx.x >> tpr_log2;
-    constexpr int V = VECTOR ? Vec16<T>::N : 1;
-    const int units = dim / V;
+    constexpr int V = Vec16<T>::N;
     for (int64_t t = (int64_t)blockIdx.x * per_block + row_in_block; t < n_tokens; t += (int64_t)gridDim.x * per_block) {
         const uint32_t key = index_key(index, t, rows);
         const bool live = key < rows;
         const T* src = table + (int64_t)key * dim;
         T* dst = out + t * out_stride;
-        for (int u0 = lane; u0 < units; u0 += 4 * tpr) {
-            if constexpr (VECTOR) {
-                uint4 raw[4];
+        const int mis = VECTOR ? 0 : (int)(((uintptr_t)dst % 16) / sizeof(T));
+        const int head = min(mis ? V - mis : 0, dim), vecs = (dim - head) / V;
+        for (int u0 = lane; u0 < vecs; u0 += 4 * tpr) {
+            uint4 raw[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int u = u0 + k * tpr;
-                    raw[k] = live && u < units ? __ldg(reinterpret_cast<const uint4*>(src) + u) : make_uint4(0, 0, 0, 0);
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int u = u0 + k * tpr;
-                    if (u >= units) break;
-                    float v[V];
-                    Vec16<T>::unpack(raw[k], v);
-#pragma unroll
-                    for (int e = 0; e < V; ++e) v[e] *= scale;
-                    __stcs(reinterpret_cast<uint4*>(dst) + u, Vec16<T>::pack(v));
-                }
-            } else {
-                float v[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int u = u0 + k * tpr;
-                    v[k] = live && u < units ? load1(src + u) : 0.0f;
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int u = u0 + k * tpr;
-                    if (u < units) emb_store1<T>(dst + u, v[k] * scale);
+            for (int k = 0; k < 4; ++k) {
+                const int u = u0 + k * tpr;
+                raw[k] = make_uint4(0, 0, 0, 0);
+                if (live && u < vecs) {
+                    if constexpr (VECTOR) raw[k] = __ldg(reinterpret_cast<const uint4*>(src) + u);
+                    else raw[k] = load16_anywhere(src + head + u * V, src, src + dim);
                 }
             }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int u = u0 + k * tpr;
+                if (u >= vecs) break;
+                float v[V];
+                Vec16<T>::unpack(raw[k], v);
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] *= scale;
+                __stcs(reinterpret_cast<uint4*>(dst + head) + u, Vec16<T>::pack(v));
+            }
+        }
+        if constexpr (!VECTOR) {
+            const int tail0 = head + vecs * V;
+            if (lane < head) emb_store1<T>(dst + lane, live ? load1(src + lane) * scale : 0.0f);
+            if (lane < dim - tail0) emb_store1<T>(dst + tail0 + lane, live ? load1(src + tail0 + lane) * scale : 0.0f);
         }
     }
 }
@@ -406,17 +430,12 @@ embed_join_kernel(const uint2* sorted, int64_t n, uint32_t rows, int dim, float 
     const uint32_t key_before = w > 0 ? sorted[w * EMB_WINDOW - 1].x : key_first;
     if (key >= rows || key_next != key) return;                  // nothing goes on into the next window
     if (w > 0 && key_first == key && key_before == key) return;  // it began earlier
-    // first position after `next` with another token
-    int64_t lo = next, hi = n;                                   // sorted[lo] == key, sorted[hi] != key (or hi == n)
-    for (int64_t step = EMB_WINDOW; lo + step < hi; step *= 2) { // most segments are short: gallop, then halve
-        if (sorted[lo + step].x != key) { hi = lo + step; break; }
-        lo += step;
+    // the windows it reaches: those that begin with it, one behind the other (every thread looks at one)
+    int64_t pieces = 1;                                          // window w holds partial row 2 w + 1, the later ones 2 x index
+    for (int found = EMB_THREADS; found == EMB_THREADS; pieces += found) {
+        const int64_t at = (w + pieces + threadIdx.x) * EMB_WINDOW;
+        found = __syncthreads_count(at < n && sorted[at].x == key);
     }
-    while (hi - lo > 1) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (sorted[mid].x == key) lo = mid; else hi = mid;
-    }
-    const int64_t pieces = (hi - 1) / EMB_WINDOW - w + 1;        // window w holds partial row 2 w + 1, the later ones 2 x index
     auto piece_at = [&](int64_t p) { return partial + (2 * (w + p) + (p == 0 ? 1 : 0)) * dim; };
     auto write = [&](int c, const float (&total)[V]) {
 #pragma unroll
@@ -501,7 +520,7 @@ void run_embed(const void* table, int64_t rows, int dim, const void* index, int6
 {
     const bool vector = (size_t)dim * sizeof(T) % 16 == 0 && (size_t)stride * sizeof(T) % 16 == 0 &&
                         (uintptr_t)table % 16 == 0 && (uintptr_t)out % 16 == 0;
-    const int units = vector ? dim / Vec16<T>::N : dim;
+    const int units = (dim + Vec16<T>::N - 1) / Vec16<T>::N;
     int lg = log2_ceil((units + 3) / 4);
     if (lg < 3) lg = 3;
     if (lg > 8) lg = 8;
