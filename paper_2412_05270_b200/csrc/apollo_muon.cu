@@ -214,13 +214,16 @@ int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_confi
         if (g.tiles > INT32_MAX / 2) return APOLLO_ERR_SHAPE;
         plan.n_tiles += g.tiles;
     }
+    if (plan.n_ops > 1 << TILE_OP_BITS) return APOLLO_ERR_SHAPE;
+    static_assert(MAX_SIDE / MUON_TILE <= 1 << TILE_M_BITS && MAX_SIDE / 128 <= 1 << TILE_N_BITS && 3 * (MAX_SIDE / 64) < 1 << TILE_K_BITS,
+                  "the fields of a tile hold the longest sides, three segments of the contraction included");
     size_t off = 0;
     plan.off_status = off; off += ALIGN;
     plan.off_counters = off; off = align_up(off + sizeof(uint32_t) * ((size_t)n_mat + 1));   // the ticket, then one per matrix
     plan.off_table = off;
     plan.off_maps = off; off = align_up(off + 128 * (size_t)plan.maps_per_mat * n_mat);
     plan.off_ops = off; off = align_up(off + sizeof(GemmOp) * (size_t)plan.n_ops);
-    plan.off_list = off; off = align_up(off + sizeof(uint4) * (size_t)plan.n_tiles);
+    plan.off_list = off; off = align_up(off + sizeof(uint64_t) * (size_t)plan.n_tiles);
     plan.table_bytes = off - plan.off_table;
     for (int i = 0; i < n_mat; ++i) {
         Mat& m = plan.mats[i];
@@ -337,7 +340,7 @@ int build_table(apollo_muon_ctx* ctx)
             }
     }
     GemmOp* d_ops = reinterpret_cast<GemmOp*>(at(plan.off_ops));
-    uint4* list = reinterpret_cast<uint4*>(at(plan.off_list));
+    uint64_t* list = reinterpret_cast<uint64_t*>(at(plan.off_list));
     int op = 0;
     for (const Group& g : plan.groups) {
         std::vector<std::vector<GemmOp>> ops(g.mats.size());
@@ -346,7 +349,7 @@ int build_table(apollo_muon_ctx* ctx)
             ops_of(ctx, g.mats[k], g.bn, ops[k]);
             products = std::max(products, ops[k].size());
         }
-        uint4* out = list + g.tile_begin;
+        uint64_t* out = list + g.tile_begin;
         for (size_t p = 0; p < products; ++p)
             for (size_t k = 0; k < g.mats.size(); ++k) {
                 if (p >= ops[k].size()) continue;
@@ -357,7 +360,7 @@ int build_table(apollo_muon_ctx* ctx)
                 // column by column: the tiles at work at one time share few columns of R and all rows of L
                 for (int tn = 0; tn < cols; ++tn)
                     for (int tm = 0; tm < (o.sym ? std::min(rows, tn / per + 1) : rows); ++tm)
-                        *out++ = make_uint4((uint32_t)op, (uint32_t)tm | (uint32_t)tn << 16, kb, (uint32_t)o.r_mn);
+                        *out++ = pack_tile((uint32_t)op, (uint32_t)tm, (uint32_t)tn, kb, (uint32_t)o.r_mn);
                 ++op;
             }
         if (out != list + g.tile_begin + g.tiles) return APOLLO_ERR_INVALID_ARG;      // the plan counted otherwise
@@ -392,7 +395,7 @@ int run(apollo_muon_ctx* ctx, void* const* d_W, const void* const* d_G, float* c
         }
     }
     const GemmOp* d_ops = reinterpret_cast<const GemmOp*>(ctx->ws + plan.off_ops);
-    const uint4* d_list = reinterpret_cast<const uint4*>(ctx->ws + plan.off_list);
+    const uint64_t* d_list = reinterpret_cast<const uint64_t*>(ctx->ws + plan.off_list);
     uint32_t* d_ticket = reinterpret_cast<uint32_t*>(ctx->ws + plan.off_counters);
     const int dtype = ctx->cfg.dtype;
     int launches = 0;

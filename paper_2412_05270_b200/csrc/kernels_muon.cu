@@ -117,7 +117,7 @@ __device__ __forceinline__ void load_term(uint4 (&e)[4], const __half* p, bool i
 // is not done.  BN: columns of a tile.
 template <bool SPLIT, int BN>
 __global__ void __launch_bounds__(MG_THREADS, 1)
-muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list, uint32_t tiles, uint32_t* __restrict__ ticket,
+muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint64_t* __restrict__ list, uint32_t tiles, uint32_t* __restrict__ ticket,
                  int32_t* __restrict__ status)
 {
     using Cfg = GemmCfg<BN>;
@@ -171,7 +171,12 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint4* __restrict__ list,
     // leader's producer: fetches entry `n` (ticket t) and hands it to both CTAs
     auto deal = [&](uint32_t n, uint32_t t) {
         const uint32_t b = n % MG_RING;
-        const uint4 e = t < tiles ? __ldg(list + t) : make_uint4(MG_END, 0, 0, 0);
+        uint4 e = make_uint4(MG_END, 0, 0, 0);
+        if (t < tiles) {
+            const uint64_t p = __ldg(list + t);
+            e = make_uint4(tile_field(p, 0, TILE_OP_BITS), tile_field(p, TILE_M_AT, TILE_M_BITS) | tile_field(p, TILE_N_AT, TILE_N_BITS) << 16,
+                           tile_field(p, TILE_K_AT, TILE_K_BITS), tile_field(p, TILE_R_AT, 1));
+        }
         for (uint32_t c = 0; c < 2; ++c)
             ptx::st_async_v4(ptx::map_to_cta(slots + 16 * b, c), e.x, e.y, e.z, e.w, ptx::map_to_cta(bar_entry + 8 * b, c));
     };
@@ -821,7 +826,7 @@ cudaError_t launch_muon_apply(int dtype, bool step, const MuonArgs& a, int tiles
 namespace {
 
 template <bool SPLIT, int BN>
-cudaError_t launch_gemm(const GemmOp* d_ops, const uint4* d_list, int tiles, uint32_t* d_ticket, MuonLaunch& state, int32_t* d_status, cudaStream_t stream)
+cudaError_t launch_gemm(const GemmOp* d_ops, const uint64_t* d_list, int tiles, uint32_t* d_ticket, MuonLaunch& state, int32_t* d_status, cudaStream_t stream)
 {
     const auto kernel = muon_gemm_kernel<SPLIT, BN>;
     cudaLaunchConfig_t cfg = {};
@@ -853,7 +858,7 @@ cudaError_t launch_gemm(const GemmOp* d_ops, const uint4* d_list, int tiles, uin
 
 }  // namespace
 
-cudaError_t launch_muon_gemm(bool split, int bn, const GemmOp* d_ops, const uint4* d_list, int tiles, uint32_t* d_ticket, MuonLaunch& state,
+cudaError_t launch_muon_gemm(bool split, int bn, const GemmOp* d_ops, const uint64_t* d_list, int tiles, uint32_t* d_ticket, MuonLaunch& state,
                              int32_t* d_status, cudaStream_t stream)
 {
     if (bn == 256) return split ? launch_gemm<true, 256>(d_ops, d_list, tiles, d_ticket, state, d_status, stream) : launch_gemm<false, 256>(d_ops, d_list, tiles, d_ticket, state, d_status, stream);

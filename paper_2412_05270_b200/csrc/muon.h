@@ -65,9 +65,19 @@ cudaError_t launch_muon_apply(int dtype, bool step, const MuonArgs& a, int tiles
 __host__ __device__ inline bool muon_stream_vectors(int cols, bool tall) { return !tall && cols % 8 == 0; }
 int muon_stream_tiles(int rows, int cols, bool tall, bool apply);
 
-// All products of a group: d_list holds per tile {op, tm | tn << 16, k-blocks of its contraction, R along n} (DEVICE);
-// d_ticket: DEVICE, zero.
-cudaError_t launch_muon_gemm(bool split, int bn, const GemmOp* d_ops, const uint4* d_list, int tiles, uint32_t* d_ticket, MuonLaunch& state,
+// A tile of the list in 64 bits (16 bytes a tile were a fortieth of a workspace cut into small groups): the product, its
+// place, the k-blocks of its contraction, R along n.
+constexpr int TILE_OP_BITS = 22, TILE_M_BITS = 12, TILE_N_BITS = 13, TILE_K_BITS = 16;
+constexpr int TILE_M_AT = TILE_OP_BITS, TILE_N_AT = TILE_M_AT + TILE_M_BITS, TILE_K_AT = TILE_N_AT + TILE_N_BITS, TILE_R_AT = TILE_K_AT + TILE_K_BITS;
+static_assert(TILE_R_AT == 63, "a tile has 64 bits");
+__host__ __device__ inline uint64_t pack_tile(uint32_t op, uint32_t tm, uint32_t tn, uint32_t kb, uint32_t r_mn)
+{
+    return (uint64_t)op | (uint64_t)tm << TILE_M_AT | (uint64_t)tn << TILE_N_AT | (uint64_t)kb << TILE_K_AT | (uint64_t)r_mn << TILE_R_AT;
+}
+__host__ __device__ inline uint32_t tile_field(uint64_t tile, int at, int bits) { return (uint32_t)(tile >> at) & ((1u << bits) - 1); }
+
+// All products of a group; d_list: its tiles (DEVICE), d_ticket: DEVICE, zero.
+cudaError_t launch_muon_gemm(bool split, int bn, const GemmOp* d_ops, const uint64_t* d_list, int tiles, uint32_t* d_ticket, MuonLaunch& state,
                              int32_t* d_status, cudaStream_t stream);
 
 // Tensor maps of a rows x cols matrix of 16-bit floats (pitch a multiple of 8), 128 bytes each at maps[kind]: boxes of
