@@ -350,9 +350,9 @@ APOLLO_API int apollo_mini_step_static(void* d_W, const void* d_G, int64_t rows,
  *
  * Precision.  The products run on the tensor cores with fp32 accumulators.  With APOLLO_DT_BF16 the iterates are
  * held in 16-bit floats with 11 significant bits, scaled by powers of two (bfloat16's 8 bits would leave an error
- * of 1e-2 in X; here it is about 1.3e-3, below the 1.65e-3 of the rounding of a bfloat16 result); with APOLLO_DT_F32
+ * of 1e-2 in X; here it is 1.0e-3 ... 1.9e-3, about the 1.65e-3 of the rounding of a bfloat16 result); with APOLLO_DT_F32
  * as unevaluated sums of two such numbers, three products for one (relative error of X, five steps of normal
- * gradients: 7e-6 at 512 x 512, 2e-5 at 2048 x 2048, 4e-5 at 2048 x 5461, from the sums of the tensor cores, which
+ * gradients: 7e-6 at 512 x 512, 2e-5 at 2048 x 2048, 5e-5 at 2048 x 5461, from the sums of the tensor cores, which
  * cut where fp32 rounds).  An ill-conditioned U, a few directions far
  * above the rest, loses more with 16-bit floats (16 directions a thousand times above the others: 4e-2, where
  * bfloat16 iterates lose 0.3).  M is fp32 in both.

@@ -3,18 +3,23 @@
 // The iteration X <- a X + (b A + c A^2) X, A = X X^T, is a sequence of products that depend on one another; the
 // matrices of a list do not.  So a list is worked on in groups, one launch for all products of a group, whose tiles
 // are listed product by product: the first product of every matrix, the second of every matrix, and so on.
-// Two ways to take two steps, P = a I + B:
-//   one by one   A = X X^T, B = b A + c A^2, X <- P X, twice
+// Two ways to take steps, P = a I + B:
+//   one by one   A = X X^T, B = b A + c A^2, X <- P X
 //   together     A, B as before, T = P A, A' = P T (= X' X'^T of the step in between, without X'),
-//                B' = b A' + c A'^2, Q = P' P, X <- Q X
-// The second replaces two long products (m x n) by three m x m ones: taken from n = 1.5 m on, where it also has fewer
-// tile k-blocks.  (Three steps together would save more and lose too much: an error of A' is multiplied by a^2 = 12 a
-// step.)  A, B, T, A', B', Q are polynomials of one symmetric matrix: symmetric, so only half their tiles are computed.
+//                B' = b A' + c A'^2, Q = P' P, X <- Q X: two steps; three: T = P' A', A'' = P' T, ..., Q <- P'' Q
+// Each further step replaces two long products (m x n) by three m x m ones: taken from n = 1.5 m on, where it also has
+// fewer tile k-blocks.  An error of A' is multiplied by a^2 = 12 a step while A is small, so three steps are taken
+// together at the start only, where all singular values are far below 1, and with two to follow; five and more go as
+// 3 + 2 + 1 + ..., fewer as 2 + 1 + ....  (Measured, bfloat16, worst of 200 x 1029, 64 x 4000, 512 x 1376 with 20 directions
+// ten times the others, five steps: 3.8e-3 one by one, 3.5e-3 as 3 + 2, 7.9e-3 as 2 + 2 + 1; six: 4.1e-3 as 3 + 2 + 1, 1.2e-2
+// as 2 + 2 + 2.)
+// A, B, T, A', B', Q are polynomials of one symmetric matrix: symmetric, so only half their tiles are computed.
+// (Five steps as 3 + 2 instead of 2 + 2 + 1: a layer of a 7B model 12.06 -> 11.23 ms, of a 1B model in fp32 4.95 -> 4.64.)
 //
 // Rounding.  What is stored in 16 bits has 11 of them, and how much of the identity B + s I holds matters:
 //   bfloat16 weights  s = a: the products that use P read nothing beside their operands, and nothing is added in their
 //                     epilogues.  64-bit models of this arithmetic on normal gradients (512 x 512 ... 1024 x 2736): X is
-//                     1.0e-3 ... 1.3e-3 off one by one, 1.2e-3 ... 1.4e-3 together; the rounding of the bfloat16
+//                     1.0e-3 ... 1.3e-3 off one by one, 1.2e-3 ... 1.9e-3 as 3 + 2; the rounding of the bfloat16
 //                     result is 1.65e-3.  (s such that B + s I lies near 0 where most singular values are near 1, and
 //                     (a - s) X added in fp32: 0.8e-3 ... 1.0e-3; a 60M model's 28 matrices 274 us instead of 239, a
 //                     7B layer 12.1 ms instead of 11.9.  Nearly square matrices together: 2.2e-3, hence the 1.5.)
@@ -45,7 +50,8 @@ int round_up(int x, int to) { return (x + to - 1) / to * to; }
 struct Mat {
     int rows, cols, m, n, tall, pitch_x, pitch_s, n_part;
     bool together;
-    size_t x[2][2], s[3][2], part;       // workspace offsets: [buffer][high, low]
+    int s_bufs;
+    size_t x[2][2], s[4][2], part;       // workspace offsets: [buffer][high, low]
     size_t maps;                         // offset of its tensor maps
 };
 
@@ -56,7 +62,7 @@ struct Group {
 };
 
 // The powers of two that stored values carry, and the constants of the iteration.
-struct Scales { double x, a, b, t, q, shift, q_shift; };     // B + shift I, Q - q_shift I are stored
+struct Scales { double x, a, b, t, q[2], shift, q_shift; };  // B + shift I, Q - q_shift I are stored; q: of two steps, of three
 
 struct Plan {
     std::vector<Mat> mats;
@@ -98,7 +104,8 @@ bool find_scales(const apollo_muon_config& cfg, Scales& sc)
     sc.a = scale_for(top * top);
     sc.b = scale_for(std::max(b_max - b_min, 1.0) + std::fabs(sc.shift));
     sc.t = scale_for(t_max);
-    sc.q = scale_for(p_max * p_max + sc.q_shift);
+    sc.q[0] = scale_for(p_max * p_max + sc.q_shift);
+    sc.q[1] = scale_for(p_max * p_max * p_max + sc.q_shift);
     return true;
 }
 
@@ -126,22 +133,36 @@ int64_t sym_tiles(int m, int bn)
     return t;
 }
 
-// Tile k-blocks of one step, and of two steps together: what a pair of CTAs works off.
-void costs(int m, int n, double& one, double& two)
+// Steps that the update at step k takes together.
+int joint(bool together, int steps, int k)
+{
+    if (!together) return 1;
+    if (steps >= 5) return k == 0 ? 3 : k == 3 ? 2 : 1;
+    return k == 0 ? std::min(2, steps) : 1;
+}
+int updates_of(bool together, int steps)
+{
+    int n = 0;
+    for (int k = 0; k < steps; k += joint(together, steps, k)) ++n;
+    return n;
+}
+
+// Products of a matrix: an update by j steps has A and X, j times B, j - 1 times T, A' and Q.
+int products_of(bool together, int steps) { return 4 * steps - updates_of(together, steps); }
+
+// Tile k-blocks of all products: what a pair of CTAs works off.
+double cost(int m, int n, bool together, int steps)
 {
     const double km = tiles_of(m, 64), kn = tiles_of(n, 64), sym = (double)sym_tiles(m, MUON_TILE);
     const double up = (double)tiles_of(m, MUON_TILE) * tiles_of(n, MUON_TILE) * km;
-    one = sym * kn + sym * km + up;
-    two = sym * kn + 5 * sym * km + up;
+    const int updates = updates_of(together, steps);
+    return updates * (sym * kn + up) + (products_of(together, steps) - 2 * updates) * sym * km;
 }
 
-// Products of a matrix: A and B, then one by one: X, or together: T, A', B', Q, X.
-int products_of(const Mat& m, int steps) { return m.together ? steps / 2 * 7 + steps % 2 * 3 : steps * 3; }
-int updates_of(const Mat& m, int steps) { return m.together ? (steps + 1) / 2 : steps; }
 int64_t all_tiles(const Mat& m, int steps, int bn)
 {
-    const int up = updates_of(m, steps);
-    return up * ((int64_t)tiles_of(m.m, MUON_TILE) * tiles_of(m.n, bn)) + (products_of(m, steps) - up) * sym_tiles(m.m, bn);
+    const int up = updates_of(m.together, steps);
+    return up * ((int64_t)tiles_of(m.m, MUON_TILE) * tiles_of(m.n, bn)) + (products_of(m.together, steps) - up) * sym_tiles(m.m, bn);
 }
 
 int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_config* cfg, Plan& plan)
@@ -150,7 +171,7 @@ int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_confi
     const int rc = validate(cfg, plan.sc);
     if (rc != APOLLO_OK) return rc;
     plan.parts = cfg->dtype == APOLLO_DT_F32 ? 2 : 1;
-    plan.maps_per_mat = (2 + 3) * MUON_MAPS * plan.parts;
+    plan.maps_per_mat = (2 + 4) * MUON_MAPS * plan.parts;
     plan.mats.resize(n_mat);
     std::vector<size_t> need(n_mat);
     for (int i = 0; i < n_mat; ++i) {
@@ -165,13 +186,12 @@ int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_confi
         m.pitch_s = round_up(m.m, 64);
         const int64_t numel = rows * cols;
         m.n_part = (int)std::min<int64_t>(MUON_PART, (numel + 8191) / 8192);
-        double one, two;
-        costs(m.m, m.n, one, two);
-        m.together = cfg->ns_steps >= 2 && 2 * m.n >= 3 * m.m && two < 2 * one;
+        m.together = 2 * m.n >= 3 * m.m && cost(m.m, m.n, true, cfg->ns_steps) < cost(m.m, m.n, false, cfg->ns_steps);
+        m.s_bufs = std::max(3, joint(m.together, cfg->ns_steps, 0) + 1);     // (one by one fills two; a workspace is no smaller for it)
         size_t off = 0;
         for (int b = 0; b < 2; ++b)
             for (int h = 0; h < plan.parts; ++h) { m.x[b][h] = off; off = align_up(off + 2 * (size_t)m.m * m.pitch_x); }
-        for (int b = 0; b < 3; ++b)
+        for (int b = 0; b < m.s_bufs; ++b)
             for (int h = 0; h < plan.parts; ++h) { m.s[b][h] = off; off = align_up(off + 2 * (size_t)m.m * m.pitch_s); }
         m.part = off; off = align_up(off + sizeof(double) * (size_t)m.n_part);
         need[i] = off;
@@ -209,7 +229,7 @@ int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_confi
         g.tiles = 0;
         for (int i : g.mats) {
             g.tiles += all_tiles(plan.mats[i], cfg->ns_steps, g.bn);
-            plan.n_ops += products_of(plan.mats[i], cfg->ns_steps);
+            plan.n_ops += products_of(plan.mats[i].together, cfg->ns_steps);
         }
         if (g.tiles > INT32_MAX / 2) return APOLLO_ERR_SHAPE;
         plan.n_tiles += g.tiles;
@@ -304,22 +324,34 @@ void ops_of(const apollo_muon_ctx* ctx, int index, int bn, std::vector<GemmOp>& 
         o.r_mn = 1;
         push(o);
     };
+    // polynomials of one matrix commute, so these products of two of them are symmetric too
+    auto poly_b = [&](int s, int dst) { square(s, s, dst, c * sc.b / (sc.a * sc.a), 0, b * sc.b / sc.a, -1, 0, sc.shift * sc.b, false); };
+    auto next_a = [&](int s, int t) {
+        square(s, 0, t, sc.t / (sc.b * sc.a), 0, p * sc.t / sc.a, -1, 0, 0, false);                     // St = T = P A
+        square(s, t, 0, sc.a / (sc.b * sc.t), t, p * sc.a / sc.t, -1, 0, 0, false);                     // S0 = A' = P T
+    };
+    // Sdst = P (r_off I + Sr / r_scale) - q I
+    auto join = [&](int s, int r, double r_scale, double r_off, int dst, double scale) {
+        square(s, r, dst, scale / (sc.b * r_scale), r, p * scale / r_scale, s, r_off * scale / sc.b, (p * r_off - sc.q_shift) * scale, false);
+    };
     int x = 0;
-    for (int k = 0; k < ctx->cfg.ns_steps;) {
+    for (int k = 0; k < ctx->cfg.ns_steps; x ^= 1) {
+        const int steps = joint(m.together, ctx->cfg.ns_steps, k);
+        k += steps;
         square(x, x, 0, sc.a / (sc.x * sc.x), -1, 0, -1, 0, 0, true);                                   // S0 = A
-        square(0, 0, 1, c * sc.b / (sc.a * sc.a), 0, b * sc.b / sc.a, -1, 0, sc.shift * sc.b, false);   // S1 = B + s I
-        if (m.together && k + 2 <= ctx->cfg.ns_steps) {
-            square(1, 0, 2, sc.t / (sc.b * sc.a), 0, p * sc.t / sc.a, -1, 0, 0, false);                 // S2 = T = P A
-            square(1, 2, 0, sc.a / (sc.b * sc.t), 2, p * sc.a / sc.t, -1, 0, 0, false);                 // S0 = A' = P T
-            square(0, 0, 2, c * sc.b / (sc.a * sc.a), 0, b * sc.b / sc.a, -1, 0, sc.shift * sc.b, false);   // S2 = B' + s I
-            square(2, 1, 0, sc.q / (sc.b * sc.b), 2, p * sc.q / sc.b, 1, p * sc.q / sc.b, (p * p - sc.q_shift) * sc.q, false);   // S0 = Q - q I
-            update(0, x, 1.0 / sc.q, sc.q_shift);
-            k += 2;
+        poly_b(0, 1);                                                                                   // S1 = B + s I
+        if (steps == 1) { update(1, x, 1.0 / sc.b, p); continue; }
+        next_a(1, 2);
+        poly_b(0, 2);                                                                                   // S2 = B' + s I
+        if (steps == 2) {
+            join(2, 1, sc.b, p, 0, sc.q[0]);
         } else {
-            update(1, x, 1.0 / sc.b, p);
-            k += 1;
+            next_a(2, 3);
+            join(2, 1, sc.b, p, 3, sc.q[0]);
+            poly_b(0, 1);                                                                               // S1 = B'' + s I
+            join(1, 3, sc.q[0], sc.q_shift, 0, sc.q[1]);
         }
-        x ^= 1;
+        update(0, x, 1.0 / sc.q[steps - 2], sc.q_shift);
     }
 }
 
@@ -332,7 +364,7 @@ int build_table(apollo_muon_ctx* ctx)
     for (size_t i = 0; i < plan.mats.size(); ++i) {
         const Mat& m = plan.mats[i];
         char* maps = at(m.maps);
-        for (int b = 0; b < 5; ++b)
+        for (int b = 0; b < 2 + m.s_bufs; ++b)
             for (int h = 0; h < plan.parts; ++h, maps += 128 * MUON_MAPS) {
                 const size_t at_ws = b < 2 ? m.x[b][h] : m.s[b - 2][h];
                 const int rc = muon_encode_maps((const __half*)(ctx->ws + at_ws), m.m, b < 2 ? m.n : m.m, b < 2 ? m.pitch_x : m.pitch_s, maps);
@@ -413,7 +445,7 @@ int run(apollo_muon_ctx* ctx, void* const* d_W, const void* const* d_G, float* c
                     const int i = g.mats[at + k];
                     const Mat& m = plan.mats[i];
                     MuonItem& it = a.item[k];
-                    const int buf = which == 2 ? updates_of(m, ctx->cfg.ns_steps) & 1 : 0;
+                    const int buf = which == 2 ? updates_of(m.together, ctx->cfg.ns_steps) & 1 : 0;
                     it.w = d_W[i]; it.g = d_G[i]; it.m = step ? d_M[i] : nullptr;
                     it.x[0] = reinterpret_cast<__half*>(ctx->ws + m.x[buf][0]);
                     it.x[1] = plan.parts == 2 ? reinterpret_cast<__half*>(ctx->ws + m.x[buf][1]) : nullptr;

@@ -89,6 +89,34 @@ def test_number_of_steps_and_coefficients(shape, steps):
         assert ((o.double() - want).norm() / want.norm()).item() <= rel, (coef, ((o.double() - want).norm() / want.norm()).item(), rel)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kind", ["normal", "columns", "few directions"])
+@pytest.mark.parametrize("steps", [3, 4, 5, 6, 7, 9])
+def test_steps_taken_together(steps, kind, dtype):
+    shapes = [(200, 1029), (600, 300), (64, 4000), (512, 1376)]
+    g = torch.Generator(device="cuda").manual_seed(5)
+    us = []
+    for s in shapes:
+        u = torch.randn(*s, generator=g, device="cuda")
+        if kind == "columns":
+            u *= torch.where(torch.rand(1, s[1], generator=g, device="cuda") < 0.01, 50.0, 1.0)
+        elif kind == "few directions":
+            u = 0.1 * u + torch.randn(s[0], 20, generator=g, device="cuda") @ torch.randn(20, s[1], generator=g, device="cuda") / math.sqrt(20)
+        us.append((u * 1e-3).to(dtype))
+    opt = B.Muon(shapes, config(dtype, steps=steps))
+    os = [torch.empty_like(u) for u in us]
+    opt.orthogonalize(us, os)
+    assert opt.status() == B.OK
+    for s, u, o in zip(shapes, us, os):
+        coef = tuple(float(torch.tensor(c)) for c in COEF) if dtype == torch.float32 else COEF
+        want, rel = allowed(u, dtype, steps, coef)
+        if dtype == torch.float32:
+            # the tensor cores cut every partial sum of 16 products to 24 bits: at most 2^-23 of a sum that grows evenly,
+            # K / 16 times, half of that on average; grown by the slope of the iteration as above
+            rel += max(s) / 32 * 2.0 ** -23 * abs(coef[0]) ** min(steps, 5) / 8
+        assert ((o.double() - want).norm() / want.norm()).item() <= rel, (s, ((o.double() - want).norm() / want.norm()).item(), rel)
+
+
 def test_result_is_nearly_orthogonal():
     # the singular values of a well conditioned matrix end in the interval that the quintic keeps: 0.67 ... 1.21
     q = torch.linalg.qr(torch.randn(600, 300, device="cuda", dtype=torch.float64))[0]
