@@ -294,13 +294,15 @@ def _index_of(x: torch.Tensor, what: str) -> int:
 
 def _rows_of(x: torch.Tensor, what: str) -> int:
     """The row stride of a 2-D CUDA tensor whose rows are contiguous."""
-    if not x.is_cuda or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+    shape = x.shape
+    if not x.is_cuda or len(shape) != 2 or (shape[1] > 1 and x.stride(1) != 1):
         raise ValueError(f"{what} must be a 2-D CUDA tensor with contiguous rows")
-    if x.shape[0] <= 1:
-        return max(x.shape[1], 1)
-    if x.stride(0) < x.shape[1]:
+    if shape[0] <= 1:
+        return max(shape[1], 1)
+    stride = x.stride(0)
+    if stride < shape[1]:
         raise ValueError(f"{what} must not have overlapping rows")
-    return x.stride(0)
+    return stride
 
 
 _here = contextlib.nullcontext()
@@ -386,11 +388,13 @@ def token_logprobs(logits, targets, scale: float = 1.0, top: int = 0, stream=Non
     if targets.numel() != n:
         raise ValueError("targets must have one entry per row of logits")
     with _on(stream, logits.device):
-        stats = torch.empty((3, n), dtype=torch.float32, device=logits.device)
+        # (empty_strided: 0.8 us less a call than empty, and for few rows the call is what takes the time)
+        device = logits.device
+        stats = torch.empty_strided((3, n), (n, 1), dtype=torch.float32, device=device)
         best = best_at = None
         if top > 0:
-            best = torch.empty((n, top), dtype=torch.float32, device=logits.device)
-            best_at = torch.empty((n, top), dtype=torch.int32, device=logits.device)
+            best = torch.empty_strided((n, top), (top, 1), dtype=torch.float32, device=device)
+            best_at = torch.empty_strided((n, top), (top, 1), dtype=torch.int32, device=device)
         base = stats.data_ptr()
         _check(load().apollo_token_logprobs(logits.data_ptr(), stride, n, vocab, dtype, targets.data_ptr(), itype, scale, top,
                                             base, base + 4 * n, base + 8 * n, None if best is None else best.data_ptr(),

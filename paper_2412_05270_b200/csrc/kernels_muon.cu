@@ -102,7 +102,8 @@ __device__ __forceinline__ void load_term(uint4 (&e)[4], const __half* p, bool i
 //                      st.async puts it into a ring of 16 slots in both CTAs, one tile ahead of its use.  Nobody has to
 //                      say that a slot is free: the producer is at most STAGES k-blocks (>= one tile each) ahead of the
 //                      MMAs, those at most two tiles ahead of the epilogue, so a slot is read long before its turn.
-//   warp 2             waits for the tile's operands and passes that on (`dep` barriers, same ring)
+//   warp 2             makes the tensor maps of the tile's product visible to this CTA, waits for the tile's operands and
+//                      passes both on (`dep` barriers, same ring)
 //   warp 3             counts the tile once the eight epilogue warps say that their stores have landed
 //
 // Symmetric results are computed in 256-row blocks from the diagonal on; a tile beyond the diagonal block is stored a
@@ -268,8 +269,10 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint64_t* __restrict__ li
                 bool ok = true;
                 if (new_op) {
                     for (int h = 0; h < (SPLIT ? 2 : 1); ++h) {
-                        ptx::fence_tensormap_acquire(op->l_map[h]);
-                        ptx::fence_tensormap_acquire(op->r_map[h]);
+                        const void* const maps[4] = { op->l_map[h], op->r_map[h], op->out_map[h], op->mir_map[h] };
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (maps[i]) ptx::fence_tensormap_acquire(maps[i]);
                     }
                     ok = wait_count(op->counter, __ldg(&op->need), abort_flag, status, 206);
                     ptx::fence_proxy_async_global();     // other SMs' results, before loads through the async proxy
@@ -304,11 +307,6 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint64_t* __restrict__ li
             const void* out_map[2] = { op->out_map[0], SPLIT ? op->out_map[1] : nullptr };
             const void* mir_map[2] = { op->mir_map[0], SPLIT ? op->mir_map[1] : nullptr };
             const uint32_t mine = staging + (uint32_t)(warp - 4) * 4096u, mine_t = mine + 2048u;
-            if (lane == 0 && new_op)
-                for (int h = 0; h < (SPLIT ? 2 : 1); ++h) {
-                    ptx::fence_tensormap_acquire(out_map[h]);
-                    if (sym) ptx::fence_tensormap_acquire(mir_map[h]);
-                }
             const bool ok = __all_sync(0xFFFFFFFFu, wait_phase(bar_dep + 8 * slot, ring_phase, abort_flag, status, 210));
             const bool some = ok && row0 < M && col_first < N, in = some && row < M;
             // the terms beside the product come from L2 (other SMs wrote them in this launch), one piece ahead
