@@ -98,10 +98,12 @@ __device__ __forceinline__ void load_term(uint4 (&e)[4], const __half* p, bool i
 // neighbours share then no longer met in L2: a 7B layer took 12.9 ms instead of 11.6 ms, at equal cycles.)
 //
 // Roles that keep latency off the loads and the epilogue:
-//   leader's producer  draws: the ticket at the start of a tile, the entry of the list a few k-blocks later, from where
-//                      st.async puts it into a ring of 16 slots in both CTAs, one tile ahead of its use.  Nobody has to
-//                      say that a slot is free: the producer is at most STAGES k-blocks (>= one tile each) ahead of the
-//                      MMAs, those at most two tiles ahead of the epilogue, so a slot is read long before its turn.
+//   the peer's warp 1  (the leader's issues the MMAs) draws: when its producer begins with a tile, the ticket of the next
+//                      one and its entry of the list, which st.async puts into a ring of 16 slots in both CTAs.  (On the
+//                      producer's thread the two round trips to L2 held up 1500 cycles of loads in every tile.)
+//                      Nobody has to say that a slot is free: the dealer is one tile ahead of the producer, that one at most
+//                      STAGES k-blocks (>= one tile each) ahead of the MMAs, those at most two tiles ahead of the
+//                      epilogue, so a slot is read long before its turn.
 //   warp 2             makes the tensor maps of the tile's product visible to this CTA, waits for the tile's operands and
 //                      passes both on (`dep` barriers, same ring)
 //   warp 3             counts the tile once the eight epilogue warps say that their stores have landed
@@ -128,7 +130,7 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint64_t* __restrict__ li
     constexpr uint32_t MISC = Cfg::STAGES * Cfg::STAGE + MG_STAGING;
     const uint32_t staging = smem_base + Cfg::STAGES * Cfg::STAGE;
     const uint32_t bars = smem_base + MISC;
-    const uint32_t bar_full = bars, bar_done = bars + 64, bar_acc_full = bars + 128, bar_acc_empty = bars + 144, bar_drain = bars + 160,
+    const uint32_t bar_full = bars, bar_done = bars + 64, bar_acc_full = bars + 128, bar_acc_empty = bars + 144, bar_drain = bars + 160, bar_go = bars + 168,
                    bar_landed = bars + 192, bar_entry = bars + 256, bar_dep = bars + 384, slots = bars + 512;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + MISC + 176);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem_gen + MISC + 180);
@@ -150,6 +152,7 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint64_t* __restrict__ li
             ptx::mbar_init(bar_dep + 8 * b, 1);          // warp 2
         }
         ptx::mbar_init(bar_drain, 1);
+        ptx::mbar_init(bar_go, 1);                       // the peer's producer
         *abort_flag = 0;
         ptx::fence_mbar_init();
     }
@@ -169,7 +172,7 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint64_t* __restrict__ li
     uint32_t it = 0, stage = 0, phase = 0;
     auto next_stage = [&]() { ++it; if (++stage == (uint32_t)Cfg::STAGES) { stage = 0; phase ^= 1; } };
 
-    // leader's producer: fetches entry `n` (ticket t) and hands it to both CTAs
+    // dealer: fetches entry `n` (ticket t) and hands it to both CTAs
     auto deal = [&](uint32_t n, uint32_t t) {
         const uint32_t b = n % MG_RING;
         uint4 e = make_uint4(MG_END, 0, 0, 0);
@@ -183,10 +186,10 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint64_t* __restrict__ li
     };
     if (tid == 0) {
         ptx::mbar_arrive_expect_tx(bar_entry, 16);
-        if (rank == 0) deal(0, atomicAdd(ticket, 1u));
+        if (rank == 1) deal(0, atomicAdd(ticket, 1u));
     }
     int last_op = -1;
-    for (uint32_t n = 0; warp != 1 || rank == 0; ++n) {  // (the peer has no MMA role)
+    for (uint32_t n = 0;; ++n) {
         // the entry {op, tm | tn << 16, k-blocks, R along n}
         const uint32_t slot = n % MG_RING, ring_phase = (n / MG_RING) & 1;
         if (!__all_sync(0xFFFFFFFFu, wait_phase(bar_entry + 8 * slot, ring_phase, abort_flag, status, 208))) break;
@@ -204,8 +207,6 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint64_t* __restrict__ li
             // ---------------- TMA producer (one thread in each CTA) ----------------
             if (lane == 0) {
                 ptx::mbar_arrive_expect_tx(bar_entry + 8 * ((n + 1) % MG_RING), 16);
-                const uint32_t drawn = rank == 0 ? atomicAdd(ticket, 1u) : 0u;
-                const int deal_at = rank == 0 ? (num_kb > 4 ? 4 : num_kb - 1) : -1;
                 const void* l_hi = op->l_map[0];
                 const void* r_hi = op->r_map[0];
                 const void* l_lo = SPLIT ? op->l_map[1] : nullptr;
@@ -215,6 +216,7 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint64_t* __restrict__ li
                 const uint32_t full0 = ptx::map_to_cta(bar_full, 0);
                 const int m0 = tm * MUON_TILE + (int)rank * 128, n0 = tn * BN + (int)rank * (BN / 2);
                 const bool ok = wait_phase(bar_dep + 8 * slot, ring_phase, abort_flag, status, 205);
+                if (ok && rank == 1) ptx::mbar_arrive(bar_go);
                 int k = 0, seg = 0;
                 for (int i = 0; ok && i < num_kb; ++i, next_stage()) {
                     const uint32_t s = stage;
@@ -232,9 +234,12 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint64_t* __restrict__ li
                     }
                     k += 64;
                     if (SPLIT && k >= seg_k) { k = 0; ++seg; }
-                    if (i == deal_at) deal(n + 1, drawn);
                 }
             }
+            __syncwarp();
+        } else if (warp == 1 && rank == 1) {
+            // ---------------- dealer ----------------
+            if (lane == 0 && wait_phase(bar_go, n & 1, abort_flag, status, 211)) deal(n + 1, atomicAdd(ticket, 1u));
             __syncwarp();
         } else if (warp == 1) {
             // ---------------- MMA issuer (leader only) ----------------
