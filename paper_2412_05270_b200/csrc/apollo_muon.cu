@@ -42,7 +42,7 @@ namespace {
 
 constexpr size_t ALIGN = 256;
 constexpr int MAX_SIDE = 1 << 20;
-constexpr int WIDE_TILES = 64;
+constexpr int64_t WIDE_FROM = 660, SMALL_UP_TO = 800;     // k-blocks, see make_plan
 
 size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
 int round_up(int x, int to) { return (x + to - 1) / to * to; }
@@ -57,7 +57,7 @@ struct Mat {
 
 struct Group {
     std::vector<int> mats;
-    int bn;                              // columns of a tile
+    int tile;                            // which of MUON_TILES
     int64_t tile_begin, tiles;           // in the list of tiles
 };
 
@@ -125,13 +125,14 @@ int validate(const apollo_muon_config* cfg, Scales& sc)
 
 int tiles_of(int x, int per) { return (x + per - 1) / per; }
 
-// Tiles of a symmetric m x m product: 256-row blocks against the columns from the block's own on.
-int64_t sym_tiles(int m, int bn)
+// Tiles of a symmetric m x m product: blocks of a tile's rows against the columns from the block's own on.
+int64_t sym_tiles(int m, const MuonTile& tile)
 {
     int64_t t = 0;
-    for (int tm = 0; tm < tiles_of(m, MUON_TILE); ++tm) t += tiles_of(m, bn) - (int64_t)tm * (MUON_TILE / bn);
+    for (int tm = 0; tm < tiles_of(m, tile.m); ++tm) t += tiles_of(m, tile.n) - (int64_t)tm * (tile.m / tile.n);
     return t;
 }
+int64_t full_tiles(int m, int n, const MuonTile& tile) { return (int64_t)tiles_of(m, tile.m) * tiles_of(n, tile.n); }
 
 // Steps that the update at step k takes together.
 int joint(bool together, int steps, int k)
@@ -153,16 +154,16 @@ int products_of(bool together, int steps) { return 4 * steps - updates_of(togeth
 // Tile k-blocks of all products: what a pair of CTAs works off.
 double cost(int m, int n, bool together, int steps)
 {
-    const double km = tiles_of(m, 64), kn = tiles_of(n, 64), sym = (double)sym_tiles(m, MUON_TILE);
-    const double up = (double)tiles_of(m, MUON_TILE) * tiles_of(n, MUON_TILE) * km;
+    const double km = tiles_of(m, 64), kn = tiles_of(n, 64), sym = (double)sym_tiles(m, MUON_TILES[TILE_WIDE]);
+    const double up = (double)full_tiles(m, n, MUON_TILES[TILE_WIDE]) * km;
     const int updates = updates_of(together, steps);
     return updates * (sym * kn + up) + (products_of(together, steps) - 2 * updates) * sym * km;
 }
 
-int64_t all_tiles(const Mat& m, int steps, int bn)
+int64_t all_tiles(const Mat& m, int steps, const MuonTile& tile)
 {
     const int up = updates_of(m.together, steps);
-    return up * ((int64_t)tiles_of(m.m, MUON_TILE) * tiles_of(m.n, bn)) + (products_of(m.together, steps) - up) * sym_tiles(m.m, bn);
+    return up * full_tiles(m.m, m.n, tile) + (products_of(m.together, steps) - up) * sym_tiles(m.m, tile);
 }
 
 int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_config* cfg, Plan& plan)
@@ -219,23 +220,30 @@ int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_confi
     }
     plan.n_ops = 0; plan.n_tiles = 0;
     for (Group& g : plan.groups) {
-        // Wide tiles (256 columns) move the fewest bytes per product; narrow ones halve the latency of a product and give
-        // twice as many tiles.  By the tiles of the smallest product: 36 (one 2048 x 2048) 401 us narrow, 413 wide;
-        // 40 (four 1024 x 1024) 201, 232; 70 (a layer of 1024) 390, 370; 84 (28 matrices of a 60M model) 286, 282.
-        int64_t sym = 0;
-        for (int i : g.mats) sym += sym_tiles(plan.mats[i].m, 256);
-        g.bn = sym >= WIDE_TILES ? 256 : 128;
+        // Wide tiles move the fewest bytes per product; the others shorten a product (its tiles are loaded and stored by
+        // more CTAs), which is what counts as long as there are few.  By the k-blocks of one m x m product of all matrices,
+        // in us, wide tiles against 256 x 128:  320 (two 1024 x 4096) 265, 251;  480 (20 of 512 x 512) 153, 141;  640 (four
+        // of 1024 x 1024) 187, 177;  672 (28 of 512 x 512) 174, 178;  800 (five of 1024) 194, 200;  1152 (one 2048) 268, 294.
+        // The same count in tiles of 128 x 128, these against 256 x 128:  80 (one 512 x 512) 94, 107;  576 (one 1024) 136,
+        // 152;  640 (eight of 512) 108, 115;  960 (twelve of 512) 123, 121;  1100 (one 1280) 188, 174;  1764 (one 1536) 291, 198.
+        int64_t wide = 0, small = 0;
+        for (int i : g.mats) {
+            const int m = plan.mats[i].m;
+            wide += sym_tiles(m, MUON_TILES[TILE_WIDE]) * tiles_of(m, 64);
+            small += sym_tiles(m, MUON_TILES[TILE_SMALL]) * tiles_of(m, 64);
+        }
+        g.tile = wide >= WIDE_FROM ? TILE_WIDE : small <= SMALL_UP_TO ? TILE_SMALL : TILE_TALL;
         g.tile_begin = plan.n_tiles;
         g.tiles = 0;
         for (int i : g.mats) {
-            g.tiles += all_tiles(plan.mats[i], cfg->ns_steps, g.bn);
+            g.tiles += all_tiles(plan.mats[i], cfg->ns_steps, MUON_TILES[g.tile]);
             plan.n_ops += products_of(plan.mats[i].together, cfg->ns_steps);
         }
         if (g.tiles > INT32_MAX / 2) return APOLLO_ERR_SHAPE;
         plan.n_tiles += g.tiles;
     }
     if (plan.n_ops > 1 << TILE_OP_BITS) return APOLLO_ERR_SHAPE;
-    static_assert(MAX_SIDE / MUON_TILE <= 1 << TILE_M_BITS && MAX_SIDE / 128 <= 1 << TILE_N_BITS && 3 * (MAX_SIDE / 64) < 1 << TILE_K_BITS,
+    static_assert(MAX_SIDE / 128 <= 1 << TILE_M_BITS && MAX_SIDE / 128 <= 1 << TILE_N_BITS && 3 * (MAX_SIDE / 64) < 1 << TILE_K_BITS,
                   "the fields of a tile hold the longest sides, three segments of the contraction included");
     size_t off = 0;
     plan.off_status = off; off += ALIGN;
@@ -272,7 +280,7 @@ struct apollo_muon_ctx {
 namespace {
 
 // The products of one matrix, in order.
-void ops_of(const apollo_muon_ctx* ctx, int index, int bn, std::vector<GemmOp>& out)
+void ops_of(const apollo_muon_ctx* ctx, int index, const MuonTile& tile, std::vector<GemmOp>& out)
 {
     const Mat& m = ctx->plan.mats[index];
     const Plan& plan = ctx->plan;
@@ -284,21 +292,21 @@ void ops_of(const apollo_muon_ctx* ctx, int index, int bn, std::vector<GemmOp>& 
     auto s_map = [&](int buf, int h, int kind) { return x_map(2 + buf, h, kind); };
     auto x_ptr = [&](int buf, int h) { return (const __half*)(ws + m.x[buf][h]); };
     auto s_ptr = [&](int buf, int h) { return (const __half*)(ws + m.s[buf][h]); };
-    // the load of R: 128 rows of a 256-column tile at once, else boxes of 64
-    const int r_kind = bn == 256 ? MAP_ROWS : MAP_COLS;
+    // the loads of L, and of R with k contiguous: a CTA's half of the tile, 128 or 64 rows
+    const int l_kind = tile.m == 256 ? MAP_ROWS : MAP_COLS, r_kind = tile.n == 256 ? MAP_ROWS : MAP_COLS;
     uint32_t* counter = reinterpret_cast<uint32_t*>(ws + plan.off_counters) + 1 + index;
     uint32_t done = 0;
     auto push = [&](GemmOp& o) {
         o.counter = counter;
         o.need = done;
-        done += MUON_COUNTS_PER_TILE * (uint32_t)(o.sym ? sym_tiles(o.M, bn) : (int64_t)tiles_of(o.M, MUON_TILE) * tiles_of(o.N, bn));
+        done += MUON_COUNTS_PER_TILE * (uint32_t)(o.sym ? sym_tiles(o.M, tile) : full_tiles(o.M, o.N, tile));
         out.push_back(o);
     };
     auto square = [&](int l, int r, int dst, double alpha, int e1, double b1, int e2, double b2, double diag, bool of_x) {
         GemmOp o;
         std::memset(&o, 0, sizeof(o));
         for (int h = 0; h < parts; ++h) {
-            o.l_map[h] = of_x ? x_map(l, h, MAP_ROWS) : s_map(l, h, MAP_ROWS);
+            o.l_map[h] = of_x ? x_map(l, h, l_kind) : s_map(l, h, l_kind);
             o.r_map[h] = of_x ? x_map(r, h, r_kind) : s_map(r, h, r_kind);
             o.out_map[h] = s_map(dst, h, MAP_STORE);
             o.mir_map[h] = s_map(dst, h, MAP_MIRROR);
@@ -314,7 +322,7 @@ void ops_of(const apollo_muon_ctx* ctx, int index, int bn, std::vector<GemmOp>& 
         GemmOp o;
         std::memset(&o, 0, sizeof(o));
         for (int h = 0; h < parts; ++h) {
-            o.l_map[h] = s_map(s, h, MAP_ROWS);
+            o.l_map[h] = s_map(s, h, l_kind);
             o.r_map[h] = x_map(src, h, MAP_COLS);
             o.out_map[h] = x_map(src ^ 1, h, MAP_STORE);
             if (b1 != 0.0) o.e1[h] = x_ptr(src, h);
@@ -378,7 +386,7 @@ int build_table(apollo_muon_ctx* ctx)
         std::vector<std::vector<GemmOp>> ops(g.mats.size());
         size_t products = 0;
         for (size_t k = 0; k < g.mats.size(); ++k) {
-            ops_of(ctx, g.mats[k], g.bn, ops[k]);
+            ops_of(ctx, g.mats[k], MUON_TILES[g.tile], ops[k]);
             products = std::max(products, ops[k].size());
         }
         uint64_t* out = list + g.tile_begin;
@@ -387,7 +395,8 @@ int build_table(apollo_muon_ctx* ctx)
                 if (p >= ops[k].size()) continue;
                 const GemmOp& o = ops[k][p];
                 d_ops[op] = o;
-                const int rows = tiles_of(o.M, MUON_TILE), cols = tiles_of(o.N, g.bn), per = MUON_TILE / g.bn;
+                const MuonTile& tile = MUON_TILES[g.tile];
+                const int rows = tiles_of(o.M, tile.m), cols = tiles_of(o.N, tile.n), per = tile.m / tile.n;
                 const uint32_t kb = (uint32_t)(plan.parts == 2 ? 3 : 1) * (uint32_t)tiles_of(o.K, 64);
                 // column by column: the tiles at work at one time share few columns of R and all rows of L
                 for (int tn = 0; tn < cols; ++tn)
@@ -467,7 +476,7 @@ int run(apollo_muon_ctx* ctx, void* const* d_W, const void* const* d_G, float* c
         pass(0);
         pass(1);
         if (err == cudaSuccess) {
-            err = launch_muon_gemm(plan.parts == 2, g.bn, d_ops, d_list + g.tile_begin, (int)g.tiles, d_ticket, ctx->launch, d_status, stream);
+            err = launch_muon_gemm(plan.parts == 2, g.tile, d_ops, d_list + g.tile_begin, (int)g.tiles, d_ticket, ctx->launch, d_status, stream);
             ++launches;
         }
         pass(2);

@@ -28,14 +28,15 @@ namespace {
 
 constexpr int MG_THREADS = 384;
 constexpr int MG_HALF = 8192;                            // 64 x 64 16-bit floats: one TMA box
-constexpr int MG_OPERAND = 2 * MG_HALF;                  // a CTA's 128 rows of L, or half of R
 constexpr int MG_EPI_WARPS = 8;
 constexpr int MG_STAGING = MG_EPI_WARPS * 4096;          // per epilogue warp: a piece of 32 x 32, and the piece transposed
 constexpr uint32_t MG_RING = 16;                         // entries of the list in flight
 constexpr uint32_t MG_END = 0xFFFFFFFFu;                 // no more entries
-template <int BN> struct GemmCfg {
-    static constexpr int STAGE = MG_OPERAND + BN * 64;   // 128 rows of L and BN / 2 of R, 64 deep
-    static constexpr int STAGES = BN == 256 ? 6 : 8;
+template <int TILE> struct GemmCfg {
+    static constexpr int BM = MUON_TILES[TILE].m, BN = MUON_TILES[TILE].n;
+    static constexpr int L_BYTES = BM / 2 * 128;         // a CTA's half of L, 64 deep
+    static constexpr int STAGE = L_BYTES + BN / 2 * 128; // and its half of R
+    static constexpr int STAGES = TILE == TILE_WIDE ? 6 : 8;
     static constexpr int SMEM = STAGES * STAGE + MG_STAGING + 768 + 1024;
     static_assert(SMEM <= 227 * 1024 && STAGES <= 8, "shared memory and barriers of a CTA");
 };
@@ -108,7 +109,7 @@ __device__ __forceinline__ void load_term(uint4 (&e)[4], const __half* p, bool i
 //                      passes both on (`dep` barriers, same ring)
 //   warp 3             counts the tile once the eight epilogue warps say that their stores have landed
 //
-// Symmetric results are computed in 256-row blocks from the diagonal on; a tile beyond the diagonal block is stored a
+// Symmetric results are computed in blocks of a tile's rows from the diagonal on; a tile beyond the diagonal block is stored a
 // second time, transposed.  (Storing it once, and reading what lies below the diagonal as the transposed tile of what
 // lies above, which the tensor cores also take, saves those stores and cost 5 % on 4096 x 4096: operands in that
 // order take 10 % more cycles per k-block.)
@@ -117,13 +118,14 @@ __device__ __forceinline__ void load_term(uint4 (&e)[4], const __half* p, bool i
 // lo hi + hi lo + hi hi (what is dropped, lo lo, is 2^-24 of a term), the small ones first: every addition to a large
 // accumulator cuts it toward zero (relative error of X after five steps, 2048 x 2048 normal gradients: 2.0e-5, with
 // hi hi first 5.0e-5).  Summing in pieces of 512, rounded to nearest in between, gave 6e-6 at 1.8 times the time, and
-// is not done.  BN: columns of a tile.
-template <bool SPLIT, int BN>
+// is not done.  TILE: which of MUON_TILES.
+template <bool SPLIT, int TILE>
 __global__ void __launch_bounds__(MG_THREADS, 1)
 muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint64_t* __restrict__ list, uint32_t tiles, uint32_t* __restrict__ ticket,
                  int32_t* __restrict__ status)
 {
-    using Cfg = GemmCfg<BN>;
+    using Cfg = GemmCfg<TILE>;
+    constexpr int BM = Cfg::BM, BN = Cfg::BN;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (ptx::smem_addr(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem_gen = smem_raw + (smem_base - ptx::smem_addr(smem_raw));
@@ -214,7 +216,7 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint64_t* __restrict__ li
                 const int seg_k = SPLIT ? num_kb / 3 * 64 : 0;
                 const uint64_t pol = ptx::policy_evict_normal();
                 const uint32_t full0 = ptx::map_to_cta(bar_full, 0);
-                const int m0 = tm * MUON_TILE + (int)rank * 128, n0 = tn * BN + (int)rank * (BN / 2);
+                const int m0 = tm * BM + (int)rank * (BM / 2), n0 = tn * BN + (int)rank * (BN / 2);
                 const bool ok = wait_phase(bar_dep + 8 * slot, ring_phase, abort_flag, status, 205);
                 if (ok && rank == 1) ptx::mbar_arrive(bar_go);
                 int k = 0, seg = 0;
@@ -227,10 +229,10 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint64_t* __restrict__ li
                     const void* rm = SPLIT && seg == 1 ? r_lo : r_hi;
                     ptx::tma_load_2d_pair(dst, lm, k, m0, full, pol);
                     if (r_mn) {
-                        ptx::tma_load_2d_pair(dst + MG_OPERAND, rm, n0, k, full, pol);
-                        if (BN == 256) ptx::tma_load_2d_pair(dst + MG_OPERAND + MG_HALF, rm, n0 + 64, k, full, pol);
+                        ptx::tma_load_2d_pair(dst + Cfg::L_BYTES, rm, n0, k, full, pol);
+                        if (BN == 256) ptx::tma_load_2d_pair(dst + Cfg::L_BYTES + MG_HALF, rm, n0 + 64, k, full, pol);
                     } else {
-                        ptx::tma_load_2d_pair(dst + MG_OPERAND, rm, k, n0, full, pol);
+                        ptx::tma_load_2d_pair(dst + Cfg::L_BYTES, rm, k, n0, full, pol);
                     }
                     k += 64;
                     if (SPLIT && k >= seg_k) { k = 0; ++seg; }
@@ -244,15 +246,15 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint64_t* __restrict__ li
         } else if (warp == 1) {
             // ---------------- MMA issuer (leader only) ----------------
             if (lane == 0) {
-                const uint32_t idesc = ptx::instr_desc_f16_pair(BN, r_mn);
+                const uint32_t idesc = ptx::instr_desc_f16_pair(BM, BN, r_mn);
                 const uint32_t d_tmem = tmem_base + buf * BN;
                 bool ok = wait_phase(bar_acc_empty + 8 * buf, (use & 1) ^ 1, abort_flag, status, 202);
                 ptx::tc_fence_after_sync();
                 // K-major operand: 64 k = 128 bytes a row, 8-row groups 1024 bytes apart, 16 k = 32 bytes on.
                 // n-contiguous R: 64 n = 128 bytes a k-row, 16 k-rows = 2048 bytes on, the next 64 n one box further.
                 const uint64_t a_desc0 = ptx::smem_desc_sw128(smem_base, 16, 1024);
-                const uint64_t b_desc0 = r_mn ? ptx::smem_desc_sw128(smem_base + MG_OPERAND, MG_HALF, 1024)
-                                              : ptx::smem_desc_sw128(smem_base + MG_OPERAND, 16, 1024);
+                const uint64_t b_desc0 = r_mn ? ptx::smem_desc_sw128(smem_base + Cfg::L_BYTES, MG_HALF, 1024)
+                                              : ptx::smem_desc_sw128(smem_base + Cfg::L_BYTES, 16, 1024);
                 const uint32_t b_step = r_mn ? 2048u >> 4 : 32u >> 4;
                 int i = 0;
                 for (; ok && i < num_kb; ++i, next_stage()) {
@@ -300,15 +302,19 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint64_t* __restrict__ li
             // ---------------- epilogue ----------------
             const int q = warp & 3, half = (warp - 4) >> 2;
             const int M = __ldg(&op->M), N = __ldg(&op->N), e_pitch = __ldg(&op->e_pitch);
-            const int row0 = tm * MUON_TILE + (int)rank * 128 + q * 32, row = row0 + lane;
-            const int col_first = tn * BN + half * (BN / 2);
+            // Accumulators: 128 rows a CTA lie one per lane; of 64 rows the lower 64 lanes hold the first half of the
+            // columns, the upper ones the second.  A warp reads its quarter of the lanes and half of the columns there.
+            constexpr int PIECES = BM == 256 ? BN / 64 : BN / 128;
+            const int row0 = tm * BM + (int)rank * (BM / 2) + (BM == 256 ? q : q & 1) * 32, row = row0 + lane;
+            const int col_first = tn * BN + (BM == 256 ? half : (q & 2) + half) * (32 * PIECES);
+            const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + buf * BN + (uint32_t)(half * 32 * PIECES);
             const float alpha = __ldg(&op->alpha), b1 = __ldg(&op->b1), b2 = __ldg(&op->b2), diag = __ldg(&op->diag);
             const int64_t at0 = (int64_t)row * e_pitch + col_first;
             const __half* e1 = op->e1[0];
             const __half* e2 = SPLIT ? op->e2[0] : nullptr;
             const __half* e1l = SPLIT ? op->e1[1] : nullptr;
             const __half* e2l = SPLIT ? op->e2[1] : nullptr;
-            const bool sym = __ldg(&op->sym) != 0, mirror = sym && tn * BN >= (tm + 1) * MUON_TILE;
+            const bool sym = __ldg(&op->sym) != 0, mirror = sym && tn * BN >= (tm + 1) * BM;
             const void* out_map[2] = { op->out_map[0], SPLIT ? op->out_map[1] : nullptr };
             const void* mir_map[2] = { op->mir_map[0], SPLIT ? op->mir_map[1] : nullptr };
             const uint32_t mine = staging + (uint32_t)(warp - 4) * 4096u, mine_t = mine + 2048u;
@@ -325,7 +331,7 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint64_t* __restrict__ li
             ptx::tc_fence_after_sync();
             if (acc_ok && some) {
 #pragma unroll 1
-                for (int ch = 0; ch < BN / 64; ++ch) {
+                for (int ch = 0; ch < PIECES; ++ch) {
                     const int col = col_first + ch * 32;
                     if (col >= N) break;
                     const int64_t at = at0 + ch * 32;
@@ -337,13 +343,13 @@ muon_gemm_kernel(const GemmOp* __restrict__ ops, const uint64_t* __restrict__ li
                         }
                     }
                     float v[32];
-                    ptx::tmem_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + buf * BN + (uint32_t)(half * (BN / 2) + ch * 32), v);
+                    ptx::tmem_ld32(acc + (uint32_t)(ch * 32), v);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] *= alpha;
                     if (e1) {
                         add_term(v, b1, t1);
                         if constexpr (SPLIT) add_term(v, b1, t1l);
-                        if (ch + 1 < BN / 64 && col + 32 < N) {
+                        if (ch + 1 < PIECES && col + 32 < N) {
                             load_term(t1, e1 + at + 32, in);
                             if constexpr (SPLIT) load_term(t1l, e1l + at + 32, in);
                         }
@@ -828,14 +834,14 @@ cudaError_t launch_muon_apply(int dtype, bool step, const MuonArgs& a, int tiles
 
 namespace {
 
-template <bool SPLIT, int BN>
+template <bool SPLIT, int TILE>
 cudaError_t launch_gemm(const GemmOp* d_ops, const uint64_t* d_list, int tiles, uint32_t* d_ticket, MuonLaunch& state, int32_t* d_status, cudaStream_t stream)
 {
-    const auto kernel = muon_gemm_kernel<SPLIT, BN>;
+    const auto kernel = muon_gemm_kernel<SPLIT, TILE>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(state.sm_count / 2 * 2));
     cfg.blockDim = dim3(MG_THREADS);
-    cfg.dynamicSmemBytes = GemmCfg<BN>::SMEM;
+    cfg.dynamicSmemBytes = GemmCfg<TILE>::SMEM;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -844,9 +850,9 @@ cudaError_t launch_gemm(const GemmOp* d_ops, const uint64_t* d_list, int tiles, 
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    int& pairs = state.max_pairs[BN == 256 ? 0 : 1];
+    int& pairs = state.max_pairs[TILE];
     if (pairs == 0) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmCfg<BN>::SMEM);
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmCfg<TILE>::SMEM);
         if (e != cudaSuccess) return e;
         int clusters = 0;
         const cudaError_t o = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg);
@@ -861,11 +867,14 @@ cudaError_t launch_gemm(const GemmOp* d_ops, const uint64_t* d_list, int tiles, 
 
 }  // namespace
 
-cudaError_t launch_muon_gemm(bool split, int bn, const GemmOp* d_ops, const uint64_t* d_list, int tiles, uint32_t* d_ticket, MuonLaunch& state,
+cudaError_t launch_muon_gemm(bool split, int tile, const GemmOp* d_ops, const uint64_t* d_list, int tiles, uint32_t* d_ticket, MuonLaunch& state,
                              int32_t* d_status, cudaStream_t stream)
 {
-    if (bn == 256) return split ? launch_gemm<true, 256>(d_ops, d_list, tiles, d_ticket, state, d_status, stream) : launch_gemm<false, 256>(d_ops, d_list, tiles, d_ticket, state, d_status, stream);
-    return split ? launch_gemm<true, 128>(d_ops, d_list, tiles, d_ticket, state, d_status, stream) : launch_gemm<false, 128>(d_ops, d_list, tiles, d_ticket, state, d_status, stream);
+    using Launch = cudaError_t (*)(const GemmOp*, const uint64_t*, int, uint32_t*, MuonLaunch&, int32_t*, cudaStream_t);
+    static constexpr Launch by_tile[MUON_TILE_KINDS][2] = { { launch_gemm<false, TILE_WIDE>, launch_gemm<true, TILE_WIDE> },
+                                                            { launch_gemm<false, TILE_TALL>, launch_gemm<true, TILE_TALL> },
+                                                            { launch_gemm<false, TILE_SMALL>, launch_gemm<true, TILE_SMALL> } };
+    return by_tile[tile][split](d_ops, d_list, tiles, d_ticket, state, d_status, stream);
 }
 
 int muon_encode_maps(const __half* base, int rows, int cols, int pitch, void* maps)

@@ -6,14 +6,17 @@
 
 namespace apollo {
 
-constexpr int MUON_TILE = 256;          // rows of a product's tile, shared by the two CTAs of a pair; it has 256 or 128 columns
+// Tiles of a product, rows x columns; the rows are shared by the two CTAs of a pair.
+struct MuonTile { int m, n; };
+constexpr MuonTile MUON_TILES[] = { { 256, 256 }, { 256, 128 }, { 128, 128 } };
+enum { TILE_WIDE, TILE_TALL, TILE_SMALL, MUON_TILE_KINDS };
 constexpr int MUON_CHUNK = 48;          // matrices whose pointers travel in one launch of a streaming kernel
 constexpr int MUON_PART = 256;          // most partial sums of squares per matrix
 
 // out = alpha L R + b1 E1 + b2 E2 + diag I on stored (scaled) values; L is M x K with k contiguous, R is K x N, with
 // k contiguous (r_mn = 0: given as the N x K matrix) or with n contiguous (r_mn = 1).  [0] / [1]: the high and low
-// parts of split operands.  sym: M = N and the result is symmetric: it is computed from the diagonal's 256 x 256 blocks
-// on, and what lies beyond them also stored transposed.
+// parts of split operands.  sym: M = N and the result is symmetric: it is computed from the diagonal's blocks of
+// MuonTile::m rows and columns on, and what lies beyond them also stored transposed.
 struct GemmOp {
     const void* l_map[2];               // DEVICE tensor maps
     const void* r_map[2];
@@ -52,7 +55,7 @@ struct MuonArgs {
 
 struct MuonLaunch {                     // what the launches of a context need to know about the device
     int sm_count;
-    int max_pairs[2];                   // resident pairs of the kernels with 256 and 128 columns a tile; 0 = not asked yet
+    int max_pairs[MUON_TILE_KINDS];     // resident pairs of the kernels by tile; 0 = not asked yet
 };
 
 // Sum of squares of U (and M <- mu M + (1 - mu) G with `step`), X = U x_scale / (|U| + eps) in 16 bits, and the end:
@@ -67,7 +70,7 @@ int muon_stream_tiles(int rows, int cols, bool tall, bool apply);
 
 // A tile of the list in 64 bits (16 bytes a tile were a fortieth of a workspace cut into small groups): the product, its
 // place, the k-blocks of its contraction, R along n.
-constexpr int TILE_OP_BITS = 22, TILE_M_BITS = 12, TILE_N_BITS = 13, TILE_K_BITS = 16;
+constexpr int TILE_OP_BITS = 21, TILE_M_BITS = 13, TILE_N_BITS = 13, TILE_K_BITS = 16;
 constexpr int TILE_M_AT = TILE_OP_BITS, TILE_N_AT = TILE_M_AT + TILE_M_BITS, TILE_K_AT = TILE_N_AT + TILE_N_BITS, TILE_R_AT = TILE_K_AT + TILE_K_BITS;
 static_assert(TILE_R_AT == 63, "a tile has 64 bits");
 __host__ __device__ inline uint64_t pack_tile(uint32_t op, uint32_t tm, uint32_t tn, uint32_t kb, uint32_t r_mn)
@@ -77,7 +80,7 @@ __host__ __device__ inline uint64_t pack_tile(uint32_t op, uint32_t tm, uint32_t
 __host__ __device__ inline uint32_t tile_field(uint64_t tile, int at, int bits) { return (uint32_t)(tile >> at) & ((1u << bits) - 1); }
 
 // All products of a group; d_list: its tiles (DEVICE), d_ticket: DEVICE, zero.
-cudaError_t launch_muon_gemm(bool split, int bn, const GemmOp* d_ops, const uint64_t* d_list, int tiles, uint32_t* d_ticket, MuonLaunch& state,
+cudaError_t launch_muon_gemm(bool split, int tile, const GemmOp* d_ops, const uint64_t* d_list, int tiles, uint32_t* d_ticket, MuonLaunch& state,
                              int32_t* d_status, cudaStream_t stream);
 
 // Tensor maps of a rows x cols matrix of 16-bit floats (pitch a multiple of 8), 128 bytes each at maps[kind]: boxes of

@@ -358,10 +358,10 @@ __device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t addr, uint32_t lbo_
     return d;
 }
 
-// The same for fp16 A and B (format 0 in both), M = 256 over a CTA pair.
-__device__ __forceinline__ uint32_t instr_desc_f16_pair(uint32_t n, bool b_mn_major)
+// The same for fp16 A and B (format 0 in both), M = 256 or 128 over a CTA pair.
+__device__ __forceinline__ uint32_t instr_desc_f16_pair(uint32_t m, uint32_t n, bool b_mn_major)
 {
-    return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((256u >> 4) << 24);
+    return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((m >> 4) << 24);
 }
 
 // Instruction descriptor for kind::f16 with bf16 A and B, fp32 D, M = 128 (256 for a CTA pair).

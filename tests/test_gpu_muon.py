@@ -117,6 +117,22 @@ def test_steps_taken_together(steps, kind, dtype):
         assert ((o.double() - want).norm() / want.norm()).item() <= rel, (s, ((o.double() - want).norm() / want.norm()).item(), rel)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("shapes", [[(512, 512)] * 3, [(1400, 1290)], [(2100, 2050), (300, 3000)]])
+def test_every_tile_shape(shapes, dtype):
+    """Little, some and much work at a time: the products go by tiles of three shapes, each with ragged edges here."""
+    opt = B.Muon(shapes, config(dtype))
+    us = [gradient(s, "rows", 40 + i, dtype) for i, s in enumerate(shapes)]
+    os = [torch.full(s, float("nan"), dtype=dtype, device="cuda") for s in shapes]
+    opt.orthogonalize(us, os)
+    assert opt.status() == B.OK
+    for s, u, o in zip(shapes, us, os):
+        want, rel = allowed(u, dtype)
+        if dtype == torch.float32:
+            rel += max(s) / 32 * 2.0 ** -23 * abs(COEF[0]) ** 5 / 8         # the tensor cores cut, as above
+        assert ((o.double() - want).norm() / want.norm()).item() <= rel, (s, ((o.double() - want).norm() / want.norm()).item(), rel)
+
+
 def test_result_is_nearly_orthogonal():
     # the singular values of a well conditioned matrix end in the interval that the quintic keeps: 0.67 ... 1.21
     q = torch.linalg.qr(torch.randn(600, 300, device="cuda", dtype=torch.float64))[0]
