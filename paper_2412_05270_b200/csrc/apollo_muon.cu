@@ -226,6 +226,8 @@ int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_confi
         // of 1024 x 1024) 187, 177;  672 (28 of 512 x 512) 174, 178;  800 (five of 1024) 194, 200;  1152 (one 2048) 268, 294.
         // The same count in tiles of 128 x 128, these against 256 x 128:  80 (one 512 x 512) 94, 107;  576 (one 1024) 136,
         // 152;  640 (eight of 512) 108, 115;  960 (twelve of 512) 123, 121;  1100 (one 1280) 188, 174;  1764 (one 1536) 291, 198.
+        // (fp32, three times the k-blocks, changes sides at the same counts: 480: 373, 361;  640: 458, 463;  1152: 732, 808;  and
+        // 576: 310, 355;  640: 225, 242;  960: 278, 260.)
         int64_t wide = 0, small = 0;
         for (int i : g.mats) {
             const int m = plan.mats[i].m;
