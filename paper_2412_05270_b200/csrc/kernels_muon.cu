@@ -4,10 +4,12 @@
 //                   accumulators in TMEM, so that the epilogue of a tile runs under the main loop of the next
 // muon_moment / muon_load / muon_apply   the streaming passes before and after
 //
-// A product's tile is 256 x 256 (256 x 128 in short lists): each CTA of a pair loads its 128 rows of L and half of the
-// columns of R, 32 KB per 64-deep k-block, six stages; four MMAs of 256 x 256 x 16 consume them.  Roles of the 12 warps: 0 TMA producer,
-// 1 MMA issuer (leader CTA) and TMEM owner, 2 and 3 bookkeeping, 4-11 epilogue (a warp reads the 32 TMEM lanes it may read and one half
-// of the columns).  The epilogue adds the terms that the iteration needs beside some products, rounds to 16 bits and
+// A product's tile is 256 x 256 (256 x 128 or 128 x 128 in short lists): each CTA of a pair loads half of the rows of L and
+// half of the columns of R, 32 KB per 64-deep k-block, six stages; four MMAs of 256 x 256 x 16 consume them.  Measured on
+// four 4096 x 4096 matrices, five steps: 1305 TFLOP/s, the tensor pipe active in 84 % of the cycles, 54 bytes a cycle and SM
+// from L2 (of 64), 1.34 GHz under the board's power cap.  Roles of the 12 warps: 0 TMA producer, 1 TMEM owner and MMA
+// issuer (leader) or dealer of tiles (peer), 2 and 3 bookkeeping, 4-11 epilogue (a warp reads the 32 TMEM lanes it may read and
+// one half of the columns).  The epilogue adds the terms that the iteration needs beside some products, rounds to 16 bits and
 // hands 32 x 32 pieces to TMA stores; a symmetric product's tile above the diagonal is stored a second time,
 // transposed, so that half of the symmetric products is never computed.
 // Bound: the tensor pipe (and with it the board's power).
