@@ -349,13 +349,14 @@ APOLLO_API int apollo_mini_step_static(void* d_W, const void* d_G, int64_t rows,
  * 0.2 sqrt(max(rows, cols)).
  *
  * Precision.  The products run on the tensor cores with fp32 accumulators.  With APOLLO_DT_BF16 the iterates are
- * held in 16-bit floats with 11 significant bits, scaled by powers of two (bfloat16's 8 bits would leave an error
- * of 1e-2 in X; here it is 1.0e-3 ... 1.9e-3, about the 1.65e-3 of the rounding of a bfloat16 result); with APOLLO_DT_F32
- * as unevaluated sums of two such numbers, three products for one (relative error of X, five steps of normal
- * gradients: 7e-6 at 512 x 512, 2e-5 at 2048 x 2048, 5e-5 at 2048 x 5461, from the sums of the tensor cores, which
- * cut where fp32 rounds).  An ill-conditioned U, a few directions far
- * above the rest, loses more with 16-bit floats (16 directions a thousand times above the others: 4e-2, where
- * bfloat16 iterates lose 0.3).  M is fp32 in both.
+ * held in 16-bit floats with 11 significant bits, scaled by powers of two: after five steps X is 0.7e-3 ... 1.5e-3 off
+ * (relative, in the 2-norm of the entries; short sides below 256: to 1.7e-3), whether the rows and columns of U are alike or
+ * differ by up to two powers of ten to either side; bfloat16's 8 bits would leave 1e-2, and the rounding of a bfloat16 result
+ * is 1.65e-3 beside it.  With APOLLO_DT_F32 they are unevaluated sums of two such numbers, three products for one (the same
+ * inputs: 4e-6 ... 9e-6 at 256 x 512, to 4e-5 at 2048 x 5461, to 9e-5 at 4096 x 11008, from the sums of the tensor cores, which
+ * cut where fp32 rounds).  An ill-conditioned U, a few directions far above the rest, loses more with 16-bit floats
+ * (20 directions ten times the others: 3e-3;  16 a thousand times: 4e-2, where bfloat16 iterates lose 0.3;  pairs: 1e-4 ... 3e-4).
+ * M is fp32 in both.
  */
 #define APOLLO_MUON_SCALE_NONE 0
 #define APOLLO_MUON_SCALE_SHAPE 1 /* sqrt(max(1, rows / cols)) */

@@ -5,24 +5,32 @@
 // are listed product by product: the first product of every matrix, the second of every matrix, and so on.
 // Two ways to take steps, P = a I + B:
 //   one by one   A = X X^T, B = b A + c A^2, X <- P X
-//   together     A, B as before, T = P A, A' = P T (= X' X'^T of the step in between, without X'),
-//                B' = b A' + c A'^2, Q = P' P, X <- Q X: two steps; three: T = P' A', A'' = P' T, ..., Q <- P'' Q
-// Each further step replaces two long products (m x n) by three m x m ones: taken from n = 1.5 m on, where it also has
-// fewer tile k-blocks.  An error of A' is multiplied by a^2 = 12 a step while A is small, so three steps are taken
-// together at the start only, where all singular values are far below 1, and with two to follow; five and more go as
-// 3 + 2 + 1 + ..., fewer as 2 + 1 + ....  (Measured, bfloat16, worst of 200 x 1029, 64 x 4000, 512 x 1376 with 20 directions
-// ten times the others, five steps: 3.8e-3 one by one, 3.5e-3 as 3 + 2, 7.9e-3 as 2 + 2 + 1; six: 4.1e-3 as 3 + 2 + 1, 1.2e-2
-// as 2 + 2 + 2.)
+//   two together A, B as before, T = P A, A' = P T (= X' X'^T of the step in between, without X'),
+//                B' = b A' + c A'^2, Q = P' P, X <- Q X
+// The second form replaces two long products (m x n) by three m x m ones: taken from n = 1.5 m on, where it also has fewer
+// tile k-blocks, from m = 256 on, and for the first two steps only.  There it costs no accuracy: what A' loses beside X' X'^T
+// is what rounding X' would have lost.  Later steps would lose more: an error of A' is absolute, while a direction that the
+// input holds little of has grown to a few hundredths by then and counts with its square (nearly square matrices have many).
+// How many there are depends on the input, not on its shape: rows or columns of different size make a wide matrix act like a
+// nearly square one.
+// (64-bit models of the code's arithmetic, bfloat16, five steps, error of X: one by one, 2 + 1 + 1 + 1, 2 + 2 + 1, 3 + 1 + 1, 3 + 2.
+//   2048 x 5461, normal                                 0.93e-3  0.87e-3  1.20e-3  0.87e-3  0.82e-3
+//   the same, columns scaled by 10^-1 ... 10            1.08e-3  1.01e-3  1.31e-3  1.08e-3  2.19e-3
+//   the same, 10^-2 ... 10^2                            1.05e-3  0.98e-3  1.47e-3  1.08e-3  3.14e-3
+//   384 x 256, normal                                   1.05e-3  1.06e-3  1.41e-3  1.55e-3  1.54e-3
+//   384 x 256, rows scaled by 10^-2 ... 10^2            1.20e-3  1.19e-3  3.62e-3  1.91e-3  3.76e-3
+//   64 x 1000, heavy tails, worst of six                1.45e-3  2.29e-3
+// the last is why m = 256: fewer directions average less.  The kernels bear the model out to 5 %; fp32 weights, 5461 x 2048,
+// rows scaled by 10^-1 ... 10: 3.2e-5 as 2 + 1 + 1 + 1, 1.1e-4 as 3 + 2.  Orthogonalising a 7B layer takes 12.0 ms, 11.1 as 3 + 1 + 1,
+// 10.2 as 3 + 2.)
 // A, B, T, A', B', Q are polynomials of one symmetric matrix: symmetric, so only half their tiles are computed.
-// (Five steps as 3 + 2 instead of 2 + 2 + 1: a layer of a 7B model 12.06 -> 11.23 ms, of a 1B model in fp32 4.95 -> 4.64.)
 //
 // Rounding.  What is stored in 16 bits has 11 of them, and how much of the identity B + s I holds matters:
 //   bfloat16 weights  s = a: the products that use P read nothing beside their operands, and nothing is added in their
 //                     epilogues.  64-bit models of this arithmetic on normal gradients (512 x 512 ... 1024 x 2736): X is
-//                     1.0e-3 ... 1.3e-3 off one by one, 1.2e-3 ... 1.9e-3 as 3 + 2; the rounding of the bfloat16
-//                     result is 1.65e-3.  (s such that B + s I lies near 0 where most singular values are near 1, and
-//                     (a - s) X added in fp32: 0.8e-3 ... 1.0e-3; a 60M model's 28 matrices 274 us instead of 239, a
-//                     7B layer 12.1 ms instead of 11.9.  Nearly square matrices together: 2.2e-3, hence the 1.5.)
+//                     1.0e-3 ... 1.3e-3 off; the rounding of the bfloat16 result is 1.65e-3.  (s such that B + s I lies near 0 where most singular values are near 1, and
+//                     (a - s) X added in fp32: 0.8e-3 ... 1.0e-3, and 15 % more time for a 60M model's 28 matrices, 2 % for
+//                     a 7B layer: not done.)
 //   fp32 weights      the second form: the sums of the tensor cores lose more on a X + B X as one product than the
 //                     fp32 addition does (200 x 200, five steps: 6e-6 instead of 2e-6).
 #include "../../include/apollo.h"
@@ -42,6 +50,8 @@ namespace {
 
 constexpr size_t ALIGN = 256;
 constexpr int MAX_SIDE = 1 << 20;
+constexpr int S_BUFS = 3;                                 // m x m matrices at a time
+constexpr int TOGETHER_FROM = 256;                        // short side
 constexpr int64_t WIDE_FROM = 660, SMALL_UP_TO = 800;     // k-blocks, see make_plan
 
 size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
@@ -49,9 +59,8 @@ int round_up(int x, int to) { return (x + to - 1) / to * to; }
 
 struct Mat {
     int rows, cols, m, n, tall, pitch_x, pitch_s, n_part;
-    bool together;
-    int s_bufs;
-    size_t x[2][2], s[4][2], part;       // workspace offsets: [buffer][high, low]
+    bool together;                       // the first two steps
+    size_t x[2][2], s[S_BUFS][2], part;  // workspace offsets: [buffer][high, low]
     size_t maps;                         // offset of its tensor maps
 };
 
@@ -62,7 +71,7 @@ struct Group {
 };
 
 // The powers of two that stored values carry, and the constants of the iteration.
-struct Scales { double x, a, b, t, q[2], shift, q_shift; };  // B + shift I, Q - q_shift I are stored; q: of two steps, of three
+struct Scales { double x, a, b, t, q, shift, q_shift; };     // B + shift I, Q - q_shift I are stored
 
 struct Plan {
     std::vector<Mat> mats;
@@ -104,8 +113,7 @@ bool find_scales(const apollo_muon_config& cfg, Scales& sc)
     sc.a = scale_for(top * top);
     sc.b = scale_for(std::max(b_max - b_min, 1.0) + std::fabs(sc.shift));
     sc.t = scale_for(t_max);
-    sc.q[0] = scale_for(p_max * p_max + sc.q_shift);
-    sc.q[1] = scale_for(p_max * p_max * p_max + sc.q_shift);
+    sc.q = scale_for(p_max * p_max + sc.q_shift);
     return true;
 }
 
@@ -134,13 +142,8 @@ int64_t sym_tiles(int m, const MuonTile& tile)
 }
 int64_t full_tiles(int m, int n, const MuonTile& tile) { return (int64_t)tiles_of(m, tile.m) * tiles_of(n, tile.n); }
 
-// Steps that the update at step k takes together.
-int joint(bool together, int steps, int k)
-{
-    if (!together) return 1;
-    if (steps >= 5) return k == 0 ? 3 : k == 3 ? 2 : 1;
-    return k == 0 ? std::min(2, steps) : 1;
-}
+// Steps that the update at step k takes.
+int joint(bool together, int steps, int k) { return together && k == 0 ? std::min(2, steps) : 1; }
 int updates_of(bool together, int steps)
 {
     int n = 0;
@@ -172,7 +175,7 @@ int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_confi
     const int rc = validate(cfg, plan.sc);
     if (rc != APOLLO_OK) return rc;
     plan.parts = cfg->dtype == APOLLO_DT_F32 ? 2 : 1;
-    plan.maps_per_mat = (2 + 4) * MUON_MAPS * plan.parts;
+    plan.maps_per_mat = (2 + S_BUFS) * MUON_MAPS * plan.parts;
     plan.mats.resize(n_mat);
     std::vector<size_t> need(n_mat);
     for (int i = 0; i < n_mat; ++i) {
@@ -187,12 +190,11 @@ int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_confi
         m.pitch_s = round_up(m.m, 64);
         const int64_t numel = rows * cols;
         m.n_part = (int)std::min<int64_t>(MUON_PART, (numel + 8191) / 8192);
-        m.together = 2 * m.n >= 3 * m.m && cost(m.m, m.n, true, cfg->ns_steps) < cost(m.m, m.n, false, cfg->ns_steps);
-        m.s_bufs = std::max(3, joint(m.together, cfg->ns_steps, 0) + 1);     // (one by one fills two; a workspace is no smaller for it)
+        m.together = m.m >= TOGETHER_FROM && 2 * m.n >= 3 * m.m && cost(m.m, m.n, true, cfg->ns_steps) < cost(m.m, m.n, false, cfg->ns_steps);
         size_t off = 0;
         for (int b = 0; b < 2; ++b)
             for (int h = 0; h < plan.parts; ++h) { m.x[b][h] = off; off = align_up(off + 2 * (size_t)m.m * m.pitch_x); }
-        for (int b = 0; b < m.s_bufs; ++b)
+        for (int b = 0; b < S_BUFS; ++b)
             for (int h = 0; h < plan.parts; ++h) { m.s[b][h] = off; off = align_up(off + 2 * (size_t)m.m * m.pitch_s); }
         m.part = off; off = align_up(off + sizeof(double) * (size_t)m.n_part);
         need[i] = off;
@@ -336,14 +338,6 @@ void ops_of(const apollo_muon_ctx* ctx, int index, const MuonTile& tile, std::ve
     };
     // polynomials of one matrix commute, so these products of two of them are symmetric too
     auto poly_b = [&](int s, int dst) { square(s, s, dst, c * sc.b / (sc.a * sc.a), 0, b * sc.b / sc.a, -1, 0, sc.shift * sc.b, false); };
-    auto next_a = [&](int s, int t) {
-        square(s, 0, t, sc.t / (sc.b * sc.a), 0, p * sc.t / sc.a, -1, 0, 0, false);                     // St = T = P A
-        square(s, t, 0, sc.a / (sc.b * sc.t), t, p * sc.a / sc.t, -1, 0, 0, false);                     // S0 = A' = P T
-    };
-    // Sdst = P (r_off I + Sr / r_scale) - q I
-    auto join = [&](int s, int r, double r_scale, double r_off, int dst, double scale) {
-        square(s, r, dst, scale / (sc.b * r_scale), r, p * scale / r_scale, s, r_off * scale / sc.b, (p * r_off - sc.q_shift) * scale, false);
-    };
     int x = 0;
     for (int k = 0; k < ctx->cfg.ns_steps; x ^= 1) {
         const int steps = joint(m.together, ctx->cfg.ns_steps, k);
@@ -351,17 +345,11 @@ void ops_of(const apollo_muon_ctx* ctx, int index, const MuonTile& tile, std::ve
         square(x, x, 0, sc.a / (sc.x * sc.x), -1, 0, -1, 0, 0, true);                                   // S0 = A
         poly_b(0, 1);                                                                                   // S1 = B + s I
         if (steps == 1) { update(1, x, 1.0 / sc.b, p); continue; }
-        next_a(1, 2);
+        square(1, 0, 2, sc.t / (sc.b * sc.a), 0, p * sc.t / sc.a, -1, 0, 0, false);                     // S2 = T = P A
+        square(1, 2, 0, sc.a / (sc.b * sc.t), 2, p * sc.a / sc.t, -1, 0, 0, false);                     // S0 = A' = P T
         poly_b(0, 2);                                                                                   // S2 = B' + s I
-        if (steps == 2) {
-            join(2, 1, sc.b, p, 0, sc.q[0]);
-        } else {
-            next_a(2, 3);
-            join(2, 1, sc.b, p, 3, sc.q[0]);
-            poly_b(0, 1);                                                                               // S1 = B'' + s I
-            join(1, 3, sc.q[0], sc.q_shift, 0, sc.q[1]);
-        }
-        update(0, x, 1.0 / sc.q[steps - 2], sc.q_shift);
+        square(2, 1, 0, sc.q / (sc.b * sc.b), 1, p * sc.q / sc.b, 2, p * sc.q / sc.b, (p * p - sc.q_shift) * sc.q, false);      // S0 = Q = P' P - q I
+        update(0, x, 1.0 / sc.q, sc.q_shift);
     }
 }
 
@@ -374,7 +362,7 @@ int build_table(apollo_muon_ctx* ctx)
     for (size_t i = 0; i < plan.mats.size(); ++i) {
         const Mat& m = plan.mats[i];
         char* maps = at(m.maps);
-        for (int b = 0; b < 2 + m.s_bufs; ++b)
+        for (int b = 0; b < 2 + S_BUFS; ++b)
             for (int h = 0; h < plan.parts; ++h, maps += 128 * MUON_MAPS) {
                 const size_t at_ws = b < 2 ? m.x[b][h] : m.s[b - 2][h];
                 const int rc = muon_encode_maps((const __half*)(ctx->ws + at_ws), m.m, b < 2 ? m.n : m.m, b < 2 ? m.pitch_x : m.pitch_s, maps);
