@@ -391,7 +391,9 @@ APOLLO_API int apollo_muon_destroy(apollo_muon_ctx* ctx);
 /*
  * One step over the list.  d_W, d_G, d_M: HOST arrays of DEVICE pointers (16-byte aligned, row-major rows x cols,
  * contiguous); W and M (fp32, zeroed by the caller before the first step) are updated in place.  Asynchronous on
- * `cuda_stream`; two calls of one context must not overlap on the GPU (they share the workspace).
+ * `cuda_stream`; two calls of one context must not overlap on the GPU (they share the workspace).  The first call of a
+ * context (this one or the next) uploads its tables and is refused (APOLLO_ERR_INVALID_ARG) while the stream is being
+ * captured; later ones can be captured, and the graph launched as long as the context and its workspace live.
  */
 APOLLO_API int apollo_muon_step(apollo_muon_ctx* ctx, void* const* d_W, const void* const* d_G, float* const* d_M,
                                 float lr, float wd, void* cuda_stream);

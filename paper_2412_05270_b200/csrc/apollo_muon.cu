@@ -419,6 +419,12 @@ int run(apollo_muon_ctx* ctx, void* const* d_W, const void* const* d_G, float* c
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     int32_t* d_status = reinterpret_cast<int32_t*>(ctx->ws + plan.off_status);
     if (ctx->first) {
+        // A capture would only record the upload: the tables would be missing until the graph is launched.
+        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+        if (cudaStreamIsCapturing(stream, &capture) != cudaSuccess || capture != cudaStreamCaptureStatusNone) {
+            cudaGetLastError();
+            return APOLLO_ERR_INVALID_ARG;
+        }
         if (cudaMemsetAsync(d_status, 0, ALIGN, stream) != cudaSuccess ||
             cudaMemcpyAsync(ctx->ws + plan.off_table, ctx->table, plan.table_bytes, cudaMemcpyHostToDevice, stream) != cudaSuccess) {
             cudaGetLastError();
