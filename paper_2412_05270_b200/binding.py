@@ -362,6 +362,8 @@ def embedding_grad(d_out, index, rows: int, scale: float = 1.0, out=None, accumu
             out = torch.empty((rows, dim), dtype=d_out.dtype, device=d_out.device)
         elif out.dtype != d_out.dtype or tuple(out.shape) != (rows, dim) or not out.is_contiguous() or not out.is_cuda:
             raise ValueError("out must be a contiguous CUDA tensor (rows, dim) of d_out's dtype")
+        if workspace is not None and (not workspace.is_cuda or not workspace.is_contiguous()):
+            raise ValueError("workspace must be a contiguous CUDA tensor")
         if workspace is None:
             workspace = torch.empty(embedding_grad_workspace_bytes(n, rows, dim), dtype=torch.uint8, device=d_out.device)
         _check(load().apollo_embedding_grad(d_out.data_ptr(), stride, index.data_ptr(), itype, n, rows, dim, dtype, scale,

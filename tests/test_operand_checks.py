@@ -1,0 +1,53 @@
+"""What the binding refuses before a pointer reaches a kernel, with stand-ins for tensors of other devices (no GPU needed)."""
+import math
+
+import pytest
+import torch
+
+from paper_2412_05270_b200 import binding as B
+
+
+class Operand:
+    """As much of a CUDA tensor as the checks look at; whoever asks for its address fails the test."""
+
+    def __init__(self, *shape, dtype=torch.float32, device="cuda:0", strides=None):
+        self.shape, self.dtype, self.device = torch.Size(shape), dtype, torch.device(device)
+        self.is_cuda = self.device.type == "cuda"
+        self.strides = strides or [math.prod(shape[i + 1:]) for i in range(len(shape))]
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return math.prod(self.shape)
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def stride(self, i):
+        return self.strides[i]
+
+    def is_contiguous(self):
+        return self.strides == [math.prod(self.shape[i + 1:]) for i in range(len(self.shape))]
+
+    def contiguous(self):
+        return self
+
+    def data_ptr(self):
+        raise AssertionError("an address was taken before the checks were over")
+
+
+@pytest.fixture(autouse=True)
+def _device_zero(monkeypatch):
+    monkeypatch.setattr(B, "_current_device", lambda: 0)
+    monkeypatch.setattr(B, "_raw_stream", lambda device: 0)
+
+
+def index(n, **kw):
+    return Operand(n, dtype=torch.int64, **kw)
+
+
+@pytest.mark.parametrize("workspace", [Operand(4096, dtype=torch.uint8, device="cpu"), Operand(4096, dtype=torch.uint8, strides=[2])])
+def test_a_workspace_that_kernels_cannot_use(workspace):
+    with pytest.raises(ValueError, match="workspace"):
+        B.embedding_grad(Operand(4, 8), index(4), 10, out=Operand(10, 8), workspace=workspace)
