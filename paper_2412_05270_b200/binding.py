@@ -305,12 +305,20 @@ def _rows_of(x: torch.Tensor, what: str) -> int:
     return stride
 
 
+def _one_device(device, *operands):
+    for x in operands:
+        if x is not None and x.device != device:
+            raise ValueError(f"the tensors of a call must be on one device, got {device} and {x.device}")
+
+
 _here = contextlib.nullcontext()
 
 
 def _on(stream, device):
     """The tensors' device; what the call allocates belongs to the stream that it runs on."""
     if stream is not None:
+        if stream.device != device:
+            raise ValueError(f"a stream of {stream.device} cannot work on tensors of {device}")
         return torch.cuda.stream(stream)
     return _here if device.index == _current_device() else torch.cuda.device(device)
 
@@ -323,6 +331,7 @@ def embedding(table, index, scale: float = 1.0, out=None, stream=None) -> torch.
     dtype, itype = _dtype_of(table, "table"), _index_of(index, "index")
     if table.dim() != 2 or not table.is_contiguous() or not table.is_cuda:
         raise ValueError("table must be a 2-D contiguous CUDA tensor")
+    _one_device(table.device, index, out)
     rows, dim = table.shape
     n = index.numel()
     with _on(stream, table.device):
@@ -355,6 +364,9 @@ def embedding_grad(d_out, index, rows: int, scale: float = 1.0, out=None, accumu
     n, dim = d_out.shape
     if n != index.numel():
         raise ValueError("d_out must have one row per index")
+    if workspace is not None and (not workspace.is_cuda or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous CUDA tensor")
+    _one_device(d_out.device, index, out, workspace)
     with _on(stream, d_out.device):
         if out is None:
             if accumulate:
@@ -362,8 +374,6 @@ def embedding_grad(d_out, index, rows: int, scale: float = 1.0, out=None, accumu
             out = torch.empty((rows, dim), dtype=d_out.dtype, device=d_out.device)
         elif out.dtype != d_out.dtype or tuple(out.shape) != (rows, dim) or not out.is_contiguous() or not out.is_cuda:
             raise ValueError("out must be a contiguous CUDA tensor (rows, dim) of d_out's dtype")
-        if workspace is not None and (not workspace.is_cuda or not workspace.is_contiguous()):
-            raise ValueError("workspace must be a contiguous CUDA tensor")
         if workspace is None:
             workspace = torch.empty(embedding_grad_workspace_bytes(n, rows, dim), dtype=torch.uint8, device=d_out.device)
         _check(load().apollo_embedding_grad(d_out.data_ptr(), stride, index.data_ptr(), itype, n, rows, dim, dtype, scale,
@@ -389,6 +399,7 @@ def token_logprobs(logits, targets, scale: float = 1.0, top: int = 0, stream=Non
     n, vocab = logits.shape
     if targets.numel() != n:
         raise ValueError("targets must have one entry per row of logits")
+    _one_device(logits.device, targets)
     with _on(stream, logits.device):
         # (empty_strided: 0.8 us less a call than empty, and for few rows the call is what takes the time)
         device = logits.device
@@ -418,6 +429,7 @@ def token_logprobs_grad(logits, targets, lse, entropy, d_logprob, d_entropy=None
             raise ValueError(f"{what} must be a contiguous float32 CUDA tensor with one entry per row")
     if targets.numel() != n:
         raise ValueError("targets must have one entry per row of logits")
+    _one_device(logits.device, targets, lse, entropy, d_logprob, d_entropy, out)
     with _on(stream, logits.device):
         if out is None:
             out = torch.empty((n, vocab), dtype=logits.dtype, device=logits.device)

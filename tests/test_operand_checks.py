@@ -51,3 +51,45 @@ def index(n, **kw):
 def test_a_workspace_that_kernels_cannot_use(workspace):
     with pytest.raises(ValueError, match="workspace"):
         B.embedding_grad(Operand(4, 8), index(4), 10, out=Operand(10, 8), workspace=workspace)
+
+
+class Stream:
+    def __init__(self, device):
+        self.device, self.cuda_stream = torch.device(device), 0
+
+
+ELSEWHERE = dict(device="cuda:1")
+
+
+def rows(n, **kw):
+    return Operand(n, **kw)
+
+
+@pytest.mark.parametrize("call", [
+    lambda: B.embedding(Operand(10, 8), index(4, **ELSEWHERE)),
+    lambda: B.embedding(Operand(10, 8), index(4), out=Operand(4, 8, **ELSEWHERE)),
+    lambda: B.embedding_grad(Operand(4, 8), index(4, **ELSEWHERE), 10),
+    lambda: B.embedding_grad(Operand(4, 8), index(4), 10, out=Operand(10, 8, **ELSEWHERE)),
+    lambda: B.embedding_grad(Operand(4, 8), index(4), 10, out=Operand(10, 8), workspace=Operand(4096, dtype=torch.uint8, **ELSEWHERE)),
+    lambda: B.token_logprobs(Operand(4, 30), index(4, **ELSEWHERE)),
+    lambda: B.token_logprobs_grad(Operand(4, 30), index(4, **ELSEWHERE), rows(4), rows(4), rows(4)),
+    lambda: B.token_logprobs_grad(Operand(4, 30), index(4), rows(4, **ELSEWHERE), rows(4), rows(4)),
+    lambda: B.token_logprobs_grad(Operand(4, 30), index(4), rows(4), rows(4, **ELSEWHERE), rows(4), rows(4)),
+    lambda: B.token_logprobs_grad(Operand(4, 30), index(4), rows(4), rows(4), rows(4, **ELSEWHERE)),
+    lambda: B.token_logprobs_grad(Operand(4, 30), index(4), rows(4), rows(4), rows(4), rows(4, **ELSEWHERE)),
+    lambda: B.token_logprobs_grad(Operand(4, 30), index(4), rows(4), rows(4), rows(4), out=Operand(4, 30, **ELSEWHERE)),
+])
+def test_tensors_of_two_devices(call):
+    with pytest.raises(ValueError, match="one device"):
+        call()
+
+
+@pytest.mark.parametrize("call", [
+    lambda s: B.embedding(Operand(10, 8), index(4), stream=s),
+    lambda s: B.embedding_grad(Operand(4, 8), index(4), 10, stream=s),
+    lambda s: B.token_logprobs(Operand(4, 30), index(4), stream=s),
+    lambda s: B.token_logprobs_grad(Operand(4, 30), index(4), rows(4), rows(4), rows(4), stream=s),
+])
+def test_a_stream_of_another_device(call):
+    with pytest.raises(ValueError, match="stream"):
+        call(Stream("cuda:1"))
