@@ -458,17 +458,18 @@ def muon_workspace_bytes(shapes, cfg: MuonConfig) -> int:
 
 class Muon:
     """apollo_muon_create / apollo_muon_step: orthogonalised updates of a list of 2-D CUDA tensors (one dtype,
-    contiguous); the fp32 momenta are the caller's."""
+    contiguous, on the context's device); the fp32 momenta are the caller's.  Calls run on `stream` or the device's
+    current one, whichever device is current."""
 
     def __init__(self, shapes, cfg: MuonConfig, device="cuda"):
         self.lib = load()
         self.shapes = [(int(r), int(c)) for r, c in shapes]
         self.cfg = cfg
-        self.device = torch.device(device)
         nbytes = muon_workspace_bytes(self.shapes, cfg)
         self.workspace_bytes = nbytes
-        with torch.cuda.device(self.device):
-            self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        with torch.cuda.device(device):
+            self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
+            self.device = self.workspace.device              # with its index
             base = (self.workspace.data_ptr() + 255) // 256 * 256
             ctx = ctypes.c_void_p()
             _check(self.lib.apollo_muon_create(ctypes.byref(ctx), _shape_array(self.shapes), len(self.shapes),
@@ -497,22 +498,27 @@ class Muon:
             for i, (x, shp) in enumerate(zip(xs, self.shapes)):
                 if x.dtype != dt or x.shape != shp or not x.is_cuda or not x.is_contiguous():
                     raise ValueError("tensors must be contiguous CUDA tensors of the context's dtype and shapes (momenta: float32)")
+                if x.device != self.device:
+                    raise ValueError(f"tensors must be on the context's device {self.device}, got {x.device}")
                 arr[i] = x.data_ptr()
 
     def step(self, Ws, Gs, Ms, lr: float, wd: float = 0.0, stream=None):
         """One update of the weights Ws and the momenta Ms (float32, zero before the first step) from the gradients Gs."""
         self._marshal((Ws, Gs, Ms))
         w, g, m = self._arrays
-        _check(self.lib.apollo_muon_step(self.ctx, w, g, m, lr, wd, _stream_ptr(stream)), "apollo_muon_step")
+        with _on(stream, self.device):
+            _check(self.lib.apollo_muon_step(self.ctx, w, g, m, lr, wd, _stream_ptr(stream)), "apollo_muon_step")
 
     def orthogonalize(self, Us, Os, stream=None):
         """Os <- the orthogonalised Us (Os may be Us)."""
         self._marshal((Os, Us))
         o, u, _ = self._arrays
-        _check(self.lib.apollo_muon_orthogonalize(self.ctx, u, o, _stream_ptr(stream)), "apollo_muon_orthogonalize")
+        with _on(stream, self.device):
+            _check(self.lib.apollo_muon_orthogonalize(self.ctx, u, o, _stream_ptr(stream)), "apollo_muon_orthogonalize")
 
     def status(self, stream=None) -> int:
-        return self.lib.apollo_muon_status(self.ctx, _stream_ptr(stream))
+        with _on(stream, self.device):
+            return self.lib.apollo_muon_status(self.ctx, _stream_ptr(stream))
 
     def last_launches(self) -> int:
         out = ctypes.c_int32(0)

@@ -93,3 +93,88 @@ def test_tensors_of_two_devices(call):
 def test_a_stream_of_another_device(call):
     with pytest.raises(ValueError, match="stream"):
         call(Stream("cuda:1"))
+
+
+class Library:
+    """Records the device and the stream that a call of the library would run on."""
+
+    def __init__(self, on):
+        self.on, self.calls = on, []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, self.on["device"], args[-1]))
+            return 0
+        return call
+
+
+class Tensors(Operand):
+    def data_ptr(self):
+        return 4096
+
+
+@pytest.fixture
+def context(monkeypatch):
+    """A context of the second of two devices while the first is the current one."""
+    on = {"device": 0}
+
+    class Device:
+        def __init__(self, device):
+            index = torch.device(device).index
+            self.index = on["device"] if index is None else index
+
+        def __enter__(self):
+            self.before, on["device"] = on["device"], self.index
+
+        def __exit__(self, *_):
+            on["device"] = self.before
+
+    class OnStream(Device):
+        def __init__(self, stream):
+            super().__init__(stream.device)
+    monkeypatch.setattr(B, "_current_device", lambda: on["device"])
+    monkeypatch.setattr(B, "_raw_stream", lambda device: 1000 + device)
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(torch.cuda, "stream", OnStream)
+    library = Library(on)
+    monkeypatch.setattr(B, "load", lambda: library)
+    monkeypatch.setattr(B, "muon_workspace_bytes", lambda shapes, cfg: 4096)
+    monkeypatch.setattr(torch, "empty", lambda n, dtype, device: Tensors(n, dtype=dtype, device=f"cuda:{on['device']}"))
+    opt = B.Muon([(4, 8)], B.make_muon_config(dtype=B.DT_F32), device="cuda:1")
+    library.calls.clear()
+    return opt, library
+
+
+def tensor_lists(device):
+    return [[Tensors(4, 8, device=device)] for _ in range(3)]
+
+
+def test_a_context_works_on_its_own_device(context):
+    opt, library = context
+    ws, gs, ms = tensor_lists("cuda:1")
+    opt.step(ws, gs, ms, 0.1)
+    opt.orthogonalize(gs, ws)
+    opt.status()
+    opt.step(ws, gs, ms, 0.1, stream=Stream("cuda:1"))
+    assert [c[1] for c in library.calls] == [1, 1, 1, 1]
+    assert [c[2] for c in library.calls] == [1001, 1001, 1001, 0]
+    assert B._current_device() == 0
+
+
+def test_a_context_refuses_other_devices(context):
+    opt, library = context
+    for k in range(3):
+        lists = tensor_lists("cuda:1")
+        lists[k] = tensor_lists("cuda:0")[0]
+        with pytest.raises(ValueError, match="device"):
+            opt.step(*lists, 0.1)
+    with pytest.raises(ValueError, match="stream"):
+        opt.step(*tensor_lists("cuda:1"), 0.1, stream=Stream("cuda:0"))
+    assert not library.calls
+
+
+def test_a_context_without_an_index_takes_the_current_device(context):
+    opt = B.Muon([(4, 8)], B.make_muon_config(dtype=B.DT_F32))
+    opt.step(*tensor_lists("cuda:0"), 0.1)
+    with pytest.raises(ValueError, match="device"):
+        opt.step(*tensor_lists("cuda:1"), 0.1)
