@@ -470,6 +470,7 @@ class Muon:
         with torch.cuda.device(device):
             self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
             self.device = self.workspace.device              # with its index
+            self._home = _stream_ptr(None)                   # the stream that the workspace belongs to
             base = (self.workspace.data_ptr() + 255) // 256 * 256
             ctx = ctypes.c_void_p()
             _check(self.lib.apollo_muon_create(ctypes.byref(ctx), _shape_array(self.shapes), len(self.shapes),
@@ -502,19 +503,25 @@ class Muon:
                     raise ValueError(f"tensors must be on the context's device {self.device}, got {x.device}")
                 arr[i] = x.data_ptr()
 
+    def _call(self, name, stream, *args):
+        with _on(stream, self.device):
+            ptr = _stream_ptr(stream)
+            if ptr != self._home:
+                # freed, the workspace must not be handed out again before this stream is done with it
+                self.workspace.record_stream(torch.cuda.current_stream())
+            _check(getattr(self.lib, name)(self.ctx, *args, ptr), name)
+
     def step(self, Ws, Gs, Ms, lr: float, wd: float = 0.0, stream=None):
         """One update of the weights Ws and the momenta Ms (float32, zero before the first step) from the gradients Gs."""
         self._marshal((Ws, Gs, Ms))
         w, g, m = self._arrays
-        with _on(stream, self.device):
-            _check(self.lib.apollo_muon_step(self.ctx, w, g, m, lr, wd, _stream_ptr(stream)), "apollo_muon_step")
+        self._call("apollo_muon_step", stream, w, g, m, lr, wd)
 
     def orthogonalize(self, Us, Os, stream=None):
         """Os <- the orthogonalised Us (Os may be Us)."""
         self._marshal((Os, Us))
         o, u, _ = self._arrays
-        with _on(stream, self.device):
-            _check(self.lib.apollo_muon_orthogonalize(self.ctx, u, o, _stream_ptr(stream)), "apollo_muon_orthogonalize")
+        self._call("apollo_muon_orthogonalize", stream, u, o)
 
     def status(self, stream=None) -> int:
         with _on(stream, self.device):

@@ -112,6 +112,9 @@ class Tensors(Operand):
     def data_ptr(self):
         return 4096
 
+    def record_stream(self, stream):
+        self.used_on = getattr(self, "used_on", []) + [stream]
+
 
 @pytest.fixture
 def context(monkeypatch):
@@ -136,6 +139,7 @@ def context(monkeypatch):
     monkeypatch.setattr(B, "_raw_stream", lambda device: 1000 + device)
     monkeypatch.setattr(torch.cuda, "device", Device)
     monkeypatch.setattr(torch.cuda, "stream", OnStream)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: "the current stream")
     library = Library(on)
     monkeypatch.setattr(B, "load", lambda: library)
     monkeypatch.setattr(B, "muon_workspace_bytes", lambda shapes, cfg: 4096)
@@ -178,3 +182,12 @@ def test_a_context_without_an_index_takes_the_current_device(context):
     opt.step(*tensor_lists("cuda:0"), 0.1)
     with pytest.raises(ValueError, match="device"):
         opt.step(*tensor_lists("cuda:1"), 0.1)
+
+
+def test_the_allocator_hears_of_another_stream(context):
+    opt, _ = context
+    opt.step(*tensor_lists("cuda:1"), 0.1)
+    assert not hasattr(opt.workspace, "used_on")
+    opt.step(*tensor_lists("cuda:1"), 0.1, stream=Stream("cuda:1"))
+    opt.orthogonalize(*tensor_lists("cuda:1")[:2], stream=Stream("cuda:1"))
+    assert opt.workspace.used_on == ["the current stream"] * 2
