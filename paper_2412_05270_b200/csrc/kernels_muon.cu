@@ -511,7 +511,8 @@ __device__ __forceinline__ void store_elem(__nv_bfloat16* p, float v) { *p = __f
 }  // namespace
 
 // A block takes one of the matrix's n_part contiguous pieces (a multiple of 8 elements long): momentum in place,
-// squares added in fp32 over eight elements and in fp64 from there on, one partial sum per block in a fixed order.
+// squares added in fp32 over eight elements (in fp64 where those leave the range of fp32: entries above 1e19 or below
+// 1e-15) and in fp64 from there on, one partial sum per block in a fixed order.
 template <typename T, bool STEP>
 __global__ void __launch_bounds__(MS_THREADS)
 muon_moment_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ status)
@@ -533,8 +534,7 @@ muon_moment_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ sta
     double sum = 0.0;
     auto one = [&](float g, float& m) {
         if constexpr (STEP) m = fmaf(a.mu, m, (1.0f - a.mu) * g);
-        const float u = update_of<STEP>(g, m, a);
-        return u * u;
+        return update_of<STEP>(g, m, a);
     };
     for (int64_t e = begin + (int64_t)threadIdx.x * 8; e < end; e += MS_THREADS * 16) {
         // two vectors of eight per round, all loads before the first use
@@ -558,8 +558,16 @@ muon_moment_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ sta
             if (count <= 0) break;
             float s = 0.0f;
 #pragma unroll
-            for (int x = 0; x < 8; ++x) s += one(g[u][x], m[u][x]);
-            sum += (double)s;
+            for (int x = 0; x < 8; ++x) {
+                g[u][x] = one(g[u][x], m[u][x]);
+                s += g[u][x] * g[u][x];
+            }
+            if (s >= 1e-30f && s <= 1e38f) {
+                sum += (double)s;
+            } else {
+#pragma unroll
+                for (int x = 0; x < 8; ++x) sum += (double)g[u][x] * (double)g[u][x];
+            }
             if constexpr (STEP) {
                 if (count == 8 && APOLLO_DBG_RANGE(p, p + 7, numel, status)) {
                     reinterpret_cast<float4*>(M + p)[0] = make_float4(m[u][0], m[u][1], m[u][2], m[u][3]);
@@ -598,9 +606,15 @@ muon_load_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ statu
     __half* __restrict__ hi = it.x[0];
     __half* __restrict__ lo = it.x[1];
     // the sum of squares comes last: its loads and the reduction hide behind those of the elements
+    float pre = 1.0f, f = 0.0f;
     auto factor = [&]() {
-        const double total = block_sum((int)threadIdx.x < it.n_part ? it.part[threadIdx.x] : 0.0, scratch);
-        return a.x_scale / ((float)sqrt(total) + a.eps);
+        const double norm = sqrt(block_sum((int)threadIdx.x < it.n_part ? it.part[threadIdx.x] : 0.0, scratch));
+        const float to = (float)norm + a.eps;
+        f = a.x_scale / to;
+        if (!(to >= 0x1p-60f && to <= 0x1p74f)) {        // the factor or its product with an element could leave fp32: in two parts
+            pre = norm > 1.0 ? 0x1p-64f : 0x1p64f;
+            f = (float)(a.x_scale / (norm + (double)a.eps) / pre);
+        }
     };
     if (vectors) {
         // rows are whole vectors on both sides
@@ -621,7 +635,7 @@ muon_load_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ statu
 #pragma unroll
             for (int e = 0; e < 8; ++e) u[i][e] = update_of<STEP>(u[i][e], m[e], a);
         }
-        const float f = factor();
+        factor();
 #pragma unroll
         for (int i = 0; i < MS_LOAD_VEC; ++i) {
             const int r = r1 + 32 * i;
@@ -630,7 +644,7 @@ muon_load_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ statu
             uint32_t w[4], l[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float v0 = u[i][2 * e] * f, v1 = u[i][2 * e + 1] * f;
+                const float v0 = u[i][2 * e] * pre * f, v1 = u[i][2 * e + 1] * pre * f;
                 w[e] = pack_half2(v0, v1);
                 if constexpr (SPLIT) {
                     const float2 h = unpack_half2(w[e]);
@@ -655,7 +669,12 @@ muon_load_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ statu
         u[i][0] = update_of<STEP>(u[i][0], m[0], a);
         u[i][1] = update_of<STEP>(u[i][1], m[1], a);
     }
-    const float f = factor();
+    factor();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        u[i][0] = u[i][0] * pre * f;
+        u[i][1] = u[i][1] * pre * f;
+    }
     // two neighbours of one row of X (its pitch is a multiple of 64: pairs are always aligned)
     auto put = [&](int64_t at, float v0, float v1) {
         if (!APOLLO_DBG_RANGE(at, at + 1, extent, status)) return;
@@ -670,11 +689,11 @@ muon_load_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ statu
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int r = r0 + rr + 8 * i;
-            if (r < rows && c0 + c < cols) put((int64_t)r * it.x_pitch + c0 + c, u[i][0] * f, u[i][1] * f);
+            if (r < rows && c0 + c < cols) put((int64_t)r * it.x_pitch + c0 + c, u[i][0], u[i][1]);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { tile[rr + 8 * i][c] = u[i][0] * f; tile[rr + 8 * i][c + 1] = u[i][1] * f; }
+        for (int i = 0; i < 8; ++i) { tile[rr + 8 * i][c] = u[i][0]; tile[rr + 8 * i][c + 1] = u[i][1]; }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
