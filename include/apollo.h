@@ -444,7 +444,9 @@ APOLLO_API int apollo_embedding_grad(const void* d_out, int64_t out_stride, cons
  * int32 or int64; logprob, entropy, lse: DEVICE, n_rows floats; top_logprob, top_index: DEVICE, n_rows x top (may be
  * null with top = 0).  Pointers need the alignment of their elements.  The gradient takes lse and entropy of the
  * forward pass; grad_entropy (and then entropy) may be null: no entropy term.  grad_logits may be the logits
- * themselves (same stride).  Statistics are fp32.
+ * themselves (same stride).  Statistics are fp32.  Log probabilities are differences to the row's largest logits, not to the
+ * rounded lse: an offset that all logits of a row share costs them no digits, and none is above 0.  The gradient knows the
+ * row by lse, whose rounding (2^-24 of its size) is the relative error of its p_j.
  */
 #define APOLLO_MAX_TOP 32
 APOLLO_API int apollo_token_logprobs(const void* d_logits, int64_t row_stride, int64_t n_rows, int64_t vocab, int32_t dtype,

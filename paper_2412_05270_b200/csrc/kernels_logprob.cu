@@ -7,6 +7,9 @@
 // Conventions: logits of -inf are masked words (p = 0, no gradient).  A row in which every word is masked has
 // lse = -inf, logp = -inf, H = 0, no gradient.  A target outside [0, vocab) is ignored: logp = 0, g counts as 0.
 //
+// A log probability is formed as (logit - m) scale - log s, not as z - lse: lse is rounded at the size of the logits, and a
+// common offset of them (1e4, say) must not cost the digits of a difference.
+//
 // Forward: one pass.  A thread keeps a reference m near the maximum of its elements and, with t = (logit - m) scale log2 e,
 // s = sum 2^t and u = sum 2^t t; a new reference rescales both (u by the shift too).  Joined over the block, then over
 // the cluster of CTAs that share a row, H = log s - log 2 u / s: the difference of small numbers, not of lse and a mean.
@@ -192,6 +195,15 @@ __device__ __forceinline__ float vec_max(const uint4& r, const float*)
 }
 __device__ __forceinline__ uint4 vec_masked(const __nv_bfloat16*) { return make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u); }
 __device__ __forceinline__ uint4 vec_masked(const float*) { return make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u); }
+
+// Log probability of a logit v beside the statistics (m, log s); rounding must not make it positive.
+__device__ __forceinline__ float log_prob(float v, float scale, float m, float log_s)
+{
+    const float d = v - m;
+    // (masked words and differences that overflow: the products, whose difference may not)
+    const float lp = isinf(d) ? __fmul_rn(v, scale) - fmaf(m, scale, log_s) : fmaf(d, scale, -log_s);
+    return lp > 0.0f ? 0.0f : lp;
+}
 
 // Order of the alternatives: larger value first, then the lower index.  As one 64-bit key: the value's bits made
 // monotone, then the complement of the index.  -0 counts as +0, NaN as the lowest value.  0 is "no entry".
@@ -486,7 +498,7 @@ logprob_kernel(LogprobArgs a)
             if (tid == 0) {
                 a.lse[r] = lse;
                 a.entropy[r] = dead ? 0.0f : log_s - LN2 * (all.u / all.s);
-                a.logprob[r] = !live ? 0.0f : dead ? -INFINITY : __fmul_rn(chosen, scale) - lse;
+                a.logprob[r] = !live ? 0.0f : dead ? -INFINITY : log_prob(chosen, scale, all.m, log_s);
             }
             if constexpr (TOP) {
                 const int n = parts * a.top;              // at most 8 x 32
@@ -502,9 +514,9 @@ logprob_kernel(LogprobArgs a)
                         for (int o = 0; o < n; ++o) ahead += cand[o] > k ? 1 : 0;
                     }
                     if (k != 0 && ahead < a.top) {
-                        const float z = (uint32_t)(k >> 32) == 1u ? NAN : top_value(k);
-                        a.top_index[r * a.top + ahead] = (int)~(uint32_t)k;
-                        a.top_logprob[r * a.top + ahead] = dead ? -INFINITY : z - lse;
+                        const int i = (int)~(uint32_t)k;
+                        a.top_index[r * a.top + ahead] = i;
+                        a.top_logprob[r * a.top + ahead] = dead ? -INFINITY : log_prob(load1(row + i), scale, all.m, log_s);
                     }
                 }
             }
