@@ -13,13 +13,17 @@ class _Embedding(torch.autograd.Function):
     @staticmethod
     def forward(ctx, table, index, scale):
         ctx.save_for_backward(index)
-        ctx.rows, ctx.scale = table.shape[0], scale
+        ctx.rows, ctx.dim, ctx.scale = *table.shape, scale
         return B.embedding(table, index, scale)
 
     @staticmethod
     def backward(ctx, d_out):
         index, = ctx.saved_tensors
-        return B.embedding_grad(d_out.reshape(index.numel(), -1), index, ctx.rows, scale=ctx.scale), None, None
+        d_out = d_out.reshape(index.numel(), ctx.dim)
+        # (a gradient that was broadcast or transposed: the kernels read contiguous rows that do not overlap)
+        if (ctx.dim > 1 and d_out.stride(1) != 1) or (d_out.shape[0] > 1 and d_out.stride(0) < ctx.dim):
+            d_out = d_out.contiguous()
+        return B.embedding_grad(d_out, index, ctx.rows, scale=ctx.scale), None, None
 
 
 class _TokenLogprobs(torch.autograd.Function):

@@ -295,7 +295,7 @@ def _index_of(x: torch.Tensor, what: str) -> int:
 def _rows_of(x: torch.Tensor, what: str) -> int:
     """The row stride of a 2-D CUDA tensor whose rows are contiguous."""
     shape = x.shape
-    if not x.is_cuda or len(shape) != 2 or (shape[1] > 1 and x.stride(1) != 1):
+    if not x.is_cuda or len(shape) != 2 or (shape[0] > 0 and shape[1] > 1 and x.stride(1) != 1):
         raise ValueError(f"{what} must be a 2-D CUDA tensor with contiguous rows")
     if shape[0] <= 1:
         return max(shape[1], 1)

@@ -1,0 +1,48 @@
+"""The autograd functions: gradients of every layout that autograd hands back, empty indices."""
+import pytest
+import torch
+
+from paper_2412_05270_b200 import autograd as A
+
+pytestmark = pytest.mark.gpu
+
+
+def lookup(table, index, scale):
+    """The definition in 64 bits."""
+    live = ((index >= 0) & (index < table.shape[0]))[..., None]
+    return torch.where(live, table[index.clamp(0, table.shape[0] - 1)], 0.0) * scale
+
+
+CONSUMERS = {
+    "sum": lambda y, w: y.sum(),                                                    # strides (0, 0)
+    "sum over the columns": lambda y, w: (y.sum(-1) * w[..., 0]).sum(),             # strides (1, 0)
+    "sum over the positions": lambda y, w: (y.sum(-2) * w[..., 0, :]).sum(),        # strides (0, 1)
+    "transposed": lambda y, w: (y.transpose(-1, -2).contiguous() * w.transpose(-1, -2).contiguous()).sum(),
+    "sliced": lambda y, w: (y[..., 1:3] * w[..., 1:3]).sum(),
+    "as it is": lambda y, w: (y * w).sum(),
+}
+
+
+@pytest.mark.parametrize("how", list(CONSUMERS))
+@pytest.mark.parametrize("shape", [(7,), (1, 6), (3, 5), (1, 1)])
+def test_table_gradient_of_any_layout(shape, how):
+    g = torch.Generator(device="cuda").manual_seed(3)
+    index = torch.randint(-1, 9, shape, generator=g, device="cuda")
+    table = torch.randn(8, 5, generator=g, device="cuda").requires_grad_()
+    w = torch.randn(*shape, 5, generator=g, device="cuda")
+    CONSUMERS[how](A.embedding(table, index, 1.5), w).backward()
+    t = table.detach().double().requires_grad_()
+    CONSUMERS[how](lookup(t, index, 1.5), w.double()).backward()
+    # at most 15 terms of one row summed in fp32, each up to 4 x 1.5 and rounded once before
+    assert bool(((table.grad.double() - t.grad).abs() <= 2 * 15 * 16 * 6 * 2.0 ** -24).all())
+
+
+@pytest.mark.parametrize("shape", [(0,), (0, 4), (3, 0)])
+def test_an_empty_index_has_a_zero_gradient(shape):
+    table = torch.randn(8, 5, device="cuda", requires_grad=True)
+    out = A.embedding(table, torch.empty(shape, dtype=torch.int64, device="cuda"))
+    assert out.shape == (*shape, 5)
+    (out.sum() + table[0, 0]).backward()
+    want = torch.zeros(8, 5, device="cuda")
+    want[0, 0] = 1
+    assert torch.equal(table.grad, want)
