@@ -1,12 +1,29 @@
 """The two ends of a language model as autograd functions: token embedding and token log probabilities.
 
 Both call the library's kernels in either direction (no PyTorch arithmetic in between); see `binding` for the shapes
-and types they take."""
+and types they take.  They have first derivatives; differentiating one of those raises."""
 from __future__ import annotations
 
 import torch
 
 from . import binding as B
+
+
+class _FirstOrder(torch.autograd.Function):
+    """Hands a gradient on as a function of the tensors it was computed from, and refuses to be differentiated: without it a
+    term made of the gradient (create_graph=True) would count as constant and drop out of another loss's backward pass."""
+
+    @staticmethod
+    def forward(ctx, grad, *sources):
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("embedding and token_logprobs have a first derivative only")
+
+
+def _first_order(grad, *sources):
+    return _FirstOrder.apply(grad, *sources) if torch.is_grad_enabled() else grad          # enabled: create_graph=True
 
 
 class _Embedding(torch.autograd.Function):
@@ -23,7 +40,7 @@ class _Embedding(torch.autograd.Function):
         # (a gradient that was broadcast or transposed: the kernels read contiguous rows that do not overlap)
         if (ctx.dim > 1 and d_out.stride(1) != 1) or (d_out.shape[0] > 1 and d_out.stride(0) < ctx.dim):
             d_out = d_out.contiguous()
-        return B.embedding_grad(d_out, index, ctx.rows, scale=ctx.scale), None, None
+        return _first_order(B.embedding_grad(d_out, index, ctx.rows, scale=ctx.scale), d_out), None, None
 
 
 class _TokenLogprobs(torch.autograd.Function):
@@ -39,8 +56,9 @@ class _TokenLogprobs(torch.autograd.Function):
         logits, targets, lse, entropy = ctx.saved_tensors
         if d_logprob is None:
             d_logprob = torch.zeros_like(lse)
-        return B.token_logprobs_grad(logits, targets, lse, entropy, d_logprob.contiguous(),
-                                     None if d_entropy is None else d_entropy.contiguous(), scale=ctx.scale), None, None
+        grad = B.token_logprobs_grad(logits, targets, lse, entropy, d_logprob.contiguous(),
+                                     None if d_entropy is None else d_entropy.contiguous(), scale=ctx.scale)
+        return _first_order(grad, logits, d_logprob, d_entropy), None, None
 
 
 def embedding(table: torch.Tensor, index: torch.Tensor, scale: float = 1.0) -> torch.Tensor:

@@ -1,4 +1,4 @@
-"""The autograd functions: gradients of every layout that autograd hands back, empty indices."""
+"""The autograd functions: gradients of every layout that autograd hands back, empty indices, second order."""
 import pytest
 import torch
 
@@ -46,3 +46,26 @@ def test_an_empty_index_has_a_zero_gradient(shape):
     want = torch.zeros(8, 5, device="cuda")
     want[0, 0] = 1
     assert torch.equal(table.grad, want)
+
+
+def test_a_second_derivative_is_refused():
+    index = torch.tensor([1, 2, 2], device="cuda")
+    target = torch.tensor([0, 3, 1], device="cuda")
+    table = torch.randn(6, 4, device="cuda", requires_grad=True)
+    logits = torch.randn(3, 7, device="cuda", requires_grad=True)
+    cases = [(table, A.embedding(table, index).square().sum()),
+             (logits, A.token_logprobs(logits, target)[0].square().sum()),
+             (logits, A.token_logprobs(logits, target)[0].sum()),          # its first derivative depends on the logits all the same
+             (logits, A.token_logprobs(logits, target)[1].sum())]
+    for x, loss in cases:
+        once, = torch.autograd.grad(loss, x, create_graph=True)
+        with pytest.raises(RuntimeError, match="first derivative"):
+            # beside a term that has a gradient a penalty must not drop out without a word
+            (once.square().sum() + x.sum()).backward()
+
+
+def test_create_graph_gives_the_same_first_derivative():
+    target = torch.tensor([0, 3, -1], device="cuda")
+    logits = torch.randn(3, 7, device="cuda", requires_grad=True)
+    grads = [torch.autograd.grad(A.token_logprobs(logits, target)[0].sum(), logits, create_graph=c)[0] for c in (False, True)]
+    assert torch.equal(grads[0], grads[1].detach())
