@@ -69,3 +69,18 @@ def test_create_graph_gives_the_same_first_derivative():
     logits = torch.randn(3, 7, device="cuda", requires_grad=True)
     grads = [torch.autograd.grad(A.token_logprobs(logits, target)[0].sum(), logits, create_graph=c)[0] for c in (False, True)]
     assert torch.equal(grads[0], grads[1].detach())
+
+
+def test_outputs_can_be_changed_in_place():
+    z = torch.randn(4, 9, device="cuda", requires_grad=True)
+    t = torch.tensor([1, 8, -1, 0], device="cuda")
+    weight = torch.tensor([0.5, 2.0, 1.0, 0.0], device="cuda")
+    want, = torch.autograd.grad((A.token_logprobs(z, t)[0] * weight).sum(), z)
+    logprob, entropy = A.token_logprobs(z, t)
+    logprob.mul_(weight)
+    logprob[3] = 0
+    assert torch.equal(torch.autograd.grad(logprob.sum(), z)[0], want)
+    logprob, entropy = A.token_logprobs(z, t)
+    entropy.add_(1.0)                                  # the gradient needs the entropy as it was computed
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        entropy.sum().backward()
