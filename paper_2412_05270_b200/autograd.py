@@ -48,6 +48,7 @@ class _TokenLogprobs(torch.autograd.Function):
     def forward(ctx, logits, targets, scale):
         r = B.token_logprobs(logits, targets, scale=scale)
         ctx.save_for_backward(logits, targets, r.lse, r.entropy)
+        ctx.set_materialize_grads(False)               # an output that no loss uses: None, no entropy term
         ctx.scale = scale
         return r.logprob, r.entropy
 

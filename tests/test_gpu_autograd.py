@@ -1,8 +1,9 @@
-"""The autograd functions: gradients of every layout that autograd hands back, empty indices, second order."""
+"""The autograd functions: gradients of every layout that autograd hands back, empty indices, second order, unused outputs."""
 import pytest
 import torch
 
 from paper_2412_05270_b200 import autograd as A
+from paper_2412_05270_b200 import binding as B
 
 pytestmark = pytest.mark.gpu
 
@@ -84,3 +85,28 @@ def test_outputs_can_be_changed_in_place():
     entropy.add_(1.0)                                  # the gradient needs the entropy as it was computed
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         entropy.sum().backward()
+
+
+def test_outputs_that_no_loss_uses(monkeypatch):
+    seen = []
+    plain = B.token_logprobs_grad
+
+    def watched(logits, targets, lse, entropy, d_logprob, d_entropy=None, **kw):
+        seen.append((d_logprob, d_entropy))
+        return plain(logits, targets, lse, entropy, d_logprob, d_entropy, **kw)
+    monkeypatch.setattr(A.B, "token_logprobs_grad", watched)
+    z = torch.randn(5, 40, device="cuda", requires_grad=True)
+    t = torch.tensor([0, 3, 39, -1, 7], device="cuda")
+    A.token_logprobs(z, t)[0].sum().backward()
+    assert seen[0][1] is None                          # no entropy term is computed, no zeros are made for it
+    zz = z.detach().double().requires_grad_()
+    lp = torch.log_softmax(zz, -1)
+    torch.where(t >= 0, lp.gather(1, t.clamp(min=0)[:, None])[:, 0], 0.0).sum().backward()
+    assert ((z.grad.double() - zz.grad).norm() / zz.grad.norm()).item() < 1e-5
+    z.grad = None
+    A.token_logprobs(z, t)[1].sum().backward()         # the entropy alone
+    zz.grad = None
+    lp = torch.log_softmax(zz, -1)
+    (-(lp.exp() * lp).sum()).backward()
+    assert ((z.grad.double() - zz.grad).norm() / zz.grad.norm()).item() < 1e-5
+    assert not seen[1][0].any()
