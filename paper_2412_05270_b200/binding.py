@@ -287,8 +287,8 @@ def _dtype_of(x: torch.Tensor, what: str) -> int:
 
 
 def _index_of(x: torch.Tensor, what: str) -> int:
-    if x.dtype not in (torch.int32, torch.int64) or not x.is_cuda or not x.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous CUDA tensor of int32 or int64")
+    if x.dtype not in (torch.int32, torch.int64) or not x.is_cuda:
+        raise ValueError(f"{what} must be a CUDA tensor of int32 or int64")
     return INDEX_I64 if x.dtype == torch.int64 else INDEX_I32
 
 
@@ -326,7 +326,7 @@ def _on(stream, device):
 def embedding(table, index, scale: float = 1.0, out=None, stream=None) -> torch.Tensor:
     """apollo_embedding: scale * table[index], a zero row where the index is outside the table.
 
-    table: (rows, dim), contiguous; index: any shape, int32 or int64; out: (index.numel(), dim) rows, made if None
+    table: (rows, dim), contiguous; index: any shape and strides, int32 or int64; out: (index.numel(), dim) rows, made if None
     (then of the index's shape with dim appended)."""
     dtype, itype = _dtype_of(table, "table"), _index_of(index, "index")
     if table.dim() != 2 or not table.is_contiguous() or not table.is_cuda:
@@ -335,6 +335,7 @@ def embedding(table, index, scale: float = 1.0, out=None, stream=None) -> torch.
     rows, dim = table.shape
     n = index.numel()
     with _on(stream, table.device):
+        index = index.contiguous()
         res = flat = out
         if out is None:
             res = torch.empty((*index.shape, dim), dtype=table.dtype, device=table.device)
@@ -368,6 +369,7 @@ def embedding_grad(d_out, index, rows: int, scale: float = 1.0, out=None, accumu
         raise ValueError("workspace must be a contiguous CUDA tensor")
     _one_device(d_out.device, index, out, workspace)
     with _on(stream, d_out.device):
+        index = index.contiguous()
         if out is None:
             if accumulate:
                 raise ValueError("accumulate needs the gradient to add to")
@@ -392,7 +394,7 @@ class TokenLogprobs(NamedTuple):
 
 
 def token_logprobs(logits, targets, scale: float = 1.0, top: int = 0, stream=None) -> TokenLogprobs:
-    """apollo_token_logprobs over the rows of `logits` (n, vocab); targets: n of int32 or int64, outside [0, vocab) =
+    """apollo_token_logprobs over the rows of `logits` (n, vocab); targets: n of int32 or int64 in any shape, outside [0, vocab) =
     ignored; top: how many of the best alternatives (<= MAX_TOP) come back as (n, top) log probabilities and indices."""
     dtype, itype = _dtype_of(logits, "logits"), _index_of(targets, "targets")
     stride = _rows_of(logits, "logits")
@@ -401,6 +403,7 @@ def token_logprobs(logits, targets, scale: float = 1.0, top: int = 0, stream=Non
         raise ValueError("targets must have one entry per row of logits")
     _one_device(logits.device, targets)
     with _on(stream, logits.device):
+        targets = targets.contiguous()
         # (empty_strided: 0.8 us less a call than empty, and for few rows the call is what takes the time; tensors of their own,
         # not views of one, 0.2 us more: autograd allows no view among several outputs to be changed in place)
         device = logits.device
@@ -431,6 +434,7 @@ def token_logprobs_grad(logits, targets, lse, entropy, d_logprob, d_entropy=None
         raise ValueError("targets must have one entry per row of logits")
     _one_device(logits.device, targets, lse, entropy, d_logprob, d_entropy, out)
     with _on(stream, logits.device):
+        targets = targets.contiguous()
         if out is None:
             out = torch.empty((n, vocab), dtype=logits.dtype, device=logits.device)
         elif out.dtype != logits.dtype or tuple(out.shape) != (n, vocab):
