@@ -352,7 +352,7 @@ APOLLO_API int apollo_mini_step_static(void* d_W, const void* d_G, int64_t rows,
  * held in 16-bit floats with 11 significant bits, scaled by powers of two: after five steps X is 0.7e-3 ... 1.5e-3 off
  * (relative, in the 2-norm of the entries; short sides below 256: to 1.7e-3), whether the rows and columns of U are alike or
  * differ by up to two powers of ten to either side; bfloat16's 8 bits would leave 1e-2, and the rounding of a bfloat16 result
- * is 1.65e-3 beside it.  With APOLLO_DT_F32 they are unevaluated sums of two such numbers, three products for one (the same
+ * is 1.65e-3 beside it.  With APOLLO_DT_F32, or APOLLO_MUON_PRODUCTS_PAIRS, they are unevaluated sums of two such numbers, three products for one (the same
  * inputs: 4e-6 ... 9e-6 at 256 x 512, to 4e-5 at 2048 x 5461, to 9e-5 at 4096 x 11008, from the sums of the tensor cores, which
  * cut where fp32 rounds).  An ill-conditioned U, a few directions far above the rest, loses more with 16-bit floats
  * (20 directions ten times the others: 3e-3;  16 a thousand times: 4e-2, where bfloat16 iterates lose 0.3;  pairs: 1e-4 ... 3e-4).
@@ -362,6 +362,8 @@ APOLLO_API int apollo_mini_step_static(void* d_W, const void* d_G, int64_t rows,
 #define APOLLO_MUON_SCALE_SHAPE 1 /* sqrt(max(1, rows / cols)) */
 #define APOLLO_MUON_SCALE_RMS 2   /* 0.2 sqrt(max(rows, cols)): entries of the size of an AdamW update */
 #define APOLLO_MUON_MAX_STEPS 32
+#define APOLLO_MUON_PRODUCTS_DEFAULT 0 /* by dtype: 16-bit floats with bfloat16 weights, pairs with fp32 */
+#define APOLLO_MUON_PRODUCTS_PAIRS 1   /* pairs with either: X as exact as with fp32 weights, three times the products */
 
 typedef struct apollo_muon_ctx apollo_muon_ctx; /* opaque HOST object */
 
@@ -375,6 +377,7 @@ typedef struct {
     float eps;            /* > 0 (1e-7) */
     int32_t workspace_mb; /* the matrices are worked on in groups whose iterates fit this many MB (a single matrix may
                              exceed it); 0 = default (2048) */
+    int32_t products;     /* APOLLO_MUON_PRODUCTS_* */
 } apollo_muon_config;
 
 /*

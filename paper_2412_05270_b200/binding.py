@@ -33,6 +33,7 @@ P_SCRATCH, P_SHARED = 0, 1
 PATH_STREAM, PATH_SIMT, PATH_TENSOR = 0, 1, 2
 MUON_SCALE_NONE, MUON_SCALE_SHAPE, MUON_SCALE_RMS = 0, 1, 2
 MUON_MAX_STEPS = 32
+MUON_PRODUCTS_DEFAULT, MUON_PRODUCTS_PAIRS = 0, 1
 INDEX_I32, INDEX_I64 = 0, 1
 MAX_TOP = 32
 
@@ -74,7 +75,7 @@ class MuonConfig(ctypes.Structure):
     """apollo_muon_config."""
     _fields_ = [("dtype", ctypes.c_int32), ("ns_steps", ctypes.c_int32), ("coef", ctypes.c_float * 3),
                 ("momentum", ctypes.c_float), ("nesterov", ctypes.c_int32), ("scale", ctypes.c_int32),
-                ("eps", ctypes.c_float), ("workspace_mb", ctypes.c_int32)]
+                ("eps", ctypes.c_float), ("workspace_mb", ctypes.c_int32), ("products", ctypes.c_int32)]
 
 
 class Tuning(ctypes.Structure):
@@ -448,9 +449,10 @@ def token_logprobs_grad(logits, targets, lse, entropy, d_logprob, d_entropy=None
 
 
 def make_muon_config(dtype=DT_BF16, steps=5, coef=(3.4445, -4.7750, 2.0315), momentum=0.95, nesterov=True,
-                     scale=MUON_SCALE_SHAPE, eps=1e-7, workspace_mb=0) -> MuonConfig:
+                     scale=MUON_SCALE_SHAPE, eps=1e-7, workspace_mb=0, products=MUON_PRODUCTS_DEFAULT) -> MuonConfig:
+    """products: MUON_PRODUCTS_PAIRS takes bfloat16 weights through products as exact as those of float32 ones."""
     return MuonConfig(int(dtype), int(steps), (ctypes.c_float * 3)(*coef), float(momentum), int(bool(nesterov)),
-                      int(scale), float(eps), int(workspace_mb))
+                      int(scale), float(eps), int(workspace_mb), int(products))
 
 
 def muon_workspace_bytes(shapes, cfg: MuonConfig) -> int:

@@ -26,12 +26,12 @@
 // A, B, T, A', B', Q are polynomials of one symmetric matrix: symmetric, so only half their tiles are computed.
 //
 // Rounding.  What is stored in 16 bits has 11 of them, and how much of the identity B + s I holds matters:
-//   bfloat16 weights  s = a: the products that use P read nothing beside their operands, and nothing is added in their
+//   16-bit floats     s = a: the products that use P read nothing beside their operands, and nothing is added in their
 //                     epilogues.  64-bit models of this arithmetic on normal gradients (512 x 512 ... 1024 x 2736): X is
 //                     1.0e-3 ... 1.3e-3 off; the rounding of the bfloat16 result is 1.65e-3.  (s such that B + s I lies near 0 where most singular values are near 1, and
 //                     (a - s) X added in fp32: 0.8e-3 ... 1.0e-3, and 15 % more time for a 60M model's 28 matrices, 2 % for
 //                     a 7B layer: not done.)
-//   fp32 weights      the second form: the sums of the tensor cores lose more on a X + B X as one product than the
+//   pairs             the second form: the sums of the tensor cores lose more on a X + B X as one product than the
 //                     fp32 addition does (200 x 200, five steps: 6e-6 instead of 2e-6).
 #include "../../include/apollo.h"
 
@@ -82,6 +82,9 @@ struct Plan {
     Scales sc;
 };
 
+// Whether iterates are sums of two 16-bit floats.
+bool split_of(const apollo_muon_config& cfg) { return cfg.dtype == APOLLO_DT_F32 || cfg.products == APOLLO_MUON_PRODUCTS_PAIRS; }
+
 double poly(const float* c, double x) { const double y = x * x; return x * (c[0] + y * (c[1] + y * c[2])); }
 
 // Bounds of everything stored, from the iteration on [0, 1] (the singular values of X start there).
@@ -104,7 +107,7 @@ bool find_scales(const apollo_muon_config& cfg, Scales& sc)
         t_max = std::max(t_max, std::fabs(y * p));
         p_max = std::max(p_max, std::fabs(p));
     }
-    const bool fold = cfg.dtype == APOLLO_DT_BF16;
+    const bool fold = !split_of(cfg);
     sc.shift = fold ? a : -(0.7 * b_min + 0.3 * b_max);
     sc.q_shift = fold ? 0.0 : 1.0;
     // the largest power of two that keeps a value of this size at or below 2^15 (16-bit floats end at 65504)
@@ -127,6 +130,7 @@ int validate(const apollo_muon_config* cfg, Scales& sc)
     if (!(cfg->momentum >= 0.0f && cfg->momentum < 1.0f) || (cfg->nesterov != 0 && cfg->nesterov != 1)) return APOLLO_ERR_INVALID_ARG;
     if (cfg->scale < APOLLO_MUON_SCALE_NONE || cfg->scale > APOLLO_MUON_SCALE_RMS) return APOLLO_ERR_INVALID_ARG;
     if (!std::isfinite(cfg->eps) || !(cfg->eps > 0.0f)) return APOLLO_ERR_INVALID_ARG;
+    if (cfg->products != APOLLO_MUON_PRODUCTS_DEFAULT && cfg->products != APOLLO_MUON_PRODUCTS_PAIRS) return APOLLO_ERR_INVALID_ARG;
     if (cfg->workspace_mb < 0 || cfg->workspace_mb > 65536) return APOLLO_ERR_INVALID_ARG;
     return find_scales(*cfg, sc) ? APOLLO_OK : APOLLO_ERR_INVALID_ARG;
 }
@@ -174,7 +178,7 @@ int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_confi
     if (!shapes || n_mat < 1) return APOLLO_ERR_INVALID_ARG;
     const int rc = validate(cfg, plan.sc);
     if (rc != APOLLO_OK) return rc;
-    plan.parts = cfg->dtype == APOLLO_DT_F32 ? 2 : 1;
+    plan.parts = split_of(*cfg) ? 2 : 1;
     plan.maps_per_mat = (2 + S_BUFS) * MUON_MAPS * plan.parts;
     plan.mats.resize(n_mat);
     std::vector<size_t> need(n_mat);
@@ -435,6 +439,7 @@ int run(apollo_muon_ctx* ctx, void* const* d_W, const void* const* d_G, float* c
     const uint64_t* d_list = reinterpret_cast<const uint64_t*>(ctx->ws + plan.off_list);
     uint32_t* d_ticket = reinterpret_cast<uint32_t*>(ctx->ws + plan.off_counters);
     const int dtype = ctx->cfg.dtype;
+    const bool split = plan.parts == 2;
     int launches = 0;
     cudaError_t err = cudaSuccess;
     for (const Group& g : plan.groups) {
@@ -464,15 +469,15 @@ int run(apollo_muon_ctx* ctx, void* const* d_W, const void* const* d_G, float* c
                 for (int k = a.n; k <= MUON_CHUNK; ++k) a.tile_begin[k] = (int)tiles;
                 if (tiles > INT32_MAX) { err = cudaErrorInvalidValue; return; }
                 if (which == 0) err = launch_muon_moment(dtype, step, a, (int)tiles, d_status, stream);
-                else if (which == 1) err = launch_muon_load(dtype, step, a, (int)tiles, d_status, stream);
-                else err = launch_muon_apply(dtype, step, a, (int)tiles, d_status, stream);
+                else if (which == 1) err = launch_muon_load(dtype, split, step, a, (int)tiles, d_status, stream);
+                else err = launch_muon_apply(dtype, split, step, a, (int)tiles, d_status, stream);
                 ++launches;
             }
         };
         pass(0);
         pass(1);
         if (err == cudaSuccess) {
-            err = launch_muon_gemm(plan.parts == 2, g.tile, d_ops, d_list + g.tile_begin, (int)g.tiles, d_ticket, ctx->launch, d_status, stream);
+            err = launch_muon_gemm(split, g.tile, d_ops, d_list + g.tile_begin, (int)g.tiles, d_ticket, ctx->launch, d_status, stream);
             ++launches;
         }
         pass(2);

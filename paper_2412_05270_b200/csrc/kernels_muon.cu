@@ -584,12 +584,11 @@ muon_moment_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ sta
     if (threadIdx.x == 0) it.part[piece] = total;
 }
 
-// X = U x_scale / (|U| + eps) as 16-bit floats (high and low part with `SPLIT` = fp32 weights), transposed when tall.
-template <typename T, bool STEP>
+// X = U x_scale / (|U| + eps) as 16-bit floats (high and low part with `SPLIT`), transposed when tall.
+template <typename T, bool STEP, bool SPLIT>
 __global__ void __launch_bounds__(MS_THREADS)
 muon_load_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ status)
 {
-    constexpr bool SPLIT = sizeof(T) == 4;
     __shared__ double scratch[32];
     __shared__ float tile[MS_ROWS][MS_COLS + 1];
     const int k = find_item(a, blockIdx.x);
@@ -704,11 +703,10 @@ muon_load_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ statu
 }
 
 // W <- W - lr (gain X + wd W), or O = X; X is read back transposed when tall.
-template <typename T, bool STEP>
+template <typename T, bool STEP, bool SPLIT>
 __global__ void __launch_bounds__(MS_THREADS)
 muon_apply_kernel(const __grid_constant__ MuonArgs a, int32_t* __restrict__ status)
 {
-    constexpr bool SPLIT = sizeof(T) == 4;
     __shared__ float tile[MS_ROWS][MS_COLS + 1];
     ptx::grid_wait_previous();
     if (*reinterpret_cast<volatile int32_t*>(status) != STATUS_OK) return;      // a product gave up: leave the weights
@@ -839,17 +837,20 @@ cudaError_t launch_muon_moment(int dtype, bool step, const MuonArgs& a, int tile
     return cudaGetLastError();
 }
 
-cudaError_t launch_muon_load(int dtype, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream)
+// (fp32 weights are always split)
+cudaError_t launch_muon_load(int dtype, bool split, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream)
 {
-    const auto kernel = dtype == APOLLO_DT_BF16 ? (step ? muon_load_kernel<__nv_bfloat16, true> : muon_load_kernel<__nv_bfloat16, false>)
-                                                : (step ? muon_load_kernel<float, true> : muon_load_kernel<float, false>);
+    const auto kernel = dtype == APOLLO_DT_F32 ? (step ? muon_load_kernel<float, true, true> : muon_load_kernel<float, false, true>)
+                        : split                ? (step ? muon_load_kernel<__nv_bfloat16, true, true> : muon_load_kernel<__nv_bfloat16, false, true>)
+                                               : (step ? muon_load_kernel<__nv_bfloat16, true, false> : muon_load_kernel<__nv_bfloat16, false, false>);
     return launch_after(kernel, dim3((unsigned)tiles), dim3(MS_THREADS), stream, a, d_status);
 }
 
-cudaError_t launch_muon_apply(int dtype, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream)
+cudaError_t launch_muon_apply(int dtype, bool split, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream)
 {
-    const auto kernel = dtype == APOLLO_DT_BF16 ? (step ? muon_apply_kernel<__nv_bfloat16, true> : muon_apply_kernel<__nv_bfloat16, false>)
-                                                : (step ? muon_apply_kernel<float, true> : muon_apply_kernel<float, false>);
+    const auto kernel = dtype == APOLLO_DT_F32 ? (step ? muon_apply_kernel<float, true, true> : muon_apply_kernel<float, false, true>)
+                        : split                ? (step ? muon_apply_kernel<__nv_bfloat16, true, true> : muon_apply_kernel<__nv_bfloat16, false, true>)
+                                               : (step ? muon_apply_kernel<__nv_bfloat16, true, false> : muon_apply_kernel<__nv_bfloat16, false, false>);
     return launch_after(kernel, dim3((unsigned)tiles), dim3(MS_THREADS), stream, a, d_status);
 }
 

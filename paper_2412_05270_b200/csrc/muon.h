@@ -61,8 +61,8 @@ struct MuonLaunch {                     // what the launches of a context need t
 // Sum of squares of U (and M <- mu M + (1 - mu) G with `step`), X = U x_scale / (|U| + eps) in 16 bits, and the end:
 // W <- W - lr (gain X + wd W) with `step`, O = X without.
 cudaError_t launch_muon_moment(int dtype, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream);
-cudaError_t launch_muon_load(int dtype, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream);
-cudaError_t launch_muon_apply(int dtype, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream);
+cudaError_t launch_muon_load(int dtype, bool split, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream);
+cudaError_t launch_muon_apply(int dtype, bool split, bool step, const MuonArgs& a, int tiles, int32_t* d_status, cudaStream_t stream);
 // Tiles of one matrix in the load and apply kernels, and whether they go by vectors of eight (rows of the matrix and of
 // the iterate are whole vectors, and nothing is transposed).
 __host__ __device__ inline bool muon_stream_vectors(int cols, bool tall) { return !tall && cols % 8 == 0; }
