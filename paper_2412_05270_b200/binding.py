@@ -288,9 +288,12 @@ def _dtype_of(x: torch.Tensor, what: str) -> int:
 
 
 def _index_of(x: torch.Tensor, what: str) -> int:
-    if x.dtype not in (torch.int32, torch.int64) or not x.is_cuda:
-        raise ValueError(f"{what} must be a CUDA tensor of int32 or int64")
-    return INDEX_I64 if x.dtype == torch.int64 else INDEX_I32
+    dtype = x.dtype
+    if dtype is torch.int64:
+        return INDEX_I64
+    if dtype is not torch.int32:
+        raise ValueError(f"{what} must be of int32 or int64")
+    return INDEX_I32
 
 
 def _rows_of(x: torch.Tensor, what: str) -> int:
@@ -306,10 +309,8 @@ def _rows_of(x: torch.Tensor, what: str) -> int:
     return stride
 
 
-def _one_device(device, *operands):
-    for x in operands:
-        if x is not None and x.device != device:
-            raise ValueError(f"the tensors of a call must be on one device, got {device} and {x.device}")
+def _two_devices():
+    return ValueError("the tensors of a call, out and workspace among them, must be on one device")
 
 
 _here = contextlib.nullcontext()
@@ -332,14 +333,16 @@ def embedding(table, index, scale: float = 1.0, out=None, stream=None) -> torch.
     dtype, itype = _dtype_of(table, "table"), _index_of(index, "index")
     if table.dim() != 2 or not table.is_contiguous() or not table.is_cuda:
         raise ValueError("table must be a 2-D contiguous CUDA tensor")
-    _one_device(table.device, index, out)
+    device = table.device
+    if index.device != device or (out is not None and out.device != device):
+        raise _two_devices()
     rows, dim = table.shape
     n = index.numel()
-    with _on(stream, table.device):
+    with _on(stream, device):
         index = index.contiguous()
         res = flat = out
         if out is None:
-            res = torch.empty((*index.shape, dim), dtype=table.dtype, device=table.device)
+            res = torch.empty((*index.shape, dim), dtype=table.dtype, device=device)
             flat = res.view(n, dim)
         elif out.dtype != table.dtype or tuple(out.shape) != (n, dim):
             raise ValueError("out must have the table's dtype and one row per index")
@@ -366,19 +369,21 @@ def embedding_grad(d_out, index, rows: int, scale: float = 1.0, out=None, accumu
     n, dim = d_out.shape
     if n != index.numel():
         raise ValueError("d_out must have one row per index")
-    if workspace is not None and (not workspace.is_cuda or not workspace.is_contiguous()):
-        raise ValueError("workspace must be a contiguous CUDA tensor")
-    _one_device(d_out.device, index, out, workspace)
-    with _on(stream, d_out.device):
+    device = d_out.device
+    if index.device != device or (out is not None and out.device != device) or (workspace is not None and workspace.device != device):
+        raise _two_devices()
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    with _on(stream, device):
         index = index.contiguous()
         if out is None:
             if accumulate:
                 raise ValueError("accumulate needs the gradient to add to")
-            out = torch.empty((rows, dim), dtype=d_out.dtype, device=d_out.device)
-        elif out.dtype != d_out.dtype or tuple(out.shape) != (rows, dim) or not out.is_contiguous() or not out.is_cuda:
+            out = torch.empty((rows, dim), dtype=d_out.dtype, device=device)
+        elif out.dtype != d_out.dtype or tuple(out.shape) != (rows, dim) or not out.is_contiguous():
             raise ValueError("out must be a contiguous CUDA tensor (rows, dim) of d_out's dtype")
         if workspace is None:
-            workspace = torch.empty(embedding_grad_workspace_bytes(n, rows, dim), dtype=torch.uint8, device=d_out.device)
+            workspace = torch.empty(embedding_grad_workspace_bytes(n, rows, dim), dtype=torch.uint8, device=device)
         _check(load().apollo_embedding_grad(d_out.data_ptr(), stride, index.data_ptr(), itype, n, rows, dim, dtype, scale,
                                             int(bool(accumulate)), out.data_ptr(), workspace.data_ptr(),
                                             workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
@@ -402,12 +407,13 @@ def token_logprobs(logits, targets, scale: float = 1.0, top: int = 0, stream=Non
     n, vocab = logits.shape
     if targets.numel() != n:
         raise ValueError("targets must have one entry per row of logits")
-    _one_device(logits.device, targets)
-    with _on(stream, logits.device):
+    device = logits.device
+    if targets.device != device:
+        raise _two_devices()
+    with _on(stream, device):
         targets = targets.contiguous()
         # (empty_strided: 0.8 us less a call than empty, and for few rows the call is what takes the time; tensors of their own,
         # not views of one, 0.2 us more: autograd allows no view among several outputs to be changed in place)
-        device = logits.device
         logprob = torch.empty_strided((n,), (1,), dtype=torch.float32, device=device)
         entropy, lse = torch.empty_like(logprob), torch.empty_like(logprob)
         best = best_at = None
@@ -428,16 +434,22 @@ def token_logprobs_grad(logits, targets, lse, entropy, d_logprob, d_entropy=None
     dtype, itype = _dtype_of(logits, "logits"), _index_of(targets, "targets")
     stride = _rows_of(logits, "logits")
     n, vocab = logits.shape
+    device = logits.device
     for x, what in ((lse, "lse"), (entropy, "entropy"), (d_logprob, "d_logprob"), (d_entropy, "d_entropy")):
-        if x is not None and (x.dtype != torch.float32 or x.numel() != n or not x.is_contiguous() or not x.is_cuda):
+        if x is None:
+            continue
+        if x.dtype != torch.float32 or x.numel() != n or not x.is_contiguous():
             raise ValueError(f"{what} must be a contiguous float32 CUDA tensor with one entry per row")
+        if x.device != device:
+            raise _two_devices()
     if targets.numel() != n:
         raise ValueError("targets must have one entry per row of logits")
-    _one_device(logits.device, targets, lse, entropy, d_logprob, d_entropy, out)
-    with _on(stream, logits.device):
+    if targets.device != device or (out is not None and out.device != device):
+        raise _two_devices()
+    with _on(stream, device):
         targets = targets.contiguous()
         if out is None:
-            out = torch.empty((n, vocab), dtype=logits.dtype, device=logits.device)
+            out = torch.empty((n, vocab), dtype=logits.dtype, device=device)
         elif out.dtype != logits.dtype or tuple(out.shape) != (n, vocab):
             raise ValueError("out must have the logits' dtype and shape")
         _check(load().apollo_token_logprobs_grad(

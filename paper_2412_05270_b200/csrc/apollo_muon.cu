@@ -228,12 +228,14 @@ int make_plan(const apollo_shape* shapes, int32_t n_mat, const apollo_muon_confi
     for (Group& g : plan.groups) {
         // Wide tiles move the fewest bytes per product; the others shorten a product (its tiles are loaded and stored by
         // more CTAs), which is what counts as long as there are few.  By the k-blocks of one m x m product of all matrices,
-        // in us, wide tiles against 256 x 128:  320 (two 1024 x 4096) 265, 251;  480 (20 of 512 x 512) 153, 141;  640 (four
-        // of 1024 x 1024) 187, 177;  672 (28 of 512 x 512) 174, 178;  800 (five of 1024) 194, 200;  1152 (one 2048) 268, 294.
-        // The same count in tiles of 128 x 128, these against 256 x 128:  80 (one 512 x 512) 94, 107;  576 (one 1024) 136,
-        // 152;  640 (eight of 512) 108, 115;  960 (twelve of 512) 123, 121;  1100 (one 1280) 188, 174;  1764 (one 1536) 291, 198.
-        // (fp32, three times the k-blocks, changes sides at the same counts: 480: 373, 361;  640: 458, 463;  1152: 732, 808;  and
-        // 576: 310, 355;  640: 225, 242;  960: 278, 260.)
+        // five steps of apollo_muon_orthogonalize in us, wide tiles against 256 x 128:  288 (12 of 512 x 512) 146, 123;  480 (20 of
+        // 512 x 512) 155, 145;  640 (four of 1024 x 1024) 188, 179;  672 (28 of 512 x 512) 173, 169;  672 (a 60M model's 28, eight of
+        // them 512 x 1376, four 1376 x 512) 230, 239;  800 (five of 1024) 197, 198;  1152 (one 2048) 270, 297.
+        // The same count in tiles of 128 x 128, these against 256 x 128:  80 (one 512 x 512) 94, 108;  576 (one 1024) 137,
+        // 151;  640 (eight of 512) 109, 116;  960 (twelve of 512) 125, 123;  1100 (one 1280) 189, 174;  1872 (one 1536) 294, 199.
+        // (fp32, three times the k-blocks, changes sides at the same counts: 480: 365, 321;  640: 459, 429;  1152: 701, 762;  and
+        // 576: 309, 354;  640: 226, 243;  960: 279, 262.  Long sides, which the counts leave out, change them earlier: two
+        // of 1024 x 4096, 320: 276, 283;  one of them, 576 small: 278, 252.)
         int64_t wide = 0, small = 0;
         for (int i : g.mats) {
             const int m = plan.mats[i].m;

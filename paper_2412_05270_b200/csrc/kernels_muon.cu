@@ -98,7 +98,7 @@ __device__ __forceinline__ void load_term(uint4 (&e)[4], const __half* p, bool i
 // that is not: no CTA has to be resident for another to finish.  With several matrices the products before are
 // complete by the time a tile comes up, and there is neither a launch nor a drained pipeline between products.
 // (Dealing the tiles out by index instead let the pairs drift apart where long and short contractions meet; what
-// neighbours share then no longer met in L2: a 7B layer took 12.9 ms instead of 11.6 ms, at equal cycles.)
+// neighbours share then no longer met in L2: a 7B layer took 11 % more time, at equal cycles.)
 //
 // Roles that keep latency off the loads and the epilogue:
 //   the peer's warp 1  (the leader's issues the MMAs) draws: when its producer begins with a tile, the ticket of the next
