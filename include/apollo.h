@@ -462,6 +462,111 @@ APOLLO_API int apollo_token_logprobs_grad(const void* d_logits, int64_t row_stri
                                           const float* d_grad_entropy, void* d_grad_logits, int64_t grad_stride,
                                           void* cuda_stream);
 
+/*
+ * Global norm of a list of gradients and the factor that clips it (stateless, asynchronous on `cuda_stream`):
+ *   norm = sqrt(sum_i sum_e G_i[e]^2),   factor = min(1, max_norm / norm)   (1 for norm = 0; NaN where the norm is not finite).
+ * d_G: HOST array of n_tensors DEVICE pointers (16-byte aligned, contiguous; a null entry is left out); numel, dtype: HOST,
+ * per tensor.  max_norm > 0 (may be infinite: the norm alone).  d_out: DEVICE, two floats {norm, factor}.  Entries of any size:
+ * squares that leave the range of fp32 are summed in fp64.  The order of the sum is fixed by the list and the number of
+ * multiprocessors: equal bits in every run.  d_workspace: DEVICE, 16-byte aligned, keeps nothing between calls.
+ */
+APOLLO_API int apollo_grad_norm_workspace_bytes(int32_t n_tensors, size_t* out_bytes);
+APOLLO_API int apollo_grad_norm(const void* const* d_G, const int64_t* numel, const int32_t* dtype, int32_t n_tensors,
+                                double max_norm, float* d_out, void* d_workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * AdamW over a list of tensors of mixed types at once, with moments of 8 or 32 bits in one DEVICE buffer of the caller's
+ * (apollo_adamw_step: fp32 moments per tensor, one dtype).  With g = factor G:
+ *   m <- b1 m + (1-b1) g,  v <- b2 v + (1-b2) g^2,  P <- P - lr ((m / c1) / (sqrt(v / c2) + eps) + wd P),  c_i = 1 - b_i^(t+1)
+ * (c_i = 1 with bias_correction = 0).  The update is formed from m and v before they are rounded to 8 bits.
+ *
+ * The state: every tensor takes ceil(numel / 256) blocks of 256 elements, in list order, B blocks in all.
+ *   32 bits:  m (256 B floats), v (256 B floats).
+ *    8 bits:  codes of m (256 B bytes), codes of v (256 B bytes), then per block two bytes: the exponents k of m and of v.
+ *             v: code c is (1 + (c % 8) / 8) 2^(k + c / 8 - 127): 32 binades of 8 steps below the block's largest; c = 0 is
+ *                the smallest of them, not zero, once k > 0, so that no v of a block in use vanishes below its m.
+ *             m: the top bit is the sign, c the lower 7: zero for c = 0, else the same: 16 binades of 8 steps.
+ *             (k + c / 8 = 0: (c % 8) / 8 2^-126.)
+ * All bytes zero is the state before the first step.  Codes are rounded stochastically: a value between two neighbours becomes
+ * the upper one with the probability of its place between them, in steps of 2^-16 (v moves by a thousandth of itself a step,
+ * the codes are 6 to 12 % apart: rounded to nearest it would never move).  The 16 random bits of element e of a block are
+ * halfword e % 8 of Philox4x32-10 with key `seed` and counter (block, (e % 256) / 8, t, t >> 32), the same for m and v: equal
+ * inputs, seed and t give equal bits, on any stream and in any run.  The padding behind a tensor's last element holds zeros
+ * (32 bits) or what elements of zero become.  An infinite or NaN gradient makes m and v of its element so, and spoils the
+ * moments of its block of 256 in 8 bits.
+ *
+ * d_P, d_G: HOST arrays of n_tensors DEVICE pointers (16-byte aligned, contiguous), numel, dtype_P, dtype_G: HOST, per tensor
+ * (APOLLO_DT_*, any combination).  A null d_G entry leaves its tensor and its moments alone.  Tensors must not overlap.
+ * d_state: DEVICE, 16-byte aligned, apollo_adamw_list_state_bytes().  t: steps already taken.  Optional DEVICE scalars, read when
+ * the step runs: d_factor (one float, as apollo_grad_norm leaves it in d_out[1]; a factor that is not finite: the step writes nothing), d_lr
+ * (one float) in the place of lr, d_t (one int64) in the place of t: what a captured step needs.  Asynchronous on `cuda_stream`.
+ */
+#define APOLLO_ADAMW_BLOCK 256
+typedef struct {
+    int32_t state_bits;          /* 8 or 32 */
+    int32_t bias_correction;     /* 0 or 1 */
+    double beta1, beta2, eps;    /* 0.9, 0.999, 1e-8 */
+    uint64_t seed;               /* Philox key of the rounding (8 bits) */
+} apollo_adamw_list_config;
+APOLLO_API int apollo_adamw_list_state_bytes(const int64_t* numel, int32_t n_tensors, int32_t state_bits, size_t* out_bytes);
+APOLLO_API int apollo_adamw_list_step(const apollo_adamw_list_config* cfg, void* const* d_P, const void* const* d_G,
+                                      const int64_t* numel, const int32_t* dtype_P, const int32_t* dtype_G, int32_t n_tensors,
+                                      void* d_state, size_t state_bytes, double lr, double wd, int64_t t, const float* d_factor,
+                                      const float* d_lr, const int64_t* d_t, void* cuda_stream);
+/* The values that an 8-bit state of n_blocks blocks stands for: d_M, d_V: DEVICE, 256 n_blocks bfloat16 each (exact), 16-byte
+ * aligned. */
+APOLLO_API int apollo_adamw_list_moments(const void* d_state, size_t state_bytes, int64_t n_blocks, void* d_M, void* d_V,
+                                         void* cuda_stream);
+
+/*
+ * Logits adjusted before a token is drawn or its log probability taken, and the gradient (stateless, asynchronous on
+ * `cuda_stream`).  Per row, with c_j how often word j occurs in the row's history and d_j how often from position `start` on:
+ *   x = logit_j;
+ *   c_j > 0:  x <- x > 0 ? x / repetition : x repetition;      d_j > 0:  x <- x - (frequency d_j + presence);
+ *   x <- x + bias_j;    x <- x + (sum of the values whose word is j);    bit j of the mask is 0:  x <- -inf.
+ * fp32, rounded once to the logits' type.  The gradient, a_j = dout_j where the mask allows j, else 0:
+ *   dlogit_j = a_j (c_j = 0: 1;  logit_j > 0: 1 / repetition;  else repetition),
+ *   dbias_j = a_j (summed over the rows in fp32, in a fixed order, for a shared bias),   dvalue_i = a_j of its word j.
+ * logits, out, dout, dlogits: DEVICE, n_rows rows of `vocab` elements of `dtype`, rows >= vocab elements apart.  out may be the
+ * logits, dlogits may be dout (same stride): then only the words that change are written, and read only where they must be.
+ * Pointers need the alignment of their elements; rows that are whole 16-byte vectors are faster.
+ */
+typedef struct {
+    const void* d_history;        /* DEVICE, history_rows x history_len tokens, or null: no penalties.  Row r of the logits
+                                     takes history row r / (n_rows / history_rows); tokens outside [0, vocab) count nowhere */
+    int32_t history_type;         /* APOLLO_INDEX_* */
+    int32_t bias_word_type;       /* APOLLO_INDEX_* of d_bias_word */
+    int64_t history_rows;         /* divides n_rows */
+    int64_t history_len;          /* at most APOLLO_MAX_HISTORY */
+    int64_t history_stride;       /* elements between rows; 0: one row for all */
+    const int32_t* d_length;      /* DEVICE, n_rows: how many tokens of its history a row has (cut to [0, history_len]); null: all */
+    const int32_t* d_start;       /* DEVICE, n_rows: first position that counts for frequency and presence; null: 0 */
+    const float* d_repetition;    /* DEVICE, n_rows, > 0, or null: `repetition` for every row; likewise the next two */
+    const float* d_frequency;
+    const float* d_presence;
+    float repetition, frequency, presence;   /* > 0; finite (1, 0, 0: no penalty) */
+    const void* d_bias;           /* DEVICE, vocab (bias_stride 0: shared by the rows) or n_rows x vocab of `dtype`, or null */
+    int64_t bias_stride;
+    const void* d_bias_word;      /* DEVICE, n_rows x n_bias words, contiguous (outside [0, vocab): none; one may be named twice), or null */
+    const float* d_bias_value;    /* DEVICE, n_rows x n_bias (the gradient does not read it) */
+    int64_t n_bias;               /* at most APOLLO_MAX_BIAS_WORDS */
+    const uint32_t* d_mask;       /* DEVICE, bit j % 32 of word j / 32 set: word j is allowed; or null: all are */
+    int64_t mask_stride;          /* 32-bit words between rows (0: one mask for all), else >= ceil(vocab / 32) */
+} apollo_logit_rules;
+#define APOLLO_MAX_HISTORY ((1 << 20) - 1)
+#define APOLLO_MAX_BIAS_WORDS 1024
+APOLLO_API int apollo_adjust_logits(const void* d_logits, int64_t row_stride, int64_t n_rows, int64_t vocab, int32_t dtype,
+                                    const apollo_logit_rules* rules, void* d_out, int64_t out_stride, void* cuda_stream);
+/* d_grad_bias: DEVICE, `dtype`: n_rows rows grad_bias_stride apart, or with grad_bias_stride = 0 one row, the sum; or null.
+ * d_grad_value: DEVICE, n_rows x n_bias floats, or null.  Of the rules it reads history, lengths, repetition, mask and words.  The shared
+ * bias' gradient needs a DEVICE workspace (16-byte aligned) of apollo_adjust_logits_grad_workspace_bytes(); it keeps nothing there. */
+APOLLO_API int apollo_adjust_logits_grad_workspace_bytes(int64_t n_rows, int64_t vocab, size_t* out_bytes);
+APOLLO_API int apollo_adjust_logits_grad(const void* d_logits, int64_t row_stride, int64_t n_rows, int64_t vocab, int32_t dtype,
+                                         const apollo_logit_rules* rules, const void* d_grad_out, int64_t grad_out_stride,
+                                         void* d_grad_logits, int64_t grad_logits_stride, void* d_grad_bias,
+                                         int64_t grad_bias_stride, float* d_grad_value, void* d_workspace,
+                                         size_t workspace_bytes, void* cuda_stream);
+
 /* Self-test of the error path (the paper has no counterpart).  Every wait inside the tensor-core
  * kernel is bounded: after 2^20 polls it gives up, sets the context's device status word and the
  * kernel winds down instead of hanging.  This call launches, on the stream, a one-block kernel whose

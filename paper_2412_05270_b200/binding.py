@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import math
 from pathlib import Path
 from typing import NamedTuple
 
@@ -36,6 +37,9 @@ MUON_MAX_STEPS = 32
 MUON_PRODUCTS_DEFAULT, MUON_PRODUCTS_PAIRS = 0, 1
 INDEX_I32, INDEX_I64 = 0, 1
 MAX_TOP = 32
+ADAMW_BLOCK = 256
+MAX_HISTORY = (1 << 20) - 1
+MAX_BIAS_WORDS = 1024
 
 EXPORTS = [
     "apollo_workspace_bytes", "apollo_create", "apollo_step", "apollo_destroy", "apollo_step_count",
@@ -47,6 +51,8 @@ EXPORTS = [
     "apollo_muon_workspace_bytes", "apollo_muon_create", "apollo_muon_destroy", "apollo_muon_step", "apollo_muon_orthogonalize",
     "apollo_muon_status", "apollo_muon_last_launches", "apollo_embedding", "apollo_embedding_grad_workspace_bytes",
     "apollo_embedding_grad", "apollo_token_logprobs", "apollo_token_logprobs_grad",
+    "apollo_grad_norm_workspace_bytes", "apollo_grad_norm", "apollo_adamw_list_state_bytes", "apollo_adamw_list_step",
+    "apollo_adamw_list_moments", "apollo_adjust_logits", "apollo_adjust_logits_grad_workspace_bytes", "apollo_adjust_logits_grad",
 ]
 
 
@@ -76,6 +82,24 @@ class MuonConfig(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("ns_steps", ctypes.c_int32), ("coef", ctypes.c_float * 3),
                 ("momentum", ctypes.c_float), ("nesterov", ctypes.c_int32), ("scale", ctypes.c_int32),
                 ("eps", ctypes.c_float), ("workspace_mb", ctypes.c_int32), ("products", ctypes.c_int32)]
+
+
+class AdamWListConfig(ctypes.Structure):
+    """apollo_adamw_list_config."""
+    _fields_ = [("state_bits", ctypes.c_int32), ("bias_correction", ctypes.c_int32), ("beta1", ctypes.c_double),
+                ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("seed", ctypes.c_uint64)]
+
+
+class LogitRules(ctypes.Structure):
+    """apollo_logit_rules."""
+    _fields_ = [("history", ctypes.c_void_p), ("history_type", ctypes.c_int32), ("bias_word_type", ctypes.c_int32),
+                ("history_rows", ctypes.c_int64), ("history_len", ctypes.c_int64), ("history_stride", ctypes.c_int64),
+                ("length", ctypes.c_void_p), ("start", ctypes.c_void_p),
+                ("repetition_at", ctypes.c_void_p), ("frequency_at", ctypes.c_void_p), ("presence_at", ctypes.c_void_p),
+                ("repetition", ctypes.c_float), ("frequency", ctypes.c_float), ("presence", ctypes.c_float),
+                ("bias", ctypes.c_void_p), ("bias_stride", ctypes.c_int64),
+                ("bias_word", ctypes.c_void_p), ("bias_value", ctypes.c_void_p), ("n_bias", ctypes.c_int64),
+                ("mask", ctypes.c_void_p), ("mask_stride", ctypes.c_int64)]
 
 
 class Tuning(ctypes.Structure):
@@ -171,6 +195,15 @@ def _load_from(path: Path):
     lib.apollo_embedding_grad.argtypes = [vp, i64, vp, i32, i64, i64, i64, i32, f32, i32, vp, vp, ctypes.c_size_t, vp]
     lib.apollo_token_logprobs.argtypes = [vp, i64, i64, i64, i32, vp, i32, f32, i32, vp, vp, vp, vp, vp, vp]
     lib.apollo_token_logprobs_grad.argtypes = [vp, i64, i64, i64, i32, vp, i32, f32, vp, vp, vp, vp, vp, i64, vp]
+    f64, size_p = ctypes.c_double, ctypes.POINTER(ctypes.c_size_t)
+    lib.apollo_grad_norm_workspace_bytes.argtypes = [i32, size_p]
+    lib.apollo_grad_norm.argtypes = [vp, vp, vp, i32, f64, vp, vp, ctypes.c_size_t, vp]
+    lib.apollo_adamw_list_state_bytes.argtypes = [vp, i32, i32, size_p]
+    lib.apollo_adamw_list_step.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, ctypes.c_size_t, f64, f64, i64, vp, vp, vp, vp]
+    lib.apollo_adamw_list_moments.argtypes = [vp, ctypes.c_size_t, i64, vp, vp, vp]
+    lib.apollo_adjust_logits.argtypes = [vp, i64, i64, i64, i32, vp, vp, i64, vp]
+    lib.apollo_adjust_logits_grad_workspace_bytes.argtypes = [i64, i64, size_p]
+    lib.apollo_adjust_logits_grad.argtypes = [vp, i64, i64, i64, i32, vp, vp, i64, vp, i64, vp, i64, vp, vp, ctypes.c_size_t, vp]
     lib.apollo_cuda_error_string.argtypes = []
     lib.apollo_cuda_error_string.restype = ctypes.c_char_p
     for name in EXPORTS:
@@ -458,6 +491,312 @@ def token_logprobs_grad(logits, targets, lse, entropy, d_logprob, d_entropy=None
             None if d_entropy is None else d_entropy.data_ptr(), out.data_ptr(), _rows_of(out, "out"), _stream_ptr(stream)),
             "apollo_token_logprobs_grad")
     return out
+
+
+class _List:
+    """A list of gradients as the library takes it: addresses, lengths and types, and the device that they are on."""
+
+    def __init__(self, tensors, what: str, device=None):
+        live = [x for x in tensors if x is not None]
+        dtypes = {x.dtype for x in live}
+        if not dtypes <= {torch.bfloat16, torch.float32}:
+            raise ValueError(f"{what} must be bfloat16 or float32, got {dtypes}")
+        if not all([x.is_cuda and x.is_contiguous() for x in live]):
+            raise ValueError(f"{what} must be contiguous CUDA tensors")
+        devices = {x.get_device() for x in live}
+        if len(devices) > 1 or (device is not None and devices and devices != {device.index}):
+            raise _two_devices()
+        self.n = n = len(tensors)
+        self.device = device if device is not None else live[0].device if live else None
+        bf16 = torch.bfloat16
+        if len(live) == n:
+            self.pointers = (ctypes.c_uint64 * n)(*[x.data_ptr() for x in live])
+            self.dtypes = (ctypes.c_int32 * n)(*[x.dtype is bf16 for x in live])
+        else:
+            self.pointers = (ctypes.c_uint64 * n)(*[0 if x is None else x.data_ptr() for x in tensors])
+            self.dtypes = (ctypes.c_int32 * n)(*[x is not None and x.dtype is bf16 for x in tensors])
+
+
+def grad_norm(grads, max_norm: float = math.inf, out=None, workspace=None, stream=None) -> torch.Tensor:
+    """apollo_grad_norm: two floats on the device, the global norm of the list and min(1, max_norm / norm).
+
+    grads: contiguous CUDA tensors, bfloat16 or float32 in any mixture, None for one that is left out; workspace: a uint8 CUDA
+    tensor of grad_norm_workspace_bytes(), made if None."""
+    grads = list(grads)
+    xs = _List(grads, "grads")
+    device = xs.device
+    if device is None:
+        raise ValueError("grad_norm needs a gradient")
+    for x, what in ((out, "out"), (workspace, "workspace")):
+        if x is not None:
+            if x.device != device:
+                raise _two_devices()
+            if not x.is_contiguous():
+                raise ValueError(f"{what} must be contiguous")
+    if out is not None and (out.dtype != torch.float32 or out.numel() != 2):
+        raise ValueError("out must hold two float32 values")
+    numel = (ctypes.c_int64 * xs.n)(*[0 if x is None else x.numel() for x in grads])
+    with _on(stream, device):
+        if out is None:
+            out = torch.empty_strided((2,), (1,), dtype=torch.float32, device=device)
+        if workspace is None:
+            workspace = torch.empty_strided((grad_norm_workspace_bytes(xs.n),), (1,), dtype=torch.uint8, device=device)
+        _check(load().apollo_grad_norm(xs.pointers, numel, xs.dtypes, xs.n, max_norm, out.data_ptr(), workspace.data_ptr(),
+                                       workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "apollo_grad_norm")
+    return out
+
+
+def grad_norm_workspace_bytes(n_tensors: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().apollo_grad_norm_workspace_bytes(n_tensors, ctypes.byref(out)), "apollo_grad_norm_workspace_bytes")
+    return out.value
+
+
+def adamw_state_bytes(numels, bits: int = 8) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().apollo_adamw_list_state_bytes((ctypes.c_int64 * len(numels))(*numels), len(numels), bits, ctypes.byref(out)),
+           "apollo_adamw_list_state_bytes")
+    return out.value
+
+
+class AdamW:
+    """apollo_adamw_list_step over a list of parameters (contiguous CUDA tensors on one device, bfloat16 or float32 in any
+    mixture, none of them twice), with the moments of all of them in one buffer, `state`: of 8 or 32 bits, zero before the first step.
+
+    state: a uint8 CUDA tensor of adamw_state_bytes() to go on with (a checkpoint is a copy of it, with the step count and the
+    seed), made if None.  Calls run on `stream` or the device's current one, whichever device is current."""
+
+    def __init__(self, params, bits: int = 8, beta1=0.9, beta2=0.999, eps=1e-8, seed: int = 0, bias_correction: bool = True,
+                 state=None):
+        self.lib = load()
+        self.params = list(params)
+        if not self.params or any(p is None for p in self.params):
+            raise ValueError("AdamW needs a list of parameters")
+        xs = _List(self.params, "params")
+        if len({a for a, p in zip(xs.pointers, self.params) if p.numel()}) < sum(p.numel() > 0 for p in self.params):
+            raise ValueError("a parameter is in the list twice")
+        self.device, self.bits = xs.device, bits
+        self._shapes = [p.shape for p in self.params]
+        numels = [p.numel() for p in self.params]
+        self._numel = (ctypes.c_int64 * xs.n)(*numels)
+        self.cfg = AdamWListConfig(int(bits), int(bool(bias_correction)), float(beta1), float(beta2), float(eps), int(seed))
+        nbytes = adamw_state_bytes(numels, bits)
+        self.n_blocks = nbytes // (2 * ADAMW_BLOCK + 2 if bits == 8 else 8 * ADAMW_BLOCK)
+        with _on(None, self.device):
+            if state is None:
+                state = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+            elif state.dtype != torch.uint8 or state.numel() != nbytes or not state.is_contiguous():
+                raise ValueError(f"state must be a contiguous uint8 CUDA tensor of {nbytes} bytes")
+            elif state.device != self.device:
+                raise _two_devices()
+            self._home = _stream_ptr(None)                   # the stream that the state belongs to
+        self.state = state
+
+    def _run(self, stream) -> int:
+        ptr = _stream_ptr(stream)
+        if ptr != self._home:
+            # freed, the state must not be handed out again before this stream is done with it
+            self.state.record_stream(torch.cuda.current_stream())
+        return ptr
+
+    def _scalar(self, x, dtype, what):
+        if x.dtype != dtype or x.numel() != 1:
+            raise ValueError(f"{what} must be one value of {dtype}")
+        if x.device != self.device:
+            raise _two_devices()
+        return x.data_ptr()
+
+    def step(self, grads, lr, t, wd: float = 0.0, factor=None, stream=None):
+        """One step from the gradients (None: that parameter and its moments stay as they are), after t earlier ones.
+
+        lr: a number, or a float32 CUDA tensor of one value; t: a number, or an int64 CUDA tensor of one value (read when the step
+        runs: a captured step can be replayed with other values); factor: a float32 CUDA tensor of one value that the gradients are multiplied by
+        (grad_norm(...)[1:]); where it is not finite the step changes nothing."""
+        grads = list(grads)
+        params = _List(self.params, "params", self.device)
+        if len(grads) != params.n:
+            raise ValueError("parameter list length differs from the context's")
+        xs = _List(grads, "grads", self.device)
+        if [p.shape for p in self.params] != self._shapes or not all([g is None or g.shape == s for g, s in zip(grads, self._shapes)]):
+            raise ValueError("gradients must have their parameters' shapes")
+        lr_at = t_at = factor_at = None
+        if isinstance(lr, torch.Tensor):
+            lr, lr_at = 0.0, self._scalar(lr, torch.float32, "lr")
+        if isinstance(t, torch.Tensor):
+            t, t_at = 0, self._scalar(t, torch.int64, "t")
+        if factor is not None:
+            factor_at = self._scalar(factor, torch.float32, "factor")
+        with _on(stream, self.device):
+            _check(self.lib.apollo_adamw_list_step(ctypes.byref(self.cfg), params.pointers, xs.pointers, self._numel, params.dtypes,
+                                                   xs.dtypes, xs.n, self.state.data_ptr(), self.state.numel(), lr, wd, t, factor_at,
+                                                   lr_at, t_at, self._run(stream)), "apollo_adamw_list_step")
+
+    def moments(self, stream=None):
+        """(m, v) of all blocks in list order, ADAMW_BLOCK n_blocks values each: what 8-bit codes stand for, exactly, in bfloat16; of
+        32 bits the state itself, not a copy."""
+        if self.bits == 32:
+            return self.state.view(torch.float32).chunk(2)
+        with _on(stream, self.device):
+            m, v = (torch.empty(self.n_blocks * ADAMW_BLOCK, dtype=torch.bfloat16, device=self.device) for _ in range(2))
+            _check(self.lib.apollo_adamw_list_moments(self.state.data_ptr(), self.state.numel(), self.n_blocks, m.data_ptr(),
+                                                      v.data_ptr(), self._run(stream)), "apollo_adamw_list_moments")
+        return m, v
+
+
+def _rules_of(logits, device, history, lengths, start, repetition, frequency, presence, bias, bias_index, bias_value, mask):
+    """The rules as the library takes them, and the tensors that they point into."""
+    n, vocab = logits.shape
+    r = LogitRules(repetition=1.0)
+    kept = []
+
+    def here(x, what, dtype, shape):
+        if x.dtype != dtype or tuple(x.shape) != shape:
+            raise ValueError(f"{what} must be {dtype} of shape {shape}")
+        if x.device != device:
+            raise _two_devices()
+        if not x.is_contiguous():
+            x = x.contiguous()
+            kept.append(x)
+        return x
+    if history is not None:
+        r.history_type = _index_of(history, "history")
+        if history.dim() != 2 or (n and (history.shape[0] < 1 or n % history.shape[0])):
+            raise ValueError("history must have a row for each row of logits, or for the same number of them each")
+        if history.device != device:
+            raise _two_devices()
+        rows, length = history.shape
+        stride = history.stride(0) if rows > 1 else 0
+        if (length > 1 and history.stride(1) != 1) or 0 < stride < length:
+            history = history.contiguous()
+            kept.append(history)
+            stride = length if rows > 1 else 0
+        r.history, r.history_rows, r.history_len, r.history_stride = history.data_ptr() if history.numel() else None, max(rows, 1), length, stride
+        for x, at in ((lengths, "length"), (start, "start")):
+            if x is not None:
+                setattr(r, at, here(x, at, torch.int32, (n,)).data_ptr())
+        for x, at in ((repetition, "repetition"), (frequency, "frequency"), (presence, "presence")):
+            if isinstance(x, torch.Tensor):
+                setattr(r, at + "_at", here(x, at, torch.float32, (n,)).data_ptr())
+            else:
+                setattr(r, at, x)
+    if bias is not None:
+        if bias.dtype != logits.dtype or tuple(bias.shape) not in ((vocab,), (n, vocab)):
+            raise ValueError("bias must have the logits' dtype and be a row of the vocabulary, or one for each row of logits")
+        if bias.device != device:
+            raise _two_devices()
+        if bias.dim() == 2 and n > 1 and bias.stride(0) >= vocab and (vocab == 1 or bias.stride(1) == 1):
+            r.bias_stride = bias.stride(0)
+        elif not bias.is_contiguous():
+            bias = bias.contiguous()
+            kept.append(bias)
+            r.bias_stride = vocab if bias.dim() == 2 else 0
+        elif bias.dim() == 2:
+            r.bias_stride = vocab
+        r.bias = bias.data_ptr()
+    if bias_index is not None:
+        r.bias_word_type = _index_of(bias_index, "bias_index")
+        if bias_index.dim() != 2 or bias_index.shape[0] != n:
+            raise ValueError("bias_index must have a row for each row of logits")
+        r.n_bias = bias_index.shape[1]
+        r.bias_word = here(bias_index, "bias_index", bias_index.dtype, tuple(bias_index.shape)).data_ptr()
+        if bias_value is not None:
+            r.bias_value = here(bias_value, "bias_value", torch.float32, tuple(bias_index.shape)).data_ptr()
+    elif bias_value is not None:
+        raise ValueError("bias_value needs bias_index")
+    if mask is not None:
+        words = (vocab + 31) // 32
+        if mask.dtype != torch.int32 or tuple(mask.shape) not in ((words,), (1, words), (n, words)):
+            raise ValueError(f"mask must be int32 with {words} words of 32 bits a row, one row or one for each row of logits")
+        if mask.device != device:
+            raise _two_devices()
+        if not mask.is_contiguous():
+            mask = mask.contiguous()
+            kept.append(mask)
+        r.mask, r.mask_stride = mask.data_ptr(), words if mask.dim() == 2 and mask.shape[0] > 1 else 0
+    return r, kept
+
+
+def adjust_logits(logits, history=None, lengths=None, start=None, repetition=1.0, frequency=0.0, presence=0.0, bias=None,
+                  bias_index=None, bias_value=None, mask=None, out=None, stream=None) -> torch.Tensor:
+    """apollo_adjust_logits over the rows of `logits` (n, vocab); out: made if None, may be the logits.
+
+    history: (h, length) tokens, int32 or int64 (outside [0, vocab): none), h a divisor of n: row r of the logits has history row
+    r // (n / h), of which the first lengths[r] (int32) count, for frequency and presence those from start[r] (int32) on; repetition,
+    frequency, presence: numbers, or float32 (n,);  bias: (vocab,) or (n, vocab) of the logits' dtype;  bias_index, bias_value: (n, k)
+    words and float32 values;  mask: int32 words of 32 bits, (1 or n, ceil(vocab / 32)), bit set = word allowed."""
+    dtype = _dtype_of(logits, "logits")
+    stride = _rows_of(logits, "logits")
+    n, vocab = logits.shape
+    device = logits.device
+    if out is not None:
+        if out.dtype != logits.dtype or out.shape != logits.shape:
+            raise ValueError("out must have the logits' dtype and shape")
+        if out.device != device:
+            raise _two_devices()
+    if bias_index is not None and bias_value is None:
+        raise ValueError("bias_index needs bias_value")
+    with _on(stream, device):
+        rules, kept = _rules_of(logits, device, history, lengths, start, repetition, frequency, presence, bias, bias_index, bias_value, mask)
+        if out is None:
+            out = torch.empty_strided((n, vocab), (vocab, 1), dtype=logits.dtype, device=device)
+        _check(load().apollo_adjust_logits(logits.data_ptr(), stride, n, vocab, dtype, ctypes.byref(rules), out.data_ptr(),
+                                           _rows_of(out, "out"), _stream_ptr(stream)), "apollo_adjust_logits")
+    return out
+
+
+def adjust_logits_grad_workspace_bytes(n_rows: int, vocab: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().apollo_adjust_logits_grad_workspace_bytes(n_rows, vocab, ctypes.byref(out)), "apollo_adjust_logits_grad_workspace_bytes")
+    return out.value
+
+
+class AdjustLogitsGrad(NamedTuple):
+    logits: torch.Tensor
+    bias: torch.Tensor | None
+    value: torch.Tensor | None
+
+
+def adjust_logits_grad(logits, d_out, history=None, lengths=None, repetition=1.0, mask=None, bias: str = "none", bias_index=None,
+                       out=None, workspace=None, stream=None) -> AdjustLogitsGrad:
+    """apollo_adjust_logits_grad: the gradients of `adjust_logits` for its logits, a bias ("shared": (vocab,), "row": (n, vocab), "none")
+    and, where bias_index is given, the values; rules as there.  out: of the logits' gradient, made if None, may be d_out;
+    workspace ("shared"): a uint8 CUDA tensor of adjust_logits_grad_workspace_bytes(), made if None."""
+    dtype = _dtype_of(logits, "logits")
+    stride, d_stride = _rows_of(logits, "logits"), _rows_of(d_out, "d_out")
+    n, vocab = logits.shape
+    device = logits.device
+    if bias not in ("none", "shared", "row"):
+        raise ValueError('bias must be "none", "shared" or "row"')
+    for x, what in ((d_out, "d_out"), (out, "out")):
+        if x is not None:
+            if x.dtype != logits.dtype or x.shape != logits.shape:
+                raise ValueError(f"{what} must have the logits' dtype and shape")
+            if x.device != device:
+                raise _two_devices()
+    if workspace is not None:
+        if workspace.device != device:
+            raise _two_devices()
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+    with _on(stream, device):
+        rules, kept = _rules_of(logits, device, history, lengths, None, repetition, 0.0, 0.0, None, bias_index, None, mask)
+        if out is None:
+            out = torch.empty_strided((n, vocab), (vocab, 1), dtype=logits.dtype, device=device)
+        d_bias = d_value = None
+        if bias == "shared":
+            d_bias = torch.empty_strided((vocab,), (1,), dtype=logits.dtype, device=device)
+            if workspace is None:
+                workspace = torch.empty_strided((adjust_logits_grad_workspace_bytes(n, vocab),), (1,), dtype=torch.uint8, device=device)
+        elif bias == "row":
+            d_bias = torch.empty_strided((n, vocab), (vocab, 1), dtype=logits.dtype, device=device)
+        if bias_index is not None:
+            d_value = torch.empty(tuple(bias_index.shape), dtype=torch.float32, device=device)
+        _check(load().apollo_adjust_logits_grad(
+            logits.data_ptr(), stride, n, vocab, dtype, ctypes.byref(rules), d_out.data_ptr(), d_stride, out.data_ptr(), _rows_of(out, "out"),
+            None if d_bias is None else d_bias.data_ptr(), vocab if bias == "row" else 0, None if d_value is None else d_value.data_ptr(),
+            None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+            _stream_ptr(stream)), "apollo_adjust_logits_grad")
+    return AdjustLogitsGrad(out, d_bias, d_value)
 
 
 def make_muon_config(dtype=DT_BF16, steps=5, coef=(3.4445, -4.7750, 2.0315), momentum=0.95, nesterov=True,

@@ -10,7 +10,8 @@ CSRC = PKG / "csrc"
 LIB = PKG / "libapollo.so"
 LIB_DEBUG = PKG / "libapollo_debug.so"      # the same sources with -DAPOLLO_DEBUG: index checks inside the kernels
 SOURCES = ["apollo_api.cu", "kernels_basic.cu", "kernels_tensor.cu", "apollo_static.cu", "kernels_adamw.cu",
-           "apollo_muon.cu", "kernels_muon.cu", "kernels_embedding.cu", "kernels_logprob.cu"]
+           "apollo_muon.cu", "kernels_muon.cu", "kernels_embedding.cu", "kernels_logprob.cu", "kernels_adamw_list.cu",
+           "kernels_adjust.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
