@@ -32,7 +32,8 @@ namespace {
 constexpr int AL_BLOCK = APOLLO_ADAMW_BLOCK;
 constexpr int AL_THREADS = 256;
 constexpr int AL_WARPS = AL_THREADS / 32;
-constexpr int AL_TILE = 32;              // blocks of one tile: four for each warp
+constexpr int AL_TILE32 = 4096;          // elements of one tile, 32 bits
+constexpr int AL_WAVES = 16;             // 8 bits: how many times the blocks that are resident at once, at most
 constexpr int AL_FEW = 48, AL_MANY = 960;   // tensors whose pointers travel as parameters of one launch (CUDA: 32,764 bytes)
 
 __device__ __forceinline__ void store8(float* p, const float (&v)[8])
@@ -164,6 +165,10 @@ grad_norm_join_kernel(const double* __restrict__ partial, int n, double max_norm
 }
 
 // ---------------------------------------------------------------- step
+// What every element of a step needs.  The corrections are folded in: with r = sqrt(inv_c2),
+//   lr (inv_c1 m / (sqrt(inv_c2 v) + eps) + wd P) = rate (m / (sqrt(v) + eps / r) + decay P),  rate = lr inv_c1 / r,  decay = wd r / inv_c1.
+struct Scalars { float rate, decay, eps, factor; uint32_t t_lo, t_hi; };
+
 template <int CAP>
 struct ListArgs {
     void* p[CAP];
@@ -175,18 +180,123 @@ struct ListArgs {
     char* m;                             // 8 bits: codes; 32 bits: floats
     char* v;
     uint16_t* k;                         // 8 bits: m's exponent, v's exponent << 8
+    int whole_grid;                      // 8 bits: blocks of threads for whole tiles; the tensors' ends have the others
     const float* factor;
     const float* lr_at;
     const long long* t_at;
-    float lr, wd, eps, b1, a1, b2, a2;   // a = 1 - b
-    float inv_c1, inv_c2;
+    float b1, a1, b2, root_a2;           // a = 1 - b
+    double lr, wd, eps, inv_c1, root;    // root = sqrt(inv_c2)
     double log_b1, log_b2;               // for the step count on the device
     int bias_correction;
+    int fast;                            // eps is large enough for FAST roots
     unsigned long long t;
+    Scalars scalars;
     uint32_t keys[20];
 };
 
-struct Scalars { float lr, factor, inv_c1, inv_c2; uint32_t t_lo, t_hi; };
+__host__ __device__ inline Scalars scalars_of(double lr, double wd, double eps, double inv_c1, double root, unsigned long long t)
+{
+    Scalars s;
+    s.rate = (float)(lr * inv_c1 / root);
+    s.decay = (float)(wd * root / inv_c1);
+    s.eps = (float)(eps / root);
+    s.factor = 1.0f;
+    s.t_lo = (uint32_t)t; s.t_hi = (uint32_t)(t >> 32);
+    return s;
+}
+
+// By one thread of a block; the host's unless lr or the step count is on the device.
+template <int CAP>
+__device__ __forceinline__ Scalars read_scalars(const ListArgs<CAP>& a)
+{
+    Scalars s = a.scalars;
+    if (a.lr_at || a.t_at) {
+        const double lr = a.lr_at ? *a.lr_at : a.lr;
+        double inv_c1 = a.inv_c1, root = a.root;
+        unsigned long long t = a.t;
+        if (a.t_at) {
+            t = (unsigned long long)*a.t_at;
+            if (a.bias_correction) {
+                inv_c1 = -1.0 / expm1((double)(t + 1) * a.log_b1);
+                root = sqrt(-1.0 / expm1((double)(t + 1) * a.log_b2));
+            }
+        }
+        s = scalars_of(lr, a.wd, a.eps, inv_c1, root, t);
+    }
+    if (a.factor) s.factor = *a.factor;
+    return s;
+}
+
+// Pairs of floats in one 64-bit register: one instruction for two elements.
+__device__ __forceinline__ uint64_t pair2(float lo, float hi)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// On the special-function unit, relative errors about 2^-23.  FAST flushes what is below the normal range: a root that is off by
+// 1.1e-19 at most, beside an eps of 1e-12 or more nothing; a smaller eps takes the other form (three instructions more each).
+template <bool FAST>
+__device__ __forceinline__ float root_of(float x)
+{
+    float y;
+    if constexpr (FAST) asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    else asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+template <bool FAST>
+__device__ __forceinline__ float inverse_of(float x)
+{
+    float y;
+    if constexpr (FAST) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    else asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// m, v and p of eight elements, one step on: m comes in as b1 m = scale * m[]; v takes the square of sqrt(a2) factor g.
+struct Update {
+    uint64_t a1, b2, a2, eps, rate, decay;
+    template <int CAP>
+    __device__ __forceinline__ Update(const ListArgs<CAP>& a, const Scalars& s)
+        : a1(pair2(a.a1 * s.factor, a.a1 * s.factor)), b2(pair2(a.b2, a.b2)), a2(pair2(a.root_a2 * s.factor, a.root_a2 * s.factor)),
+          eps(pair2(s.eps, s.eps)), rate(pair2(-s.rate, -s.rate)), decay(pair2(s.decay, s.decay)) {}
+    template <bool FAST>
+    __device__ __forceinline__ void apply(const float (&g)[8], float scale, float (&m)[8], float (&v)[8], float (&p)[8]) const
+    {
+        const uint64_t b1 = pair2(scale, scale);
+#pragma unroll
+        for (int x = 0; x < 8; x += 2) {
+            const uint64_t gg = pair2(g[x], g[x + 1]), hh = mul2(a2, gg);
+            const uint64_t mm = fma2(a1, gg, mul2(b1, pair2(m[x], m[x + 1])));
+            const uint64_t vv = fma2(hh, hh, mul2(b2, pair2(v[x], v[x + 1])));
+            unpack2(mm, m[x], m[x + 1]);
+            unpack2(vv, v[x], v[x + 1]);
+            float d0, d1;
+            unpack2(add2(pair2(root_of<FAST>(v[x]), root_of<FAST>(v[x + 1])), eps), d0, d1);
+            const uint64_t pp = pair2(p[x], p[x + 1]);
+            unpack2(fma2(rate, fma2(decay, pp, mul2(mm, pair2(inverse_of<FAST>(d0), inverse_of<FAST>(d1)))), pp), p[x], p[x + 1]);
+        }
+    }
+};
 
 // Exponent byte of a block whose largest magnitude has these bits, for codes of TOP + 1 binades.
 template <int TOP>
@@ -196,108 +306,335 @@ __device__ __forceinline__ int exponent_of(uint32_t largest)
     return min(max(e, 0), 255 - TOP);
 }
 
-template <typename PT, typename GT, bool Q8, int CAP>
-__global__ void __launch_bounds__(AL_THREADS)
-adamw_list_kernel(const __grid_constant__ ListArgs<CAP> a)
+__device__ __forceinline__ uint32_t permute(uint32_t a, uint32_t b, uint32_t selector)
+{
+    uint32_t r;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(selector));
+    return r;
+}
+
+// Largest of three, NaN if one is.
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t largest_bits(const float (&x)[8])
+{
+    float r = max3(fabsf(x[0]), fabsf(x[1]), fabsf(x[2]));
+    r = max3(r, fabsf(x[3]), fabsf(x[4]));
+    r = max3(r, fabsf(x[5]), fabsf(x[6]));
+    return __float_as_uint(max3(r, fabsf(x[7]), fabsf(x[7])));
+}
+
+// Four integers cut to [0, 255], a byte each.
+__device__ __forceinline__ uint32_t pack4(int a, int b, int c, int d)
+{
+    uint32_t hi, r;
+    asm("cvt.pack.sat.u8.s32.b32 %0, %1, %2, %3;" : "=r"(hi) : "r"(d), "r"(c), "r"(0));
+    asm("cvt.pack.sat.u8.s32.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(b), "r"(a), "r"(hi));
+    return r;
+}
+// The top bytes of four words.
+__device__ __forceinline__ uint32_t top4(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    return permute(permute(a, b, 0x0073), permute(c, d, 0x0073), 0x5410);
+}
+
+// m's codes as floats for k = 112 (exponents -15 ... 0): times 2^(k - 112) they are the values, for every k but the lowest, whose first codes
+// are subnormal, and the highest, whose last ones are infinity and NaN.
+__device__ __forceinline__ float code_value(int b)
+{
+    const uint32_t c = b & 127;
+    return __uint_as_float((c ? (c << 20) + (112u << 23) : 0u) | (uint32_t)(b & 128) << 24);
+}
+
+// Codes to values; m = scale * m[].
+__device__ __forceinline__ void decode8(uint2 cm, uint2 cv, uint32_t k, const float* table, float& scale, float (&m)[8], float (&v)[8])
+{
+    const uint32_t km = k & 255u, kv = (k >> 8) << 23;
+#pragma unroll
+    for (int x = 0; x < 8; ++x)           // the code in bits 16 to 23
+        v[x] = __uint_as_float(permute(x < 4 ? cv.x : cv.y, 0, 0x4044 | (x & 3) << 8) * 16 + kv);
+    if (km - 1u < 239u) {
+        scale = __uint_as_float((km + 15u) << 23);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) m[x] = table[permute(x < 4 ? cm.x : cm.y, 0, 0x4440 | (x & 3))];
+        return;
+    }
+    scale = 1.0f;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+        // the code in bits 16 to 23, its sign in those above too
+        uint32_t f = permute(x < 4 ? cm.x : cm.y, 0, 0x8044 | (x & 3) << 12 | (x & 3) << 8) * 16 & 0x87F00000u;
+        if (f & 0x07F00000u) f += km << 23;
+        m[x] = __uint_as_float(f);
+    }
+}
+
+__device__ __forceinline__ void encode8(const float (&m)[8], const float (&v)[8], uint4 r4, uint2& cm, uint2& cv, uint32_t& k)
+{
+    const uint32_t top_m = __reduce_max_sync(0xFFFFFFFFu, largest_bits(m)), top_v = __reduce_max_sync(0xFFFFFFFFu, largest_bits(v));
+    const int km = exponent_of<15>(top_m), kv = exponent_of<31>(top_v);
+    uint32_t r[4] = { r4.x, r4.y, r4.z, r4.w };
+    if (max(top_m, top_v) >= 0x7F800000u) r[0] = r[1] = r[2] = r[3] = 0;       // an infinity or NaN is not rounded on
+    // Codes are bits 20 to 26 (m, its sign is bit 31) and 20 to 27 (v) of these, unless an element is below the lowest one.
+    uint32_t em[8], ev[8], out_m = 0, out_v = 0;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+        const uint32_t dither = permute(r[x >> 1], 0, x & 1 ? 0x4432 : 0x4410) * 16;
+        em[x] = __float_as_uint(m[x]) + dither - ((uint32_t)km << 23);
+        ev[x] = __float_as_uint(v[x]) + dither - ((uint32_t)kv << 23);
+        out_m |= em[x];
+        out_v |= ev[x];
+    }
+    k = (uint32_t)(km | kv << 8);
+    if ((out_m & 0x78000000u) == 0 && out_v < 0x10000000u) {
+        uint32_t bm[8], bv[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            bm[x] = (em[x] * 16 & 0x7FFFFFFFu) | (em[x] & 0x80000000u);
+            bv[x] = ev[x] * 16;
+        }
+        cm = make_uint2(top4(bm[0], bm[1], bm[2], bm[3]), top4(bm[4], bm[5], bm[6], bm[7]));
+        cv = make_uint2(top4(bv[0], bv[1], bv[2], bv[3]), top4(bv[4], bv[5], bv[6], bv[7]));
+        return;
+    }
+    int cut[8];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) cut[x] = (int)(em[x] ^ (__float_as_uint(m[x]) & 0x80000000u)) >> 20;
+    const uint32_t sign[2] = { top4(__float_as_uint(m[0]), __float_as_uint(m[1]), __float_as_uint(m[2]), __float_as_uint(m[3])),
+                               top4(__float_as_uint(m[4]), __float_as_uint(m[5]), __float_as_uint(m[6]), __float_as_uint(m[7])) };
+    cm.x = (pack4(cut[0], cut[1], cut[2], cut[3]) & 0x7F7F7F7Fu) | (sign[0] & 0x80808080u);
+    cm.y = (pack4(cut[4], cut[5], cut[6], cut[7]) & 0x7F7F7F7Fu) | (sign[1] & 0x80808080u);
+#pragma unroll
+    for (int x = 0; x < 8; ++x) cut[x] = (int)ev[x] >> 20;
+    cv = make_uint2(pack4(cut[0], cut[1], cut[2], cut[3]), pack4(cut[4], cut[5], cut[6], cut[7]));
+}
+
+// Loads run a tile ahead of the arithmetic, through a ring of blocks in shared memory that each warp has for itself: a warp waits for no
+// other one, and its registers hold one block.  Copies are 512 contiguous bytes an instruction (with lanes 32 bytes apart every
+// sector of fp32 was fetched twice: 1.4 times the time).
+__device__ __forceinline__ void copy16(uint32_t to, const void* from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy8(uint32_t to, const void* from)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" :: "r"(to), "l"(from) : "memory");
+}
+// A block of 256 elements to shared memory, from the lane's 16 bytes on.  fp32: a lane will read two pieces side by side; every other
+// group of eight pieces is swapped in pairs, so that neither read hits a bank twice.
+__device__ __forceinline__ void copy_block(uint32_t to, const __nv_bfloat16* from, int lane) { copy16(to + lane * 16, from); }
+__device__ __forceinline__ void copy_block(uint32_t to, const float* from, int lane)
+{
+    const uint32_t at = to + (lane ^ (lane >> 3 & 1)) * 16;
+    copy16(at, from);
+    copy16(at + 512, from + 128);
+}
+__device__ __forceinline__ Raw8<__nv_bfloat16> read_block(const char* from, int lane, __nv_bfloat16)
+{
+    return Raw8<__nv_bfloat16>{ reinterpret_cast<const uint4*>(from)[lane] };
+}
+__device__ __forceinline__ Raw8<float> read_block(const char* from, int lane, float)
+{
+    const int at = 2 * lane, flip = lane >> 2 & 1;
+    return Raw8<float>{ reinterpret_cast<const float4*>(from)[at ^ flip], reinterpret_cast<const float4*>(from)[(at + 1) ^ flip] };
+}
+// (a tensor's last elements: `count` of them, zeros behind)
+__device__ __forceinline__ Raw8<float> guarded(const float* p, int count)
+{
+    float v[8];
+    load8_guarded(p, count, v);
+    return Raw8<float>{ make_float4(v[0], v[1], v[2], v[3]), make_float4(v[4], v[5], v[6], v[7]) };
+}
+__device__ __forceinline__ Raw8<__nv_bfloat16> guarded(const __nv_bfloat16* p, int count)
+{
+    float v[8];
+    load8_guarded(p, count, v);
+    return Raw8<__nv_bfloat16>{ make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])) };
+}
+
+// The tensor that a tile belongs to.
+template <int CAP>
+__device__ __forceinline__ int find_tensor(const ListArgs<CAP>& a, int tile)
+{
+    int at = 0, hi = a.n;
+    while (hi - at > 1) {
+        const int mid = (at + hi) >> 1;
+        if (a.tile_begin[mid] <= tile) at = mid; else hi = mid;
+    }
+    return at;
+}
+
+// A tile is RING blocks of each warp, side by side: the warps' first blocks, their second ones, ...
+template <typename PT, typename GT>
+struct Stage {
+    static constexpr int P = 0, G = P + AL_BLOCK * sizeof(PT), M = G + AL_BLOCK * sizeof(GT), V = M + AL_BLOCK, BYTES = V + AL_BLOCK;
+    static constexpr int RING = 4, BLOCKS = RING * AL_WARPS, TILE = BLOCKS * AL_BLOCK, SMEM = BLOCKS * BYTES;
+    static constexpr int FIT = 227 * 1024 / (SMEM + 2 * 1024), RESIDENT = FIT < 3 ? FIT : 3;
+};
+
+// 8 bits.  Bound by instruction issue with bfloat16 weights and gradients (49 an element, of which Philox 5, decoding 9, encoding 13; the
+// issue limit at the copy rate is 55), by memory otherwise.  What that shaped:
+//   * m's codes are looked up in shared memory (an add that must not happen for code 0 costs three instructions more);
+//   * pairs of floats (fma.rn.f32x2) for the update;
+//   * codes are cut out of four words at a time, clamped only where an element of a lane is below the lowest code;
+//   * whole tiles and the tensors' ends are different blocks of threads: with both in one loop it took 5 instructions an element more;
+//   * up to AL_WAVES times as many blocks as are resident: with one wave the slowest multiprocessor sets the time (529 us for 504).
+// 262 M parameters: bfloat16 454 us, 5.8 TB/s; fp32 weights with bfloat16 gradients 550, all fp32 628 (at the copy rate 401, 561, 641).
+template <typename PT, typename GT, int CAP>
+__global__ void __launch_bounds__(AL_THREADS, (Stage<PT, GT>::RESIDENT))
+adamw8_kernel(const __grid_constant__ ListArgs<CAP> a)
+{
+    using S = Stage<PT, GT>;
+    constexpr int RING = S::RING, STEP = AL_WARPS * AL_BLOCK;
+    extern __shared__ __align__(16) char ring[];
+    __shared__ Scalars shared;
+    __shared__ float table[256];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    auto prologue = [&] {
+        if (threadIdx.x == 0) shared = read_scalars(a);
+        table[threadIdx.x] = code_value((int)threadIdx.x);
+        __syncthreads();
+        return shared;
+    };
+    auto step = [&](const Scalars& s, const Update& update, const Raw8<PT>& rp, const Raw8<GT>& rg, int block, float (&p)[8], uint2& cm, uint2& cv, uint32_t& k) {
+        float g[8], m[8], v[8], scale;
+        unpack_raw8(rp, p);
+        unpack_raw8(rg, g);
+        decode8(cm, cv, k, table, scale, m, v);
+        if (a.fast) update.template apply<true>(g, scale * a.b1, m, v, p);
+        else update.template apply<false>(g, scale * a.b1, m, v, p);
+        encode8(m, v, philox4x32_10_keys((uint32_t)block, (uint32_t)lane, s.t_lo, s.t_hi, a.keys), cm, cv, k);
+    };
+    if ((int)blockIdx.x >= a.whole_grid) {             // the end of a tensor, behind its last whole tile
+        const int at = (int)blockIdx.x - a.whole_grid;
+        const long long numel = a.numel[at], done = numel / S::TILE * S::TILE;
+        if (done == numel) return;
+        const Scalars s = prologue();
+        if (!isfinite(s.factor)) return;
+        const Update update(a, s);
+#pragma unroll 1
+        for (long long e = done + warp * AL_BLOCK; e < numel; e += STEP) {
+            const int block = a.block_begin[at] + (int)(e / AL_BLOCK), count = (int)max(0ll, min(8ll, numel - e - lane * 8));
+            const long long se = (long long)block * AL_BLOCK + lane * 8;
+            PT* const P = static_cast<PT*>(a.p[at]) + e + lane * 8;
+            const GT* const G = static_cast<const GT*>(a.g[at]) + e + lane * 8;
+            const Raw8<PT> rp = count == 8 ? load_raw8_stream(P) : guarded(P, count);
+            const Raw8<GT> rg = count == 8 ? load_raw8_stream(G) : guarded(G, count);
+            uint2 cm = *reinterpret_cast<const uint2*>(a.m + se), cv = *reinterpret_cast<const uint2*>(a.v + se);
+            uint32_t k = a.k[block];
+            float p[8];
+            step(s, update, rp, rg, block, p, cm, cv, k);
+            if (count == 8) {
+                store8(P, p);
+            } else {
+#pragma unroll
+                for (int x = 0; x < 8; ++x) if (x < count) store1(P + x, p[x]);
+            }
+            *reinterpret_cast<uint2*>(a.m + se) = cm;
+            *reinterpret_cast<uint2*>(a.v + se) = cv;
+            if (lane == 0) a.k[block] = (uint16_t)k;
+        }
+        return;
+    }
+    const char* const mine = ring + warp * (RING * S::BYTES);
+    const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
+    const int tiles = a.tile_begin[a.n];
+    // The warp's first block of a tile: the lane's elements and codes of it, its number.
+    struct Place { PT* p; const GT* g; char* m; char* v; int block; };
+    auto find = [&](int tile) {
+        const int at = find_tensor(a, tile), local = (tile - a.tile_begin[at]) * S::BLOCKS + warp, block = a.block_begin[at] + local;
+        const long long e = (long long)local * AL_BLOCK + lane * 8, se = (long long)block * AL_BLOCK + lane * 8;
+        return Place{ static_cast<PT*>(a.p[at]) + e, static_cast<const GT*>(a.g[at]) + e, a.m + se, a.v + se, block };
+    };
+    // Copies the warp's block i of a tile and closes a group.
+    auto fetch = [&](const Place& w, bool there, int i) {
+        if (there) {
+            const uint32_t to = mine_at + i * S::BYTES;
+            copy_block(to + S::P, w.p + i * STEP + lane * (16 / (int)sizeof(PT) - 8), lane);
+            copy_block(to + S::G, w.g + i * STEP + lane * (16 / (int)sizeof(GT) - 8), lane);
+            copy8(to + S::M + lane * 8, w.m + i * STEP);
+            copy8(to + S::V + lane * 8, w.v + i * STEP);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    // The exponents of the warp's blocks, one a lane.
+    auto exponents = [&](const Place& w) { return lane < RING ? a.k[w.block + lane * AL_WARPS] : (uint16_t)0; };
+    int tile = blockIdx.x;
+    Place now = find(tile);
+#pragma unroll
+    for (int i = 0; i < RING; ++i) fetch(now, true, i);
+    uint32_t k = exponents(now);
+    const Scalars s = prologue();
+    if (!isfinite(s.factor)) {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        return;
+    }
+    const Update update(a, s);
+    for (; tile < tiles; tile += a.whole_grid) {
+        const bool more = tile + a.whole_grid < tiles;
+        const Place next = more ? find(tile + a.whole_grid) : now;
+        const uint32_t next_k = exponents(next);
+#pragma unroll 1
+        for (int i = 0; i < RING; ++i) {
+            asm volatile("cp.async.wait_group %0;" :: "n"(RING - 1) : "memory");
+            __syncwarp();                              // what the other lanes copied is there as well
+            const char* const from = mine + i * S::BYTES;
+            const Raw8<PT> rp = read_block(from + S::P, lane, PT());
+            const Raw8<GT> rg = read_block(from + S::G, lane, GT());
+            uint2 cm = reinterpret_cast<const uint2*>(from + S::M)[lane], cv = reinterpret_cast<const uint2*>(from + S::V)[lane];
+            uint32_t kk = __shfl_sync(0xFFFFFFFFu, k, i);
+            __syncwarp();                              // every lane has read: the next tile's block takes its place
+            fetch(next, more, i);
+            float p[8];
+            step(s, update, rp, rg, now.block + i * AL_WARPS, p, cm, cv, kk);
+            store8(now.p + i * STEP, p);
+            __stcs(reinterpret_cast<uint2*>(now.m + i * STEP), cm);
+            __stcs(reinterpret_cast<uint2*>(now.v + i * STEP), cv);
+            if (lane == i) k = kk;
+        }
+        if (lane < RING) a.k[now.block + lane * AL_WARPS] = (uint16_t)k;
+        now = next;
+        k = next_k;
+    }
+}
+
+// Moments of 32 bits: nothing but the traffic.  A block of threads has one tile, so that fast and slow multiprocessors share the work as
+// they can (blocks that stay and loop: 906 us instead of 842).  262 M parameters: bfloat16 842 us, 6.8 TB/s; fp32 weights with bfloat16
+// gradients 1000, all fp32 1069 (at the copy rate 882, 1042, 1122).
+template <typename PT, typename GT, int CAP>
+__global__ void __launch_bounds__(AL_THREADS, 4)
+adamw32_kernel(const __grid_constant__ ListArgs<CAP> a)
 {
     __shared__ Scalars shared;
-    if (threadIdx.x == 0) {
-        Scalars s;
-        s.lr = a.lr_at ? *a.lr_at : a.lr;
-        s.factor = a.factor ? *a.factor : 1.0f;
-        unsigned long long t = a.t;
-        s.inv_c1 = a.inv_c1; s.inv_c2 = a.inv_c2;
-        if (a.t_at) {
-            t = (unsigned long long)*a.t_at;
-            if (a.bias_correction) {
-                s.inv_c1 = (float)(-1.0 / expm1((double)(t + 1) * a.log_b1));
-                s.inv_c2 = (float)(-1.0 / expm1((double)(t + 1) * a.log_b2));
-            }
-        }
-        s.t_lo = (uint32_t)t; s.t_hi = (uint32_t)(t >> 32);
-        shared = s;
-    }
+    if (threadIdx.x == 0) shared = read_scalars(a);
     __syncthreads();
     const Scalars s = shared;
     if (!isfinite(s.factor)) return;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int tiles = a.tile_begin[a.n];
-    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        int at = 0, hi = a.n;
-        while (hi - at > 1) {
-            const int mid = (at + hi) >> 1;
-            if (a.tile_begin[mid] <= tile) at = mid; else hi = mid;
-        }
-        PT* __restrict__ P = static_cast<PT*>(a.p[at]);
-        const GT* __restrict__ G = static_cast<const GT*>(a.g[at]);
-        const long long numel = a.numel[at];
-        const int first = (tile - a.tile_begin[at]) * AL_TILE + warp;
-        for (int i = 0; i < AL_TILE / AL_WARPS; ++i) {
-            const int local = first + i * AL_WARPS;
-            const long long e = (long long)local * AL_BLOCK + lane * 8;
-            if (e - lane * 8 >= numel) break;
-            const int block = a.block_begin[at] + local;
-            const long long se = (long long)block * AL_BLOCK + lane * 8;
-            const int count = (int)max(0ll, min(8ll, numel - e));
-            float g[8], p[8], m[8], v[8];
-            if (count == 8) { load8_stream(G + e, g); load8_stream(P + e, p); }
-            else { load8_guarded(G + e, count, g); load8_guarded(P + e, count, p); }
-            if constexpr (Q8) {
-                const uint2 cm = __ldcs(reinterpret_cast<const uint2*>(a.m + se)), cv = __ldcs(reinterpret_cast<const uint2*>(a.v + se));
-                const uint32_t k = a.k[block];
-                const uint32_t km = (k & 255u) << 23, kv = (k >> 8) << 23;
+    const Update update(a, s);
+    const int at = find_tensor(a, blockIdx.x);
+    const long long first = (long long)(blockIdx.x - a.tile_begin[at]) * AL_TILE32;
+    const long long left = a.numel[at] - first;
+    PT* const P = static_cast<PT*>(a.p[at]) + first;
+    const GT* const G = static_cast<const GT*>(a.g[at]) + first;
+    float* const M = reinterpret_cast<float*>(a.m) + (long long)a.block_begin[at] * AL_BLOCK + first;
+    float* const V = reinterpret_cast<float*>(a.v) + (long long)a.block_begin[at] * AL_BLOCK + first;
+#pragma unroll 1
+    for (int e = threadIdx.x * 8; e < AL_TILE32; e += AL_THREADS * 8) {
+        const int count = (int)max(0ll, min(8ll, left - e));
+        if (count == 0) break;
+        float g[8], p[8], m[8], v[8];
+        if (count == 8) { load8_stream(P + e, p); load8_stream(G + e, g); load8_stream(M + e, m); load8_stream(V + e, v); }
+        else { load8_guarded(P + e, count, p); load8_guarded(G + e, count, g); load8_guarded(M + e, count, m); load8_guarded(V + e, count, v); }
+        if (a.fast) update.template apply<true>(g, a.b1, m, v, p);
+        else update.template apply<false>(g, a.b1, m, v, p);
+        if (count == 8) { store8(P + e, p); store8(M + e, m); store8(V + e, v); }
+        else {
 #pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    const uint32_t bm = ((x < 4 ? cm.x : cm.y) >> (8 * (x & 3))) & 255u, bv = ((x < 4 ? cv.x : cv.y) >> (8 * (x & 3))) & 255u;
-                    const uint32_t mag = bm & 127u;
-                    m[x] = __uint_as_float((mag ? (mag << 20) + km : 0u) | (bm & 128u) << 24);
-                    v[x] = __uint_as_float((bv << 20) + kv);
-                }
-            } else {
-                const float* M = reinterpret_cast<const float*>(a.m) + se;
-                const float* V = reinterpret_cast<const float*>(a.v) + se;
-                if (count == 8) { load8_stream(M, m); load8_stream(V, v); }
-                else { load8_guarded(M, count, m); load8_guarded(V, count, v); }
-            }
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                const float gx = g[x] * s.factor;
-                m[x] = fmaf(a.b1, m[x], a.a1 * gx);
-                v[x] = fmaf(a.b2, v[x], a.a2 * gx * gx);
-                const float update = __fdividef(m[x] * s.inv_c1, sqrtf(v[x] * s.inv_c2) + a.eps);
-                p[x] = fmaf(-s.lr, fmaf(a.wd, p[x], update), p[x]);
-            }
-            if (count == 8) store8(P + e, p);
-            else for (int x = 0; x < count; ++x) store1(P + e + x, p[x]);
-            if constexpr (Q8) {
-                uint32_t top_m = 0, top_v = 0;
-#pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    top_m = max(top_m, __float_as_uint(m[x]) & 0x7FFFFFFFu);
-                    top_v = max(top_v, __float_as_uint(v[x]));
-                }
-                const int km = exponent_of<15>(__reduce_max_sync(0xFFFFFFFFu, top_m)), kv = exponent_of<31>(__reduce_max_sync(0xFFFFFFFFu, top_v));
-                const uint4 r4 = philox4x32_10_keys((uint32_t)block, (uint32_t)lane, s.t_lo, s.t_hi, a.keys);
-                const uint32_t r[4] = { r4.x, r4.y, r4.z, r4.w };
-                uint32_t cm[2] = { 0, 0 }, cv[2] = { 0, 0 };
-#pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    const uint32_t dither = (x & 1 ? r[x >> 1] >> 16 : r[x >> 1] & 0xFFFFu) << 4;
-                    const uint32_t bits = __float_as_uint(m[x]);
-                    const int em = min(max((int)(((bits & 0x7FFFFFFFu) + dither) >> 20) - km * 8, 0), 127);
-                    const int ev = min(max((int)((__float_as_uint(v[x]) + dither) >> 20) - kv * 8, 0), 255);
-                    cm[x >> 2] |= ((uint32_t)em | (bits >> 24 & 128u)) << (8 * (x & 3));
-                    cv[x >> 2] |= (uint32_t)ev << (8 * (x & 3));
-                }
-                __stcs(reinterpret_cast<uint2*>(a.m + se), make_uint2(cm[0], cm[1]));
-                __stcs(reinterpret_cast<uint2*>(a.v + se), make_uint2(cv[0], cv[1]));
-                if (lane == 0) a.k[block] = (uint16_t)(km | kv << 8);
-            } else {
-                float* M = reinterpret_cast<float*>(a.m) + se;
-                float* V = reinterpret_cast<float*>(a.v) + se;
-                if (count == 8) { store8(M, m); store8(V, v); }
-                else for (int x = 0; x < count; ++x) { M[x] = m[x]; V[x] = v[x]; }
-            }
+            for (int x = 0; x < 8; ++x) if (x < count) { store1(P + e + x, p[x]); M[e + x] = m[x]; V[e + x] = v[x]; }
         }
     }
 }
@@ -307,7 +644,8 @@ __global__ void __launch_bounds__(AL_THREADS)
 adamw_moments_kernel(const uint4* __restrict__ cm, const uint4* __restrict__ cv, const uint16_t* __restrict__ ks, long long n,
                      uint4* __restrict__ m, uint4* __restrict__ v)
 {
-    for (long long i = (long long)blockIdx.x * AL_THREADS + threadIdx.x; i < n; i += (long long)gridDim.x * AL_THREADS) {
+    const long long i = (long long)blockIdx.x * AL_THREADS + threadIdx.x;
+    if (i < n) {
         const uint4 m4 = __ldcs(cm + i), v4 = __ldcs(cv + i);
         const uint32_t k = __ldg(ks + (i >> 4)), km = (k & 255u) << 7, kv = (k >> 8) << 7;
         const uint32_t mw[4] = { m4.x, m4.y, m4.z, m4.w }, vw[4] = { v4.x, v4.y, v4.z, v4.w };
@@ -373,11 +711,27 @@ int norm_launch(const void* const* d_G, const int64_t* numel, const int32_t* dty
     return cudaGetLastError() == cudaSuccess ? APOLLO_OK : APOLLO_ERR_CUDA;
 }
 
-template <typename PT, typename GT, bool Q8, int CAP>
-cudaError_t list_launch(const ListArgs<CAP>& a, int64_t tiles, int sms, cudaStream_t stream)
+template <typename PT, typename GT, int CAP>
+cudaError_t list_launch(ListArgs<CAP>& a, bool q8, int sms, cudaStream_t stream)
 {
-    const int64_t most = 8LL * sms;
-    adamw_list_kernel<PT, GT, Q8, CAP><<<(unsigned)(tiles < most ? tiles : most), AL_THREADS, 0, stream>>>(a);
+    using S = Stage<PT, GT>;
+    int64_t tiles = 0;
+    bool ends = false;
+    for (int k = 0; k < a.n; ++k) {
+        a.tile_begin[k] = (int)tiles;
+        tiles += q8 ? a.numel[k] / S::TILE : (a.numel[k] + AL_TILE32 - 1) / AL_TILE32;
+        ends |= a.numel[k] % S::TILE != 0;
+    }
+    a.tile_begin[a.n] = (int)tiles;
+    if (!q8) {
+        adamw32_kernel<PT, GT, CAP><<<(unsigned)tiles, AL_THREADS, 0, stream>>>(a);
+        return cudaGetLastError();
+    }
+    const cudaError_t e = cudaFuncSetAttribute(adamw8_kernel<PT, GT, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+    if (e != cudaSuccess) return e;
+    const int64_t most = (int64_t)S::RESIDENT * sms * AL_WAVES;
+    a.whole_grid = (int)(tiles < most ? tiles : most);
+    adamw8_kernel<PT, GT, CAP><<<(unsigned)(a.whole_grid + (ends ? a.n : 0)), AL_THREADS, S::SMEM, stream>>>(a);
     return cudaGetLastError();
 }
 
@@ -396,29 +750,21 @@ struct ListCall {
 template <int CAP>
 int list_launches(const ListCall& c, ListArgs<CAP>& a, int32_t dp, int32_t dg)
 {
-    int64_t block = 0, tiles = 0;
+    int64_t block = 0;
     a.n = 0;
     for (int32_t i = 0; i <= c.n; ++i) {
         if ((i == c.n || a.n == CAP) && a.n > 0) {
-            a.tile_begin[a.n] = (int)tiles;
             const bool pb = dp == APOLLO_DT_BF16, gb = dg == APOLLO_DT_BF16;
-            cudaError_t e;
-            if (c.q8)
-                e = pb ? (gb ? list_launch<__nv_bfloat16, __nv_bfloat16, true>(a, tiles, c.sms, c.stream) : list_launch<__nv_bfloat16, float, true>(a, tiles, c.sms, c.stream))
-                       : (gb ? list_launch<float, __nv_bfloat16, true>(a, tiles, c.sms, c.stream) : list_launch<float, float, true>(a, tiles, c.sms, c.stream));
-            else
-                e = pb ? (gb ? list_launch<__nv_bfloat16, __nv_bfloat16, false>(a, tiles, c.sms, c.stream) : list_launch<__nv_bfloat16, float, false>(a, tiles, c.sms, c.stream))
-                       : (gb ? list_launch<float, __nv_bfloat16, false>(a, tiles, c.sms, c.stream) : list_launch<float, float, false>(a, tiles, c.sms, c.stream));
+            const cudaError_t e = pb ? (gb ? list_launch<__nv_bfloat16, __nv_bfloat16>(a, c.q8, c.sms, c.stream) : list_launch<__nv_bfloat16, float>(a, c.q8, c.sms, c.stream))
+                                     : (gb ? list_launch<float, __nv_bfloat16>(a, c.q8, c.sms, c.stream) : list_launch<float, float>(a, c.q8, c.sms, c.stream));
             if (e != cudaSuccess) return APOLLO_ERR_CUDA;
             a.n = 0;
-            tiles = 0;
         }
         if (i == c.n) break;
         const int64_t blocks = (c.numel[i] + AL_BLOCK - 1) / AL_BLOCK;
         if (c.G[i] && blocks > 0 && c.dtype_P[i] == dp && c.dtype_G[i] == dg) {
             a.p[a.n] = c.P[i]; a.g[a.n] = c.G[i]; a.numel[a.n] = c.numel[i];
-            a.tile_begin[a.n] = (int)tiles; a.block_begin[a.n] = (int)block;
-            tiles += (blocks + AL_TILE - 1) / AL_TILE;
+            a.block_begin[a.n] = (int)block;
             ++a.n;
         }
         block += blocks;
@@ -434,16 +780,18 @@ int list_step(const ListCall& c, const apollo_adamw_list_config* cfg, void* d_st
     const size_t codes = (size_t)blocks * AL_BLOCK * (c.q8 ? 1 : 4);
     a.m = static_cast<char*>(d_state); a.v = a.m + codes; a.k = reinterpret_cast<uint16_t*>(a.v + codes);
     a.factor = d_factor; a.lr_at = d_lr; a.t_at = reinterpret_cast<const long long*>(d_t);
-    a.lr = (float)lr; a.wd = (float)wd; a.eps = (float)cfg->eps;
-    a.b1 = (float)cfg->beta1; a.a1 = (float)(1.0 - cfg->beta1); a.b2 = (float)cfg->beta2; a.a2 = (float)(1.0 - cfg->beta2);
+    a.lr = lr; a.wd = wd; a.eps = cfg->eps;
+    a.b1 = (float)cfg->beta1; a.a1 = (float)(1.0 - cfg->beta1); a.b2 = (float)cfg->beta2; a.root_a2 = (float)std::sqrt(1.0 - cfg->beta2);
     a.bias_correction = cfg->bias_correction;
+    a.fast = cfg->eps >= 1e-12;
     a.log_b1 = std::log(cfg->beta1); a.log_b2 = std::log(cfg->beta2);      // (-inf for 0: expm1 is -1, c = 1)
-    a.inv_c1 = a.inv_c2 = 1.0f;
+    a.inv_c1 = a.root = 1.0;
     if (cfg->bias_correction) {
-        a.inv_c1 = (float)(-1.0 / std::expm1(((double)t + 1) * a.log_b1));
-        a.inv_c2 = (float)(-1.0 / std::expm1(((double)t + 1) * a.log_b2));
+        a.inv_c1 = -1.0 / std::expm1(((double)t + 1) * a.log_b1);
+        a.root = std::sqrt(-1.0 / std::expm1(((double)t + 1) * a.log_b2));
     }
     a.t = (unsigned long long)t;
+    a.scalars = scalars_of(lr, wd, cfg->eps, a.inv_c1, a.root, a.t);
     uint32_t k0 = (uint32_t)cfg->seed, k1 = (uint32_t)(cfg->seed >> 32);
     for (int r = 0; r < 10; ++r) {
         a.keys[2 * r] = k0; a.keys[2 * r + 1] = k1;
@@ -556,14 +904,10 @@ extern "C" int apollo_adamw_list_moments(const void* d_state, size_t state_bytes
     if (!d_state || !d_M || !d_V) return APOLLO_ERR_INVALID_ARG;
     if ((uintptr_t)d_state % 16 || (uintptr_t)d_M % 16 || (uintptr_t)d_V % 16) return APOLLO_ERR_ALIGN;
     if (state_bytes < state_size(n_blocks, 8)) return APOLLO_ERR_WORKSPACE;
-    int sms = 0;
-    const int drc = device_sms(&sms);
-    if (drc != APOLLO_OK) return drc;
     const char* m = static_cast<const char*>(d_state);
     const char* v = m + (size_t)n_blocks * AL_BLOCK;
-    const int64_t vectors = n_blocks * (AL_BLOCK / 16), most = 8LL * sms;
-    const int64_t grid = (vectors + AL_THREADS - 1) / AL_THREADS;
-    adamw_moments_kernel<<<(unsigned)(grid < most ? grid : most), AL_THREADS, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
+    const int64_t vectors = n_blocks * (AL_BLOCK / 16);
+    adamw_moments_kernel<<<(unsigned)((vectors + AL_THREADS - 1) / AL_THREADS), AL_THREADS, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
         reinterpret_cast<const uint4*>(m), reinterpret_cast<const uint4*>(v), reinterpret_cast<const uint16_t*>(v + (size_t)n_blocks * AL_BLOCK),
         vectors, static_cast<uint4*>(d_M), static_cast<uint4*>(d_V));
     return cudaGetLastError() == cudaSuccess ? APOLLO_OK : APOLLO_ERR_CUDA;
