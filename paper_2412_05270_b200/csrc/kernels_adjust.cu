@@ -5,8 +5,12 @@
 //   mask bit 0: x <- -inf
 //   a_j = allowed ? dout_j : 0;  dlogit_j = a_j {1, 1 / rho, rho};  dbias_j = a_j (summed over rows if shared);  dvalue_i = a_j
 //
-// A CTA takes a chunk of the vocabulary of one row.  It reads the row's history and counts the tokens of its chunk in a table in
-// shared memory (integer atomics: their order does not matter), then streams the chunk once.  A table word holds
+// A block of threads takes a chunk of the vocabulary for one row, or for a few rows in turn.  It counts the tokens of its chunk in a table in
+// shared memory and lists the words that occur (integer atomics: their order decides the order of the list, not the results).  Then
+// two passes: a stream over the whole chunk that knows of bias and mask alone, and the listed words once more, one a thread.  (With
+// both in one pass, vectors looking into the table, nearly every warp of a training batch had a word to look up: 376 instructions
+// a vector of eight instead of 40.)  Rows that share a history (the positions of a sequence in training) go on with the table of the row
+// before: they add the tokens in between.  A table word holds
 // [31] seen at all  [30..20] 1 + slot of the word's named value  [19..0] how often from `start` on.
 #include "../../include/apollo.h"
 
@@ -20,8 +24,8 @@ namespace apollo {
 namespace {
 
 constexpr int AJ_THREADS = 256;
-constexpr int AJ_MAX_CHUNK = 8192;
-constexpr int AJ_MIN_CHUNK = 2048;
+constexpr int AJ_UNITS = 4;              // vectors a thread has of a row's chunk at once
+constexpr int AJ_ROWS = 16;              // most rows in turn, without sums
 constexpr uint32_t AJ_SEEN = 0x80000000u;
 constexpr int AJ_SLOT_SHIFT = 20;
 constexpr uint32_t AJ_COUNT = (1u << AJ_SLOT_SHIFT) - 1, AJ_SLOT = 0x7FFu;
@@ -55,20 +59,59 @@ __device__ __forceinline__ int token_at(const void* p, long long i, int is64, in
     return v < vocab ? v : -1;
 }
 
-// Counts the tokens of [j0, j0 + width) in the table (zeroed; a barrier before and after is the caller's).
-__device__ __forceinline__ void count_history(const Rules& r, long long row, int vocab, int j0, int width, uint32_t* table)
-{
-    const long long first = row / r.share * r.history_stride;
-    const int length = r.length ? min(max(r.length[row], 0), r.history_len) : r.history_len;
-    const int start = r.start ? r.start[row] : 0;
-    for (int i = threadIdx.x; i < length; i += AJ_THREADS) {
-        const int j = token_at(r.history, first + i, r.history64, vocab) - j0;
-        if (j >= 0 && j < width) {
-            if (i >= start) atomicAdd(table + j, 1u);
-            else atomicOr(table + j, AJ_SEEN);
+// The table of a chunk: `chunk` words, and the list of those that are not zero.
+struct Table {
+    uint32_t* word;
+    uint16_t* list;                      // chunk <= 65536
+    int* count;
+    int j0, width;
+    long long history = -1;              // what it holds: row of the history, tokens, first counted one
+    int length = 0, start = 0;
+
+    __device__ __forceinline__ Table(uint32_t* at, int* n, int chunk, int first, int w)
+        : word(at), list(reinterpret_cast<uint16_t*>(at + chunk)), count(n), j0(first), width(w) {}
+    static __host__ __device__ constexpr int words(int chunk, int entries) { return chunk + (entries + 1) / 2; }
+    __device__ __forceinline__ void clear(int chunk)
+    {
+        for (int i = threadIdx.x * 4; i < chunk; i += AJ_THREADS * 4) *reinterpret_cast<uint4*>(word + i) = make_uint4(0, 0, 0, 0);
+        if (threadIdx.x == 0) *count = 0;
+    }
+    __device__ __forceinline__ void append(int j) { list[atomicAdd(count, 1)] = (uint16_t)j; }
+    // f(word, position) for the tokens of the chunk at positions [from, to).
+    template <typename F>
+    __device__ __forceinline__ void scan(const Rules& r, int vocab, int from, int to, F f)
+    {
+        const long long first = history * r.history_stride;
+#pragma unroll 4
+        for (int i = from + (int)threadIdx.x; i < to; i += AJ_THREADS) {
+            const int j = token_at(r.history, first + i, r.history64, vocab) - j0;
+            if (j >= 0 && j < width) f(j, i);
         }
     }
-}
+    // The table of `row`, from that of the row before it where both have the same history.  Begins with a barrier; the caller ends with one.
+    __device__ __forceinline__ void set(const Rules& r, long long row, int vocab, int chunk)
+    {
+        const long long mine = row / r.share;
+        const int len = r.length ? min(max(r.length[row], 0), r.history_len) : r.history_len;
+        const int from = r.start ? min(max(r.start[row], 0), len) : 0;
+        __syncthreads();
+        if (mine != history || len < length) {
+            clear(chunk);
+            __syncthreads();
+            history = mine;
+            length = start = 0;
+        }
+        // positions whose count begins or ends, among those the table has
+        if (start < min(from, length)) scan(r, vocab, start, min(from, length), [&](int j, int) { atomicSub(word + j, 1u); });
+        if (from < min(start, length)) scan(r, vocab, from, min(start, length), [&](int j, int) { atomicAdd(word + j, 1u); });
+        scan(r, vocab, length, len, [&](int j, int i) {
+            if (!(atomicOr(word + j, AJ_SEEN) & AJ_SEEN)) append(j);
+            if (i >= from) atomicAdd(word + j, 1u);
+        });
+        length = len;
+        start = from;
+    }
+};
 
 template <typename T, int N> struct Vec;
 template <typename T> struct Vec<T, 1> {
@@ -90,121 +133,202 @@ template <> struct Vec<__nv_bfloat16, 8> {
     }
 };
 
-template <typename T, int N>
-__device__ __forceinline__ void load_n(const T* p, int count, float (&x)[N])
+// N bits from `bit` on.
+template <int N>
+__device__ __forceinline__ uint32_t bits_at(const uint32_t* words, int bit, int n_words)
 {
-    if (count == N) reinterpret_cast<const Vec<T, N>*>(p)->get(x);
-    else
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = e < count ? (float)p[e] : 0.0f;
-}
-template <typename T, int N>
-__device__ __forceinline__ void store_n(T* p, int count, const float (&x)[N])
-{
-    if (count == N) {
-        Vec<T, N> v;
-        v.set(x);
-        *reinterpret_cast<Vec<T, N>*>(p) = v;
-    } else
-#pragma unroll
-        for (int e = 0; e < N; ++e) if (e < count) p[e] = (T)x[e];
+    const int w = bit >> 5, at = bit & 31;
+    const uint32_t lo = words[w], hi = N > 1 && at + N > 32 && w + 1 < n_words ? words[w + 1] : 0;
+    return __funnelshift_r(lo, hi, at) & ((1u << N) - 1u);
 }
 
-// Mask bits of words j .. j + N - 1 (j a multiple of N, N a divisor of 32).
-template <int N>
-__device__ __forceinline__ uint32_t mask_bits(const uint32_t* mask, int j)
+// The vectors of a chunk of a row: they start where 16-byte boundaries of `out` are, the first and the last are cut at the chunk's ends.
+template <typename T, int N>
+struct Grid {
+    static constexpr uint32_t ALL = (1u << N) - 1u;
+    int j0, j1, shift;
+    __device__ __forceinline__ Grid(const T* out, int first, int width) : j0(first), j1(first + width)
+    {
+        shift = N == 1 ? 0 : (int)(((uintptr_t)(out + first) & 15) / sizeof(T));
+    }
+    __device__ __forceinline__ int first(int u) const { return j0 - shift + u * N; }
+    __device__ __forceinline__ uint32_t valid(int s) const
+    {
+        uint32_t v = ALL;
+        if (s < j0) v = v << (j0 - s) & ALL;
+        if (s + N > j1) v &= j1 > s ? (1u << (j1 - s)) - 1u : 0u;
+        return v;
+    }
+    // bits of the vector's elements, those outside the chunk unset
+    __device__ __forceinline__ uint32_t bits(const uint32_t* words, int s, int base, int n_words, uint32_t valid) const
+    {
+        const int lo = s > j0 ? s : j0;
+        return bits_at<N>(words, lo - base, n_words) << (lo - s) & valid;
+    }
+};
+
+template <typename T, int N>
+__device__ __forceinline__ bool same_phase(const T* p, int shift, int first)
 {
-    return mask ? mask[j >> 5] >> (j & 31) & ((1u << N) - 1u) : (1u << N) - 1u;
+    return N == 1 || (int)(((uintptr_t)(p + first) & 15) / sizeof(T)) == shift;
 }
+
+// Elements of a vector at columns s ...: one access where it is whole and on a 16-byte boundary.
+template <typename T, int N>
+__device__ __forceinline__ void load_vec(const T* row, int s, uint32_t valid, bool phase, float (&x)[N])
+{
+    if (valid == Grid<T, N>::ALL && phase) {
+        reinterpret_cast<const Vec<T, N>*>(row + s)->get(x);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = valid >> e & 1 ? (float)row[s + e] : 0.0f;
+    }
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_vec(T* row, int s, uint32_t valid, bool phase, const float (&x)[N])
+{
+    if (valid == Grid<T, N>::ALL && phase) {
+        Vec<T, N> v;
+        v.set(x);
+        *reinterpret_cast<Vec<T, N>*>(row + s) = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) if (valid >> e & 1) row[s + e] = (T)x[e];
+    }
+}
+
+// The whole vectors of a row that a thread will need, read before its table is there.
+template <typename T, int N>
+struct Ahead {
+    Vec<T, N> v[AJ_UNITS];
+    __device__ __forceinline__ void read(const T* in, const T* out, int j0, int width)
+    {
+        const Grid<T, N> grid(out, j0, width);
+        if (!same_phase<T, N>(in, grid.shift, j0)) return;
+#pragma unroll
+        for (int q = 0; q < AJ_UNITS; ++q) {
+            const int s = grid.first(q * AJ_THREADS + threadIdx.x);
+            if (s >= j0 && s + N <= grid.j1) v[q] = *reinterpret_cast<const Vec<T, N>*>(in + s);
+        }
+    }
+};
 
 struct AdjustArgs {
     const void* logits;
     void* out;
     long long stride, out_stride, n_rows;
-    int vocab, chunk;
+    int vocab, chunk, chunks, rows;      // rows: in turn
+    int entries;                         // of the list at most
     Rules r;
 };
 
-// N: elements of a vector; 1 where rows are not whole vectors.  TABLE: there is a history or there are named values.
-template <typename T, int N, bool TABLE>
+// TABLE: there is a history or there are named values.
+template <typename T, bool TABLE>
 __global__ void __launch_bounds__(AJ_THREADS)
 adjust_kernel(const __grid_constant__ AdjustArgs a)
 {
-    extern __shared__ uint32_t table[];
-    const int j0 = blockIdx.y * a.chunk, width = min(a.chunk, a.vocab - j0);
-    float* sums = reinterpret_cast<float*>(table + a.chunk);
+    constexpr int N = 16 / sizeof(T);
+    extern __shared__ __align__(16) uint32_t shared[];
+    __shared__ int listed;
+    const int part = blockIdx.x % a.chunks;
+    const long long begin = (long long)(blockIdx.x / a.chunks) * a.rows, end = min(begin + a.rows, a.n_rows);
+    const int j0 = part * a.chunk, width = min(a.chunk, a.vocab - j0), mask_words = (a.vocab + 31) / 32;
+    Table table(shared, &listed, a.chunk, j0, width);
+    float* sums = reinterpret_cast<float*>(shared + Table::words(a.chunk, a.entries));
     int* words = reinterpret_cast<int*>(sums + a.r.n_bias);
-    const bool place = a.logits == a.out;
-    for (long long row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
+    const bool place = a.logits == a.out, sparse = place && !a.r.bias;
+    for (long long row = begin; row < end; ++row) {
+        const T* const x0 = static_cast<const T*>(a.logits) + row * a.stride;
+        T* const y0 = static_cast<T*>(a.out) + row * a.out_stride;
+        const T* const b0 = a.r.bias ? static_cast<const T*>(a.r.bias) + row * a.r.bias_stride : nullptr;
+        const uint32_t* const m0 = a.r.mask ? a.r.mask + row * a.r.mask_stride : nullptr;
+        Ahead<T, N> ahead;
+        if (!sparse) ahead.read(x0, y0, j0, width);
         float rho = 1.0f, phi = 0.0f, pi = 0.0f;
+        // the word's logit with everything that concerns it
+        auto adjusted = [&](int j) {
+            const uint32_t t = table.word[j];
+            float x = (float)x0[j0 + j];
+            if (t & (AJ_SEEN | AJ_COUNT)) x = x > 0.0f ? __fdiv_rn(x, rho) : x * rho;
+            if (t & AJ_COUNT) x -= fmaf(phi, (float)(t & AJ_COUNT), pi);
+            if (b0) x += (float)b0[j0 + j];
+            const uint32_t slot = t >> AJ_SLOT_SHIFT & AJ_SLOT;
+            return slot ? x + sums[slot - 1] : x;
+        };
+        auto allowed = [&](int j) { return !m0 || (m0[(j0 + j) >> 5] >> ((j0 + j) & 31) & 1u); };
         if constexpr (TABLE) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < width; i += AJ_THREADS) table[i] = 0;
             for (int i = threadIdx.x; i < a.r.n_bias; i += AJ_THREADS) words[i] = token_at(a.r.word, row * a.r.n_bias + i, a.r.words64, a.vocab);
-            __syncthreads();
             if (a.r.history) {
                 rho = a.r.rho_at ? a.r.rho_at[row] : a.r.rho;
                 phi = a.r.phi_at ? a.r.phi_at[row] : a.r.phi;
                 pi = a.r.pi_at ? a.r.pi_at[row] : a.r.pi;
-                count_history(a.r, row, a.vocab, j0, width, table);
+                table.set(a.r, row, a.vocab, a.chunk);
+            } else {
+                table.clear(a.chunk);
             }
-            // the first pair of a word sums the values of all its pairs, in order
-            for (int i = threadIdx.x; i < a.r.n_bias; i += AJ_THREADS) {
-                const int w = words[i];
-                if (w < j0 || w >= j0 + width) continue;
-                bool first = true;
-                for (int k = 0; k < i && first; ++k) first = words[k] != w;
-                if (!first) continue;
-                float sum = 0.0f;
-                for (int k = i; k < a.r.n_bias; ++k) if (words[k] == w) sum += a.r.value[row * a.r.n_bias + k];
-                sums[i] = sum;
-                atomicOr(table + (w - j0), (uint32_t)(i + 1) << AJ_SLOT_SHIFT);
-            }
-            __syncthreads();
-        }
-        const T* x0 = static_cast<const T*>(a.logits) + row * a.stride;
-        T* y0 = static_cast<T*>(a.out) + row * a.out_stride;
-        const T* b0 = a.r.bias ? static_cast<const T*>(a.r.bias) + row * a.r.bias_stride : nullptr;
-        const uint32_t* m0 = a.r.mask ? a.r.mask + row * a.r.mask_stride : nullptr;
-        constexpr uint32_t ALL = (1u << N) - 1u;
-        for (int u = threadIdx.x * N; u < width; u += AJ_THREADS * N) {
-            const int j = j0 + u, count = min(N, width - u);
-            const uint32_t live = mask_bits<N>(m0, j);
-            uint32_t t[N], any = 0;
-            if constexpr (TABLE) {
-#pragma unroll
-                for (int e = 0; e < N; ++e) { t[e] = e < count ? table[u + e] : 0; any |= t[e]; }
-            }
-            if (place && !b0 && any == 0 && live == ALL) continue;
-            float x[N];
-            if (live != 0) load_n<T, N>(x0 + j, count, x);
-            if constexpr (TABLE) {
-                if (any) {
-#pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        if (t[e] & (AJ_SEEN | AJ_COUNT)) x[e] = x[e] > 0.0f ? __fdiv_rn(x[e], rho) : x[e] * rho;
-                        if (t[e] & AJ_COUNT) x[e] -= fmaf(phi, (float)(t[e] & AJ_COUNT), pi);
-                    }
+            if (a.r.n_bias) {                          // (such rows are not taken in turn)
+                __syncthreads();
+                // the first pair of a word sums the values of all its pairs, in order
+                for (int i = threadIdx.x; i < a.r.n_bias; i += AJ_THREADS) {
+                    const int w = words[i];
+                    if (w < j0 || w >= j0 + width) continue;
+                    bool first = true;
+                    for (int k = 0; k < i && first; ++k) first = words[k] != w;
+                    if (!first) continue;
+                    float sum = 0.0f;
+                    for (int k = i; k < a.r.n_bias; ++k) if (words[k] == w) sum += a.r.value[row * a.r.n_bias + k];
+                    sums[i] = sum;
+                    if (atomicOr(table.word + (w - j0), (uint32_t)(i + 1) << AJ_SLOT_SHIFT) == 0) table.append(w - j0);
                 }
+            }
+            if (place && b0) {                         // the logits will be gone: results go to the table (such rows are not taken in turn either)
+                __syncthreads();
+                for (int i = threadIdx.x; i < listed; i += AJ_THREADS) {
+                    const int j = table.list[i];
+                    table.word[j] = __float_as_uint(adjusted(j));
+                }
+                __syncthreads();
+            }
+        }
+        const Grid<T, N> grid(y0, j0, width);
+        const bool x_phase = same_phase<T, N>(x0, grid.shift, j0), b_phase = b0 && same_phase<T, N>(b0, grid.shift, j0);
+        auto vector = [&](int s, const Vec<T, N>* there) {
+            const uint32_t valid = grid.valid(s);
+            const uint32_t live = m0 ? grid.bits(m0, s, 0, mask_words, valid) : valid;
+            if (sparse && live == valid) return;
+            float x[N];
+            if (live != 0) {
+                if (there && valid == grid.ALL && x_phase) there->get(x);
+                else load_vec<T, N>(x0, s, valid, x_phase, x);
             }
             if (b0) {
                 float b[N];
-                load_n<T, N>(b0 + j, count, b);
+                load_vec<T, N>(b0, s, valid, b_phase, b);
 #pragma unroll
                 for (int e = 0; e < N; ++e) x[e] += b[e];
             }
-            if constexpr (TABLE) {
-                if (any) {
+            if (live != valid) {
 #pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        const uint32_t slot = t[e] >> AJ_SLOT_SHIFT & AJ_SLOT;
-                        if (slot) x[e] += sums[slot - 1];
-                    }
-                }
+                for (int e = 0; e < N; ++e) if (!(live >> e & 1)) x[e] = -INFINITY;
             }
+            store_vec<T, N>(y0, s, valid, true, x);
+        };
+        if (!sparse) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) if (!(live >> e & 1)) x[e] = -INFINITY;
-            store_n<T, N>(y0 + j, count, x);
+            for (int q = 0; q < AJ_UNITS; ++q) {
+                const int s = grid.first(q * AJ_THREADS + threadIdx.x);
+                if (s < grid.j1) vector(s, &ahead.v[q]);
+            }
+        }
+        // (out of place: the vector more that a chunk has when it starts between two boundaries)
+        if (!sparse || m0)
+            for (int s = grid.first((sparse ? 0 : AJ_UNITS * AJ_THREADS) + threadIdx.x); s < grid.j1; s += AJ_THREADS * N) vector(s, nullptr);
+        if constexpr (TABLE) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < listed; i += AJ_THREADS) {
+                const int j = table.list[i];
+                if (allowed(j)) y0[j0 + j] = (T)(place && b0 ? __uint_as_float(table.word[j]) : adjusted(j));
+            }
         }
     }
 }
@@ -214,94 +338,101 @@ struct AdjustGradArgs {
     const void* dout;
     void* dlogits;
     void* dbias;                         // rows of its own (dbias_stride > 0), or null
-    float* partial;                      // shared bias: sums of a group of rows, vocab floats each
+    float* partial;                      // shared bias: sums over the rows of a block of threads, vocab floats each
     float* dvalue;
     long long stride, dout_stride, dlogits_stride, dbias_stride, n_rows;
-    int vocab, chunk, rows_per_group;
+    int vocab, chunk, chunks, rows;
     Rules r;
 };
 
-// A CTA takes a chunk of the vocabulary for a group of rows; SUM: the sums over the group's rows stay in registers, UNITS vectors
-// a thread.
+// SUM: the sums over the rows stay in registers (every row's vectors start at the same column then: 16-byte boundaries, or N = 1).
 template <typename T, int N, bool TABLE, bool SUM>
 __global__ void __launch_bounds__(AJ_THREADS)
 adjust_grad_kernel(const __grid_constant__ AdjustGradArgs a)
 {
-    constexpr int UNITS = SUM ? AJ_MIN_CHUNK / (AJ_THREADS * N) : 1;
-    extern __shared__ uint32_t table[];
-    const int j0 = blockIdx.y * a.chunk, width = min(a.chunk, a.vocab - j0);
+    extern __shared__ __align__(16) uint32_t shared[];
+    __shared__ int listed;
+    const int part = blockIdx.x % a.chunks;
+    const long long group = blockIdx.x / a.chunks, begin = group * a.rows, end = min(begin + a.rows, a.n_rows);
+    const int j0 = part * a.chunk, width = min(a.chunk, a.vocab - j0), mask_words = (a.vocab + 31) / 32;
+    Table table(shared, &listed, a.chunk, j0, width);
     const bool place = a.dlogits == a.dout;
-    const long long begin = (long long)blockIdx.x * a.rows_per_group, end = min(begin + a.rows_per_group, a.n_rows);
-    float sum[UNITS][N];
+    const bool sparse = place && !SUM && !a.dbias;
+    float sum[SUM ? AJ_UNITS : 1][N];
 #pragma unroll
-    for (int k = 0; k < UNITS; ++k)
+    for (int q = 0; q < (SUM ? AJ_UNITS : 1); ++q)
 #pragma unroll
-        for (int e = 0; e < N; ++e) sum[k][e] = 0.0f;
+        for (int e = 0; e < N; ++e) sum[q][e] = 0.0f;
     for (long long row = begin; row < end; ++row) {
-        const T* x0 = static_cast<const T*>(a.logits) + row * a.stride;
-        const T* g0 = static_cast<const T*>(a.dout) + row * a.dout_stride;
-        T* y0 = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
-        T* b0 = a.dbias ? static_cast<T*>(a.dbias) + row * a.dbias_stride : nullptr;
-        const uint32_t* m0 = a.r.mask ? a.r.mask + row * a.r.mask_stride : nullptr;
+        const T* const x0 = static_cast<const T*>(a.logits) + row * a.stride;
+        const T* const g0 = static_cast<const T*>(a.dout) + row * a.dout_stride;
+        T* const y0 = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
+        T* const b0 = a.dbias ? static_cast<T*>(a.dbias) + row * a.dbias_stride : nullptr;
+        const uint32_t* const m0 = a.r.mask ? a.r.mask + row * a.r.mask_stride : nullptr;
+        auto allowed = [&](int w) { return !m0 || (m0[w >> 5] >> (w & 31) & 1u); };
+        Ahead<T, N> ahead;
+        if (!sparse) ahead.read(g0, y0, j0, width);
         float rho = 1.0f;
         if constexpr (TABLE) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < width; i += AJ_THREADS) table[i] = 0;
-            __syncthreads();
             rho = a.r.rho_at ? a.r.rho_at[row] : a.r.rho;
-            count_history(a.r, row, a.vocab, j0, width, table);
-            __syncthreads();
+            table.set(a.r, row, a.vocab, a.chunk);
         }
         if (a.dvalue) {
             // (in place: before anything of the row is overwritten)
             for (int i = threadIdx.x; i < a.r.n_bias; i += AJ_THREADS) {
                 const int w = token_at(a.r.word, row * a.r.n_bias + i, a.r.words64, a.vocab);
-                const bool none = w < 0;
-                if (none ? j0 == 0 : w >= j0 && w < j0 + width)
-                    a.dvalue[row * a.r.n_bias + i] = !none && (mask_bits<1>(m0, w) & 1u) ? (float)g0[w] : 0.0f;
+                if (w < 0 ? j0 == 0 : w >= j0 && w < j0 + width) a.dvalue[row * a.r.n_bias + i] = w >= 0 && allowed(w) ? (float)g0[w] : 0.0f;
             }
             if (place) __syncthreads();
         }
-        constexpr uint32_t ALL = (1u << N) - 1u;
-        int k = 0;
-        for (int u = threadIdx.x * N; u < width; u += AJ_THREADS * N, ++k) {
-            const int j = j0 + u, count = min(N, width - u);
-            const uint32_t live = mask_bits<N>(m0, j);
-            uint32_t t[N], any = 0;
-            if constexpr (TABLE) {
-#pragma unroll
-                for (int e = 0; e < N; ++e) { t[e] = e < count ? table[u + e] : 0; any |= t[e]; }
-            }
-            if (!SUM && place && !b0 && any == 0 && live == ALL) continue;
+        const Grid<T, N> grid(y0, j0, width);
+        const bool g_phase = same_phase<T, N>(g0, grid.shift, j0), b_phase = b0 && same_phase<T, N>(b0, grid.shift, j0);
+        auto vector = [&](int s, const Vec<T, N>* there, float (&total)[N]) {
+            const uint32_t valid = grid.valid(s);
+            const uint32_t live = m0 ? grid.bits(m0, s, 0, mask_words, valid) : valid;
+            if (sparse && live == valid) return;
             float g[N];
-            if (live != 0) load_n<T, N>(g0 + j, count, g);
+            if (there && valid == grid.ALL && g_phase) there->get(g);
+            else load_vec<T, N>(g0, s, live, g_phase && live == grid.ALL, g);
+            if (live != valid) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) if (!(live >> e & 1)) g[e] = 0.0f;
+                for (int e = 0; e < N; ++e) if (!(live >> e & 1)) g[e] = 0.0f;
+            }
             if constexpr (SUM) {
 #pragma unroll
-                for (int q = 0; q < UNITS; ++q)
-                    if (q == k)
-#pragma unroll
-                        for (int e = 0; e < N; ++e) sum[q][e] += g[e];
+                for (int e = 0; e < N; ++e) total[e] += g[e];
             }
-            if (b0) store_n<T, N>(b0 + j, count, g);
-            if constexpr (TABLE) {
-                if (any) {
+            if (b0) store_vec<T, N>(b0, s, valid, b_phase, g);
+            if (!place || live != valid) store_vec<T, N>(y0, s, valid, true, g);
+        };
+        if (!sparse) {
 #pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        if (t[e] && (live >> e & 1)) g[e] = (float)x0[j + e] > 0.0f ? __fdiv_rn(g[e], rho) : g[e] * rho;
-                }
+            for (int q = 0; q < AJ_UNITS; ++q) {
+                const int s = grid.first(q * AJ_THREADS + threadIdx.x);
+                if (s < grid.j1) vector(s, &ahead.v[q], sum[SUM ? q : 0]);
             }
-            if (!place || any || live != ALL) store_n<T, N>(y0 + j, count, g);
+        }
+        if constexpr (!SUM) {
+            if (!sparse || m0)
+                for (int s = grid.first((sparse ? 0 : AJ_UNITS * AJ_THREADS) + threadIdx.x); s < grid.j1; s += AJ_THREADS * N) vector(s, nullptr, sum[0]);
+        }
+        if constexpr (TABLE) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < listed; i += AJ_THREADS) {
+                const int w = j0 + table.list[i];
+                if (!allowed(w)) continue;
+                const float g = (float)g0[w];
+                y0[w] = (T)((float)x0[w] > 0.0f ? __fdiv_rn(g, rho) : g * rho);
+            }
         }
     }
     if constexpr (SUM) {
 #pragma unroll
-        for (int k = 0; k < UNITS; ++k) {
-            const int u = (k * AJ_THREADS + threadIdx.x) * N;
+        for (int q = 0; q < AJ_UNITS; ++q) {
+            const int u = (q * AJ_THREADS + (int)threadIdx.x) * N;
 #pragma unroll
             for (int e = 0; e < N; ++e)
-                if (u + e < width) a.partial[(long long)blockIdx.x * a.vocab + j0 + u + e] = sum[k][e];
+                if (u + e < width) a.partial[group * a.vocab + j0 + u + e] = sum[q][e];
         }
     }
 }
@@ -317,7 +448,9 @@ adjust_bias_join_kernel(const float* __restrict__ partial, int groups, int vocab
     dbias[j] = (T)sum;
 }
 
-constexpr int AJ_MAX_GROUPS = 256;
+constexpr int AJ_MAX_GROUPS = 256;       // rows of partial sums for a shared bias
+constexpr int AJ_PLACE_CHUNK = 16384;    // in place: little is read, so more words for one reading of the history
+constexpr int AJ_MOST_SMEM = (Table::words(AJ_PLACE_CHUNK, AJ_PLACE_CHUNK) + 2 * APOLLO_MAX_BIAS_WORDS) * 4;
 
 bool whole_vectors(const void* p, int64_t stride, size_t e) { return (uintptr_t)p % 16 == 0 && (size_t)stride * e % 16 == 0; }
 
@@ -370,35 +503,80 @@ int check_shape(int64_t n_rows, int64_t vocab, int64_t stride, int32_t dtype)
     return APOLLO_OK;
 }
 
-int pick_chunk(int64_t n_rows, int64_t vocab, int sms)
+// How a call is cut up: chunks of the vocabulary, rows in turn.
+struct Cut { int chunk, chunks, rows; };
+
+// `most`: elements a block of threads can have of a row.  Smaller chunks while there are fewer blocks than the chip holds (a row of
+// history is read once per chunk, so no smaller than that); rows that share a history in turn, as long as 16 blocks per multiprocessor remain.
+Cut cut_up(int64_t n_rows, int64_t vocab, const Rules& r, int most, bool in_turn, int sms)
 {
-    int chunk = AJ_MAX_CHUNK;
-    while (chunk > AJ_MIN_CHUNK && n_rows * ((vocab + chunk - 1) / chunk) < 4LL * sms) chunk /= 2;
-    return chunk;
+    Cut c;
+    c.chunk = most;
+    while (c.chunk > 1024 && n_rows * ((vocab + c.chunk - 1) / c.chunk) < 4LL * sms) c.chunk /= 2;
+    c.chunks = (int)((vocab + c.chunk - 1) / c.chunk);
+    int64_t rows = 1;
+    if (in_turn && r.history && r.share > 1) {
+        rows = n_rows * c.chunks / (16LL * sms);
+        rows = rows < 1 ? 1 : rows > AJ_ROWS ? AJ_ROWS : rows;
+    }
+    c.rows = (int)rows;
+    return c;
 }
 
-template <typename T, int N>
-cudaError_t run_adjust(const AdjustArgs& a, cudaStream_t stream)
+// Words of a chunk that can be listed.
+int list_entries(const Rules& r, int named, int chunk)
 {
-    const dim3 grid((unsigned)a.n_rows, (unsigned)((a.vocab + a.chunk - 1) / a.chunk));
-    if (a.r.history || a.r.n_bias) adjust_kernel<T, N, true><<<grid, AJ_THREADS, (size_t)(a.chunk + 2 * a.r.n_bias) * 4, stream>>>(a);
-    else adjust_kernel<T, N, false><<<grid, AJ_THREADS, 0, stream>>>(a);
-    return cudaGetLastError();
+    const int64_t n = (int64_t)(r.history ? r.history_len : 0) + named;
+    return (int)(n < chunk ? n : chunk);
 }
 
-template <typename T, int N>
-cudaError_t run_adjust_grad(AdjustGradArgs a, int groups, cudaStream_t stream)
+template <typename T>
+cudaError_t run_adjust(AdjustArgs a, int sms, cudaStream_t stream)
 {
-    const dim3 grid((unsigned)groups, (unsigned)((a.vocab + a.chunk - 1) / a.chunk));
-    const size_t smem = a.r.history ? (size_t)a.chunk * 4 : 0;
-    if (a.partial) {
-        if (a.r.history) adjust_grad_kernel<T, N, true, true><<<grid, AJ_THREADS, smem, stream>>>(a);
-        else adjust_grad_kernel<T, N, false, true><<<grid, AJ_THREADS, smem, stream>>>(a);
+    constexpr int N = 16 / sizeof(T);
+    const bool place = a.logits == a.out;
+    const Cut c = cut_up(a.n_rows, a.vocab, a.r, place && !a.r.bias ? AJ_PLACE_CHUNK : AJ_UNITS * AJ_THREADS * N, !(place && a.r.bias) && a.r.n_bias == 0, sms);
+    a.chunk = c.chunk; a.chunks = c.chunks; a.rows = c.rows;
+    a.entries = list_entries(a.r, a.r.n_bias, c.chunk);
+    const int64_t blocks = (a.n_rows + c.rows - 1) / c.rows * c.chunks;
+    if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
+    const unsigned grid = (unsigned)blocks;
+    if (a.r.history || a.r.n_bias) {
+        const int smem = (Table::words(c.chunk, a.entries) + 2 * a.r.n_bias) * 4;
+        const cudaError_t e = cudaFuncSetAttribute(adjust_kernel<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AJ_MOST_SMEM);
+        if (e != cudaSuccess) return e;
+        adjust_kernel<T, true><<<grid, AJ_THREADS, smem, stream>>>(a);
     } else {
-        if (a.r.history) adjust_grad_kernel<T, N, true, false><<<grid, AJ_THREADS, smem, stream>>>(a);
-        else adjust_grad_kernel<T, N, false, false><<<grid, AJ_THREADS, smem, stream>>>(a);
+        adjust_kernel<T, false><<<grid, AJ_THREADS, 0, stream>>>(a);
     }
     return cudaGetLastError();
+}
+
+template <typename T, int N>
+cudaError_t run_adjust_grad(AdjustGradArgs a, int sms, int* groups, cudaStream_t stream)
+{
+    const bool sum = a.partial != nullptr, sparse = a.dlogits == a.dout && !sum && !a.dbias;
+    Cut c;
+    if (sum) {
+        c.chunk = AJ_UNITS * AJ_THREADS * N;
+        c.chunks = (a.vocab + c.chunk - 1) / c.chunk;
+        c.rows = (int)((a.n_rows + AJ_MAX_GROUPS - 1) / AJ_MAX_GROUPS);
+    } else {
+        c = cut_up(a.n_rows, a.vocab, a.r, sparse ? AJ_PLACE_CHUNK : AJ_UNITS * AJ_THREADS * N, true, sms);
+    }
+    a.chunk = c.chunk; a.chunks = c.chunks; a.rows = c.rows;
+    *groups = (int)((a.n_rows + c.rows - 1) / c.rows);
+    if ((int64_t)*groups * c.chunks > INT32_MAX) return cudaErrorInvalidConfiguration;
+    const unsigned grid = (unsigned)(*groups * c.chunks);
+    const int smem = a.r.history ? Table::words(c.chunk, list_entries(a.r, 0, c.chunk)) * 4 : 0;
+    auto launch = [&](auto* kernel) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, AJ_MOST_SMEM);
+        if (e != cudaSuccess) return e;
+        kernel<<<grid, AJ_THREADS, smem, stream>>>(a);
+        return cudaGetLastError();
+    };
+    if (sum) return a.r.history ? launch(adjust_grad_kernel<T, N, true, true>) : launch(adjust_grad_kernel<T, N, false, true>);
+    return a.r.history ? launch(adjust_grad_kernel<T, N, true, false>) : launch(adjust_grad_kernel<T, N, false, false>);
 }
 
 }  // namespace
@@ -425,12 +603,8 @@ extern "C" int apollo_adjust_logits(const void* d_logits, int64_t row_stride, in
     rc = device_sms(&sms);
     if (rc != APOLLO_OK) return rc;
     a.logits = d_logits; a.out = d_out; a.stride = row_stride; a.out_stride = out_stride; a.n_rows = n_rows; a.vocab = (int)vocab;
-    a.chunk = pick_chunk(n_rows, vocab, sms);
-    const bool vec = whole_vectors(d_logits, row_stride, e) && whole_vectors(d_out, out_stride, e) && whole_vectors(a.r.bias, a.r.bias_stride, e);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    cudaError_t err;
-    if (dtype == APOLLO_DT_BF16) err = vec ? run_adjust<__nv_bfloat16, 8>(a, stream) : run_adjust<__nv_bfloat16, 1>(a, stream);
-    else err = vec ? run_adjust<float, 4>(a, stream) : run_adjust<float, 1>(a, stream);
+    const cudaError_t err = dtype == APOLLO_DT_BF16 ? run_adjust<__nv_bfloat16>(a, sms, stream) : run_adjust<float>(a, sms, stream);
     return err == cudaSuccess ? APOLLO_OK : APOLLO_ERR_CUDA;
 }
 
@@ -481,14 +655,12 @@ extern "C" int apollo_adjust_logits_grad(const void* d_logits, int64_t row_strid
     a.partial = shared ? static_cast<float*>(d_workspace) : nullptr; a.dvalue = a.r.n_bias ? d_grad_value : nullptr;
     a.stride = row_stride; a.dout_stride = grad_out_stride; a.dlogits_stride = grad_logits_stride; a.dbias_stride = grad_bias_stride;
     a.n_rows = n_rows; a.vocab = (int)vocab;
-    a.chunk = shared ? AJ_MIN_CHUNK : pick_chunk(n_rows, vocab, sms);
-    a.rows_per_group = shared ? (int)((n_rows + AJ_MAX_GROUPS - 1) / AJ_MAX_GROUPS) : 1;
-    const int groups = (int)((n_rows + a.rows_per_group - 1) / a.rows_per_group);
-    const bool vec = whole_vectors(d_grad_out, grad_out_stride, e) && whole_vectors(d_grad_logits, grad_logits_stride, e) &&
-                     whole_vectors(a.dbias, a.dbias ? grad_bias_stride : 0, e);
+    // sums over rows whose vectors start at different columns go element by element
+    const bool vec = !shared || whole_vectors(d_grad_logits, grad_logits_stride, e);
+    int groups = 0;
     cudaError_t err;
-    if (dtype == APOLLO_DT_BF16) err = vec ? run_adjust_grad<__nv_bfloat16, 8>(a, groups, stream) : run_adjust_grad<__nv_bfloat16, 1>(a, groups, stream);
-    else err = vec ? run_adjust_grad<float, 4>(a, groups, stream) : run_adjust_grad<float, 1>(a, groups, stream);
+    if (dtype == APOLLO_DT_BF16) err = vec ? run_adjust_grad<__nv_bfloat16, 8>(a, sms, &groups, stream) : run_adjust_grad<__nv_bfloat16, 1>(a, sms, &groups, stream);
+    else err = vec ? run_adjust_grad<float, 4>(a, sms, &groups, stream) : run_adjust_grad<float, 1>(a, sms, &groups, stream);
     if (err == cudaSuccess && shared) {
         const unsigned grid = (unsigned)((vocab + AJ_THREADS - 1) / AJ_THREADS);
         if (dtype == APOLLO_DT_BF16) adjust_bias_join_kernel<<<grid, AJ_THREADS, 0, stream>>>(a.partial, groups, (int)vocab, static_cast<__nv_bfloat16*>(d_grad_bias));
