@@ -25,6 +25,7 @@ namespace {
 
 constexpr int AJ_THREADS = 256;
 constexpr int AJ_UNITS = 4;              // vectors a thread has of a row's chunk at once
+constexpr int AJ_BATCH = 4;              // loads a thread has in flight where they are scattered
 constexpr int AJ_ROWS = 16;              // most rows in turn, without sums
 constexpr uint32_t AJ_SEEN = 0x80000000u;
 constexpr int AJ_SLOT_SHIFT = 20;
@@ -82,10 +83,15 @@ struct Table {
     __device__ __forceinline__ void scan(const Rules& r, int vocab, int from, int to, F f)
     {
         const long long first = history * r.history_stride;
-#pragma unroll 4
-        for (int i = from + (int)threadIdx.x; i < to; i += AJ_THREADS) {
-            const int j = token_at(r.history, first + i, r.history64, vocab) - j0;
-            if (j >= 0 && j < width) f(j, i);
+        for (int i = from + (int)threadIdx.x; i < to; i += AJ_THREADS * AJ_BATCH) {
+            int j[AJ_BATCH];
+#pragma unroll
+            for (int k = 0; k < AJ_BATCH; ++k) {
+                const int at = i + k * AJ_THREADS;
+                j[k] = at < to ? token_at(r.history, first + at, r.history64, vocab) - j0 : -1;
+            }
+#pragma unroll
+            for (int k = 0; k < AJ_BATCH; ++k) if (j[k] >= 0 && j[k] < width) f(j[k], i + k * AJ_THREADS);
         }
     }
     // The table of `row`, from that of the row before it where both have the same history.  Begins with a barrier; the caller ends with one.
@@ -113,105 +119,93 @@ struct Table {
     }
 };
 
-template <typename T, int N> struct Vec;
-template <typename T> struct Vec<T, 1> {
-    T v;
-    __device__ __forceinline__ void get(float (&x)[1]) const { x[0] = (float)v; }
-    __device__ __forceinline__ void set(const float (&x)[1]) { v = (T)x[0]; }
-};
-template <> struct Vec<float, 4> {
-    float4 v;
-    __device__ __forceinline__ void get(float (&x)[4]) const { x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
-    __device__ __forceinline__ void set(const float (&x)[4]) { v = make_float4(x[0], x[1], x[2], x[3]); }
-};
-template <> struct Vec<__nv_bfloat16, 8> {
-    uint4 v;
-    __device__ __forceinline__ void get(float (&x)[8]) const { unpack_bf16x8(v, x); }
-    __device__ __forceinline__ void set(const float (&x)[8])
+// Sixteen bytes of a row: N elements.
+template <typename T> struct Sixteen;
+template <> struct Sixteen<float> {
+    static constexpr int N = 4;
+    using Entry = uint4;                 // of the table that makes 32-bit masks of mask bits, four bits at a time
+    __device__ static __forceinline__ Entry entry(int bits) { return make_uint4(-(bits & 1), -(bits >> 1 & 1), -(bits >> 2 & 1), -(bits >> 3 & 1)); }
+    __device__ static __forceinline__ uint4 masks(const Entry* t, uint32_t bits) { return t[bits]; }
+    __device__ static __forceinline__ uint32_t minus_inf() { return 0xFF800000u; }
+    __device__ static __forceinline__ void unpack(const uint4& w, float (&x)[4])
     {
-        v = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+        x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
+    }
+    __device__ static __forceinline__ uint4 pack(const float (&x)[4])
+    {
+        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    }
+    __device__ static __forceinline__ uint4 gather(const float* p)
+    {
+        return make_uint4(__float_as_uint(p[0]), __float_as_uint(p[1]), __float_as_uint(p[2]), __float_as_uint(p[3]));
+    }
+};
+template <> struct Sixteen<__nv_bfloat16> {
+    static constexpr int N = 8;
+    using Entry = uint2;
+    __device__ static __forceinline__ Entry entry(int bits)
+    {
+        return make_uint2((bits & 1) * 0xFFFFu | (bits >> 1 & 1) * 0xFFFF0000u, (bits >> 2 & 1) * 0xFFFFu | (bits >> 3 & 1) * 0xFFFF0000u);
+    }
+    __device__ static __forceinline__ uint4 masks(const Entry* t, uint32_t bits)
+    {
+        const uint2 a = t[bits & 15], b = t[bits >> 4];
+        return make_uint4(a.x, a.y, b.x, b.y);
+    }
+    __device__ static __forceinline__ uint32_t minus_inf() { return 0xFF80FF80u; }
+    __device__ static __forceinline__ void unpack(const uint4& w, float (&x)[8]) { unpack_bf16x8(w, x); }
+    __device__ static __forceinline__ uint4 pack(const float (&x)[8])
+    {
+        return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+    }
+    __device__ static __forceinline__ uint4 gather(const __nv_bfloat16* p)
+    {
+        const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
+        return make_uint4(q[0] | (uint32_t)q[1] << 16, q[2] | (uint32_t)q[3] << 16, q[4] | (uint32_t)q[5] << 16, q[6] | (uint32_t)q[7] << 16);
     }
 };
 
-// N bits from `bit` on.
-template <int N>
-__device__ __forceinline__ uint32_t bits_at(const uint32_t* words, int bit, int n_words)
+__device__ __forceinline__ uint4 select4(const uint4& m, const uint4& w, uint32_t other)
 {
-    const int w = bit >> 5, at = bit & 31;
-    const uint32_t lo = words[w], hi = N > 1 && at + N > 32 && w + 1 < n_words ? words[w + 1] : 0;
+    return make_uint4((w.x & m.x) | (other & ~m.x), (w.y & m.y) | (other & ~m.y), (w.z & m.z) | (other & ~m.z), (w.w & m.w) | (other & ~m.w));
+}
+
+// N mask bits from column j on.
+template <int N>
+__device__ __forceinline__ uint32_t bits_at(const uint32_t* words, int j, int n_words)
+{
+    const int w = j >> 5, at = j & 31;
+    const uint32_t lo = words[w], hi = at + N > 32 && w + 1 < n_words ? words[w + 1] : 0;
     return __funnelshift_r(lo, hi, at) & ((1u << N) - 1u);
 }
+__device__ __forceinline__ bool allowed(const uint32_t* words, int j) { return !words || (words[j >> 5] >> (j & 31) & 1u); }
 
-// The vectors of a chunk of a row: they start where 16-byte boundaries of `out` are, the first and the last are cut at the chunk's ends.
-template <typename T, int N>
-struct Grid {
-    static constexpr uint32_t ALL = (1u << N) - 1u;
-    int j0, j1, shift;
-    __device__ __forceinline__ Grid(const T* out, int first, int width) : j0(first), j1(first + width)
+// A chunk of a row cut at the 16-byte boundaries of `out`: `full` vectors from column `first` on, the columns before and behind one by one.
+template <typename T>
+struct Span {
+    static constexpr int N = Sixteen<T>::N;
+    int first, full, head, tail;
+    __device__ __forceinline__ Span(const T* out, int j0, int width)
     {
-        shift = N == 1 ? 0 : (int)(((uintptr_t)(out + first) & 15) / sizeof(T));
+        head = min((int)((16 - ((uintptr_t)(out + j0) & 15)) % 16 / sizeof(T)), width);
+        first = j0 + head;
+        full = (width - head) / N;
+        tail = width - head - full * N;
     }
-    __device__ __forceinline__ int first(int u) const { return j0 - shift + u * N; }
-    __device__ __forceinline__ uint32_t valid(int s) const
+    // the column that this thread has apart from the vectors, or -1 (N <= 8: lanes of the first two warps)
+    __device__ __forceinline__ int single() const
     {
-        uint32_t v = ALL;
-        if (s < j0) v = v << (j0 - s) & ALL;
-        if (s + N > j1) v &= j1 > s ? (1u << (j1 - s)) - 1u : 0u;
-        return v;
-    }
-    // bits of the vector's elements, those outside the chunk unset
-    __device__ __forceinline__ uint32_t bits(const uint32_t* words, int s, int base, int n_words, uint32_t valid) const
-    {
-        const int lo = s > j0 ? s : j0;
-        return bits_at<N>(words, lo - base, n_words) << (lo - s) & valid;
+        const int t = threadIdx.x;
+        return t < head ? first - head + t : t >= 32 && t - 32 < tail ? first + full * N + t - 32 : -1;
     }
 };
-
-template <typename T, int N>
-__device__ __forceinline__ bool same_phase(const T* p, int shift, int first)
+template <typename T>
+__device__ __forceinline__ bool on_boundary(const T* row, int first) { return ((uintptr_t)(row + first) & 15) == 0; }
+template <typename T>
+__device__ __forceinline__ uint4 load16(const T* p, bool aligned)
 {
-    return N == 1 || (int)(((uintptr_t)(p + first) & 15) / sizeof(T)) == shift;
+    return aligned ? *reinterpret_cast<const uint4*>(p) : Sixteen<T>::gather(p);
 }
-
-// Elements of a vector at columns s ...: one access where it is whole and on a 16-byte boundary.
-template <typename T, int N>
-__device__ __forceinline__ void load_vec(const T* row, int s, uint32_t valid, bool phase, float (&x)[N])
-{
-    if (valid == Grid<T, N>::ALL && phase) {
-        reinterpret_cast<const Vec<T, N>*>(row + s)->get(x);
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = valid >> e & 1 ? (float)row[s + e] : 0.0f;
-    }
-}
-template <typename T, int N>
-__device__ __forceinline__ void store_vec(T* row, int s, uint32_t valid, bool phase, const float (&x)[N])
-{
-    if (valid == Grid<T, N>::ALL && phase) {
-        Vec<T, N> v;
-        v.set(x);
-        *reinterpret_cast<Vec<T, N>*>(row + s) = v;
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) if (valid >> e & 1) row[s + e] = (T)x[e];
-    }
-}
-
-// The whole vectors of a row that a thread will need, read before its table is there.
-template <typename T, int N>
-struct Ahead {
-    Vec<T, N> v[AJ_UNITS];
-    __device__ __forceinline__ void read(const T* in, const T* out, int j0, int width)
-    {
-        const Grid<T, N> grid(out, j0, width);
-        if (!same_phase<T, N>(in, grid.shift, j0)) return;
-#pragma unroll
-        for (int q = 0; q < AJ_UNITS; ++q) {
-            const int s = grid.first(q * AJ_THREADS + threadIdx.x);
-            if (s >= j0 && s + N <= grid.j1) v[q] = *reinterpret_cast<const Vec<T, N>*>(in + s);
-        }
-    }
-};
 
 struct AdjustArgs {
     const void* logits;
@@ -227,9 +221,13 @@ template <typename T, bool TABLE>
 __global__ void __launch_bounds__(AJ_THREADS)
 adjust_kernel(const __grid_constant__ AdjustArgs a)
 {
-    constexpr int N = 16 / sizeof(T);
+    using S = Sixteen<T>;
+    constexpr int N = S::N;
     extern __shared__ __align__(16) uint32_t shared[];
+    __shared__ typename S::Entry masks[16];
     __shared__ int listed;
+    if (threadIdx.x < 16) masks[threadIdx.x] = S::entry((int)threadIdx.x);
+    if constexpr (!TABLE) __syncthreads();             // (otherwise there will be one)
     const int part = blockIdx.x % a.chunks;
     const long long begin = (long long)(blockIdx.x / a.chunks) * a.rows, end = min(begin + a.rows, a.n_rows);
     const int j0 = part * a.chunk, width = min(a.chunk, a.vocab - j0), mask_words = (a.vocab + 31) / 32;
@@ -242,8 +240,17 @@ adjust_kernel(const __grid_constant__ AdjustArgs a)
         T* const y0 = static_cast<T*>(a.out) + row * a.out_stride;
         const T* const b0 = a.r.bias ? static_cast<const T*>(a.r.bias) + row * a.r.bias_stride : nullptr;
         const uint32_t* const m0 = a.r.mask ? a.r.mask + row * a.r.mask_stride : nullptr;
-        Ahead<T, N> ahead;
-        if (!sparse) ahead.read(x0, y0, j0, width);
+        const Span<T> span(y0, j0, width);
+        const bool x_aligned = on_boundary(x0, span.first), b_aligned = b0 && on_boundary(b0, span.first);
+        // read before the table is there
+        uint4 ahead[AJ_UNITS];
+        if (!sparse) {
+#pragma unroll
+            for (int q = 0; q < AJ_UNITS; ++q) {
+                const int u = q * AJ_THREADS + threadIdx.x;
+                if (u < span.full) ahead[q] = load16(x0 + span.first + u * N, x_aligned);
+            }
+        }
         float rho = 1.0f, phi = 0.0f, pi = 0.0f;
         // the word's logit with everything that concerns it
         auto adjusted = [&](int j) {
@@ -255,7 +262,6 @@ adjust_kernel(const __grid_constant__ AdjustArgs a)
             const uint32_t slot = t >> AJ_SLOT_SHIFT & AJ_SLOT;
             return slot ? x + sums[slot - 1] : x;
         };
-        auto allowed = [&](int j) { return !m0 || (m0[(j0 + j) >> 5] >> ((j0 + j) & 31) & 1u); };
         if constexpr (TABLE) {
             for (int i = threadIdx.x; i < a.r.n_bias; i += AJ_THREADS) words[i] = token_at(a.r.word, row * a.r.n_bias + i, a.r.words64, a.vocab);
             if (a.r.history) {
@@ -290,44 +296,50 @@ adjust_kernel(const __grid_constant__ AdjustArgs a)
                 __syncthreads();
             }
         }
-        const Grid<T, N> grid(y0, j0, width);
-        const bool x_phase = same_phase<T, N>(x0, grid.shift, j0), b_phase = b0 && same_phase<T, N>(b0, grid.shift, j0);
-        auto vector = [&](int s, const Vec<T, N>* there) {
-            const uint32_t valid = grid.valid(s);
-            const uint32_t live = m0 ? grid.bits(m0, s, 0, mask_words, valid) : valid;
-            if (sparse && live == valid) return;
-            float x[N];
-            if (live != 0) {
-                if (there && valid == grid.ALL && x_phase) there->get(x);
-                else load_vec<T, N>(x0, s, valid, x_phase, x);
-            }
-            if (b0) {
-                float b[N];
-                load_vec<T, N>(b0, s, valid, b_phase, b);
-#pragma unroll
-                for (int e = 0; e < N; ++e) x[e] += b[e];
-            }
-            if (live != valid) {
-#pragma unroll
-                for (int e = 0; e < N; ++e) if (!(live >> e & 1)) x[e] = -INFINITY;
-            }
-            store_vec<T, N>(y0, s, valid, true, x);
-        };
         if (!sparse) {
 #pragma unroll
             for (int q = 0; q < AJ_UNITS; ++q) {
-                const int s = grid.first(q * AJ_THREADS + threadIdx.x);
-                if (s < grid.j1) vector(s, &ahead.v[q]);
+                const int u = q * AJ_THREADS + threadIdx.x, j = span.first + u * N;
+                if (u >= span.full) break;
+                uint4 w = ahead[q];
+                if (b0) {
+                    float x[N], b[N];
+                    S::unpack(w, x);
+                    S::unpack(load16(b0 + j, b_aligned), b);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) x[e] += b[e];
+                    w = S::pack(x);
+                }
+                if (m0) w = select4(S::masks(masks, bits_at<N>(m0, j, mask_words)), w, S::minus_inf());
+                *reinterpret_cast<uint4*>(y0 + j) = w;
+            }
+        } else if (m0) {
+            for (int u = threadIdx.x; u < span.full; u += AJ_THREADS) {
+                const int j = span.first + u * N;
+                const uint32_t live = bits_at<N>(m0, j, mask_words);
+                if (live == (1u << N) - 1u) continue;
+                uint4* const y = reinterpret_cast<uint4*>(y0 + j);
+                *y = select4(S::masks(masks, live), live ? *y : make_uint4(0, 0, 0, 0), S::minus_inf());
             }
         }
-        // (out of place: the vector more that a chunk has when it starts between two boundaries)
-        if (!sparse || m0)
-            for (int s = grid.first((sparse ? 0 : AJ_UNITS * AJ_THREADS) + threadIdx.x); s < grid.j1; s += AJ_THREADS * N) vector(s, nullptr);
+        if (const int j = span.single(); j >= 0) {
+            if (!allowed(m0, j)) y0[j] = (T)-INFINITY;
+            else if (!sparse) y0[j] = (T)(b0 ? (float)x0[j] + (float)b0[j] : (float)x0[j]);
+        }
         if constexpr (TABLE) {
             __syncthreads();
-            for (int i = threadIdx.x; i < listed; i += AJ_THREADS) {
-                const int j = table.list[i];
-                if (allowed(j)) y0[j0 + j] = (T)(place && b0 ? __uint_as_float(table.word[j]) : adjusted(j));
+            const int n = listed;
+            for (int i = threadIdx.x; i < n; i += AJ_THREADS * AJ_BATCH) {
+                float y[AJ_BATCH];
+                int at[AJ_BATCH];
+#pragma unroll
+                for (int k = 0; k < AJ_BATCH; ++k) {
+                    const int j = i + k * AJ_THREADS < n ? table.list[i + k * AJ_THREADS] : -1;
+                    at[k] = j >= 0 && allowed(m0, j0 + j) ? j0 + j : -1;
+                    if (at[k] >= 0) y[k] = place && b0 ? __uint_as_float(table.word[j]) : adjusted(j);
+                }
+#pragma unroll
+                for (int k = 0; k < AJ_BATCH; ++k) if (at[k] >= 0) y0[at[k]] = (T)y[k];
             }
         }
     }
@@ -345,20 +357,28 @@ struct AdjustGradArgs {
     Rules r;
 };
 
-// SUM: the sums over the rows stay in registers (every row's vectors start at the same column then: 16-byte boundaries, or N = 1).
-template <typename T, int N, bool TABLE, bool SUM>
+__device__ __forceinline__ void store_partial(float* p, float a, float b, float c, float d) { p[0] = a; p[1] = b; p[2] = c; p[3] = d; }
+
+// SUM: the sums over the rows stay in registers.  Every row's vectors have to start at the same columns then; where they do not,
+// WIDE = false takes the columns one by one.
+template <typename T, bool TABLE, bool SUM, bool WIDE>
 __global__ void __launch_bounds__(AJ_THREADS)
 adjust_grad_kernel(const __grid_constant__ AdjustGradArgs a)
 {
+    using S = Sixteen<T>;
+    constexpr int N = WIDE ? S::N : 1;
     extern __shared__ __align__(16) uint32_t shared[];
+    __shared__ typename S::Entry masks[16];
     __shared__ int listed;
+    if (threadIdx.x < 16) masks[threadIdx.x] = S::entry((int)threadIdx.x);
+    if constexpr (!TABLE) __syncthreads();             // (otherwise there will be one)
     const int part = blockIdx.x % a.chunks;
     const long long group = blockIdx.x / a.chunks, begin = group * a.rows, end = min(begin + a.rows, a.n_rows);
     const int j0 = part * a.chunk, width = min(a.chunk, a.vocab - j0), mask_words = (a.vocab + 31) / 32;
     Table table(shared, &listed, a.chunk, j0, width);
     const bool place = a.dlogits == a.dout;
     const bool sparse = place && !SUM && !a.dbias;
-    float sum[SUM ? AJ_UNITS : 1][N];
+    float sum[SUM ? AJ_UNITS : 1][N], edge = 0.0f;
 #pragma unroll
     for (int q = 0; q < (SUM ? AJ_UNITS : 1); ++q)
 #pragma unroll
@@ -369,9 +389,19 @@ adjust_grad_kernel(const __grid_constant__ AdjustGradArgs a)
         T* const y0 = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
         T* const b0 = a.dbias ? static_cast<T*>(a.dbias) + row * a.dbias_stride : nullptr;
         const uint32_t* const m0 = a.r.mask ? a.r.mask + row * a.r.mask_stride : nullptr;
-        auto allowed = [&](int w) { return !m0 || (m0[w >> 5] >> (w & 31) & 1u); };
-        Ahead<T, N> ahead;
-        if (!sparse) ahead.read(g0, y0, j0, width);
+        const Span<T> span(y0, j0, width);
+        const bool g_aligned = on_boundary(g0, span.first), b_aligned = b0 && on_boundary(b0, span.first);
+        // read before the table is there
+        uint4 ahead[WIDE ? AJ_UNITS : 1];
+        if constexpr (WIDE) {
+            if (!sparse) {
+#pragma unroll
+                for (int q = 0; q < AJ_UNITS; ++q) {
+                    const int u = q * AJ_THREADS + threadIdx.x;
+                    if (u < span.full) ahead[q] = load16(g0 + span.first + u * N, g_aligned);
+                }
+            }
+        }
         float rho = 1.0f;
         if constexpr (TABLE) {
             rho = a.r.rho_at ? a.r.rho_at[row] : a.r.rho;
@@ -381,48 +411,74 @@ adjust_grad_kernel(const __grid_constant__ AdjustGradArgs a)
             // (in place: before anything of the row is overwritten)
             for (int i = threadIdx.x; i < a.r.n_bias; i += AJ_THREADS) {
                 const int w = token_at(a.r.word, row * a.r.n_bias + i, a.r.words64, a.vocab);
-                if (w < 0 ? j0 == 0 : w >= j0 && w < j0 + width) a.dvalue[row * a.r.n_bias + i] = w >= 0 && allowed(w) ? (float)g0[w] : 0.0f;
+                if (w < 0 ? j0 == 0 : w >= j0 && w < j0 + width) a.dvalue[row * a.r.n_bias + i] = w >= 0 && allowed(m0, w) ? (float)g0[w] : 0.0f;
             }
             if (place) __syncthreads();
         }
-        const Grid<T, N> grid(y0, j0, width);
-        const bool g_phase = same_phase<T, N>(g0, grid.shift, j0), b_phase = b0 && same_phase<T, N>(b0, grid.shift, j0);
-        auto vector = [&](int s, const Vec<T, N>* there, float (&total)[N]) {
-            const uint32_t valid = grid.valid(s);
-            const uint32_t live = m0 ? grid.bits(m0, s, 0, mask_words, valid) : valid;
-            if (sparse && live == valid) return;
-            float g[N];
-            if (there && valid == grid.ALL && g_phase) there->get(g);
-            else load_vec<T, N>(g0, s, live, g_phase && live == grid.ALL, g);
-            if (live != valid) {
-#pragma unroll
-                for (int e = 0; e < N; ++e) if (!(live >> e & 1)) g[e] = 0.0f;
-            }
-            if constexpr (SUM) {
-#pragma unroll
-                for (int e = 0; e < N; ++e) total[e] += g[e];
-            }
-            if (b0) store_vec<T, N>(b0, s, valid, b_phase, g);
-            if (!place || live != valid) store_vec<T, N>(y0, s, valid, true, g);
+        auto column = [&](int j, float& total) {
+            const float g = allowed(m0, j) ? (float)g0[j] : 0.0f;
+            if constexpr (SUM) total += g;
+            if (b0) b0[j] = (T)g;
+            y0[j] = (T)g;
         };
-        if (!sparse) {
+        if constexpr (!WIDE) {
 #pragma unroll
             for (int q = 0; q < AJ_UNITS; ++q) {
-                const int s = grid.first(q * AJ_THREADS + threadIdx.x);
-                if (s < grid.j1) vector(s, &ahead.v[q], sum[SUM ? q : 0]);
+                const int u = q * AJ_THREADS + threadIdx.x;
+                if (u < width) column(j0 + u, sum[q][0]);
             }
-        }
-        if constexpr (!SUM) {
-            if (!sparse || m0)
-                for (int s = grid.first((sparse ? 0 : AJ_UNITS * AJ_THREADS) + threadIdx.x); s < grid.j1; s += AJ_THREADS * N) vector(s, nullptr, sum[0]);
+        } else {
+            if (!sparse) {
+#pragma unroll
+                for (int q = 0; q < AJ_UNITS; ++q) {
+                    const int u = q * AJ_THREADS + threadIdx.x, j = span.first + u * N;
+                    if (u >= span.full) break;
+                    uint4 w = ahead[q];
+                    if (m0) w = select4(S::masks(masks, bits_at<N>(m0, j, mask_words)), w, 0);
+                    if constexpr (SUM) {
+                        float g[N];
+                        S::unpack(w, g);
+#pragma unroll
+                        for (int e = 0; e < N; ++e) sum[q][e] += g[e];
+                    }
+                    if (b0) {
+                        if (b_aligned) {
+                            *reinterpret_cast<uint4*>(b0 + j) = w;
+                        } else {
+                            float g[N];
+                            S::unpack(w, g);
+#pragma unroll
+                            for (int e = 0; e < N; ++e) b0[j + e] = (T)g[e];
+                        }
+                    }
+                    if (!place || m0) *reinterpret_cast<uint4*>(y0 + j) = w;
+                }
+            } else if (m0) {
+                for (int u = threadIdx.x; u < span.full; u += AJ_THREADS) {
+                    const int j = span.first + u * N;
+                    const uint32_t live = bits_at<N>(m0, j, mask_words);
+                    if (live == (1u << N) - 1u) continue;
+                    uint4* const y = reinterpret_cast<uint4*>(y0 + j);
+                    *y = select4(S::masks(masks, live), live ? *y : make_uint4(0, 0, 0, 0), 0);
+                }
+            }
+            if (const int j = span.single(); j >= 0) column(j, edge);
         }
         if constexpr (TABLE) {
             __syncthreads();
-            for (int i = threadIdx.x; i < listed; i += AJ_THREADS) {
-                const int w = j0 + table.list[i];
-                if (!allowed(w)) continue;
-                const float g = (float)g0[w];
-                y0[w] = (T)((float)x0[w] > 0.0f ? __fdiv_rn(g, rho) : g * rho);
+            const int n = listed;
+            for (int i = threadIdx.x; i < n; i += AJ_THREADS * AJ_BATCH) {
+                float g[AJ_BATCH], x[AJ_BATCH];
+                int at[AJ_BATCH];
+#pragma unroll
+                for (int k = 0; k < AJ_BATCH; ++k) {
+                    const int w = i + k * AJ_THREADS < n ? j0 + table.list[i + k * AJ_THREADS] : -1;
+                    at[k] = w >= 0 && allowed(m0, w) ? w : -1;
+                    if (at[k] >= 0) { g[k] = (float)g0[w]; x[k] = (float)x0[w]; }
+                }
+#pragma unroll
+                for (int k = 0; k < AJ_BATCH; ++k)
+                    if (at[k] >= 0) y0[at[k]] = (T)(x[k] > 0.0f ? __fdiv_rn(g[k], rho) : g[k] * rho);
             }
         }
     }
@@ -430,10 +486,16 @@ adjust_grad_kernel(const __grid_constant__ AdjustGradArgs a)
 #pragma unroll
         for (int q = 0; q < AJ_UNITS; ++q) {
             const int u = (q * AJ_THREADS + (int)threadIdx.x) * N;
+            if (WIDE && u + N <= width) {
 #pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (u + e < width) a.partial[group * a.vocab + j0 + u + e] = sum[q][e];
+                for (int e = 0; e < N; e += 4)
+                    if constexpr (N >= 4) store_partial(a.partial + group * a.vocab + j0 + u + e, sum[q][e], sum[q][e + 1], sum[q][e + 2], sum[q][e + 3]);
+            } else if (!WIDE && u < width) {
+                a.partial[group * a.vocab + j0 + u] = sum[q][0];
+            }
         }
+        // (wide rows start on a boundary: the columns left are behind the last whole vector)
+        if (WIDE && threadIdx.x >= 32 && (int)threadIdx.x - 32 < width % N) a.partial[group * a.vocab + j0 + width / N * N + threadIdx.x - 32] = edge;
     }
 }
 
@@ -533,7 +595,7 @@ int list_entries(const Rules& r, int named, int chunk)
 template <typename T>
 cudaError_t run_adjust(AdjustArgs a, int sms, cudaStream_t stream)
 {
-    constexpr int N = 16 / sizeof(T);
+    constexpr int N = Sixteen<T>::N;
     const bool place = a.logits == a.out;
     const Cut c = cut_up(a.n_rows, a.vocab, a.r, place && !a.r.bias ? AJ_PLACE_CHUNK : AJ_UNITS * AJ_THREADS * N, !(place && a.r.bias) && a.r.n_bias == 0, sms);
     a.chunk = c.chunk; a.chunks = c.chunks; a.rows = c.rows;
@@ -552,9 +614,10 @@ cudaError_t run_adjust(AdjustArgs a, int sms, cudaStream_t stream)
     return cudaGetLastError();
 }
 
-template <typename T, int N>
-cudaError_t run_adjust_grad(AdjustGradArgs a, int sms, int* groups, cudaStream_t stream)
+template <typename T>
+cudaError_t run_adjust_grad(AdjustGradArgs a, bool wide, int sms, int* groups, cudaStream_t stream)
 {
+    const int N = wide ? Sixteen<T>::N : 1;
     const bool sum = a.partial != nullptr, sparse = a.dlogits == a.dout && !sum && !a.dbias;
     Cut c;
     if (sum) {
@@ -575,8 +638,9 @@ cudaError_t run_adjust_grad(AdjustGradArgs a, int sms, int* groups, cudaStream_t
         kernel<<<grid, AJ_THREADS, smem, stream>>>(a);
         return cudaGetLastError();
     };
-    if (sum) return a.r.history ? launch(adjust_grad_kernel<T, N, true, true>) : launch(adjust_grad_kernel<T, N, false, true>);
-    return a.r.history ? launch(adjust_grad_kernel<T, N, true, false>) : launch(adjust_grad_kernel<T, N, false, false>);
+    if (!sum) return a.r.history ? launch(adjust_grad_kernel<T, true, false, true>) : launch(adjust_grad_kernel<T, false, false, true>);
+    if (wide) return a.r.history ? launch(adjust_grad_kernel<T, true, true, true>) : launch(adjust_grad_kernel<T, false, true, true>);
+    return a.r.history ? launch(adjust_grad_kernel<T, true, true, false>) : launch(adjust_grad_kernel<T, false, true, false>);
 }
 
 }  // namespace
@@ -656,11 +720,9 @@ extern "C" int apollo_adjust_logits_grad(const void* d_logits, int64_t row_strid
     a.stride = row_stride; a.dout_stride = grad_out_stride; a.dlogits_stride = grad_logits_stride; a.dbias_stride = grad_bias_stride;
     a.n_rows = n_rows; a.vocab = (int)vocab;
     // sums over rows whose vectors start at different columns go element by element
-    const bool vec = !shared || whole_vectors(d_grad_logits, grad_logits_stride, e);
+    const bool wide = !shared || whole_vectors(d_grad_logits, grad_logits_stride, e);
     int groups = 0;
-    cudaError_t err;
-    if (dtype == APOLLO_DT_BF16) err = vec ? run_adjust_grad<__nv_bfloat16, 8>(a, sms, &groups, stream) : run_adjust_grad<__nv_bfloat16, 1>(a, sms, &groups, stream);
-    else err = vec ? run_adjust_grad<float, 4>(a, sms, &groups, stream) : run_adjust_grad<float, 1>(a, sms, &groups, stream);
+    cudaError_t err = dtype == APOLLO_DT_BF16 ? run_adjust_grad<__nv_bfloat16>(a, wide, sms, &groups, stream) : run_adjust_grad<float>(a, wide, sms, &groups, stream);
     if (err == cudaSuccess && shared) {
         const unsigned grid = (unsigned)((vocab + AJ_THREADS - 1) / AJ_THREADS);
         if (dtype == APOLLO_DT_BF16) adjust_bias_join_kernel<<<grid, AJ_THREADS, 0, stream>>>(a.partial, groups, (int)vocab, static_cast<__nv_bfloat16*>(d_grad_bias));
