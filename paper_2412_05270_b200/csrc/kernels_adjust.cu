@@ -60,14 +60,32 @@ __device__ __forceinline__ int token_at(const void* p, long long i, int is64, in
     return v < vocab ? v : -1;
 }
 
+// What a row's table is made of, and its penalties.
+struct Plan { int history, length, start; float rho, phi, pi; };
+
+__device__ __forceinline__ Plan plan_of(const Rules& r, long long row)
+{
+    Plan p{ 0, 0, 0, 1.0f, 0.0f, 0.0f };
+    if (r.history) {
+        p.history = (int)((uint32_t)row / (uint32_t)r.share);             // (both below 2^31)
+        p.length = r.length ? min(max(r.length[row], 0), r.history_len) : r.history_len;
+        p.start = r.start ? min(max(r.start[row], 0), p.length) : 0;
+        p.rho = r.rho_at ? r.rho_at[row] : r.rho;
+        p.phi = r.phi_at ? r.phi_at[row] : r.phi;
+        p.pi = r.pi_at ? r.pi_at[row] : r.pi;
+    }
+    return p;
+}
+
 // The table of a chunk: `chunk` words, and the list of those that are not zero.
 struct Table {
     uint32_t* word;
     uint16_t* list;                      // chunk <= 65536
     int* count;
     int j0, width;
-    long long history = -1;              // what it holds: row of the history, tokens, first counted one
-    int length = 0, start = 0;
+    Plan now{ -1, 0, 0, 0.0f, 0.0f, 0.0f };                // what it holds
+    bool quick = false;
+    int token_more, token_less;
 
     __device__ __forceinline__ Table(uint32_t* at, int* n, int chunk, int first, int w)
         : word(at), list(reinterpret_cast<uint16_t*>(at + chunk)), count(n), j0(first), width(w) {}
@@ -82,7 +100,7 @@ struct Table {
     template <typename F>
     __device__ __forceinline__ void scan(const Rules& r, int vocab, int from, int to, F f)
     {
-        const long long first = history * r.history_stride;
+        const long long first = (long long)now.history * r.history_stride;
         for (int i = from + (int)threadIdx.x; i < to; i += AJ_THREADS * AJ_BATCH) {
             int j[AJ_BATCH];
 #pragma unroll
@@ -94,69 +112,72 @@ struct Table {
             for (int k = 0; k < AJ_BATCH; ++k) if (j[k] >= 0 && j[k] < width) f(j[k], i + k * AJ_THREADS);
         }
     }
-    // The table of `row`, from that of the row before it where both have the same history.  Begins with a barrier; the caller ends with one.
-    __device__ __forceinline__ void set(const Rules& r, long long row, int vocab, int chunk)
+    // Whether the next row's table is this one with a few tokens more, at most one a thread; then they are read now.
+    __device__ __forceinline__ void look_ahead(const Rules& r, const Plan& p, int vocab)
     {
-        const long long mine = row / r.share;
-        const int len = r.length ? min(max(r.length[row], 0), r.history_len) : r.history_len;
-        const int from = r.start ? min(max(r.start[row], 0), len) : 0;
-        __syncthreads();
-        if (mine != history || len < length) {
-            clear(chunk);
-            __syncthreads();
-            history = mine;
-            length = start = 0;
-        }
-        // positions whose count begins or ends, among those the table has
-        if (start < min(from, length)) scan(r, vocab, start, min(from, length), [&](int j, int) { atomicSub(word + j, 1u); });
-        if (from < min(start, length)) scan(r, vocab, from, min(start, length), [&](int j, int) { atomicAdd(word + j, 1u); });
-        scan(r, vocab, length, len, [&](int j, int i) {
+        quick = p.history == now.history && p.length >= now.length && p.length - now.length <= AJ_THREADS && p.start >= now.start &&
+                p.start - now.start <= AJ_THREADS && p.start <= now.length;
+        if (!quick) return;
+        const long long first = (long long)p.history * r.history_stride;
+        const int more = now.length + threadIdx.x, less = now.start + threadIdx.x;
+        token_more = more < p.length ? token_at(r.history, first + more, r.history64, vocab) - j0 : -1;
+        token_less = less < p.start ? token_at(r.history, first + less, r.history64, vocab) - j0 : -1;
+    }
+    // The table of a row, from that of the row before it where both have the same history.  Begins with a barrier; the caller ends with one.
+    __device__ __forceinline__ void set(const Rules& r, const Plan& p, int vocab, int chunk)
+    {
+        auto add = [&](int j, int i) {
             if (!(atomicOr(word + j, AJ_SEEN) & AJ_SEEN)) append(j);
-            if (i >= from) atomicAdd(word + j, 1u);
-        });
-        length = len;
-        start = from;
+            if (i >= p.start) atomicAdd(word + j, 1u);
+        };
+        __syncthreads();
+        if (quick) {
+            if (token_less >= 0 && token_less < width) atomicSub(word + token_less, 1u);
+            if (token_more >= 0 && token_more < width) add(token_more, now.length + (int)threadIdx.x);
+        } else {
+            if (p.history != now.history || p.length < now.length) {
+                clear(chunk);
+                __syncthreads();
+                now.history = p.history;
+                now.length = now.start = 0;
+            }
+            // positions whose count begins or ends, among those the table has
+            scan(r, vocab, now.start, min(p.start, now.length), [&](int j, int) { atomicSub(word + j, 1u); });
+            scan(r, vocab, p.start, min(now.start, now.length), [&](int j, int) { atomicAdd(word + j, 1u); });
+            scan(r, vocab, now.length, p.length, add);
+        }
+        now = p;
     }
 };
 
-// Sixteen bytes of a row: N elements.
+// Sixteen bytes of a row: N elements.  masks: a table in shared memory that makes 128-bit masks of N mask bits.
 template <typename T> struct Sixteen;
 template <> struct Sixteen<float> {
-    static constexpr int N = 4;
-    using Entry = uint4;                 // of the table that makes 32-bit masks of mask bits, four bits at a time
-    __device__ static __forceinline__ Entry entry(int bits) { return make_uint4(-(bits & 1), -(bits >> 1 & 1), -(bits >> 2 & 1), -(bits >> 3 & 1)); }
-    __device__ static __forceinline__ uint4 masks(const Entry* t, uint32_t bits) { return t[bits]; }
+    static constexpr int N = 4, MASKS = 16;
+    __device__ static __forceinline__ uint4 mask(int bits) { return make_uint4(-(bits & 1), -(bits >> 1 & 1), -(bits >> 2 & 1), -(bits >> 3 & 1)); }
     __device__ static __forceinline__ uint32_t minus_inf() { return 0xFF800000u; }
     __device__ static __forceinline__ void unpack(const uint4& w, float (&x)[4])
     {
         x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
     }
-    __device__ static __forceinline__ uint4 pack(const float (&x)[4])
-    {
-        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-    }
+    __device__ static __forceinline__ uint32_t add(uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }
     __device__ static __forceinline__ uint4 gather(const float* p)
     {
         return make_uint4(__float_as_uint(p[0]), __float_as_uint(p[1]), __float_as_uint(p[2]), __float_as_uint(p[3]));
     }
 };
 template <> struct Sixteen<__nv_bfloat16> {
-    static constexpr int N = 8;
-    using Entry = uint2;
-    __device__ static __forceinline__ Entry entry(int bits)
-    {
-        return make_uint2((bits & 1) * 0xFFFFu | (bits >> 1 & 1) * 0xFFFF0000u, (bits >> 2 & 1) * 0xFFFFu | (bits >> 3 & 1) * 0xFFFF0000u);
-    }
-    __device__ static __forceinline__ uint4 masks(const Entry* t, uint32_t bits)
-    {
-        const uint2 a = t[bits & 15], b = t[bits >> 4];
-        return make_uint4(a.x, a.y, b.x, b.y);
-    }
+    static constexpr int N = 8, MASKS = 256;
+    __device__ static __forceinline__ uint32_t pair(int bits) { return (bits & 1) * 0xFFFFu | (bits >> 1 & 1) * 0xFFFF0000u; }
+    __device__ static __forceinline__ uint4 mask(int bits) { return make_uint4(pair(bits), pair(bits >> 2), pair(bits >> 4), pair(bits >> 6)); }
     __device__ static __forceinline__ uint32_t minus_inf() { return 0xFF80FF80u; }
     __device__ static __forceinline__ void unpack(const uint4& w, float (&x)[8]) { unpack_bf16x8(w, x); }
-    __device__ static __forceinline__ uint4 pack(const float (&x)[8])
+    // (the sum of two bfloat16 rounded once)
+    __device__ static __forceinline__ uint32_t add(uint32_t a, uint32_t b)
     {
-        return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+        uint32_t r;
+        asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
     }
     __device__ static __forceinline__ uint4 gather(const __nv_bfloat16* p)
     {
@@ -165,6 +186,11 @@ template <> struct Sixteen<__nv_bfloat16> {
     }
 };
 
+template <typename T>
+__device__ __forceinline__ uint4 add16(const uint4& a, const uint4& b)
+{
+    return make_uint4(Sixteen<T>::add(a.x, b.x), Sixteen<T>::add(a.y, b.y), Sixteen<T>::add(a.z, b.z), Sixteen<T>::add(a.w, b.w));
+}
 __device__ __forceinline__ uint4 select4(const uint4& m, const uint4& w, uint32_t other)
 {
     return make_uint4((w.x & m.x) | (other & ~m.x), (w.y & m.y) | (other & ~m.y), (w.z & m.z) | (other & ~m.z), (w.w & m.w) | (other & ~m.w));
@@ -178,6 +204,13 @@ __device__ __forceinline__ uint32_t bits_at(const uint32_t* words, int j, int n_
     const uint32_t lo = words[w], hi = at + N > 32 && w + 1 < n_words ? words[w + 1] : 0;
     return __funnelshift_r(lo, hi, at) & ((1u << N) - 1u);
 }
+// The same where j is a multiple of N: in one byte.
+template <int N>
+__device__ __forceinline__ uint32_t bits_in_byte(const uint32_t* words, int j)
+{
+    const uint32_t b = reinterpret_cast<const uint8_t*>(words)[j >> 3];
+    return N == 8 ? b : b >> (j & 4) & 15u;
+}
 __device__ __forceinline__ bool allowed(const uint32_t* words, int j) { return !words || (words[j >> 5] >> (j & 31) & 1u); }
 
 // A chunk of a row cut at the 16-byte boundaries of `out`: `full` vectors from column `first` on, the columns before and behind one by one.
@@ -187,7 +220,7 @@ struct Span {
     int first, full, head, tail;
     __device__ __forceinline__ Span(const T* out, int j0, int width)
     {
-        head = min((int)((16 - ((uintptr_t)(out + j0) & 15)) % 16 / sizeof(T)), width);
+        head = min((int)((16u - ((uint32_t)(uintptr_t)(out + j0) & 15u)) % 16u / (uint32_t)sizeof(T)), width);
         first = j0 + head;
         full = (width - head) / N;
         tail = width - head - full * N;
@@ -200,7 +233,7 @@ struct Span {
     }
 };
 template <typename T>
-__device__ __forceinline__ bool on_boundary(const T* row, int first) { return ((uintptr_t)(row + first) & 15) == 0; }
+__device__ __forceinline__ bool on_boundary(const T* row, int first) { return ((uint32_t)(uintptr_t)(row + first) & 15u) == 0; }
 template <typename T>
 __device__ __forceinline__ uint4 load16(const T* p, bool aligned)
 {
@@ -216,133 +249,247 @@ struct AdjustArgs {
     Rules r;
 };
 
-// TABLE: there is a history or there are named values.
-template <typename T, bool TABLE>
+// The logit x of a word with table entry t, before bias and mask.
+__device__ __forceinline__ float penalised(float x, uint32_t t, const Plan& p)
+{
+    if (t & (AJ_SEEN | AJ_COUNT)) x = x > 0.0f ? __fdiv_rn(x, p.rho) : x * p.rho;
+    if (t & AJ_COUNT) x -= fmaf(p.phi, (float)(t & AJ_COUNT), p.pi);
+    return x;
+}
+
+// Words of a row's pairs to shared memory; a barrier later the first pair of a word sums the values of all its pairs, in order.
+__device__ __forceinline__ void read_words(const Rules& r, long long row, int vocab, int* words)
+{
+    for (int i = threadIdx.x; i < r.n_bias; i += AJ_THREADS) words[i] = token_at(r.word, row * r.n_bias + i, r.words64, vocab);
+}
+__device__ __forceinline__ void sum_words(const Rules& r, long long row, Table& table, const int* words, float* sums)
+{
+    for (int i = threadIdx.x; i < r.n_bias; i += AJ_THREADS) {
+        const int w = words[i], j = w - table.j0;
+        if (w < 0 || j < 0 || j >= table.width) continue;
+        bool first = true;
+        for (int k = 0; k < i && first; ++k) first = words[k] != w;
+        if (!first) continue;
+        float sum = 0.0f;
+        for (int k = i; k < r.n_bias; ++k) if (words[k] == w) sum += r.value[row * r.n_bias + k];
+        sums[i] = sum;
+        if (atomicOr(table.word + j, (uint32_t)(i + 1) << AJ_SLOT_SHIFT) == 0) table.append(j);
+    }
+}
+
+// A row's chunk on its way through a block of threads, AJ_UNITS vectors a thread: read(), which asks for it, hold(), which puts it into shared
+// memory (the columns from `held` on; up to N - 1 lie before the first boundary), each(), which takes it from there.
+// EVEN: all rows start on 16-byte boundaries (and chunks are whole vectors), so addresses differ by constants.
+template <typename T, bool EVEN>
+struct Stream {
+    using S = Sixteen<T>;
+    static constexpr int N = S::N;
+    uint4 ahead[AJ_UNITS];
+    T ahead_single;
+    T* held;
+    Span<T> span;
+    int single;
+    __device__ __forceinline__ Stream(uint32_t* shared, const T* out, int j0, int width)
+        : held(reinterpret_cast<T*>(shared) + N), span(out, j0, width), single(span.single()) {}
+    static __host__ __device__ constexpr int words(int chunk) { return chunk * (int)sizeof(T) / 4 + 8; }
+    __device__ __forceinline__ void place(const T* out, int j0, int width)
+    {
+        if constexpr (!EVEN) { span = Span<T>(out, j0, width); single = span.single(); }
+    }
+    __device__ __forceinline__ void read(const T* x)
+    {
+        if constexpr (EVEN) {
+            const uint4* const p = reinterpret_cast<const uint4*>(x + span.first) + threadIdx.x;
+#pragma unroll
+            for (int q = 0; q < AJ_UNITS; ++q) if ((int)threadIdx.x < span.full - q * AJ_THREADS) ahead[q] = p[q * AJ_THREADS];
+        } else {
+            const bool aligned = on_boundary(x, span.first);
+#pragma unroll
+            for (int q = 0; q < AJ_UNITS; ++q) {
+                const int u = q * AJ_THREADS + threadIdx.x;
+                if (u < span.full) ahead[q] = load16(x + span.first + u * N, aligned);
+            }
+        }
+        if (single >= 0) ahead_single = x[single];
+    }
+    __device__ __forceinline__ void hold()
+    {
+        uint4* const p = reinterpret_cast<uint4*>(held) + threadIdx.x;
+#pragma unroll
+        for (int q = 0; q < AJ_UNITS; ++q) if ((int)threadIdx.x < span.full - q * AJ_THREADS) p[q * AJ_THREADS] = ahead[q];
+        if (single >= 0) held[single - span.first] = ahead_single;
+    }
+    // out = f(vector or column, its first column), from shared memory (HELD) or as read
+    template <bool HELD, typename F, typename G>
+    __device__ __forceinline__ void each(T* out, F f, G g) const
+    {
+        const uint4* const p = reinterpret_cast<const uint4*>(held) + threadIdx.x;
+        uint4* const y = reinterpret_cast<uint4*>(out + span.first) + threadIdx.x;
+#pragma unroll
+        for (int q = 0; q < AJ_UNITS; ++q)
+            if ((int)threadIdx.x < span.full - q * AJ_THREADS)
+                y[q * AJ_THREADS] = f(HELD ? p[q * AJ_THREADS] : ahead[q], span.first + (q * AJ_THREADS + (int)threadIdx.x) * N, q);
+        if (single >= 0) out[single] = g(HELD ? held[single - span.first] : ahead_single, single);
+    }
+};
+
+// Every word of the chunk is written.  TABLE: there is a history or there are named values.  A row's logits wait in shared memory while the
+// next row's are on their way; two barriers a row: one before anything reads them or the table, one between the stream's stores and those of
+// the listed words.
+template <typename T, bool TABLE, bool EVEN>
 __global__ void __launch_bounds__(AJ_THREADS)
 adjust_kernel(const __grid_constant__ AdjustArgs a)
 {
     using S = Sixteen<T>;
     constexpr int N = S::N;
     extern __shared__ __align__(16) uint32_t shared[];
-    __shared__ typename S::Entry masks[16];
+    __shared__ uint4 masks[S::MASKS];
+    __shared__ Plan plans[AJ_ROWS];
     __shared__ int listed;
-    if (threadIdx.x < 16) masks[threadIdx.x] = S::entry((int)threadIdx.x);
-    if constexpr (!TABLE) __syncthreads();             // (otherwise there will be one)
     const int part = blockIdx.x % a.chunks;
-    const long long begin = (long long)(blockIdx.x / a.chunks) * a.rows, end = min(begin + a.rows, a.n_rows);
+    const long long begin = (long long)(blockIdx.x / a.chunks) * a.rows;
+    const int rows = (int)min((long long)a.rows, a.n_rows - begin);
     const int j0 = part * a.chunk, width = min(a.chunk, a.vocab - j0), mask_words = (a.vocab + 31) / 32;
-    Table table(shared, &listed, a.chunk, j0, width);
-    float* sums = reinterpret_cast<float*>(shared + Table::words(a.chunk, a.entries));
-    int* words = reinterpret_cast<int*>(sums + a.r.n_bias);
-    const bool place = a.logits == a.out, sparse = place && !a.r.bias;
-    for (long long row = begin; row < end; ++row) {
-        const T* const x0 = static_cast<const T*>(a.logits) + row * a.stride;
-        T* const y0 = static_cast<T*>(a.out) + row * a.out_stride;
-        const T* const b0 = a.r.bias ? static_cast<const T*>(a.r.bias) + row * a.r.bias_stride : nullptr;
-        const uint32_t* const m0 = a.r.mask ? a.r.mask + row * a.r.mask_stride : nullptr;
-        const Span<T> span(y0, j0, width);
-        const bool x_aligned = on_boundary(x0, span.first), b_aligned = b0 && on_boundary(b0, span.first);
-        // read before the table is there
-        uint4 ahead[AJ_UNITS];
-        if (!sparse) {
-#pragma unroll
-            for (int q = 0; q < AJ_UNITS; ++q) {
-                const int u = q * AJ_THREADS + threadIdx.x;
-                if (u < span.full) ahead[q] = load16(x0 + span.first + u * N, x_aligned);
-            }
+    const T* x0 = static_cast<const T*>(a.logits) + begin * a.stride;
+    T* y0 = static_cast<T*>(a.out) + begin * a.out_stride;
+    const T* b0 = a.r.bias ? static_cast<const T*>(a.r.bias) + begin * a.r.bias_stride : nullptr;
+    const uint32_t* m0 = a.r.mask ? a.r.mask + begin * a.r.mask_stride : nullptr;
+    Stream<T, EVEN> stream(shared, y0, j0, width);
+    stream.read(x0);
+    if (threadIdx.x < S::MASKS) masks[threadIdx.x] = S::mask((int)threadIdx.x);
+    if (TABLE && (int)threadIdx.x < rows) plans[threadIdx.x] = plan_of(a.r, begin + threadIdx.x);
+    __syncthreads();
+    uint32_t* const rest = shared + Stream<T, EVEN>::words(a.chunk);
+    Table table(rest, &listed, a.chunk, j0, width);
+    float* const sums = reinterpret_cast<float*>(rest + Table::words(a.chunk, a.entries));
+    int* const words = reinterpret_cast<int*>(sums + a.r.n_bias);
+    // a vector, and a column, with bias and mask
+    auto vector = [&](uint4 w, int j, int q) {
+        if constexpr (EVEN) {
+            if (b0) w = add16<T>(w, reinterpret_cast<const uint4*>(b0 + j0)[q * AJ_THREADS + threadIdx.x]);
+            if (m0) w = select4(masks[bits_in_byte<N>(m0, j)], w, S::minus_inf());
+        } else {
+            if (b0) w = add16<T>(w, load16(b0 + j, on_boundary(b0, j)));
+            if (m0) w = select4(masks[bits_at<N>(m0, j, mask_words)], w, S::minus_inf());
         }
-        float rho = 1.0f, phi = 0.0f, pi = 0.0f;
-        // the word's logit with everything that concerns it
-        auto adjusted = [&](int j) {
-            const uint32_t t = table.word[j];
-            float x = (float)x0[j0 + j];
-            if (t & (AJ_SEEN | AJ_COUNT)) x = x > 0.0f ? __fdiv_rn(x, rho) : x * rho;
-            if (t & AJ_COUNT) x -= fmaf(phi, (float)(t & AJ_COUNT), pi);
-            if (b0) x += (float)b0[j0 + j];
-            const uint32_t slot = t >> AJ_SLOT_SHIFT & AJ_SLOT;
-            return slot ? x + sums[slot - 1] : x;
-        };
-        if constexpr (TABLE) {
-            for (int i = threadIdx.x; i < a.r.n_bias; i += AJ_THREADS) words[i] = token_at(a.r.word, row * a.r.n_bias + i, a.r.words64, a.vocab);
-            if (a.r.history) {
-                rho = a.r.rho_at ? a.r.rho_at[row] : a.r.rho;
-                phi = a.r.phi_at ? a.r.phi_at[row] : a.r.phi;
-                pi = a.r.pi_at ? a.r.pi_at[row] : a.r.pi;
-                table.set(a.r, row, a.vocab, a.chunk);
-            } else {
-                table.clear(a.chunk);
+        return w;
+    };
+    auto column = [&](T x, int j) { return !allowed(m0, j) ? (T)-INFINITY : b0 ? (T)((float)x + (float)b0[j]) : x; };
+    for (int i = 0; i < rows; ++i) {
+        if constexpr (!TABLE) {
+            stream.template each<false>(y0, vector, column);
+            if (i + 1 < rows) {
+                stream.place(y0 + a.out_stride, j0, width);
+                stream.read(x0 + a.stride);
             }
-            if (a.r.n_bias) {                          // (such rows are not taken in turn)
+        } else {
+            const Plan plan = plans[i];
+            stream.hold();
+            if (a.r.n_bias) read_words(a.r, begin + i, a.vocab, words);   // (such rows are not taken in turn)
+            if (a.r.history) table.set(a.r, plan, a.vocab, a.chunk);
+            else table.clear(a.chunk);
+            if (a.r.n_bias) {
                 __syncthreads();
-                // the first pair of a word sums the values of all its pairs, in order
-                for (int i = threadIdx.x; i < a.r.n_bias; i += AJ_THREADS) {
-                    const int w = words[i];
-                    if (w < j0 || w >= j0 + width) continue;
-                    bool first = true;
-                    for (int k = 0; k < i && first; ++k) first = words[k] != w;
-                    if (!first) continue;
-                    float sum = 0.0f;
-                    for (int k = i; k < a.r.n_bias; ++k) if (words[k] == w) sum += a.r.value[row * a.r.n_bias + k];
-                    sums[i] = sum;
-                    if (atomicOr(table.word + (w - j0), (uint32_t)(i + 1) << AJ_SLOT_SHIFT) == 0) table.append(w - j0);
-                }
+                sum_words(a.r, begin + i, table, words, sums);
             }
-            if (place && b0) {                         // the logits will be gone: results go to the table (such rows are not taken in turn either)
-                __syncthreads();
-                for (int i = threadIdx.x; i < listed; i += AJ_THREADS) {
-                    const int j = table.list[i];
-                    table.word[j] = __float_as_uint(adjusted(j));
-                }
-                __syncthreads();
-            }
-        }
-        if (!sparse) {
-#pragma unroll
-            for (int q = 0; q < AJ_UNITS; ++q) {
-                const int u = q * AJ_THREADS + threadIdx.x, j = span.first + u * N;
-                if (u >= span.full) break;
-                uint4 w = ahead[q];
-                if (b0) {
-                    float x[N], b[N];
-                    S::unpack(w, x);
-                    S::unpack(load16(b0 + j, b_aligned), b);
-#pragma unroll
-                    for (int e = 0; e < N; ++e) x[e] += b[e];
-                    w = S::pack(x);
-                }
-                if (m0) w = select4(S::masks(masks, bits_at<N>(m0, j, mask_words)), w, S::minus_inf());
-                *reinterpret_cast<uint4*>(y0 + j) = w;
-            }
-        } else if (m0) {
-            for (int u = threadIdx.x; u < span.full; u += AJ_THREADS) {
-                const int j = span.first + u * N;
-                const uint32_t live = bits_at<N>(m0, j, mask_words);
-                if (live == (1u << N) - 1u) continue;
-                uint4* const y = reinterpret_cast<uint4*>(y0 + j);
-                *y = select4(S::masks(masks, live), live ? *y : make_uint4(0, 0, 0, 0), S::minus_inf());
-            }
-        }
-        if (const int j = span.single(); j >= 0) {
-            if (!allowed(m0, j)) y0[j] = (T)-INFINITY;
-            else if (!sparse) y0[j] = (T)(b0 ? (float)x0[j] + (float)b0[j] : (float)x0[j]);
-        }
-        if constexpr (TABLE) {
             __syncthreads();
             const int n = listed;
-            for (int i = threadIdx.x; i < n; i += AJ_THREADS * AJ_BATCH) {
-                float y[AJ_BATCH];
-                int at[AJ_BATCH];
+            auto word = [&](int i, float& y) {         // the column of a listed word, and what it becomes
+                const int k = table.list[i], j = j0 + k;
+                if (!allowed(m0, j)) return -1;
+                const uint32_t t = table.word[k], slot = t >> AJ_SLOT_SHIFT & AJ_SLOT;
+                y = penalised((float)stream.held[j - stream.span.first], t, plan);
+                if (b0) y += (float)b0[j];
+                if (slot) y += sums[slot - 1];
+                return j;
+            };
+            int at[AJ_BATCH];
+            float y[AJ_BATCH];
 #pragma unroll
-                for (int k = 0; k < AJ_BATCH; ++k) {
-                    const int j = i + k * AJ_THREADS < n ? table.list[i + k * AJ_THREADS] : -1;
-                    at[k] = j >= 0 && allowed(m0, j0 + j) ? j0 + j : -1;
-                    if (at[k] >= 0) y[k] = place && b0 ? __uint_as_float(table.word[j]) : adjusted(j);
+            for (int k = 0; k < AJ_BATCH; ++k) at[k] = k * AJ_THREADS + (int)threadIdx.x < n ? word(k * AJ_THREADS + threadIdx.x, y[k]) : -1;
+            if (i + 1 < rows) {
+                if (a.r.history) table.look_ahead(a.r, plans[i + 1], a.vocab);
+                if constexpr (EVEN) stream.read(x0 + a.stride);
+            }
+            stream.template each<true>(y0, vector, column);
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < AJ_BATCH; ++k) if (at[k] >= 0) y0[at[k]] = (T)y[k];
+            if (n > AJ_BATCH * AJ_THREADS) {
+                for (int k = AJ_BATCH * AJ_THREADS + threadIdx.x; k < n; k += AJ_THREADS) {
+                    const int j = word(k, y[0]);
+                    if (j >= 0) y0[j] = (T)y[0];
                 }
-#pragma unroll
-                for (int k = 0; k < AJ_BATCH; ++k) if (at[k] >= 0) y0[at[k]] = (T)y[k];
+                __syncthreads();
+            }
+            if (!EVEN && i + 1 < rows) {
+                stream.place(y0 + a.out_stride, j0, width);
+                stream.read(x0 + a.stride);
             }
         }
+        x0 += a.stride;
+        y0 += a.out_stride;
+        if (b0) b0 += a.r.bias_stride;
+        if (m0) m0 += a.r.mask_stride;
     }
+}
+
+// In place without a bias: words of the history, named ones and masked ones are all that is read or written.
+template <typename T>
+__global__ void __launch_bounds__(AJ_THREADS)
+adjust_place_kernel(const __grid_constant__ AdjustArgs a)
+{
+    using S = Sixteen<T>;
+    constexpr int N = S::N;
+    extern __shared__ __align__(16) uint32_t shared[];
+    __shared__ uint4 masks[S::MASKS];
+    __shared__ int listed;
+    if (threadIdx.x < S::MASKS) masks[threadIdx.x] = S::mask((int)threadIdx.x);
+    const long long row = blockIdx.x / a.chunks;
+    const int j0 = (int)(blockIdx.x % a.chunks) * a.chunk, width = min(a.chunk, a.vocab - j0), mask_words = (a.vocab + 31) / 32;
+    Table table(shared, &listed, a.chunk, j0, width);
+    float* const sums = reinterpret_cast<float*>(shared + Table::words(a.chunk, a.entries));
+    int* const words = reinterpret_cast<int*>(sums + a.r.n_bias);
+    T* const y0 = static_cast<T*>(a.out) + row * a.out_stride;
+    const uint32_t* const m0 = a.r.mask ? a.r.mask + row * a.r.mask_stride : nullptr;
+    const Plan p = plan_of(a.r, row);
+    if (a.r.n_bias) read_words(a.r, row, a.vocab, words);
+    if (a.r.history) table.set(a.r, p, a.vocab, a.chunk);
+    else table.clear(a.chunk);
+    if (a.r.n_bias) {
+        __syncthreads();
+        sum_words(a.r, row, table, words, sums);
+    }
+    __syncthreads();
+    const int n = listed;
+    for (int i = threadIdx.x; i < n; i += AJ_THREADS * AJ_BATCH) {
+        int at[AJ_BATCH];
+        T x[AJ_BATCH];
+#pragma unroll
+        for (int k = 0; k < AJ_BATCH; ++k) {
+            at[k] = i + k * AJ_THREADS < n ? table.list[i + k * AJ_THREADS] : -1;
+            if (at[k] >= 0 && !allowed(m0, j0 + at[k])) at[k] = -1;
+            if (at[k] >= 0) x[k] = y0[j0 + at[k]];
+        }
+#pragma unroll
+        for (int k = 0; k < AJ_BATCH; ++k) {
+            if (at[k] < 0) continue;
+            const uint32_t t = table.word[at[k]], slot = t >> AJ_SLOT_SHIFT & AJ_SLOT;
+            const float y = penalised((float)x[k], t, p);
+            y0[j0 + at[k]] = (T)(slot ? y + sums[slot - 1] : y);
+        }
+    }
+    if (!m0) return;
+    __syncthreads();                                   // a vector with a masked word may hold one of those
+    const Span<T> span(y0, j0, width);
+    for (int u = threadIdx.x; u < span.full; u += AJ_THREADS) {
+        const int j = span.first + u * N;
+        const uint32_t live = bits_at<N>(m0, j, mask_words);
+        if (live == (1u << N) - 1u) continue;
+        uint4* const y = reinterpret_cast<uint4*>(y0 + j);
+        *y = select4(masks[live], live ? *y : make_uint4(0, 0, 0, 0), S::minus_inf());
+    }
+    if (const int j = span.single(); j >= 0 && !allowed(m0, j)) y0[j] = (T)-INFINITY;
 }
 
 struct AdjustGradArgs {
@@ -368,9 +515,9 @@ adjust_grad_kernel(const __grid_constant__ AdjustGradArgs a)
     using S = Sixteen<T>;
     constexpr int N = WIDE ? S::N : 1;
     extern __shared__ __align__(16) uint32_t shared[];
-    __shared__ typename S::Entry masks[16];
+    __shared__ uint4 masks[S::MASKS];
     __shared__ int listed;
-    if (threadIdx.x < 16) masks[threadIdx.x] = S::entry((int)threadIdx.x);
+    if (threadIdx.x < S::MASKS) masks[threadIdx.x] = S::mask((int)threadIdx.x);
     if constexpr (!TABLE) __syncthreads();             // (otherwise there will be one)
     const int part = blockIdx.x % a.chunks;
     const long long group = blockIdx.x / a.chunks, begin = group * a.rows, end = min(begin + a.rows, a.n_rows);
@@ -383,7 +530,11 @@ adjust_grad_kernel(const __grid_constant__ AdjustGradArgs a)
     for (int q = 0; q < (SUM ? AJ_UNITS : 1); ++q)
 #pragma unroll
         for (int e = 0; e < N; ++e) sum[q][e] = 0.0f;
+    Plan plan{};
+    if constexpr (TABLE) plan = plan_of(a.r, begin);
     for (long long row = begin; row < end; ++row) {
+        Plan next{};
+        if (TABLE && row + 1 < end) next = plan_of(a.r, row + 1);
         const T* const x0 = static_cast<const T*>(a.logits) + row * a.stride;
         const T* const g0 = static_cast<const T*>(a.dout) + row * a.dout_stride;
         T* const y0 = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
@@ -404,8 +555,8 @@ adjust_grad_kernel(const __grid_constant__ AdjustGradArgs a)
         }
         float rho = 1.0f;
         if constexpr (TABLE) {
-            rho = a.r.rho_at ? a.r.rho_at[row] : a.r.rho;
-            table.set(a.r, row, a.vocab, a.chunk);
+            rho = plan.rho;
+            table.set(a.r, plan, a.vocab, a.chunk);
         }
         if (a.dvalue) {
             // (in place: before anything of the row is overwritten)
@@ -434,7 +585,7 @@ adjust_grad_kernel(const __grid_constant__ AdjustGradArgs a)
                     const int u = q * AJ_THREADS + threadIdx.x, j = span.first + u * N;
                     if (u >= span.full) break;
                     uint4 w = ahead[q];
-                    if (m0) w = select4(S::masks(masks, bits_at<N>(m0, j, mask_words)), w, 0);
+                    if (m0) w = select4(masks[span.first % N == 0 ? bits_in_byte<N>(m0, j) : bits_at<N>(m0, j, mask_words)], w, 0);
                     if constexpr (SUM) {
                         float g[N];
                         S::unpack(w, g);
@@ -459,12 +610,14 @@ adjust_grad_kernel(const __grid_constant__ AdjustGradArgs a)
                     const uint32_t live = bits_at<N>(m0, j, mask_words);
                     if (live == (1u << N) - 1u) continue;
                     uint4* const y = reinterpret_cast<uint4*>(y0 + j);
-                    *y = select4(S::masks(masks, live), live ? *y : make_uint4(0, 0, 0, 0), 0);
+                    *y = select4(masks[live], live ? *y : make_uint4(0, 0, 0, 0), 0);
                 }
             }
             if (const int j = span.single(); j >= 0) column(j, edge);
         }
         if constexpr (TABLE) {
+            if (row + 1 < end) table.look_ahead(a.r, next, a.vocab);
+            plan = next;
             __syncthreads();
             const int n = listed;
             for (int i = threadIdx.x; i < n; i += AJ_THREADS * AJ_BATCH) {
@@ -533,7 +686,7 @@ int check_rules(const apollo_logit_rules* r, int64_t n_rows, int64_t vocab, size
             return APOLLO_ERR_ALIGN;
         q.history = r->d_history; q.history_stride = r->history_stride; q.share = n_rows / r->history_rows; q.history_len = (int)r->history_len;
         q.history64 = r->history_type == APOLLO_INDEX_I64;
-        q.length = r->d_length; q.start = r->d_start;
+        q.length = r->d_length; q.start = gradient ? nullptr : r->d_start;
         q.rho_at = r->d_repetition; q.phi_at = r->d_frequency; q.pi_at = r->d_presence;
         q.rho = r->repetition; q.phi = r->frequency; q.pi = r->presence;
     }
@@ -596,22 +749,26 @@ template <typename T>
 cudaError_t run_adjust(AdjustArgs a, int sms, cudaStream_t stream)
 {
     constexpr int N = Sixteen<T>::N;
-    const bool place = a.logits == a.out;
-    const Cut c = cut_up(a.n_rows, a.vocab, a.r, place && !a.r.bias ? AJ_PLACE_CHUNK : AJ_UNITS * AJ_THREADS * N, !(place && a.r.bias) && a.r.n_bias == 0, sms);
+    const bool sparse = a.logits == a.out && !a.r.bias;
+    const Cut c = cut_up(a.n_rows, a.vocab, a.r, sparse ? AJ_PLACE_CHUNK : AJ_UNITS * AJ_THREADS * N, !sparse && a.r.n_bias == 0, sms);
     a.chunk = c.chunk; a.chunks = c.chunks; a.rows = c.rows;
     a.entries = list_entries(a.r, a.r.n_bias, c.chunk);
     const int64_t blocks = (a.n_rows + c.rows - 1) / c.rows * c.chunks;
     if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
-    const unsigned grid = (unsigned)blocks;
-    if (a.r.history || a.r.n_bias) {
-        const int smem = (Table::words(c.chunk, a.entries) + 2 * a.r.n_bias) * 4;
-        const cudaError_t e = cudaFuncSetAttribute(adjust_kernel<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AJ_MOST_SMEM);
+    const bool table = a.r.history || a.r.n_bias;
+    if (sparse && !table && !a.r.mask) return cudaSuccess;
+    const int smem = sparse ? (Table::words(c.chunk, a.entries) + 2 * a.r.n_bias) * 4
+                            : table ? (Table::words(c.chunk, a.entries) + 2 * a.r.n_bias + Stream<T, true>::words(c.chunk)) * 4 : 0;
+    auto launch = [&](auto* kernel) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, AJ_MOST_SMEM);
         if (e != cudaSuccess) return e;
-        adjust_kernel<T, true><<<grid, AJ_THREADS, smem, stream>>>(a);
-    } else {
-        adjust_kernel<T, false><<<grid, AJ_THREADS, 0, stream>>>(a);
-    }
-    return cudaGetLastError();
+        kernel<<<(unsigned)blocks, AJ_THREADS, smem, stream>>>(a);
+        return cudaGetLastError();
+    };
+    if (sparse) return launch(adjust_place_kernel<T>);
+    const bool even = whole_vectors(a.logits, a.stride, sizeof(T)) && whole_vectors(a.out, a.out_stride, sizeof(T)) && whole_vectors(a.r.bias, a.r.bias_stride, sizeof(T));
+    if (table) return even ? launch(adjust_kernel<T, true, true>) : launch(adjust_kernel<T, true, false>);
+    return even ? launch(adjust_kernel<T, false, true>) : launch(adjust_kernel<T, false, false>);
 }
 
 template <typename T>
