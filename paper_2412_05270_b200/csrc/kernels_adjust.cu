@@ -5,19 +5,22 @@
 //   mask bit 0: x <- -inf
 //   a_j = allowed ? dout_j : 0;  dlogit_j = a_j {1, 1 / rho, rho};  dbias_j = a_j (summed over rows if shared);  dvalue_i = a_j
 //
-// A block of threads takes a chunk of the vocabulary for one row, or for a few rows in turn.  It counts the tokens of its chunk in a table in
-// shared memory and lists the words that occur (integer atomics: their order decides the order of the list, not the results).  Then
-// two passes: a stream over the whole chunk that knows of bias and mask alone, and the listed words once more, one a thread.  (With
-// both in one pass, vectors looking into the table, nearly every warp of a training batch had a word to look up: 376 instructions
-// a vector of eight instead of 40.)  Rows that share a history (the positions of a sequence in training) go on with the table of the row
-// before: they add the tokens in between.  A table word holds
+// Two kernels.  One streams over rows and knows of bias and mask alone.  The other takes a chunk of the vocabulary for one row, or for a few
+// rows in turn: it counts the tokens of its chunk in a table in shared memory and lists the words that occur (integer atomics: their
+// order decides the order of the list, not the results), then writes the listed words, one a thread.  In place without a bias the second one
+// does everything: the listed words and the masked ones are all that changes.  Rows that share a history (the positions of a sequence in
+// training) go on with the table of the row before: they add the tokens in between.  A table word holds
 // [31] seen at all  [30..20] 1 + slot of the word's named value  [19..0] how often from `start` on.
+// What was tried: vectors that look into the table (in a training batch nearly every warp had a word to look up: 376 instructions a
+// vector of eight; 8192 x 32000 bfloat16 785 us), both passes in one kernel with barriers between them (351 us), the same with the next row's
+// loads under way (266 us: what waits for barriers and scattered loads holds up what waits for memory).
 #include "../../include/apollo.h"
 
 #include <cmath>
 
 #include "device_utils.cuh"
 #include "host_utils.h"
+#include "tc_ptx.cuh"
 
 namespace apollo {
 
@@ -26,7 +29,7 @@ namespace {
 constexpr int AJ_THREADS = 256;
 constexpr int AJ_UNITS = 4;              // vectors a thread has of a row's chunk at once
 constexpr int AJ_BATCH = 4;              // loads a thread has in flight where they are scattered
-constexpr int AJ_ROWS = 16;              // most rows in turn, without sums
+constexpr int AJ_ROWS = 16;              // most rows in turn
 constexpr uint32_t AJ_SEEN = 0x80000000u;
 constexpr int AJ_SLOT_SHIFT = 20;
 constexpr uint32_t AJ_COUNT = (1u << AJ_SLOT_SHIFT) - 1, AJ_SLOT = 0x7FFu;
@@ -123,14 +126,13 @@ struct Table {
         token_more = more < p.length ? token_at(r.history, first + more, r.history64, vocab) - j0 : -1;
         token_less = less < p.start ? token_at(r.history, first + less, r.history64, vocab) - j0 : -1;
     }
-    // The table of a row, from that of the row before it where both have the same history.  Begins with a barrier; the caller ends with one.
+    // The table of a row, from that of the row before it where both have the same history.  Between two barriers of the caller's.
     __device__ __forceinline__ void set(const Rules& r, const Plan& p, int vocab, int chunk)
     {
         auto add = [&](int j, int i) {
             if (!(atomicOr(word + j, AJ_SEEN) & AJ_SEEN)) append(j);
             if (i >= p.start) atomicAdd(word + j, 1u);
         };
-        __syncthreads();
         if (quick) {
             if (token_less >= 0 && token_less < width) atomicSub(word + token_less, 1u);
             if (token_more >= 0 && token_more < width) add(token_more, now.length + (int)threadIdx.x);
@@ -150,12 +152,14 @@ struct Table {
     }
 };
 
-// Sixteen bytes of a row: N elements.  masks: a table in shared memory that makes 128-bit masks of N mask bits.
+// Sixteen bytes of a row: N elements.  Entry: of the table in shared memory that makes element masks of four mask bits.
 template <typename T> struct Sixteen;
 template <> struct Sixteen<float> {
-    static constexpr int N = 4, MASKS = 16;
-    __device__ static __forceinline__ uint4 mask(int bits) { return make_uint4(-(bits & 1), -(bits >> 1 & 1), -(bits >> 2 & 1), -(bits >> 3 & 1)); }
-    __device__ static __forceinline__ uint32_t minus_inf() { return 0xFF800000u; }
+    static constexpr int N = 4;
+    using Entry = uint4;
+    __device__ static __forceinline__ Entry entry(int bits) { return make_uint4(-(bits & 1), -(bits >> 1 & 1), -(bits >> 2 & 1), -(bits >> 3 & 1)); }
+    __device__ static __forceinline__ uint4 masks(const Entry* t, uint32_t bits) { return t[bits]; }
+    static constexpr uint32_t MINUS_INF = 0xFF800000u;
     __device__ static __forceinline__ void unpack(const uint4& w, float (&x)[4])
     {
         x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
@@ -167,10 +171,16 @@ template <> struct Sixteen<float> {
     }
 };
 template <> struct Sixteen<__nv_bfloat16> {
-    static constexpr int N = 8, MASKS = 256;
+    static constexpr int N = 8;
+    using Entry = uint2;
     __device__ static __forceinline__ uint32_t pair(int bits) { return (bits & 1) * 0xFFFFu | (bits >> 1 & 1) * 0xFFFF0000u; }
-    __device__ static __forceinline__ uint4 mask(int bits) { return make_uint4(pair(bits), pair(bits >> 2), pair(bits >> 4), pair(bits >> 6)); }
-    __device__ static __forceinline__ uint32_t minus_inf() { return 0xFF80FF80u; }
+    __device__ static __forceinline__ Entry entry(int bits) { return make_uint2(pair(bits), pair(bits >> 2)); }
+    __device__ static __forceinline__ uint4 masks(const Entry* t, uint32_t bits)
+    {
+        const uint2 a = t[bits & 15], b = t[bits >> 4];
+        return make_uint4(a.x, a.y, b.x, b.y);
+    }
+    static constexpr uint32_t MINUS_INF = 0xFF80FF80u;
     __device__ static __forceinline__ void unpack(const uint4& w, float (&x)[8]) { unpack_bf16x8(w, x); }
     // (the sum of two bfloat16 rounded once)
     __device__ static __forceinline__ uint32_t add(uint32_t a, uint32_t b)
@@ -201,17 +211,17 @@ template <int N>
 __device__ __forceinline__ uint32_t bits_at(const uint32_t* words, int j, int n_words)
 {
     const int w = j >> 5, at = j & 31;
-    const uint32_t lo = words[w], hi = at + N > 32 && w + 1 < n_words ? words[w + 1] : 0;
+    const uint32_t lo = __ldg(words + w), hi = at + N > 32 && w + 1 < n_words ? __ldg(words + w + 1) : 0;
     return __funnelshift_r(lo, hi, at) & ((1u << N) - 1u);
 }
 // The same where j is a multiple of N: in one byte.
 template <int N>
 __device__ __forceinline__ uint32_t bits_in_byte(const uint32_t* words, int j)
 {
-    const uint32_t b = reinterpret_cast<const uint8_t*>(words)[j >> 3];
+    const uint32_t b = __ldg(reinterpret_cast<const uint8_t*>(words) + (j >> 3));
     return N == 8 ? b : b >> (j & 4) & 15u;
 }
-__device__ __forceinline__ bool allowed(const uint32_t* words, int j) { return !words || (words[j >> 5] >> (j & 31) & 1u); }
+__device__ __forceinline__ bool allowed(const uint32_t* words, int j) { return !words || (__ldg(words + (j >> 5)) >> (j & 31) & 1u); }
 
 // A chunk of a row cut at the 16-byte boundaries of `out`: `full` vectors from column `first` on, the columns before and behind one by one.
 template <typename T>
@@ -239,15 +249,6 @@ __device__ __forceinline__ uint4 load16(const T* p, bool aligned)
 {
     return aligned ? *reinterpret_cast<const uint4*>(p) : Sixteen<T>::gather(p);
 }
-
-struct AdjustArgs {
-    const void* logits;
-    void* out;
-    long long stride, out_stride, n_rows;
-    int vocab, chunk, chunks, rows;      // rows: in turn
-    int entries;                         // of the list at most
-    Rules r;
-};
 
 // The logit x of a word with table entry t, before bias and mask.
 __device__ __forceinline__ float penalised(float x, uint32_t t, const Plan& p)
@@ -277,379 +278,268 @@ __device__ __forceinline__ void sum_words(const Rules& r, long long row, Table& 
     }
 }
 
-// A row's chunk on its way through a block of threads, AJ_UNITS vectors a thread: read(), which asks for it, hold(), which puts it into shared
-// memory (the columns from `held` on; up to N - 1 lie before the first boundary), each(), which takes it from there.
-// EVEN: all rows start on 16-byte boundaries (and chunks are whole vectors), so addresses differ by constants.
-template <typename T, bool EVEN>
-struct Stream {
+// What a vector, or a column, becomes on the way: bias, mask.  OTHER: what a masked word becomes.
+template <typename T>
+struct Dense {
     using S = Sixteen<T>;
     static constexpr int N = S::N;
-    uint4 ahead[AJ_UNITS];
-    T ahead_single;
-    T* held;
-    Span<T> span;
-    int single;
-    __device__ __forceinline__ Stream(uint32_t* shared, const T* out, int j0, int width)
-        : held(reinterpret_cast<T*>(shared) + N), span(out, j0, width), single(span.single()) {}
-    static __host__ __device__ constexpr int words(int chunk) { return chunk * (int)sizeof(T) / 4 + 8; }
-    __device__ __forceinline__ void place(const T* out, int j0, int width)
+    const T* bias;
+    const uint32_t* mask;
+    const typename S::Entry* masks;
+    uint32_t other;
+    int mask_words;
+    template <bool EVEN>
+    __device__ __forceinline__ uint4 vector(uint4 w, int j) const
     {
-        if constexpr (!EVEN) { span = Span<T>(out, j0, width); single = span.single(); }
+        if (bias) w = add16<T>(w, EVEN ? __ldg(reinterpret_cast<const uint4*>(bias + j)) : load16(bias + j, on_boundary(bias, j)));
+        if (mask) w = select4(S::masks(masks, EVEN ? bits_in_byte<N>(mask, j) : bits_at<N>(mask, j, mask_words)), w, other);
+        return w;
     }
-    __device__ __forceinline__ void read(const T* x)
+    __device__ __forceinline__ T column(T x, int j) const
     {
-        if constexpr (EVEN) {
-            const uint4* const p = reinterpret_cast<const uint4*>(x + span.first) + threadIdx.x;
-#pragma unroll
-            for (int q = 0; q < AJ_UNITS; ++q) if ((int)threadIdx.x < span.full - q * AJ_THREADS) ahead[q] = p[q * AJ_THREADS];
-        } else {
-            const bool aligned = on_boundary(x, span.first);
-#pragma unroll
-            for (int q = 0; q < AJ_UNITS; ++q) {
-                const int u = q * AJ_THREADS + threadIdx.x;
-                if (u < span.full) ahead[q] = load16(x + span.first + u * N, aligned);
-            }
-        }
-        if (single >= 0) ahead_single = x[single];
-    }
-    __device__ __forceinline__ void hold()
-    {
-        uint4* const p = reinterpret_cast<uint4*>(held) + threadIdx.x;
-#pragma unroll
-        for (int q = 0; q < AJ_UNITS; ++q) if ((int)threadIdx.x < span.full - q * AJ_THREADS) p[q * AJ_THREADS] = ahead[q];
-        if (single >= 0) held[single - span.first] = ahead_single;
-    }
-    // out = f(vector or column, its first column), from shared memory (HELD) or as read
-    template <bool HELD, typename F, typename G>
-    __device__ __forceinline__ void each(T* out, F f, G g) const
-    {
-        const uint4* const p = reinterpret_cast<const uint4*>(held) + threadIdx.x;
-        uint4* const y = reinterpret_cast<uint4*>(out + span.first) + threadIdx.x;
-#pragma unroll
-        for (int q = 0; q < AJ_UNITS; ++q)
-            if ((int)threadIdx.x < span.full - q * AJ_THREADS)
-                y[q * AJ_THREADS] = f(HELD ? p[q * AJ_THREADS] : ahead[q], span.first + (q * AJ_THREADS + (int)threadIdx.x) * N, q);
-        if (single >= 0) out[single] = g(HELD ? held[single - span.first] : ahead_single, single);
+        return !allowed(mask, j) ? (other ? (T)-INFINITY : (T)0.0f) : bias ? (T)((float)x + (float)bias[j]) : x;
     }
 };
 
-// Every word of the chunk is written.  TABLE: there is a history or there are named values.  A row's logits wait in shared memory while the
-// next row's are on their way; two barriers a row: one before anything reads them or the table, one between the stream's stores and those of
-// the listed words.
-template <typename T, bool TABLE, bool EVEN>
-__global__ void __launch_bounds__(AJ_THREADS)
-adjust_kernel(const __grid_constant__ AdjustArgs a)
-{
-    using S = Sixteen<T>;
-    constexpr int N = S::N;
-    extern __shared__ __align__(16) uint32_t shared[];
-    __shared__ uint4 masks[S::MASKS];
-    __shared__ Plan plans[AJ_ROWS];
-    __shared__ int listed;
-    const int part = blockIdx.x % a.chunks;
-    const long long begin = (long long)(blockIdx.x / a.chunks) * a.rows;
-    const int rows = (int)min((long long)a.rows, a.n_rows - begin);
-    const int j0 = part * a.chunk, width = min(a.chunk, a.vocab - j0), mask_words = (a.vocab + 31) / 32;
-    const T* x0 = static_cast<const T*>(a.logits) + begin * a.stride;
-    T* y0 = static_cast<T*>(a.out) + begin * a.out_stride;
-    const T* b0 = a.r.bias ? static_cast<const T*>(a.r.bias) + begin * a.r.bias_stride : nullptr;
-    const uint32_t* m0 = a.r.mask ? a.r.mask + begin * a.r.mask_stride : nullptr;
-    Stream<T, EVEN> stream(shared, y0, j0, width);
-    stream.read(x0);
-    if (threadIdx.x < S::MASKS) masks[threadIdx.x] = S::mask((int)threadIdx.x);
-    if (TABLE && (int)threadIdx.x < rows) plans[threadIdx.x] = plan_of(a.r, begin + threadIdx.x);
-    __syncthreads();
-    uint32_t* const rest = shared + Stream<T, EVEN>::words(a.chunk);
-    Table table(rest, &listed, a.chunk, j0, width);
-    float* const sums = reinterpret_cast<float*>(rest + Table::words(a.chunk, a.entries));
-    int* const words = reinterpret_cast<int*>(sums + a.r.n_bias);
-    // a vector, and a column, with bias and mask
-    auto vector = [&](uint4 w, int j, int q) {
-        if constexpr (EVEN) {
-            if (b0) w = add16<T>(w, reinterpret_cast<const uint4*>(b0 + j0)[q * AJ_THREADS + threadIdx.x]);
-            if (m0) w = select4(masks[bits_in_byte<N>(m0, j)], w, S::minus_inf());
-        } else {
-            if (b0) w = add16<T>(w, load16(b0 + j, on_boundary(b0, j)));
-            if (m0) w = select4(masks[bits_at<N>(m0, j, mask_words)], w, S::minus_inf());
-        }
-        return w;
-    };
-    auto column = [&](T x, int j) { return !allowed(m0, j) ? (T)-INFINITY : b0 ? (T)((float)x + (float)b0[j]) : x; };
-    for (int i = 0; i < rows; ++i) {
-        if constexpr (!TABLE) {
-            stream.template each<false>(y0, vector, column);
-            if (i + 1 < rows) {
-                stream.place(y0 + a.out_stride, j0, width);
-                stream.read(x0 + a.stride);
-            }
-        } else {
-            const Plan plan = plans[i];
-            stream.hold();
-            if (a.r.n_bias) read_words(a.r, begin + i, a.vocab, words);   // (such rows are not taken in turn)
-            if (a.r.history) table.set(a.r, plan, a.vocab, a.chunk);
-            else table.clear(a.chunk);
-            if (a.r.n_bias) {
-                __syncthreads();
-                sum_words(a.r, begin + i, table, words, sums);
-            }
-            __syncthreads();
-            const int n = listed;
-            auto word = [&](int i, float& y) {         // the column of a listed word, and what it becomes
-                const int k = table.list[i], j = j0 + k;
-                if (!allowed(m0, j)) return -1;
-                const uint32_t t = table.word[k], slot = t >> AJ_SLOT_SHIFT & AJ_SLOT;
-                y = penalised((float)stream.held[j - stream.span.first], t, plan);
-                if (b0) y += (float)b0[j];
-                if (slot) y += sums[slot - 1];
-                return j;
-            };
-            int at[AJ_BATCH];
-            float y[AJ_BATCH];
-#pragma unroll
-            for (int k = 0; k < AJ_BATCH; ++k) at[k] = k * AJ_THREADS + (int)threadIdx.x < n ? word(k * AJ_THREADS + threadIdx.x, y[k]) : -1;
-            if (i + 1 < rows) {
-                if (a.r.history) table.look_ahead(a.r, plans[i + 1], a.vocab);
-                if constexpr (EVEN) stream.read(x0 + a.stride);
-            }
-            stream.template each<true>(y0, vector, column);
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < AJ_BATCH; ++k) if (at[k] >= 0) y0[at[k]] = (T)y[k];
-            if (n > AJ_BATCH * AJ_THREADS) {
-                for (int k = AJ_BATCH * AJ_THREADS + threadIdx.x; k < n; k += AJ_THREADS) {
-                    const int j = word(k, y[0]);
-                    if (j >= 0) y0[j] = (T)y[0];
-                }
-                __syncthreads();
-            }
-            if (!EVEN && i + 1 < rows) {
-                stream.place(y0 + a.out_stride, j0, width);
-                stream.read(x0 + a.stride);
-            }
-        }
-        x0 += a.stride;
-        y0 += a.out_stride;
-        if (b0) b0 += a.r.bias_stride;
-        if (m0) m0 += a.r.mask_stride;
-    }
-}
-
-// In place without a bias: words of the history, named ones and masked ones are all that is read or written.
-template <typename T>
-__global__ void __launch_bounds__(AJ_THREADS)
-adjust_place_kernel(const __grid_constant__ AdjustArgs a)
-{
-    using S = Sixteen<T>;
-    constexpr int N = S::N;
-    extern __shared__ __align__(16) uint32_t shared[];
-    __shared__ uint4 masks[S::MASKS];
-    __shared__ int listed;
-    if (threadIdx.x < S::MASKS) masks[threadIdx.x] = S::mask((int)threadIdx.x);
-    const long long row = blockIdx.x / a.chunks;
-    const int j0 = (int)(blockIdx.x % a.chunks) * a.chunk, width = min(a.chunk, a.vocab - j0), mask_words = (a.vocab + 31) / 32;
-    Table table(shared, &listed, a.chunk, j0, width);
-    float* const sums = reinterpret_cast<float*>(shared + Table::words(a.chunk, a.entries));
-    int* const words = reinterpret_cast<int*>(sums + a.r.n_bias);
-    T* const y0 = static_cast<T*>(a.out) + row * a.out_stride;
-    const uint32_t* const m0 = a.r.mask ? a.r.mask + row * a.r.mask_stride : nullptr;
-    const Plan p = plan_of(a.r, row);
-    if (a.r.n_bias) read_words(a.r, row, a.vocab, words);
-    if (a.r.history) table.set(a.r, p, a.vocab, a.chunk);
-    else table.clear(a.chunk);
-    if (a.r.n_bias) {
-        __syncthreads();
-        sum_words(a.r, row, table, words, sums);
-    }
-    __syncthreads();
-    const int n = listed;
-    for (int i = threadIdx.x; i < n; i += AJ_THREADS * AJ_BATCH) {
-        int at[AJ_BATCH];
-        T x[AJ_BATCH];
-#pragma unroll
-        for (int k = 0; k < AJ_BATCH; ++k) {
-            at[k] = i + k * AJ_THREADS < n ? table.list[i + k * AJ_THREADS] : -1;
-            if (at[k] >= 0 && !allowed(m0, j0 + at[k])) at[k] = -1;
-            if (at[k] >= 0) x[k] = y0[j0 + at[k]];
-        }
-#pragma unroll
-        for (int k = 0; k < AJ_BATCH; ++k) {
-            if (at[k] < 0) continue;
-            const uint32_t t = table.word[at[k]], slot = t >> AJ_SLOT_SHIFT & AJ_SLOT;
-            const float y = penalised((float)x[k], t, p);
-            y0[j0 + at[k]] = (T)(slot ? y + sums[slot - 1] : y);
-        }
-    }
-    if (!m0) return;
-    __syncthreads();                                   // a vector with a masked word may hold one of those
-    const Span<T> span(y0, j0, width);
-    for (int u = threadIdx.x; u < span.full; u += AJ_THREADS) {
-        const int j = span.first + u * N;
-        const uint32_t live = bits_at<N>(m0, j, mask_words);
-        if (live == (1u << N) - 1u) continue;
-        uint4* const y = reinterpret_cast<uint4*>(y0 + j);
-        *y = select4(masks[live], live ? *y : make_uint4(0, 0, 0, 0), S::minus_inf());
-    }
-    if (const int j = span.single(); j >= 0 && !allowed(m0, j)) y0[j] = (T)-INFINITY;
-}
-
-struct AdjustGradArgs {
-    const void* logits;
-    const void* dout;
-    void* dlogits;
-    void* dbias;                         // rows of its own (dbias_stride > 0), or null
-    float* partial;                      // shared bias: sums over the rows of a block of threads, vocab floats each
-    float* dvalue;
-    long long stride, dout_stride, dlogits_stride, dbias_stride, n_rows;
-    int vocab, chunk, chunks, rows;
-    Rules r;
+struct StreamArgs {
+    const void* in;
+    void* out;                           // may be `in`
+    void* copy;                          // the same once more (rows of a bias), or null
+    float* partial;                      // SUM: sums over the rows of a block of threads, vocab floats each
+    const void* bias;
+    const uint32_t* mask;
+    long long in_stride, out_stride, copy_stride, bias_stride, mask_stride, n_rows;
+    uint32_t other;
+    int vocab, chunk, chunks, rows;      // rows: of a block of threads
 };
 
 __device__ __forceinline__ void store_partial(float* p, float a, float b, float c, float d) { p[0] = a; p[1] = b; p[2] = c; p[3] = d; }
 
-// SUM: the sums over the rows stay in registers.  Every row's vectors have to start at the same columns then; where they do not,
-// WIDE = false takes the columns one by one.
-template <typename T, bool TABLE, bool SUM, bool WIDE>
+// Four vectors a thread, all loads before the first store.  EVEN: all rows start on 16-byte boundaries, so addresses differ by constants.
+// SUM: the sums over a block's rows stay in registers; every row's vectors have to start at the same columns then, so where rows are not
+// even (and SUM) the columns go one by one.
+template <typename T, bool EVEN, bool SUM>
 __global__ void __launch_bounds__(AJ_THREADS)
-adjust_grad_kernel(const __grid_constant__ AdjustGradArgs a)
+adjust_stream_kernel(const __grid_constant__ StreamArgs a)
 {
     using S = Sixteen<T>;
+    constexpr bool WIDE = EVEN || !SUM;
     constexpr int N = WIDE ? S::N : 1;
-    extern __shared__ __align__(16) uint32_t shared[];
-    __shared__ uint4 masks[S::MASKS];
-    __shared__ int listed;
-    if (threadIdx.x < S::MASKS) masks[threadIdx.x] = S::mask((int)threadIdx.x);
-    if constexpr (!TABLE) __syncthreads();             // (otherwise there will be one)
-    const int part = blockIdx.x % a.chunks;
-    const long long group = blockIdx.x / a.chunks, begin = group * a.rows, end = min(begin + a.rows, a.n_rows);
-    const int j0 = part * a.chunk, width = min(a.chunk, a.vocab - j0), mask_words = (a.vocab + 31) / 32;
-    Table table(shared, &listed, a.chunk, j0, width);
-    const bool place = a.dlogits == a.dout;
-    const bool sparse = place && !SUM && !a.dbias;
+    __shared__ typename S::Entry masks[16];
+    ptx::grid_launch_dependents();
+    if (threadIdx.x < 16) masks[threadIdx.x] = S::entry((int)threadIdx.x);
+    __syncthreads();
+    const int tid = threadIdx.x, part = blockIdx.x % a.chunks;
+    const long long group = blockIdx.x / a.chunks, begin = group * a.rows;
+    const int rows = (int)min((long long)a.rows, a.n_rows - begin);
+    const int j0 = part * a.chunk, width = min(a.chunk, a.vocab - j0);
+    const T* x0 = static_cast<const T*>(a.in) + begin * a.in_stride;
+    T* y0 = static_cast<T*>(a.out) + begin * a.out_stride;
+    T* c0 = a.copy ? static_cast<T*>(a.copy) + begin * a.copy_stride : nullptr;
+    Dense<T> dense{ a.bias ? static_cast<const T*>(a.bias) + begin * a.bias_stride : nullptr, a.mask ? a.mask + begin * a.mask_stride : nullptr,
+                    masks, a.other, (a.vocab + 31) / 32 };
+    const bool keep = a.in == a.out && !a.bias && !a.mask;                // nothing to write there
     float sum[SUM ? AJ_UNITS : 1][N], edge = 0.0f;
 #pragma unroll
     for (int q = 0; q < (SUM ? AJ_UNITS : 1); ++q)
 #pragma unroll
         for (int e = 0; e < N; ++e) sum[q][e] = 0.0f;
-    Plan plan{};
-    if constexpr (TABLE) plan = plan_of(a.r, begin);
-    for (long long row = begin; row < end; ++row) {
-        Plan next{};
-        if (TABLE && row + 1 < end) next = plan_of(a.r, row + 1);
-        const T* const x0 = static_cast<const T*>(a.logits) + row * a.stride;
-        const T* const g0 = static_cast<const T*>(a.dout) + row * a.dout_stride;
-        T* const y0 = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
-        T* const b0 = a.dbias ? static_cast<T*>(a.dbias) + row * a.dbias_stride : nullptr;
-        const uint32_t* const m0 = a.r.mask ? a.r.mask + row * a.r.mask_stride : nullptr;
-        const Span<T> span(y0, j0, width);
-        const bool g_aligned = on_boundary(g0, span.first), b_aligned = b0 && on_boundary(b0, span.first);
-        // read before the table is there
-        uint4 ahead[WIDE ? AJ_UNITS : 1];
+    for (int i = 0; i < rows; ++i) {
         if constexpr (WIDE) {
-            if (!sparse) {
+            const Span<T> span(y0, j0, width);
+            const bool aligned = EVEN || on_boundary(x0, span.first), c_aligned = EVEN || (c0 && on_boundary(c0, span.first)), plain = span.first % N == 0;
+            uint4 w[AJ_UNITS];
+            const T* const x = x0 + span.first + tid * N;
 #pragma unroll
-                for (int q = 0; q < AJ_UNITS; ++q) {
-                    const int u = q * AJ_THREADS + threadIdx.x;
-                    if (u < span.full) ahead[q] = load16(g0 + span.first + u * N, g_aligned);
-                }
-            }
-        }
-        float rho = 1.0f;
-        if constexpr (TABLE) {
-            rho = plan.rho;
-            table.set(a.r, plan, a.vocab, a.chunk);
-        }
-        if (a.dvalue) {
-            // (in place: before anything of the row is overwritten)
-            for (int i = threadIdx.x; i < a.r.n_bias; i += AJ_THREADS) {
-                const int w = token_at(a.r.word, row * a.r.n_bias + i, a.r.words64, a.vocab);
-                if (w < 0 ? j0 == 0 : w >= j0 && w < j0 + width) a.dvalue[row * a.r.n_bias + i] = w >= 0 && allowed(m0, w) ? (float)g0[w] : 0.0f;
-            }
-            if (place) __syncthreads();
-        }
-        auto column = [&](int j, float& total) {
-            const float g = allowed(m0, j) ? (float)g0[j] : 0.0f;
-            if constexpr (SUM) total += g;
-            if (b0) b0[j] = (T)g;
-            y0[j] = (T)g;
-        };
-        if constexpr (!WIDE) {
+            for (int q = 0; q < AJ_UNITS; ++q) if (tid < span.full - q * AJ_THREADS) w[q] = load16(x + q * AJ_THREADS * N, aligned);
 #pragma unroll
             for (int q = 0; q < AJ_UNITS; ++q) {
-                const int u = q * AJ_THREADS + threadIdx.x;
-                if (u < width) column(j0 + u, sum[q][0]);
+                if (tid >= span.full - q * AJ_THREADS) continue;
+                const int j = span.first + (q * AJ_THREADS + tid) * N;
+                w[q] = EVEN || (plain && !dense.bias) ? dense.template vector<true>(w[q], j) : dense.template vector<false>(w[q], j);
+                if constexpr (SUM) {
+                    float g[N];
+                    S::unpack(w[q], g);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) sum[q][e] += g[e];
+                }
+            }
+            T* const y = y0 + span.first + tid * N;
+#pragma unroll
+            for (int q = 0; q < AJ_UNITS; ++q) {
+                if (tid >= span.full - q * AJ_THREADS) continue;
+                if (!keep) *reinterpret_cast<uint4*>(y + q * AJ_THREADS * N) = w[q];
+                if (c0) {
+                    T* const c = c0 + span.first + (q * AJ_THREADS + tid) * N;
+                    if (c_aligned) {
+                        *reinterpret_cast<uint4*>(c) = w[q];
+                    } else {
+                        float g[N];
+                        S::unpack(w[q], g);
+#pragma unroll
+                        for (int e = 0; e < N; ++e) c[e] = (T)g[e];
+                    }
+                }
+            }
+            if (const int j = span.single(); j >= 0) {
+                const T r = dense.column(x0[j], j);
+                y0[j] = r;
+                if (c0) c0[j] = r;
+                if constexpr (SUM) edge += (float)r;
             }
         } else {
-            if (!sparse) {
 #pragma unroll
-                for (int q = 0; q < AJ_UNITS; ++q) {
-                    const int u = q * AJ_THREADS + threadIdx.x, j = span.first + u * N;
-                    if (u >= span.full) break;
-                    uint4 w = ahead[q];
-                    if (m0) w = select4(masks[span.first % N == 0 ? bits_in_byte<N>(m0, j) : bits_at<N>(m0, j, mask_words)], w, 0);
-                    if constexpr (SUM) {
-                        float g[N];
-                        S::unpack(w, g);
-#pragma unroll
-                        for (int e = 0; e < N; ++e) sum[q][e] += g[e];
-                    }
-                    if (b0) {
-                        if (b_aligned) {
-                            *reinterpret_cast<uint4*>(b0 + j) = w;
-                        } else {
-                            float g[N];
-                            S::unpack(w, g);
-#pragma unroll
-                            for (int e = 0; e < N; ++e) b0[j + e] = (T)g[e];
-                        }
-                    }
-                    if (!place || m0) *reinterpret_cast<uint4*>(y0 + j) = w;
-                }
-            } else if (m0) {
-                for (int u = threadIdx.x; u < span.full; u += AJ_THREADS) {
-                    const int j = span.first + u * N;
-                    const uint32_t live = bits_at<N>(m0, j, mask_words);
-                    if (live == (1u << N) - 1u) continue;
-                    uint4* const y = reinterpret_cast<uint4*>(y0 + j);
-                    *y = select4(masks[live], live ? *y : make_uint4(0, 0, 0, 0), 0);
-                }
-            }
-            if (const int j = span.single(); j >= 0) column(j, edge);
-        }
-        if constexpr (TABLE) {
-            if (row + 1 < end) table.look_ahead(a.r, next, a.vocab);
-            plan = next;
-            __syncthreads();
-            const int n = listed;
-            for (int i = threadIdx.x; i < n; i += AJ_THREADS * AJ_BATCH) {
-                float g[AJ_BATCH], x[AJ_BATCH];
-                int at[AJ_BATCH];
-#pragma unroll
-                for (int k = 0; k < AJ_BATCH; ++k) {
-                    const int w = i + k * AJ_THREADS < n ? j0 + table.list[i + k * AJ_THREADS] : -1;
-                    at[k] = w >= 0 && allowed(m0, w) ? w : -1;
-                    if (at[k] >= 0) { g[k] = (float)g0[w]; x[k] = (float)x0[w]; }
-                }
-#pragma unroll
-                for (int k = 0; k < AJ_BATCH; ++k)
-                    if (at[k] >= 0) y0[at[k]] = (T)(x[k] > 0.0f ? __fdiv_rn(g[k], rho) : g[k] * rho);
+            for (int q = 0; q < AJ_UNITS; ++q) {
+                const int j = j0 + q * AJ_THREADS + tid;
+                if (j >= j0 + width) continue;
+                const T r = dense.column(x0[j], j);
+                y0[j] = r;
+                if constexpr (SUM) sum[q][0] += (float)r;
             }
         }
+        x0 += a.in_stride;
+        y0 += a.out_stride;
+        if (c0) c0 += a.copy_stride;
+        if (dense.bias) dense.bias += a.bias_stride;
+        if (dense.mask) dense.mask += a.mask_stride;
     }
     if constexpr (SUM) {
+        float* const p = a.partial + group * a.vocab + j0;
 #pragma unroll
         for (int q = 0; q < AJ_UNITS; ++q) {
-            const int u = (q * AJ_THREADS + (int)threadIdx.x) * N;
-            if (WIDE && u + N <= width) {
+            const int u = (q * AJ_THREADS + tid) * N;
+            if constexpr (WIDE) {
 #pragma unroll
-                for (int e = 0; e < N; e += 4)
-                    if constexpr (N >= 4) store_partial(a.partial + group * a.vocab + j0 + u + e, sum[q][e], sum[q][e + 1], sum[q][e + 2], sum[q][e + 3]);
-            } else if (!WIDE && u < width) {
-                a.partial[group * a.vocab + j0 + u] = sum[q][0];
+                for (int e = 0; e < N; e += 4) if (u + N <= width) store_partial(p + u + e, sum[q][e], sum[q][e + 1], sum[q][e + 2], sum[q][e + 3]);
+            } else {
+                if (u < width) p[u] = sum[q][0];
             }
         }
-        // (wide rows start on a boundary: the columns left are behind the last whole vector)
-        if (WIDE && threadIdx.x >= 32 && (int)threadIdx.x - 32 < width % N) a.partial[group * a.vocab + j0 + width / N * N + threadIdx.x - 32] = edge;
+        // (the columns left are behind the last whole vector)
+        if (WIDE && tid >= 32 && tid - 32 < width % N) p[width / N * N + tid - 32] = edge;
     }
+}
+
+// What the kernel of the listed words does beside them.
+enum : int {
+    AJ_WORDS_ONLY = 0,                   // the stream has written the others
+    AJ_MASKED_TOO = 1,                   // in place: the masked words
+    AJ_ALL_TOO = 2,                      // in place with a bias: every other word (one row a block; the listed words' results wait in the table)
+};
+
+struct WordsArgs {
+    const void* logits;
+    const void* dout;                    // gradient: of the adjusted logits
+    void* out;                           // adjusted logits, or the gradient of the logits
+    float* dvalue;
+    long long stride, dout_stride, out_stride, n_rows;
+    uint32_t other;
+    int vocab, chunk, chunks, rows;      // rows: in turn
+    int entries;                         // of the list at most
+    int mode;
+    Rules r;
+};
+
+template <typename T, bool GRAD>
+__global__ void __launch_bounds__(AJ_THREADS)
+adjust_words_kernel(const __grid_constant__ WordsArgs a)
+{
+    using S = Sixteen<T>;
+    constexpr int N = S::N;
+    extern __shared__ __align__(16) uint32_t shared[];
+    __shared__ typename S::Entry masks[16];
+    __shared__ Plan plans[AJ_ROWS];
+    __shared__ int listed;
+    const int part = blockIdx.x % a.chunks;
+    const long long begin = (long long)(blockIdx.x / a.chunks) * a.rows;
+    const int rows = (int)min((long long)a.rows, a.n_rows - begin);
+    const int j0 = part * a.chunk, width = min(a.chunk, a.vocab - j0);
+    if (threadIdx.x < 16) masks[threadIdx.x] = S::entry((int)threadIdx.x);
+    if ((int)threadIdx.x < rows) plans[threadIdx.x] = plan_of(a.r, begin + threadIdx.x);
+    Table table(shared, &listed, a.chunk, j0, width);
+    float* const sums = reinterpret_cast<float*>(shared + Table::words(a.chunk, a.entries));
+    int* const words = reinterpret_cast<int*>(sums + (GRAD ? 0 : a.r.n_bias));
+    table.clear(a.chunk);
+    __syncthreads();
+    table.now.history = plans[0].history;              // with nothing of it yet
+    bool waited = a.mode != AJ_WORDS_ONLY;             // for the stream: its stores come first
+    for (int i = 0; i < rows; ++i) {
+        const long long row = begin + i;
+        const Plan plan = plans[i];
+        const T* const x0 = static_cast<const T*>(a.logits) + row * a.stride;
+        const T* const g0 = GRAD ? static_cast<const T*>(a.dout) + row * a.dout_stride : nullptr;
+        T* const y0 = static_cast<T*>(a.out) + row * a.out_stride;
+        const T* const b0 = !GRAD && a.r.bias ? static_cast<const T*>(a.r.bias) + row * a.r.bias_stride : nullptr;
+        const uint32_t* const m0 = a.r.mask ? a.r.mask + row * a.r.mask_stride : nullptr;
+        if (a.r.history) table.set(a.r, plan, a.vocab, a.chunk);
+        if constexpr (GRAD) {
+            // (in place: before anything of the row is overwritten)
+            if (a.dvalue)
+                for (int k = threadIdx.x; k < a.r.n_bias; k += AJ_THREADS) {
+                    const int w = token_at(a.r.word, row * a.r.n_bias + k, a.r.words64, a.vocab);
+                    if (w < 0 ? j0 == 0 : w >= j0 && w < j0 + width) a.dvalue[row * a.r.n_bias + k] = w >= 0 && allowed(m0, w) ? (float)g0[w] : 0.0f;
+                }
+        } else if (a.r.n_bias) {                       // (such rows are not taken in turn)
+            read_words(a.r, row, a.vocab, words);
+            __syncthreads();
+            sum_words(a.r, row, table, words, sums);
+        }
+        __syncthreads();
+        const int n = listed;
+        if (i + 1 < rows && a.r.history) table.look_ahead(a.r, plans[i + 1], a.vocab);
+        // what a listed word becomes
+        auto result = [&](int k, float x, float g) {
+            const uint32_t t = table.word[k];
+            if constexpr (GRAD) return x > 0.0f ? __fdiv_rn(g, plan.rho) : g * plan.rho;
+            float y = penalised(x, t, plan);
+            if (b0) y += (float)b0[j0 + k];
+            const uint32_t slot = t >> AJ_SLOT_SHIFT & AJ_SLOT;
+            return slot ? y + sums[slot - 1] : y;
+        };
+        for (int first = threadIdx.x; first < n; first += AJ_THREADS * AJ_BATCH) {
+            int at[AJ_BATCH];
+            T x[AJ_BATCH], g[AJ_BATCH];
+#pragma unroll
+            for (int k = 0; k < AJ_BATCH; ++k) {
+                at[k] = first + k * AJ_THREADS < n ? table.list[first + k * AJ_THREADS] : -1;
+                if (at[k] >= 0 && !allowed(m0, j0 + at[k])) at[k] = -1;
+                if (at[k] >= 0) {
+                    x[k] = x0[j0 + at[k]];
+                    if constexpr (GRAD) g[k] = g0[j0 + at[k]];
+                }
+            }
+            if (!waited) { ptx::grid_wait_previous(); waited = true; }
+#pragma unroll
+            for (int k = 0; k < AJ_BATCH; ++k) {
+                if (at[k] < 0) continue;
+                const float y = result(at[k], (float)x[k], GRAD ? (float)g[k] : 0.0f);
+                if (a.mode == AJ_ALL_TOO) table.word[at[k]] = __float_as_uint(y);
+                else y0[j0 + at[k]] = (T)y;
+            }
+        }
+        __syncthreads();                               // done with the table, and with vectors that hold listed words and masked ones
+        if (a.mode == AJ_WORDS_ONLY || (a.mode == AJ_MASKED_TOO && !m0)) continue;
+        const Span<T> span(y0, j0, width);
+        const Dense<T> dense{ b0, m0, masks, a.other, (a.vocab + 31) / 32 };
+        for (int u = threadIdx.x; u < span.full; u += AJ_THREADS) {
+            const int j = span.first + u * N;
+            uint4* const y = reinterpret_cast<uint4*>(y0 + j);
+            if (a.mode == AJ_ALL_TOO) {
+                *y = dense.template vector<false>(*y, j);
+            } else {
+                const uint32_t live = bits_at<N>(m0, j, dense.mask_words);
+                if (live != (1u << N) - 1u) *y = select4(S::masks(masks, live), live ? *y : make_uint4(0, 0, 0, 0), a.other);
+            }
+        }
+        if (const int j = span.single(); j >= 0 && (a.mode == AJ_ALL_TOO || !allowed(m0, j))) y0[j] = dense.column(y0[j], j);
+        if (a.mode != AJ_ALL_TOO) continue;
+        __syncthreads();
+        for (int k = threadIdx.x; k < n; k += AJ_THREADS) {
+            const int j = table.list[k];
+            if (allowed(m0, j0 + j)) y0[j0 + j] = (T)__uint_as_float(table.word[j]);
+        }
+    }
+    if (!waited) ptx::grid_wait_previous();            // what comes next in the stream may count on both
 }
 
 template <typename T>
@@ -664,8 +554,9 @@ adjust_bias_join_kernel(const float* __restrict__ partial, int groups, int vocab
 }
 
 constexpr int AJ_MAX_GROUPS = 256;       // rows of partial sums for a shared bias
-constexpr int AJ_PLACE_CHUNK = 16384;    // in place: little is read, so more words for one reading of the history
-constexpr int AJ_MOST_SMEM = (Table::words(AJ_PLACE_CHUNK, AJ_PLACE_CHUNK) + 2 * APOLLO_MAX_BIAS_WORDS) * 4;
+constexpr int AJ_WORDS_CHUNK = 16384;
+constexpr int AJ_DEPTH = 16;
+constexpr int AJ_MOST_SMEM = (Table::words(AJ_WORDS_CHUNK, AJ_WORDS_CHUNK) + 2 * APOLLO_MAX_BIAS_WORDS) * 4;
 
 bool whole_vectors(const void* p, int64_t stride, size_t e) { return (uintptr_t)p % 16 == 0 && (size_t)stride * e % 16 == 0; }
 
@@ -718,26 +609,6 @@ int check_shape(int64_t n_rows, int64_t vocab, int64_t stride, int32_t dtype)
     return APOLLO_OK;
 }
 
-// How a call is cut up: chunks of the vocabulary, rows in turn.
-struct Cut { int chunk, chunks, rows; };
-
-// `most`: elements a block of threads can have of a row.  Smaller chunks while there are fewer blocks than the chip holds (a row of
-// history is read once per chunk, so no smaller than that); rows that share a history in turn, as long as 16 blocks per multiprocessor remain.
-Cut cut_up(int64_t n_rows, int64_t vocab, const Rules& r, int most, bool in_turn, int sms)
-{
-    Cut c;
-    c.chunk = most;
-    while (c.chunk > 1024 && n_rows * ((vocab + c.chunk - 1) / c.chunk) < 4LL * sms) c.chunk /= 2;
-    c.chunks = (int)((vocab + c.chunk - 1) / c.chunk);
-    int64_t rows = 1;
-    if (in_turn && r.history && r.share > 1) {
-        rows = n_rows * c.chunks / (16LL * sms);
-        rows = rows < 1 ? 1 : rows > AJ_ROWS ? AJ_ROWS : rows;
-    }
-    c.rows = (int)rows;
-    return c;
-}
-
 // Words of a chunk that can be listed.
 int list_entries(const Rules& r, int named, int chunk)
 {
@@ -745,59 +616,96 @@ int list_entries(const Rules& r, int named, int chunk)
     return (int)(n < chunk ? n : chunk);
 }
 
+// Launches the stream.  Small calls in smaller chunks, so that every multiprocessor has a block.
 template <typename T>
-cudaError_t run_adjust(AdjustArgs a, int sms, cudaStream_t stream)
+cudaError_t run_stream(StreamArgs a, int sms, int* groups, cudaStream_t stream)
 {
-    constexpr int N = Sixteen<T>::N;
-    const bool sparse = a.logits == a.out && !a.r.bias;
-    const Cut c = cut_up(a.n_rows, a.vocab, a.r, sparse ? AJ_PLACE_CHUNK : AJ_UNITS * AJ_THREADS * N, !sparse && a.r.n_bias == 0, sms);
-    a.chunk = c.chunk; a.chunks = c.chunks; a.rows = c.rows;
-    a.entries = list_entries(a.r, a.r.n_bias, c.chunk);
-    const int64_t blocks = (a.n_rows + c.rows - 1) / c.rows * c.chunks;
+    constexpr size_t e = sizeof(T);
+    const bool sum = a.partial != nullptr;
+    const bool even = whole_vectors(a.in, a.in_stride, e) && whole_vectors(a.out, a.out_stride, e) && whole_vectors(a.copy, a.copy ? a.copy_stride : 0, e) &&
+                      whole_vectors(a.bias, a.bias ? a.bias_stride : 0, e);
+    a.chunk = AJ_UNITS * AJ_THREADS * (even || !sum ? Sixteen<T>::N : 1);
+    if (!sum)
+        while (a.chunk > 2048 && a.n_rows * ((a.vocab + a.chunk - 1) / a.chunk) < 2LL * sms) a.chunk /= 2;
+    a.chunks = (a.vocab + a.chunk - 1) / a.chunk;
+    a.rows = sum ? (int)((a.n_rows + AJ_MAX_GROUPS - 1) / AJ_MAX_GROUPS) : 1;
+    const int64_t n = (a.n_rows + a.rows - 1) / a.rows;
+    *groups = (int)n;
+    if (n * a.chunks > INT32_MAX) return cudaErrorInvalidConfiguration;
+    const unsigned grid = (unsigned)(n * a.chunks);
+    if (sum) {
+        if (even) adjust_stream_kernel<T, true, true><<<grid, AJ_THREADS, 0, stream>>>(a);
+        else adjust_stream_kernel<T, false, true><<<grid, AJ_THREADS, 0, stream>>>(a);
+    } else {
+        if (even) adjust_stream_kernel<T, true, false><<<grid, AJ_THREADS, 0, stream>>>(a);
+        else adjust_stream_kernel<T, false, false><<<grid, AJ_THREADS, 0, stream>>>(a);
+    }
+    return cudaGetLastError();
+}
+
+// Launches the kernel of the listed words, after the stream where that has run.  Chunks as large as shared memory holds for several blocks
+// (a row of the history is read once per chunk), smaller ones while there are fewer blocks than the chip holds; rows that share a history in
+// turn, as long as AJ_DEPTH blocks per multiprocessor remain.
+template <typename T, bool GRAD>
+cudaError_t run_words(WordsArgs a, int sms, cudaStream_t stream)
+{
+    const int named = GRAD ? 0 : a.r.n_bias;
+    a.chunk = AJ_WORDS_CHUNK;
+    while (a.chunk > 1024 && a.n_rows * ((a.vocab + a.chunk - 1) / a.chunk) < 4LL * sms) a.chunk /= 2;
+    a.chunks = (a.vocab + a.chunk - 1) / a.chunk;
+    a.entries = list_entries(a.r, named, a.chunk);
+    int64_t rows = 1;
+    if (a.r.history && a.r.share > 1 && named == 0 && a.mode != AJ_ALL_TOO) {
+        rows = a.n_rows * a.chunks / ((int64_t)AJ_DEPTH * sms);
+        rows = rows < 1 ? 1 : rows > AJ_ROWS ? AJ_ROWS : rows;
+    }
+    a.rows = (int)rows;
+    const int64_t blocks = (a.n_rows + rows - 1) / rows * a.chunks;
     if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
-    const bool table = a.r.history || a.r.n_bias;
-    if (sparse && !table && !a.r.mask) return cudaSuccess;
-    const int smem = sparse ? (Table::words(c.chunk, a.entries) + 2 * a.r.n_bias) * 4
-                            : table ? (Table::words(c.chunk, a.entries) + 2 * a.r.n_bias + Stream<T, true>::words(c.chunk)) * 4 : 0;
-    auto launch = [&](auto* kernel) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, AJ_MOST_SMEM);
-        if (e != cudaSuccess) return e;
-        kernel<<<(unsigned)blocks, AJ_THREADS, smem, stream>>>(a);
-        return cudaGetLastError();
-    };
-    if (sparse) return launch(adjust_place_kernel<T>);
-    const bool even = whole_vectors(a.logits, a.stride, sizeof(T)) && whole_vectors(a.out, a.out_stride, sizeof(T)) && whole_vectors(a.r.bias, a.r.bias_stride, sizeof(T));
-    if (table) return even ? launch(adjust_kernel<T, true, true>) : launch(adjust_kernel<T, true, false>);
-    return even ? launch(adjust_kernel<T, false, true>) : launch(adjust_kernel<T, false, false>);
+    const int smem = (Table::words(a.chunk, a.entries) + 2 * named) * 4;
+    cudaError_t e = cudaFuncSetAttribute(adjust_words_kernel<T, GRAD>, cudaFuncAttributeMaxDynamicSharedMemorySize, AJ_MOST_SMEM);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(AJ_THREADS);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.mode == AJ_WORDS_ONLY ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, adjust_words_kernel<T, GRAD>, a);
 }
 
 template <typename T>
-cudaError_t run_adjust_grad(AdjustGradArgs a, bool wide, int sms, int* groups, cudaStream_t stream)
+cudaError_t run_adjust(WordsArgs a, int sms, cudaStream_t stream)
 {
-    const int N = wide ? Sixteen<T>::N : 1;
-    const bool sum = a.partial != nullptr, sparse = a.dlogits == a.dout && !sum && !a.dbias;
-    Cut c;
-    if (sum) {
-        c.chunk = AJ_UNITS * AJ_THREADS * N;
-        c.chunks = (a.vocab + c.chunk - 1) / c.chunk;
-        c.rows = (int)((a.n_rows + AJ_MAX_GROUPS - 1) / AJ_MAX_GROUPS);
-    } else {
-        c = cut_up(a.n_rows, a.vocab, a.r, sparse ? AJ_PLACE_CHUNK : AJ_UNITS * AJ_THREADS * N, true, sms);
-    }
-    a.chunk = c.chunk; a.chunks = c.chunks; a.rows = c.rows;
-    *groups = (int)((a.n_rows + c.rows - 1) / c.rows);
-    if ((int64_t)*groups * c.chunks > INT32_MAX) return cudaErrorInvalidConfiguration;
-    const unsigned grid = (unsigned)(*groups * c.chunks);
-    const int smem = a.r.history ? Table::words(c.chunk, list_entries(a.r, 0, c.chunk)) * 4 : 0;
-    auto launch = [&](auto* kernel) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, AJ_MOST_SMEM);
+    const bool place = a.logits == a.out, table = a.r.history || a.r.n_bias;
+    a.other = Sixteen<T>::MINUS_INF;
+    a.mode = !place || !table ? AJ_WORDS_ONLY : a.r.bias ? AJ_ALL_TOO : AJ_MASKED_TOO;
+    if (a.mode == AJ_WORDS_ONLY && (!place || a.r.bias || a.r.mask)) {
+        StreamArgs s = {};
+        s.in = a.logits; s.out = a.out; s.bias = a.r.bias; s.mask = a.r.mask;
+        s.in_stride = a.stride; s.out_stride = a.out_stride; s.bias_stride = a.r.bias_stride; s.mask_stride = a.r.mask_stride;
+        s.n_rows = a.n_rows; s.vocab = a.vocab; s.other = a.other;
+        int groups = 0;
+        const cudaError_t e = run_stream<T>(s, sms, &groups, stream);
         if (e != cudaSuccess) return e;
-        kernel<<<grid, AJ_THREADS, smem, stream>>>(a);
-        return cudaGetLastError();
-    };
-    if (!sum) return a.r.history ? launch(adjust_grad_kernel<T, true, false, true>) : launch(adjust_grad_kernel<T, false, false, true>);
-    if (wide) return a.r.history ? launch(adjust_grad_kernel<T, true, true, true>) : launch(adjust_grad_kernel<T, false, true, true>);
-    return a.r.history ? launch(adjust_grad_kernel<T, true, true, false>) : launch(adjust_grad_kernel<T, false, true, false>);
+    }
+    return table ? run_words<T, false>(a, sms, stream) : cudaSuccess;
+}
+
+template <typename T>
+cudaError_t run_adjust_grad(WordsArgs a, StreamArgs s, int sms, int* groups, cudaStream_t stream)
+{
+    const bool place = a.dout == a.out, table = a.r.history || a.dvalue;
+    a.mode = !place || s.copy || s.partial || !a.r.history ? AJ_WORDS_ONLY : AJ_MASKED_TOO;
+    if (a.mode == AJ_WORDS_ONLY && (!place || s.copy || s.partial || s.mask)) {
+        const cudaError_t e = run_stream<T>(s, sms, groups, stream);
+        if (e != cudaSuccess) return e;
+    }
+    return table ? run_words<T, true>(a, sms, stream) : cudaSuccess;
 }
 
 }  // namespace
@@ -814,7 +722,7 @@ extern "C" int apollo_adjust_logits(const void* d_logits, int64_t row_stride, in
     if (out_stride < vocab) return APOLLO_ERR_SHAPE;
     if (!rules) return APOLLO_ERR_INVALID_ARG;
     const size_t e = dtype == APOLLO_DT_BF16 ? 2 : 4;
-    AdjustArgs a = {};
+    WordsArgs a = {};
     rc = check_rules(rules, n_rows, vocab, e, false, &a.r);
     if (rc != APOLLO_OK) return rc;
     if (n_rows == 0) return APOLLO_OK;
@@ -848,7 +756,7 @@ extern "C" int apollo_adjust_logits_grad(const void* d_logits, int64_t row_strid
     if (grad_out_stride < vocab || grad_logits_stride < vocab || (grad_bias_stride != 0 && grad_bias_stride < vocab)) return APOLLO_ERR_SHAPE;
     if (!rules) return APOLLO_ERR_INVALID_ARG;
     const size_t e = dtype == APOLLO_DT_BF16 ? 2 : 4;
-    AdjustGradArgs a = {};
+    WordsArgs a = {};
     rc = check_rules(rules, n_rows, vocab, e, true, &a.r);
     if (rc != APOLLO_OK) return rc;
     const bool shared = d_grad_bias && grad_bias_stride == 0;
@@ -872,18 +780,18 @@ extern "C" int apollo_adjust_logits_grad(const void* d_logits, int64_t row_strid
     int sms = 0;
     rc = device_sms(&sms);
     if (rc != APOLLO_OK) return rc;
-    a.logits = d_logits; a.dout = d_grad_out; a.dlogits = d_grad_logits; a.dbias = shared ? nullptr : d_grad_bias;
-    a.partial = shared ? static_cast<float*>(d_workspace) : nullptr; a.dvalue = a.r.n_bias ? d_grad_value : nullptr;
-    a.stride = row_stride; a.dout_stride = grad_out_stride; a.dlogits_stride = grad_logits_stride; a.dbias_stride = grad_bias_stride;
-    a.n_rows = n_rows; a.vocab = (int)vocab;
-    // sums over rows whose vectors start at different columns go element by element
-    const bool wide = !shared || whole_vectors(d_grad_logits, grad_logits_stride, e);
+    a.logits = d_logits; a.dout = d_grad_out; a.out = d_grad_logits; a.dvalue = a.r.n_bias ? d_grad_value : nullptr;
+    a.stride = row_stride; a.dout_stride = grad_out_stride; a.out_stride = grad_logits_stride; a.n_rows = n_rows; a.vocab = (int)vocab;
+    StreamArgs s = {};
+    s.in = d_grad_out; s.out = d_grad_logits; s.copy = shared ? nullptr : d_grad_bias; s.partial = shared ? static_cast<float*>(d_workspace) : nullptr;
+    s.mask = a.r.mask; s.in_stride = grad_out_stride; s.out_stride = grad_logits_stride; s.copy_stride = grad_bias_stride;
+    s.mask_stride = a.r.mask_stride; s.n_rows = n_rows; s.vocab = (int)vocab;
     int groups = 0;
-    cudaError_t err = dtype == APOLLO_DT_BF16 ? run_adjust_grad<__nv_bfloat16>(a, wide, sms, &groups, stream) : run_adjust_grad<float>(a, wide, sms, &groups, stream);
+    cudaError_t err = dtype == APOLLO_DT_BF16 ? run_adjust_grad<__nv_bfloat16>(a, s, sms, &groups, stream) : run_adjust_grad<float>(a, s, sms, &groups, stream);
     if (err == cudaSuccess && shared) {
         const unsigned grid = (unsigned)((vocab + AJ_THREADS - 1) / AJ_THREADS);
-        if (dtype == APOLLO_DT_BF16) adjust_bias_join_kernel<<<grid, AJ_THREADS, 0, stream>>>(a.partial, groups, (int)vocab, static_cast<__nv_bfloat16*>(d_grad_bias));
-        else adjust_bias_join_kernel<<<grid, AJ_THREADS, 0, stream>>>(a.partial, groups, (int)vocab, static_cast<float*>(d_grad_bias));
+        if (dtype == APOLLO_DT_BF16) adjust_bias_join_kernel<<<grid, AJ_THREADS, 0, stream>>>(s.partial, groups, (int)vocab, static_cast<__nv_bfloat16*>(d_grad_bias));
+        else adjust_bias_join_kernel<<<grid, AJ_THREADS, 0, stream>>>(s.partial, groups, (int)vocab, static_cast<float*>(d_grad_bias));
         err = cudaGetLastError();
     }
     return err == cudaSuccess ? APOLLO_OK : APOLLO_ERR_CUDA;
