@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import importlib.util
 import math
 from pathlib import Path
 from typing import NamedTuple
@@ -16,6 +17,7 @@ import torch
 
 _PKG = Path(__file__).resolve().parent
 LIB_PATH = _PKG / "libapollo.so"
+MARSHAL_PATH = _PKG / "_marshal.so"
 DEBUG_LIB_PATH = _PKG / "libapollo_debug.so"     # built with -DAPOLLO_DEBUG: index checks inside every kernel
 
 OK = 0
@@ -493,28 +495,27 @@ def token_logprobs_grad(logits, targets, lse, entropy, d_logprob, d_entropy=None
     return out
 
 
-class _List:
-    """A list of gradients as the library takes it: addresses, lengths and types, and the device that they are on."""
+_marshal_module = None
 
-    def __init__(self, tensors, what: str, device=None):
-        live = [x for x in tensors if x is not None]
-        dtypes = {x.dtype for x in live}
-        if not dtypes <= {torch.bfloat16, torch.float32}:
-            raise ValueError(f"{what} must be bfloat16 or float32, got {dtypes}")
-        if not all([x.is_cuda and x.is_contiguous() for x in live]):
-            raise ValueError(f"{what} must be contiguous CUDA tensors")
-        devices = {x.get_device() for x in live}
-        if len(devices) > 1 or (device is not None and devices and devices != {device.index}):
-            raise _two_devices()
-        self.n = n = len(tensors)
-        self.device = device if device is not None else live[0].device if live else None
-        bf16 = torch.bfloat16
-        if len(live) == n:
-            self.pointers = (ctypes.c_uint64 * n)(*[x.data_ptr() for x in live])
-            self.dtypes = (ctypes.c_int32 * n)(*[x.dtype is bf16 for x in live])
-        else:
-            self.pointers = (ctypes.c_uint64 * n)(*[0 if x is None else x.data_ptr() for x in tensors])
-            self.dtypes = (ctypes.c_int32 * n)(*[x is not None and x.dtype is bf16 for x in tensors])
+
+def _marshal():
+    """The extension that reads tensors (csrc/marshal.cpp); raises if it has not been built (there is no fallback)."""
+    global _marshal_module
+    if _marshal_module is None:
+        if not MARSHAL_PATH.exists():
+            raise ImportError(f"{MARSHAL_PATH} is missing: run `python -m paper_2412_05270_b200.build`")
+        spec = importlib.util.spec_from_file_location("_marshal", MARSHAL_PATH)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        _marshal_module = module
+    return _marshal_module
+
+
+def _on_index(stream, index: int):
+    """As _on, for the device with that index."""
+    if stream is None and index == _current_device():
+        return _here
+    return _on(stream, torch.device("cuda", index))
 
 
 def grad_norm(grads, max_norm: float = math.inf, out=None, workspace=None, stream=None) -> torch.Tensor:
@@ -523,25 +524,24 @@ def grad_norm(grads, max_norm: float = math.inf, out=None, workspace=None, strea
     grads: contiguous CUDA tensors, bfloat16 or float32 in any mixture, None for one that is left out; workspace: a uint8 CUDA
     tensor of grad_norm_workspace_bytes(), made if None."""
     grads = list(grads)
-    xs = _List(grads, "grads")
-    device = xs.device
-    if device is None:
+    pointers, lengths, types, device, live = _marshal().pack("grads", grads, None, -1)
+    if live == 0:
         raise ValueError("grad_norm needs a gradient")
+    n = len(grads)
     for x, what in ((out, "out"), (workspace, "workspace")):
         if x is not None:
-            if x.device != device:
+            if x.get_device() != device:
                 raise _two_devices()
             if not x.is_contiguous():
                 raise ValueError(f"{what} must be contiguous")
     if out is not None and (out.dtype != torch.float32 or out.numel() != 2):
         raise ValueError("out must hold two float32 values")
-    numel = (ctypes.c_int64 * xs.n)(*[0 if x is None else x.numel() for x in grads])
-    with _on(stream, device):
+    with _on_index(stream, device):
         if out is None:
-            out = torch.empty_strided((2,), (1,), dtype=torch.float32, device=device)
+            out = torch.empty_strided((2,), (1,), dtype=torch.float32, device="cuda")
         if workspace is None:
-            workspace = torch.empty_strided((grad_norm_workspace_bytes(xs.n),), (1,), dtype=torch.uint8, device=device)
-        _check(load().apollo_grad_norm(xs.pointers, numel, xs.dtypes, xs.n, max_norm, out.data_ptr(), workspace.data_ptr(),
+            workspace = torch.empty_strided((grad_norm_workspace_bytes(n),), (1,), dtype=torch.uint8, device="cuda")
+        _check(load().apollo_grad_norm(pointers, lengths, types, n, max_norm, out.data_ptr(), workspace.data_ptr(),
                                        workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "apollo_grad_norm")
     return out
 
@@ -569,17 +569,20 @@ class AdamW:
     def __init__(self, params, bits: int = 8, beta1=0.9, beta2=0.999, eps=1e-8, seed: int = 0, bias_correction: bool = True,
                  state=None):
         self.lib = load()
+        self._pack = _marshal().pack
         self.params = list(params)
         if not self.params or any(p is None for p in self.params):
             raise ValueError("AdamW needs a list of parameters")
-        xs = _List(self.params, "params")
-        if len({a for a, p in zip(xs.pointers, self.params) if p.numel()}) < sum(p.numel() > 0 for p in self.params):
+        _, _, _, index, _ = self._pack("params", self.params, None, -1)
+        used = [p.data_ptr() for p in self.params if p.numel()]
+        if len(set(used)) < len(used):
             raise ValueError("a parameter is in the list twice")
-        self.device, self.bits = xs.device, bits
-        self._shapes = [p.shape for p in self.params]
+        self.device, self._index, self.bits = torch.device("cuda", index), index, bits
+        # (the list as it is now: what a step must find again, whatever becomes of the parameters' data)
+        self._like = [p.detach() for p in self.params]
         numels = [p.numel() for p in self.params]
-        self._numel = (ctypes.c_int64 * xs.n)(*numels)
         self.cfg = AdamWListConfig(int(bits), int(bool(bias_correction)), float(beta1), float(beta2), float(eps), int(seed))
+        self._cfg_at = ctypes.addressof(self.cfg)
         nbytes = adamw_state_bytes(numels, bits)
         self.n_blocks = nbytes // (2 * ADAMW_BLOCK + 2 if bits == 8 else 8 * ADAMW_BLOCK)
         with _on(None, self.device):
@@ -612,13 +615,9 @@ class AdamW:
         lr: a number, or a float32 CUDA tensor of one value; t: a number, or an int64 CUDA tensor of one value (read when the step
         runs: a captured step can be replayed with other values); factor: a float32 CUDA tensor of one value that the gradients are multiplied by
         (grad_norm(...)[1:]); where it is not finite the step changes nothing."""
-        grads = list(grads)
-        params = _List(self.params, "params", self.device)
-        if len(grads) != params.n:
-            raise ValueError("parameter list length differs from the context's")
-        xs = _List(grads, "grads", self.device)
-        if [p.shape for p in self.params] != self._shapes or not all([g is None or g.shape == s for g, s in zip(grads, self._shapes)]):
-            raise ValueError("gradients must have their parameters' shapes")
+        index = self._index
+        pointers, lengths, types, _, _ = self._pack("params", self.params, self._like, index)
+        g_pointers, _, g_types, _, _ = self._pack("grads", grads, self.params, index)
         lr_at = t_at = factor_at = None
         if isinstance(lr, torch.Tensor):
             lr, lr_at = 0.0, self._scalar(lr, torch.float32, "lr")
@@ -626,10 +625,10 @@ class AdamW:
             t, t_at = 0, self._scalar(t, torch.int64, "t")
         if factor is not None:
             factor_at = self._scalar(factor, torch.float32, "factor")
-        with _on(stream, self.device):
-            _check(self.lib.apollo_adamw_list_step(ctypes.byref(self.cfg), params.pointers, xs.pointers, self._numel, params.dtypes,
-                                                   xs.dtypes, xs.n, self.state.data_ptr(), self.state.numel(), lr, wd, t, factor_at,
-                                                   lr_at, t_at, self._run(stream)), "apollo_adamw_list_step")
+        with _on_index(stream, index):
+            _check(self.lib.apollo_adamw_list_step(self._cfg_at, pointers, g_pointers, lengths, types, g_types, len(self.params),
+                                                   self.state.data_ptr(), self.state.numel(), lr, wd, t, factor_at, lr_at, t_at,
+                                                   self._run(stream)), "apollo_adamw_list_step")
 
     def moments(self, stream=None):
         """(m, v) of all blocks in list order, ADAMW_BLOCK n_blocks values each: what 8-bit codes stand for, exactly, in bfloat16; of
@@ -643,76 +642,114 @@ class AdamW:
         return m, v
 
 
-def _rules_of(logits, device, history, lengths, start, repetition, frequency, presence, bias, bias_index, bias_value, mask):
-    """The rules as the library takes them, and the tensors that they point into."""
-    n, vocab = logits.shape
+# What _marshal().describe() gives of a tensor, by place.
+_AT, _DEVICE, _TYPE, _DIM, _ROWS, _COLS, _STEP, _NEXT, _WHOLE = range(9)
+_F32, _BF16, _I32, _I64 = range(4)
+
+
+def _described_rows(x, what: str, like=None):
+    """describe() of a 2-D CUDA tensor, bfloat16 or float32, whose rows are contiguous and do not overlap, and the stride between them;
+    like: describe() of one with the same type, shape and device."""
+    d = _marshal().describe(x)
+    if like is not None and (d[_TYPE] != like[_TYPE] or d[_DIM] != 2 or d[_ROWS:_COLS + 1] != like[_ROWS:_COLS + 1]):
+        raise ValueError(f"{what} must have the logits' dtype and shape")
+    if d[_TYPE] not in (_F32, _BF16):
+        raise ValueError(f"{what} must be bfloat16 or float32, got {x.dtype}")
+    if like is not None and d[_DEVICE] != like[_DEVICE]:
+        raise _two_devices()
+    rows, cols = d[_ROWS], d[_COLS]
+    if d[_DEVICE] < 0 or d[_DIM] != 2 or (rows > 0 and cols > 1 and d[_NEXT] != 1):
+        raise ValueError(f"{what} must be a 2-D CUDA tensor with contiguous rows")
+    if rows <= 1:
+        return d, max(cols, 1)
+    if d[_STEP] < cols:
+        raise ValueError(f"{what} must not have overlapping rows")
+    return d, d[_STEP]
+
+
+def _rules_of(of, history, lengths, start, repetition, frequency, presence, bias, bias_index, bias_value, mask):
+    """The rules for logits described by `of` as the library takes them, and copies that they point into."""
+    describe = _marshal().describe
+    n, vocab, device, logits_type = of[_ROWS], of[_COLS], of[_DEVICE], of[_TYPE]
     r = LogitRules(repetition=1.0)
     kept = []
 
-    def here(x, what, dtype, shape):
-        if x.dtype != dtype or tuple(x.shape) != shape:
-            raise ValueError(f"{what} must be {dtype} of shape {shape}")
-        if x.device != device:
+    def whole(x, d):
+        if d[_DEVICE] != device:
             raise _two_devices()
-        if not x.is_contiguous():
+        if not d[_WHOLE]:
             x = x.contiguous()
             kept.append(x)
-        return x
+            return x.data_ptr()
+        return d[_AT]
+
+    def per_row(x, kind, what):
+        d = describe(x)
+        if d[_TYPE] != kind or d[_DIM] != 1 or d[_ROWS] != n:
+            raise ValueError(f"{what} must be {'int32' if kind == _I32 else 'float32'} with one entry per row of logits")
+        return whole(x, d)
     if history is not None:
-        r.history_type = _index_of(history, "history")
-        if history.dim() != 2 or (n and (history.shape[0] < 1 or n % history.shape[0])):
+        d = describe(history)
+        if d[_TYPE] not in (_I32, _I64):
+            raise ValueError("history must be of int32 or int64")
+        rows, length, stride = d[_ROWS], d[_COLS], d[_STEP]
+        if d[_DIM] != 2 or (n and (rows < 1 or n % rows)):
             raise ValueError("history must have a row for each row of logits, or for the same number of them each")
-        if history.device != device:
-            raise _two_devices()
-        rows, length = history.shape
-        stride = history.stride(0) if rows > 1 else 0
-        if (length > 1 and history.stride(1) != 1) or 0 < stride < length:
+        if (length > 1 and d[_NEXT] != 1) or (rows > 1 and 0 < stride < length):
             history = history.contiguous()
             kept.append(history)
-            stride = length if rows > 1 else 0
-        r.history, r.history_rows, r.history_len, r.history_stride = history.data_ptr() if history.numel() else None, max(rows, 1), length, stride
-        for x, at in ((lengths, "length"), (start, "start")):
-            if x is not None:
-                setattr(r, at, here(x, at, torch.int32, (n,)).data_ptr())
-        for x, at in ((repetition, "repetition"), (frequency, "frequency"), (presence, "presence")):
-            if isinstance(x, torch.Tensor):
-                setattr(r, at + "_at", here(x, at, torch.float32, (n,)).data_ptr())
-            else:
-                setattr(r, at, x)
-    if bias is not None:
-        if bias.dtype != logits.dtype or tuple(bias.shape) not in ((vocab,), (n, vocab)):
-            raise ValueError("bias must have the logits' dtype and be a row of the vocabulary, or one for each row of logits")
-        if bias.device != device:
+            d, stride = describe(history), length
+        if d[_DEVICE] != device:
             raise _two_devices()
-        if bias.dim() == 2 and n > 1 and bias.stride(0) >= vocab and (vocab == 1 or bias.stride(1) == 1):
-            r.bias_stride = bias.stride(0)
-        elif not bias.is_contiguous():
-            bias = bias.contiguous()
-            kept.append(bias)
-            r.bias_stride = vocab if bias.dim() == 2 else 0
-        elif bias.dim() == 2:
-            r.bias_stride = vocab
-        r.bias = bias.data_ptr()
+        if rows and length:
+            r.history, r.history_rows, r.history_len, r.history_stride = d[_AT], rows, length, stride if rows > 1 else 0
+            r.history_type = INDEX_I64 if d[_TYPE] == _I64 else INDEX_I32
+        if lengths is not None:
+            r.length = per_row(lengths, _I32, "lengths")
+        if start is not None:
+            r.start = per_row(start, _I32, "start")
+        if isinstance(repetition, torch.Tensor):
+            r.repetition_at = per_row(repetition, _F32, "repetition")
+        else:
+            r.repetition = repetition
+        if isinstance(frequency, torch.Tensor):
+            r.frequency_at = per_row(frequency, _F32, "frequency")
+        else:
+            r.frequency = frequency
+        if isinstance(presence, torch.Tensor):
+            r.presence_at = per_row(presence, _F32, "presence")
+        else:
+            r.presence = presence
+    if bias is not None:
+        d = describe(bias)
+        if d[_TYPE] != logits_type or not ((d[_DIM] == 1 and d[_ROWS] == vocab) or (d[_DIM] == 2 and d[_ROWS] == n and d[_COLS] == vocab)):
+            raise ValueError("bias must have the logits' dtype and be a row of the vocabulary, or one for each row of logits")
+        if d[_DIM] == 2 and n > 1 and d[_STEP] >= vocab and (vocab == 1 or d[_NEXT] == 1):
+            if d[_DEVICE] != device:
+                raise _two_devices()
+            r.bias, r.bias_stride = d[_AT], d[_STEP]
+        else:
+            r.bias, r.bias_stride = whole(bias, d), vocab if d[_DIM] == 2 else 0
     if bias_index is not None:
-        r.bias_word_type = _index_of(bias_index, "bias_index")
-        if bias_index.dim() != 2 or bias_index.shape[0] != n:
+        d = describe(bias_index)
+        if d[_TYPE] not in (_I32, _I64):
+            raise ValueError("bias_index must be of int32 or int64")
+        if d[_DIM] != 2 or d[_ROWS] != n:
             raise ValueError("bias_index must have a row for each row of logits")
-        r.n_bias = bias_index.shape[1]
-        r.bias_word = here(bias_index, "bias_index", bias_index.dtype, tuple(bias_index.shape)).data_ptr()
+        r.bias_word, r.n_bias, r.bias_word_type = whole(bias_index, d), d[_COLS], INDEX_I64 if d[_TYPE] == _I64 else INDEX_I32
         if bias_value is not None:
-            r.bias_value = here(bias_value, "bias_value", torch.float32, tuple(bias_index.shape)).data_ptr()
+            v = describe(bias_value)
+            if v[_TYPE] != _F32 or v[_DIM] != 2 or v[_ROWS] != n or v[_COLS] != d[_COLS]:
+                raise ValueError("bias_value must be float32 of bias_index's shape")
+            r.bias_value = whole(bias_value, v)
     elif bias_value is not None:
         raise ValueError("bias_value needs bias_index")
     if mask is not None:
+        d = describe(mask)
         words = (vocab + 31) // 32
-        if mask.dtype != torch.int32 or tuple(mask.shape) not in ((words,), (1, words), (n, words)):
+        if d[_TYPE] != _I32 or not ((d[_DIM] == 1 and d[_ROWS] == words) or (d[_DIM] == 2 and d[_ROWS] in (1, n) and d[_COLS] == words)):
             raise ValueError(f"mask must be int32 with {words} words of 32 bits a row, one row or one for each row of logits")
-        if mask.device != device:
-            raise _two_devices()
-        if not mask.is_contiguous():
-            mask = mask.contiguous()
-            kept.append(mask)
-        r.mask, r.mask_stride = mask.data_ptr(), words if mask.dim() == 2 and mask.shape[0] > 1 else 0
+        r.mask, r.mask_stride = whole(mask, d), words if d[_DIM] == 2 and d[_ROWS] > 1 else 0
     return r, kept
 
 
@@ -724,23 +761,22 @@ def adjust_logits(logits, history=None, lengths=None, start=None, repetition=1.0
     r // (n / h), of which the first lengths[r] (int32) count, for frequency and presence those from start[r] (int32) on; repetition,
     frequency, presence: numbers, or float32 (n,);  bias: (vocab,) or (n, vocab) of the logits' dtype;  bias_index, bias_value: (n, k)
     words and float32 values;  mask: int32 words of 32 bits, (1 or n, ceil(vocab / 32)), bit set = word allowed."""
-    dtype = _dtype_of(logits, "logits")
-    stride = _rows_of(logits, "logits")
-    n, vocab = logits.shape
-    device = logits.device
-    if out is not None:
-        if out.dtype != logits.dtype or out.shape != logits.shape:
-            raise ValueError("out must have the logits' dtype and shape")
-        if out.device != device:
-            raise _two_devices()
+    of, stride = _described_rows(logits, "logits")
+    n, vocab = of[_ROWS], of[_COLS]
+    if out is not None and out is not logits:
+        to, out_stride = _described_rows(out, "out", of)
+    else:
+        to, out_stride = of, stride
     if bias_index is not None and bias_value is None:
         raise ValueError("bias_index needs bias_value")
-    with _on(stream, device):
-        rules, kept = _rules_of(logits, device, history, lengths, start, repetition, frequency, presence, bias, bias_index, bias_value, mask)
+    with _on_index(stream, of[_DEVICE]):
+        rules, kept = _rules_of(of, history, lengths, start, repetition, frequency, presence, bias, bias_index, bias_value, mask)
+        out_at = to[_AT]
         if out is None:
-            out = torch.empty_strided((n, vocab), (vocab, 1), dtype=logits.dtype, device=device)
-        _check(load().apollo_adjust_logits(logits.data_ptr(), stride, n, vocab, dtype, ctypes.byref(rules), out.data_ptr(),
-                                           _rows_of(out, "out"), _stream_ptr(stream)), "apollo_adjust_logits")
+            out = torch.empty_strided((n, vocab), (vocab, 1), dtype=logits.dtype, device="cuda")
+            out_at, out_stride = out.data_ptr(), vocab
+        _check(load().apollo_adjust_logits(of[_AT], stride, n, vocab, of[_TYPE], ctypes.byref(rules), out_at, out_stride, _stream_ptr(stream)),
+               "apollo_adjust_logits")
     return out
 
 
@@ -761,41 +797,37 @@ def adjust_logits_grad(logits, d_out, history=None, lengths=None, repetition=1.0
     """apollo_adjust_logits_grad: the gradients of `adjust_logits` for its logits, a bias ("shared": (vocab,), "row": (n, vocab), "none")
     and, where bias_index is given, the values; rules as there.  out: of the logits' gradient, made if None, may be d_out;
     workspace ("shared"): a uint8 CUDA tensor of adjust_logits_grad_workspace_bytes(), made if None."""
-    dtype = _dtype_of(logits, "logits")
-    stride, d_stride = _rows_of(logits, "logits"), _rows_of(d_out, "d_out")
-    n, vocab = logits.shape
-    device = logits.device
+    of, stride = _described_rows(logits, "logits")
+    d, d_stride = _described_rows(d_out, "d_out", of)
+    n, vocab = of[_ROWS], of[_COLS]
     if bias not in ("none", "shared", "row"):
         raise ValueError('bias must be "none", "shared" or "row"')
-    for x, what in ((d_out, "d_out"), (out, "out")):
-        if x is not None:
-            if x.dtype != logits.dtype or x.shape != logits.shape:
-                raise ValueError(f"{what} must have the logits' dtype and shape")
-            if x.device != device:
-                raise _two_devices()
+    to, out_stride = (d, d_stride) if out is d_out else (None, vocab) if out is None else _described_rows(out, "out", of)
     if workspace is not None:
-        if workspace.device != device:
+        if workspace.get_device() != of[_DEVICE]:
             raise _two_devices()
         if not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous")
-    with _on(stream, device):
-        rules, kept = _rules_of(logits, device, history, lengths, None, repetition, 0.0, 0.0, None, bias_index, None, mask)
+    with _on_index(stream, of[_DEVICE]):
+        rules, kept = _rules_of(of, history, lengths, None, repetition, 0.0, 0.0, None, bias_index, None, mask)
         if out is None:
-            out = torch.empty_strided((n, vocab), (vocab, 1), dtype=logits.dtype, device=device)
+            out = torch.empty_strided((n, vocab), (vocab, 1), dtype=logits.dtype, device="cuda")
         d_bias = d_value = None
+        workspace_at, workspace_bytes = None, 0
         if bias == "shared":
-            d_bias = torch.empty_strided((vocab,), (1,), dtype=logits.dtype, device=device)
+            d_bias = torch.empty_strided((vocab,), (1,), dtype=logits.dtype, device="cuda")
             if workspace is None:
-                workspace = torch.empty_strided((adjust_logits_grad_workspace_bytes(n, vocab),), (1,), dtype=torch.uint8, device=device)
+                workspace = torch.empty_strided((adjust_logits_grad_workspace_bytes(n, vocab),), (1,), dtype=torch.uint8, device="cuda")
+            workspace_at, workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
         elif bias == "row":
-            d_bias = torch.empty_strided((n, vocab), (vocab, 1), dtype=logits.dtype, device=device)
+            d_bias = torch.empty_strided((n, vocab), (vocab, 1), dtype=logits.dtype, device="cuda")
         if bias_index is not None:
-            d_value = torch.empty(tuple(bias_index.shape), dtype=torch.float32, device=device)
+            k = rules.n_bias
+            d_value = torch.empty_strided((n, k), (k, 1), dtype=torch.float32, device="cuda")
         _check(load().apollo_adjust_logits_grad(
-            logits.data_ptr(), stride, n, vocab, dtype, ctypes.byref(rules), d_out.data_ptr(), d_stride, out.data_ptr(), _rows_of(out, "out"),
+            of[_AT], stride, n, vocab, of[_TYPE], ctypes.byref(rules), d[_AT], d_stride, out.data_ptr() if to is None else to[_AT], out_stride,
             None if d_bias is None else d_bias.data_ptr(), vocab if bias == "row" else 0, None if d_value is None else d_value.data_ptr(),
-            None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-            _stream_ptr(stream)), "apollo_adjust_logits_grad")
+            workspace_at, workspace_bytes, _stream_ptr(stream)), "apollo_adjust_logits_grad")
     return AdjustLogitsGrad(out, d_bias, d_value)
 
 

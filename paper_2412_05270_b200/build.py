@@ -26,10 +26,36 @@ def _stale(lib: Path = LIB) -> bool:
     return any(p.stat().st_mtime > built for p in deps)
 
 
+MARSHAL = PKG / "_marshal.so"               # csrc/marshal.cpp: what the binding asks of tensors
+
+
+def build_marshal(force: bool = False) -> Path:
+    """Compiles the Python extension that reads tensors for the binding (against torch's headers; torch is loaded first)."""
+    src = CSRC / "marshal.cpp"
+    if not force and MARSHAL.exists() and MARSHAL.stat().st_mtime >= max(src.stat().st_mtime, Path(__file__).stat().st_mtime):
+        return MARSHAL
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    tmp = MARSHAL.with_suffix(f".{os.getpid()}.tmp")
+    include = [f"-I{p}" for p in cpp_extension.include_paths()] + [f"-I{sysconfig.get_paths()['include']}"]
+    libs = [f"-L{p}" for p in cpp_extension.library_paths()] + ["-lc10", "-ltorch_cpu", "-ltorch_python"]
+    out = subprocess.run([os.environ.get("CXX", "g++"), "-shared", "-fPIC", "-O2", "-std=c++17", "-fvisibility=hidden", "-w",
+                          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *include, str(src), "-o", str(tmp), *libs],
+                         stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if out.returncode != 0:
+        print(out.stdout)
+        raise RuntimeError("g++ failed on marshal.cpp")
+    os.replace(tmp, MARSHAL)
+    return MARSHAL
+
+
 def build_library(force: bool = False, verbose: bool = False, debug: bool = False) -> Path:
     """Compiles the library in-tree.  debug=True builds libapollo_debug.so: every kernel checks the index
     range of its global loads and stores and reports a violation through the context's status word
     (apollo_status returns APOLLO_ERR_INTERNAL) instead of making the access."""
+    build_marshal()
     lib = LIB_DEBUG if debug else LIB
     if not force and not _stale(lib):
         return lib

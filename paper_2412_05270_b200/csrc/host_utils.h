@@ -30,6 +30,20 @@ inline int device_sms(int* sms)
     return APOLLO_OK;
 }
 
+// Lets a kernel have `bytes` of dynamic shared memory (asked for once per kernel and device: the call costs as much as a small launch).
+template <typename K>
+cudaError_t allow_shared(K* kernel, int bytes, std::atomic<unsigned long long>& done)
+{
+    int device = 0;
+    const cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = device >= 0 && device < 64 ? 1ull << device : 0;
+    if (bit && (done.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+    const cudaError_t set = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (set == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return set;
+}
+
 // Launch whose blocks may start while the launch before it in the stream is still ending (they wait for it themselves:
 // ptx::grid_wait_previous).
 template <typename... P, typename... A>

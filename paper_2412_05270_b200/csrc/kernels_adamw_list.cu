@@ -34,7 +34,8 @@ constexpr int AL_THREADS = 256;
 constexpr int AL_WARPS = AL_THREADS / 32;
 constexpr int AL_TILE32 = 4096;          // elements of one tile, 32 bits
 constexpr int AL_WAVES = 16;             // 8 bits: how many times the blocks that are resident at once, at most
-constexpr int AL_FEW = 48, AL_MANY = 960;   // tensors whose pointers travel as parameters of one launch (CUDA: 32,764 bytes)
+// Tensors whose pointers travel as parameters of one launch: as many as fit CUDA's 32,764 bytes, or few, which launch faster.
+constexpr int AL_FEW = 96, AL_MANY = 960;
 
 __device__ __forceinline__ void store8(float* p, const float (&v)[8])
 {
@@ -727,7 +728,8 @@ cudaError_t list_launch(ListArgs<CAP>& a, bool q8, int sms, cudaStream_t stream)
         adamw32_kernel<PT, GT, CAP><<<(unsigned)tiles, AL_THREADS, 0, stream>>>(a);
         return cudaGetLastError();
     }
-    const cudaError_t e = cudaFuncSetAttribute(adamw8_kernel<PT, GT, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+    static std::atomic<unsigned long long> allowed{ 0 };
+    const cudaError_t e = allow_shared(adamw8_kernel<PT, GT, CAP>, S::SMEM, allowed);
     if (e != cudaSuccess) return e;
     const int64_t most = (int64_t)S::RESIDENT * sms * AL_WAVES;
     a.whole_grid = (int)(tiles < most ? tiles : most);

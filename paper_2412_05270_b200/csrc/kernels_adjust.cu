@@ -554,8 +554,8 @@ adjust_bias_join_kernel(const float* __restrict__ partial, int groups, int vocab
 }
 
 constexpr int AJ_MAX_GROUPS = 256;       // rows of partial sums for a shared bias
-constexpr int AJ_WORDS_CHUNK = 16384;
-constexpr int AJ_DEPTH = 16;
+constexpr int AJ_WORDS_CHUNK = 8192;
+constexpr int AJ_DEPTH = 32;
 constexpr int AJ_MOST_SMEM = (Table::words(AJ_WORDS_CHUNK, AJ_WORDS_CHUNK) + 2 * APOLLO_MAX_BIAS_WORDS) * 4;
 
 bool whole_vectors(const void* p, int64_t stride, size_t e) { return (uintptr_t)p % 16 == 0 && (size_t)stride * e % 16 == 0; }
@@ -663,7 +663,8 @@ cudaError_t run_words(WordsArgs a, int sms, cudaStream_t stream)
     const int64_t blocks = (a.n_rows + rows - 1) / rows * a.chunks;
     if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
     const int smem = (Table::words(a.chunk, a.entries) + 2 * named) * 4;
-    cudaError_t e = cudaFuncSetAttribute(adjust_words_kernel<T, GRAD>, cudaFuncAttributeMaxDynamicSharedMemorySize, AJ_MOST_SMEM);
+    static std::atomic<unsigned long long> allowed{ 0 };
+    const cudaError_t e = allow_shared(adjust_words_kernel<T, GRAD>, AJ_MOST_SMEM, allowed);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
