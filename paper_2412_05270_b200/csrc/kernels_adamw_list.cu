@@ -185,7 +185,7 @@ struct ListArgs {
     const float* factor;
     const float* lr_at;
     const long long* t_at;
-    float b1, a1, b2, root_a2;           // a = 1 - b
+    float b1, a1, b2, a2;                // a = 1 - b
     double lr, wd, eps, inv_c1, root;    // root = sqrt(inv_c2)
     double log_b1, log_b2;               // for the step count on the device
     int bias_correction;
@@ -273,12 +273,14 @@ __device__ __forceinline__ float inverse_of(float x)
     return y;
 }
 
-// m, v and p of eight elements, one step on: m comes in as b1 m = scale * m[]; v takes the square of sqrt(a2) factor g.
+// m, v and p of eight elements, one step on: m comes in as b1 m = scale * m[].  Every product and sum of m and v is rounded by itself, as a
+// program of elementwise operations in fp32 rounds them: the same bits, so the same codes (fused: 1.5 instructions an element less, and one
+// code in a million another one).
 struct Update {
-    uint64_t a1, b2, a2, eps, rate, decay;
+    uint64_t factor, a1, b2, a2, eps, rate, decay;
     template <int CAP>
     __device__ __forceinline__ Update(const ListArgs<CAP>& a, const Scalars& s)
-        : a1(pair2(a.a1 * s.factor, a.a1 * s.factor)), b2(pair2(a.b2, a.b2)), a2(pair2(a.root_a2 * s.factor, a.root_a2 * s.factor)),
+        : factor(pair2(s.factor, s.factor)), a1(pair2(a.a1, a.a1)), b2(pair2(a.b2, a.b2)), a2(pair2(a.a2, a.a2)),
           eps(pair2(s.eps, s.eps)), rate(pair2(-s.rate, -s.rate)), decay(pair2(s.decay, s.decay)) {}
     template <bool FAST>
     __device__ __forceinline__ void apply(const float (&g)[8], float scale, float (&m)[8], float (&v)[8], float (&p)[8]) const
@@ -286,9 +288,9 @@ struct Update {
         const uint64_t b1 = pair2(scale, scale);
 #pragma unroll
         for (int x = 0; x < 8; x += 2) {
-            const uint64_t gg = pair2(g[x], g[x + 1]), hh = mul2(a2, gg);
-            const uint64_t mm = fma2(a1, gg, mul2(b1, pair2(m[x], m[x + 1])));
-            const uint64_t vv = fma2(hh, hh, mul2(b2, pair2(v[x], v[x + 1])));
+            const uint64_t gg = mul2(pair2(g[x], g[x + 1]), factor);
+            const uint64_t mm = add2(mul2(pair2(m[x], m[x + 1]), b1), mul2(gg, a1));
+            const uint64_t vv = add2(mul2(pair2(v[x], v[x + 1]), b2), mul2(mul2(gg, gg), a2));
             unpack2(mm, m[x], m[x + 1]);
             unpack2(vv, v[x], v[x + 1]);
             float d0, d1;
@@ -484,7 +486,7 @@ struct Stage {
 //   * codes are cut out of four words at a time, clamped only where an element of a lane is below the lowest code;
 //   * whole tiles and the tensors' ends are different blocks of threads: with both in one loop it took 5 instructions an element more;
 //   * up to AL_WAVES times as many blocks as are resident: with one wave the slowest multiprocessor sets the time (529 us for 504).
-// 262 M parameters: bfloat16 454 us, 5.8 TB/s; fp32 weights with bfloat16 gradients 550, all fp32 628 (at the copy rate 401, 561, 641).
+// 262 M parameters: bfloat16 461 us, 5.7 TB/s; fp32 weights with bfloat16 gradients 550, all fp32 635 (at the copy rate 401, 561, 641).
 template <typename PT, typename GT, int CAP>
 __global__ void __launch_bounds__(AL_THREADS, (Stage<PT, GT>::RESIDENT))
 adamw8_kernel(const __grid_constant__ ListArgs<CAP> a)
@@ -783,7 +785,7 @@ int list_step(const ListCall& c, const apollo_adamw_list_config* cfg, void* d_st
     a.m = static_cast<char*>(d_state); a.v = a.m + codes; a.k = reinterpret_cast<uint16_t*>(a.v + codes);
     a.factor = d_factor; a.lr_at = d_lr; a.t_at = reinterpret_cast<const long long*>(d_t);
     a.lr = lr; a.wd = wd; a.eps = cfg->eps;
-    a.b1 = (float)cfg->beta1; a.a1 = (float)(1.0 - cfg->beta1); a.b2 = (float)cfg->beta2; a.root_a2 = (float)std::sqrt(1.0 - cfg->beta2);
+    a.b1 = (float)cfg->beta1; a.a1 = (float)(1.0 - cfg->beta1); a.b2 = (float)cfg->beta2; a.a2 = (float)(1.0 - cfg->beta2);
     a.bias_correction = cfg->bias_correction;
     a.fast = cfg->eps >= 1e-12;
     a.log_b1 = std::log(cfg->beta1); a.log_b2 = std::log(cfg->beta2);      // (-inf for 0: expm1 is -1, c = 1)
