@@ -50,6 +50,8 @@ __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
 // ---------------------------------------------------------------- norm
+// One read of every gradient: 262 M bfloat16 in 82 us, 6.4 TB/s; fp32 in 150 us, 7.0 TB/s.  A thread sums 32 squares in fp32 and adds them up in
+// fp64; where the sum is near either end of fp32's range it squares the same 32 in fp64.
 constexpr int GN_TILE = 8192;            // elements of one tile
 constexpr int GN_THREADS = 256;
 constexpr int GN_MAX_GRID = 2048;        // partial sums of one launch at most
@@ -274,8 +276,8 @@ __device__ __forceinline__ float inverse_of(float x)
 }
 
 // m, v and p of eight elements, one step on: m comes in as b1 m = scale * m[].  Every product and sum of m and v is rounded by itself, as a
-// program of elementwise operations in fp32 rounds them: the same bits, so the same codes (fused: 1.5 instructions an element less, and one
-// code in a million another one).
+// program of elementwise operations in fp32 rounds them: the same bits, so the same codes (fused: 2 instructions an element less, and one
+// code in two million another one).  The sums are not in pairs: the compiler fuses a product and a sum of pairs although both say .rn.
 struct Update {
     uint64_t factor, a1, b2, a2, eps, rate, decay;
     template <int CAP>
@@ -289,10 +291,16 @@ struct Update {
 #pragma unroll
         for (int x = 0; x < 8; x += 2) {
             const uint64_t gg = mul2(pair2(g[x], g[x + 1]), factor);
-            const uint64_t mm = add2(mul2(pair2(m[x], m[x + 1]), b1), mul2(gg, a1));
-            const uint64_t vv = add2(mul2(pair2(v[x], v[x + 1]), b2), mul2(mul2(gg, gg), a2));
-            unpack2(mm, m[x], m[x + 1]);
-            unpack2(vv, v[x], v[x + 1]);
+            float s0, s1, t0, t1;
+            unpack2(mul2(pair2(m[x], m[x + 1]), b1), s0, s1);
+            unpack2(mul2(gg, a1), t0, t1);
+            m[x] = __fadd_rn(s0, t0);
+            m[x + 1] = __fadd_rn(s1, t1);
+            unpack2(mul2(pair2(v[x], v[x + 1]), b2), s0, s1);
+            unpack2(mul2(mul2(gg, gg), a2), t0, t1);
+            v[x] = __fadd_rn(s0, t0);
+            v[x + 1] = __fadd_rn(s1, t1);
+            const uint64_t mm = pair2(m[x], m[x + 1]);
             float d0, d1;
             unpack2(add2(pair2(root_of<FAST>(v[x]), root_of<FAST>(v[x + 1])), eps), d0, d1);
             const uint64_t pp = pair2(p[x], p[x + 1]);
@@ -479,14 +487,15 @@ struct Stage {
     static constexpr int FIT = 227 * 1024 / (SMEM + 2 * 1024), RESIDENT = FIT < 3 ? FIT : 3;
 };
 
-// 8 bits.  Bound by instruction issue with bfloat16 weights and gradients (49 an element, of which Philox 5, decoding 9, encoding 13; the
+// 8 bits.  Bound by instruction issue with bfloat16 weights and gradients (50 an element, of which Philox 5, decoding 9, encoding 13; the
 // issue limit at the copy rate is 55), by memory otherwise.  What that shaped:
 //   * m's codes are looked up in shared memory (an add that must not happen for code 0 costs three instructions more);
 //   * pairs of floats (fma.rn.f32x2) for the update;
 //   * codes are cut out of four words at a time, clamped only where an element of a lane is below the lowest code;
 //   * whole tiles and the tensors' ends are different blocks of threads: with both in one loop it took 5 instructions an element more;
-//   * up to AL_WAVES times as many blocks as are resident: with one wave the slowest multiprocessor sets the time (529 us for 504).
-// 262 M parameters: bfloat16 461 us, 5.7 TB/s; fp32 weights with bfloat16 gradients 550, all fp32 635 (at the copy rate 401, 561, 641).
+//   * up to AL_WAVES times as many blocks as are resident: with one wave the slowest multiprocessor sets the time (529 us for 504);
+//   * loads through registers instead: 613 us (too few bytes under way beside what the arithmetic holds).
+// 262 M parameters: bfloat16 472 us, 5.6 TB/s; fp32 weights with bfloat16 gradients 551, all fp32 638 (at the copy rate 401, 561, 641).
 template <typename PT, typename GT, int CAP>
 __global__ void __launch_bounds__(AL_THREADS, (Stage<PT, GT>::RESIDENT))
 adamw8_kernel(const __grid_constant__ ListArgs<CAP> a)
@@ -642,7 +651,7 @@ adamw32_kernel(const __grid_constant__ ListArgs<CAP> a)
     }
 }
 
-// Values of 8-bit moments, sixteen elements a thread.
+// Values of 8-bit moments, sixteen elements a thread, a block for each 4096 (262 M: 242 us, 6.5 TB/s; blocks that loop: 327 us).
 __global__ void __launch_bounds__(AL_THREADS)
 adamw_moments_kernel(const uint4* __restrict__ cm, const uint4* __restrict__ cv, const uint16_t* __restrict__ ks, long long n,
                      uint4* __restrict__ m, uint4* __restrict__ v)
