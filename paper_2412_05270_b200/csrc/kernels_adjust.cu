@@ -10,13 +10,14 @@
 // order decides the order of the list, not the results), then writes the listed words, one a thread.  In place without a bias the second one
 // does everything: the listed words and the masked ones are all that changes.  Rows that share a history (the positions of a sequence in
 // training) go on with the table of the row before: they add the tokens in between.  A table word holds
-// [31] seen at all  [30..20] 1 + slot of the word's named value  [19..0] how often from `start` on.
+// [31] seen at all  [30..20] 1 + slot of the word's named value  [19..0] how often from `start` on;  of short histories half of that.
 // What was tried: vectors that look into the table (in a training batch nearly every warp had a word to look up: 376 instructions a
 // vector of eight; 8192 x 32000 bfloat16 785 us), both passes in one kernel with barriers between them (351 us), the same with the next row's
 // loads under way (266 us, at three times the code), the words of some rows beside the stream of the next ones in one launch (six slabs of rows:
 // 375 us, the blocks of words are the long ones).
 // 8192 x 32000 bfloat16 with a bias and a mask: stream 157 us, 6.7 TB/s (its sums over rows for a bias' gradient: 201 us); words of histories of
-// 512 tokens on average, 2 M of them: 113 us, where warps wait for barriers (8 cycles an instruction) and memory is at 12 %.
+// 512 tokens on average, 2 M of them: 98 us (113 with 32-bit entries), where warps wait for barriers (8 cycles an instruction) and memory
+// is at 12 %.
 #include "../../include/apollo.h"
 
 #include <cmath>
@@ -33,6 +34,7 @@ constexpr int AJ_THREADS = 256;
 constexpr int AJ_UNITS = 4;              // vectors a thread has of a row's chunk at once
 constexpr int AJ_BATCH = 4;              // loads a thread has in flight where they are scattered
 constexpr int AJ_ROWS = 16;              // most rows in turn
+constexpr int AJ_SHORT = 4096;           // tokens of a history that is counted in 16 bits (at most 2^15 - 1)
 constexpr uint32_t AJ_SEEN = 0x80000000u;
 constexpr int AJ_SLOT_SHIFT = 20;
 constexpr uint32_t AJ_COUNT = (1u << AJ_SLOT_SHIFT) - 1, AJ_SLOT = 0x7FFu;
@@ -83,8 +85,11 @@ __device__ __forceinline__ Plan plan_of(const Rules& r, long long row)
     return p;
 }
 
-// The table of a chunk: `chunk` words, and the list of those that are not zero.
+// The table of a chunk: `chunk` entries, and the list of those that are not zero.  HALF: entries of 16 bits, two in a word ([15] seen at all
+// [14..0] how often): histories of up to AJ_SHORT tokens, no named values.  Half the shared memory, so twice the blocks, of half the threads.
+template <bool HALF>
 struct Table {
+    static constexpr int THREADS = HALF ? AJ_THREADS / 2 : AJ_THREADS;
     uint32_t* word;
     uint16_t* list;                      // chunk <= 65536
     int* count;
@@ -94,12 +99,42 @@ struct Table {
     int token_more, token_less;
 
     __device__ __forceinline__ Table(uint32_t* at, int* n, int chunk, int first, int w)
-        : word(at), list(reinterpret_cast<uint16_t*>(at + chunk)), count(n), j0(first), width(w) {}
-    static __host__ __device__ constexpr int words(int chunk, int entries) { return chunk + (entries + 1) / 2; }
+        : word(at), list(reinterpret_cast<uint16_t*>(at + (HALF ? chunk / 2 : chunk))), count(n), j0(first), width(w) {}
+    static __host__ __device__ constexpr int words(int chunk, int entries) { return (HALF ? chunk / 2 : chunk) + (entries + 1) / 2; }
     __device__ __forceinline__ void clear(int chunk)
     {
-        for (int i = threadIdx.x * 4; i < chunk; i += AJ_THREADS * 4) *reinterpret_cast<uint4*>(word + i) = make_uint4(0, 0, 0, 0);
+        for (int i = threadIdx.x * 4; i < (HALF ? chunk / 2 : chunk); i += THREADS * 4) *reinterpret_cast<uint4*>(word + i) = make_uint4(0, 0, 0, 0);
         if (threadIdx.x == 0) *count = 0;
+    }
+    // An entry as [31] seen [30..20] slot [19..0] how often.
+    __device__ __forceinline__ uint32_t entry(int j) const
+    {
+        if constexpr (!HALF) return word[j];
+        const uint32_t e = word[j >> 1] >> (16 * (j & 1));
+        return (e & 0x8000u) << 16 | (e & 0x7FFFu);
+    }
+    // Whether the word has been seen before; from now on it has, and with `counted` once more.
+    __device__ __forceinline__ bool see(int j, bool counted)
+    {
+        if constexpr (!HALF) {
+            const bool before = atomicOr(word + j, AJ_SEEN) & AJ_SEEN;
+            if (counted) atomicAdd(word + j, 1u);
+            return before;
+        }
+        const int shift = 16 * (j & 1);
+        const bool before = atomicOr(word + (j >> 1), 0x8000u << shift) >> shift & 0x8000u;
+        if (counted) atomicAdd(word + (j >> 1), 1u << shift);
+        return before;
+    }
+    __device__ __forceinline__ void count_more(int j)
+    {
+        if constexpr (HALF) atomicAdd(word + (j >> 1), 1u << (16 * (j & 1)));
+        else atomicAdd(word + j, 1u);
+    }
+    __device__ __forceinline__ void count_less(int j)
+    {
+        if constexpr (HALF) atomicSub(word + (j >> 1), 1u << (16 * (j & 1)));
+        else atomicSub(word + j, 1u);
     }
     __device__ __forceinline__ void append(int j) { list[atomicAdd(count, 1)] = (uint16_t)j; }
     // f(word, position) for the tokens of the chunk at positions [from, to).
@@ -107,22 +142,22 @@ struct Table {
     __device__ __forceinline__ void scan(const Rules& r, int vocab, int from, int to, F f)
     {
         const long long first = (long long)now.history * r.history_stride;
-        for (int i = from + (int)threadIdx.x; i < to; i += AJ_THREADS * AJ_BATCH) {
+        for (int i = from + (int)threadIdx.x; i < to; i += THREADS * AJ_BATCH) {
             int j[AJ_BATCH];
 #pragma unroll
             for (int k = 0; k < AJ_BATCH; ++k) {
-                const int at = i + k * AJ_THREADS;
+                const int at = i + k * THREADS;
                 j[k] = at < to ? token_at(r.history, first + at, r.history64, vocab) - j0 : -1;
             }
 #pragma unroll
-            for (int k = 0; k < AJ_BATCH; ++k) if (j[k] >= 0 && j[k] < width) f(j[k], i + k * AJ_THREADS);
+            for (int k = 0; k < AJ_BATCH; ++k) if (j[k] >= 0 && j[k] < width) f(j[k], i + k * THREADS);
         }
     }
     // Whether the next row's table is this one with a few tokens more, at most one a thread; then they are read now.
     __device__ __forceinline__ void look_ahead(const Rules& r, const Plan& p, int vocab)
     {
-        quick = p.history == now.history && p.length >= now.length && p.length - now.length <= AJ_THREADS && p.start >= now.start &&
-                p.start - now.start <= AJ_THREADS && p.start <= now.length;
+        quick = p.history == now.history && p.length >= now.length && p.length - now.length <= THREADS && p.start >= now.start &&
+                p.start - now.start <= THREADS && p.start <= now.length;
         if (!quick) return;
         const long long first = (long long)p.history * r.history_stride;
         const int more = now.length + threadIdx.x, less = now.start + threadIdx.x;
@@ -133,11 +168,10 @@ struct Table {
     __device__ __forceinline__ void set(const Rules& r, const Plan& p, int vocab, int chunk)
     {
         auto add = [&](int j, int i) {
-            if (!(atomicOr(word + j, AJ_SEEN) & AJ_SEEN)) append(j);
-            if (i >= p.start) atomicAdd(word + j, 1u);
+            if (!see(j, i >= p.start)) append(j);
         };
         if (quick) {
-            if (token_less >= 0 && token_less < width) atomicSub(word + token_less, 1u);
+            if (token_less >= 0 && token_less < width) count_less(token_less);
             if (token_more >= 0 && token_more < width) add(token_more, now.length + (int)threadIdx.x);
         } else {
             if (p.history != now.history || p.length < now.length) {
@@ -147,8 +181,8 @@ struct Table {
                 now.length = now.start = 0;
             }
             // positions whose count begins or ends, among those the table has
-            scan(r, vocab, now.start, min(p.start, now.length), [&](int j, int) { atomicSub(word + j, 1u); });
-            scan(r, vocab, p.start, min(now.start, now.length), [&](int j, int) { atomicAdd(word + j, 1u); });
+            scan(r, vocab, now.start, min(p.start, now.length), [&](int j, int) { count_less(j); });
+            scan(r, vocab, p.start, min(now.start, now.length), [&](int j, int) { count_more(j); });
             scan(r, vocab, now.length, p.length, add);
         }
         now = p;
@@ -266,7 +300,7 @@ __device__ __forceinline__ void read_words(const Rules& r, long long row, int vo
 {
     for (int i = threadIdx.x; i < r.n_bias; i += AJ_THREADS) words[i] = token_at(r.word, row * r.n_bias + i, r.words64, vocab);
 }
-__device__ __forceinline__ void sum_words(const Rules& r, long long row, Table& table, const int* words, float* sums)
+__device__ __forceinline__ void sum_words(const Rules& r, long long row, Table<false>& table, const int* words, float* sums)
 {
     for (int i = threadIdx.x; i < r.n_bias; i += AJ_THREADS) {
         const int w = words[i], j = w - table.j0;
@@ -443,12 +477,12 @@ struct WordsArgs {
     Rules r;
 };
 
-template <typename T, bool GRAD>
-__global__ void __launch_bounds__(AJ_THREADS)
+template <typename T, bool GRAD, bool HALF>
+__global__ void __launch_bounds__(Table<HALF>::THREADS)
 adjust_words_kernel(const __grid_constant__ WordsArgs a)
 {
     using S = Sixteen<T>;
-    constexpr int N = S::N;
+    constexpr int N = S::N, THREADS = Table<HALF>::THREADS;
     extern __shared__ __align__(16) uint32_t shared[];
     __shared__ typename S::Entry masks[16];
     __shared__ Plan plans[AJ_ROWS];
@@ -459,8 +493,8 @@ adjust_words_kernel(const __grid_constant__ WordsArgs a)
     const int j0 = part * a.chunk, width = min(a.chunk, a.vocab - j0);
     if (threadIdx.x < 16) masks[threadIdx.x] = S::entry((int)threadIdx.x);
     if ((int)threadIdx.x < rows) plans[threadIdx.x] = plan_of(a.r, begin + threadIdx.x);
-    Table table(shared, &listed, a.chunk, j0, width);
-    float* const sums = reinterpret_cast<float*>(shared + Table::words(a.chunk, a.entries));
+    Table<HALF> table(shared, &listed, a.chunk, j0, width);
+    float* const sums = reinterpret_cast<float*>(shared + Table<HALF>::words(a.chunk, a.entries));
     int* const words = reinterpret_cast<int*>(sums + (GRAD ? 0 : a.r.n_bias));
     table.clear(a.chunk);
     __syncthreads();
@@ -478,33 +512,35 @@ adjust_words_kernel(const __grid_constant__ WordsArgs a)
         if constexpr (GRAD) {
             // (in place: before anything of the row is overwritten)
             if (a.dvalue)
-                for (int k = threadIdx.x; k < a.r.n_bias; k += AJ_THREADS) {
+                for (int k = threadIdx.x; k < a.r.n_bias; k += THREADS) {
                     const int w = token_at(a.r.word, row * a.r.n_bias + k, a.r.words64, a.vocab);
                     if (w < 0 ? j0 == 0 : w >= j0 && w < j0 + width) a.dvalue[row * a.r.n_bias + k] = w >= 0 && allowed(m0, w) ? (float)g0[w] : 0.0f;
                 }
         } else if (a.r.n_bias) {                       // (such rows are not taken in turn)
-            read_words(a.r, row, a.vocab, words);
-            __syncthreads();
-            sum_words(a.r, row, table, words, sums);
+            if constexpr (!HALF) {
+                read_words(a.r, row, a.vocab, words);
+                __syncthreads();
+                sum_words(a.r, row, table, words, sums);
+            }
         }
         __syncthreads();
         const int n = listed;
         if (i + 1 < rows && a.r.history) table.look_ahead(a.r, plans[i + 1], a.vocab);
         // what a listed word becomes
         auto result = [&](int k, float x, float g) {
-            const uint32_t t = table.word[k];
+            const uint32_t t = table.entry(k);
             if constexpr (GRAD) return x > 0.0f ? __fdiv_rn(g, plan.rho) : g * plan.rho;
             float y = penalised(x, t, plan);
             if (b0) y += (float)b0[j0 + k];
             const uint32_t slot = t >> AJ_SLOT_SHIFT & AJ_SLOT;
             return slot ? y + sums[slot - 1] : y;
         };
-        for (int first = threadIdx.x; first < n; first += AJ_THREADS * AJ_BATCH) {
+        for (int first = threadIdx.x; first < n; first += THREADS * AJ_BATCH) {
             int at[AJ_BATCH];
             T x[AJ_BATCH], g[AJ_BATCH];
 #pragma unroll
             for (int k = 0; k < AJ_BATCH; ++k) {
-                at[k] = first + k * AJ_THREADS < n ? table.list[first + k * AJ_THREADS] : -1;
+                at[k] = first + k * THREADS < n ? table.list[first + k * THREADS] : -1;
                 if (at[k] >= 0 && !allowed(m0, j0 + at[k])) at[k] = -1;
                 if (at[k] >= 0) {
                     x[k] = x0[j0 + at[k]];
@@ -524,7 +560,7 @@ adjust_words_kernel(const __grid_constant__ WordsArgs a)
         if (a.mode == AJ_WORDS_ONLY || (a.mode == AJ_MASKED_TOO && !m0)) continue;
         const Span<T> span(y0, j0, width);
         const Dense<T> dense{ b0, m0, masks, a.other, (a.vocab + 31) / 32 };
-        for (int u = threadIdx.x; u < span.full; u += AJ_THREADS) {
+        for (int u = threadIdx.x; u < span.full; u += THREADS) {
             const int j = span.first + u * N;
             uint4* const y = reinterpret_cast<uint4*>(y0 + j);
             if (a.mode == AJ_ALL_TOO) {
@@ -537,7 +573,7 @@ adjust_words_kernel(const __grid_constant__ WordsArgs a)
         if (const int j = span.single(); j >= 0 && (a.mode == AJ_ALL_TOO || !allowed(m0, j))) y0[j] = dense.column(y0[j], j);
         if (a.mode != AJ_ALL_TOO) continue;
         __syncthreads();
-        for (int k = threadIdx.x; k < n; k += AJ_THREADS) {
+        for (int k = threadIdx.x; k < n; k += THREADS) {
             const int j = table.list[k];
             if (allowed(m0, j0 + j)) y0[j0 + j] = (T)__uint_as_float(table.word[j]);
         }
@@ -558,8 +594,8 @@ adjust_bias_join_kernel(const float* __restrict__ partial, int groups, int vocab
 
 constexpr int AJ_MAX_GROUPS = 256;       // rows of partial sums for a shared bias
 constexpr int AJ_WORDS_CHUNK = 8192;
-constexpr int AJ_DEPTH = 32;
-constexpr int AJ_MOST_SMEM = (Table::words(AJ_WORDS_CHUNK, AJ_WORDS_CHUNK) + 2 * APOLLO_MAX_BIAS_WORDS) * 4;
+constexpr int AJ_DEPTH = 64;
+constexpr int AJ_MOST_SMEM = (Table<false>::words(AJ_WORDS_CHUNK, AJ_WORDS_CHUNK) + 2 * APOLLO_MAX_BIAS_WORDS) * 4;
 
 bool whole_vectors(const void* p, int64_t stride, size_t e) { return (uintptr_t)p % 16 == 0 && (size_t)stride * e % 16 == 0; }
 
@@ -665,13 +701,14 @@ cudaError_t run_words(WordsArgs a, int sms, cudaStream_t stream)
     a.rows = (int)rows;
     const int64_t blocks = (a.n_rows + rows - 1) / rows * a.chunks;
     if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
-    const int smem = (Table::words(a.chunk, a.entries) + 2 * named) * 4;
-    static std::atomic<unsigned long long> allowed{ 0 };
-    const cudaError_t e = allow_shared(adjust_words_kernel<T, GRAD>, AJ_MOST_SMEM, allowed);
+    const bool half = a.r.history_len <= AJ_SHORT && named == 0 && a.mode != AJ_ALL_TOO;
+    const int smem = half ? Table<true>::words(a.chunk, a.entries) * 4 : (Table<false>::words(a.chunk, a.entries) + 2 * named) * 4;
+    static std::atomic<unsigned long long> allowed[2];
+    const cudaError_t e = half ? allow_shared(adjust_words_kernel<T, GRAD, true>, AJ_MOST_SMEM, allowed[1]) : allow_shared(adjust_words_kernel<T, GRAD, false>, AJ_MOST_SMEM, allowed[0]);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
-    cfg.blockDim = dim3(AJ_THREADS);
+    cfg.blockDim = dim3(half ? Table<true>::THREADS : Table<false>::THREADS);
     cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -679,7 +716,7 @@ cudaError_t run_words(WordsArgs a, int sms, cudaStream_t stream)
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = a.mode == AJ_WORDS_ONLY ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, adjust_words_kernel<T, GRAD>, a);
+    return half ? cudaLaunchKernelEx(&cfg, adjust_words_kernel<T, GRAD, true>, a) : cudaLaunchKernelEx(&cfg, adjust_words_kernel<T, GRAD, false>, a);
 }
 
 template <typename T>
