@@ -487,8 +487,10 @@ adjust_words_kernel(const __grid_constant__ WordsArgs a)
     __shared__ typename S::Entry masks[16];
     __shared__ Plan plans[AJ_ROWS];
     __shared__ int listed;
-    const int part = blockIdx.x % a.chunks;
-    const long long begin = (long long)(blockIdx.x / a.chunks) * a.rows;
+    // (the first chunk's blocks first: where common words have low numbers they are the long ones)
+    const unsigned groups = gridDim.x / (unsigned)a.chunks;
+    const int part = (int)(blockIdx.x / groups);
+    const long long begin = (long long)(blockIdx.x % groups) * a.rows;
     const int rows = (int)min((long long)a.rows, a.n_rows - begin);
     const int j0 = part * a.chunk, width = min(a.chunk, a.vocab - j0);
     if (threadIdx.x < 16) masks[threadIdx.x] = S::entry((int)threadIdx.x);
