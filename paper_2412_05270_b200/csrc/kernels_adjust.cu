@@ -684,11 +684,12 @@ cudaError_t run_stream(StreamArgs a, int sms, int* groups, cudaStream_t stream)
     return cudaGetLastError();
 }
 
-// Launches the kernel of the listed words, after the stream where that has run.  Chunks as large as shared memory holds for several blocks
+// Launches the kernel of the listed words, after the stream where that has run (only then may its blocks start early: what else comes before
+// it in the caller's stream may write what it reads).  Chunks as large as shared memory holds for several blocks
 // (a row of the history is read once per chunk), smaller ones while there are fewer blocks than the chip holds; rows that share a history in
 // turn, as long as AJ_DEPTH blocks per multiprocessor remain.
 template <typename T, bool GRAD>
-cudaError_t run_words(WordsArgs a, int sms, cudaStream_t stream)
+cudaError_t run_words(WordsArgs a, bool streamed, int sms, cudaStream_t stream)
 {
     const int named = GRAD ? 0 : a.r.n_bias;
     a.chunk = AJ_WORDS_CHUNK;
@@ -717,7 +718,7 @@ cudaError_t run_words(WordsArgs a, int sms, cudaStream_t stream)
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = a.mode == AJ_WORDS_ONLY ? 1 : 0;
+    cfg.numAttrs = streamed ? 1 : 0;
     return half ? cudaLaunchKernelEx(&cfg, adjust_words_kernel<T, GRAD, true>, a) : cudaLaunchKernelEx(&cfg, adjust_words_kernel<T, GRAD, false>, a);
 }
 
@@ -727,7 +728,8 @@ cudaError_t run_adjust(WordsArgs a, int sms, cudaStream_t stream)
     const bool place = a.logits == a.out, table = a.r.history || a.r.n_bias;
     a.other = Sixteen<T>::MINUS_INF;
     a.mode = !place || !table ? AJ_WORDS_ONLY : a.r.bias ? AJ_ALL_TOO : AJ_MASKED_TOO;
-    if (a.mode == AJ_WORDS_ONLY && (!place || a.r.bias || a.r.mask)) {
+    const bool streamed = a.mode == AJ_WORDS_ONLY && (!place || a.r.bias || a.r.mask);
+    if (streamed) {
         StreamArgs s = {};
         s.in = a.logits; s.out = a.out; s.bias = a.r.bias; s.mask = a.r.mask;
         s.in_stride = a.stride; s.out_stride = a.out_stride; s.bias_stride = a.r.bias_stride; s.mask_stride = a.r.mask_stride;
@@ -736,7 +738,7 @@ cudaError_t run_adjust(WordsArgs a, int sms, cudaStream_t stream)
         const cudaError_t e = run_stream<T>(s, sms, &groups, stream);
         if (e != cudaSuccess) return e;
     }
-    return table ? run_words<T, false>(a, sms, stream) : cudaSuccess;
+    return table ? run_words<T, false>(a, streamed, sms, stream) : cudaSuccess;
 }
 
 template <typename T>
@@ -744,11 +746,12 @@ cudaError_t run_adjust_grad(WordsArgs a, StreamArgs s, int sms, int* groups, cud
 {
     const bool place = a.dout == a.out, table = a.r.history || a.dvalue;
     a.mode = !place || s.copy || s.partial || !a.r.history ? AJ_WORDS_ONLY : AJ_MASKED_TOO;
-    if (a.mode == AJ_WORDS_ONLY && (!place || s.copy || s.partial || s.mask)) {
+    const bool streamed = a.mode == AJ_WORDS_ONLY && (!place || s.copy || s.partial || s.mask);
+    if (streamed) {
         const cudaError_t e = run_stream<T>(s, sms, groups, stream);
         if (e != cudaSuccess) return e;
     }
-    return table ? run_words<T, true>(a, sms, stream) : cudaSuccess;
+    return table ? run_words<T, true>(a, streamed, sms, stream) : cudaSuccess;
 }
 
 }  // namespace

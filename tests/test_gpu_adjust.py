@@ -319,3 +319,18 @@ def test_calls_that_are_refused():
         B.adjust_logits_grad(z, z.clone(), bias="shared", workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     assert e.value.code == B.ERR_WORKSPACE
     assert not z.any()
+
+
+def test_values_of_a_gradient_that_the_call_before_has_left():
+    """In place, words alone: nothing of the call may start before the masks of the call before it are written."""
+    g = torch.Generator(device="cuda").manual_seed(11)
+    start = torch.randn(4096, 32000, generator=g, device="cuda").bfloat16()
+    mask = torch.randint(-2 ** 31, 2 ** 31, (4096, 1000), generator=g, device="cuda").to(torch.int32)
+    index = torch.randint(0, 32000, (4096, 8), generator=g, device="cuda")
+    allowed = mask.gather(1, index // 32) >> (index % 32) & 1
+    want = torch.where(allowed == 1, start.gather(1, index).float(), -math.inf)
+    for _ in range(3):
+        d = start.clone()
+        B.adjust_logits(d, mask=mask, out=d)
+        r = B.adjust_logits_grad(d, d, bias_index=index, out=d)
+        assert torch.equal(r.value, want)
