@@ -529,6 +529,7 @@ APOLLO_API int apollo_adamw_list_moments(const void* d_state, size_t state_bytes
  *   dbias_j = a_j (summed over the rows in fp32, in a fixed order, for a shared bias),   dvalue_i = a_j of its word j.
  * logits, out, dout, dlogits: DEVICE, n_rows rows of `vocab` elements of `dtype`, rows >= vocab elements apart.  out may be the
  * logits, dlogits may be dout (same stride): then only the words that change are written, and read only where they must be.
+ * With a history dlogits must not be the logits.
  * Pointers need the alignment of their elements; rows that are whole 16-byte vectors are faster.
  */
 typedef struct {

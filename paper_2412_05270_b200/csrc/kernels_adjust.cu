@@ -816,6 +816,7 @@ extern "C" int apollo_adjust_logits_grad(const void* d_logits, int64_t row_strid
     }
     if ((a.r.history && !d_logits) || !d_grad_out || !d_grad_logits || (d_grad_logits == d_grad_out && grad_logits_stride != grad_out_stride))
         return APOLLO_ERR_INVALID_ARG;
+    if (a.r.history && d_grad_logits == d_logits && d_logits != d_grad_out) return APOLLO_ERR_INVALID_ARG;     // their signs are read beside the stream
     if (shared) {
         size_t need = 0;
         rc = apollo_adjust_logits_grad_workspace_bytes(n_rows, vocab, &need);

@@ -133,3 +133,7 @@ def test_tensors_that_the_binding_refuses():
     assert d(torch.zeros((), dtype=f32))[3:] == (0, 1, 1, 1, 1, 1) and d(torch.zeros(2, dtype=torch.bool))[2] == -1
     pointers, lengths, types, device, live = B._marshal().pack("grads", [None, None], None, -1)
     assert pointers == b"\0" * 16 and lengths == b"\0" * 16 and types == b"\0" * 8 and device == -1 and live == 0
+
+
+def test_a_gradient_over_the_logits_whose_signs_it_asks_for():
+    assert adjust(True, logits=8192, out=8192, **HISTORY) == B.ERR_INVALID_ARG
