@@ -185,3 +185,44 @@ def test_codes_are_those_of_an_elementwise_program():
         m = m * 0.9 + grad * (1 - 0.9)
         v = v * 0.999 + grad.square() * (1 - 0.999)
         assert torch.equal(opt.moments()[0], m) and torch.equal(opt.moments()[1], v)
+
+
+def test_a_captured_training_step_is_that_of_single_calls():
+    """Lookup, adjusted logits, log probabilities, their backward pass, clipping and the list step in one graph, replayed for several steps."""
+    g = torch.Generator(device="cuda").manual_seed(21)
+    table, bias = torch.randn(301, 1000, generator=g, device="cuda"), torch.randn(1000, generator=g, device="cuda")
+    index = torch.randint(0, 301, (6, 64), generator=g, device="cuda")
+    history = torch.randint(0, 1000, (6, 64, 30), generator=g, device="cuda", dtype=torch.int32)
+    target = torch.randint(0, 1000, (6, 64), generator=g, device="cuda")
+
+    def step(params, opt, index, history, target, lr, t):
+        for p in params:
+            p.grad = None
+        logits = A.adjust_logits(A.embedding(params[0], index), history, repetition=1.3, presence=0.2, bias=params[1])
+        logprob, entropy = A.token_logprobs(logits, target)
+        (-(logprob.sum() + 0.1 * entropy.sum())).backward()
+        grads = [p.grad for p in params]
+        opt.step(grads, lr=lr, t=t, wd=0.1, factor=B.grad_norm(grads, 1.0)[1:])
+
+    def made():
+        params = [x.clone().requires_grad_() for x in (table, bias)]
+        return params, B.AdamW(params, seed=5)
+    params, opt = made()
+    lr = torch.full((1,), 0.01, device="cuda")
+    for i in range(6):
+        step(params, opt, index[i], history[i], target[i], lr, torch.tensor([i], device="cuda"))
+    again, opt2 = made()
+    held = [x[0].clone() for x in (index, history, target)]
+    t = torch.zeros(1, dtype=torch.int64, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(again, opt2, *held, lr, t)
+    for i in range(6):
+        for x, new in zip(held, (index, history, target)):
+            x.copy_(new[i])
+        t.fill_(i)
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(params + [opt.state], again + [opt2.state]))
