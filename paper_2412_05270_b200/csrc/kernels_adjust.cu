@@ -16,7 +16,7 @@
 // loads under way (266 us, at three times the code), the words of some rows beside the stream of the next ones in one launch (six slabs of rows:
 // 375 us, the blocks of words are the long ones).
 // 8192 x 32000 bfloat16 with a bias and a mask: stream 157 us, 6.7 TB/s (its sums over rows for a bias' gradient: 201 us); words of histories of
-// 512 tokens on average, 2 M of them: 98 us (113 with 32-bit entries), where warps wait for barriers (8 cycles an instruction) and memory
+// 512 tokens on average, 2 M of them: 95 us (113 with 32-bit entries), where warps wait for barriers (8 cycles an instruction) and memory
 // is at 12 %.
 #include "../../include/apollo.h"
 
@@ -32,7 +32,6 @@ namespace {
 
 constexpr int AJ_THREADS = 256;
 constexpr int AJ_UNITS = 4;              // vectors a thread has of a row's chunk at once
-constexpr int AJ_BATCH = 4;              // loads a thread has in flight where they are scattered
 constexpr int AJ_ROWS = 16;              // most rows in turn
 constexpr int AJ_SHORT = 4096;           // tokens of a history that is counted in 16 bits (at most 2^15 - 1)
 constexpr uint32_t AJ_SEEN = 0x80000000u;
@@ -85,11 +84,16 @@ __device__ __forceinline__ Plan plan_of(const Rules& r, long long row)
     return p;
 }
 
+__host__ __device__ constexpr int four(int n) { return (n + 3) / 4 * 4; }
+
 // The table of a chunk: `chunk` entries, and the list of those that are not zero.  HALF: entries of 16 bits, two in a word ([15] seen at all
 // [14..0] how often): histories of up to AJ_SHORT tokens, no named values.  Half the shared memory, so twice the blocks, of half the threads.
 template <bool HALF>
 struct Table {
     static constexpr int THREADS = HALF ? AJ_THREADS / 2 : AJ_THREADS;
+    // Scattered loads that a thread has in flight.  Long histories: 8, 21.8 us for 129 rows of 8191 tokens (4: 26.3, 16: 29.3 and 36.8).  Short ones,
+    // most of them a few tokens more than the row before: 4 (8: 8192 x 32000 261 us instead of 254).
+    static constexpr int BATCH = HALF ? 4 : 8;
     uint32_t* word;
     uint16_t* list;                      // chunk <= 65536
     int* count;
@@ -142,15 +146,15 @@ struct Table {
     __device__ __forceinline__ void scan(const Rules& r, int vocab, int from, int to, F f)
     {
         const long long first = (long long)now.history * r.history_stride;
-        for (int i = from + (int)threadIdx.x; i < to; i += THREADS * AJ_BATCH) {
-            int j[AJ_BATCH];
+        for (int i = from + (int)threadIdx.x; i < to; i += THREADS * BATCH) {
+            int j[BATCH];
 #pragma unroll
-            for (int k = 0; k < AJ_BATCH; ++k) {
+            for (int k = 0; k < BATCH; ++k) {
                 const int at = i + k * THREADS;
                 j[k] = at < to ? token_at(r.history, first + at, r.history64, vocab) - j0 : -1;
             }
 #pragma unroll
-            for (int k = 0; k < AJ_BATCH; ++k) if (j[k] >= 0 && j[k] < width) f(j[k], i + k * THREADS);
+            for (int k = 0; k < BATCH; ++k) if (j[k] >= 0 && j[k] < width) f(j[k], i + k * THREADS);
         }
     }
     // Whether the next row's table is this one with a few tokens more, at most one a thread; then they are read now.
@@ -295,21 +299,35 @@ __device__ __forceinline__ float penalised(float x, uint32_t t, const Plan& p)
     return x;
 }
 
-// Words of a row's pairs to shared memory; a barrier later the first pair of a word sums the values of all its pairs, in order.
+// Words of a row's pairs to shared memory (-1 up to a multiple of four); a barrier later the first pair of a word sums the values of all its
+// pairs, in order.  Four words a look, no look depends on the one before it; only a word that is named again is looked for once more.
+template <int THREADS>
 __device__ __forceinline__ void read_words(const Rules& r, long long row, int vocab, int* words)
 {
-    for (int i = threadIdx.x; i < r.n_bias; i += AJ_THREADS) words[i] = token_at(r.word, row * r.n_bias + i, r.words64, vocab);
+    for (int i = threadIdx.x; i < four(r.n_bias); i += THREADS) words[i] = i < r.n_bias ? token_at(r.word, row * r.n_bias + i, r.words64, vocab) : -1;
 }
+template <int THREADS>
 __device__ __forceinline__ void sum_words(const Rules& r, long long row, Table<false>& table, const int* words, float* sums)
 {
-    for (int i = threadIdx.x; i < r.n_bias; i += AJ_THREADS) {
+    for (int i = threadIdx.x; i < r.n_bias; i += THREADS) {
         const int w = words[i], j = w - table.j0;
         if (w < 0 || j < 0 || j >= table.width) continue;
-        bool first = true;
-        for (int k = 0; k < i && first; ++k) first = words[k] != w;
-        if (!first) continue;
-        float sum = 0.0f;
-        for (int k = i; k < r.n_bias; ++k) if (words[k] == w) sum += r.value[row * r.n_bias + k];
+        const float* const values = r.value + row * r.n_bias;
+        float sum = values[i];
+        int earlier = 0, all = 0;
+#pragma unroll 4
+        for (int k = 0; k < r.n_bias; k += 4) {
+            const int4 q = *reinterpret_cast<const int4*>(words + k);
+            const int same[4] = { q.x == w, q.y == w, q.z == w, q.w == w };
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                all += same[x];
+                earlier += same[x] && k + x < i;
+            }
+        }
+        if (earlier) continue;
+        if (all > 1)
+            for (int k = i + 1; k < r.n_bias; ++k) if (words[k] == w) sum += values[k];
         sums[i] = sum;
         if (atomicOr(table.word + j, (uint32_t)(i + 1) << AJ_SLOT_SHIFT) == 0) table.append(j);
     }
@@ -477,8 +495,12 @@ struct WordsArgs {
     Rules r;
 };
 
+// Blocks a multiprocessor that the registers are to allow: it decides how the compiler orders the scattered loads.  8192 x 32000 bfloat16:
+// forward 9 252 us, 8 254, 10 260; gradient 6 304 us, 8 306, 9 330; in fp32 (777 x 50001) 9 88 us, 6 90.
+constexpr int words_resident(bool half, bool grad, size_t e) { return !half ? 4 : grad && e == 2 ? 6 : 9; }
+
 template <typename T, bool GRAD, bool HALF>
-__global__ void __launch_bounds__(Table<HALF>::THREADS)
+__global__ void __launch_bounds__(Table<HALF>::THREADS, words_resident(HALF, GRAD, sizeof(T)))
 adjust_words_kernel(const __grid_constant__ WordsArgs a)
 {
     using S = Sixteen<T>;
@@ -496,8 +518,8 @@ adjust_words_kernel(const __grid_constant__ WordsArgs a)
     if (threadIdx.x < 16) masks[threadIdx.x] = S::entry((int)threadIdx.x);
     if ((int)threadIdx.x < rows) plans[threadIdx.x] = plan_of(a.r, begin + threadIdx.x);
     Table<HALF> table(shared, &listed, a.chunk, j0, width);
-    float* const sums = reinterpret_cast<float*>(shared + Table<HALF>::words(a.chunk, a.entries));
-    int* const words = reinterpret_cast<int*>(sums + (GRAD ? 0 : a.r.n_bias));
+    int* const words = reinterpret_cast<int*>(shared + four(Table<HALF>::words(a.chunk, a.entries)));
+    float* const sums = reinterpret_cast<float*>(words + (GRAD ? 0 : four(a.r.n_bias)));
     table.clear(a.chunk);
     __syncthreads();
     table.now.history = plans[0].history;              // with nothing of it yet
@@ -510,6 +532,7 @@ adjust_words_kernel(const __grid_constant__ WordsArgs a)
         T* const y0 = static_cast<T*>(a.out) + row * a.out_stride;
         const T* const b0 = !GRAD && a.r.bias ? static_cast<const T*>(a.r.bias) + row * a.r.bias_stride : nullptr;
         const uint32_t* const m0 = a.r.mask ? a.r.mask + row * a.r.mask_stride : nullptr;
+        if constexpr (!GRAD && !HALF) if (a.r.n_bias) read_words<THREADS>(a.r, row, a.vocab, words);       // (such rows are not taken in turn)
         if (a.r.history) table.set(a.r, plan, a.vocab, a.chunk);
         if constexpr (GRAD) {
             // (in place: before anything of the row is overwritten)
@@ -518,11 +541,10 @@ adjust_words_kernel(const __grid_constant__ WordsArgs a)
                     const int w = token_at(a.r.word, row * a.r.n_bias + k, a.r.words64, a.vocab);
                     if (w < 0 ? j0 == 0 : w >= j0 && w < j0 + width) a.dvalue[row * a.r.n_bias + k] = w >= 0 && allowed(m0, w) ? (float)g0[w] : 0.0f;
                 }
-        } else if (a.r.n_bias) {                       // (such rows are not taken in turn)
-            if constexpr (!HALF) {
-                read_words(a.r, row, a.vocab, words);
+        } else if constexpr (!HALF) {
+            if (a.r.n_bias) {
                 __syncthreads();
-                sum_words(a.r, row, table, words, sums);
+                sum_words<THREADS>(a.r, row, table, words, sums);
             }
         }
         __syncthreads();
@@ -537,11 +559,11 @@ adjust_words_kernel(const __grid_constant__ WordsArgs a)
             const uint32_t slot = t >> AJ_SLOT_SHIFT & AJ_SLOT;
             return slot ? y + sums[slot - 1] : y;
         };
-        for (int first = threadIdx.x; first < n; first += THREADS * AJ_BATCH) {
-            int at[AJ_BATCH];
-            T x[AJ_BATCH], g[AJ_BATCH];
+        for (int first = threadIdx.x; first < n; first += THREADS * Table<HALF>::BATCH) {
+            int at[Table<HALF>::BATCH];
+            T x[Table<HALF>::BATCH], g[Table<HALF>::BATCH];
 #pragma unroll
-            for (int k = 0; k < AJ_BATCH; ++k) {
+            for (int k = 0; k < Table<HALF>::BATCH; ++k) {
                 at[k] = first + k * THREADS < n ? table.list[first + k * THREADS] : -1;
                 if (at[k] >= 0 && !allowed(m0, j0 + at[k])) at[k] = -1;
                 if (at[k] >= 0) {
@@ -551,7 +573,7 @@ adjust_words_kernel(const __grid_constant__ WordsArgs a)
             }
             if (!waited) { ptx::grid_wait_previous(); waited = true; }
 #pragma unroll
-            for (int k = 0; k < AJ_BATCH; ++k) {
+            for (int k = 0; k < Table<HALF>::BATCH; ++k) {
                 if (at[k] < 0) continue;
                 const float y = result(at[k], (float)x[k], GRAD ? (float)g[k] : 0.0f);
                 if (a.mode == AJ_ALL_TOO) table.word[at[k]] = __float_as_uint(y);
@@ -597,7 +619,7 @@ adjust_bias_join_kernel(const float* __restrict__ partial, int groups, int vocab
 constexpr int AJ_MAX_GROUPS = 256;       // rows of partial sums for a shared bias
 constexpr int AJ_WORDS_CHUNK = 8192;
 constexpr int AJ_DEPTH = 64;
-constexpr int AJ_MOST_SMEM = (Table<false>::words(AJ_WORDS_CHUNK, AJ_WORDS_CHUNK) + 2 * APOLLO_MAX_BIAS_WORDS) * 4;
+constexpr int AJ_MOST_SMEM = (four(Table<false>::words(AJ_WORDS_CHUNK, AJ_WORDS_CHUNK)) + 2 * APOLLO_MAX_BIAS_WORDS) * 4;
 
 bool whole_vectors(const void* p, int64_t stride, size_t e) { return (uintptr_t)p % 16 == 0 && (size_t)stride * e % 16 == 0; }
 
@@ -705,7 +727,7 @@ cudaError_t run_words(WordsArgs a, bool streamed, int sms, cudaStream_t stream)
     const int64_t blocks = (a.n_rows + rows - 1) / rows * a.chunks;
     if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
     const bool half = a.r.history_len <= AJ_SHORT && named == 0 && a.mode != AJ_ALL_TOO;
-    const int smem = half ? Table<true>::words(a.chunk, a.entries) * 4 : (Table<false>::words(a.chunk, a.entries) + 2 * named) * 4;
+    const int smem = half ? Table<true>::words(a.chunk, a.entries) * 4 : (four(Table<false>::words(a.chunk, a.entries)) + four(named) + named) * 4;
     static std::atomic<unsigned long long> allowed[2];
     const cudaError_t e = half ? allow_shared(adjust_words_kernel<T, GRAD, true>, AJ_MOST_SMEM, allowed[1]) : allow_shared(adjust_words_kernel<T, GRAD, false>, AJ_MOST_SMEM, allowed[0]);
     if (e != cudaSuccess) return e;
