@@ -15,9 +15,9 @@
 // vector of eight; 8192 x 32000 bfloat16 785 us), both passes in one kernel with barriers between them (351 us), the same with the next row's
 // loads under way (266 us, at three times the code), the words of some rows beside the stream of the next ones in one launch (six slabs of rows:
 // 375 us, the blocks of words are the long ones).
-// 8192 x 32000 bfloat16 with a bias and a mask: stream 157 us, 6.7 TB/s (its sums over rows for a bias' gradient: 201 us); words of histories of
-// 512 tokens on average, 2 M of them: 95 us (113 with 32-bit entries), where warps wait for barriers (8 cycles an instruction) and memory
-// is at 12 %.
+// 8192 x 32000 bfloat16 with a bias and a mask: stream 153 us, 6.9 TB/s (its sums over rows for a bias' gradient: 177 us, 5.9 TB/s; rows ahead in
+// shared memory made that no faster: 296 instead of 292 us for the whole gradient); words of histories of 512 tokens on average, 2 M of them: 93 us
+// (113 with 32-bit entries), gradient 103 us, where warps wait for barriers (5 cycles an instruction) and memory is at 16 %.
 #include "../../include/apollo.h"
 
 #include <cmath>
@@ -605,18 +605,30 @@ adjust_words_kernel(const __grid_constant__ WordsArgs a)
     if (!waited) ptx::grid_wait_previous();            // what comes next in the stream may count on both
 }
 
+// Sums over the groups of rows: a warp takes every eighth group for 32 columns, the eight sums are added in order (256 groups of 32000: 8 us, 20 us with
+// one thread for all groups of a column).
 template <typename T>
 __global__ void __launch_bounds__(AJ_THREADS)
 adjust_bias_join_kernel(const float* __restrict__ partial, int groups, int vocab, T* __restrict__ dbias)
 {
-    const int j = blockIdx.x * AJ_THREADS + threadIdx.x;
-    if (j >= vocab) return;
+    constexpr int WARPS = AJ_THREADS / 32;
+    __shared__ float sums[WARPS][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = blockIdx.x * 32 + lane;
     float sum = 0.0f;
-    for (int g = 0; g < groups; ++g) sum += partial[(long long)g * vocab + j];
+    if (j < vocab) {
+#pragma unroll 8
+        for (int g = warp; g < groups; g += WARPS) sum += partial[(long long)g * vocab + j];
+    }
+    sums[warp][lane] = sum;
+    __syncthreads();
+    if (warp > 0 || j >= vocab) return;
+#pragma unroll
+    for (int w = 1; w < WARPS; ++w) sum += sums[w][lane];
     dbias[j] = (T)sum;
 }
 
-constexpr int AJ_MAX_GROUPS = 256;       // rows of partial sums for a shared bias
+// Rows of partial sums for a shared bias (8192 x 32000: 128 286 us, 148 288, 256 292, 512 305).
+constexpr int AJ_MAX_GROUPS = 128;
 constexpr int AJ_WORDS_CHUNK = 8192;
 constexpr int AJ_DEPTH = 64;
 constexpr int AJ_MOST_SMEM = (four(Table<false>::words(AJ_WORDS_CHUNK, AJ_WORDS_CHUNK)) + 2 * APOLLO_MAX_BIAS_WORDS) * 4;
@@ -858,7 +870,7 @@ extern "C" int apollo_adjust_logits_grad(const void* d_logits, int64_t row_strid
     int groups = 0;
     cudaError_t err = dtype == APOLLO_DT_BF16 ? run_adjust_grad<__nv_bfloat16>(a, s, sms, &groups, stream) : run_adjust_grad<float>(a, s, sms, &groups, stream);
     if (err == cudaSuccess && shared) {
-        const unsigned grid = (unsigned)((vocab + AJ_THREADS - 1) / AJ_THREADS);
+        const unsigned grid = (unsigned)((vocab + 31) / 32);
         if (dtype == APOLLO_DT_BF16) adjust_bias_join_kernel<<<grid, AJ_THREADS, 0, stream>>>(s.partial, groups, (int)vocab, static_cast<__nv_bfloat16*>(d_grad_bias));
         else adjust_bias_join_kernel<<<grid, AJ_THREADS, 0, stream>>>(s.partial, groups, (int)vocab, static_cast<float*>(d_grad_bias));
         err = cudaGetLastError();
