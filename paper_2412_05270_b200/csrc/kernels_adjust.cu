@@ -15,7 +15,7 @@
 // vector of eight; 8192 x 32000 bfloat16 785 us), both passes in one kernel with barriers between them (351 us), the same with the next row's
 // loads under way (266 us, at three times the code), the words of some rows beside the stream of the next ones in one launch (six slabs of rows:
 // 375 us, the blocks of words are the long ones).
-// 8192 x 32000 bfloat16 with a bias and a mask: stream 153 us, 6.9 TB/s (its sums over rows for a bias' gradient: 177 us, 5.9 TB/s; rows ahead in
+// 8192 x 32000 bfloat16 with a bias and a mask: stream 153 us, 6.9 TB/s (its sums over rows for a bias' gradient: 170 us, 6.2 TB/s; rows ahead in
 // shared memory made that no faster: 296 instead of 292 us for the whole gradient); words of histories of 512 tokens on average, 2 M of them: 93 us
 // (113 with 32-bit entries), gradient 103 us, where warps wait for barriers (5 cycles an instruction) and memory is at 16 %.
 #include "../../include/apollo.h"
@@ -32,6 +32,9 @@ namespace {
 
 constexpr int AJ_THREADS = 256;
 constexpr int AJ_UNITS = 4;              // vectors a thread has of a row's chunk at once
+constexpr int AJ_STEP = 8;               // rows whose strides make a multiple of 16 bytes
+// Rows of partial sums for a shared bias, a multiple of AJ_STEP (8192 x 32000: 128 284 us, 256 290).
+constexpr int AJ_MAX_GROUPS = 128;
 constexpr int AJ_ROWS = 16;              // most rows in turn
 constexpr int AJ_SHORT = 4096;           // tokens of a history that is counted in 16 bits (at most 2^15 - 1)
 constexpr uint32_t AJ_SEEN = 0x80000000u;
@@ -365,28 +368,26 @@ struct StreamArgs {
     const uint32_t* mask;
     long long in_stride, out_stride, copy_stride, bias_stride, mask_stride, n_rows;
     uint32_t other;
-    int vocab, chunk, chunks, rows;      // rows: of a block of threads
+    int vocab, chunk, chunks, rows;      // rows: of a block of threads (1 unless they are summed), every AJ_STEP-th
 };
 
-__device__ __forceinline__ void store_partial(float* p, float a, float b, float c, float d) { p[0] = a; p[1] = b; p[2] = c; p[3] = d; }
-
 // Four vectors a thread, all loads before the first store.  EVEN: all rows start on 16-byte boundaries, so addresses differ by constants.
-// SUM: the sums over a block's rows stay in registers; every row's vectors have to start at the same columns then, so where rows are not
-// even (and SUM) the columns go one by one.
+// SUM: the sums over a block's rows stay in registers.  Every row's vectors have to start at the same columns then: a block has every eighth
+// row, which start alike whatever the stride (4096 x 50257 bfloat16 225 us; rows in order, column by column: 406), and the sums' order does
+// not depend on the layout.
 template <typename T, bool EVEN, bool SUM>
 __global__ void __launch_bounds__(AJ_THREADS)
 adjust_stream_kernel(const __grid_constant__ StreamArgs a)
 {
     using S = Sixteen<T>;
-    constexpr bool WIDE = EVEN || !SUM;
-    constexpr int N = WIDE ? S::N : 1;
+    constexpr int N = S::N;
     __shared__ typename S::Entry masks[16];
     ptx::grid_launch_dependents();
     if (threadIdx.x < 16) masks[threadIdx.x] = S::entry((int)threadIdx.x);
     __syncthreads();
     const int tid = threadIdx.x, part = blockIdx.x % a.chunks;
-    const long long group = blockIdx.x / a.chunks, begin = group * a.rows;
-    const int rows = (int)min((long long)a.rows, a.n_rows - begin);
+    const long long group = blockIdx.x / a.chunks, step = SUM ? AJ_STEP : 1, begin = SUM ? group % step + group / step * step * a.rows : group;
+    const int rows = SUM ? (int)max(0ll, min((long long)a.rows, (a.n_rows - begin + step - 1) / step)) : 1;
     const int j0 = part * a.chunk, width = min(a.chunk, a.vocab - j0);
     const T* x0 = static_cast<const T*>(a.in) + begin * a.in_stride;
     T* y0 = static_cast<T*>(a.out) + begin * a.out_stride;
@@ -399,79 +400,63 @@ adjust_stream_kernel(const __grid_constant__ StreamArgs a)
     for (int q = 0; q < (SUM ? AJ_UNITS : 1); ++q)
 #pragma unroll
         for (int e = 0; e < N; ++e) sum[q][e] = 0.0f;
+    const Span<T> span(y0, j0, width);
     for (int i = 0; i < rows; ++i) {
-        if constexpr (WIDE) {
-            const Span<T> span(y0, j0, width);
-            const bool aligned = EVEN || on_boundary(x0, span.first), c_aligned = EVEN || (c0 && on_boundary(c0, span.first)), plain = span.first % N == 0;
-            uint4 w[AJ_UNITS];
-            const T* const x = x0 + span.first + tid * N;
+        const bool aligned = EVEN || on_boundary(x0, span.first), c_aligned = EVEN || (c0 && on_boundary(c0, span.first)), plain = span.first % N == 0;
+        uint4 w[AJ_UNITS];
+        const T* const x = x0 + span.first + tid * N;
 #pragma unroll
-            for (int q = 0; q < AJ_UNITS; ++q) if (tid < span.full - q * AJ_THREADS) w[q] = load16(x + q * AJ_THREADS * N, aligned);
+        for (int q = 0; q < AJ_UNITS; ++q) if (tid < span.full - q * AJ_THREADS) w[q] = load16(x + q * AJ_THREADS * N, aligned);
 #pragma unroll
-            for (int q = 0; q < AJ_UNITS; ++q) {
-                if (tid >= span.full - q * AJ_THREADS) continue;
-                const int j = span.first + (q * AJ_THREADS + tid) * N;
-                w[q] = EVEN || (plain && !dense.bias) ? dense.template vector<true>(w[q], j) : dense.template vector<false>(w[q], j);
-                if constexpr (SUM) {
+        for (int q = 0; q < AJ_UNITS; ++q) {
+            if (tid >= span.full - q * AJ_THREADS) continue;
+            const int j = span.first + (q * AJ_THREADS + tid) * N;
+            w[q] = EVEN || (plain && !dense.bias) ? dense.template vector<true>(w[q], j) : dense.template vector<false>(w[q], j);
+            if constexpr (SUM) {
+                float g[N];
+                S::unpack(w[q], g);
+#pragma unroll
+                for (int e = 0; e < N; ++e) sum[q][e] += g[e];
+            }
+        }
+        T* const y = y0 + span.first + tid * N;
+#pragma unroll
+        for (int q = 0; q < AJ_UNITS; ++q) {
+            if (tid >= span.full - q * AJ_THREADS) continue;
+            if (!keep) *reinterpret_cast<uint4*>(y + q * AJ_THREADS * N) = w[q];
+            if (c0) {
+                T* const c = c0 + span.first + (q * AJ_THREADS + tid) * N;
+                if (c_aligned) {
+                    *reinterpret_cast<uint4*>(c) = w[q];
+                } else {
                     float g[N];
                     S::unpack(w[q], g);
 #pragma unroll
-                    for (int e = 0; e < N; ++e) sum[q][e] += g[e];
+                    for (int e = 0; e < N; ++e) c[e] = (T)g[e];
                 }
-            }
-            T* const y = y0 + span.first + tid * N;
-#pragma unroll
-            for (int q = 0; q < AJ_UNITS; ++q) {
-                if (tid >= span.full - q * AJ_THREADS) continue;
-                if (!keep) *reinterpret_cast<uint4*>(y + q * AJ_THREADS * N) = w[q];
-                if (c0) {
-                    T* const c = c0 + span.first + (q * AJ_THREADS + tid) * N;
-                    if (c_aligned) {
-                        *reinterpret_cast<uint4*>(c) = w[q];
-                    } else {
-                        float g[N];
-                        S::unpack(w[q], g);
-#pragma unroll
-                        for (int e = 0; e < N; ++e) c[e] = (T)g[e];
-                    }
-                }
-            }
-            if (const int j = span.single(); j >= 0) {
-                const T r = dense.column(x0[j], j);
-                y0[j] = r;
-                if (c0) c0[j] = r;
-                if constexpr (SUM) edge += (float)r;
-            }
-        } else {
-#pragma unroll
-            for (int q = 0; q < AJ_UNITS; ++q) {
-                const int j = j0 + q * AJ_THREADS + tid;
-                if (j >= j0 + width) continue;
-                const T r = dense.column(x0[j], j);
-                y0[j] = r;
-                if constexpr (SUM) sum[q][0] += (float)r;
             }
         }
-        x0 += a.in_stride;
-        y0 += a.out_stride;
+        if (const int j = span.single(); j >= 0) {
+            const T r = dense.column(x0[j], j);
+            y0[j] = r;
+            if (c0) c0[j] = r;
+            if constexpr (SUM) edge += (float)r;
+        }
+        x0 += step * a.in_stride;
+        y0 += step * a.out_stride;
         if (c0) c0 += a.copy_stride;
         if (dense.bias) dense.bias += a.bias_stride;
-        if (dense.mask) dense.mask += a.mask_stride;
+        if (dense.mask) dense.mask += step * a.mask_stride;
     }
     if constexpr (SUM) {
-        float* const p = a.partial + group * a.vocab + j0;
+        float* const p = a.partial + group * a.vocab;
 #pragma unroll
         for (int q = 0; q < AJ_UNITS; ++q) {
-            const int u = (q * AJ_THREADS + tid) * N;
-            if constexpr (WIDE) {
+            if (tid >= span.full - q * AJ_THREADS) continue;
 #pragma unroll
-                for (int e = 0; e < N; e += 4) if (u + N <= width) store_partial(p + u + e, sum[q][e], sum[q][e + 1], sum[q][e + 2], sum[q][e + 3]);
-            } else {
-                if (u < width) p[u] = sum[q][0];
-            }
+            for (int e = 0; e < N; ++e) p[span.first + (q * AJ_THREADS + tid) * N + e] = sum[q][e];
         }
-        // (the columns left are behind the last whole vector)
-        if (WIDE && tid >= 32 && tid - 32 < width % N) p[width / N * N + tid - 32] = edge;
+        if (const int j = span.single(); j >= 0) p[j] = edge;
     }
 }
 
@@ -627,8 +612,6 @@ adjust_bias_join_kernel(const float* __restrict__ partial, int groups, int vocab
     dbias[j] = (T)sum;
 }
 
-// Rows of partial sums for a shared bias (8192 x 32000: 128 286 us, 148 288, 256 292, 512 305).
-constexpr int AJ_MAX_GROUPS = 128;
 constexpr int AJ_WORDS_CHUNK = 8192;
 constexpr int AJ_DEPTH = 64;
 constexpr int AJ_MOST_SMEM = (four(Table<false>::words(AJ_WORDS_CHUNK, AJ_WORDS_CHUNK)) + 2 * APOLLO_MAX_BIAS_WORDS) * 4;
@@ -699,12 +682,17 @@ cudaError_t run_stream(StreamArgs a, int sms, int* groups, cudaStream_t stream)
     const bool sum = a.partial != nullptr;
     const bool even = whole_vectors(a.in, a.in_stride, e) && whole_vectors(a.out, a.out_stride, e) && whole_vectors(a.copy, a.copy ? a.copy_stride : 0, e) &&
                       whole_vectors(a.bias, a.bias ? a.bias_stride : 0, e);
-    a.chunk = AJ_UNITS * AJ_THREADS * (even || !sum ? Sixteen<T>::N : 1);
+    a.chunk = AJ_UNITS * AJ_THREADS * Sixteen<T>::N;
     if (!sum)
         while (a.chunk > 2048 && a.n_rows * ((a.vocab + a.chunk - 1) / a.chunk) < 2LL * sms) a.chunk /= 2;
     a.chunks = (a.vocab + a.chunk - 1) / a.chunk;
-    a.rows = sum ? (int)((a.n_rows + AJ_MAX_GROUPS - 1) / AJ_MAX_GROUPS) : 1;
-    const int64_t n = (a.n_rows + a.rows - 1) / a.rows;
+    a.rows = 1;
+    int64_t n = a.n_rows;
+    if (sum) {
+        const int64_t each = (a.n_rows + AJ_STEP - 1) / AJ_STEP, most = AJ_MAX_GROUPS / AJ_STEP;
+        a.rows = (int)((each + most - 1) / most);
+        if (a.rows > 1) n = (each + a.rows - 1) / a.rows * AJ_STEP;       // (one row each: group and row have the same number)
+    }
     *groups = (int)n;
     if (n * a.chunks > INT32_MAX) return cudaErrorInvalidConfiguration;
     const unsigned grid = (unsigned)(n * a.chunks);

@@ -334,3 +334,29 @@ def test_values_of_a_gradient_that_the_call_before_has_left():
         B.adjust_logits(d, mask=mask, out=d)
         r = B.adjust_logits_grad(d, d, bias_index=index, out=d)
         assert torch.equal(r.value, want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape", [(129, 20011), (300, 16391), (1111, 515)])
+def test_a_shared_bias_of_odd_rows_in_several_chunks(shape, dtype):
+    g = torch.Generator().manual_seed(13)
+    z, r = make(*shape, dtype, g, allowed=0.7)
+    dy = torch.randn(*shape, generator=g).to(dtype)
+    a = torch.where(rules_in_64(*shape, r)[-1], dy.double(), 0.0)
+    got = B.adjust_logits_grad(z.cuda(), dy.cuda(), bias="shared", mask=r["mask"].cuda())
+    assert torch.equal(got.logits.cpu().double(), a)
+    # a sum of n values in fp32, rounded once more to the type: n - 1 half steps of the partial sums' sizes, half a step of the result
+    want, half = a.sum(0), torch.finfo(dtype).eps / 2
+    assert bool(((got.bias.cpu().double() - want).abs() <= shape[0] * U * a.abs().sum(0) + half * want.abs() * (1 + half)).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_in_place_with_a_bias_in_several_chunks(dtype):
+    g = torch.Generator().manual_seed(14)
+    z, r = make(3, 40_005, dtype, g, length=6000, bias="shared", words=63, allowed=0.8)
+    want, bound = plain(z, r)
+    zc, rc = z.cuda(), cuda(r)
+    got = B.adjust_logits(zc, **rc)
+    check(got, want, bound)
+    B.adjust_logits(zc, **rc, out=zc)
+    assert torch.equal(zc, got)
