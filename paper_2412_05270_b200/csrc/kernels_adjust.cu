@@ -7,8 +7,8 @@
 //
 // Two kernels.  One streams over rows and knows of bias and mask alone.  The other takes a chunk of the vocabulary for one row, or for a few
 // rows in turn: it counts the tokens of its chunk in a table in shared memory and lists the words that occur (integer atomics: their
-// order decides the order of the list, not the results), then writes the listed words, one a thread.  In place without a bias the second one
-// does everything: the listed words and the masked ones are all that changes.  Rows that share a history (the positions of a sequence in
+// order decides the order of the list, not the results), then writes the listed words, one a thread.  In place the second one
+// does everything: without a bias the listed words and the masked ones are all that changes.  Rows that share a history (the positions of a sequence in
 // training) go on with the table of the row before: they add the tokens in between.  A table word holds
 // [31] seen at all  [30..20] 1 + slot of the word's named value  [19..0] how often from `start` on;  of short histories half of that.
 // What was tried: vectors that look into the table (in a training batch nearly every warp had a word to look up: 376 instructions a
@@ -16,7 +16,7 @@
 // loads under way (266 us, at three times the code), the words of some rows beside the stream of the next ones in one launch (six slabs of rows:
 // 375 us, the blocks of words are the long ones).
 // 8192 x 32000 bfloat16 with a bias and a mask: stream 153 us, 6.9 TB/s (its sums over rows for a bias' gradient: 170 us, 6.2 TB/s; rows ahead in
-// shared memory made that no faster: 296 instead of 292 us for the whole gradient); words of histories of 512 tokens on average, 2 M of them: 93 us
+// shared memory made that no faster: 296 instead of 292 us for the whole gradient); words of histories of 512 tokens on average, 2 M of them: 97 us
 // (113 with 32-bit entries), gradient 103 us, where warps wait for barriers (5 cycles an instruction) and memory is at 16 %.
 #include "../../include/apollo.h"
 
@@ -95,7 +95,7 @@ template <bool HALF>
 struct Table {
     static constexpr int THREADS = HALF ? AJ_THREADS / 2 : AJ_THREADS;
     // Scattered loads that a thread has in flight.  Long histories: 8, 21.8 us for 129 rows of 8191 tokens (4: 26.3, 16: 29.3 and 36.8).  Short ones,
-    // most of them a few tokens more than the row before: 4 (8: 8192 x 32000 261 us instead of 254).
+    // most of them a few tokens more than the row before: 4 (8: 8192 x 32000 261 us for 254).
     static constexpr int BATCH = HALF ? 4 : 8;
     uint32_t* word;
     uint16_t* list;                      // chunk <= 65536
@@ -464,7 +464,8 @@ adjust_stream_kernel(const __grid_constant__ StreamArgs a)
 enum : int {
     AJ_WORDS_ONLY = 0,                   // the stream has written the others
     AJ_MASKED_TOO = 1,                   // in place: the masked words
-    AJ_ALL_TOO = 2,                      // in place with a bias: every other word (one row a block; the listed words' results wait in the table)
+    AJ_ALL_TOO = 2,                      // in place with a bias: every other word (one row a block; the listed words' results wait in the table, the
+                                         // row is on its way while the table is made)
 };
 
 struct WordsArgs {
@@ -480,11 +481,13 @@ struct WordsArgs {
     Rules r;
 };
 
-// Blocks a multiprocessor that the registers are to allow: it decides how the compiler orders the scattered loads.  8192 x 32000 bfloat16:
-// forward 9 252 us, 8 254, 10 260; gradient 6 304 us, 8 306, 9 330; in fp32 (777 x 50001) 9 88 us, 6 90.
-constexpr int words_resident(bool half, bool grad, size_t e) { return !half ? 4 : grad && e == 2 ? 6 : 9; }
+// Blocks a multiprocessor that the registers are to allow: it decides how the compiler orders the scattered loads.  Short histories, forward:
+// 12 (8192 x 32000 bfloat16 257 us, 4096 x 50256 in place 57.5; 6 255 and 65.7; 9 260 and 59.5); gradient: bfloat16 6 (8192 x 32000 304 us,
+// 9 330), fp32 9 (777 x 50001 88 us, 6 90).  Others 4: what shared memory holds (in place with a bias, 4096 x 50256 bfloat16: 280 us, 5 344).
+constexpr int words_resident(bool half, bool grad, size_t e) { return !half ? 4 : !grad ? 12 : e == 2 ? 6 : 9; }
 
-template <typename T, bool GRAD, bool HALF>
+// ALL: mode AJ_ALL_TOO.
+template <typename T, bool GRAD, bool HALF, bool ALL>
 __global__ void __launch_bounds__(Table<HALF>::THREADS, words_resident(HALF, GRAD, sizeof(T)))
 adjust_words_kernel(const __grid_constant__ WordsArgs a)
 {
@@ -517,6 +520,14 @@ adjust_words_kernel(const __grid_constant__ WordsArgs a)
         T* const y0 = static_cast<T*>(a.out) + row * a.out_stride;
         const T* const b0 = !GRAD && a.r.bias ? static_cast<const T*>(a.r.bias) + row * a.r.bias_stride : nullptr;
         const uint32_t* const m0 = a.r.mask ? a.r.mask + row * a.r.mask_stride : nullptr;
+        const Span<T> span(y0, j0, width);
+        uint4 w[AJ_UNITS];
+        auto load = [&](int first) {
+#pragma unroll
+            for (int q = 0; q < AJ_UNITS; ++q)
+                if (const int u = first + q * THREADS; u < span.full) w[q] = *reinterpret_cast<const uint4*>(y0 + span.first + u * N);
+        };
+        if constexpr (ALL) load(threadIdx.x);
         if constexpr (!GRAD && !HALF) if (a.r.n_bias) read_words<THREADS>(a.r, row, a.vocab, words);       // (such rows are not taken in turn)
         if (a.r.history) table.set(a.r, plan, a.vocab, a.chunk);
         if constexpr (GRAD) {
@@ -561,30 +572,34 @@ adjust_words_kernel(const __grid_constant__ WordsArgs a)
             for (int k = 0; k < Table<HALF>::BATCH; ++k) {
                 if (at[k] < 0) continue;
                 const float y = result(at[k], (float)x[k], GRAD ? (float)g[k] : 0.0f);
-                if (a.mode == AJ_ALL_TOO) table.word[at[k]] = __float_as_uint(y);
+                if constexpr (ALL) table.word[at[k]] = __float_as_uint(y);
                 else y0[j0 + at[k]] = (T)y;
             }
         }
         __syncthreads();                               // done with the table, and with vectors that hold listed words and masked ones
-        if (a.mode == AJ_WORDS_ONLY || (a.mode == AJ_MASKED_TOO && !m0)) continue;
-        const Span<T> span(y0, j0, width);
+        if (!ALL && (a.mode == AJ_WORDS_ONLY || !m0)) continue;
         const Dense<T> dense{ b0, m0, masks, a.other, (a.vocab + 31) / 32 };
-        for (int u = threadIdx.x; u < span.full; u += THREADS) {
-            const int j = span.first + u * N;
-            uint4* const y = reinterpret_cast<uint4*>(y0 + j);
-            if (a.mode == AJ_ALL_TOO) {
-                *y = dense.template vector<false>(*y, j);
-            } else {
-                const uint32_t live = bits_at<N>(m0, j, dense.mask_words);
-                if (live != (1u << N) - 1u) *y = select4(S::masks(masks, live), live ? *y : make_uint4(0, 0, 0, 0), a.other);
+        auto at = [&](int u) { return reinterpret_cast<uint4*>(y0 + span.first + u * N); };
+        if constexpr (ALL) {
+            for (int first = threadIdx.x; first < span.full; first += THREADS * AJ_UNITS) {
+                if (first != (int)threadIdx.x) load(first);
+#pragma unroll
+                for (int q = 0; q < AJ_UNITS; ++q)
+                    if (const int u = first + q * THREADS; u < span.full) *at(u) = dense.template vector<false>(w[q], span.first + u * N);
+            }
+        } else {
+            for (int u = threadIdx.x; u < span.full; u += THREADS) {
+                const uint32_t live = bits_at<N>(m0, span.first + u * N, dense.mask_words);
+                if (live != (1u << N) - 1u) *at(u) = select4(S::masks(masks, live), live ? *at(u) : make_uint4(0, 0, 0, 0), a.other);
             }
         }
-        if (const int j = span.single(); j >= 0 && (a.mode == AJ_ALL_TOO || !allowed(m0, j))) y0[j] = dense.column(y0[j], j);
-        if (a.mode != AJ_ALL_TOO) continue;
-        __syncthreads();
-        for (int k = threadIdx.x; k < n; k += THREADS) {
-            const int j = table.list[k];
-            if (allowed(m0, j0 + j)) y0[j0 + j] = (T)__uint_as_float(table.word[j]);
+        if (const int j = span.single(); j >= 0 && (ALL || !allowed(m0, j))) y0[j] = dense.column(y0[j], j);
+        if constexpr (ALL) {
+            __syncthreads();
+            for (int k = threadIdx.x; k < n; k += THREADS) {
+                const int j = table.list[k];
+                if (allowed(m0, j0 + j)) y0[j0 + j] = (T)__uint_as_float(table.word[j]);
+            }
         }
     }
     if (!waited) ptx::grid_wait_previous();            // what comes next in the stream may count on both
@@ -728,8 +743,10 @@ cudaError_t run_words(WordsArgs a, bool streamed, int sms, cudaStream_t stream)
     if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
     const bool half = a.r.history_len <= AJ_SHORT && named == 0 && a.mode != AJ_ALL_TOO;
     const int smem = half ? Table<true>::words(a.chunk, a.entries) * 4 : (four(Table<false>::words(a.chunk, a.entries)) + four(named) + named) * 4;
-    static std::atomic<unsigned long long> allowed[2];
-    const cudaError_t e = half ? allow_shared(adjust_words_kernel<T, GRAD, true>, AJ_MOST_SMEM, allowed[1]) : allow_shared(adjust_words_kernel<T, GRAD, false>, AJ_MOST_SMEM, allowed[0]);
+    void (*kernel)(WordsArgs) = half ? adjust_words_kernel<T, GRAD, true, false> : adjust_words_kernel<T, GRAD, false, false>;
+    if constexpr (!GRAD) if (a.mode == AJ_ALL_TOO) kernel = adjust_words_kernel<T, false, false, true>;
+    static std::atomic<unsigned long long> allowed[3];
+    const cudaError_t e = allow_shared(kernel, AJ_MOST_SMEM, allowed[a.mode == AJ_ALL_TOO ? 2 : half]);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
@@ -741,7 +758,7 @@ cudaError_t run_words(WordsArgs a, bool streamed, int sms, cudaStream_t stream)
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = streamed ? 1 : 0;
-    return half ? cudaLaunchKernelEx(&cfg, adjust_words_kernel<T, GRAD, true>, a) : cudaLaunchKernelEx(&cfg, adjust_words_kernel<T, GRAD, false>, a);
+    return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 template <typename T>
