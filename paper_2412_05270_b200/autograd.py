@@ -1,7 +1,10 @@
 """The two ends of a language model as autograd functions: token embedding, adjusted logits and token log probabilities.
 
 All call the library's kernels in either direction (no PyTorch arithmetic in between); see `binding` for the shapes
-and types they take.  They have first derivatives; differentiating one of those raises."""
+and types they take.  They have first derivatives; differentiating one of those raises.
+
+Forward and backward pass can be captured into a CUDA graph together.  No graph of autograd's that was made outside the capture may then
+hold the same leaves: PyTorch would add up their gradients on the stream of that one."""
 from __future__ import annotations
 
 import torch
