@@ -235,8 +235,13 @@ template <> struct Sixteen<__nv_bfloat16> {
     }
     __device__ static __forceinline__ uint4 gather(const __nv_bfloat16* p)
     {
+        // (words of 32 bits from the first boundary on: a bias shared by odd rows, 4096 x 50257, 135 us; eight halves each 170)
         const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
-        return make_uint4(q[0] | (uint32_t)q[1] << 16, q[2] | (uint32_t)q[3] << 16, q[4] | (uint32_t)q[5] << 16, q[6] | (uint32_t)q[7] << 16);
+        const int odd = (uint32_t)(uintptr_t)p >> 1 & 1;
+        const uint32_t* const w = reinterpret_cast<const uint32_t*>(q + odd);
+        if (!odd) return make_uint4(w[0], w[1], w[2], w[3]);
+        const uint32_t first = q[0], last = q[7];
+        return make_uint4(first | w[0] << 16, __funnelshift_r(w[0], w[1], 16), __funnelshift_r(w[1], w[2], 16), w[2] >> 16 | last << 16);
     }
 };
 
