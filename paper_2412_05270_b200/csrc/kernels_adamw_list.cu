@@ -50,8 +50,10 @@ __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
 // ---------------------------------------------------------------- norm
-// One read of every gradient: 262 M bfloat16 in 82 us, 6.4 TB/s; fp32 in 150 us, 7.0 TB/s.  A thread sums 32 squares in fp32 and adds them up in
-// fp64; where the sum is near either end of fp32's range it squares the same 32 in fp64.
+// One read of every gradient, squares and sums in fp64: the norm is rounded once.  262 M bfloat16 in 87 us, 6.0 TB/s; fp32 in 152 us, 6.9 TB/s.
+// (32 squares at a time in fp32: 81 us, but squares of bfloat16 end in few bit patterns, so the rounding of their sums is biased: 1e-8 of the
+// norm, one seed in eight had another last bit, and with the factor's last bit a clipped step has other codes.  Values converted by cvt instead of
+// moved bits: 90.5 us.  The next tile's loads under way in registers: 81 us, but fp32 154 to 162, and a 60M model's gradients 27 us either way.)
 constexpr int GN_TILE = 8192;            // elements of one tile
 constexpr int GN_THREADS = 256;
 constexpr int GN_MAX_GRID = 2048;        // partial sums of one launch at most
@@ -66,10 +68,30 @@ struct NormArgs {
     double* partial;
 };
 
-// Sum of the squares of eight raw 16-byte vectors (a thread's share of a tile is 32 elements of either type).
+// A thread's share of a tile is 32 elements of either type, in vectors of 16 bytes.  squares() adds up those of a word (one fp32, two bfloat16) times
+// 2^-256: the bits of |v| moved to a double's place, with an exponent that makes it 2^-128 |v|.  Zero becomes 2^-255 instead, a subnormal number
+// 2^-255 to 2^-254, infinity and NaN at least 1: sums outside [2^-436, 1) are formed once more from converted values.
 template <typename T> struct NormShare;
-template <> struct NormShare<__nv_bfloat16> { static constexpr int VECS = 4, N = 8; };
-template <> struct NormShare<float> { static constexpr int VECS = 8, N = 4; };
+template <> struct NormShare<__nv_bfloat16> {
+    static constexpr int VECS = 4, N = 8;
+    static constexpr uint32_t MAGNITUDE = 0x7FFF7FFFu;
+    __device__ static __forceinline__ double moved(uint32_t h) { return __hiloint2double((int)((h & 0x0FFFE000u) | 0x30000000u), 0); }
+    __device__ static __forceinline__ void squares(uint32_t w, double& s, double& t)
+    {
+        const double a = moved(w << 13), b = moved(w >> 3);
+        s = fma(a, a, s);
+        t = fma(b, b, t);
+    }
+};
+template <> struct NormShare<float> {
+    static constexpr int VECS = 8, N = 4;
+    static constexpr uint32_t MAGNITUDE = 0x7FFFFFFFu;
+    __device__ static __forceinline__ void squares(uint32_t w, double& s, double&)
+    {
+        const double a = __hiloint2double((int)((w >> 3 & 0x0FFFFFFFu) | 0x30000000u), (int)(w << 29));
+        s = fma(a, a, s);
+    }
+};
 
 __device__ __forceinline__ void norm_unpack(const uint4& r, float (&v)[8], __nv_bfloat16) { unpack_bf16x8(r, v); }
 __device__ __forceinline__ void norm_unpack(const uint4& r, float (&v)[4], float)
@@ -102,20 +124,20 @@ __device__ __forceinline__ double tile_squares(const T* __restrict__ g, long lon
             }
         }
     }
-    float s = 0.0f;
+    double s = 0.0, t = 0.0, u = 0.0, w = 0.0;
 #pragma unroll
     for (int i = 0; i < VECS; ++i) {
-        float v[N];
-        norm_unpack(raw[i], v, T());
-#pragma unroll
-        for (int x = 0; x < N; ++x) s = fmaf(v[x], v[x], s);
+        NormShare<T>::squares(raw[i].x, s, t);
+        NormShare<T>::squares(raw[i].y, u, w);
+        NormShare<T>::squares(raw[i].z, s, t);
+        NormShare<T>::squares(raw[i].w, u, w);
     }
-    // In the middle of fp32's range nothing has overflowed, and what may have underflowed is below 2^-36 of the sum.
-    if (s >= 0x1p-90f && s <= 0x1p120f) return (double)s;
+    const double sum = (s + t) + (u + w);
+    if (sum >= 0x1p-436 && sum < 1.0) return sum * 0x1p256;
     uint32_t any = 0;
 #pragma unroll
     for (int i = 0; i < VECS; ++i) any |= raw[i].x | raw[i].y | raw[i].z | raw[i].w;
-    if (any == 0) return 0.0;
+    if ((any & NormShare<T>::MAGNITUDE) == 0) return 0.0;
     double d = 0.0;
 #pragma unroll 1
     for (int i = 0; i < VECS; ++i) {
