@@ -564,7 +564,8 @@ class AdamW:
     mixture, none of them twice), with the moments of all of them in one buffer, `state`: of 8 or 32 bits, zero before the first step.
 
     state: a uint8 CUDA tensor of adamw_state_bytes() to go on with (a checkpoint is a copy of it, with the step count and the
-    seed), made if None.  Calls run on `stream` or the device's current one, whichever device is current."""
+    seed), made if None (the constructor waits for the current stream then).  Calls run on `stream` or the device's current one,
+    whichever device is current; steps on different streams are the caller's to order."""
 
     def __init__(self, params, bits: int = 8, beta1=0.9, beta2=0.999, eps=1e-8, seed: int = 0, bias_correction: bool = True,
                  state=None):
@@ -585,21 +586,27 @@ class AdamW:
         self._cfg_at = ctypes.addressof(self.cfg)
         nbytes = adamw_state_bytes(numels, bits)
         self.n_blocks = nbytes // (2 * ADAMW_BLOCK + 2 if bits == 8 else 8 * ADAMW_BLOCK)
+        self._streams = set()                                # what the allocator knows of the state's use
         with _on(None, self.device):
             if state is None:
                 state = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+                self._streams.add(_stream_ptr(None))         # the state belongs to this one
+                if not torch.cuda.is_current_stream_capturing():
+                    # whichever stream the first step runs on (or is captured on), the zeros are there
+                    torch.cuda.current_stream().synchronize()
             elif state.dtype != torch.uint8 or state.numel() != nbytes or not state.is_contiguous():
                 raise ValueError(f"state must be a contiguous uint8 CUDA tensor of {nbytes} bytes")
             elif state.device != self.device:
                 raise _two_devices()
-            self._home = _stream_ptr(None)                   # the stream that the state belongs to
         self.state = state
 
     def _run(self, stream) -> int:
         ptr = _stream_ptr(stream)
-        if ptr != self._home:
-            # freed, the state must not be handed out again before this stream is done with it
+        if ptr not in self._streams:
+            # freed, the state must not be handed out again before this stream is done with it (which stream a state of the caller's belongs to
+            # is not known here)
             self.state.record_stream(torch.cuda.current_stream())
+            self._streams.add(ptr)
         return ptr
 
     def _scalar(self, x, dtype, what):
