@@ -64,3 +64,31 @@ def test_a_state_of_the_callers_is_not_handed_out_while_a_step_uses_it(bits):
         assert torch.empty(nbytes, dtype=torch.uint8, device="cuda").data_ptr() != at
     torch.cuda.synchronize()
     assert bool((p < 0).all())
+
+
+def test_lists_on_several_streams_that_are_under_way_together():
+    """Steps, norms and logits of three streams queued in turn with no wait between them are those of single calls."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    made = []
+    for _ in range(3):
+        ps = [torch.randn(n, generator=g, device="cuda") for n in (70_000, 300, 5_000_000)]
+        gs = [torch.randn(p.numel(), generator=g, device="cuda") for p in ps]
+        made.append((ps, gs, torch.randn(300, 5001, generator=g, device="cuda"), torch.randint(0, 5001, (300, 700), generator=g, device="cuda")))
+
+    def queue(opt, gs, z, h, t, stream):
+        factor = B.grad_norm(gs, 1.0, stream=stream)
+        opt.step(gs, lr=0.1, t=t, factor=factor[1:], stream=stream)
+        y = B.adjust_logits(z, history=h, repetition=1.5, presence=0.5, stream=stream)
+        d = B.adjust_logits_grad(z, y, history=h, repetition=1.5, bias="shared", stream=stream)
+        return [factor, y, d.logits, d.bias]
+    ends = []
+    for streams in ([None] * 3, [torch.cuda.Stream() for _ in range(3)]):
+        opts = [B.AdamW([p.clone() for p in ps], seed=3) for ps, *_ in made]
+        torch.cuda.synchronize()
+        for s in streams:
+            with torch.cuda.stream(s):
+                busy()                                    # all three streams have their work queued before any of it runs
+        out = [queue(opt, gs, z, h, t, s) for t in range(3) for opt, (_, gs, z, h), s in zip(opts, made, streams)]
+        torch.cuda.synchronize()
+        ends.append([x for o in out for x in o] + [x for o in opts for x in o.params + [o.state]])
+    assert all(torch.equal(a, b) for a, b in zip(*ends))
