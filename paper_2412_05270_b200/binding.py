@@ -15,9 +15,10 @@ from typing import NamedTuple
 
 import torch
 
+from .build import marshal_path
+
 _PKG = Path(__file__).resolve().parent
 LIB_PATH = _PKG / "libapollo.so"
-MARSHAL_PATH = _PKG / "_marshal.so"
 DEBUG_LIB_PATH = _PKG / "libapollo_debug.so"     # built with -DAPOLLO_DEBUG: index checks inside every kernel
 
 OK = 0
@@ -502,9 +503,10 @@ def _marshal():
     """The extension that reads tensors (csrc/marshal.cpp); raises if it has not been built (there is no fallback)."""
     global _marshal_module
     if _marshal_module is None:
-        if not MARSHAL_PATH.exists():
-            raise ImportError(f"{MARSHAL_PATH} is missing: run `python -m paper_2412_05270_b200.build`")
-        spec = importlib.util.spec_from_file_location("_marshal", MARSHAL_PATH)
+        path = marshal_path()
+        if not path.exists():
+            raise ImportError(f"{path} is missing (it is built for one Python and one torch): run `python -m paper_2412_05270_b200.build`")
+        spec = importlib.util.spec_from_file_location("_marshal", path)
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
         _marshal_module = module

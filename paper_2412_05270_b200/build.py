@@ -1,6 +1,7 @@
 """Builds libapollo.so (hand-written CUDA for sm_100a) in-tree with nvcc."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 from pathlib import Path
@@ -26,19 +27,25 @@ def _stale(lib: Path = LIB) -> bool:
     return any(p.stat().st_mtime > built for p in deps)
 
 
-MARSHAL = PKG / "_marshal.so"               # csrc/marshal.cpp: what the binding asks of tensors
+def marshal_path() -> Path:
+    """The binding's extension (csrc/marshal.cpp: what it asks of tensors) for the Python and the torch that are running; one built for others has
+    another name (their tensors lie otherwise in memory)."""
+    import sysconfig
+
+    import torch
+    return PKG / f"_marshal.{sysconfig.get_config_var('SOABI')}.torch-{torch.__version__}.so"
 
 
 def build_marshal(force: bool = False) -> Path:
     """Compiles the Python extension that reads tensors for the binding (against torch's headers; torch is loaded first)."""
-    src = CSRC / "marshal.cpp"
-    if not force and MARSHAL.exists() and MARSHAL.stat().st_mtime >= max(src.stat().st_mtime, Path(__file__).stat().st_mtime):
-        return MARSHAL
+    src, path = CSRC / "marshal.cpp", marshal_path()
+    if not force and path.exists() and path.stat().st_mtime >= max(src.stat().st_mtime, Path(__file__).stat().st_mtime):
+        return path
     import sysconfig
 
     import torch
     from torch.utils import cpp_extension
-    tmp = MARSHAL.with_suffix(f".{os.getpid()}.tmp")
+    tmp = path.with_name(f"{path.name}.{os.getpid()}.tmp")
     include = [f"-I{p}" for p in cpp_extension.include_paths()] + [f"-I{sysconfig.get_paths()['include']}"]
     libs = [f"-L{p}" for p in cpp_extension.library_paths()] + ["-lc10", "-ltorch_cpu", "-ltorch_python"]
     out = subprocess.run([os.environ.get("CXX", "g++"), "-shared", "-fPIC", "-O2", "-std=c++17", "-fvisibility=hidden", "-w",
@@ -47,15 +54,21 @@ def build_marshal(force: bool = False) -> Path:
     if out.returncode != 0:
         print(out.stdout)
         raise RuntimeError("g++ failed on marshal.cpp")
-    os.replace(tmp, MARSHAL)
-    return MARSHAL
+    os.replace(tmp, path)
+    return path
 
 
 def build_library(force: bool = False, verbose: bool = False, debug: bool = False) -> Path:
-    """Compiles the library in-tree.  debug=True builds libapollo_debug.so: every kernel checks the index
-    range of its global loads and stores and reports a violation through the context's status word
-    (apollo_status returns APOLLO_ERR_INTERNAL) instead of making the access."""
-    build_marshal()
+    """Compiles the library in-tree, with nvcc alone, and then, where torch is installed, the binding's extension.  debug=True builds
+    libapollo_debug.so: every kernel checks the index range of its global loads and stores and reports a violation through the
+    context's status word (apollo_status returns APOLLO_ERR_INTERNAL) instead of making the access."""
+    lib = _compile(force, verbose, debug)
+    if importlib.util.find_spec("torch") is not None:
+        build_marshal(force)
+    return lib
+
+
+def _compile(force: bool, verbose: bool, debug: bool) -> Path:
     lib = LIB_DEBUG if debug else LIB
     if not force and not _stale(lib):
         return lib
