@@ -581,8 +581,7 @@ class AdamW:
         if len(set(used)) < len(used):
             raise ValueError("a parameter is in the list twice")
         self.device, self._index, self.bits = torch.device("cuda", index), index, bits
-        # (the list as it is now: what a step must find again, whatever becomes of the parameters' data)
-        self._like = [p.detach() for p in self.params]
+        self._shapes = [tuple(p.shape) for p in self.params]               # what a step must find again, whatever becomes of the parameters' data
         numels = [p.numel() for p in self.params]
         self.cfg = AdamWListConfig(int(bits), int(bool(bias_correction)), float(beta1), float(beta2), float(eps), int(seed))
         self._cfg_at = ctypes.addressof(self.cfg)
@@ -625,7 +624,7 @@ class AdamW:
         runs: a captured step can be replayed with other values); factor: a float32 CUDA tensor of one value that the gradients are multiplied by
         (grad_norm(...)[1:]); where it is not finite the step changes nothing."""
         index = self._index
-        pointers, lengths, types, _, _ = self._pack("params", self.params, self._like, index)
+        pointers, lengths, types, _, _ = self._pack("params", self.params, self._shapes, index)
         g_pointers, _, g_types, _, _ = self._pack("grads", grads, self.params, index)
         lr_at = t_at = factor_at = None
         if isinstance(lr, torch.Tensor):

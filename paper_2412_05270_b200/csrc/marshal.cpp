@@ -54,9 +54,24 @@ PyObject* refuse(const char* what, const char* why)
     return nullptr;
 }
 
+// Whether a tensor, or a tuple of whole numbers, has these sizes.
+bool same_shape(PyObject* other, at::IntArrayRef sizes)
+{
+    if (THPVariable_Check(other)) return THPVariable_Unpack(other).sizes().equals(sizes);
+    if (!PyTuple_Check(other) || (size_t)PyTuple_GET_SIZE(other) != sizes.size()) return false;
+    for (size_t i = 0; i < sizes.size(); ++i) {
+        const long long n = PyLong_AsLongLong(PyTuple_GET_ITEM(other, (Py_ssize_t)i));
+        if (n != (long long)sizes[i]) {
+            PyErr_Clear();
+            return false;
+        }
+    }
+    return true;
+}
+
 // pack(what, tensors, like, device): addresses (uint64), lengths (int64) and types (int32, 0 = float32, 1 = bfloat16) of a list of contiguous
-// CUDA tensors as bytes, their device and how many there are.  None: address 0.  like: a list whose shapes they must have, or None; device: the
-// index they must be on, or -1.
+// CUDA tensors as bytes, their device and how many there are.  None: address 0.  like: a list of the shapes (tuples) or tensors whose shapes they must
+// have, or None; device: the index they must be on, or -1.
 PyObject* pack(PyObject*, PyObject* args)
 {
     const char* what;
@@ -91,7 +106,7 @@ PyObject* pack(PyObject*, PyObject* args)
                 if (device_index(t) != device) return refuse("the tensors of a call, out and workspace among them,", "must be on one device");
                 if (shapes) {
                     PyObject* other = PySequence_Fast_GET_ITEM(shapes, i);
-                    if (!THPVariable_Check(other) || !THPVariable_Unpack(other).sizes().equals(t.sizes())) return refuse(what, "must have their parameters' shapes");
+                    if (!same_shape(other, t.sizes())) return refuse(what, "must have their parameters' shapes");
                 }
                 address[(size_t)i] = (uint64_t)(uintptr_t)t.data_ptr();
                 length[(size_t)i] = t.numel();
