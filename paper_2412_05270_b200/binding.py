@@ -538,6 +538,7 @@ def grad_norm(grads, max_norm: float = math.inf, out=None, workspace=None, strea
                 raise ValueError(f"{what} must be contiguous")
     if out is not None and (out.dtype != torch.float32 or out.numel() != 2):
         raise ValueError("out must hold two float32 values")
+    given = out
     with _on_index(stream, device):
         if out is None:
             out = torch.empty_strided((2,), (1,), dtype=torch.float32, device="cuda")
@@ -545,6 +546,8 @@ def grad_norm(grads, max_norm: float = math.inf, out=None, workspace=None, strea
             workspace = torch.empty_strided((grad_norm_workspace_bytes(n),), (1,), dtype=torch.uint8, device="cuda")
         _check(load().apollo_grad_norm(pointers, lengths, types, n, max_norm, out.data_ptr(), workspace.data_ptr(),
                                        workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "apollo_grad_norm")
+    if given is not None:
+        _marshal().changed((given,), None)
     return out
 
 
@@ -572,7 +575,7 @@ class AdamW:
     def __init__(self, params, bits: int = 8, beta1=0.9, beta2=0.999, eps=1e-8, seed: int = 0, bias_correction: bool = True,
                  state=None):
         self.lib = load()
-        self._pack = _marshal().pack
+        self._pack, self._changed = _marshal().pack, _marshal().changed
         self.params = list(params)
         if not self.params or any(p is None for p in self.params):
             raise ValueError("AdamW needs a list of parameters")
@@ -624,6 +627,8 @@ class AdamW:
         runs: a captured step can be replayed with other values); factor: a float32 CUDA tensor of one value that the gradients are multiplied by
         (grad_norm(...)[1:]); where it is not finite the step changes nothing."""
         index = self._index
+        if not isinstance(grads, (list, tuple)):
+            grads = list(grads)                              # read twice
         pointers, lengths, types, _, _ = self._pack("params", self.params, self._shapes, index)
         g_pointers, _, g_types, _, _ = self._pack("grads", grads, self.params, index)
         lr_at = t_at = factor_at = None
@@ -637,6 +642,7 @@ class AdamW:
             _check(self.lib.apollo_adamw_list_step(self._cfg_at, pointers, g_pointers, lengths, types, g_types, len(self.params),
                                                    self.state.data_ptr(), self.state.numel(), lr, wd, t, factor_at, lr_at, t_at,
                                                    self._run(stream)), "apollo_adamw_list_step")
+        self._changed(self.params, grads)
 
     def moments(self, stream=None):
         """(m, v) of all blocks in list order, ADAMW_BLOCK n_blocks values each: what 8-bit codes stand for, exactly, in bfloat16; of
@@ -777,6 +783,7 @@ def adjust_logits(logits, history=None, lengths=None, start=None, repetition=1.0
         to, out_stride = of, stride
     if bias_index is not None and bias_value is None:
         raise ValueError("bias_index needs bias_value")
+    given = out
     with _on_index(stream, of[_DEVICE]):
         rules, kept = _rules_of(of, history, lengths, start, repetition, frequency, presence, bias, bias_index, bias_value, mask)
         out_at = to[_AT]
@@ -785,6 +792,8 @@ def adjust_logits(logits, history=None, lengths=None, start=None, repetition=1.0
             out_at, out_stride = out.data_ptr(), vocab
         _check(load().apollo_adjust_logits(of[_AT], stride, n, vocab, of[_TYPE], ctypes.byref(rules), out_at, out_stride, _stream_ptr(stream)),
                "apollo_adjust_logits")
+    if given is not None:
+        _marshal().changed((given,), None)
     return out
 
 
@@ -836,6 +845,8 @@ def adjust_logits_grad(logits, d_out, history=None, lengths=None, repetition=1.0
             of[_AT], stride, n, vocab, of[_TYPE], ctypes.byref(rules), d[_AT], d_stride, out.data_ptr() if to is None else to[_AT], out_stride,
             None if d_bias is None else d_bias.data_ptr(), vocab if bias == "row" else 0, None if d_value is None else d_value.data_ptr(),
             workspace_at, workspace_bytes, _stream_ptr(stream)), "apollo_adjust_logits_grad")
+    if to is not None:
+        _marshal().changed((out,), None)
     return AdjustLogitsGrad(out, d_bias, d_value)
 
 

@@ -10,6 +10,9 @@
 
 namespace {
 
+// (the exact types first: asking whether an object is an instance costs 50 ns)
+bool is_tensor(PyObject* x) { return THPVariable_CheckTypeExact(Py_TYPE(x)) || THPVariable_Check(x); }
+
 int type_code(const at::Tensor& t)
 {
     switch (t.scalar_type()) {
@@ -27,7 +30,7 @@ long device_index(const at::Tensor& t) { return t.is_cuda() ? (long)t.get_device
 // (address, device index or -1, type code, dimensions, sizes and strides of the first two, contiguous)
 PyObject* describe(PyObject*, PyObject* arg)
 {
-    if (!THPVariable_Check(arg)) {
+    if (!is_tensor(arg)) {
         PyErr_SetString(PyExc_TypeError, "a tensor is wanted");
         return nullptr;
     }
@@ -57,8 +60,8 @@ PyObject* refuse(const char* what, const char* why)
 // Whether a tensor, or a tuple of whole numbers, has these sizes.
 bool same_shape(PyObject* other, at::IntArrayRef sizes)
 {
-    if (THPVariable_Check(other)) return THPVariable_Unpack(other).sizes().equals(sizes);
-    if (!PyTuple_Check(other) || (size_t)PyTuple_GET_SIZE(other) != sizes.size()) return false;
+    if (!PyTuple_Check(other)) return is_tensor(other) && THPVariable_Unpack(other).sizes().equals(sizes);
+    if ((size_t)PyTuple_GET_SIZE(other) != sizes.size()) return false;
     for (size_t i = 0; i < sizes.size(); ++i) {
         const long long n = PyLong_AsLongLong(PyTuple_GET_ITEM(other, (Py_ssize_t)i));
         if (n != (long long)sizes[i]) {
@@ -97,7 +100,7 @@ PyObject* pack(PyObject*, PyObject* args)
             for (Py_ssize_t i = 0; i < n; ++i) {
                 PyObject* item = PySequence_Fast_GET_ITEM(list, i);
                 if (item == Py_None) continue;
-                if (!THPVariable_Check(item)) return refuse(what, "must be tensors");
+                if (!is_tensor(item)) return refuse(what, "must be tensors");
                 const at::Tensor& t = THPVariable_Unpack(item);
                 if (!t.is_cuda() || t.layout() != at::kStrided || !t.is_contiguous()) return refuse(what, "must be contiguous CUDA tensors");
                 const int code = type_code(t);
@@ -124,9 +127,36 @@ PyObject* pack(PyObject*, PyObject* args)
     return result;
 }
 
+// changed(tensors, where): tells autograd that a call has written to them, so that a saved one is not used for a gradient; where: a list of as many
+// (tensors whose place in it is None were left alone), or None.  A None among the tensors is left out.
+PyObject* changed(PyObject*, PyObject* args)
+{
+    PyObject *tensors, *where;
+    if (!PyArg_ParseTuple(args, "OO", &tensors, &where)) return nullptr;
+    PyObject* list = PySequence_Fast(tensors, "a list of tensors is wanted");
+    if (!list) return nullptr;
+    PyObject* written = where == Py_None ? nullptr : PySequence_Fast(where, "a list is wanted");
+    if (where != Py_None && !written) {
+        Py_DECREF(list);
+        return nullptr;
+    }
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(list);
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        PyObject* item = PySequence_Fast_GET_ITEM(list, i);
+        if (!is_tensor(item)) continue;
+        if (written && (i >= PySequence_Fast_GET_SIZE(written) || PySequence_Fast_GET_ITEM(written, i) == Py_None)) continue;
+        const at::Tensor& t = THPVariable_Unpack(item);
+        if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+    }
+    Py_XDECREF(written);
+    Py_DECREF(list);
+    Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {
     { "describe", describe, METH_O, "(address, device index or -1, type code, dimensions, size 0, size 1, stride 0, stride 1, contiguous)" },
     { "pack", pack, METH_VARARGS, "(addresses, lengths, types, device, tensors that are not None)" },
+    { "changed", changed, METH_VARARGS, "autograd is told that the tensors (those whose place in the second list is not None) were written" },
     { nullptr, nullptr, 0, nullptr },
 };
 
