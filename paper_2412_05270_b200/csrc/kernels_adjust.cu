@@ -798,6 +798,14 @@ cudaError_t run_adjust_grad(WordsArgs a, StreamArgs s, int sms, int* groups, cud
     return table ? run_words<T, true>(a, streamed, sms, stream) : cudaSuccess;
 }
 
+// The status of a call's launches.  A launch that failed leaves its error with the runtime, where the next call would take it for its own.
+int launched(cudaError_t e)
+{
+    if (e == cudaSuccess) return APOLLO_OK;
+    cudaGetLastError();
+    return APOLLO_ERR_CUDA;
+}
+
 }  // namespace
 
 }  // namespace apollo
@@ -824,7 +832,7 @@ extern "C" int apollo_adjust_logits(const void* d_logits, int64_t row_stride, in
     a.logits = d_logits; a.out = d_out; a.stride = row_stride; a.out_stride = out_stride; a.n_rows = n_rows; a.vocab = (int)vocab;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const cudaError_t err = dtype == APOLLO_DT_BF16 ? run_adjust<__nv_bfloat16>(a, sms, stream) : run_adjust<float>(a, sms, stream);
-    return err == cudaSuccess ? APOLLO_OK : APOLLO_ERR_CUDA;
+    return launched(err);
 }
 
 extern "C" int apollo_adjust_logits_grad_workspace_bytes(int64_t n_rows, int64_t vocab, size_t* out_bytes)
@@ -885,5 +893,5 @@ extern "C" int apollo_adjust_logits_grad(const void* d_logits, int64_t row_strid
         else adjust_bias_join_kernel<<<grid, AJ_THREADS, 0, stream>>>(s.partial, groups, (int)vocab, static_cast<float*>(d_grad_bias));
         err = cudaGetLastError();
     }
-    return err == cudaSuccess ? APOLLO_OK : APOLLO_ERR_CUDA;
+    return launched(err);
 }
