@@ -60,14 +60,15 @@ struct Rules {
     long long mask_stride;
 };
 
+// A token, or -1 for one outside [0, vocab) (whatever it is: the caller subtracts the first word of a chunk from it).
 __device__ __forceinline__ int token_at(const void* p, long long i, int is64, int vocab)
 {
     if (is64) {
-        const long long v = static_cast<const long long*>(p)[i];
-        return v >= 0 && v < vocab ? (int)v : -1;
+        const unsigned long long v = static_cast<const unsigned long long*>(p)[i];
+        return v < (unsigned long long)vocab ? (int)v : -1;
     }
-    const int v = static_cast<const int*>(p)[i];
-    return v < vocab ? v : -1;
+    const unsigned v = static_cast<const unsigned*>(p)[i];
+    return v < (unsigned)vocab ? (int)v : -1;
 }
 
 // What a row's table is made of, and its penalties.
