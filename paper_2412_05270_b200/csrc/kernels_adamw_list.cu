@@ -213,7 +213,7 @@ struct ListArgs {
     double lr, wd, eps, inv_c1, root;    // root = sqrt(inv_c2)
     double log_b1, log_b2;               // for the step count on the device
     int bias_correction;
-    int fast;                            // eps is large enough for FAST roots
+    int fast;                            // 8 bits: eps is large enough for FLUSHED roots
     unsigned long long t;
     Scalars scalars;
     uint32_t keys[20];
@@ -278,21 +278,24 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-// On the special-function unit, relative errors about 2^-23.  FAST flushes what is below the normal range: a root that is off by
-// 1.1e-19 at most, beside an eps of 1e-12 or more nothing; a smaller eps takes the other form (three instructions more each).
-template <bool FAST>
+// Roots and quotients are rounded correctly where that is free (moments of 32 bits: 262 M in 844 us, 843 without).  The step of 8 bits is bound by
+// instruction issue (262 M bfloat16: 614 us instead of 472) and takes them from the special-function unit, relative errors about 2^-23, beside
+// codes of three bits.  FLUSHED drops what is below the normal range: a root that is off by 1.1e-19 at most, beside an eps of 1e-12 or more nothing;
+// a smaller eps takes APPROXIMATE (three instructions more each).
+enum : int { APPROXIMATE, FLUSHED, EXACT };
+template <int HOW>
 __device__ __forceinline__ float root_of(float x)
 {
     float y;
-    if constexpr (FAST) asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    if constexpr (HOW == FLUSHED) asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     else asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-template <bool FAST>
+template <int HOW>
 __device__ __forceinline__ float inverse_of(float x)
 {
     float y;
-    if constexpr (FAST) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    if constexpr (HOW == FLUSHED) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     else asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
@@ -306,7 +309,7 @@ struct Update {
     __device__ __forceinline__ Update(const ListArgs<CAP>& a, const Scalars& s)
         : factor(pair2(s.factor, s.factor)), a1(pair2(a.a1, a.a1)), b2(pair2(a.b2, a.b2)), a2(pair2(a.a2, a.a2)),
           eps(pair2(s.eps, s.eps)), rate(pair2(-s.rate, -s.rate)), decay(pair2(s.decay, s.decay)) {}
-    template <bool FAST>
+    template <int HOW>
     __device__ __forceinline__ void apply(const float (&g)[8], float scale, float (&m)[8], float (&v)[8], float (&p)[8]) const
     {
         const uint64_t b1 = pair2(scale, scale);
@@ -324,9 +327,16 @@ struct Update {
             v[x + 1] = __fadd_rn(s1, t1);
             const uint64_t mm = pair2(m[x], m[x + 1]);
             float d0, d1;
-            unpack2(add2(pair2(root_of<FAST>(v[x]), root_of<FAST>(v[x + 1])), eps), d0, d1);
             const uint64_t pp = pair2(p[x], p[x + 1]);
-            unpack2(fma2(rate, fma2(decay, pp, mul2(mm, pair2(inverse_of<FAST>(d0), inverse_of<FAST>(d1)))), pp), p[x], p[x + 1]);
+            uint64_t quotient;
+            if constexpr (HOW == EXACT) {
+                unpack2(add2(pair2(__fsqrt_rn(v[x]), __fsqrt_rn(v[x + 1])), eps), d0, d1);
+                quotient = pair2(__fdiv_rn(m[x], d0), __fdiv_rn(m[x + 1], d1));
+            } else {
+                unpack2(add2(pair2(root_of<HOW>(v[x]), root_of<HOW>(v[x + 1])), eps), d0, d1);
+                quotient = mul2(mm, pair2(inverse_of<HOW>(d0), inverse_of<HOW>(d1)));
+            }
+            unpack2(fma2(rate, fma2(decay, pp, quotient), pp), p[x], p[x + 1]);
         }
     }
 };
@@ -539,8 +549,8 @@ adamw8_kernel(const __grid_constant__ ListArgs<CAP> a)
         unpack_raw8(rp, p);
         unpack_raw8(rg, g);
         decode8(cm, cv, k, table, scale, m, v);
-        if (a.fast) update.template apply<true>(g, scale * a.b1, m, v, p);
-        else update.template apply<false>(g, scale * a.b1, m, v, p);
+        if (a.fast) update.template apply<FLUSHED>(g, scale * a.b1, m, v, p);
+        else update.template apply<APPROXIMATE>(g, scale * a.b1, m, v, p);
         encode8(m, v, philox4x32_10_keys((uint32_t)block, (uint32_t)lane, s.t_lo, s.t_hi, a.keys), cm, cv, k);
     };
     if ((int)blockIdx.x >= a.whole_grid) {             // the end of a tensor, behind its last whole tile
@@ -637,8 +647,8 @@ adamw8_kernel(const __grid_constant__ ListArgs<CAP> a)
 }
 
 // Moments of 32 bits: nothing but the traffic.  A block of threads has one tile, so that fast and slow multiprocessors share the work as
-// they can (blocks that stay and loop: 906 us instead of 842).  262 M parameters: bfloat16 842 us, 6.8 TB/s; fp32 weights with bfloat16
-// gradients 1000, all fp32 1069 (at the copy rate 882, 1042, 1122).
+// they can (blocks that stay and loop: 906 us instead of 842).  262 M parameters: bfloat16 844 us, 6.8 TB/s; fp32 weights with bfloat16
+// gradients 1000, all fp32 1069 (at the copy rate 882, 1042, 1122); with lr and the step count on the device the same.
 template <typename PT, typename GT, int CAP>
 __global__ void __launch_bounds__(AL_THREADS, 4)
 adamw32_kernel(const __grid_constant__ ListArgs<CAP> a)
@@ -663,8 +673,7 @@ adamw32_kernel(const __grid_constant__ ListArgs<CAP> a)
         float g[8], p[8], m[8], v[8];
         if (count == 8) { load8_stream(P + e, p); load8_stream(G + e, g); load8_stream(M + e, m); load8_stream(V + e, v); }
         else { load8_guarded(P + e, count, p); load8_guarded(G + e, count, g); load8_guarded(M + e, count, m); load8_guarded(V + e, count, v); }
-        if (a.fast) update.template apply<true>(g, a.b1, m, v, p);
-        else update.template apply<false>(g, a.b1, m, v, p);
+        update.template apply<EXACT>(g, a.b1, m, v, p);
         if (count == 8) { store8(P + e, p); store8(M + e, m); store8(V + e, v); }
         else {
 #pragma unroll
