@@ -489,7 +489,9 @@ APOLLO_API int apollo_grad_norm(const void* const* d_G, const int64_t* numel, co
  *             (k + c / 8 = 0: (c % 8) / 8 2^-126.)
  * All bytes zero is the state before the first step.  Codes are rounded stochastically: a value between two neighbours becomes
  * the upper one with the probability of its place between them, in steps of 2^-16 (v moves by a thousandth of itself a step,
- * the codes are 6 to 12 % apart: rounded to nearest it would never move).  The 16 random bits of element e of a block are
+ * the codes are 6 to 12 % apart: rounded to nearest it would never move).  For this the m of code 0 counts as 2^(k - 127), the
+ * power of two below code 1, once k > 0: a smaller m (less than about 2^-15 of its block's largest) always becomes zero, a
+ * smaller v always code 0.  The 16 random bits of element e of a block are
  * halfword e % 8 of Philox4x32-10 with key `seed` and counter (block, (e % 256) / 8, t, t >> 32), the same for m and v: equal
  * inputs, seed and t give equal bits, on any stream and in any run.  The padding behind a tensor's last element holds zeros
  * (32 bits) or what elements of zero become.  An infinite or NaN gradient makes m and v of its element so, and spoils the

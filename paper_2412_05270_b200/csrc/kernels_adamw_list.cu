@@ -14,8 +14,10 @@
 //      below it is not divided by eps.
 // Why stochastic: v moves by (1-b2) = 1/1000 of itself a step and the codes are 6 to 12 % apart; rounded to nearest it would
 // never move (m likewise once g is within 60 % of it).  16 random bits per element: a probability of 1/100 then is right to
-// 0.2 %.  One Philox4x32-10 call a lane gives the 128 bits that its eight elements need; m and v share them (each is unbiased,
-// and errors of the same sign cancel in m / sqrt(v)).
+// 0.2 %.  One Philox4x32-10 call a lane gives the 128 bits that its eight elements need; m and v share them (errors of the same sign
+// cancel in m / sqrt(v)).  Rounding is unbiased from code 1 on.  Below it an m is rounded as if code 0 were the power of two under code 1, but held
+// as zero, and an m below that power (about 2^-15 of its block's largest) is zero every time (it has its part in the update before);
+// a v below code 0 is raised to it.
 #include "../../include/apollo.h"
 
 #include <cmath>
