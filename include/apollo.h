@@ -464,7 +464,8 @@ APOLLO_API int apollo_token_logprobs_grad(const void* d_logits, int64_t row_stri
 
 /*
  * Global norm of a list of gradients and the factor that clips it (stateless, asynchronous on `cuda_stream`):
- *   norm = sqrt(sum_i sum_e G_i[e]^2),   factor = min(1, max_norm / norm)   (1 for norm = 0; NaN where the norm is not finite).
+ *   norm = sqrt(sum_i sum_e G_i[e]^2),   factor = min(1, max_norm / norm)   (1 for norm = 0; NaN where the norm is not finite;
+ * a norm beyond fp32 reads as infinity, its factor is right).
  * d_G: HOST array of n_tensors DEVICE pointers (16-byte aligned, contiguous; a null entry is left out); numel, dtype: HOST,
  * per tensor.  max_norm > 0 (may be infinite: the norm alone).  d_out: DEVICE, two floats {norm, factor}.  Squares and sums are
  * in fp64, norm and factor rounded once.  The order of the sum is fixed by the list and the number of

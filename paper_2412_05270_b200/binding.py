@@ -19,7 +19,7 @@ from .build import marshal_path
 
 _PKG = Path(__file__).resolve().parent
 LIB_PATH = _PKG / "libapollo.so"
-DEBUG_LIB_PATH = _PKG / "libapollo_debug.so"     # built with -DAPOLLO_DEBUG: index checks inside every kernel
+DEBUG_LIB_PATH = _PKG / "libapollo_debug.so"     # built with -DAPOLLO_DEBUG: index checks inside the kernels of contexts
 
 OK = 0
 ERR_INVALID_ARG, ERR_SHAPE, ERR_RANK, ERR_ALIGN, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, ERR_UNSUPPORTED = (

@@ -9,7 +9,7 @@ from pathlib import Path
 PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libapollo.so"
-LIB_DEBUG = PKG / "libapollo_debug.so"      # the same sources with -DAPOLLO_DEBUG: index checks inside the kernels
+LIB_DEBUG = PKG / "libapollo_debug.so"      # the same sources with -DAPOLLO_DEBUG: index checks inside the kernels of contexts
 SOURCES = ["apollo_api.cu", "kernels_basic.cu", "kernels_tensor.cu", "apollo_static.cu", "kernels_adamw.cu",
            "apollo_muon.cu", "kernels_muon.cu", "kernels_embedding.cu", "kernels_logprob.cu", "kernels_adamw_list.cu",
            "kernels_adjust.cu"]
@@ -60,8 +60,9 @@ def build_marshal(force: bool = False) -> Path:
 
 def build_library(force: bool = False, verbose: bool = False, debug: bool = False) -> Path:
     """Compiles the library in-tree, with nvcc alone, and then, where torch is installed, the binding's extension.  debug=True builds
-    libapollo_debug.so: every kernel checks the index range of its global loads and stores and reports a violation through the
-    context's status word (apollo_status returns APOLLO_ERR_INTERNAL) instead of making the access."""
+    libapollo_debug.so: the kernels of contexts (apollo_create, apollo_muon_create) check the index range of their global loads and stores and
+    report a violation through the status word (apollo_status returns APOLLO_ERR_INTERNAL) instead of making the access; the stateless
+    entry points have no status word, and their kernels no checks."""
     lib = _compile(force, verbose, debug)
     if importlib.util.find_spec("torch") is not None:
         build_marshal(force)

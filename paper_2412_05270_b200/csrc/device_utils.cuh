@@ -9,7 +9,7 @@
 
 namespace apollo {
 
-// Debug build (-DAPOLLO_DEBUG): every kernel checks the index range of its global loads and stores against
+// Debug build (-DAPOLLO_DEBUG): the kernels that have a status word check the index range of their global loads and stores against
 // the extent of the array before the access; a range that is not inside sets the status word to STATUS_BOUNDS
 // and the access is skipped (the kernel goes on and ends normally).  In the release build the macro is `true`.
 #ifdef APOLLO_DEBUG

@@ -529,7 +529,9 @@ struct Stage {
 //   * whole tiles and the tensors' ends are different blocks of threads: with both in one loop it took 5 instructions an element more;
 //   * up to AL_WAVES times as many blocks as are resident: with one wave the slowest multiprocessor sets the time (529 us for 504);
 //   * loads through registers instead: 613 us (too few bytes under way beside what the arithmetic holds).
-// 262 M parameters: bfloat16 472 us, 5.6 TB/s; fp32 weights with bfloat16 gradients 551, all fp32 638 (at the copy rate 401, 561, 641).
+// 262 M parameters: bfloat16 472 us, 5.6 TB/s; fp32 weights with bfloat16 gradients 550, all fp32 622 (at the copy rate 401, 561, 641), in twenty
+// calls at 1965 MHz.  Bound by issue it goes with the clock: after seconds of it the board is at 1000 W and 1760 MHz, bfloat16 559 us.  With lr and the
+// step count on the device bfloat16 takes 482 (every block works the scalars out), the others the same.
 template <typename PT, typename GT, int CAP>
 __global__ void __launch_bounds__(AL_THREADS, (Stage<PT, GT>::RESIDENT))
 adamw8_kernel(const __grid_constant__ ListArgs<CAP> a)

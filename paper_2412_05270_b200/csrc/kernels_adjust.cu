@@ -489,7 +489,7 @@ struct WordsArgs {
 
 // Blocks a multiprocessor that the registers are to allow: it decides how the compiler orders the scattered loads.  Short histories, forward:
 // 12 (8192 x 32000 bfloat16 257 us, 4096 x 50256 in place 57.5; 6 255 and 65.7; 9 260 and 59.5); gradient: bfloat16 6 (8192 x 32000 304 us,
-// 9 330), fp32 9 (777 x 50001 88 us, 6 90).  Others 4: what shared memory holds (in place with a bias, 4096 x 50256 bfloat16: 280 us, 5 344).
+// 9 330), fp32 9 (777 x 50001 88 us, 6 90; why the types differ is not known, the bounds are what these shapes took).  Others 4: what shared memory holds (in place with a bias, 4096 x 50256 bfloat16: 280 us, 5 344).
 constexpr int words_resident(bool half, bool grad, size_t e) { return !half ? 4 : !grad ? 12 : e == 2 ? 6 : 9; }
 
 // ALL: mode AJ_ALL_TOO.
