@@ -1,4 +1,5 @@
-"""What a build needs and when it is done again (no GPU needed; the compilers are stand-ins that write down how they were called)."""
+"""What a build needs and when it is done again (no GPU needed; the compilers are stand-ins that write down how they were called, and so is torch, of
+which a build asks little)."""
 import os
 import shutil
 import subprocess
@@ -15,9 +16,18 @@ while [ $# -gt 0 ]; do if [ "$1" = -o ]; then echo built > "$2"; fi; shift; done
 """
 
 
+def torch_of(tree, version):
+    """Another torch for the interpreters that run() starts."""
+    (tree / "torch" / "utils").mkdir(parents=True, exist_ok=True)
+    (tree / "torch" / "__init__.py").write_text(f"__version__ = '{version}'\nclass _C: _GLIBCXX_USE_CXX11_ABI = True\n")
+    (tree / "torch" / "utils" / "__init__.py").write_text("")
+    (tree / "torch" / "utils" / "cpp_extension.py").write_text("include_paths = library_paths = lambda: ['/nowhere']\n")
+
+
 @pytest.fixture
 def tree(tmp_path):
-    """A copy of the package's sources and of the C header, and stand-ins for nvcc and g++."""
+    """A copy of the package's sources and of the C header, and stand-ins for nvcc, g++ and torch."""
+    torch_of(tmp_path, "1.0")
     shutil.copytree(ROOT / "paper_2412_05270_b200", tmp_path / "paper_2412_05270_b200", ignore=shutil.ignore_patterns("*.so", "_build", "__pycache__"))
     shutil.copytree(ROOT / "include", tmp_path / "include")
     for name in ("nvcc", "g++"):
@@ -36,7 +46,6 @@ def run(tree, code):
 
 
 BUILD = "from paper_2412_05270_b200.build import *\n"
-ONLY_EXTENSION = "import paper_2412_05270_b200.build as b\n"
 
 
 def test_the_library_is_built_without_torch(tree):
@@ -53,12 +62,11 @@ def test_the_extension_is_built_again_for_another_torch_and_when_forced(tree):
     log = run(tree, BUILD + "build_library(force=True)")
     assert sum(line.startswith("g++") for line in log) == 1 and sum(line.startswith("nvcc") for line in log) > 1
     # after an upgrade the old one is younger than every source
-    log = run(tree, "import torch; torch.__version__ = '99.0'\n" + BUILD + "build_library()")
+    torch_of(tree, "99.0")
+    log = run(tree, BUILD + "build_library()")
     assert [line.split()[0] for line in log] == ["g++"]
-    os.utime(package / "csrc" / "marshal.cpp")
     os.utime(package / "csrc" / "marshal.cpp", (2 ** 31 - 1, 2 ** 31 - 1))
-    log = run(tree, "import torch; torch.__version__ = '99.0'\n" + ONLY_EXTENSION + "b.build_marshal()")
-    assert [line.split()[0] for line in log] == ["g++"]
+    assert [line.split()[0] for line in run(tree, BUILD + "build_marshal()")] == ["g++"]
 
 
 def test_an_extension_for_another_torch_is_not_loaded(monkeypatch):
